@@ -161,7 +161,7 @@ def run(state):
             if s["top"]:
                 out["top_logp"], out["top_ids"] = r.top_logp, r.top_ids
             if s["train"]:
-                out["dlogits"] = lib.token_logprobs_backward(s["dlogp"], s["dentropy"], s["logits"], s["targets"], r.lse, r.entropy)
+                out["dlogits"] = lib.token_logprobs_backward(s["dlogp"], s["dentropy"], s["logits"], s["targets"], r.stats, r.entropy)
             return out
         if s["op"] == "embedding":
             out = {"out": lib.embedding_forward(s["table"], s["ids"], s["scale"])}
