@@ -388,6 +388,79 @@ olsgd_status olsgd_class_pairs(uint64_t seed, int32_t m, int32_t* dst, void* str
 #define OLSGD_NOALLOC_MAX_WORKERS 16384
 olsgd_status olsgd_class_pairs_noalloc(uint64_t seed, int32_t m, int32_t* dst, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators on caller-owned tensors: what a caller that computes its own gradients
+ * (OLSGD_FLAT) needs to train worker-stacked language models next to this library's own
+ * models.  (The paper has no counterpart; its method takes any gradient.)
+ *
+ * They need no context.  Every call takes its stream, launches asynchronously on it and on
+ * the CURRENT device, where all its tensors must live; it allocates nothing, keeps nothing
+ * between calls, and may be captured into a CUDA graph.  Where a call takes a workspace, its
+ * contents before and after the call mean nothing; two calls that may run at the same time
+ * (other streams, other graphs) need workspaces of their own.  Pointers are device memory,
+ * aligned to their element (workspaces to 256 bytes); strides are in elements and need not be
+ * multiples of 16 bytes.  Outputs must not overlap inputs unless stated, nor other outputs.
+ * Errors are reported as everywhere: a status, and olsgd_last_error(NULL).  Sizes of zero
+ * rows, tokens or tensors are no error; such a call returns without touching its outputs.   */
+typedef enum { OLSGD_F32 = 0, OLSGD_BF16 = 1, OLSGD_F16 = 2 } olsgd_dtype;
+
+/* Log probabilities of given tokens, with entropy and the most likely alternatives.
+ * For each row x of V logits, p = softmax(x):
+ *   logp[r]      log p[targets[r]]; 0 where the target lies outside [0, V) (no token)
+ *   entropy[r]   -sum_j p_j log p_j
+ *   stats        float [rows][2]: max x, and the logarithm of sum exp(x - max x); their sum is
+ *                the row's logarithm of the partition function.  The gradient takes them.
+ *   top_logp, top_ids   [rows][top]: the `top` most likely tokens in order of falling
+ *                probability, ties to the lowest index; top <= min(V, OLSGD_MAX_TOP), 0: none
+ *                (the pointers may then be NULL)
+ * Logits of -inf are tokens that are masked out.  A row of nothing but -inf has no
+ * distribution: logp of a token and top_logp are -inf, the entropy is 0, the gradient is 0.
+ * A row with a NaN or +inf has logp (of a token), entropy and gradients of NaN; its
+ * alternatives are ordered with NaN first.
+ *   logits   [rows][V], rows row_stride >= V elements apart; V in [1, 2^27]
+ *   targets  int32 [rows]                                                               */
+#define OLSGD_MAX_TOP 32
+olsgd_status olsgd_token_logprobs_workspace(int32_t dtype, int64_t rows, int64_t V, int32_t top,
+                                            size_t* out_bytes);
+olsgd_status olsgd_token_logprobs(const void* logits, int32_t dtype, int64_t rows, int64_t V,
+                                  int64_t row_stride, const int32_t* targets, int32_t top,
+                                  float* logp, float* entropy, float* stats, float* top_logp,
+                                  int32_t* top_ids, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+/* Its gradient: d_logits[r][j] = d_logp[r] (1[j = targets[r]] - p_j)
+ *                                - d_entropy[r] p_j (log p_j + entropy[r]).
+ *   d_logp, d_entropy   float [rows]; NULL: zeros.  d_logp of a row without a token is not used.
+ *   stats, entropy      as olsgd_token_logprobs left them for the same logits
+ *   d_logits            [rows][V] of the logits' type, rows d_row_stride >= V apart; it may be
+ *                       the logits themselves (same pointer and stride)                   */
+olsgd_status olsgd_token_logprobs_backward(const float* d_logp, const float* d_entropy,
+                                           const void* logits, int32_t dtype, int64_t rows,
+                                           int64_t V, int64_t row_stride, const int32_t* targets,
+                                           const float* stats, const float* entropy,
+                                           void* d_logits, int64_t d_row_stride, void* stream);
+
+/* Per-worker gradient norm over many tensors, and clipping.  For each worker i,
+ *   n_i = sqrt(sum over all tensors of the worker's squares),
+ *   out = in * min(1, max_norm / (n_i + 1e-6)), rounded once to the output's type.
+ * A norm of NaN makes that worker's gradients NaN; an infinite one makes them 0 (and NaN where
+ * they are infinite).  Other workers are not affected.
+ *   tensors    n_tensors descriptors in host memory, read before the call returns; tensor t
+ *              holds, for worker i, n contiguous elements at in + i * in_stride; the result
+ *              goes to out + i * out_stride, of its own type.  out may be in (same pointer,
+ *              type and stride).  Widening to fp32 rows of a flat gradient [m][P] is an
+ *              out_stride of P.
+ *   norms      float [m]                                                                */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t n, in_stride, out_stride;
+  int32_t in_dtype, out_dtype; /* olsgd_dtype */
+} olsgd_clip_tensor;
+olsgd_status olsgd_clip_grads_workspace(int32_t m, int32_t n_tensors, size_t* out_bytes);
+olsgd_status olsgd_clip_grads(const olsgd_clip_tensor* tensors, int32_t n_tensors, int32_t m,
+                              float max_norm, float* norms, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
 /* Iteration counter k.                                                      */
 int64_t olsgd_iteration(const olsgd_ctx* ctx);
 

@@ -1,0 +1,192 @@
+"""Operators on caller-owned tensors (the section of that name in include/olsgd.h): argument
+checks and marshalling only, like `binding`.
+
+They serve a caller that computes its own gradients for `OverlapLocalSGD("flat", ...)`: tensors
+carry the worker dimension first.  Every call runs on the current stream of its tensors'
+device, allocates its outputs and workspace with torch (so it may be captured into a CUDA
+graph), and returns without waiting.  Tensors that live on another stream are the caller's to
+order, as with any torch operation.  Forward and backward are separate calls; nothing is kept
+between them but what the caller passes on.
+"""
+import ctypes as C
+import functools
+from collections import namedtuple
+
+import torch
+
+from .binding import _check, load_library
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MAX_TOP = 32
+
+TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy stats top_logp top_ids")
+
+_vp, _i32, _i64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+_SIGNATURES = {
+    "olsgd_token_logprobs_workspace": [_i32, _i64, _i64, _i32, C.POINTER(_sz)],
+    "olsgd_token_logprobs": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "olsgd_token_logprobs_backward": [_vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp],
+    "olsgd_clip_grads_workspace": [_i32, _i32, C.POINTER(_sz)],
+    "olsgd_clip_grads": [_vp, _i32, _i32, C.c_float, _vp, _vp, _sz, _vp],
+}
+_OPS = None
+
+
+def _ops():
+    global _OPS
+    if _OPS is None:
+        lib = load_library()
+        for name, args in _SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = _i32, args
+        _OPS = lib
+    return _OPS
+
+
+def _need(ok, text, *args):
+    if not ok:
+        raise ValueError(text % args if args else text)
+
+
+def _dtype(t, name):
+    code = DTYPES.get(t.dtype)
+    _need(code is not None, "%s must be float32, bfloat16 or float16", name)
+    return code
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        _need(t is None or t.device == dev, "%s must be on %s", name, dev)
+
+
+def _run(fn, dev, *args):
+    """fn(*args, stream) on the tensors' device and its current stream."""
+    if torch.cuda.current_device() == dev.index:
+        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if st:
+        _check(_ops(), st)
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(query, *sizes):
+    n = _sz()
+    _check(_ops(), getattr(_ops(), query)(*sizes, C.byref(n)))
+    return n.value
+
+
+def _workspace(dev, query, *sizes):
+    """(tensor, pointer, bytes) of a fresh workspace; torch's allocations are 512-byte aligned."""
+    n = _workspace_bytes(query, *sizes)
+    if n == 0:
+        return None, None, 0
+    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    return ws, ws.data_ptr(), n
+
+
+# ------------------------------------------------------------------ token log probabilities
+
+def _rows_of(t, name):
+    """(view [N][V], stride between rows) of a tensor [..., V] whose rows are evenly spaced."""
+    _need(t.dim() >= 1 and t.is_cuda, "%s must be a CUDA tensor with at least one dimension", name)
+    V = t.shape[-1]
+    _need(V >= 1 and (t.stride(-1) == 1 or V == 1), "%s: the last dimension must be contiguous and not empty", name)
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, V)
+        except RuntimeError:
+            raise ValueError("%s: rows must be evenly spaced" % name) from None
+    return t, (t.stride(0) if t.shape[0] > 1 else V)
+
+
+def _per_row(t, shape, dtype, name):
+    _need(t.dtype == dtype and t.shape == shape and t.is_contiguous(), "%s must be contiguous %s of shape %s", name, dtype,
+          tuple(shape))
+    return t.data_ptr()
+
+
+def token_logprobs(logits, targets, top=0):
+    """olsgd_token_logprobs.  logits [..., V] (rows evenly spaced), targets int32 [...]; a target outside
+    [0, V) is a row without a token.  Returns TokenLogprobs(logp, entropy, stats, top_logp, top_ids): float32
+    [...], [...], [..., 2], [..., top] and int32 [..., top] (the last two None when top == 0)."""
+    lib = _ops()
+    rows, ld = _rows_of(logits, "logits")
+    code, dev, lead = _dtype(logits, "logits"), logits.device, logits.shape[:-1]
+    _same_device(dev, targets=targets)
+    tp = _per_row(targets, lead, torch.int32, "targets")
+    N, V = rows.shape
+    top = int(top)
+    _need(0 <= top <= min(V, MAX_TOP), "top must be in [0, min(V, %d)]", MAX_TOP)
+    logp = torch.empty(lead, dtype=torch.float32, device=dev)
+    entropy = torch.empty(lead, dtype=torch.float32, device=dev)
+    stats = torch.empty(lead + (2,), dtype=torch.float32, device=dev)
+    top_logp = top_ids = None
+    if top:
+        top_logp = torch.empty(lead + (top,), dtype=torch.float32, device=dev)
+        top_ids = torch.empty(lead + (top,), dtype=torch.int32, device=dev)
+    ws, wp, wn = _workspace(dev, "olsgd_token_logprobs_workspace", code, N, V, top)
+    _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, top, logp.data_ptr(), entropy.data_ptr(),
+         stats.data_ptr(), top_logp.data_ptr() if top else None, top_ids.data_ptr() if top else None, wp, wn)
+    return TokenLogprobs(logp, entropy, stats, top_logp, top_ids)
+
+
+def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
+    """olsgd_token_logprobs_backward: the gradient of the logits, contiguous, of their type.  d_logp and d_entropy
+    are float32 [...] or None (zeros); stats and entropy are token_logprobs' for the same logits."""
+    lib = _ops()
+    rows, ld = _rows_of(logits, "logits")
+    code, dev, lead = _dtype(logits, "logits"), logits.device, logits.shape[:-1]
+    _same_device(dev, targets=targets, stats=stats, entropy=entropy, d_logp=d_logp, d_entropy=d_entropy)
+    N, V = rows.shape
+    d = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    _run(lib.olsgd_token_logprobs_backward, dev,
+         None if d_logp is None else _per_row(d_logp, lead, torch.float32, "d_logp"),
+         None if d_entropy is None else _per_row(d_entropy, lead, torch.float32, "d_entropy"),
+         rows.data_ptr(), code, N, V, ld, _per_row(targets, lead, torch.int32, "targets"),
+         _per_row(stats, lead + (2,), torch.float32, "stats"), _per_row(entropy, lead, torch.float32, "entropy"),
+         d.data_ptr(), V)
+    return d
+
+
+# ------------------------------------------------------------------------ gradient clipping
+
+def _worker_rows(t, m, name):
+    """Elements between workers of a tensor [m, ...] whose workers' parts are contiguous."""
+    _need(t.dim() >= 1 and t.shape[0] == m, "%s must have %s workers", name, m)
+    n = t.numel() // m
+    if t.is_contiguous():
+        return n, n
+    _need(t[0].is_contiguous(), "%s: each worker's part must be contiguous", name)
+    return n, t.stride(0)
+
+
+def clip_grads(grads, max_norm, out=None):
+    """olsgd_clip_grads.  grads: a tensor or a list of tensors [m, ...], each worker's part contiguous.  Each worker's
+    gradients, over all tensors, are scaled by min(1, max_norm / (norm + 1e-6)).  out: tensors of the same shapes, of any
+    of the three types, that take the result (the gradients themselves: in place; views of a flat float32 gradient [m][P]:
+    widened into it); None: new tensors like the gradients.  Returns (out, norms), norms float32 [m]."""
+    lib = _ops()
+    single = isinstance(grads, torch.Tensor)
+    if single:
+        grads, out = [grads], None if out is None else [out]
+    _need(len(grads) > 0, "grads is empty")
+    if out is None:
+        out = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads]
+    _need(len(out) == len(grads), "out must hold one tensor for each gradient")
+    m, dev = grads[0].shape[0] if grads[0].dim() else 0, grads[0].device
+    _need(dev.type == "cuda" and m >= 1, "grads must be CUDA tensors with the workers first")
+    flat = []
+    for g, o in zip(grads, out):
+        gc, oc = DTYPES.get(g.dtype), DTYPES.get(o.dtype)
+        _need(gc is not None and oc is not None, "gradients and out must be float32, bfloat16 or float16")
+        _need(g.shape == o.shape and g.device == dev and o.device == dev, "gradients and out must match in shape and device")
+        n, gs = _worker_rows(g, m, "a gradient")
+        _, os_ = _worker_rows(o, m, "out")
+        flat += (g.data_ptr(), o.data_ptr(), n, gs, os_, gc | (oc << 32))
+    table = (_i64 * len(flat))(*flat)
+    norms = torch.empty(m, dtype=torch.float32, device=dev)
+    ws, wp, wn = _workspace(dev, "olsgd_clip_grads_workspace", m, len(grads))
+    _run(lib.olsgd_clip_grads, dev, table, len(grads), m, float(max_norm), norms.data_ptr(), wp, wn)
+    return (out[0] if single else out), norms

@@ -1,0 +1,316 @@
+"""The operators on caller-owned tensors against their definitions in 64 bits.
+
+Tolerances count roundings.  u = 2^-24 is half a step of fp32; a sum of n positive terms in fp32, added up in a chain
+of length c, is off by at most about c u relative; a result rounded to type t by finfo(t).eps / 2 relative."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2002_09539_b200 as lib
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, shape, dtype=torch.float32, std=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(dtype)
+
+
+# ------------------------------------------------------------------- token log probabilities
+
+def _logprobs_64(x, t):
+    """Definition in 64 bits: log p of every token, entropy, log p of the targets."""
+    x = x.double()
+    empty = torch.isneginf(x).all(dim=-1)
+    # relative to the maximum: at the type's lowest value even 64 bits lose log V beside it
+    d = x - x.max(dim=-1, keepdim=True).values
+    lp = d - torch.logsumexp(d, dim=-1, keepdim=True)
+    lp = torch.where(empty[..., None], torch.full_like(lp, -math.inf), lp)
+    p = torch.exp(lp)
+    h = -torch.xlogy(p, p).sum(dim=-1)
+    has = (t >= 0) & (t < x.shape[-1])
+    at = torch.where(has, t, torch.zeros_like(t)).long()
+    picked = torch.where(has, lp.gather(-1, at[..., None])[..., 0], torch.zeros_like(h))
+    return lp, h, picked, has, empty
+
+
+def _sum_error(V, spread):
+    """Relative error of sum exp(x - max) and of its terms: a chain of at most V / 32 + 64 additions in a lane, the
+    joins, and terms e^d whose exponent |d| <= spread is rounded three times (difference, constant, product) and whose
+    power of two has 2 steps."""
+    return (V / 32 + 64 + 3 * spread + 4) * U
+
+
+def _check_logprobs(x, t, top, r):
+    lp, h, picked, has, empty = _logprobs_64(x, t)
+    V = x.shape[-1]
+    finite = torch.where(torch.isneginf(lp), torch.zeros_like(lp), lp)
+    spread = float(min(150.0, (-finite).max() + 1.0))
+    rel = _sum_error(V, spread)
+    err = (r.logp.double() - picked).abs()
+    ok = (r.logp.double() == picked) | (err <= rel + 4 * U * picked.abs())
+    assert bool(ok.all()), float(err[torch.isfinite(err)].max())
+    mean_d = (torch.exp(lp) * (finite - finite.max(dim=-1, keepdim=True).values).abs()).sum(dim=-1)
+    err = (r.entropy.double() - h).abs()
+    assert bool((err <= rel * (1 + 2 * mean_d) + 4 * U * (h + mean_d + math.log(V))).all()), float(err.max())
+    if top:
+        v, i = torch.sort(x.double(), dim=-1, descending=True, stable=True)
+        assert torch.equal(r.top_ids.long(), i[..., :top])
+        want = lp.gather(-1, i[..., :top])
+        got = r.top_logp.double()
+        err = (got - want).abs()
+        assert bool(((got == want) | (err <= rel + 4 * U * want.abs())).all())
+    return lp, h, has, empty, rel
+
+
+def _check_logprobs_grad(x, t, r, dlp, dh):
+    lp, h, has, empty, rel = _check_logprobs(x, t, 0, r)
+    d = lib.token_logprobs_backward(dlp, dh, x, t, r.stats, r.entropy)
+    p = torch.exp(lp)
+    a = torch.zeros_like(h) if dlp is None else torch.where(has, dlp.double(), torch.zeros_like(h))
+    b = torch.zeros_like(h) if dh is None else dh.double()
+    one = torch.zeros_like(p).scatter_(-1, torch.where(has, t, torch.zeros_like(t)).long()[..., None], 1.0)
+    want = a[..., None] * (one - p) - b[..., None] * (torch.xlogy(p, p) + p * h[..., None])
+    want = torch.where(empty[..., None], torch.zeros_like(want), want)
+    # p is off by `rel` and by the rounding of its own exponent; H by what its own test allows
+    lpz = torch.where(p > 0, lp.abs(), torch.zeros_like(p))
+    scale = p * (a.abs()[..., None] + b.abs()[..., None] * (lpz + h[..., None] + 1))
+    ep = rel + 8 * U * (lpz + 2)
+    tol = scale * (4 * ep) + a.abs()[..., None] * one * 2 * U + want.abs() * (torch.finfo(x.dtype).eps / 2 + 4 * U)
+    tol = tol + (2.0 ** -25 if x.dtype == torch.float16 else 2.0 ** -126) * 1.01   # below the type's least steps
+    err = (d.double() - want).abs()
+    assert bool((err <= tol).all()), float((err - tol).max())
+    return d
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,top", [(1, 1, 1), (5, 2, 2), (3, 10, 1), (33, 31, 31), (7, 32, 32), (2, 33, 32), (9, 257, 5), (4, 1000, 20),
+                                     (6, 1024, 32), (5, 1025, 7), (3, 1031, 32), (300, 4099, 3), (1, 8191, 20), (2, 50021, 32), (1, 131072, 20),
+                                     (700, 2049, 0), (1, 200003, 1)])
+def test_token_logprobs(dtype, N, V, top):
+    g = _gen(N * 1000 + V)
+    x = _randn(g, (N, V), dtype, 3.0)
+    t = torch.randint(-1, V + 1, (N,), generator=g, device="cuda", dtype=torch.int32)   # -1 and V: no token
+    r = lib.token_logprobs(x, t, top)
+    _check_logprobs(x, t, top, r)
+    _check_logprobs_grad(x, t, r, _randn(g, (N,)), _randn(g, (N,)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [40, 1500, 20011])
+@pytest.mark.parametrize("pattern", ["half masked", "one left", "nothing left", "constant", "lowest", "rising", "falling", "far", "certain"])
+def test_token_logprobs_masks_ties_and_extremes(dtype, V, pattern):
+    g = _gen(V)
+    N, low = 6, torch.finfo(dtype).min
+    x = _randn(g, (N, V), dtype, 3.0)
+    if pattern == "half masked":
+        x.masked_fill_(torch.rand((N, V), generator=g, device="cuda") < 0.5, -math.inf)
+        x[:, 3] = 0.5
+    elif pattern == "one left":
+        keep = x[:, V - 2].clone()
+        x.fill_(-math.inf)
+        x[:, V - 2] = keep
+    elif pattern == "nothing left":
+        x.fill_(-math.inf)
+        x[0, 5] = 1.0
+    elif pattern == "constant":
+        x.fill_(1.5)
+    elif pattern == "lowest":
+        x.fill_(low)          # every token masked with the type's lowest value: uniform
+        x[1, 7] = 0.0         # ... and one token left among them
+    elif pattern == "rising":
+        x = torch.arange(V, device="cuda").float().mul_(8.0 / V).to(dtype).repeat(N, 1).contiguous()
+    elif pattern == "falling":
+        x = torch.arange(V, 0, -1, device="cuda").float().mul_(8.0 / V).to(dtype).repeat(N, 1).contiguous()
+    elif pattern == "far":
+        x = (x.float() + 20000.0).to(dtype)
+    else:
+        x[:, 11] = 300.0
+    t = torch.full((N,), 5, dtype=torch.int32, device="cuda")
+    r = lib.token_logprobs(x, t, 32)
+    _check_logprobs(x, t, 32, r)
+    assert bool(torch.isfinite(r.entropy).all()) and bool((r.entropy >= 0).all())
+    d = _check_logprobs_grad(x, t, r, _randn(g, (N,)), _randn(g, (N,)))
+    if pattern == "nothing left":
+        assert bool((d[1:] == 0).all()) and bool((r.entropy[1:] == 0).all())
+    if pattern == "lowest":
+        assert bool(((r.entropy[0].double() - math.log(V)).abs() <= (V / 32 + 80) * U * (1 + math.log(V))).all())
+
+
+@pytest.mark.parametrize("V", [100, 5000])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_token_logprobs_nan_and_inf_stay_in_their_row(V, bad):
+    g = _gen(V)
+    x = _randn(g, (5, V))
+    t = torch.tensor([1, 2, -1, 4, 5], dtype=torch.int32, device="cuda")
+    want = lib.token_logprobs(x, t, 4)
+    x[1, 77], x[2, 30] = bad, bad
+    r = lib.token_logprobs(x, t, 4)
+    good = torch.tensor([0, 3, 4], device="cuda")
+    for a, b in zip(r, want):
+        assert torch.equal(a[good], b[good])
+    assert bool(torch.isnan(r.logp[1])) and float(r.logp[2]) == 0.0 and bool(torch.isnan(r.entropy[1:3]).all())
+    assert int(r.top_ids[1, 0]) == 77 and int(r.top_ids[2, 0]) == 30   # first in their order
+    d = lib.token_logprobs_backward(torch.ones(5, device="cuda"), None, x, t, r.stats, r.entropy)
+    assert bool(torch.isnan(d[1]).all()) and bool(torch.isfinite(d[good]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,pitch,offset", [(1000, 1003, 1), (4097, 4101, 3), (9000, 9001, 5)])
+def test_token_logprobs_of_strided_rows(dtype, V, pitch, offset):
+    g = _gen(V)
+    buf = _randn(g, (9 * pitch + 16,), dtype, 2.0)
+    x = buf[offset:offset + 9 * pitch].view(9, pitch)[:, :V]
+    t = torch.randint(0, V, (9,), generator=g, device="cuda", dtype=torch.int32)
+    r = lib.token_logprobs(x, t, 6)
+    dlp, dh = _randn(g, (9,)), _randn(g, (9,))
+    _check_logprobs(x, t, 6, r)
+    _check_logprobs_grad(x, t, r, dlp, dh)
+    _check_logprobs_grad(x, t, r, None, dh)
+    _check_logprobs_grad(x, t, r, dlp, None)
+    # the same rows at another alignment: the same alternatives
+    assert torch.equal(lib.token_logprobs(x.contiguous(), t, 6).top_ids, r.top_ids)
+
+
+def test_token_logprobs_gradient_against_differences():
+    g = _gen(3)
+    N, V, step = 2, 1100, 1e-2
+    x = _randn(g, (N, V), torch.float32, 1.0)
+    t = torch.tensor([3, 1099], dtype=torch.int32, device="cuda")
+    dlp, dh = _randn(g, (N,)), _randn(g, (N,))
+    r = lib.token_logprobs(x, t)
+    d = lib.token_logprobs_backward(dlp, dh, x, t, r.stats, r.entropy)
+
+    def value(y):   # the function itself in 64 bits
+        _, h, picked, _, _ = _logprobs_64(y, t)
+        return picked * dlp.double() + h * dh.double()
+
+    for j in (0, 3, 500, 1099):
+        e = torch.zeros((N, V), dtype=torch.float64, device="cuda")
+        e[:, j] = step
+        diff = (value(x.double() + e) - value(x.double() - e)) / (2 * step)
+        # central differences: the third derivative is at most about 6 (|dlp| + |dh| (log V + 2)); and the kernel's own error
+        scale = dlp.abs().double() + dh.abs().double() * (math.log(V) + 2)
+        assert bool(((d[:, j].double() - diff).abs() <= step * step * scale + 1e-5 * scale).all())
+
+
+def test_token_logprobs_batch_dims_empty_batches_and_refusals():
+    g = _gen(5)
+    x = _randn(g, (3, 4, 50))
+    t = torch.zeros((3, 4), dtype=torch.int32, device="cuda")
+    r = lib.token_logprobs(x, t, 2)
+    assert r.logp.shape == (3, 4) and r.stats.shape == (3, 4, 2) and r.top_ids.shape == (3, 4, 2)
+    assert torch.equal(r.logp.view(-1), lib.token_logprobs(x.view(12, 50), t.view(-1), 2).logp)
+    e = lib.token_logprobs(x[:0], t[:0], 2)
+    assert e.logp.shape == (0, 4)
+    assert lib.token_logprobs_backward(None, None, x[:0], t[:0], e.stats, e.entropy).shape == (0, 4, 50)
+    for bad in (lambda: lib.token_logprobs(x.transpose(0, 2), t), lambda: lib.token_logprobs(x, t.long()),
+                lambda: lib.token_logprobs(x, t, 33), lambda: lib.token_logprobs(x, t, 51), lambda: lib.token_logprobs(x, t[:2]),
+                lambda: lib.token_logprobs(x.double(), t), lambda: lib.token_logprobs(x.cpu(), t), lambda: lib.token_logprobs(x, t.cpu()),
+                lambda: lib.token_logprobs_backward(t, None, x, t, r.stats, r.entropy),
+                lambda: lib.token_logprobs_backward(None, None, x, t, r.entropy, r.entropy)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+# ------------------------------------------------------------------------- gradient clipping
+
+def _check_clip(grads, max_norm, out, norms):
+    whole = torch.stack([g.double().flatten(1).square().sum(dim=1) for g in grads]).sum(dim=0).sqrt()
+    # squares and sums in 64 bits: the norm is rounded once
+    assert bool(((norms.double() - whole).abs() <= whole * 2 * U).all())
+    c = torch.clamp(max_norm / (whole + 1e-6), max=1.0)
+    for g, o in zip(grads, out):
+        want = g.double() * c.view(-1, *[1] * (g.dim() - 1))
+        # the factor and the product are rounded to fp32, the result to its type
+        tol = want.abs() * (3 * U + torch.finfo(o.dtype).eps / 2) + torch.finfo(o.dtype).smallest_normal * torch.finfo(o.dtype).eps
+        assert bool(((o.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("m", [1, 3, 16])
+@pytest.mark.parametrize("tin,tout", [(torch.float32, torch.float32), (torch.bfloat16, torch.float32), (torch.float16, torch.float32),
+                                      (torch.float32, torch.bfloat16), (torch.bfloat16, torch.bfloat16), (torch.float16, torch.float16)])
+@pytest.mark.parametrize("sizes", [[1], [7, 4096, 33, 1], [50001, 3], [123457]])
+def test_clip_grads(m, tin, tout, sizes):
+    g = _gen(m + sum(sizes))
+    std = torch.tensor([1.0 if i % 2 == 0 else 1e-5 for i in range(m)], device="cuda")[:, None]
+    grads = [(torch.randn((m, n), generator=g, device="cuda") * std).to(tin) for n in sizes]
+    keep = [t.clone() for t in grads]
+    out = [torch.empty_like(t, dtype=tout) for t in grads]
+    got, norms = lib.clip_grads(grads, 0.5, out=out)
+    assert got is out
+    _check_clip(grads, 0.5, out, norms)
+    assert all(torch.equal(a, b) for a, b in zip(grads, keep))
+    again = [torch.empty_like(t) for t in out]
+    _, n2 = lib.clip_grads(grads, 0.5, out=again)
+    assert torch.equal(n2, norms) and all(torch.equal(a, b) for a, b in zip(again, out))
+    if tin == tout:
+        _, n3 = lib.clip_grads(grads, 0.5, out=grads)   # in place
+        assert torch.equal(n3, norms) and all(torch.equal(a, b) for a, b in zip(grads, out))
+
+
+def test_clip_grads_into_a_flat_gradient_leaves_the_rest_alone():
+    g = _gen(1)
+    m, shapes = 3, [(5, 7), (1001,), (4, 3, 11)]
+    P = 2000
+    flat = torch.full((m, P), -7.0, device="cuda")
+    grads = [_randn(g, (m,) + s, torch.bfloat16) for s in shapes]
+    out, at = [], 3
+    for s in shapes:
+        n = int(np.prod(s))
+        out.append(flat[:, at:at + n].unflatten(1, s))
+        at += n + 5
+    _, norms = lib.clip_grads(grads, 1.0, out=out)
+    _check_clip(grads, 1.0, out, norms)
+    mask = torch.ones(P, dtype=torch.bool, device="cuda")
+    at = 3
+    for s in shapes:
+        n = int(np.prod(s))
+        mask[at:at + n] = False
+        at += n + 5
+    assert bool((flat[:, mask] == -7.0).all())
+
+
+def test_clip_grads_of_more_tensors_than_one_launch_takes():
+    g = _gen(2)
+    grads = [_randn(g, (2, 1 + (i * 37) % 300), torch.float32 if i % 3 else torch.bfloat16) for i in range(601)]
+    grads.insert(300, torch.empty((2, 0), device="cuda"))
+    out, norms = lib.clip_grads(grads, 2.0)
+    _check_clip(grads, 2.0, out, norms)
+    _, n2 = lib.clip_grads(grads, 2.0, out=grads)
+    assert torch.equal(norms, n2) and all(torch.equal(a, b) for a, b in zip(grads, out))
+
+
+def test_clip_grads_extremes():
+    x = torch.zeros((5, 1000), device="cuda")
+    x[0, 3], x[0, 4] = 3e30, 4e30          # squares beyond fp32
+    x[1, 5] = math.nan
+    x[2, 6], x[2, 7] = math.inf, 1.0
+    x[3, 8] = 1e-30                        # squares below fp32
+    out, norms = lib.clip_grads(x, 1.0)
+    assert abs(float(norms[0]) / 5e30 - 1) < 1e-6 and abs(float(out[0, 3]) - 0.6) < 1e-6
+    assert bool(torch.isnan(out[1]).all())
+    assert math.isinf(float(norms[2])) and float(out[2, 7]) == 0.0 and bool(torch.isnan(out[2, 6]))
+    assert abs(float(norms[3]) / 1e-30 - 1) < 1e-6 and torch.equal(out[3], x[3])
+    assert float(norms[4]) == 0.0 and torch.equal(out[4], x[4])
+
+
+def test_clip_grads_refusals():
+    x = torch.ones((2, 10), device="cuda")
+    for bad in (lambda: lib.clip_grads([], 1.0), lambda: lib.clip_grads([x, x[:1]], 1.0), lambda: lib.clip_grads(x.cpu(), 1.0),
+                lambda: lib.clip_grads(x, 1.0, out=x[:, :5]), lambda: lib.clip_grads(x.double(), 1.0),
+                lambda: lib.clip_grads([x], 1.0, out=[]), lambda: lib.clip_grads(torch.ones((10, 2), device="cuda").t(), 1.0)):
+        with pytest.raises(ValueError):
+            bad()
+    for norm in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(lib.OlsgdError):
+            lib.clip_grads(x, norm)
