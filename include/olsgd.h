@@ -461,6 +461,47 @@ olsgd_status olsgd_clip_grads(const olsgd_clip_tensor* tensors, int32_t n_tensor
                               float max_norm, float* norms, void* workspace,
                               size_t workspace_bytes, void* stream);
 
+/* Gated feed-forward block, worker-batched:
+ *   a = x Wg^T,  b = x Wu^T,  h = act(a) * b
+ * x [m][T][D], Wg and Wu [m][F][D], h [m][T][F], all bf16 or all fp16; products are accumulated
+ * in fp32 on the tensor cores, h is rounded once.  gelu is the tanh form.  Any T, D, F; rows
+ * whose base or strides are not multiples of 16 bytes are copied to the workspace first.
+ *   x, w_gate, w_up   with the elements between workers and between rows of each (a dimension
+ *                     of size one may have any stride); neither may overlap themselves
+ *   h                 contiguous
+ *   pre               NULL, or [m][T][2][Fp] of the same type, Fp = F rounded up to a multiple
+ *                     of 8, 16-byte aligned: a and b, for the backward pass
+ * olsgd_gated_workspace: `backward` 0 or 1; `aligned` nonzero when x, w_gate and w_up have
+ * bases on 16 bytes and strides in multiples of 8 elements (then nothing is copied).       */
+typedef enum { OLSGD_ACT_SILU = 0, OLSGD_ACT_GELU = 1, OLSGD_ACT_RELU = 2, OLSGD_ACT_SIGMOID = 3 } olsgd_activation;
+olsgd_status olsgd_gated_workspace(int32_t m, int64_t T, int64_t D, int64_t F, int32_t backward,
+                                   int32_t aligned, size_t* out_bytes);
+olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int32_t dtype,
+                                 int32_t activation, const void* x, int64_t x_worker_stride,
+                                 int64_t x_row_stride, const void* w_gate,
+                                 int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
+                                 const void* w_up, int64_t w_up_worker_stride,
+                                 int64_t w_up_row_stride, void* h, void* pre, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+/* Its gradient.  With da = d_h b act'(a) and db = d_h act(a), both rounded to the operand type:
+ *   d_x = da Wg + db Wu,  d_w_gate = da^T x,  d_w_up = db^T x,
+ * each rounded once.  pre is what the forward call left for the same x, w_gate and w_up.
+ * d_x may be NULL, and so may d_w_gate and d_w_up together; all three are contiguous.
+ * relu's derivative at 0 is 0.  T == 0 leaves the weight gradients untouched.             */
+olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, int32_t dtype,
+                                  int32_t activation, const void* d_h, int64_t d_h_worker_stride,
+                                  int64_t d_h_row_stride, const void* x, int64_t x_worker_stride,
+                                  int64_t x_row_stride, const void* w_gate,
+                                  int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
+                                  const void* w_up, int64_t w_up_worker_stride,
+                                  int64_t w_up_row_stride, const void* pre, void* d_x,
+                                  void* d_w_gate, void* d_w_up, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+/* Blocks the host until `stream` is idle.  OLSGD_ETIMEOUT if a bounded wait inside an operator
+ * on the current device gave up since the last such call (the outputs of the calls in between
+ * are not valid then); the report is cleared.                                              */
+olsgd_status olsgd_operators_join(void* stream);
+
 /* Iteration counter k.                                                      */
 int64_t olsgd_iteration(const olsgd_ctx* ctx);
 

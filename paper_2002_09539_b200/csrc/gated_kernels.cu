@@ -1,0 +1,685 @@
+// Gated feed-forward block on the fifth-generation tensor cores, worker-batched:
+//   a = x Wg^T,  b = x Wu^T,  h = act(a) * b                                   (forward)
+//   da = dh * b * act'(a),  db = dh * act(a)                                   (element-wise)
+//   dx = da Wg + db Wu,  dWg = da^T x,  dWu = db^T x                           (backward)
+// x [m][T][D], Wg and Wu [m][F][D], h [m][T][F]; 16-bit operands, fp32 accumulation in tensor
+// memory, one rounding of each result.  Training keeps a and b in the operand type: 2 T F
+// 16-bit values written once and read once, against 4 T D F more multiply-adds to form them
+// again; da and db have to be rounded to that type as operands in any case.
+//
+// One kernel, three modes, persistent: a CTA (or a pair of CTAs on one 256-row tile,
+// tcgen05 cta_group::2) walks over tiles of its output.  Warp 0 feeds a ring of shared-memory
+// stages with TMA, warp 1 issues the MMAs into one of two accumulators in tensor memory, eight
+// warps empty the other one.
+//   FORWARD   A = x (K-major), B = the tile's rows of Wg and, below them, of Wu: both
+//             projections are one MMA, so a thread of the epilogue finds a and b of the same
+//             element in its own lane and forms h without any exchange.
+//   DX        A = da then db (K-major), B = Wg then Wu read along D (MN-major): one
+//             accumulation over 2 F, nothing transposed or concatenated in memory.
+//   DW        A = da or db, B = x, both read along their rows (MN-major), K = T.
+//
+// Tiles: 128 rows (256 by a pair) x 256 columns.  The pair halves the B bytes each SM
+// takes in and is used where there is more than one 128-row tile; where 256-column tiles
+// would leave multiprocessors idle (few tokens), tiles are 64 columns wide.
+//
+// TMA wants 16-byte row pitches: operands that do not have them are copied to padded rows in
+// the workspace first.  Every wait is bounded, as in the library's other tensor-core kernels.
+#include "operator_common.cuh"
+#include "operators_internal.h"
+#include "tc_common.cuh"
+
+namespace olsgd {
+namespace {
+
+using namespace tc;
+using namespace op;
+
+enum Mode { FORWARD = 0, DX = 1, DW = 2 };
+constexpr int kGroup = 8;            // row tiles walked together (operand reuse in L2)
+constexpr int kEpiWarps = 8;
+
+__device__ int g_operator_status;    // a bounded wait gave up (olsgd_operators_join)
+
+struct alignas(64) GatedMaps {
+  CUtensorMap a0, a1, b0, b1;
+};
+struct GatedArgs {
+  int num_kb, kb_half;        // K blocks in all; of the first half (DX)
+  int row_tiles, col_tiles;   // per problem
+  int problems;               // workers (DW: workers x 2)
+  int rows, cols;             // extents of one problem's output (FORWARD: cols = F)
+  int act, f16;
+  int out_vec;                // widest store the output's rows allow: 32, 16 or 2 bytes
+  void* out0;                 // h, dx or dWg
+  void* out1;                 // dWu
+  void* pre;                  // FORWARD: a, b [m][T][2][Fp], or null
+  int64_t pre_pitch;          // Fp
+  int pre_vec;                // widest store rows of pre allow: 32 or 16 bytes
+};
+
+template <int STAGES>
+struct Control {
+  uint64_t full[STAGES], empty[STAGES];
+  uint64_t acc_full[2], acc_empty[2];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+__device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t tb, float* a, float* b) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(ta)
+      : "memory");
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(tb)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    a[j] = __uint_as_float(r[j]);
+    b[j] = __uint_as_float(r[16 + j]);
+  }
+}
+
+// ------------------------------------------------------------------------- activations
+// tanh(z) = 1 - 2 / (1 + e^{2z}): exact limits at both ends, no cancellation that matters to
+// a result of 16 bits.
+struct ActPair {
+  float f, df;   // act(a), act'(a)
+};
+constexpr float kGeluK = 0.7978845608028654f;   // sqrt(2 / pi)
+constexpr float kGeluC = 0.044715f;
+
+__device__ __forceinline__ float sigmoid_of(float a) { return __fdividef(1.f, 1.f + ex2(-kLog2e * a)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float a) {
+  if (ACT == OLSGD_ACT_RELU) return a > 0.f ? a : (a != a ? a : 0.f);
+  if (ACT == OLSGD_ACT_SIGMOID) return sigmoid_of(a);
+  // gelu: 0.5 a (1 + tanh z) = a sigmoid(2 z)
+  const float s = ACT == OLSGD_ACT_SILU ? sigmoid_of(a) : sigmoid_of(2.f * kGeluK * a * fmaf(kGeluC * a, a, 1.f));
+  // a = -inf (an overflowed product) meets s = 0: the limit is 0
+  return s == 0.f ? 0.f : a * s;
+}
+
+template <int ACT>
+__device__ __forceinline__ ActPair act_pair(float a) {
+  ActPair r;
+  if (ACT == OLSGD_ACT_RELU) {
+    r.f = a > 0.f ? a : (a != a ? a : 0.f);
+    r.df = a > 0.f ? 1.f : (a != a ? a : 0.f);
+  } else if (ACT == OLSGD_ACT_SIGMOID) {
+    r.f = sigmoid_of(a);
+    r.df = r.f * (1.f - r.f);
+  } else if (ACT == OLSGD_ACT_SILU) {
+    const float s = sigmoid_of(a);
+    r.f = s == 0.f ? 0.f : a * s;
+    r.df = s == 0.f ? 0.f : s * fmaf(a, 1.f - s, 1.f);
+    if (s == 1.f) r.df = 1.f;
+  } else {
+    const float s = sigmoid_of(2.f * kGeluK * a * fmaf(kGeluC * a, a, 1.f));
+    r.f = s == 0.f ? 0.f : a * s;
+    // z' = k (1 + 3 c a^2); act' = s + a s (1 - s) 2 z'
+    const float w = s * (1.f - s);
+    r.df = w == 0.f ? s : fmaf(a * w, 2.f * kGeluK * fmaf(3.f * kGeluC * a, a, 1.f), s);
+  }
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, int f16) {
+  if (f16) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+// 16 results of one row, from column col on, of which those below `cols` exist.
+__device__ __forceinline__ void store16(void* row, int64_t col, int64_t cols, int vec, const float* v, int f16) {
+  uint32_t p[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) p[j] = pack2(v[2 * j], v[2 * j + 1], f16);
+  uint16_t* dst = static_cast<uint16_t*>(row) + col;
+  if (vec == 32 && col + 16 <= cols) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(p[0]), "r"(p[1]),
+                 "r"(p[2]), "r"(p[3]), "r"(p[4]), "r"(p[5]), "r"(p[6]), "r"(p[7])
+                 : "memory");
+  } else if (vec >= 16) {   // cols is a multiple of 8
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      if (col + 8 * q < cols)
+        reinterpret_cast<uint4*>(dst)[q] = make_uint4(p[4 * q], p[4 * q + 1], p[4 * q + 2], p[4 * q + 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (col + j < cols) dst[j] = (uint16_t)(p[j >> 1] >> (16 * (j & 1)));
+  }
+}
+
+struct Tile {
+  int problem, row, col;   // row and column tile
+};
+// Tiles of one problem in groups of kGroup row tiles, column by column inside a group.
+__device__ __forceinline__ Tile tile_at(const GatedArgs& g, int64_t t) {
+  const int64_t per = (int64_t)g.row_tiles * g.col_tiles;
+  Tile r;
+  r.problem = (int)(t / per);
+  const int64_t i = t - r.problem * per;
+  const int64_t group = i / ((int64_t)kGroup * g.col_tiles);
+  const int first = (int)group * kGroup;
+  const int height = min(kGroup, g.row_tiles - first);
+  const int64_t j = i - group * ((int64_t)kGroup * g.col_tiles);
+  r.row = first + (int)(j % height);
+  r.col = (int)(j / height);
+  return r;
+}
+
+// Arrives on the barrier at this offset in the pair's leader.
+__device__ __forceinline__ void arrive_leader(uint32_t bar) {
+  uint32_t remote;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(bar));
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+}
+
+template <int ACT>
+__device__ __forceinline__ void activate16(const float* a, const float* b, float* h) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) h[j] = act_value<ACT>(a[j]) * b[j];
+}
+
+template <int MODE, int CTAS, int BN, int STAGES>
+__global__ void __launch_bounds__(kThreads, 1)
+gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
+  constexpr bool A_MN = MODE == DW, B_MN = MODE != FORWARD;
+  constexpr int kBRows = BN / CTAS;                       // rows (columns of D) of B held by this CTA
+  constexpr uint32_t kABytes = kBM * kBK * 2;
+  constexpr uint32_t kBBytes = kBRows * kBK * 2;
+  constexpr uint32_t kStageBytes = kABytes + kBBytes;
+  constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;  // output columns of a tile
+  constexpr uint32_t kTmemCols = 2 * BN;
+  static_assert(kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "two accumulators");
+  static_assert(CTAS == 1 || BN == 256, "pairs take whole tiles");
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                              ~static_cast<uintptr_t>(1023));
+  Control<STAGES>* ctl = reinterpret_cast<Control<STAGES>*>(tiles + STAGES * kStageBytes);
+  volatile int* abort_flag = &ctl->abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
+  const bool leader = rank == 0;
+  const int64_t first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+  const int64_t total = (int64_t)g.problems * g.row_tiles * g.col_tiles;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&maps.a0);
+    prefetch_tensormap(&maps.b0);
+    if (MODE != FORWARD) prefetch_tensormap(&maps.a1);
+    if (MODE != DW) prefetch_tensormap(&maps.b1);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&ctl->full[s]), 1);
+      mbar_init(smem_u32(&ctl->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&ctl->acc_full[b]), 1);
+      mbar_init(smem_u32(&ctl->acc_empty[b]), CTAS * kEpiWarps);
+    }
+    ctl->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (CTAS == 2) tmem_alloc_pair(smem_u32(&ctl->tmem_base), kTmemCols);
+    else tmem_alloc(smem_u32(&ctl->tmem_base), kTmemCols);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (CTAS == 2) cluster_barrier();   // the peer's barriers are initialised
+  tc_fence_after();
+  const uint32_t tmem_base = ctl->tmem_base;
+  launch_gate();
+
+  if (warp == 0 && lane == 0) {
+    // ---------------- TMA producer (both CTAs of a pair; the leader announces both's bytes)
+    uint32_t it = 0;
+    for (int64_t t = first; t < total && !*abort_flag; t += step) {
+      const Tile tl = tile_at(g, t);
+      const int worker = MODE == DW ? tl.problem >> 1 : tl.problem;
+      const int m0 = (tl.row * CTAS + rank) * kBM;
+      for (int kb = 0; kb < g.num_kb; ++kb, ++it) {
+        const int s = it % STAGES;
+        if (!mbar_wait(smem_u32(&ctl->empty[s]), ((it / STAGES) & 1) ^ 1, abort_flag)) break;
+        const uint32_t bar_own = smem_u32(&ctl->full[s]);
+        if (leader) mbar_expect_tx(bar_own, CTAS * kStageBytes);
+        const uint32_t a_dst = smem_u32(tiles + s * kStageBytes), b_dst = a_dst + kABytes;
+        const bool second = MODE == DX && kb >= g.kb_half;
+        const int k0 = (second ? kb - g.kb_half : kb) * kBK;
+        auto load = [&](uint32_t dst, const CUtensorMap* map, int c0, int c1) {
+          if (CTAS == 2) tma_load_3d_pair(dst, map, pair_leader_addr(bar_own), c0, c1, worker);
+          else tma_load_3d(dst, map, bar_own, c0, c1, worker);
+        };
+        if (A_MN) {
+          const CUtensorMap* map = (tl.problem & 1) ? &maps.a1 : &maps.a0;
+          load(a_dst, map, m0, k0);
+          load(a_dst + kABytes / 2, map, m0 + 64, k0);
+        } else {
+          load(a_dst, second ? &maps.a1 : &maps.a0, k0, m0);
+        }
+        if (MODE == FORWARD) {
+          const int f0 = tl.col * kColsOut;
+          if (CTAS == 2) {
+            load(b_dst, rank ? &maps.b1 : &maps.b0, k0, f0);
+          } else {
+            load(b_dst, &maps.b0, k0, f0);
+            load(b_dst + kBBytes / 2, &maps.b1, k0, f0);
+          }
+        } else {
+          const int n0 = tl.col * BN + rank * kBRows;
+#pragma unroll
+          for (int j = 0; j < kBRows / 64; ++j)
+            load(b_dst + j * 8192, MODE == DX && second ? &maps.b1 : &maps.b0, n0 + 64 * j, k0);
+        }
+      }
+    }
+    // drain: whoever gave up waits (bounded) for the copies of this CTA still in flight
+    if (CTAS == 1 && *abort_flag) {
+      const uint32_t from = it > STAGES ? it - STAGES : 0;
+      for (uint32_t i = from; i < it; ++i)
+        for (uint32_t n = 0; n < kSpinLimit && !mbar_try_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1); ++n)
+          if ((n & 1023u) == 1023u && global_ns() == 0) break;
+    }
+  } else if (warp == 1 && lane == 0 && leader) {
+    // ---------------- MMA issuer
+    const uint32_t fmt = g.f16 ? 0u : ((1u << 7) | (1u << 10));
+    const uint32_t idesc = (1u << 4) | fmt | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
+                           ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((CTAS * kBM) >> 4) << 24);
+    uint32_t it = 0, n = 0;
+    bool ok = true;
+    for (int64_t t = first; t < total && ok; t += step, ++n) {
+      const uint32_t buf = n & 1;
+      ok = mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((n >> 1) & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t acc = tmem_base + buf * BN;
+      for (int kb = 0; kb < g.num_kb; ++kb, ++it) {
+        const int s = it % STAGES;
+        ok = mbar_wait(smem_u32(&ctl->full[s]), (it / STAGES) & 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t a_addr = smem_u32(tiles + s * kStageBytes), b_addr = a_addr + kABytes;
+        const uint64_t a_desc = A_MN ? smem_desc_mn_sw128(a_addr) : smem_desc_k_sw128(a_addr);
+        const uint64_t b_desc = B_MN ? smem_desc_mn_sw128(b_addr) : smem_desc_k_sw128(b_addr);
+        // 16 K elements: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major tile
+        constexpr uint64_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;
+#pragma unroll
+        for (int k = 0; k < kBK / kUmmaK; ++k) {
+          const uint32_t accumulate = (kb > 0 || k > 0) ? 1u : 0u;
+          if (CTAS == 2) umma_bf16_pair(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, accumulate);
+          else umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, accumulate);
+        }
+        if (CTAS == 2) umma_commit_pair(smem_u32(&ctl->empty[s]));
+        else umma_commit(smem_u32(&ctl->empty[s]));
+      }
+      if (CTAS == 2) umma_commit_pair(smem_u32(&ctl->acc_full[buf]));
+      else umma_commit(smem_u32(&ctl->acc_full[buf]));
+    }
+  } else if (warp >= 2) {
+    // ---------------- epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31; warps 2-5 take the
+    // left half of the tile's 16-column blocks, warps 6-9 the right half
+    const int lane_group = warp & 3, half = (warp - 2) >> 2;
+    constexpr int kBlocks = kColsOut / 16 / 2;   // per warp
+    uint32_t n = 0;
+    for (int64_t t = first; t < total; t += step, ++n) {
+      const uint32_t buf = n & 1;
+      const Tile tl = tile_at(g, t);
+      const int64_t worker = MODE == DW ? tl.problem >> 1 : tl.problem;
+      const int64_t row = (int64_t)(tl.row * CTAS + rank) * kBM + lane_group * 32 + lane;
+      const bool live = row < g.rows;
+      if (!mbar_wait(smem_u32(&ctl->acc_full[buf]), (n >> 1) & 1, abort_flag) || *abort_flag) break;
+      tc_fence_after();
+      const uint32_t acc = tmem_base + buf * BN + ((uint32_t)(lane_group * 32) << 16);
+      uint16_t* out = static_cast<uint16_t*>(MODE == DW && (tl.problem & 1) ? g.out1 : g.out0) +
+                      (worker * g.rows + row) * (int64_t)g.cols;
+      if (MODE == FORWARD) {
+        uint16_t* pre = g.pre ? static_cast<uint16_t*>(g.pre) + (worker * g.rows + row) * 2 * g.pre_pitch : nullptr;
+#pragma unroll 1
+        for (int c = half * kBlocks; c < (half + 1) * kBlocks; ++c) {
+          float a[16], b[16], h[16];
+          __syncwarp();
+          tmem_ld16x2(acc + c * 16, acc + BN / 2 + c * 16, a, b);
+          const int64_t col = (int64_t)tl.col * kColsOut + c * 16;
+          if (live && col < g.cols) {
+            switch (g.act) {
+              case OLSGD_ACT_SILU: activate16<OLSGD_ACT_SILU>(a, b, h); break;
+              case OLSGD_ACT_GELU: activate16<OLSGD_ACT_GELU>(a, b, h); break;
+              case OLSGD_ACT_RELU: activate16<OLSGD_ACT_RELU>(a, b, h); break;
+              default: activate16<OLSGD_ACT_SIGMOID>(a, b, h);
+            }
+            store16(out, col, g.cols, g.out_vec, h, g.f16);
+            if (pre) {
+              // rows of pre_pitch (a multiple of 8): columns up to it exist and are written
+              store16(pre, col, g.pre_pitch, g.pre_vec, a, g.f16);
+              store16(pre + g.pre_pitch, col, g.pre_pitch, g.pre_vec, b, g.f16);
+            }
+          }
+        }
+      } else {
+#pragma unroll 1
+        for (int c = half * kBlocks; c < (half + 1) * kBlocks; c += 2) {
+          float v[16], w[16];
+          __syncwarp();
+          tmem_ld16x2(acc + c * 16, acc + c * 16 + 16, v, w);
+          const int64_t col = (int64_t)tl.col * BN + c * 16;
+          if (live) {
+            store16(out, col, g.cols, g.out_vec, v, g.f16);
+            store16(out, col + 16, g.cols, g.out_vec, w, g.f16);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (CTAS == 2) arrive_leader(smem_u32(&ctl->acc_empty[buf]));
+        else mbar_arrive(smem_u32(&ctl->acc_empty[buf]));
+      }
+    }
+  }
+
+  // ---------------- teardown: every role arrives here, all waits above are bounded
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag && threadIdx.x == 0) {
+    // bounded grace period for copies and MMAs that may still be in flight
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 1000000ull) {
+    }
+    atomicExch(&g_operator_status, (int)OLSGD_ETIMEOUT);
+  }
+  if (CTAS == 2) cluster_barrier();
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    if (CTAS == 2) tmem_dealloc_pair(tmem_base, kTmemCols);
+    else tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------------- element-wise kernels
+
+// Rows of any pitch to rows of a pitch that TMA takes.  [m][rows][cols] of 16-bit values.
+__global__ void __launch_bounds__(256)
+pad_rows_kernel(const uint16_t* __restrict__ in, uint16_t* __restrict__ out, int64_t rows, int64_t cols,
+                int64_t in_worker, int64_t in_row, int64_t pitch) {
+  launch_gate();
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const uint16_t* src = in + (int64_t)blockIdx.y * in_worker + r * in_row;
+    uint16_t* dst = out + ((int64_t)blockIdx.y * rows + r) * pitch;
+    for (int64_t j = threadIdx.x * 8; j < cols; j += 256 * 8) {
+      uint32_t p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = j + 2 * e < cols ? src[j + 2 * e] : 0, hi = j + 2 * e + 1 < cols ? src[j + 2 * e + 1] : 0;
+        p[e] = lo | (hi << 16);
+      }
+      *reinterpret_cast<uint4*>(dst + j) = make_uint4(p[0], p[1], p[2], p[3]);
+    }
+  }
+}
+
+// da = dh b act'(a), db = dh act(a); a, b, da, db have rows of `pitch`.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256)
+gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const T* __restrict__ pre,
+                      T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec) {
+  launch_gate();
+  const int64_t per_row = pitch / 8, n = rows * per_row;
+  const T* dh_w = dh + (int64_t)blockIdx.y * dh_worker;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row, j = (i - r * per_row) * 8;
+    const int64_t wr = (int64_t)blockIdx.y * rows + r;
+    float a[8], b[8], d[8], va[8], vb[8];
+    Elem<T>::unpack(ld16_stream(pre + wr * 2 * pitch + j), a);
+    Elem<T>::unpack(ld16_stream(pre + wr * 2 * pitch + pitch + j), b);
+    const T* src = dh_w + r * dh_row + j;
+    if (vec) {
+      Elem<T>::unpack(ld16_stream(src), d);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = j + e < F ? Elem<T>::to_float(src[e]) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const ActPair p = act_pair<ACT>(a[e]);
+      va[e] = d[e] * b[e] * p.df;
+      vb[e] = d[e] * p.f;
+    }
+    *reinterpret_cast<uint4*>(da + wr * pitch + j) = Elem<T>::pack(va);
+    *reinterpret_cast<uint4*>(db + wr * pitch + j) = Elem<T>::pack(vb);
+  }
+}
+
+// --------------------------------------------------------------------------------- host
+constexpr int64_t round8(int64_t v) { return (v + 7) / 8 * 8; }
+constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+// [m][rows][cols] 16-bit, cols contiguous; boxes of 64 columns by box_rows rows.
+bool make_map16(CUtensorMap* map, const GatedOperand& o, int64_t cols, int64_t rows, int64_t m, int box_rows, bool f16) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const int64_t worker = m > 1 ? o.worker_stride : round8(cols) * rows;
+  const int64_t row = rows > 1 ? o.row_stride : round8(cols);
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)m};
+  cuuint64_t strides[2] = {(cuuint64_t)row * 2, (cuuint64_t)worker * 2};
+  cuuint32_t box[3] = {(cuuint32_t)kBK, (cuuint32_t)box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.p), dims,
+            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int MODE, int CTAS, int BN, int STAGES>
+cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
+  constexpr size_t smem =
+      (size_t)STAGES * (kBM * kBK * 2 + BN / CTAS * kBK * 2) + sizeof(Control<STAGES>) + 1024;
+  static_assert(smem <= 227 * 1024, "shared memory of one CTA");
+  static PerDeviceSmem configured;
+  auto kern = gated_gemm_kernel<MODE, CTAS, BN, STAGES>;
+  cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
+  if (e != cudaSuccess) return e;
+  constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;
+  g.row_tiles = (g.rows + CTAS * kBM - 1) / (CTAS * kBM);
+  g.col_tiles = (g.cols + kColsOut - 1) / kColsOut;
+  const int64_t total = (int64_t)g.problems * g.row_tiles * g.col_tiles;
+  const int64_t room = sm_count() / CTAS;
+  const unsigned ctas = (unsigned)((total < room ? total : room) * CTAS);
+  g_tc_launches += 1;
+  if (CTAS == 1) return launch_chained(kern, dim3(ctas), dim3(kThreads), smem, s, maps, g);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = g_launch_overlap ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, maps, g);
+}
+
+// Which tiles: 256 columns, by a pair where a problem has more than 128 rows, as long as that
+// gives most multiprocessors a tile; else 64 columns.
+struct Shape {
+  int ctas, bn;
+};
+template <int MODE>
+Shape shape_for(const GatedArgs& g) {
+  const int64_t cols256 = MODE == FORWARD ? 128 : 256;
+  const int64_t col_tiles = (g.cols + cols256 - 1) / cols256;
+  const int64_t one = (int64_t)g.problems * ((g.rows + kBM - 1) / kBM) * col_tiles;
+  if (one < 120) return Shape{1, 64};
+  return Shape{g.rows > kBM ? 2 : 1, 256};
+}
+
+template <int MODE>
+cudaError_t launch_mode(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
+  if (sh.bn == 64) return launch_variant<MODE, 1, 64, 8>(maps, g, s);
+  if (sh.ctas == 2) return launch_variant<MODE, 2, 256, 6>(maps, g, s);
+  return launch_variant<MODE, 1, 256, 4>(maps, g, s);
+}
+
+bool tma_ready(const GatedOperand& o, int64_t rows, int64_t m) {
+  return (reinterpret_cast<uintptr_t>(o.p) & 15) == 0 && (rows == 1 || o.row_stride % 8 == 0) &&
+         (m == 1 || o.worker_stride % 8 == 0);
+}
+
+// The operand itself, or its copy in rows of round8(cols) at *ws (which then moves on).
+cudaError_t ready(GatedOperand& o, int64_t rows, int64_t cols, int64_t m, uint8_t** ws, cudaStream_t s) {
+  if (tma_ready(o, rows, m)) return cudaSuccess;
+  const int64_t pitch = round8(cols);
+  uint16_t* dst = reinterpret_cast<uint16_t*>(*ws);
+  *ws += round256((size_t)m * rows * pitch * 2);
+  const cudaError_t e =
+      launch_chained(pad_rows_kernel, dim3((unsigned)(rows < 4096 ? rows : 4096), (unsigned)m), dim3(256), 0, s,
+                     static_cast<const uint16_t*>(o.p), dst, rows, cols, o.worker_stride, o.row_stride, pitch);
+  o = GatedOperand{dst, rows * pitch, pitch};
+  return e;
+}
+
+int store_width(const void* p, int64_t cols) {
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(cols * 2);
+  return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
+}
+
+template <typename T>
+cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, cudaStream_t s) {
+  const int64_t n = a.T * (pitch / 8);
+  const int64_t want = (n + 255) / 256, most = (148 * 8 + a.m - 1) / a.m;
+  const dim3 grid((unsigned)(want < most ? want : most), (unsigned)a.m);
+  const bool vec = a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m);
+  auto k = a.act == OLSGD_ACT_SILU   ? gated_backward_kernel<T, OLSGD_ACT_SILU>
+           : a.act == OLSGD_ACT_GELU ? gated_backward_kernel<T, OLSGD_ACT_GELU>
+           : a.act == OLSGD_ACT_RELU ? gated_backward_kernel<T, OLSGD_ACT_RELU>
+                                     : gated_backward_kernel<T, OLSGD_ACT_SIGMOID>;
+  return launch_chained(k, grid, dim3(256), 0, s, static_cast<const T*>(a.dh.p), a.dh.worker_stride, a.dh.row_stride,
+                        static_cast<const T*>(a.pre), static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec);
+}
+
+#define OLSGD_STEP(call)                    \
+  do {                                      \
+    const cudaError_t e_ = (call);          \
+    if (e_ != cudaSuccess) return e_;       \
+  } while (0)
+
+}  // namespace
+
+size_t gated_workspace(const GatedShape& d, bool backward, bool copies) {
+  const int64_t m = d.m, T = d.T, D = d.D, F = d.F;
+  const size_t copied = copies ? round256((size_t)m * T * round8(D) * 2) + 2 * round256((size_t)m * F * round8(D) * 2) : 0;
+  return copied + (backward ? 2 * round256((size_t)m * T * round8(F) * 2) : 0);
+}
+
+bool gated_needs_copies(const GatedShape& d, const GatedOperand& x, const GatedOperand& wg, const GatedOperand& wu) {
+  return !tma_ready(x, d.T, d.m) || !tma_ready(wg, d.F, d.m) || !tma_ready(wu, d.F, d.m);
+}
+
+cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  OLSGD_STEP(ready(a.x, a.T, a.D, a.m, &ws, s));
+  OLSGD_STEP(ready(a.wg, a.F, a.D, a.m, &ws, s));
+  OLSGD_STEP(ready(a.wu, a.F, a.D, a.m, &ws, s));
+  GatedArgs g{};
+  g.num_kb = (int)((a.D + kBK - 1) / kBK);
+  g.problems = (int)a.m;
+  g.rows = (int)a.T;
+  g.cols = (int)a.F;
+  g.act = a.act;
+  g.f16 = a.f16;
+  g.out_vec = store_width(a.h, a.F);
+  g.out0 = a.h;
+  g.pre = a.pre;
+  g.pre_pitch = round8(a.F);
+  g.pre_vec = store_width(a.pre, g.pre_pitch);
+  const Shape sh = shape_for<FORWARD>(g);
+  GatedMaps maps;
+  const int b_rows = sh.bn / 2;
+  if (!make_map16(&maps.a0, a.x, a.D, a.T, a.m, kBM, a.f16) || !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, b_rows, a.f16) ||
+      !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, b_rows, a.f16))
+    return cudaErrorInvalidValue;
+  maps.a1 = maps.a0;
+  return launch_mode<FORWARD>(sh, maps, g, s);
+}
+
+cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
+  const int64_t pitch = round8(a.F);
+  const size_t part = round256((size_t)a.m * a.T * pitch * 2);
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  void* da = ws;
+  void* db = ws + part;
+  ws += 2 * part;
+  OLSGD_STEP(a.f16 ? elementwise<__half>(a, pitch, da, db, s) : elementwise<__nv_bfloat16>(a, pitch, da, db, s));
+  const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
+  if (a.dx) {
+    OLSGD_STEP(ready(a.wg, a.F, a.D, a.m, &ws, s));
+    OLSGD_STEP(ready(a.wu, a.F, a.D, a.m, &ws, s));
+    GatedArgs g{};
+    g.kb_half = (int)((a.F + kBK - 1) / kBK);
+    g.num_kb = 2 * g.kb_half;
+    g.problems = (int)a.m;
+    g.rows = (int)a.T;
+    g.cols = (int)a.D;
+    g.f16 = a.f16;
+    g.out_vec = store_width(a.dx, a.D);
+    g.out0 = a.dx;
+    GatedMaps maps;
+    if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, kBM, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, kBM, a.f16) ||
+        !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, kBK, a.f16) || !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, kBK, a.f16))
+      return cudaErrorInvalidValue;
+    OLSGD_STEP(launch_mode<DX>(shape_for<DX>(g), maps, g, s));
+  }
+  if (a.dwg) {
+    OLSGD_STEP(ready(a.x, a.T, a.D, a.m, &ws, s));
+    GatedArgs g{};
+    g.num_kb = (int)((a.T + kBK - 1) / kBK);
+    g.problems = (int)(2 * a.m);
+    g.rows = (int)a.F;
+    g.cols = (int)a.D;
+    g.f16 = a.f16;
+    const int v0 = store_width(a.dwg, a.D), v1 = store_width(a.dwu, a.D);
+    g.out_vec = v0 < v1 ? v0 : v1;
+    g.out0 = a.dwg;
+    g.out1 = a.dwu;
+    GatedMaps maps;
+    if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, kBK, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, kBK, a.f16) ||
+        !make_map16(&maps.b0, a.x, a.D, a.T, a.m, kBK, a.f16))
+      return cudaErrorInvalidValue;
+    maps.b1 = maps.b0;
+    OLSGD_STEP(launch_mode<DW>(shape_for<DW>(g), maps, g, s));
+  }
+  return cudaSuccess;
+}
+
+cudaError_t operators_status(int* status, cudaStream_t s) {
+  OLSGD_STEP(cudaStreamSynchronize(s));
+  OLSGD_STEP(cudaMemcpyFromSymbol(status, g_operator_status, sizeof(int)));
+  if (*status != 0) {
+    const int zero = 0;
+    OLSGD_STEP(cudaMemcpyToSymbol(g_operator_status, &zero, sizeof(int)));
+  }
+  return cudaSuccess;
+}
+
+}  // namespace olsgd

@@ -52,6 +52,25 @@ olsgd_status check_workspace(void* ws, size_t have, size_t need) {
   return OLSGD_OK;
 }
 
+olsgd_status check_gated(int32_t m, int64_t T, int64_t D, int64_t F) {
+  OLSGD_REFUSE_IF(m < 1 || m > 65535, "m must be in [1, 65535]");
+  OLSGD_REFUSE_IF(T < 0 || T > (1 << 28), "T must be in [0, 2^28]");
+  OLSGD_REFUSE_IF(D < 1 || D > (1 << 24) || F < 1 || F > (1 << 24), "D and F must be in [1, 2^24]");
+  return OLSGD_OK;
+}
+olsgd_status check_gated_kind(int32_t dtype, int32_t activation) {
+  OLSGD_REFUSE_IF(dtype != OLSGD_BF16 && dtype != OLSGD_F16, "the gated block takes bf16 and fp16 operands");
+  OLSGD_REFUSE_IF(activation < OLSGD_ACT_SILU || activation > OLSGD_ACT_SIGMOID, "unknown activation %d", (int)activation);
+  return OLSGD_OK;
+}
+olsgd_status check_operand(const GatedOperand& o, const char* name, int64_t m, int64_t rows, int64_t cols) {
+  OLSGD_REFUSE_IF(!aligned_to(o.p, 2), "%s must be non-null and 2-byte aligned", name);
+  OLSGD_REFUSE_IF(rows > 1 && (o.row_stride < cols || o.row_stride > (1LL << 38)), "%s: rows must not overlap", name);
+  OLSGD_REFUSE_IF(m > 1 && (o.worker_stride < (rows - 1) * o.row_stride + cols || o.worker_stride > (1LL << 38)),
+                  "%s: workers must not overlap", name);
+  return OLSGD_OK;
+}
+
 #define OLSGD_TRY(call)                      \
   do {                                       \
     const olsgd_status st_ = (call);         \
@@ -147,6 +166,87 @@ olsgd_status olsgd_clip_grads(const olsgd_clip_tensor* tensors, int32_t n_tensor
   OLSGD_TRY(check_workspace(workspace, workspace_bytes, need));
   return launched(launch_clip(tensors, n_tensors, m, max_norm, norms, workspace, static_cast<cudaStream_t>(stream)),
                   "olsgd_clip_grads");
+}
+
+// ------------------------------------------------------------------- gated feed-forward block
+
+olsgd_status olsgd_gated_workspace(int32_t m, int64_t T, int64_t D, int64_t F, int32_t backward,
+                                   int32_t aligned, size_t* out_bytes) {
+  OLSGD_REFUSE_IF(!out_bytes, "out_bytes is NULL");
+  OLSGD_TRY(check_gated(m, T, D, F));
+  *out_bytes = T == 0 ? 0 : gated_workspace(GatedShape{m, T, D, F, 0, false}, backward != 0, aligned == 0);
+  return OLSGD_OK;
+}
+
+olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int32_t dtype,
+                                 int32_t activation, const void* x, int64_t x_worker_stride,
+                                 int64_t x_row_stride, const void* w_gate,
+                                 int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
+                                 const void* w_up, int64_t w_up_worker_stride,
+                                 int64_t w_up_row_stride, void* h, void* pre, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  OLSGD_TRY(check_gated(m, T, D, F));
+  OLSGD_TRY(check_gated_kind(dtype, activation));
+  if (T == 0) return OLSGD_OK;
+  GatedForward a;
+  static_cast<GatedShape&>(a) = GatedShape{m, T, D, F, activation, dtype == OLSGD_F16};
+  a.x = GatedOperand{x, x_worker_stride, x_row_stride};
+  a.wg = GatedOperand{w_gate, w_gate_worker_stride, w_gate_row_stride};
+  a.wu = GatedOperand{w_up, w_up_worker_stride, w_up_row_stride};
+  OLSGD_TRY(check_operand(a.x, "x", m, T, D));
+  OLSGD_TRY(check_operand(a.wg, "w_gate", m, F, D));
+  OLSGD_TRY(check_operand(a.wu, "w_up", m, F, D));
+  OLSGD_REFUSE_IF(!aligned_to(h, 2), "h must be non-null and 2-byte aligned");
+  OLSGD_REFUSE_IF(pre && !aligned_to(pre, 16), "pre must be 16-byte aligned");
+  a.h = h;
+  a.pre = pre;
+  a.ws = workspace;
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, gated_workspace(a, false, gated_needs_copies(a, a.x, a.wg, a.wu))));
+  return launched(launch_gated_forward(a, static_cast<cudaStream_t>(stream)), "olsgd_gated_forward");
+}
+
+olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, int32_t dtype,
+                                  int32_t activation, const void* d_h, int64_t d_h_worker_stride,
+                                  int64_t d_h_row_stride, const void* x, int64_t x_worker_stride,
+                                  int64_t x_row_stride, const void* w_gate,
+                                  int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
+                                  const void* w_up, int64_t w_up_worker_stride,
+                                  int64_t w_up_row_stride, const void* pre, void* d_x,
+                                  void* d_w_gate, void* d_w_up, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  OLSGD_TRY(check_gated(m, T, D, F));
+  OLSGD_TRY(check_gated_kind(dtype, activation));
+  if (T == 0) return OLSGD_OK;
+  GatedBackward a;
+  static_cast<GatedShape&>(a) = GatedShape{m, T, D, F, activation, dtype == OLSGD_F16};
+  a.dh = GatedOperand{d_h, d_h_worker_stride, d_h_row_stride};
+  a.x = GatedOperand{x, x_worker_stride, x_row_stride};
+  a.wg = GatedOperand{w_gate, w_gate_worker_stride, w_gate_row_stride};
+  a.wu = GatedOperand{w_up, w_up_worker_stride, w_up_row_stride};
+  OLSGD_TRY(check_operand(a.dh, "d_h", m, T, F));
+  OLSGD_TRY(check_operand(a.x, "x", m, T, D));
+  OLSGD_TRY(check_operand(a.wg, "w_gate", m, F, D));
+  OLSGD_TRY(check_operand(a.wu, "w_up", m, F, D));
+  OLSGD_REFUSE_IF(!aligned_to(pre, 16), "pre must be non-null and 16-byte aligned");
+  OLSGD_REFUSE_IF((d_w_gate == nullptr) != (d_w_up == nullptr), "d_w_gate and d_w_up are wanted both or neither");
+  OLSGD_REFUSE_IF((d_x && !aligned_to(d_x, 2)) || (d_w_gate && (!aligned_to(d_w_gate, 2) || !aligned_to(d_w_up, 2))),
+                  "d_x, d_w_gate and d_w_up must be 2-byte aligned");
+  if (!d_x && !d_w_gate) return OLSGD_OK;
+  a.pre = pre;
+  a.dx = d_x;
+  a.dwg = d_w_gate;
+  a.dwu = d_w_up;
+  a.ws = workspace;
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, gated_workspace(a, true, gated_needs_copies(a, a.x, a.wg, a.wu))));
+  return launched(launch_gated_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_gated_backward");
+}
+
+olsgd_status olsgd_operators_join(void* stream) {
+  int status = 0;
+  const olsgd_status st = launched(operators_status(&status, static_cast<cudaStream_t>(stream)), "olsgd_operators_join");
+  if (st != OLSGD_OK) return st;
+  if (status != 0) return refuse(OLSGD_ETIMEOUT, "a bounded device-side wait of an operator gave up: its outputs are not valid");
+  return OLSGD_OK;
 }
 
 }  // extern "C"

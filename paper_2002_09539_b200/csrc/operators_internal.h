@@ -34,4 +34,31 @@ size_t clip_workspace(int32_t m, int32_t n_tensors);
 cudaError_t launch_clip(const olsgd_clip_tensor* t, int32_t n_tensors, int32_t m, float max_norm,
                         float* norms, void* ws, cudaStream_t s);
 
+// ---- gated_kernels.cu ---------------------------------------------------------
+struct GatedOperand {      // [m][rows][cols], cols contiguous; strides in elements
+  const void* p;
+  int64_t worker_stride, row_stride;
+};
+struct GatedShape {
+  int64_t m, T, D, F;
+  int act;                 // olsgd_activation
+  bool f16;
+};
+struct GatedForward : GatedShape {
+  GatedOperand x, wg, wu;
+  void *h, *pre, *ws;
+};
+struct GatedBackward : GatedShape {
+  GatedOperand dh, x, wg, wu;
+  const void* pre;
+  void *dx, *dwg, *dwu, *ws;
+};
+// Whether an operand has to be copied to rows that TMA takes.
+bool gated_needs_copies(const GatedShape& d, const GatedOperand& x, const GatedOperand& wg, const GatedOperand& wu);
+size_t gated_workspace(const GatedShape& d, bool backward, bool copies);
+cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s);
+cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s);
+// Joins the stream; *status: OLSGD_OK, or what a bounded wait left since the last call.
+cudaError_t operators_status(int* status, cudaStream_t s);
+
 }  // namespace olsgd

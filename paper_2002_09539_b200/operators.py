@@ -17,6 +17,7 @@ import torch
 from .binding import _check, load_library
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 MAX_TOP = 32
 
 TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy stats top_logp top_ids")
@@ -27,6 +28,10 @@ _SIGNATURES = {
     "olsgd_token_logprobs": [_vp, _i32, _i64, _i64, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
     "olsgd_token_logprobs_backward": [_vp, _vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp],
     "olsgd_clip_grads_workspace": [_i32, _i32, C.POINTER(_sz)],
+    "olsgd_gated_workspace": [_i32, _i64, _i64, _i64, _i32, _i32, C.POINTER(_sz)],
+    "olsgd_gated_forward": [_i32, _i64, _i64, _i64, _i32, _i32] + 3 * [_vp, _i64, _i64] + [_vp, _vp, _vp, _sz, _vp],
+    "olsgd_gated_backward": [_i32, _i64, _i64, _i64, _i32, _i32] + 4 * [_vp, _i64, _i64] + [_vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "olsgd_operators_join": [_vp],
     "olsgd_clip_grads": [_vp, _i32, _i32, C.c_float, _vp, _vp, _sz, _vp],
 }
 _OPS = None
@@ -190,3 +195,72 @@ def clip_grads(grads, max_norm, out=None):
     ws, wp, wn = _workspace(dev, "olsgd_clip_grads_workspace", m, len(grads))
     _run(lib.olsgd_clip_grads, dev, table, len(grads), m, float(max_norm), norms.data_ptr(), wp, wn)
     return (out[0] if single else out), norms
+
+
+# ---------------------------------------------------------------------- gated feed-forward block
+
+def _matrix(t, name, shape, dtype, dev):
+    """(pointer, worker stride, row stride) of a tensor [m][rows][cols] with contiguous rows."""
+    _need(t.shape == shape and t.dtype == dtype and t.device == dev, "%s must be %s of shape %s on %s", name, dtype, tuple(shape), dev)
+    sw, sr, sc = t.stride()
+    _need(sc == 1 or shape[2] == 1, "%s: the last dimension must be contiguous", name)
+    return t.data_ptr(), sw, sr
+
+
+def _aligned(matrix, shape):
+    p, sw, sr = matrix
+    return p % 16 == 0 and (shape[0] == 1 or sw % 8 == 0) and (shape[1] == 1 or sr % 8 == 0)
+
+
+def _gated_sizes(x, w_gate, activation):
+    _need(x.is_cuda and x.dim() == 3 and w_gate.dim() == 3, "x and w_gate must be CUDA tensors [m][T][D] and [m][F][D]")
+    _need(x.dtype in (torch.bfloat16, torch.float16), "x must be bfloat16 or float16")
+    _need(activation in ACTIVATIONS, "activation must be one of %s", sorted(ACTIVATIONS))
+    m, T, D = x.shape
+    return m, T, D, w_gate.shape[1], DTYPES[x.dtype], ACTIVATIONS[activation]
+
+
+def gated_forward(x, w_gate, w_up, activation="silu", save=False):
+    """olsgd_gated_forward: h = act(x w_gate^T) * (x w_up^T) for each worker.  x [m][T][D], w_gate and w_up [m][F][D], bfloat16
+    or float16, rows contiguous, any worker and row strides.  Returns h [m][T][F], and with save=True (h, pre), pre being what
+    gated_backward takes."""
+    lib = _ops()
+    m, T, D, F, code, act = _gated_sizes(x, w_gate, activation)
+    dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
+    a, b, c = _matrix(x, "x", (m, T, D), dtype, dev), _matrix(w_gate, "w_gate", ws_shape, dtype, dev), _matrix(w_up, "w_up", ws_shape, dtype, dev)
+    h = torch.empty((m, T, F), dtype=dtype, device=dev)
+    pre = torch.empty((m, T, 2, (F + 7) // 8 * 8), dtype=dtype, device=dev) if save else None
+    ok = _aligned(a, (m, T)) and _aligned(b, ws_shape) and _aligned(c, ws_shape)
+    ws, wp, wn = _workspace(dev, "olsgd_gated_workspace", m, T, D, F, 0, ok)
+    _run(lib.olsgd_gated_forward, dev, m, T, D, F, code, act, *a, *b, *c, h.data_ptr(), pre.data_ptr() if save else None, wp, wn)
+    return (h, pre) if save else h
+
+
+def gated_backward(d_h, x, w_gate, w_up, pre, activation="silu", want_d_x=True, want_d_w=True):
+    """olsgd_gated_backward: (d_x, d_w_gate, d_w_up) from d_h [m][T][F] and the forward call's operands and pre; None for
+    those not wanted."""
+    lib = _ops()
+    m, T, D, F, code, act = _gated_sizes(x, w_gate, activation)
+    dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
+    d, a = _matrix(d_h, "d_h", (m, T, F), dtype, dev), _matrix(x, "x", (m, T, D), dtype, dev)
+    b, c = _matrix(w_gate, "w_gate", ws_shape, dtype, dev), _matrix(w_up, "w_up", ws_shape, dtype, dev)
+    _need(pre.shape == (m, T, 2, (F + 7) // 8 * 8) and pre.dtype == dtype and pre.device == dev and pre.is_contiguous(),
+          "pre must be the one that gated_forward returned")
+    d_x = torch.empty((m, T, D), dtype=dtype, device=dev) if want_d_x else None
+    d_wg = d_wu = None
+    if want_d_w:
+        new = torch.empty if T else torch.zeros   # no tokens: nothing is launched, and the gradients are zero
+        d_wg, d_wu = new(ws_shape, dtype=dtype, device=dev), new(ws_shape, dtype=dtype, device=dev)
+    ok = _aligned(a, (m, T)) and _aligned(b, ws_shape) and _aligned(c, ws_shape)
+    ws, wp, wn = _workspace(dev, "olsgd_gated_workspace", m, T, D, F, 1, ok)
+    _run(lib.olsgd_gated_backward, dev, m, T, D, F, code, act, *d, *a, *b, *c, pre.data_ptr(), d_x.data_ptr() if want_d_x else None,
+         d_wg.data_ptr() if want_d_w else None, d_wu.data_ptr() if want_d_w else None, wp, wn)
+    return d_x, d_wg, d_wu
+
+
+def operators_join(device="cuda"):
+    """olsgd_operators_join on the device's current stream: waits for it, and raises if an operator's bounded wait gave up."""
+    dev = torch.device(device)
+    if dev.index is None:
+        dev = torch.device(dev.type, torch.cuda.current_device())
+    _run(_ops().olsgd_operators_join, dev)

@@ -314,3 +314,176 @@ def test_clip_grads_refusals():
     for norm in (0.0, -1.0, math.nan, math.inf):
         with pytest.raises(lib.OlsgdError):
             lib.clip_grads(x, norm)
+
+
+# ---------------------------------------------------------------------- gated feed-forward block
+
+ACTS = ["silu", "gelu", "relu", "sigmoid"]
+
+
+def _act_64(kind, a):
+    """act(a), act'(a) in 64 bits."""
+    if kind == "relu":
+        return a.clamp(min=0.0), (a > 0).double()
+    if kind == "gelu":
+        k, c = math.sqrt(2 / math.pi), 0.044715
+        t = torch.tanh(k * (a + c * a ** 3))
+        return 0.5 * a * (1 + t), 0.5 * (1 + t) + 0.5 * a * (1 - t * t) * k * (1 + 3 * c * a * a)
+    s = torch.sigmoid(a)
+    return (s, s * (1 - s)) if kind == "sigmoid" else (a * s, s * (1 + a * (1 - s)))
+
+
+def _product_error(K):
+    """Relative to sum |x||w|: products of 16-bit values are exact in fp32; 16 of them enter an accumulator at a time,
+    which may drop its last bit rather than round it, and so may the alignment of each group of 8."""
+    return (K / 8 + 8) * 2 * U
+
+
+def _check_gated(x, wg, wu, dh, kind):
+    dtype = x.dtype
+    half, tiny = torch.finfo(dtype).eps / 2, (2.0 ** -24 if dtype == torch.float16 else 2.0 ** -126)
+    D, F = x.shape[2], wg.shape[1]
+    X, G, Up = x.double(), wg.double(), wu.double()
+    a, b = X @ G.mT, X @ Up.mT
+    f, df = _act_64(kind, a)
+    ea = _product_error(D) * (X.abs() @ G.abs().mT)
+    eb = _product_error(D) * (X.abs() @ Up.abs().mT)
+    # slopes: |act'| <= 1.13 (gelu's is the steepest), |act''| <= 1.2; the device's exponential and division: 8 steps
+    ef = 1.13 * ea + 8 * U * (f.abs() + a.abs())
+    h, pre = lib.gated_forward(x, wg, wu, kind, save=True)
+    tol = f.abs() * eb + b.abs() * ef + ef * eb + (f * b).abs() * (half + 4 * U) + tiny
+    err = (h.double() - f * b).abs()
+    assert bool((err <= tol).all()), float((err - tol).max())
+    assert torch.equal(h, lib.gated_forward(x, wg, wu, kind))
+    if dh is None:
+        return
+    E = dh.double()
+    da, db = E * b * df, E * f
+    ea, eb = ea + half * a.abs() + tiny, eb + half * b.abs() + tiny   # a and b are kept in 16 bits
+    edf = 1.2 * ea + 16 * U * (1 + a.abs())
+    if kind == "relu":
+        edf = torch.where(a.abs() <= ea, torch.ones_like(a), torch.zeros_like(a))   # the side of 0 is open only there
+    eda = E.abs() * (b.abs() * edf + df.abs() * eb + edf * eb) + (half + 4 * U) * da.abs() + tiny
+    edb = E.abs() * (1.13 * ea + 8 * U * (f.abs() + a.abs())) + (half + 4 * U) * db.abs() + tiny
+    eda, edb = eda * (1 + half), edb * (1 + half)
+    dx, dwg, dwu = lib.gated_backward(dh, x, wg, wu, pre, kind)
+    A, B = da.abs() + eda, db.abs() + edb
+    want = da @ G + db @ Up
+    tol = eda @ G.abs() + edb @ Up.abs() + _product_error(2 * F) * (A @ G.abs() + B @ Up.abs()) + half * want.abs() * 1.01 + tiny
+    err = (dx.double() - want).abs()
+    assert bool((err <= tol).all()), float((err - tol).max())
+    T = x.shape[1]
+    for got, d, e, S in ((dwg, da, eda, A), (dwu, db, edb, B)):
+        want = d.mT @ X
+        tol = e.mT @ X.abs() + _product_error(T) * (S.mT @ X.abs()) + half * want.abs() * 1.01 + tiny
+        err = (got.double() - want).abs()
+        assert bool((err <= tol).all()), float((err - tol).max())
+
+
+# tiles of every kind: 64 columns; 256 columns by one CTA and by a pair, in each of the three products; partial rows,
+# columns and K blocks; widths with and without 16-byte rows
+GATED_SHAPES = [(1, 1, 1, 1), (1, 1, 64, 32), (1, 2, 8, 8), (2, 5, 33, 47), (1, 128, 64, 128), (3, 130, 72, 136), (1, 300, 200, 520),
+                (2, 257, 1021, 515), (1, 1, 1024, 4096), (1, 17, 4096, 24), (16, 128, 256, 1024), (8, 300, 128, 1024), (8, 600, 1024, 1024),
+                (16, 100, 2048, 72), (16, 70, 1024, 100), (5, 401, 1000, 1303)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", GATED_SHAPES)
+def test_gated_block(shape, dtype):
+    m, T, D, F = shape
+    g = _gen(sum(shape))
+    x, dh = _randn(g, (m, T, D), dtype), _randn(g, (m, T, F), dtype)
+    wg, wu = _randn(g, (m, F, D), dtype, D ** -0.5), _randn(g, (m, F, D), dtype, D ** -0.5)
+    _check_gated(x, wg, wu, dh, ACTS[sum(shape) % 4])
+    lib.operators_join()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("kind", ACTS)
+def test_gated_block_activations(kind, dtype):
+    g = _gen(11)
+    x, dh = _randn(g, (2, 70, 96), dtype, 4.0), _randn(g, (2, 70, 80), dtype)
+    wg, wu = _randn(g, (2, 80, 96), dtype, 0.2), _randn(g, (2, 80, 96), dtype, 0.1)
+    _check_gated(x, wg, wu, dh, kind)
+
+
+@pytest.mark.parametrize("pad", [8, 3])
+def test_gated_block_of_strided_operands(pad):
+    """Weights as views of flat rows, tokens as a slice of longer sequences; with 16-byte pitches and without."""
+    g = _gen(pad)
+    m, T, D, F, dtype = 2, 37, 128, 72, torch.bfloat16
+    flat = _randn(g, (m, 2 * F * (D + pad) + 11 * pad), dtype, 0.1)
+    wg = flat[:, pad:pad + F * (D + pad)].unflatten(1, (F, D + pad))[:, :, :D]
+    wu = flat[:, F * (D + pad) + 2 * pad:2 * F * (D + pad) + 2 * pad].unflatten(1, (F, D + pad))[:, :, :D]
+    x = _randn(g, (m, T + 5, D + pad), dtype)[:, 2:T + 2, :D]
+    dh = _randn(g, (m, T + 1, F + pad), dtype)[:, 1:, pad:]
+    _check_gated(x, wg, wu, dh, "silu")
+    h, pre = lib.gated_forward(x, wg, wu, "silu", save=True)
+    c = [t.contiguous() for t in (x, wg, wu, dh)]
+    assert torch.equal(h, lib.gated_forward(c[0], c[1], c[2]))
+    for a, b in zip(lib.gated_backward(dh, x, wg, wu, pre), lib.gated_backward(c[3], c[0], c[1], c[2], pre)):
+        assert torch.equal(a, b)
+
+
+def test_gated_block_extremes_stay_in_their_rows():
+    g = _gen(4)
+    dtype = torch.bfloat16
+    x, dh = _randn(g, (1, 40, 64), dtype), _randn(g, (1, 40, 48), dtype)
+    wg, wu = _randn(g, (1, 48, 64), dtype), _randn(g, (1, 48, 64), dtype)
+    want = {k: lib.gated_forward(x, wg, wu, k, save=True) for k in ACTS}
+    grads = {k: lib.gated_backward(dh, x, wg, wu, want[k][1], k)[0] for k in ACTS}
+    x[0, 3, 5] = math.nan
+    x[0, 7] = 3e38 * torch.sign(wg[0, 0].float()).to(dtype)   # products beyond fp32
+    keep = [i for i in range(40) if i not in (3, 7)]
+    for k in ACTS:
+        h, pre = lib.gated_forward(x, wg, wu, k, save=True)
+        assert bool(torch.isnan(h[0, 3]).all())
+        assert torch.equal(h[0, keep], want[k][0][0, keep])
+        dx = lib.gated_backward(dh, x, wg, wu, pre, k, want_d_w=False)[0]
+        assert torch.equal(dx[0, keep], grads[k][0, keep])
+
+
+def test_gated_gradients_against_differences():
+    g = _gen(6)
+    m, T, D, F = 1, 6, 16, 24
+    x, wg, wu = _randn(g, (m, T, D), torch.float16), _randn(g, (m, F, D), torch.float16, 0.3), _randn(g, (m, F, D), torch.float16, 0.3)
+    dh = _randn(g, (m, T, F), torch.float16)
+    _, pre = lib.gated_forward(x, wg, wu, "gelu", save=True)
+    dx, dwg, dwu = lib.gated_backward(dh, x, wg, wu, pre, "gelu")
+    X, G, Up, E, step = x.double(), wg.double(), wu.double(), dh.double(), 1e-4
+
+    def loss(X, G, Up):
+        return float((_act_64("gelu", X @ G.mT)[0] * (X @ Up.mT) * E).sum())
+
+    for got, which in ((dx, 0), (dwg, 1), (dwu, 2)):
+        for at in ((0, 0, 0), (0, 3, 7), (0, 5, 15)):
+            lo, hi = [X.clone(), G.clone(), Up.clone()], [X.clone(), G.clone(), Up.clone()]
+            lo[which][at] -= step
+            hi[which][at] += step
+            diff = (loss(*hi) - loss(*lo)) / (2 * step)
+            # sums of some twenty terms of size one, each of values rounded three times to 11 bits
+            assert abs(float(got[at]) - diff) <= 60 * 3 * 2.0 ** -11
+
+
+def test_gated_parts_empty_batches_and_refusals():
+    g = _gen(8)
+    x, wg, wu = _randn(g, (2, 9, 40), torch.bfloat16), _randn(g, (2, 16, 40), torch.bfloat16), _randn(g, (2, 16, 40), torch.bfloat16)
+    dh = _randn(g, (2, 9, 16), torch.bfloat16)
+    h, pre = lib.gated_forward(x, wg, wu, "relu", save=True)
+    whole = lib.gated_backward(dh, x, wg, wu, pre, "relu")
+    dx, none, _ = lib.gated_backward(dh, x, wg, wu, pre, "relu", want_d_w=False)
+    assert none is None and torch.equal(dx, whole[0])
+    none, dwg, dwu = lib.gated_backward(dh, x, wg, wu, pre, "relu", want_d_x=False)
+    assert none is None and torch.equal(dwg, whole[1]) and torch.equal(dwu, whole[2])
+    e, epre = lib.gated_forward(x[:, :0], wg, wu, "relu", save=True)
+    assert e.shape == (2, 0, 16)
+    dx, dwg, dwu = lib.gated_backward(dh[:, :0], x[:, :0], wg, wu, epre, "relu")
+    assert dx.shape == (2, 0, 40) and not bool(dwg.any()) and not bool(dwu.any())
+    for bad in (lambda: lib.gated_forward(x, wg, wu, "tanh"), lambda: lib.gated_forward(x.float(), wg, wu), lambda: lib.gated_forward(x, wg, wu[:, :8]),
+                lambda: lib.gated_forward(x, wg, wu.half()), lambda: lib.gated_forward(x.cpu(), wg, wu), lambda: lib.gated_forward(x, wg[:1], wu),
+                lambda: lib.gated_forward(x.mT, wg, wu), lambda: lib.gated_forward(x, wg.mT.contiguous().mT, wu),
+                lambda: lib.gated_backward(dh, x, wg, wu, pre[:, :5], "relu"), lambda: lib.gated_backward(dh[:, :5], x, wg, wu, pre, "relu")):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(lib.OlsgdError):   # workers on top of each other
+        lib.gated_forward(x[:1].expand(2, 9, 40), wg, wu)
