@@ -401,7 +401,7 @@ olsgd_status olsgd_class_pairs_noalloc(uint64_t seed, int32_t m, int32_t* dst, v
  * aligned to their element (workspaces to 256 bytes); strides are in elements and need not be
  * multiples of 16 bytes.  Outputs must not overlap inputs unless stated, nor other outputs.
  * Errors are reported as everywhere: a status, and olsgd_last_error(NULL).  Sizes of zero
- * rows, tokens or tensors are no error; such a call returns without touching its outputs.   */
+ * rows, tokens or tensors are no error (a gradient of no tokens is zero).                   */
 typedef enum { OLSGD_F32 = 0, OLSGD_BF16 = 1, OLSGD_F16 = 2 } olsgd_dtype;
 
 /* Log probabilities of given tokens, with entropy and the most likely alternatives.
@@ -487,7 +487,7 @@ olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int
  *   d_x = da Wg + db Wu,  d_w_gate = da^T x,  d_w_up = db^T x,
  * each rounded once.  pre is what the forward call left for the same x, w_gate and w_up.
  * d_x may be NULL, and so may d_w_gate and d_w_up together; all three are contiguous.
- * relu's derivative at 0 is 0.  T == 0 leaves the weight gradients untouched.             */
+ * relu's derivative at 0 is 0.  T == 0 zeroes the weight gradients.                         */
 olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, int32_t dtype,
                                   int32_t activation, const void* d_h, int64_t d_h_worker_stride,
                                   int64_t d_h_row_stride, const void* x, int64_t x_worker_stride,
@@ -497,6 +497,27 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
                                   int64_t w_up_row_stride, const void* pre, void* d_x,
                                   void* d_w_gate, void* d_w_up, void* workspace,
                                   size_t workspace_bytes, void* stream);
+/* Embedding lookup with a scale, worker-batched: out[i][t] = scale * table[i][ids[i][t]], rounded
+ * once.  An id outside [0, V) marks a position without a token: a row of zeros, no gradient.
+ *   table  [m][V][D] with the elements between workers and between rows (D contiguous)
+ *   ids    int32 [m][T] contiguous;  out  [m][T][D] contiguous, of the table's type           */
+olsgd_status olsgd_embedding_forward(int32_t m, int64_t T, int64_t V, int64_t D, int32_t dtype,
+                                     const void* table, int64_t table_worker_stride,
+                                     int64_t table_row_stride, const int32_t* ids, float scale,
+                                     void* out, void* stream);
+/* Its gradient: d_table[i][v] = scale * sum of d_out[i][t] over the positions t with
+ * ids[i][t] = v, added up in fp32 in an order that the ids alone decide, rounded once.  Every
+ * element of d_table is written (zeros for tokens that do not occur).
+ *   d_out    [m][T][D] with strides, of type dtype
+ *   d_table  [m][V][D] of type d_table_dtype, each worker's part contiguous, workers
+ *            d_table_worker_stride elements apart (for example rows of a flat gradient)        */
+olsgd_status olsgd_embedding_workspace(int32_t m, int64_t T, int64_t D, size_t* out_bytes);
+olsgd_status olsgd_embedding_backward(int32_t m, int64_t T, int64_t V, int64_t D, int32_t dtype,
+                                      const void* d_out, int64_t d_out_worker_stride,
+                                      int64_t d_out_row_stride, const int32_t* ids, float scale,
+                                      int32_t d_table_dtype, void* d_table,
+                                      int64_t d_table_worker_stride, void* workspace,
+                                      size_t workspace_bytes, void* stream);
 /* Blocks the host until `stream` is idle.  OLSGD_ETIMEOUT if a bounded wait inside an operator
  * on the current device gave up since the last such call (the outputs of the calls in between
  * are not valid then); the report is cleared.                                              */

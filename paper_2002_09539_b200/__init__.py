@@ -8,5 +8,5 @@ from .binding import (OverlapLocalSGD, OlsgdError, class_pairs, class_pairs_noal
                       lib_path, load_library, set_launch_overlap, set_gemm_pairs, tensor_core_launches,
                       KERNEL_CLASSES,
                       NOALLOC_MAX_WORKERS)
-from .operators import (TokenLogprobs, clip_grads, gated_backward, gated_forward,  # noqa: F401
-                        operators_join, token_logprobs, token_logprobs_backward)
+from .operators import (TokenLogprobs, clip_grads, embedding_backward, embedding_forward,  # noqa: F401
+                        gated_backward, gated_forward, operators_join, token_logprobs, token_logprobs_backward)

@@ -1,0 +1,504 @@
+// Embedding lookup with a scale, and the gradient of the table by sorted tokens.
+//
+//   out[t] = scale * W[id_t];   dW[v] = scale * sum over {t : id_t = v} of dout[t]
+//
+// Lookup: a warp per token, 16 bytes per lane; bound by the rows read and written.
+//
+// Gradient: the tokens are sorted by id with a stable radix sort (8 bits a pass, counts and
+// prefix sums only: no order depends on timing), so that a row of the table gets its tokens in
+// the order of their positions.  The sorted list is cut into chunks of kChunk tokens; a CTA
+// adds up a chunk's rows in fp32 registers and writes every table row whose tokens all lie
+// in the chunk.  Rows that reach over a chunk's end leave partial sums, which a third kernel adds
+// in chunk order: a token that fills half of the batch costs as much as any other.  Table rows
+// without a token are zeroed by further CTAs of the same launch.  Each sum is rounded once.
+// Bound by dout read once and the table's gradient written once.
+//
+// Ids outside [0, V) mark positions without a token: a zero row, no gradient.
+#include "operator_common.cuh"
+#include "operators_internal.h"
+
+namespace olsgd {
+namespace {
+
+using namespace op;
+
+// ------------------------------------------------------------------------------ lookup
+constexpr int kLookupThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kLookupThreads)
+embedding_kernel(const T* __restrict__ table, int64_t V, int64_t D, int64_t table_worker, int64_t table_row,
+                 const int32_t* __restrict__ ids, int64_t tokens, T* __restrict__ out, float scale, bool vec) {
+  constexpr int N = Elem<T>::kVec;
+  launch_gate();
+  const int lane = threadIdx.x & 31;
+  const int64_t t = (int64_t)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5);
+  if (t >= tokens) return;
+  const int64_t row = (int64_t)blockIdx.y * tokens + t;
+  const int32_t id = ids[row];
+  const bool has = id >= 0 && id < V;
+  const T* src = table + (int64_t)blockIdx.y * table_worker + (has ? id : 0) * table_row;
+  T* dst = out + row * D;
+  if (vec) {
+    constexpr int U = 4;
+    for (int64_t j0 = lane * N; j0 < D; j0 += 32 * N * U) {
+      uint4 w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t j = j0 + u * 32 * N;
+        w[u] = (has && j < D) ? ld16(src + j) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t j = j0 + u * 32 * N;
+        float v[N];
+        Elem<T>::unpack(w[u], v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = has ? v[e] * scale : 0.f;
+        if (j < D) *reinterpret_cast<uint4*>(dst + j) = Elem<T>::pack(v);
+      }
+    }
+  } else {
+    for (int64_t j = lane; j < D; j += 32)
+      dst[j] = Elem<T>::from_float(has ? Elem<T>::to_float(src[j]) * scale : 0.f);
+  }
+}
+
+// -------------------------------------------------------------------------------- sort
+// Entries are (id << 32 | position); ids outside [0, V) become V and end up last.
+constexpr int kSortThreads = 256;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortItems = 8;                              // entries per thread
+constexpr int kSortTile = kSortThreads * kSortItems;       // entries per CTA
+constexpr int kBins = 256;
+
+__device__ __forceinline__ uint64_t entry_of(const int32_t* ids, int64_t t, uint32_t V) {
+  const int32_t id = ids[t];
+  const uint32_t key = id >= 0 && (uint32_t)id < V ? (uint32_t)id : V;
+  return ((uint64_t)key << 32) | (uint32_t)t;
+}
+
+struct SortArgs {
+  const int32_t* ids;        // [m][T]
+  const uint64_t* in;        // [m][T], or null: the ids themselves
+  uint64_t* out;             // [m][T]
+  uint32_t* counts;          // [m][kBins][tiles]
+  int64_t T;
+  uint32_t V;
+  int tiles, shift;
+};
+
+__device__ __forceinline__ uint64_t entry_at(const SortArgs& a, int64_t worker, int64_t t) {
+  return a.in ? a.in[worker * a.T + t] : entry_of(a.ids + worker * a.T, t, a.V);
+}
+__device__ __forceinline__ uint32_t digit_of(uint64_t e, int shift) { return (uint32_t)(e >> (32 + shift)) & (kBins - 1); }
+
+// How often each digit occurs in a tile.
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
+  __shared__ uint32_t hist[kBins];
+  launch_gate();
+  const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile;
+  hist[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSortItems; ++i) {
+    const int64_t t = t0 + i * kSortThreads + threadIdx.x;
+    if (t < a.T) atomicAdd(&hist[digit_of(entry_at(a, worker, t), a.shift)], 1u);
+  }
+  __syncthreads();
+  a.counts[(worker * kBins + threadIdx.x) * a.tiles + blockIdx.x] = hist[threadIdx.x];
+}
+
+// Places a tile's entries: where its digit starts among all tiles, plus what earlier tiles, earlier
+// warps and earlier entries of the warp hold of the digit.  A single tile counts for itself.
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs a) {
+  __shared__ uint32_t warp_count[kSortWarps][kBins];
+  __shared__ uint32_t start[kBins];
+  __shared__ uint32_t warp_total[kSortWarps];
+  launch_gate();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + warp * (32 * kSortItems);
+  for (int b = lane; b < kBins; b += 32) warp_count[warp][b] = 0;
+  __syncwarp();
+  uint64_t e[kSortItems];
+  uint32_t rank[kSortItems];
+#pragma unroll
+  for (int i = 0; i < kSortItems; ++i) {
+    const int64_t t = t0 + i * 32 + lane;
+    e[i] = t < a.T ? entry_at(a, worker, t) : ~0ull;
+  }
+#pragma unroll
+  for (int i = 0; i < kSortItems; ++i) {
+    const bool live = t0 + i * 32 + lane < a.T;
+    const uint32_t d = live ? digit_of(e[i], a.shift) : kBins;   // dead lanes match each other only
+    const uint32_t same = __match_any_sync(0xffffffffu, d);
+    const uint32_t before = live ? warp_count[warp][d] : 0;
+    rank[i] = before + __popc(same & ((1u << lane) - 1));
+    __syncwarp();
+    if (live && (same & ((1u << lane) - 1)) == 0) warp_count[warp][d] = before + __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  // thread b: digit b.  Sum over all tiles, and over the earlier ones.
+  const int b = threadIdx.x;
+  uint32_t total = 0, earlier = 0;
+  if (a.tiles == 1) {
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) total += warp_count[w][b];
+  } else {
+    const uint32_t* c = a.counts + (worker * kBins + b) * a.tiles;
+    for (int i = 0; i < a.tiles; ++i) {
+      const uint32_t n = c[i];
+      total += n;
+      if (i < (int)blockIdx.x) earlier += n;
+    }
+  }
+  uint32_t scan = total;   // inclusive over the digits
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t n = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += n;
+  }
+  if (lane == 31) warp_total[warp] = scan;
+  __syncthreads();
+  uint32_t base = scan - total + earlier;
+  for (int w = 0; w < warp; ++w) base += warp_total[w];
+  start[b] = base;
+  // counts of a warp become what the warps before it hold
+  uint32_t run = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) {
+    const uint32_t n = warp_count[w][b];
+    warp_count[w][b] = run;
+    run += n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSortItems; ++i) {
+    if (t0 + i * 32 + lane < a.T) {
+      const uint32_t d = digit_of(e[i], a.shift);
+      a.out[worker * a.T + start[d] + warp_count[warp][d] + rank[i]] = e[i];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------- reduction
+constexpr int kChunk = 32;             // sorted tokens per CTA
+constexpr int kSumThreads = 128;
+constexpr int kCols = 8;               // columns per thread
+constexpr int kSlice = kSumThreads * kCols;   // columns per CTA
+constexpr int kZeroRows = 64;          // table rows per zeroing CTA
+constexpr int kJoinThreads = 256;
+constexpr int kJoinCols = 128;         // columns per joining CTA
+
+struct SumArgs {
+  const uint64_t* sorted;   // [m][T]
+  const void* dout;         // [m][T][D] with strides
+  int64_t dout_worker, dout_row;
+  void* dtable;             // [m][V][D], workers out_worker apart
+  int64_t out_worker;
+  float* part;              // [m][chunks][2][pitch]: the row a chunk shares with the one before, with the one after
+  int64_t T, V, D, pitch;
+  int chunks, zero_blocks;
+  float scale;
+  bool vec_in, vec_out;
+};
+
+__device__ __forceinline__ uint32_t key_at(const uint64_t* s, int64_t i) { return (uint32_t)(s[i] >> 32); }
+
+// First position of the sorted list whose key is >= v; by a warp, 32 probes at a time.
+__device__ __forceinline__ int64_t warp_lower_bound(const uint64_t* s, int64_t n, uint32_t v) {
+  const int lane = threadIdx.x & 31;
+  int64_t lo = 0, hi = n;   // answer in [lo, hi]
+  while (lo < hi) {
+    const int64_t width = (hi - lo + 31) / 32;
+    const int64_t probe = lo + lane * width + width - 1;    // last of this lane's stretch
+    const bool below = probe < hi && key_at(s, probe) < v;
+    const int full = __popc(__ballot_sync(0xffffffffu, below));   // stretches that lie below v (a prefix)
+    lo += full * width;
+    if (lo > hi) lo = hi;
+    const int64_t end = lo + width - 1;   // the stretch that is not, if there is one
+    if (end < hi) hi = end;
+    if (width == 1) break;
+  }
+  return lo;
+}
+
+template <typename TO>
+__device__ __forceinline__ void write_cols(TO* row, int64_t c0, int64_t D, bool vec, bool strided, const float* v) {
+  if (!strided) {
+    store_floats<TO, kCols>(row, c0, D, vec, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kCols; ++e)
+      if (c0 + e * kSumThreads < D) row[c0 + e * kSumThreads] = Elem<TO>::from_float(v[e]);
+  }
+}
+
+// CTAs 0 .. chunks - 1 of a worker: one chunk each; the rest: kZeroRows table rows each.
+// VEC: rows of dout and of the table start on 16-byte boundaries; a thread has 8 consecutive
+// columns then, and columns kSumThreads apart otherwise (coalesced either way).
+template <typename TI, typename TO, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArgs a) {
+  launch_gate();
+  const int64_t worker = blockIdx.z;
+  const uint64_t* sorted = a.sorted + worker * a.T;
+  TO* table = static_cast<TO*>(a.dtable) + worker * a.out_worker;
+  const int64_t slice = (int64_t)blockIdx.y * kSlice;
+  const int64_t c0 = slice + (VEC ? threadIdx.x * kCols : threadIdx.x);
+
+  if ((int)blockIdx.x >= a.chunks) {
+    // ---- rows without a token
+    __shared__ uint32_t present[kZeroRows];
+    __shared__ int64_t range[2];
+    const int64_t v0 = (int64_t)(blockIdx.x - a.chunks) * kZeroRows;
+    const int64_t v1 = v0 + kZeroRows < a.V ? v0 + kZeroRows : a.V;
+    if (threadIdx.x < kZeroRows) present[threadIdx.x] = 0;
+    if (threadIdx.x < 64) {   // one warp for each end
+      const int64_t p = warp_lower_bound(sorted, a.T, (uint32_t)(threadIdx.x < 32 ? v0 : v1));
+      if ((threadIdx.x & 31) == 0) range[threadIdx.x >> 5] = p;
+    }
+    __syncthreads();
+    for (int64_t i = range[0] + threadIdx.x; i < range[1]; i += kSumThreads) present[key_at(sorted, i) - v0] = 1;
+    __syncthreads();
+    float zero[kCols];
+#pragma unroll
+    for (int e = 0; e < kCols; ++e) zero[e] = 0.f;
+    for (int64_t v = v0; v < v1; ++v)
+      if (!present[v - v0]) write_cols<TO>(table + v * a.D, c0, a.D, VEC, !VEC, zero);
+    return;
+  }
+
+  // ---- a chunk of the sorted tokens
+  __shared__ uint64_t entry[kChunk + 2];
+  const int64_t i0 = (int64_t)blockIdx.x * kChunk;
+  const int n = (int)(a.T - i0 < kChunk ? a.T - i0 : kChunk);
+  if (threadIdx.x < kChunk + 2) {
+    const int64_t i = i0 + threadIdx.x - 1;   // with the neighbours on both sides; ~0: none
+    entry[threadIdx.x] = i >= 0 && i < a.T && (int)threadIdx.x <= n + 1 ? sorted[i] : ~0ull;
+  }
+  __syncthreads();
+  const TI* dout = static_cast<const TI*>(a.dout) + worker * a.dout_worker;
+  float* part = a.part + (worker * a.chunks + blockIdx.x) * 2 * a.pitch;
+  constexpr int U = 4;
+  float acc[kCols];
+#pragma unroll
+  for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
+  bool from_before = (uint32_t)(entry[0] >> 32) == (uint32_t)(entry[1] >> 32);
+  for (int k0 = 0; k0 < n; k0 += U) {
+    float v[U][kCols];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint64_t en = entry[1 + min(k0 + u, n - 1)];
+      const bool live = k0 + u < n && (uint32_t)(en >> 32) < a.V;
+      const TI* row = dout + (int64_t)(uint32_t)en * a.dout_row;
+      if (VEC) {
+#pragma unroll
+        for (int q = 0; q < kCols / Elem<TI>::kVec; ++q) {
+          const int64_t c = c0 + q * Elem<TI>::kVec;
+          const uint4 w = live && c < a.D ? ld16_stream(row + c) : make_uint4(0, 0, 0, 0);
+          Elem<TI>::unpack(w, v[u] + q * Elem<TI>::kVec);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) {
+          const int64_t c = c0 + e * kSumThreads;
+          v[u][e] = live && c < a.D ? Elem<TI>::to_float(row[c]) : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u;
+      if (k >= n) break;
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) acc[e] += v[u][e];
+      const uint32_t key = (uint32_t)(entry[1 + k] >> 32), next = (uint32_t)(entry[2 + k] >> 32);
+      if (k + 1 < n && next == key) continue;
+      const bool to_after = k + 1 == n && next == key;
+      if (key < a.V) {
+        if (from_before || to_after) {
+          write_cols<float>(part + (from_before ? 0 : a.pitch), c0, a.D, VEC, !VEC, acc);
+        } else {
+          float r[kCols];
+#pragma unroll
+          for (int e = 0; e < kCols; ++e) r[e] = acc[e] * a.scale;
+          write_cols<TO>(table + (int64_t)key * a.D, c0, a.D, VEC, !VEC, r);
+        }
+      }
+      from_before = false;
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
+    }
+  }
+}
+
+// CTA (c, column slice): the table row that starts in chunk c and reaches past its end, if
+// there is one: its part of chunk c, then the parts of the chunks that follow, each eighth of
+// them by a warp of its own, joined in a fixed order.
+template <typename TO>
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumArgs a) {
+  launch_gate();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t worker = blockIdx.z;
+  const uint64_t* sorted = a.sorted + worker * a.T;
+  const int64_t c = blockIdx.x, last = (c + 1) * kChunk - 1;
+  if (last + 1 >= a.T) return;
+  const uint32_t key = key_at(sorted, last);
+  if (key >= a.V || key_at(sorted, last + 1) != key) return;
+  const int64_t first = c * kChunk;
+  // (a chunk that is all one row which began before it belongs to that row's first chunk)
+  if (first > 0 && key_at(sorted, first - 1) == key) return;
+  // the last chunk that holds the key: chunks ahead are probed a warp's width at a time
+  int64_t end = c + 1;
+  for (;;) {
+    const int64_t probe = end + lane;   // does chunk `probe` + 1 begin with the key?
+    const int64_t i = (probe + 1) * kChunk;
+    const bool more = i < a.T && key_at(sorted, i) == key;
+    const uint32_t yes = __ballot_sync(0xffffffffu, more);
+    const int run = yes == 0xffffffffu ? 32 : __ffs(~yes) - 1;
+    end += run;
+    if (run < 32) break;
+  }
+  const float* part = a.part + worker * a.chunks * 2 * a.pitch;
+  const int64_t col = (int64_t)blockIdx.y * kJoinCols + lane * 4;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float* p) {
+    const float4 v = *reinterpret_cast<const float4*>(p + col);
+    acc.x += v.x;
+    acc.y += v.y;
+    acc.z += v.z;
+    acc.w += v.w;
+  };
+  if (col < a.D) {   // (pitch is a multiple of four: whole pieces; those past D are not stored)
+    if (warp == 0) add(part + (c * 2 + 1) * a.pitch);
+#pragma unroll 4
+    for (int64_t k = c + 1 + warp; k <= end; k += kJoinThreads / 32) add(part + k * 2 * a.pitch);
+  }
+  __shared__ float4 sh[kJoinThreads / 32][32];
+  sh[warp][lane] = acc;
+  __syncthreads();
+  if (warp == 0 && col < a.D) {
+    float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) {
+      r[0] += sh[w][lane].x;
+      r[1] += sh[w][lane].y;
+      r[2] += sh[w][lane].z;
+      r[3] += sh[w][lane].w;
+    }
+    TO* row = static_cast<TO*>(a.dtable) + worker * a.out_worker + (int64_t)key * a.D;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < a.D) row[col + e] = Elem<TO>::from_float(r[e] * a.scale);
+  }
+}
+
+// --------------------------------------------------------------------------------- host
+constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+int64_t tiles_of(int64_t T) { return (T + kSortTile - 1) / kSortTile; }
+int64_t chunks_of(int64_t T) { return (T + kChunk - 1) / kChunk; }
+int64_t pitch_of(int64_t D) { return (D + 3) / 4 * 4; }
+
+struct Layout {
+  size_t a, b, counts, part, total;
+};
+Layout layout_of(int64_t m, int64_t T, int64_t D) {
+  Layout l;
+  const size_t list = round256((size_t)m * T * sizeof(uint64_t));
+  l.a = 0;
+  l.b = list;
+  l.counts = 2 * list;
+  l.part = l.counts + round256((size_t)m * kBins * tiles_of(T) * sizeof(uint32_t));
+  l.total = l.part + round256((size_t)m * chunks_of(T) * 2 * pitch_of(D) * sizeof(float));
+  return l;
+}
+
+bool rows_of_16(const void* p, int64_t worker, int64_t row, int64_t m, int64_t rows, int size) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (rows == 1 || row * size % 16 == 0) && (m == 1 || worker * size % 16 == 0);
+}
+
+template <typename TI, typename TO>
+cudaError_t sum_rows(const SumArgs& a, int64_t m, cudaStream_t s) {
+  const dim3 grid((unsigned)(a.chunks + a.zero_blocks), (unsigned)((a.D + kSlice - 1) / kSlice), (unsigned)m);
+  auto k = a.vec_in && a.vec_out ? embedding_sum_kernel<TI, TO, true> : embedding_sum_kernel<TI, TO, false>;
+  cudaError_t e = launch_chained(k, grid, dim3(kSumThreads), 0, s, a);
+  if (e != cudaSuccess || a.chunks <= 1) return e;
+  return launch_chained(embedding_join_kernel<TO>, dim3((unsigned)a.chunks, (unsigned)((a.D + kJoinCols - 1) / kJoinCols), (unsigned)m),
+                        dim3(kJoinThreads), 0, s, a);
+}
+
+template <typename TI>
+cudaError_t sum_rows_to(int dtype, const SumArgs& a, int64_t m, cudaStream_t s) {
+  if (dtype == OLSGD_F32) return sum_rows<TI, float>(a, m, s);
+  if (dtype == OLSGD_BF16) return sum_rows<TI, __nv_bfloat16>(a, m, s);
+  return sum_rows<TI, __half>(a, m, s);
+}
+
+template <typename T>
+cudaError_t lookup(const EmbeddingArgs& a, cudaStream_t s) {
+  const bool vec = a.D % Elem<T>::kVec == 0 && rows_of_16(a.table, a.table_worker, a.table_row, a.m, a.V, sizeof(T)) &&
+                   (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
+  const dim3 grid((unsigned)((a.T + kLookupThreads / 32 - 1) / (kLookupThreads / 32)), (unsigned)a.m);
+  return launch_chained(embedding_kernel<T>, grid, dim3(kLookupThreads), 0, s, static_cast<const T*>(a.table), a.V, a.D,
+                        a.table_worker, a.table_row, a.ids, a.T, static_cast<T*>(a.out), a.scale, vec);
+}
+
+}  // namespace
+
+cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t s) {
+  switch (a.dtype) {
+    case OLSGD_F32: return lookup<float>(a, s);
+    case OLSGD_BF16: return lookup<__nv_bfloat16>(a, s);
+    default: return lookup<__half>(a, s);
+  }
+}
+
+size_t embedding_workspace(int64_t m, int64_t T, int64_t D) { return layout_of(m, T, D).total; }
+
+cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s) {
+  const Layout l = layout_of(g.m, g.T, g.D);
+  uint8_t* ws = static_cast<uint8_t*>(g.ws);
+  uint64_t* lists[2] = {reinterpret_cast<uint64_t*>(ws + l.a), reinterpret_cast<uint64_t*>(ws + l.b)};
+  SortArgs sort{g.ids, nullptr, nullptr, reinterpret_cast<uint32_t*>(ws + l.counts), g.T, (uint32_t)g.V, (int)tiles_of(g.T), 0};
+  const dim3 sort_grid((unsigned)sort.tiles, (unsigned)g.m);
+  int which = 0;
+  for (int shift = 0; g.T > 0 && (g.V >> shift) > 0; shift += 8) {   // keys are 0 .. V
+    sort.shift = shift;
+    sort.out = lists[which];
+    if (sort.tiles > 1) {
+      const cudaError_t e = launch_chained(sort_count_kernel, sort_grid, dim3(kSortThreads), 0, s, sort);
+      if (e != cudaSuccess) return e;
+    }
+    const cudaError_t e = launch_chained(sort_place_kernel, sort_grid, dim3(kSortThreads), 0, s, sort);
+    if (e != cudaSuccess) return e;
+    sort.in = lists[which];
+    which ^= 1;
+  }
+  SumArgs a;
+  a.sorted = sort.in;
+  a.dout = g.dout;
+  a.dout_worker = g.dout_worker;
+  a.dout_row = g.dout_row;
+  a.dtable = g.dtable;
+  a.out_worker = g.dtable_worker;
+  a.part = reinterpret_cast<float*>(ws + l.part);
+  a.T = g.T;
+  a.V = g.V;
+  a.D = g.D;
+  a.pitch = pitch_of(g.D);
+  a.chunks = (int)chunks_of(g.T);
+  a.zero_blocks = (int)((g.V + kZeroRows - 1) / kZeroRows);
+  a.scale = g.scale;
+  const int si = g.dtype == OLSGD_F32 ? 4 : 2, so = g.out_dtype == OLSGD_F32 ? 4 : 2;
+  // whole pieces: the columns end on a piece's end too
+  a.vec_in = g.D % kCols == 0 && rows_of_16(g.dout, g.dout_worker, g.dout_row, g.m, g.T, si);
+  a.vec_out = g.D % kCols == 0 && rows_of_16(g.dtable, g.dtable_worker, g.D, g.m, g.V, so);
+  switch (g.dtype) {
+    case OLSGD_F32: return sum_rows_to<float>(g.out_dtype, a, g.m, s);
+    case OLSGD_BF16: return sum_rows_to<__nv_bfloat16>(g.out_dtype, a, g.m, s);
+    default: return sum_rows_to<__half>(g.out_dtype, a, g.m, s);
+  }
+}
+
+}  // namespace olsgd

@@ -63,11 +63,20 @@ olsgd_status check_gated_kind(int32_t dtype, int32_t activation) {
   OLSGD_REFUSE_IF(activation < OLSGD_ACT_SILU || activation > OLSGD_ACT_SIGMOID, "unknown activation %d", (int)activation);
   return OLSGD_OK;
 }
-olsgd_status check_operand(const GatedOperand& o, const char* name, int64_t m, int64_t rows, int64_t cols) {
-  OLSGD_REFUSE_IF(!aligned_to(o.p, 2), "%s must be non-null and 2-byte aligned", name);
+olsgd_status check_operand(const GatedOperand& o, const char* name, int64_t m, int64_t rows, int64_t cols,
+                           int size = 2) {
+  OLSGD_REFUSE_IF(!aligned_to(o.p, size), "%s must be non-null and aligned to its type", name);
   OLSGD_REFUSE_IF(rows > 1 && (o.row_stride < cols || o.row_stride > (1LL << 38)), "%s: rows must not overlap", name);
   OLSGD_REFUSE_IF(m > 1 && (o.worker_stride < (rows - 1) * o.row_stride + cols || o.worker_stride > (1LL << 38)),
                   "%s: workers must not overlap", name);
+  return OLSGD_OK;
+}
+
+olsgd_status check_embedding(int32_t m, int64_t T, int64_t V, int64_t D, int32_t dtype) {
+  OLSGD_REFUSE_IF(m < 1 || m > 65535, "m must be in [1, 65535]");
+  OLSGD_REFUSE_IF(T < 0 || T > (1 << 24), "T must be in [0, 2^24]");
+  OLSGD_REFUSE_IF(V < 1 || V > (1 << 24) || D < 1 || D > (1 << 24), "V and D must be in [1, 2^24]");
+  OLSGD_REFUSE_IF(!is_dtype(dtype), "unknown element type %d", (int)dtype);
   return OLSGD_OK;
 }
 
@@ -216,7 +225,12 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
                                   size_t workspace_bytes, void* stream) {
   OLSGD_TRY(check_gated(m, T, D, F));
   OLSGD_TRY(check_gated_kind(dtype, activation));
-  if (T == 0) return OLSGD_OK;
+  if (T == 0) {   // no tokens: the weights' gradients are zero
+    if (!d_w_gate || !d_w_up) return OLSGD_OK;
+    const size_t bytes = (size_t)m * F * D * 2;
+    OLSGD_TRY(launched(cudaMemsetAsync(d_w_gate, 0, bytes, static_cast<cudaStream_t>(stream)), "olsgd_gated_backward"));
+    return launched(cudaMemsetAsync(d_w_up, 0, bytes, static_cast<cudaStream_t>(stream)), "olsgd_gated_backward");
+  }
   GatedBackward a;
   static_cast<GatedShape&>(a) = GatedShape{m, T, D, F, activation, dtype == OLSGD_F16};
   a.dh = GatedOperand{d_h, d_h_worker_stride, d_h_row_stride};
@@ -239,6 +253,50 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
   a.ws = workspace;
   OLSGD_TRY(check_workspace(workspace, workspace_bytes, gated_workspace(a, true, gated_needs_copies(a, a.x, a.wg, a.wu))));
   return launched(launch_gated_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_gated_backward");
+}
+
+// -------------------------------------------------------------------------- embedding lookup
+
+olsgd_status olsgd_embedding_forward(int32_t m, int64_t T, int64_t V, int64_t D, int32_t dtype,
+                                     const void* table, int64_t table_worker_stride,
+                                     int64_t table_row_stride, const int32_t* ids, float scale,
+                                     void* out, void* stream) {
+  OLSGD_TRY(check_embedding(m, T, V, D, dtype));
+  if (T == 0) return OLSGD_OK;
+  OLSGD_TRY(check_operand(GatedOperand{table, table_worker_stride, table_row_stride}, "table", m, V, D, elem_size(dtype)));
+  OLSGD_REFUSE_IF(!aligned_to(ids, 4), "ids must be non-null and 4-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(out, elem_size(dtype)), "out must be non-null and aligned to its type");
+  const EmbeddingArgs a{dtype, m, T, V, D, table, table_worker_stride, table_row_stride, ids, out, scale};
+  return launched(launch_embedding_forward(a, static_cast<cudaStream_t>(stream)), "olsgd_embedding_forward");
+}
+
+olsgd_status olsgd_embedding_workspace(int32_t m, int64_t T, int64_t D, size_t* out_bytes) {
+  OLSGD_REFUSE_IF(!out_bytes, "out_bytes is NULL");
+  OLSGD_TRY(check_embedding(m, T, 1, D, OLSGD_F32));
+  *out_bytes = T == 0 ? 0 : embedding_workspace(m, T, D);
+  return OLSGD_OK;
+}
+
+olsgd_status olsgd_embedding_backward(int32_t m, int64_t T, int64_t V, int64_t D, int32_t dtype,
+                                      const void* d_out, int64_t d_out_worker_stride,
+                                      int64_t d_out_row_stride, const int32_t* ids, float scale,
+                                      int32_t d_table_dtype, void* d_table,
+                                      int64_t d_table_worker_stride, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  OLSGD_TRY(check_embedding(m, T, V, D, dtype));
+  OLSGD_REFUSE_IF(!is_dtype(d_table_dtype), "unknown element type %d of d_table", (int)d_table_dtype);
+  OLSGD_REFUSE_IF(!aligned_to(d_table, elem_size(d_table_dtype)), "d_table must be non-null and aligned to its type");
+  OLSGD_REFUSE_IF(m > 1 && d_table_worker_stride < V * D, "d_table: workers must not overlap");
+  size_t need = 0;
+  if (T > 0) {
+    OLSGD_TRY(check_operand(GatedOperand{d_out, d_out_worker_stride, d_out_row_stride}, "d_out", m, T, D, elem_size(dtype)));
+    OLSGD_REFUSE_IF(!aligned_to(ids, 4), "ids must be non-null and 4-byte aligned");
+    need = embedding_workspace(m, T, D);
+  }
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, need));
+  const EmbeddingGradArgs a{dtype, d_table_dtype, m, T, V, D, d_out, d_out_worker_stride, d_out_row_stride, ids, scale,
+                            d_table, d_table_worker_stride, workspace};
+  return launched(launch_embedding_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_embedding_backward");
 }
 
 olsgd_status olsgd_operators_join(void* stream) {

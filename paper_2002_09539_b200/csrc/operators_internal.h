@@ -58,6 +58,31 @@ bool gated_needs_copies(const GatedShape& d, const GatedOperand& x, const GatedO
 size_t gated_workspace(const GatedShape& d, bool backward, bool copies);
 cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s);
 cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s);
+// ---- embedding_kernels.cu -----------------------------------------------------
+struct EmbeddingArgs {
+  int dtype;
+  int64_t m, T, V, D;
+  const void* table;
+  int64_t table_worker, table_row;
+  const int32_t* ids;
+  void* out;
+  float scale;
+};
+cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t s);
+struct EmbeddingGradArgs {
+  int dtype, out_dtype;
+  int64_t m, T, V, D;
+  const void* dout;
+  int64_t dout_worker, dout_row;
+  const int32_t* ids;
+  float scale;
+  void* dtable;
+  int64_t dtable_worker;
+  void* ws;
+};
+size_t embedding_workspace(int64_t m, int64_t T, int64_t D);
+cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, cudaStream_t s);
+
 // Joins the stream; *status: OLSGD_OK, or what a bounded wait left since the last call.
 cudaError_t operators_status(int* status, cudaStream_t s);
 

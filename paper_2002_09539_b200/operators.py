@@ -31,6 +31,9 @@ _SIGNATURES = {
     "olsgd_gated_workspace": [_i32, _i64, _i64, _i64, _i32, _i32, C.POINTER(_sz)],
     "olsgd_gated_forward": [_i32, _i64, _i64, _i64, _i32, _i32] + 3 * [_vp, _i64, _i64] + [_vp, _vp, _vp, _sz, _vp],
     "olsgd_gated_backward": [_i32, _i64, _i64, _i64, _i32, _i32] + 4 * [_vp, _i64, _i64] + [_vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "olsgd_embedding_forward": [_i32, _i64, _i64, _i64, _i32, _vp, _i64, _i64, _vp, C.c_float, _vp, _vp],
+    "olsgd_embedding_workspace": [_i32, _i64, _i64, C.POINTER(_sz)],
+    "olsgd_embedding_backward": [_i32, _i64, _i64, _i64, _i32, _vp, _i64, _i64, _vp, C.c_float, _i32, _vp, _i64, _vp, _sz, _vp],
     "olsgd_operators_join": [_vp],
     "olsgd_clip_grads": [_vp, _i32, _i32, C.c_float, _vp, _vp, _sz, _vp],
 }
@@ -249,13 +252,50 @@ def gated_backward(d_h, x, w_gate, w_up, pre, activation="silu", want_d_x=True, 
     d_x = torch.empty((m, T, D), dtype=dtype, device=dev) if want_d_x else None
     d_wg = d_wu = None
     if want_d_w:
-        new = torch.empty if T else torch.zeros   # no tokens: nothing is launched, and the gradients are zero
-        d_wg, d_wu = new(ws_shape, dtype=dtype, device=dev), new(ws_shape, dtype=dtype, device=dev)
+        d_wg, d_wu = torch.empty(ws_shape, dtype=dtype, device=dev), torch.empty(ws_shape, dtype=dtype, device=dev)
     ok = _aligned(a, (m, T)) and _aligned(b, ws_shape) and _aligned(c, ws_shape)
     ws, wp, wn = _workspace(dev, "olsgd_gated_workspace", m, T, D, F, 1, ok)
     _run(lib.olsgd_gated_backward, dev, m, T, D, F, code, act, *d, *a, *b, *c, pre.data_ptr(), d_x.data_ptr() if want_d_x else None,
          d_wg.data_ptr() if want_d_w else None, d_wu.data_ptr() if want_d_w else None, wp, wn)
     return d_x, d_wg, d_wu
+
+
+# --------------------------------------------------------------------------------- embedding
+
+def embedding_forward(table, ids, scale=1.0):
+    """olsgd_embedding_forward: scale * table[i, ids[i]] for each worker i.  table [m][V][D], rows contiguous; ids int32 [m][T],
+    those outside [0, V) give rows of zeros.  Returns [m][T][D] of the table's type."""
+    lib = _ops()
+    _need(table.is_cuda and table.dim() == 3 and ids.dim() == 2, "table must be a CUDA tensor [m][V][D], ids [m][T]")
+    code, dev = _dtype(table, "table"), table.device
+    m, V, D = table.shape
+    T = ids.shape[1]
+    _same_device(dev, ids=ids)
+    p, sw, sr = _matrix(table, "table", (m, V, D), table.dtype, dev)
+    out = torch.empty((m, T, D), dtype=table.dtype, device=dev)
+    _run(lib.olsgd_embedding_forward, dev, m, T, V, D, code, p, sw, sr, _per_row(ids, (m, T), torch.int32, "ids"), float(scale),
+         out.data_ptr())
+    return out
+
+
+def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
+    """olsgd_embedding_backward: the gradient of a table [m][vocab][D] from d_out [m][T][D] and the ids of the lookup; new, of
+    type `dtype`, or written to `out` (each worker's part contiguous, for example a view of a flat gradient [m][P])."""
+    lib = _ops()
+    _need(d_out.is_cuda and d_out.dim() == 3, "d_out must be a CUDA tensor [m][T][D]")
+    code, dev = _dtype(d_out, "d_out"), d_out.device
+    m, T, D = d_out.shape
+    V = int(vocab)
+    _same_device(dev, ids=ids, out=out)
+    p, sw, sr = _matrix(d_out, "d_out", (m, T, D), d_out.dtype, dev)
+    if out is None:
+        out = torch.empty((m, V, D), dtype=dtype, device=dev)
+    _need(out.shape == (m, V, D), "out must be of shape %s", (m, V, D))
+    _, ow = _worker_rows(out, m, "out")
+    ip = _per_row(ids, (m, T), torch.int32, "ids")
+    ws, wp, wn = _workspace(dev, "olsgd_embedding_workspace", m, T, D)
+    _run(lib.olsgd_embedding_backward, dev, m, T, V, D, code, p, sw, sr, ip, float(scale), _dtype(out, "out"), out.data_ptr(), ow, wp, wn)
+    return out
 
 
 def operators_join(device="cuda"):

@@ -487,3 +487,109 @@ def test_gated_parts_empty_batches_and_refusals():
             bad()
     with pytest.raises(lib.OlsgdError):   # workers on top of each other
         lib.gated_forward(x[:1].expand(2, 9, 40), wg, wu)
+
+
+# -------------------------------------------------------------------------------- embedding
+
+def _check_embedding(table, ids, dout, scale, out_dtype, out=None):
+    m, V, D = table.shape
+    dtype = table.dtype
+    scale32 = float(np.float32(scale))
+    has = ((ids >= 0) & (ids < V))[..., None]
+    at = torch.where(has[..., 0], ids, torch.zeros_like(ids)).long()
+    rows = torch.stack([table[i][at[i]] for i in range(m)]).double() * scale32
+    want = torch.where(has, rows, torch.zeros_like(rows))
+    got = lib.embedding_forward(table, ids, scale)
+    tiny = 2.0 ** -24 if dtype == torch.float16 else 2.0 ** -126
+    assert bool(((got.double() - want).abs() <= want.abs() * (torch.finfo(dtype).eps / 2 + U) + tiny).all())
+    if dout is None:
+        return
+    d = lib.embedding_backward(dout, ids, V, scale, dtype=out_dtype, out=out)
+    E = torch.where(has, dout.double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+    want = torch.stack([torch.zeros((V, D), dtype=torch.float64, device="cuda").index_add_(0, at[i], E[i]) for i in range(m)]) * scale32
+    size = torch.stack([torch.zeros((V, D), dtype=torch.float64, device="cuda").index_add_(0, at[i], E[i].abs()) for i in range(m)]) * abs(scale32)
+    n = torch.stack([torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, at[i], has[i, :, 0].double()) for i in range(m)])
+    # a chain of at most 32 additions in a chunk, an eighth of the chunks in a warp, the join, the scale
+    chain = torch.clamp(n, max=32) + n / 256 + 12
+    tiny = 2.0 ** -24 if out_dtype == torch.float16 else 2.0 ** -126
+    tol = size * chain[..., None] * U + want.abs() * (torch.finfo(out_dtype).eps / 2 + 2 * U) + tiny
+    err = (d.double() - want).abs()
+    assert bool((err <= tol).all()), float((err - tol).max())
+    assert not bool(d[n == 0].any())
+    assert torch.equal(d, lib.embedding_backward(dout, ids, V, scale, dtype=out_dtype))   # the same bits again
+    return d
+
+
+@pytest.mark.parametrize("tin,tout", [(torch.float32, torch.float32), (torch.bfloat16, torch.float32), (torch.float16, torch.float32),
+                                      (torch.bfloat16, torch.bfloat16), (torch.float16, torch.float16), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("m,T,V,D", [(1, 1, 1, 1), (2, 5, 3, 7), (1, 31, 255, 8), (3, 33, 256, 24), (1, 2048, 1000, 16), (2, 2049, 70000, 9),
+                                     (1, 4500, 50, 1032), (2, 700, 300, 2050), (1, 64, 5, 4096)])
+def test_embedding(m, T, V, D, tin, tout):
+    g = _gen(T + V + D)
+    table, dout = _randn(g, (m, V, D), tin), _randn(g, (m, T, D), tin)
+    ids = torch.randint(-1, V + 1, (m, T), generator=g, device="cuda", dtype=torch.int32)   # -1 and V: no token
+    _check_embedding(table, ids, dout, 1.7, tout)
+
+
+@pytest.mark.parametrize("pattern", ["all one", "all missing", "two", "rising", "zipf", "last", "runs of a chunk"])
+@pytest.mark.parametrize("D", [72, 13])
+def test_embedding_patterns(pattern, D):
+    g = _gen(D)
+    m, T, V = 2, 9001, 3000
+    if pattern == "all one":
+        ids = torch.full((m, T), 17, device="cuda")
+    elif pattern == "all missing":
+        ids = torch.full((m, T), -5, device="cuda")
+    elif pattern == "two":
+        ids = torch.randint(0, 2, (m, T), generator=g, device="cuda") * (V - 1)
+    elif pattern == "rising":
+        ids = torch.arange(T, device="cuda").repeat(m, 1) % V
+    elif pattern == "zipf":
+        ids = (V ** torch.rand((m, T), generator=g, device="cuda")).long().clamp(max=V - 1)
+    elif pattern == "last":
+        ids = torch.full((m, T), V - 1, device="cuda")
+        ids[:, 5] = 2 ** 31 - 1
+    else:   # rows that begin and end on the borders of the chunks of 32
+        ids = (torch.arange(T, device="cuda") // 32).repeat(m, 1)
+    ids = ids.to(torch.int32).contiguous()
+    _check_embedding(_randn(g, (m, V, D), torch.bfloat16), ids, _randn(g, (m, T, D), torch.bfloat16), 0.5, torch.float32)
+
+
+def test_embedding_sort_is_stable():
+    """Sums of a row are formed in the order of its positions: values that only that order adds up to zero."""
+    T = 5000
+    ids = torch.full((1, T), 9, dtype=torch.int32, device="cuda")
+    ids[0, ::7] = 3
+    dout = torch.zeros((1, T, 8), device="cuda")
+    at = [i for i in range(T) if i % 7][:3]
+    dout[0, at[0]], dout[0, at[1]], dout[0, at[2]] = 1e8, 1.0, -1e8
+    d = lib.embedding_backward(dout, ids, 10)
+    assert bool((d[0, 9] == np.float32(1e8) + np.float32(1.0) - np.float32(1e8)).all())
+
+
+def test_embedding_of_strided_tensors_into_a_flat_gradient():
+    g = _gen(12)
+    m, T, V, D = 2, 300, 120, 40
+    P = V * D + 100
+    for offset, pad in ((4, 8), (3, 1)):
+        table = _randn(g, (m, V + 2, D + pad), torch.bfloat16)[:, 1:V + 1, :D]
+        dout = _randn(g, (m, T + 3, D + pad), torch.bfloat16)[:, 3:, :D]
+        ids = torch.randint(0, V, (m, T), generator=g, device="cuda", dtype=torch.int32)
+        flat = torch.full((m, P), -7.0, device="cuda")
+        out = flat[:, offset:offset + V * D].unflatten(1, (V, D))
+        d = _check_embedding(table, ids, dout, 2.0, torch.float32, out=out)
+        assert d is out and bool((flat[:, :offset] == -7).all()) and bool((flat[:, offset + V * D:] == -7).all())
+
+
+def test_embedding_empty_batches_and_refusals():
+    g = _gen(13)
+    table, ids = _randn(g, (2, 9, 16)), torch.zeros((2, 4), dtype=torch.int32, device="cuda")
+    assert lib.embedding_forward(table, ids[:, :0].contiguous()).shape == (2, 0, 16)
+    d = lib.embedding_backward(torch.empty((2, 0, 16), device="cuda"), ids[:, :0].contiguous(), 9)
+    assert d.shape == (2, 9, 16) and not bool(d.any())
+    for bad in (lambda: lib.embedding_forward(table, ids.long()), lambda: lib.embedding_forward(table, ids[:1]), lambda: lib.embedding_forward(table, ids[:, ::2]),
+                lambda: lib.embedding_forward(table.mT, ids), lambda: lib.embedding_forward(table.cpu(), ids),
+                lambda: lib.embedding_forward(table, ids.cpu()), lambda: lib.embedding_forward(table.double(), ids),
+                lambda: lib.embedding_backward(table, ids, 9), lambda: lib.embedding_backward(table[:, :4], ids, 9, out=table[:, :8])):
+        with pytest.raises(ValueError):
+            bad()
