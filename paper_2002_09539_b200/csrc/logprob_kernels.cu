@@ -3,8 +3,8 @@
 // For a row x of V logits, m = max x, S = sum exp(x - m):
 //   log p_j = (x_j - m) - log S,   H = log S - (1/S) sum exp(x_j - m) (x_j - m).
 // One pass keeps a running maximum and, relative to it, s = sum e^d and t = sum e^d d
-// (d = x - m, in units of log2): when the maximum rises from m to m', both are carried over
-// by s' = s f, t' = (t + s delta) f with delta = (m - m') log2 e, f = 2^delta.  The
+// (d = x - m): when the maximum rises from m to m', both are carried over by s' = s f,
+// t' = (t + s delta) f with delta = m - m', f = e^delta.  The
 // difference x - m is formed before it is scaled, so rows of the type's lowest value, or far
 // from zero, keep their probabilities.  All of it is held in fp32.
 //
@@ -34,25 +34,46 @@ static_assert(kMaxTop == 32, "a lane holds one candidate of each warp");
 constexpr int kMaxSplit = 64;
 
 struct RowState {
-  float m, s, t;   // running maximum; sums relative to it (t in log2 units)
+  float m, s, t;   // running maximum; sums relative to it
 };
 
-// e^(x - m) and its product with the exponent.  The clamp keeps 0 * -inf out of t (e is zero
-// long before); a NaN stays in e and reaches both sums.
+// Differences are clamped here: e^d is zero long before, and 0 * -inf stays out of t.
+constexpr float kFarBelow = -1.0e9f;
+
+// e^(x - m) and its product with the exponent; a NaN reaches both sums.
 __device__ __forceinline__ void accumulate(float x, float base, float& s, float& t) {
-  const float d = (x - base) * kLog2e;
-  const float e = ex2(d);
+  const float d = max_nan(x - base, kFarBelow);
+  const float e = ex2(d * kLog2e);
   s += e;
-  t = fmaf(e, fmaxf(d, -1000.f), t);
+  t = fmaf(e, d, t);
+}
+// The same for two elements at a time.
+__device__ __forceinline__ void accumulate2(f32x2 x, f32x2 minus_base, f32x2& s, f32x2& t) {
+  float lo, hi;
+  unpack2f(add2(x, minus_base), lo, hi);
+  lo = max_nan(lo, kFarBelow);
+  hi = max_nan(hi, kFarBelow);
+  const f32x2 d = pack2f(lo, hi);
+  unpack2f(mul2(d, pack2f(kLog2e, kLog2e)), lo, hi);
+  const f32x2 e = pack2f(ex2(lo), ex2(hi));
+  s = add2(s, e);
+  t = fma2(e, d, t);
 }
 
 // Carries (s, t) from maximum `from` to the larger maximum `to`.
 __device__ __forceinline__ void rebase(float from, float to, float& s, float& t) {
   if (from == -INFINITY) return;   // nothing but zeros (or a NaN) so far
-  const float delta = fmaxf((from - to) * kLog2e, -1000.f);
-  const float f = ex2(delta);
+  const float delta = fmaxf(from - to, kFarBelow);
+  const float f = ex2(delta * kLog2e);
   t = fmaf(s, delta, t) * f;
   s *= f;
+}
+__device__ __forceinline__ void rebase2(float from, float to, f32x2& s, f32x2& t) {
+  if (from == -INFINITY) return;
+  const float delta = fmaxf(from - to, kFarBelow);
+  const float f = ex2(delta * kLog2e);
+  t = mul2(fma2(s, pack2f(delta, delta), t), pack2f(f, f));
+  s = mul2(s, pack2f(f, f));
 }
 
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
@@ -140,7 +161,7 @@ __device__ __forceinline__ void write_row(const RowOut& o, const T* row, int64_t
   const float log_s = log_sum(v);
   const int32_t t = o.targets[r];
   const bool empty = v.m == -INFINITY && v.s == 0.f;
-  float h = empty ? 0.f : log_s - 0.6931471805599453f * (v.t / v.s);
+  float h = empty ? 0.f : log_s - v.t / v.s;
   if (h < 0.f) h = 0.f;   // rounding of a row that is certain; a NaN stays
   o.entropy[r] = h;
   o.stats[2 * r] = v.m;
@@ -202,10 +223,18 @@ logprob_warp_kernel(const T* __restrict__ x, int64_t rows, int V, int64_t ld, Ro
 }
 
 // -------------------------------------------------------------------------- long rows
-// CTA (r, split): chunks [split * cps, (split + 1) * cps) of row r, dealt to the warps in turn.
+template <typename T>
+__host__ __device__ constexpr uint32_t minus_inf() {
+  return sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
+}
+
+// CTA (r, split): chunks [split * cps, (split + 1) * cps) of row r, dealt to the warps in turn;
+// a warp's next turn is loaded while the present one is added up.  Per element the loop spends
+// about six instructions (packed fp32 for the difference, the product and both sums; the
+// maximum in the element's own type).
 template <typename T, bool TOP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads)
-logprob_row_kernel(const T* __restrict__ x, int64_t V, int64_t ld, int nchunks, int cps, RowOut o,
+logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int cps, RowOut o,
                    float4* __restrict__ part, uint32_t* __restrict__ chunk_max) {
   constexpr int VEC = Elem<T>::kVec;
   constexpr int U = kUnrollChunks;
@@ -216,54 +245,55 @@ logprob_row_kernel(const T* __restrict__ x, int64_t V, int64_t ld, int nchunks, 
   const int shift = row_shift(row);
   const int c_begin = blockIdx.y * cps, c_end = min(nchunks, c_begin + cps);
 
-  RowState st{-INFINITY, 0.f, 0.f};
-  for (int c0 = c_begin + warp; c0 < c_end; c0 += kWarps * U) {
-    float v[U][VEC];
+  float m = -INFINITY;
+  f32x2 s = 0, t = 0;
+  uint4 next[U];
+  auto load = [&](int c0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + u * kWarps;
-      if (c < c_end) {
-        load_piece<T>(row, ((int64_t)c * 32 + lane) * VEC - shift, V, -INFINITY, v[u]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[u][e] = -INFINITY;
-      }
+      // (a chunk past the end reads as elements past the row's end)
+      next[u] = load_raw<T>(row, c < c_end ? (c * 32 + lane) * VEC - shift : V, V, minus_inf<T>());
     }
-    float mx = st.m;
+  };
+  load(c_begin + warp);
+  for (int c0 = c_begin + warp; c0 < c_end; c0 += kWarps * U) {
+    uint4 now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = next[u];
+    if (c0 + kWarps * U < c_end) load(c0 + kWarps * U);
+    float mx = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float cm = v[u][0];
+      float cm = raw_max<T, TOP>(now[u]);
       if (TOP) {
-#pragma unroll
-        for (int e = 1; e < VEC; ++e) cm = max_nan(cm, v[u][e]);
         // over the warp as an ordered integer, in which a NaN comes first
         const uint32_t order = __reduce_max_sync(0xffffffffu, order_of(cm));
         const int c = c0 + u * kWarps;
         if (lane == 0 && c < c_end) chunk_max[r * nchunks + c] = order;
         cm = value_of(order);   // (a NaN does not move the running maximum)
-      } else {
-#pragma unroll
-        for (int e = 1; e < VEC; ++e) cm = fmaxf(cm, v[u][e]);
       }
       mx = fmaxf(mx, cm);
     }
-    if (!TOP) {
-      float w;
-      asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(w) : "f"(mx));
-      mx = w;
+    if (!TOP) asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(mx) : "f"(mx));
+    if (mx > m) {
+      rebase2(m, mx, s, t);
+      m = mx;
     }
-    if (mx > st.m) {
-      rebase(st.m, mx, st.s, st.t);
-      st.m = mx;
-    }
-    const float base = base_of(st.m);
+    const float base = -base_of(m);
+    const f32x2 minus_base = pack2f(base, base);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) accumulate(v[u][e], base, st.s, st.t);
+      for (int i = 0; i < VEC / 2; ++i) accumulate2(raw_pair<T>(now[u], i), minus_base, s, t);
   }
-  st.s = warp_sum(st.s);
-  st.t = warp_sum(st.t);
+  RowState st;
+  float lo, hi;
+  st.m = m;
+  unpack2f(s, lo, hi);
+  st.s = warp_sum(lo + hi);
+  unpack2f(t, lo, hi);
+  st.t = warp_sum(lo + hi);
   __shared__ RowState sh[kWarps];
   if (lane == 0) sh[warp] = st;
   __syncthreads();
@@ -279,145 +309,205 @@ logprob_row_kernel(const T* __restrict__ x, int64_t V, int64_t ld, int nchunks, 
 }
 
 // Joins a row's parts and finds its alternatives; one CTA per row.
+//
+// Both selections (the k best chunks, the k best elements of those) go by a floor: a value
+// that k candidates reach.  What is below it is dropped, which leaves little more than k
+// keys in a list, and each of those counts how many are larger: its place in the order.  Rows in
+// which very many elements tie can overflow the list; they take k rounds of a maximum instead.
+constexpr int kList = 1024;
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-logprob_finish_kernel(const T* __restrict__ x, int64_t V, int64_t ld, int nchunks, int nsplit, RowOut o,
+logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int nsplit, RowOut o,
                       const float4* __restrict__ part, const uint32_t* __restrict__ chunk_max, int top,
                       float* __restrict__ top_logp, int32_t* __restrict__ top_ids) {
   constexpr int VEC = Elem<T>::kVec;
-  __shared__ uint64_t cand[kWarps * kMaxTop];
+  constexpr int kGroups = 64;   // of four threads
+  static_assert(kGroups >= kMaxTop && kGroups * 4 == kThreads, "the k-th best group gives the floor");
+  __shared__ uint64_t group_best[kGroups];
+  __shared__ uint64_t list[kList];
   __shared__ int32_t chosen[kMaxTop];
-  __shared__ uint64_t found[kMaxTop * kMaxTop];
-  __shared__ int n_found, n_chosen;
-  __shared__ uint32_t threshold;
+  __shared__ uint64_t floor_key;
+  __shared__ int n_list[2], n_chosen;
+  __shared__ RowState whole;
   launch_gate();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t r = blockIdx.x;
   const T* row = x + r * ld;
   const int shift = row_shift(row);
 
-  RowState st{-INFINITY, 0.f, 0.f};
-  if (warp == 0) {
+  if (warp == kWarps - 1) {
+    RowState st{-INFINITY, 0.f, 0.f};
     for (int i = lane; i < nsplit; i += 32) {
       const float4 p = part[r * nsplit + i];
       st = join(st, RowState{p.x, p.y, p.z});
     }
     st = shfl_join(st);
-    if (lane == 0) write_row<T>(o, row, r, V, st);
+    if (lane == 0) {
+      write_row<T>(o, row, r, V, st);
+      whole = st;
+    }
   }
   if (top == 0) return;
-  // 1. each warp: the best chunks of its share; then warp 0: the best of those
-  if (threadIdx.x == 0) n_found = 0;
+
+  // 1. the best chunks
   const uint32_t* cm = chunk_max + r * nchunks;
-  {
-    int got = warp_select(
-        top, 0,
-        [&](uint64_t limit) {
-          uint64_t b = 0;
-          for (int c = warp * 32 + lane; c < nchunks; c += kThreads) {
-            const uint64_t key = key_of(cm[c], c);
-            if (key < limit && key > b) b = key;
-          }
-          return b;
-        },
-        [&](int q, uint64_t key) { cand[warp * kMaxTop + q] = key; });
-    for (int q = got + lane; q < kMaxTop; q += 32) cand[warp * kMaxTop + q] = 0;
+  uint64_t best = 0;
+  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
+    const uint64_t key = key_of(cm[c], c);
+    best = key > best ? key : best;
+  }
+#pragma unroll
+  for (int off = 1; off < 4; off <<= 1) {
+    const uint64_t other = __shfl_xor_sync(0xffffffffu, best, off);
+    best = other > best ? other : best;
+  }
+  if ((threadIdx.x & 3) == 0) group_best[threadIdx.x >> 2] = best;
+  if (threadIdx.x == 0) {
+    n_list[0] = n_list[1] = 0;
+    n_chosen = min(top, nchunks);
+    floor_key = 1;   // fewer groups than k: every chunk is a candidate
   }
   __syncthreads();
-  if (warp == 0) {
-    uint64_t last = 0;
-    const int got = warp_select(
+  if (threadIdx.x < kGroups) {
+    const uint64_t mine = group_best[threadIdx.x];
+    int larger = 0;
+    for (int i = 0; i < kGroups; ++i) larger += group_best[i] > mine;
+    if (mine && larger == top - 1) floor_key = mine;
+  }
+  __syncthreads();
+  const uint64_t chunk_floor = floor_key;
+  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
+    const uint64_t key = key_of(cm[c], c);
+    if (key >= chunk_floor) {
+      const int at = atomicAdd(&n_list[0], 1);
+      if (at < kList) list[at] = key;
+    }
+  }
+  __syncthreads();
+  const int n0 = n_list[0];
+  if (threadIdx.x == 0) floor_key = 0;   // (every thread has read chunk_floor)
+  __syncthreads();
+  // chosen chunks in any order; the floor for their elements is the k-th one's maximum
+  if (n0 <= kList) {
+    for (int i = threadIdx.x; i < n0; i += kThreads) {
+      const uint64_t mine = list[i];
+      int larger = 0;
+      for (int q = 0; q < n0; ++q) larger += list[q] > mine;
+      if (larger < top) chosen[larger] = index_of(mine);
+      if (larger == top - 1) floor_key = mine & 0xFFFFFFFF00000000ull;
+    }
+  } else if (warp == 0) {
+    warp_select(
         top, 0,
         [&](uint64_t limit) {
           uint64_t b = 0;
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) {
-            const uint64_t key = cand[w * kMaxTop + lane];
+          for (int c = lane; c < nchunks; c += 32) {
+            const uint64_t key = key_of(cm[c], c);
             if (key < limit && key > b) b = key;
           }
           return b;
         },
         [&](int q, uint64_t key) {
           chosen[q] = index_of(key);
-          last = key;
+          if (q == top - 1) floor_key = key & 0xFFFFFFFF00000000ull;
         });
-    if (lane == 0) {
-      n_chosen = got;
-      // with k chunks chosen, k elements are at least as large as the last one's maximum
-      threshold = got == top ? (uint32_t)(last >> 32) : 0u;
+  }
+  __syncthreads();
+
+  // 2. the elements of the chosen chunks that reach the floor
+  const uint64_t elem_floor = floor_key;
+  const int nc = n_chosen;
+  for (int i = warp; i < nc; i += kWarps) {
+    const int j0 = (chosen[i] * 32 + lane) * VEC - shift;
+    const uint4 w = load_raw<T>(row, j0, V, minus_inf<T>());
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float v, other;
+      unpack2f(raw_pair<T>(w, e / 2), v, other);
+      const uint64_t key = key_of(order_of(e % 2 ? other : v), j0 + e);
+      if (key >= elem_floor && j0 + e >= 0 && j0 + e < V) {
+        const int at = atomicAdd(&n_list[1], 1);
+        if (at < kList) list[at] = key;
+      }
     }
   }
   __syncthreads();
-  // 2. the elements of the chosen chunks that can be among the k largest
-  const uint64_t floor_key = (uint64_t)threshold << 32;
-  for (int i = warp; i < n_chosen; i += kWarps) {
-    const int64_t j0 = ((int64_t)chosen[i] * 32 + lane) * VEC - shift;
-    float v[VEC];
-    load_piece<T>(row, j0, V, -INFINITY, v);
-    warp_select(
-        top, floor_key,
-        [&](uint64_t limit) {
-          uint64_t b = 0;
+  int n1 = n_list[1];
+  if (n1 > kList) {
+    // too many ties: the first k of each chosen chunk, by rounds
+    __syncthreads();
+    if (threadIdx.x == 0) n_list[1] = 0;
+    __syncthreads();
+    for (int i = warp; i < nc; i += kWarps) {
+      const int j0 = (chosen[i] * 32 + lane) * VEC - shift;
+      float v[VEC];
+      load_piece<T>(row, j0, V, -INFINITY, v);
+      warp_select(
+          top, elem_floor,
+          [&](uint64_t limit) {
+            uint64_t b = 0;
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const int64_t j = j0 + e;
-            const uint64_t key = key_of(order_of(v[e]), j);
-            if (j >= 0 && j < V && key < limit && key > b) b = key;
-          }
-          return b;
-        },
-        [&](int, uint64_t key) { found[atomicAdd(&n_found, 1)] = key; });
+            for (int e = 0; e < VEC; ++e) {
+              const uint64_t key = key_of(order_of(v[e]), j0 + e);
+              if (j0 + e >= 0 && j0 + e < V && key < limit && key > b) b = key;
+            }
+            return b;
+          },
+          [&](int, uint64_t key) { list[atomicAdd(&n_list[1], 1)] = key; });
+    }
+    __syncthreads();
+    n1 = n_list[1];
   }
-  __syncthreads();
-  // 3. the k largest of those, in order (the list's own order does not matter: keys differ)
-  if (warp == 0) {
-    const float log_s = log_sum(st);
-    const int n = n_found;
-    warp_select(
-        top, 0,
-        [&](uint64_t limit) {
-          uint64_t b = 0;
-          for (int i = lane; i < n; i += 32) {
-            const uint64_t key = found[i];
-            if (key < limit && key > b) b = key;
-          }
-          return b;
-        },
-        [&](int q, uint64_t key) {
-          top_ids[r * top + q] = index_of(key);
-          top_logp[r * top + q] = log_prob(value_of((uint32_t)(key >> 32)), st, log_s);
-        });
+  // each takes its place (the list's own order does not matter: keys differ)
+  const RowState st = whole;
+  const float log_s = log_sum(st);
+  for (int i = threadIdx.x; i < n1; i += kThreads) {
+    const uint64_t mine = list[i];
+    int larger = 0;
+    for (int q = 0; q < n1; ++q) larger += list[q] > mine;
+    if (larger < top) {
+      top_ids[r * top + larger] = index_of(mine);
+      top_logp[r * top + larger] = log_prob(value_of((uint32_t)(mine >> 32)), st, log_s);
+    }
   }
 }
+static_assert(kMaxTop * kMaxTop <= kList, "k of each of k chunks");
 
 // ---------------------------------------------------------------------------- gradient
 // dx_j = dlp (1[j = t] - p_j) - dH p_j (log p_j + H): reads the logits once, writes once.
+// With y = x - m (clamped far below, where p is zero): p = 2^(y log2 e - log2 S) and
+// dx = -p (dH y + K), K = dlp + dH (H - log S).  A row with a NaN or +inf has log S = NaN.
 struct GradRow {
-  float base, log_s, d_lp, d_h, h;
+  float base, minus_log2_s, d_h, k, d_lp;
   int32_t target;
   bool empty;
-  __device__ __forceinline__ float operator()(float x, int64_t j) const {
-    if (empty) return 0.f;
-    const float lp = fmaxf((x - base) - log_s, -1.0e4f);   // p is zero there; a NaN is put back below
-    const float p = ex2(((x - base) - log_s) * kLog2e);
-    float d = -p * fmaf(d_h, lp + h, d_lp);
-    if (j == target) d += d_lp;
-    return d;
+  __device__ __forceinline__ float operator()(float x) const {
+    const float y = fmaxf(x - base, kFarBelow);
+    return -ex2(fmaf(y, kLog2e, minus_log2_s)) * fmaf(d_h, y, k);
+  }
+  __device__ __forceinline__ void pair(f32x2 x, float& lo, float& hi) const {
+    unpack2f(add2(x, pack2f(-base, -base)), lo, hi);
+    const f32x2 y = pack2f(fmaxf(lo, kFarBelow), fmaxf(hi, kFarBelow));
+    unpack2f(fma2(y, pack2f(kLog2e, kLog2e), pack2f(minus_log2_s, minus_log2_s)), lo, hi);
+    const f32x2 p = pack2f(ex2(lo), ex2(hi));
+    unpack2f(mul2(p, fma2(pack2f(-d_h, -d_h), y, pack2f(-k, -k))), lo, hi);
   }
 };
 
 __device__ __forceinline__ GradRow grad_row(const LogprobGradArgs& a, int64_t r) {
   GradRow g;
-  const float m = a.stats[2 * r];
-  g.log_s = a.stats[2 * r + 1];
-  g.empty = m == -INFINITY && g.log_s == 0.f;
+  const float m = a.stats[2 * r], log_s = a.stats[2 * r + 1];
+  g.empty = m == -INFINITY && log_s == 0.f;
   g.base = base_of(m);
+  g.minus_log2_s = -log_s * kLog2e;
   const int32_t t = a.targets[r];
   const bool has = t >= 0 && t < a.V;
   g.target = has ? t : -1;
   g.d_lp = has && a.d_logp ? a.d_logp[r] : 0.f;
   g.d_h = a.d_entropy ? a.d_entropy[r] : 0.f;
-  g.h = a.entropy[r];
+  g.k = fmaf(g.d_h, a.entropy[r] - log_s, g.d_lp);
+  if (g.empty) g.d_h = g.k = g.d_lp = 0.f;   // p times zero
   return g;
 }
 
@@ -430,7 +520,8 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_warp_kernel(LogprobGrad
   const T* row = static_cast<const T*>(a.logits) + r * a.ld;
   T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
   const GradRow g = grad_row(a, r);
-  for (int64_t j = lane; j < a.V; j += 32) out[j] = Elem<T>::from_float(g(Elem<T>::to_float(row[j]), j));
+  for (int j = lane; j < (int)a.V; j += 32)
+    out[j] = Elem<T>::from_float(g(Elem<T>::to_float(row[j])) + (j == g.target ? g.d_lp : 0.f));
 }
 
 // CTA (r, segment): kThreads * kUnrollChunks pieces of row r.
@@ -440,22 +531,29 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(LogprobGradArgs 
   constexpr int U = kUnrollChunks;
   launch_gate();
   const int64_t r = blockIdx.x;
+  const int V = (int)a.V;
   const T* row = static_cast<const T*>(a.logits) + r * a.ld;
   T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
   const int shift = row_shift(row);
   const bool aligned = row_shift(out) == shift;
-  const GradRow g = grad_row(a, r);
-  const int64_t q0 = (int64_t)blockIdx.y * (kThreads * U) + threadIdx.x;
-  float v[U][VEC];
+  const int j0 = ((int)blockIdx.y * (kThreads * U) + (int)threadIdx.x) * VEC - shift;
+  uint4 w[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) load_piece<T>(row, (q0 + u * kThreads) * VEC - shift, a.V, 0.f, v[u]);
+  for (int u = 0; u < U; ++u) w[u] = load_raw<T>(row, j0 + u * kThreads * VEC, V, 0);
+  const GradRow g = grad_row(a, r);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t j = (q0 + u * kThreads) * VEC - shift;
+    const int j = j0 + u * kThreads * VEC;
+    if (j >= V) break;
     float d[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) d[e] = g(v[u][e], j + e);
-    store_floats<T, VEC>(out, j, a.V, aligned, d);
+    for (int i = 0; i < VEC / 2; ++i) g.pair(raw_pair<T>(w[u], i), d[2 * i], d[2 * i + 1]);
+    if (g.target >= j && g.target < j + VEC) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (j + e == g.target) d[e] += g.d_lp;
+    }
+    store_floats<T, VEC>(out, j, V, aligned, d);
   }
 }
 
@@ -507,9 +605,9 @@ cudaError_t forward(const LogprobArgs& a, cudaStream_t s) {
   auto k = a.top > 0 ? logprob_row_kernel<T, true, false>
            : whole   ? logprob_row_kernel<T, false, true>
                      : logprob_row_kernel<T, false, false>;
-  const cudaError_t e = launch_chained(k, grid, dim3(kThreads), 0, s, x, a.V, a.ld, nchunks, cps, o, part, cmax);
+  const cudaError_t e = launch_chained(k, grid, dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks, cps, o, part, cmax);
   if (e != cudaSuccess || whole) return e;
-  return launch_chained(logprob_finish_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, x, a.V, a.ld, nchunks,
+  return launch_chained(logprob_finish_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks,
                         nsplit, o, (const float4*)part, (const uint32_t*)cmax, a.top, a.top_logp, a.top_ids);
 }
 

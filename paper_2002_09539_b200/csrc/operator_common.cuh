@@ -4,6 +4,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "olsgd_internal.h"
 
 namespace olsgd {
@@ -108,6 +110,16 @@ template <typename T, int N>
 __device__ __forceinline__ void store_floats(T* row, int64_t j, int64_t n, bool aligned, const float* v) {
   constexpr int V = Elem<T>::kVec;
   if (aligned && j >= 0 && j + N <= n) {
+    if constexpr (N * sizeof(T) == 32) {
+      // one 32-byte store (a whole sector) where the address allows it
+      if ((reinterpret_cast<uintptr_t>(row + j) & 31) == 0) {
+        const uint4 a = Elem<T>::pack(v), b = Elem<T>::pack(v + V);
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + j), "r"(a.x), "r"(a.y), "r"(a.z),
+                     "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                     : "memory");
+        return;
+      }
+    }
     if constexpr (N >= V) {
 #pragma unroll
       for (int q = 0; q < N / V; ++q) reinterpret_cast<uint4*>(row + j)[q] = Elem<T>::pack(v + q * V);
@@ -131,6 +143,89 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+
+// Two floats in one register pair: Blackwell's packed fp32 arithmetic.
+typedef uint64_t f32x2;
+__device__ __forceinline__ f32x2 pack2f(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2f(f32x2 v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// The piece that starts at element j as it lies in memory; elements outside [0, n) are `fill`
+// (the bits of one element).
+template <typename T>
+__device__ __forceinline__ uint4 load_raw(const T* row, int j, int n, uint32_t fill) {
+  constexpr int V = Elem<T>::kVec;
+  if (j >= 0 && j + V <= n) return ld16_stream(row + j);
+  uint32_t w[4];
+  if constexpr (V == 4) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (j + e >= 0 && j + e < n) ? reinterpret_cast<const uint32_t*>(row)[j + e] : fill;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = j + 2 * e;
+      const uint32_t lo = (k >= 0 && k < n) ? reinterpret_cast<const uint16_t*>(row)[k] : fill;
+      const uint32_t hi = (k + 1 >= 0 && k + 1 < n) ? reinterpret_cast<const uint16_t*>(row)[k + 1] : fill;
+      w[e] = lo | (hi << 16);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Elements 2 i and 2 i + 1 of a piece.
+template <typename T>
+__device__ __forceinline__ f32x2 raw_pair(const uint4& w, int i) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  if constexpr (sizeof(T) == 4) {
+    return pack2f(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+    return pack2f(f.x, f.y);
+  } else {
+    return pack2f(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
+  }
+}
+// The largest element of a piece; KEEP_NAN: NaN if there is one (else it is passed over).
+template <typename T, bool KEEP_NAN>
+__device__ __forceinline__ float raw_max(const uint4& w) {
+  if constexpr (sizeof(T) == 4) {
+    const float a = __uint_as_float(w.x), b = __uint_as_float(w.y), c = __uint_as_float(w.z), d = __uint_as_float(w.w);
+    if constexpr (KEEP_NAN) return max_nan(max_nan(a, b), max_nan(c, d));
+    else return fmaxf(fmaxf(a, b), fmaxf(c, d));
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const __half2* h = reinterpret_cast<const __half2*>(&w);
+    const __half2 m = KEEP_NAN ? __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]))
+                               : __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    const float2 f = __half22float2(m);
+    return KEEP_NAN ? max_nan(f.x, f.y) : fmaxf(f.x, f.y);
+  } else {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
+    const __nv_bfloat162 m = KEEP_NAN ? __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]))
+                                      : __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    const float2 f = __bfloat1622float2(m);
+    return KEEP_NAN ? max_nan(f.x, f.y) : fmaxf(f.x, f.y);
+  }
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
