@@ -8,8 +8,8 @@
 // difference x - m is formed before it is scaled, so rows of the type's lowest value, or far
 // from zero, keep their probabilities.  All of it is held in fp32.
 //
-// Alternatives: a warp reads 32 consecutive 16-byte pieces (a chunk) at a time and needs the
-// chunk's maximum for the running maximum anyway, so it also stores it.  The k largest
+// Alternatives: a warp reads 256 consecutive logits (a chunk) at a time and needs the chunk's
+// maximum for the running maximum anyway, so it also stores it.  The k largest
 // elements (ties to the lowest index) lie in the k chunks that come first by (maximum, lowest
 // index): if an element's chunk is not among them, each of those k chunks holds an element
 // that comes before it.  The finishing kernel therefore reads k chunks again and nothing else.
@@ -27,7 +27,8 @@ using namespace op;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kUnrollChunks = 4;      // 16-byte loads a lane has in flight
+constexpr int kUnroll = 4;            // 16-byte loads a lane has in flight
+constexpr int kChunkElems = 256;      // eight elements per lane: one 16-byte piece, or two of fp32
 constexpr int kWarpRowMax = 1024;     // longest row that stays in a warp's registers
 constexpr int kMaxTop = OLSGD_MAX_TOP;
 static_assert(kMaxTop == 32, "a lane holds one candidate of each warp");
@@ -155,19 +156,28 @@ __device__ __forceinline__ float log_prob(float x, const RowState& v, float log_
   return (v.m == -INFINITY && v.s == 0.f) ? -INFINITY : (x - base_of(v.m)) - log_s;
 }
 
+// The target's logit, fetched ahead of the sums: two dependent loads that nothing waits for then.
+struct Target {
+  float x;
+  bool has;
+};
 template <typename T>
-__device__ __forceinline__ void write_row(const RowOut& o, const T* row, int64_t r, int64_t V,
-                                          const RowState& v) {
-  const float log_s = log_sum(v);
+__device__ __forceinline__ Target fetch_target(const RowOut& o, const T* row, int64_t r, int64_t V) {
   const int32_t t = o.targets[r];
+  Target g;
+  g.has = t >= 0 && t < V;   // a target outside [0, V) marks a row without a token
+  g.x = g.has ? Elem<T>::to_float(row[t]) : 0.f;
+  return g;
+}
+__device__ __forceinline__ void write_row(const RowOut& o, const Target& g, int64_t r, const RowState& v) {
+  const float log_s = log_sum(v);
   const bool empty = v.m == -INFINITY && v.s == 0.f;
   float h = empty ? 0.f : log_s - v.t / v.s;
   if (h < 0.f) h = 0.f;   // rounding of a row that is certain; a NaN stays
   o.entropy[r] = h;
   o.stats[2 * r] = v.m;
   o.stats[2 * r + 1] = log_s;
-  // a target outside [0, V) marks a row without a token
-  o.logp[r] = (t >= 0 && t < V) ? log_prob(Elem<T>::to_float(row[t]), v, log_s) : 0.f;
+  o.logp[r] = g.has ? log_prob(g.x, v, log_s) : 0.f;
 }
 
 // ------------------------------------------------------------ rows in a warp's registers
@@ -180,6 +190,7 @@ logprob_warp_kernel(const T* __restrict__ x, int64_t rows, int V, int64_t ld, Ro
   const int64_t r = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (r >= rows) return;
   const T* row = x + r * ld;
+  const Target target = fetch_target<T>(o, row, r, V);
   float v[NL];
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
@@ -200,7 +211,7 @@ logprob_warp_kernel(const T* __restrict__ x, int64_t rows, int V, int64_t ld, Ro
   for (int i = 0; i < NL; ++i) accumulate(v[i], base, st.s, st.t);
   st.s = warp_sum(st.s);
   st.t = warp_sum(st.t);
-  if (lane == 0) write_row<T>(o, row, r, V, st);
+  if (lane == 0) write_row(o, target, r, st);
   if (top > 0) {
     const float log_s = log_sum(st);
     warp_select(
@@ -228,8 +239,8 @@ __host__ __device__ constexpr uint32_t minus_inf() {
   return sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
 }
 
-// CTA (r, split): chunks [split * cps, (split + 1) * cps) of row r, dealt to the warps in turn;
-// a warp's next turn is loaded while the present one is added up.  Per element the loop spends
+// CTA (r, split): chunks [split * cps, (split + 1) * cps) of row r, dealt to the warps in turn.
+// Per element the loop spends
 // about six instructions (packed fp32 for the difference, the product and both sums; the
 // maximum in the element's own type).
 template <typename T, bool TOP, bool WHOLE>
@@ -237,7 +248,8 @@ __global__ void __launch_bounds__(kThreads)
 logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int cps, RowOut o,
                    float4* __restrict__ part, uint32_t* __restrict__ chunk_max) {
   constexpr int VEC = Elem<T>::kVec;
-  constexpr int U = kUnrollChunks;
+  constexpr int Q = kChunkElems / 32 / VEC;   // pieces of a chunk per lane
+  constexpr int U = kUnroll / Q;              // chunks per turn
   launch_gate();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t r = blockIdx.x;
@@ -245,27 +257,39 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
   const int shift = row_shift(row);
   const int c_begin = blockIdx.y * cps, c_end = min(nchunks, c_begin + cps);
 
+  Target target{0.f, false};
+  if (WHOLE && threadIdx.x == 0) target = fetch_target<T>(o, row, r, V);
+
   float m = -INFINITY;
   f32x2 s = 0, t = 0;
-  uint4 next[U];
-  auto load = [&](int c0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = c0 + u * kWarps;
-      // (a chunk past the end reads as elements past the row's end)
-      next[u] = load_raw<T>(row, c < c_end ? (c * 32 + lane) * VEC - shift : V, V, minus_inf<T>());
-    }
-  };
-  load(c_begin + warp);
   for (int c0 = c_begin + warp; c0 < c_end; c0 += kWarps * U) {
-    uint4 now[U];
+    uint4 w[U][Q];
+    const int first = c0 * kChunkElems - shift, last = (c0 + (U - 1) * kWarps) * kChunkElems - shift;
+    if (first >= 0 && c0 + (U - 1) * kWarps < c_end && last + kChunkElems <= V) {
+      // every piece of this turn is whole: one address, constant distances
+      const uint4* p = reinterpret_cast<const uint4*>(row + first) + lane;
 #pragma unroll
-    for (int u = 0; u < U; ++u) now[u] = next[u];
-    if (c0 + kWarps * U < c_end) load(c0 + kWarps * U);
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) w[u][q] = ld16_stream(p + u * (kWarps * 32 * Q) + q * 32);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          const int c = c0 + u * kWarps;
+          // (a chunk past the end reads as elements past the row's end)
+          w[u][q] = load_raw<T>(row, c < c_end ? c * kChunkElems + (q * 32 + lane) * VEC - shift : V, V, minus_inf<T>());
+        }
+    }
     float mx = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float cm = raw_max<T, TOP>(now[u]);
+      float cm = raw_max<T, TOP>(w[u][0]);
+      if (Q == 2) {
+        const float other = raw_max<T, TOP>(w[u][Q - 1]);
+        cm = TOP ? max_nan(cm, other) : fmaxf(cm, other);
+      }
       if (TOP) {
         // over the warp as an ordered integer, in which a NaN comes first
         const uint32_t order = __reduce_max_sync(0xffffffffu, order_of(cm));
@@ -285,7 +309,9 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) accumulate2(raw_pair<T>(now[u], i), minus_base, s, t);
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) accumulate2(raw_pair<T>(w[u][q], i), minus_base, s, t);
   }
   RowState st;
   float lo, hi;
@@ -297,14 +323,14 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
   __shared__ RowState sh[kWarps];
   if (lane == 0) sh[warp] = st;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    RowState a = sh[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) a = join(a, sh[w]);
-    if (WHOLE)
-      write_row<T>(o, row, r, V, a);
-    else
-      part[r * gridDim.y + blockIdx.y] = make_float4(a.m, a.s, a.t, 0.f);
+  if (warp == 0) {
+    RowState a{-INFINITY, 0.f, 0.f};
+    if (lane < kWarps) a = sh[lane];
+    a = shfl_join(a);
+    if (lane == 0) {
+      if (WHOLE) write_row(o, target, r, a);
+      else part[r * gridDim.y + blockIdx.y] = make_float4(a.m, a.s, a.t, 0.f);
+    }
   }
 }
 
@@ -322,6 +348,7 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
                       const float4* __restrict__ part, const uint32_t* __restrict__ chunk_max, int top,
                       float* __restrict__ top_logp, int32_t* __restrict__ top_ids) {
   constexpr int VEC = Elem<T>::kVec;
+  constexpr int Q = kChunkElems / 32 / VEC;
   constexpr int kGroups = 64;   // of four threads
   static_assert(kGroups >= kMaxTop && kGroups * 4 == kThreads, "the k-th best group gives the floor");
   __shared__ uint64_t group_best[kGroups];
@@ -337,6 +364,7 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
   const int shift = row_shift(row);
 
   if (warp == kWarps - 1) {
+    const Target target = fetch_target<T>(o, row, r, V);
     RowState st{-INFINITY, 0.f, 0.f};
     for (int i = lane; i < nsplit; i += 32) {
       const float4 p = part[r * nsplit + i];
@@ -344,7 +372,7 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
     }
     st = shfl_join(st);
     if (lane == 0) {
-      write_row<T>(o, row, r, V, st);
+      write_row(o, target, r, st);
       whole = st;
     }
   }
@@ -419,16 +447,19 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
   const uint64_t elem_floor = floor_key;
   const int nc = n_chosen;
   for (int i = warp; i < nc; i += kWarps) {
-    const int j0 = (chosen[i] * 32 + lane) * VEC - shift;
-    const uint4 w = load_raw<T>(row, j0, V, minus_inf<T>());
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      float v, other;
-      unpack2f(raw_pair<T>(w, e / 2), v, other);
-      const uint64_t key = key_of(order_of(e % 2 ? other : v), j0 + e);
-      if (key >= elem_floor && j0 + e >= 0 && j0 + e < V) {
-        const int at = atomicAdd(&n_list[1], 1);
-        if (at < kList) list[at] = key;
+    for (int q = 0; q < Q; ++q) {
+      const int j0 = chosen[i] * kChunkElems + (q * 32 + lane) * VEC - shift;
+      const uint4 w = load_raw<T>(row, j0, V, minus_inf<T>());
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float v, other;
+        unpack2f(raw_pair<T>(w, e / 2), v, other);
+        const uint64_t key = key_of(order_of(e % 2 ? other : v), j0 + e);
+        if (key >= elem_floor && j0 + e >= 0 && j0 + e < V) {
+          const int at = atomicAdd(&n_list[1], 1);
+          if (at < kList) list[at] = key;
+        }
       }
     }
   }
@@ -440,18 +471,22 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
     if (threadIdx.x == 0) n_list[1] = 0;
     __syncthreads();
     for (int i = warp; i < nc; i += kWarps) {
-      const int j0 = (chosen[i] * 32 + lane) * VEC - shift;
-      float v[VEC];
-      load_piece<T>(row, j0, V, -INFINITY, v);
+      const int j0 = chosen[i] * kChunkElems + lane * VEC - shift;
+      float v[Q][VEC];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) load_piece<T>(row, j0 + q * 32 * VEC, V, -INFINITY, v[q]);
       warp_select(
           top, elem_floor,
           [&](uint64_t limit) {
             uint64_t b = 0;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-              const uint64_t key = key_of(order_of(v[e]), j0 + e);
-              if (j0 + e >= 0 && j0 + e < V && key < limit && key > b) b = key;
-            }
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) {
+                const int j = j0 + q * 32 * VEC + e;
+                const uint64_t key = key_of(order_of(v[q][e]), j);
+                if (j >= 0 && j < V && key < limit && key > b) b = key;
+              }
             return b;
           },
           [&](int, uint64_t key) { list[atomicAdd(&n_list[1], 1)] = key; });
@@ -524,11 +559,11 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_warp_kernel(LogprobGrad
     out[j] = Elem<T>::from_float(g(Elem<T>::to_float(row[j])) + (j == g.target ? g.d_lp : 0.f));
 }
 
-// CTA (r, segment): kThreads * kUnrollChunks pieces of row r.
+// CTA (r, segment): kThreads * kUnroll pieces of row r.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(LogprobGradArgs a) {
   constexpr int VEC = Elem<T>::kVec;
-  constexpr int U = kUnrollChunks;
+  constexpr int U = kUnroll;
   launch_gate();
   const int64_t r = blockIdx.x;
   const int V = (int)a.V;
@@ -558,18 +593,17 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(LogprobGradArgs 
 }
 
 // ------------------------------------------------------------------------------ host
-int chunk_elems(int dtype) { return 32 * (dtype == OLSGD_F32 ? 4 : 8); }
 // upper bound over every alignment of a row
 int64_t chunk_count(int64_t V, int dtype) {
-  const int64_t ce = chunk_elems(dtype);
-  return (V + ce / 32 - 1 + ce - 1) / ce;
+  return (V + (dtype == OLSGD_F32 ? 3 : 7) + kChunkElems - 1) / kChunkElems;
 }
 // Parts a row is split into.  One part per row once the rows alone give every multiprocessor
-// four CTAs; before that as many parts as fill the GPU that often, none shorter than one
-// unrolled turn of a CTA's warps (32 chunks).
+// four CTAs (1021 rows of 50021 fp32 logits: 45 us whole, 47 us in three parts); before that as
+// many parts as fill the GPU that often, none shorter than one unrolled turn of a CTA's
+// warps (32 chunks).
 int split_count(int64_t rows, int64_t nchunks) {
   const int64_t want = (4LL * 148 + rows - 1) / rows;
-  const int64_t most = (nchunks + kWarps * kUnrollChunks - 1) / (kWarps * kUnrollChunks);
+  const int64_t most = (nchunks + kWarps * kUnroll - 1) / (kWarps * kUnroll);
   int64_t n = want < most ? want : most;
   if (n > kMaxSplit) n = kMaxSplit;
   return n < 1 ? 1 : (int)n;
@@ -616,8 +650,10 @@ cudaError_t backward(const LogprobGradArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax)
     return launch_chained(logprob_grad_warp_kernel<T>, dim3((unsigned)((a.rows + kWarps - 1) / kWarps)), dim3(kThreads),
                           0, s, a);
-  const int64_t pieces = (a.V + 2 * Elem<T>::kVec - 2) / Elem<T>::kVec;
-  const int64_t per = kThreads * kUnrollChunks;
+  // rows that all start on a 16-byte boundary have no partial first piece
+  const bool on = ((reinterpret_cast<uintptr_t>(a.logits) | (uintptr_t)(a.ld * sizeof(T))) & 15) == 0;
+  const int64_t pieces = (a.V + (on ? 1 : 2) * (Elem<T>::kVec - 1)) / Elem<T>::kVec;
+  const int64_t per = kThreads * kUnroll;
   return launch_chained(logprob_grad_kernel<T>, dim3((unsigned)a.rows, (unsigned)((pieces + per - 1) / per)),
                         dim3(kThreads), 0, s, a);
 }

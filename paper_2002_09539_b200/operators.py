@@ -67,13 +67,21 @@ def _same_device(dev, **tensors):
         _need(t is None or t.device == dev, "%s must be on %s", name, dev)
 
 
+def _stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same number without the Stream object around it (2 us a call)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
+
+
 def _run(fn, dev, *args):
     """fn(*args, stream) on the tensors' device and its current stream."""
     if torch.cuda.current_device() == dev.index:
-        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+        st = fn(*args, _stream(dev.index))
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            st = fn(*args, _stream(dev.index))
     if st:
         _check(_ops(), st)
 
@@ -101,7 +109,7 @@ def _rows_of(t, name):
     _need(t.dim() >= 1 and t.is_cuda, "%s must be a CUDA tensor with at least one dimension", name)
     V = t.shape[-1]
     _need(V >= 1 and (t.stride(-1) == 1 or V == 1), "%s: the last dimension must be contiguous and not empty", name)
-    if t.dim() != 2:
+    if t.dim() != 2:   # (one launch takes rows at one distance)
         try:
             t = t.view(-1, V)
         except RuntimeError:
@@ -127,17 +135,17 @@ def token_logprobs(logits, targets, top=0):
     N, V = rows.shape
     top = int(top)
     _need(0 <= top <= min(V, MAX_TOP), "top must be in [0, min(V, %d)]", MAX_TOP)
-    logp = torch.empty(lead, dtype=torch.float32, device=dev)
-    entropy = torch.empty(lead, dtype=torch.float32, device=dev)
-    stats = torch.empty(lead + (2,), dtype=torch.float32, device=dev)
-    top_logp = top_ids = None
-    if top:
-        top_logp = torch.empty(lead + (top,), dtype=torch.float32, device=dev)
-        top_ids = torch.empty(lead + (top,), dtype=torch.int32, device=dev)
+    # the float outputs share one allocation: a small call is mostly the time that the host takes
+    out = torch.empty(N * (4 + top), dtype=torch.float32, device=dev)
+    logp, entropy, stats, top_logp = out.split((N, N, 2 * N, top * N))
+    top_ids = torch.empty(lead + (top,), dtype=torch.int32, device=dev) if top else None
     ws, wp, wn = _workspace(dev, "olsgd_token_logprobs_workspace", code, N, V, top)
-    _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, top, logp.data_ptr(), entropy.data_ptr(),
-         stats.data_ptr(), top_logp.data_ptr() if top else None, top_ids.data_ptr() if top else None, wp, wn)
-    return TokenLogprobs(logp, entropy, stats, top_logp, top_ids)
+    p = out.data_ptr()
+    _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N if top else None,
+         top_ids.data_ptr() if top else None, wp, wn)
+    if len(lead) != 1:
+        logp, entropy = logp.view(lead), entropy.view(lead)
+    return TokenLogprobs(logp, entropy, stats.view(lead + (2,)), top_logp.view(lead + (top,)) if top else None, top_ids)
 
 
 def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
