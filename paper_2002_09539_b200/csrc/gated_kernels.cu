@@ -18,9 +18,7 @@
 //             accumulation over 2 F, nothing transposed or concatenated in memory.
 //   DW        A = da or db, B = x, both read along their rows (MN-major), K = T.
 //
-// Tiles: 128 rows (256 by a pair) x 256 columns.  The pair halves the B bytes each SM
-// takes in and is used where there is more than one 128-row tile; where 256-column tiles
-// would leave multiprocessors idle (few tokens), tiles are 64 columns wide.
+// Tiles: 128 rows (256 by a pair) x 64, 128 or 256 columns, by shape_for below.
 //
 // TMA wants 16-byte row pitches: operands that do not have them are copied to padded rows in
 // the workspace first.  Every wait is bounded, as in the library's other tensor-core kernels.
@@ -49,12 +47,11 @@ struct GatedArgs {
   int problems;               // workers (DW: workers x 2)
   int rows, cols;             // extents of one problem's output (FORWARD: cols = F)
   int act, f16;
-  int out_vec;                // widest store the output's rows allow: 32, 16 or 2 bytes
+  bool out_vec;               // the output's rows are whole 16-byte pieces
   void* out0;                 // h, dx or dWg
   void* out1;                 // dWu
   void* pre;                  // FORWARD: a, b [m][T][2][Fp], or null
   int64_t pre_pitch;          // Fp
-  int pre_vec;                // widest store rows of pre allow: 32 or 16 bytes
 };
 
 template <int STAGES>
@@ -143,27 +140,45 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, int f16) {
   return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-// 16 results of one row, from column col on, of which those below `cols` exist.
-__device__ __forceinline__ void store16(void* row, int64_t col, int64_t cols, int vec, const float* v, int f16) {
-  uint32_t p[8];
+// A warp's block of 32 rows x W columns of results on its way out: TMEM hands every lane a row,
+// memory wants whole lines.  16-byte pieces, swizzled so that neither side meets bank conflicts
+// (W = 64).
+template <int W>
+struct Staged {
+  static constexpr int kPieces = W / 8;   // 16-byte pieces of a row
+  uint4* buf;
+  __device__ __forceinline__ static int at(int row, int piece) { return row * kPieces + (piece ^ (row & (kPieces - 1))); }
+  // 16 values of this lane's row, from column 16 q of the block on
+  __device__ __forceinline__ void put(int lane, int q, const float* v, int f16) {
+    uint32_t p[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) p[j] = pack2(v[2 * j], v[2 * j + 1], f16);
-  uint16_t* dst = static_cast<uint16_t*>(row) + col;
-  if (vec == 32 && col + 16 <= cols) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(p[0]), "r"(p[1]),
-                 "r"(p[2]), "r"(p[3]), "r"(p[4]), "r"(p[5]), "r"(p[6]), "r"(p[7])
-                 : "memory");
-  } else if (vec >= 16) {   // cols is a multiple of 8
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-      if (col + 8 * q < cols)
-        reinterpret_cast<uint4*>(dst)[q] = make_uint4(p[4 * q], p[4 * q + 1], p[4 * q + 2], p[4 * q + 3]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (col + j < cols) dst[j] = (uint16_t)(p[j >> 1] >> (16 * (j & 1)));
+    for (int j = 0; j < 8; ++j) p[j] = pack2(v[2 * j], v[2 * j + 1], f16);
+    buf[at(lane, 2 * q)] = make_uint4(p[0], p[1], p[2], p[3]);
+    buf[at(lane, 2 * q + 1)] = make_uint4(p[4], p[5], p[6], p[7]);
   }
-}
+  // The block to rows [0, rows) of dst (row pitch ld elements), of whose columns `cols` exist.
+  // vec: dst and ld are multiples of 16 bytes, cols of 8 elements.
+  __device__ __forceinline__ void flush(int lane, uint16_t* dst, int64_t ld, int64_t rows, int64_t cols, bool vec) {
+    __syncwarp();
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int k = i * 32 + lane, r = k / kPieces, c = k % kPieces;
+        const uint4 v = buf[at(r, c)];
+        if (r < rows && c * 8 < cols) *reinterpret_cast<uint4*>(dst + r * ld + c * 8) = v;
+      }
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(buf);
+      const int n = rows < 32 ? (int)rows : 32;
+#pragma unroll 4
+      for (int r = 0; r < n; ++r)
+#pragma unroll
+        for (int c = lane; c < W; c += 32)
+          if (c < cols) dst[r * ld + c] = h[at(r, c >> 3) * 8 + (c & 7)];
+    }
+    __syncwarp();
+  }
+};
 
 struct Tile {
   int problem, row, col;   // row and column tile
@@ -205,6 +220,8 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   constexpr uint32_t kBBytes = kBRows * kBK * 2;
   constexpr uint32_t kStageBytes = kABytes + kBBytes;
   constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;  // output columns of a tile
+  constexpr int kBlockCols = kColsOut / 2 < 64 ? kColsOut / 2 : 64;   // columns an epilogue warp stages at a time
+  constexpr uint32_t kStagingBytes = kEpiWarps * 32 * kBlockCols * 2;
   constexpr uint32_t kTmemCols = 2 * BN;
   static_assert(kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "two accumulators");
   static_assert(CTAS == 1 || BN == 256, "pairs take whole tiles");
@@ -212,7 +229,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                               ~static_cast<uintptr_t>(1023));
-  Control<STAGES>* ctl = reinterpret_cast<Control<STAGES>*>(tiles + STAGES * kStageBytes);
+  Control<STAGES>* ctl = reinterpret_cast<Control<STAGES>*>(tiles + STAGES * kStageBytes + kStagingBytes);
   volatile int* abort_flag = &ctl->abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -336,52 +353,63 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
     // ---------------- epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31; warps 2-5 take the
     // left half of the tile's 16-column blocks, warps 6-9 the right half
     const int lane_group = warp & 3, half = (warp - 2) >> 2;
-    constexpr int kBlocks = kColsOut / 16 / 2;   // per warp
+    constexpr int W = kBlockCols;
+    Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * (32 * W / 8)};
     uint32_t n = 0;
     for (int64_t t = first; t < total; t += step, ++n) {
       const uint32_t buf = n & 1;
       const Tile tl = tile_at(g, t);
       const int64_t worker = MODE == DW ? tl.problem >> 1 : tl.problem;
-      const int64_t row = (int64_t)(tl.row * CTAS + rank) * kBM + lane_group * 32 + lane;
-      const bool live = row < g.rows;
+      const int64_t row0 = (int64_t)(tl.row * CTAS + rank) * kBM + lane_group * 32;
+      const int64_t rows = g.rows - row0;   // of this warp's block that exist
       if (!mbar_wait(smem_u32(&ctl->acc_full[buf]), (n >> 1) & 1, abort_flag) || *abort_flag) break;
       tc_fence_after();
       const uint32_t acc = tmem_base + buf * BN + ((uint32_t)(lane_group * 32) << 16);
-      uint16_t* out = static_cast<uint16_t*>(MODE == DW && (tl.problem & 1) ? g.out1 : g.out0) +
-                      (worker * g.rows + row) * (int64_t)g.cols;
-      if (MODE == FORWARD) {
-        uint16_t* pre = g.pre ? static_cast<uint16_t*>(g.pre) + (worker * g.rows + row) * 2 * g.pre_pitch : nullptr;
+      uint16_t* dst = static_cast<uint16_t*>(MODE == DW && (tl.problem & 1) ? g.out1 : g.out0) + (worker * g.rows + row0) * g.cols;
+      if (rows > 0) {
+        for (int c0 = half * (kColsOut / 2); c0 < (half + 1) * (kColsOut / 2); c0 += W) {
+          const int64_t col = (int64_t)tl.col * kColsOut + c0;
+          const int64_t cols = g.cols - col;
+          if (cols <= 0) break;
+          if (MODE == FORWARD) {
 #pragma unroll 1
-        for (int c = half * kBlocks; c < (half + 1) * kBlocks; ++c) {
-          float a[16], b[16], h[16];
-          __syncwarp();
-          tmem_ld16x2(acc + c * 16, acc + BN / 2 + c * 16, a, b);
-          const int64_t col = (int64_t)tl.col * kColsOut + c * 16;
-          if (live && col < g.cols) {
-            switch (g.act) {
-              case OLSGD_ACT_SILU: activate16<OLSGD_ACT_SILU>(a, b, h); break;
-              case OLSGD_ACT_GELU: activate16<OLSGD_ACT_GELU>(a, b, h); break;
-              case OLSGD_ACT_RELU: activate16<OLSGD_ACT_RELU>(a, b, h); break;
-              default: activate16<OLSGD_ACT_SIGMOID>(a, b, h);
+            for (int q = 0; q < W / 16; ++q) {
+              float a[16], b[16], h[16];
+              tmem_ld16x2(acc + c0 + q * 16, acc + BN / 2 + c0 + q * 16, a, b);
+              switch (g.act) {
+                case OLSGD_ACT_SILU: activate16<OLSGD_ACT_SILU>(a, b, h); break;
+                case OLSGD_ACT_GELU: activate16<OLSGD_ACT_GELU>(a, b, h); break;
+                case OLSGD_ACT_RELU: activate16<OLSGD_ACT_RELU>(a, b, h); break;
+                default: activate16<OLSGD_ACT_SIGMOID>(a, b, h);
+              }
+              out.put(lane, q, h, g.f16);
             }
-            store16(out, col, g.cols, g.out_vec, h, g.f16);
-            if (pre) {
-              // rows of pre_pitch (a multiple of 8): columns up to it exist and are written
-              store16(pre, col, g.pre_pitch, g.pre_vec, a, g.f16);
-              store16(pre + g.pre_pitch, col, g.pre_pitch, g.pre_vec, b, g.f16);
-            }
-          }
-        }
-      } else {
+            out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
+            if (g.pre) {
+              // a, then b, to rows of pre_pitch (a multiple of 8): columns up to it exist
+              uint16_t* pre = static_cast<uint16_t*>(g.pre) + (worker * g.rows + row0) * 2 * g.pre_pitch + col;
 #pragma unroll 1
-        for (int c = half * kBlocks; c < (half + 1) * kBlocks; c += 2) {
-          float v[16], w[16];
-          __syncwarp();
-          tmem_ld16x2(acc + c * 16, acc + c * 16 + 16, v, w);
-          const int64_t col = (int64_t)tl.col * BN + c * 16;
-          if (live) {
-            store16(out, col, g.cols, g.out_vec, v, g.f16);
-            store16(out, col + 16, g.cols, g.out_vec, w, g.f16);
+              for (int z = 0; z < 2; ++z) {
+#pragma unroll 1
+                for (int q = 0; q < W / 16; q += W >= 32 ? 2 : 1) {
+                  float v[16], w[16];
+                  const uint32_t at = acc + z * (BN / 2) + c0 + q * 16;
+                  tmem_ld16x2(at, W >= 32 ? at + 16 : at, v, w);
+                  out.put(lane, q, v, g.f16);
+                  if (W >= 32) out.put(lane, q + 1, w, g.f16);
+                }
+                out.flush(lane, pre + z * g.pre_pitch, 2 * g.pre_pitch, rows, g.pre_pitch - col, true);
+              }
+            }
+          } else {
+#pragma unroll 1
+            for (int q = 0; q < W / 16; q += 2) {
+              float v[16], w[16];
+              tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
+              out.put(lane, q, v, g.f16);
+              out.put(lane, q + 1, w, g.f16);
+            }
+            out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
           }
         }
       }
@@ -415,23 +443,43 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
 
 // ------------------------------------------------------------------- element-wise kernels
 
-// Rows of any pitch to rows of a pitch that TMA takes.  [m][rows][cols] of 16-bit values.
+// Rows of any pitch to rows of a pitch that TMA takes: [m][rows][cols] of 16-bit values.  A thread
+// makes one aligned 16-byte piece out of the two that its elements lie in (`begin` and `end`
+// bound the tensor: nothing outside it is read).
 __global__ void __launch_bounds__(256)
 pad_rows_kernel(const uint16_t* __restrict__ in, uint16_t* __restrict__ out, int64_t rows, int64_t cols,
-                int64_t in_worker, int64_t in_row, int64_t pitch) {
+                int64_t in_worker, int64_t in_row, int64_t pitch, const uint16_t* begin, const uint16_t* end) {
   launch_gate();
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const uint16_t* src = in + (int64_t)blockIdx.y * in_worker + r * in_row;
-    uint16_t* dst = out + ((int64_t)blockIdx.y * rows + r) * pitch;
-    for (int64_t j = threadIdx.x * 8; j < cols; j += 256 * 8) {
-      uint32_t p[4];
+  const int64_t per_row = pitch / 8, n = rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row, j = (i - r * per_row) * 8;
+    const uint16_t* src = in + (int64_t)blockIdx.y * in_worker + r * in_row + j;
+    const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
+    const uint16_t* base = src - off;
+    uint32_t w[8];
+    if (j + 8 <= cols && base >= begin && base + 16 <= end) {
+      const uint4 a = *reinterpret_cast<const uint4*>(base), b = *reinterpret_cast<const uint4*>(base + 8);
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+      if (off & 4) {
+#pragma unroll
+        for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+      }
+      if (off & 2) {
+#pragma unroll
+        for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+      }
+      if (off & 1) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+      }
+    } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = j + 2 * e < cols ? src[j + 2 * e] : 0, hi = j + 2 * e + 1 < cols ? src[j + 2 * e + 1] : 0;
-        p[e] = lo | (hi << 16);
+        const uint32_t lo = j + 2 * e < cols ? src[2 * e] : 0, hi = j + 2 * e + 1 < cols ? src[2 * e + 1] : 0;
+        w[e] = lo | (hi << 16);
       }
-      *reinterpret_cast<uint4*>(dst + j) = make_uint4(p[0], p[1], p[2], p[3]);
     }
+    *reinterpret_cast<uint4*>(out + ((int64_t)blockIdx.y * rows + r) * pitch + j) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -488,14 +536,14 @@ bool make_map16(CUtensorMap* map, const GatedOperand& o, int64_t cols, int64_t r
 
 template <int MODE, int CTAS, int BN, int STAGES>
 cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
-  constexpr size_t smem =
-      (size_t)STAGES * (kBM * kBK * 2 + BN / CTAS * kBK * 2) + sizeof(Control<STAGES>) + 1024;
+  constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;
+  constexpr size_t smem = (size_t)STAGES * (kBM * kBK * 2 + BN / CTAS * kBK * 2) +
+                          kEpiWarps * 32 * (kColsOut / 2 < 64 ? kColsOut / 2 : 64) * 2 + sizeof(Control<STAGES>) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   static PerDeviceSmem configured;
   auto kern = gated_gemm_kernel<MODE, CTAS, BN, STAGES>;
   cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
   if (e != cudaSuccess) return e;
-  constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;
   g.row_tiles = (g.rows + CTAS * kBM - 1) / (CTAS * kBM);
   g.col_tiles = (g.cols + kColsOut - 1) / kColsOut;
   const int64_t total = (int64_t)g.problems * g.row_tiles * g.col_tiles;
@@ -520,23 +568,36 @@ cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kern, maps, g);
 }
 
-// Which tiles: 256 columns, by a pair where a problem has more than 128 rows, as long as that
-// gives most multiprocessors a tile; else 64 columns.
+// Which tiles.  A tile's time goes by the operand bytes that one CTA takes in per K block
+// (128 rows of A and BN / CTAS rows of B), plus an epilogue that is not hidden in the last wave;
+// the launch takes as many waves as its tiles need.  The shape with the least product is taken:
+// pairs for large problems, 128 or 64 columns where wider tiles would leave multiprocessors
+// without one.
 struct Shape {
   int ctas, bn;
 };
 template <int MODE>
 Shape shape_for(const GatedArgs& g) {
-  const int64_t cols256 = MODE == FORWARD ? 128 : 256;
-  const int64_t col_tiles = (g.cols + cols256 - 1) / cols256;
-  const int64_t one = (int64_t)g.problems * ((g.rows + kBM - 1) / kBM) * col_tiles;
-  if (one < 120) return Shape{1, 64};
-  return Shape{g.rows > kBM ? 2 : 1, 256};
+  constexpr Shape shapes[] = {{1, 64}, {1, 128}, {1, 256}, {2, 256}};
+  Shape best = shapes[0];
+  int64_t least = INT64_MAX;
+  for (const Shape& sh : shapes) {
+    const int64_t cols = MODE == FORWARD ? sh.bn / 2 : sh.bn;
+    const int64_t tiles = (int64_t)g.problems * ((g.rows + sh.ctas * kBM - 1) / (sh.ctas * kBM)) * ((g.cols + cols - 1) / cols);
+    const int64_t room = sm_count() / sh.ctas, waves = (tiles + room - 1) / room;
+    const int64_t cost = waves * (g.num_kb + 4) * (kBM + sh.bn / sh.ctas);
+    if (cost < least) {
+      least = cost;
+      best = sh;
+    }
+  }
+  return best;
 }
 
 template <int MODE>
 cudaError_t launch_mode(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
   if (sh.bn == 64) return launch_variant<MODE, 1, 64, 8>(maps, g, s);
+  if (sh.bn == 128) return launch_variant<MODE, 1, 128, 6>(maps, g, s);
   if (sh.ctas == 2) return launch_variant<MODE, 2, 256, 6>(maps, g, s);
   return launch_variant<MODE, 1, 256, 4>(maps, g, s);
 }
@@ -552,17 +613,17 @@ cudaError_t ready(GatedOperand& o, int64_t rows, int64_t cols, int64_t m, uint8_
   const int64_t pitch = round8(cols);
   uint16_t* dst = reinterpret_cast<uint16_t*>(*ws);
   *ws += round256((size_t)m * rows * pitch * 2);
+  const uint16_t* begin = static_cast<const uint16_t*>(o.p);
+  const uint16_t* end = begin + (m > 1 ? (m - 1) * o.worker_stride : 0) + (rows > 1 ? (rows - 1) * o.row_stride : 0) + cols;
+  const int64_t want = (rows * (pitch / 8) + 255) / 256, most = (148 * 16 + m - 1) / m;
   const cudaError_t e =
-      launch_chained(pad_rows_kernel, dim3((unsigned)(rows < 4096 ? rows : 4096), (unsigned)m), dim3(256), 0, s,
-                     static_cast<const uint16_t*>(o.p), dst, rows, cols, o.worker_stride, o.row_stride, pitch);
+      launch_chained(pad_rows_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)m), dim3(256), 0, s, begin, dst,
+                     rows, cols, o.worker_stride, o.row_stride, pitch, begin, end);
   o = GatedOperand{dst, rows * pitch, pitch};
   return e;
 }
 
-int store_width(const void* p, int64_t cols) {
-  const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(cols * 2);
-  return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
-}
+bool whole_pieces(const void* p, int64_t cols) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && cols % 8 == 0; }
 
 template <typename T>
 cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, cudaStream_t s) {
@@ -608,11 +669,10 @@ cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
   g.cols = (int)a.F;
   g.act = a.act;
   g.f16 = a.f16;
-  g.out_vec = store_width(a.h, a.F);
+  g.out_vec = whole_pieces(a.h, a.F);
   g.out0 = a.h;
   g.pre = a.pre;
   g.pre_pitch = round8(a.F);
-  g.pre_vec = store_width(a.pre, g.pre_pitch);
   const Shape sh = shape_for<FORWARD>(g);
   GatedMaps maps;
   const int b_rows = sh.bn / 2;
@@ -642,7 +702,7 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
     g.rows = (int)a.T;
     g.cols = (int)a.D;
     g.f16 = a.f16;
-    g.out_vec = store_width(a.dx, a.D);
+    g.out_vec = whole_pieces(a.dx, a.D);
     g.out0 = a.dx;
     GatedMaps maps;
     if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, kBM, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, kBM, a.f16) ||
@@ -658,8 +718,7 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
     g.rows = (int)a.F;
     g.cols = (int)a.D;
     g.f16 = a.f16;
-    const int v0 = store_width(a.dwg, a.D), v1 = store_width(a.dwu, a.D);
-    g.out_vec = v0 < v1 ? v0 : v1;
+    g.out_vec = whole_pieces(a.dwg, a.D) && whole_pieces(a.dwu, a.D);
     g.out0 = a.dwg;
     g.out1 = a.dwu;
     GatedMaps maps;

@@ -51,20 +51,23 @@ def _ops():
     return _OPS
 
 
+# Small calls cost what the host takes for them, so the checks below are written to be cheap where
+# they pass: one comparison each, no argument packing.
+
+def _refuse(text, *args):
+    raise ValueError(text % args if args else text)
+
+
 def _need(ok, text, *args):
     if not ok:
-        raise ValueError(text % args if args else text)
+        _refuse(text, *args)
 
 
 def _dtype(t, name):
     code = DTYPES.get(t.dtype)
-    _need(code is not None, "%s must be float32, bfloat16 or float16", name)
+    if code is None:
+        _refuse("%s must be float32, bfloat16 or float16", name)
     return code
-
-
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        _need(t is None or t.device == dev, "%s must be on %s", name, dev)
 
 
 def _stream(index):
@@ -93,12 +96,12 @@ def _workspace_bytes(query, *sizes):
     return n.value
 
 
-def _workspace(dev, query, *sizes):
-    """(tensor, pointer, bytes) of a fresh workspace; torch's allocations are 512-byte aligned."""
+def _workspace(like, query, *sizes):
+    """(tensor, pointer, bytes) of a fresh workspace on like's device; torch's allocations are 512-byte aligned."""
     n = _workspace_bytes(query, *sizes)
     if n == 0:
         return None, None, 0
-    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    ws = like.new_empty(n, dtype=torch.uint8)
     return ws, ws.data_ptr(), n
 
 
@@ -106,9 +109,11 @@ def _workspace(dev, query, *sizes):
 
 def _rows_of(t, name):
     """(view [N][V], stride between rows) of a tensor [..., V] whose rows are evenly spaced."""
-    _need(t.dim() >= 1 and t.is_cuda, "%s must be a CUDA tensor with at least one dimension", name)
+    if not t.is_cuda or t.dim() < 1:
+        _refuse("%s must be a CUDA tensor with at least one dimension", name)
     V = t.shape[-1]
-    _need(V >= 1 and (t.stride(-1) == 1 or V == 1), "%s: the last dimension must be contiguous and not empty", name)
+    if V < 1 or (V > 1 and t.stride(-1) != 1):
+        _refuse("%s: the last dimension must be contiguous and not empty", name)
     if t.dim() != 2:   # (one launch takes rows at one distance)
         try:
             t = t.view(-1, V)
@@ -117,9 +122,9 @@ def _rows_of(t, name):
     return t, (t.stride(0) if t.shape[0] > 1 else V)
 
 
-def _per_row(t, shape, dtype, name):
-    _need(t.dtype == dtype and t.shape == shape and t.is_contiguous(), "%s must be contiguous %s of shape %s", name, dtype,
-          tuple(shape))
+def _per_row(t, shape, dtype, dev, name):
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != dev:
+        _refuse("%s must be contiguous %s of shape %s on %s", name, dtype, tuple(shape), dev)
     return t.data_ptr()
 
 
@@ -130,22 +135,28 @@ def token_logprobs(logits, targets, top=0):
     lib = _ops()
     rows, ld = _rows_of(logits, "logits")
     code, dev, lead = _dtype(logits, "logits"), logits.device, logits.shape[:-1]
-    _same_device(dev, targets=targets)
-    tp = _per_row(targets, lead, torch.int32, "targets")
+    tp = _per_row(targets, lead, torch.int32, dev, "targets")
     N, V = rows.shape
     top = int(top)
-    _need(0 <= top <= min(V, MAX_TOP), "top must be in [0, min(V, %d)]", MAX_TOP)
-    # the float outputs share one allocation: a small call is mostly the time that the host takes
-    out = torch.empty(N * (4 + top), dtype=torch.float32, device=dev)
-    logp, entropy, stats, top_logp = out.split((N, N, 2 * N, top * N))
-    top_ids = torch.empty(lead + (top,), dtype=torch.int32, device=dev) if top else None
-    ws, wp, wn = _workspace(dev, "olsgd_token_logprobs_workspace", code, N, V, top)
+    if not 0 <= top <= min(V, MAX_TOP):
+        _refuse("top must be in [0, min(V, %d)]", MAX_TOP)
+    # the float outputs share one allocation: allocating is most of what the host does here
+    out = targets.new_empty(N * (4 + top), dtype=torch.float32)
     p = out.data_ptr()
-    _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N if top else None,
-         top_ids.data_ptr() if top else None, wp, wn)
+    ws, wp, wn = _workspace(targets, "olsgd_token_logprobs_workspace", code, N, V, top)
+    if top:
+        top_ids = targets.new_empty(lead + (top,))
+        _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N,
+             top_ids.data_ptr(), wp, wn)
+        logp, entropy, stats, top_logp = out.split_with_sizes((N, N, 2 * N, top * N))
+        top_logp = top_logp.view(lead + (top,))
+    else:
+        top_logp = top_ids = None
+        _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, 0, p, p + 4 * N, p + 8 * N, None, None, wp, wn)
+        logp, entropy, stats = out.split_with_sizes((N, N, 2 * N))
     if len(lead) != 1:
         logp, entropy = logp.view(lead), entropy.view(lead)
-    return TokenLogprobs(logp, entropy, stats.view(lead + (2,)), top_logp.view(lead + (top,)) if top else None, top_ids)
+    return TokenLogprobs(logp, entropy, stats.view(lead + (2,)), top_logp, top_ids)
 
 
 def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
@@ -153,29 +164,27 @@ def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
     are float32 [...] or None (zeros); stats and entropy are token_logprobs' for the same logits."""
     lib = _ops()
     rows, ld = _rows_of(logits, "logits")
-    code, dev, lead = _dtype(logits, "logits"), logits.device, logits.shape[:-1]
-    _same_device(dev, targets=targets, stats=stats, entropy=entropy, d_logp=d_logp, d_entropy=d_entropy)
+    code, dev, lead, f32 = _dtype(logits, "logits"), logits.device, logits.shape[:-1], torch.float32
     N, V = rows.shape
-    d = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    d = logits.new_empty(logits.shape)
     _run(lib.olsgd_token_logprobs_backward, dev,
-         None if d_logp is None else _per_row(d_logp, lead, torch.float32, "d_logp"),
-         None if d_entropy is None else _per_row(d_entropy, lead, torch.float32, "d_entropy"),
-         rows.data_ptr(), code, N, V, ld, _per_row(targets, lead, torch.int32, "targets"),
-         _per_row(stats, lead + (2,), torch.float32, "stats"), _per_row(entropy, lead, torch.float32, "entropy"),
-         d.data_ptr(), V)
+         None if d_logp is None else _per_row(d_logp, lead, f32, dev, "d_logp"),
+         None if d_entropy is None else _per_row(d_entropy, lead, f32, dev, "d_entropy"),
+         rows.data_ptr(), code, N, V, ld, _per_row(targets, lead, torch.int32, dev, "targets"),
+         _per_row(stats, lead + (2,), f32, dev, "stats"), _per_row(entropy, lead, f32, dev, "entropy"), d.data_ptr(), V)
     return d
 
 
 # ------------------------------------------------------------------------ gradient clipping
 
 def _worker_rows(t, m, name):
-    """Elements between workers of a tensor [m, ...] whose workers' parts are contiguous."""
-    _need(t.dim() >= 1 and t.shape[0] == m, "%s must have %s workers", name, m)
+    """(elements of a worker, elements between workers) of a tensor [m, ...] whose workers' parts are contiguous."""
     n = t.numel() // m
     if t.is_contiguous():
         return n, n
-    _need(t[0].is_contiguous(), "%s: each worker's part must be contiguous", name)
-    return n, t.stride(0)
+    if not t[0].is_contiguous():
+        _refuse("%s: each worker's part must be contiguous", name)
+    return n, (t.stride(0) if m > 1 else n)
 
 
 def clip_grads(grads, max_norm, out=None):
@@ -189,21 +198,24 @@ def clip_grads(grads, max_norm, out=None):
         grads, out = [grads], None if out is None else [out]
     _need(len(grads) > 0, "grads is empty")
     if out is None:
-        out = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads]
+        out = [g.new_empty(g.shape) for g in grads]
     _need(len(out) == len(grads), "out must hold one tensor for each gradient")
-    m, dev = grads[0].shape[0] if grads[0].dim() else 0, grads[0].device
-    _need(dev.type == "cuda" and m >= 1, "grads must be CUDA tensors with the workers first")
+    first = grads[0]
+    m, dev = first.shape[0] if first.dim() else 0, first.device
+    _need(first.is_cuda and m >= 1, "grads must be CUDA tensors with the workers first")
     flat = []
     for g, o in zip(grads, out):
+        shape = g.shape
+        if shape != o.shape or len(shape) == 0 or shape[0] != m or g.device != dev or o.device != dev:
+            _refuse("gradients and out must be on one device, of the same shapes, with %d workers first", m)
         gc, oc = DTYPES.get(g.dtype), DTYPES.get(o.dtype)
-        _need(gc is not None and oc is not None, "gradients and out must be float32, bfloat16 or float16")
-        _need(g.shape == o.shape and g.device == dev and o.device == dev, "gradients and out must match in shape and device")
+        if gc is None or oc is None:
+            _refuse("gradients and out must be float32, bfloat16 or float16")
         n, gs = _worker_rows(g, m, "a gradient")
-        _, os_ = _worker_rows(o, m, "out")
-        flat += (g.data_ptr(), o.data_ptr(), n, gs, os_, gc | (oc << 32))
+        flat += (g.data_ptr(), o.data_ptr(), n, gs, n if o.is_contiguous() else _worker_rows(o, m, "out")[1], gc | (oc << 32))
     table = (_i64 * len(flat))(*flat)
-    norms = torch.empty(m, dtype=torch.float32, device=dev)
-    ws, wp, wn = _workspace(dev, "olsgd_clip_grads_workspace", m, len(grads))
+    norms = first.new_empty(m, dtype=torch.float32)
+    ws, wp, wn = _workspace(norms, "olsgd_clip_grads_workspace", m, len(grads))
     _run(lib.olsgd_clip_grads, dev, table, len(grads), m, float(max_norm), norms.data_ptr(), wp, wn)
     return (out[0] if single else out), norms
 
@@ -212,9 +224,11 @@ def clip_grads(grads, max_norm, out=None):
 
 def _matrix(t, name, shape, dtype, dev):
     """(pointer, worker stride, row stride) of a tensor [m][rows][cols] with contiguous rows."""
-    _need(t.shape == shape and t.dtype == dtype and t.device == dev, "%s must be %s of shape %s on %s", name, dtype, tuple(shape), dev)
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
+        _refuse("%s must be %s of shape %s on %s", name, dtype, tuple(shape), dev)
     sw, sr, sc = t.stride()
-    _need(sc == 1 or shape[2] == 1, "%s: the last dimension must be contiguous", name)
+    if sc != 1 and shape[2] != 1:
+        _refuse("%s: the last dimension must be contiguous", name)
     return t.data_ptr(), sw, sr
 
 
@@ -224,11 +238,15 @@ def _aligned(matrix, shape):
 
 
 def _gated_sizes(x, w_gate, activation):
-    _need(x.is_cuda and x.dim() == 3 and w_gate.dim() == 3, "x and w_gate must be CUDA tensors [m][T][D] and [m][F][D]")
-    _need(x.dtype in (torch.bfloat16, torch.float16), "x must be bfloat16 or float16")
-    _need(activation in ACTIVATIONS, "activation must be one of %s", sorted(ACTIVATIONS))
+    if not x.is_cuda or x.dim() != 3 or w_gate.dim() != 3:
+        _refuse("x and w_gate must be CUDA tensors [m][T][D] and [m][F][D]")
+    code, act = DTYPES.get(x.dtype), ACTIVATIONS.get(activation)
+    if not code:
+        _refuse("x must be bfloat16 or float16")
+    if act is None:
+        _refuse("activation must be one of %s", sorted(ACTIVATIONS))
     m, T, D = x.shape
-    return m, T, D, w_gate.shape[1], DTYPES[x.dtype], ACTIVATIONS[activation]
+    return m, T, D, w_gate.shape[1], code, act
 
 
 def gated_forward(x, w_gate, w_up, activation="silu", save=False):
@@ -239,10 +257,10 @@ def gated_forward(x, w_gate, w_up, activation="silu", save=False):
     m, T, D, F, code, act = _gated_sizes(x, w_gate, activation)
     dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
     a, b, c = _matrix(x, "x", (m, T, D), dtype, dev), _matrix(w_gate, "w_gate", ws_shape, dtype, dev), _matrix(w_up, "w_up", ws_shape, dtype, dev)
-    h = torch.empty((m, T, F), dtype=dtype, device=dev)
-    pre = torch.empty((m, T, 2, (F + 7) // 8 * 8), dtype=dtype, device=dev) if save else None
+    h = x.new_empty((m, T, F))
+    pre = x.new_empty((m, T, 2, (F + 7) // 8 * 8)) if save else None
     ok = _aligned(a, (m, T)) and _aligned(b, ws_shape) and _aligned(c, ws_shape)
-    ws, wp, wn = _workspace(dev, "olsgd_gated_workspace", m, T, D, F, 0, ok)
+    ws, wp, wn = _workspace(h, "olsgd_gated_workspace", m, T, D, F, 0, ok)
     _run(lib.olsgd_gated_forward, dev, m, T, D, F, code, act, *a, *b, *c, h.data_ptr(), pre.data_ptr() if save else None, wp, wn)
     return (h, pre) if save else h
 
@@ -257,12 +275,10 @@ def gated_backward(d_h, x, w_gate, w_up, pre, activation="silu", want_d_x=True, 
     b, c = _matrix(w_gate, "w_gate", ws_shape, dtype, dev), _matrix(w_up, "w_up", ws_shape, dtype, dev)
     _need(pre.shape == (m, T, 2, (F + 7) // 8 * 8) and pre.dtype == dtype and pre.device == dev and pre.is_contiguous(),
           "pre must be the one that gated_forward returned")
-    d_x = torch.empty((m, T, D), dtype=dtype, device=dev) if want_d_x else None
-    d_wg = d_wu = None
-    if want_d_w:
-        d_wg, d_wu = torch.empty(ws_shape, dtype=dtype, device=dev), torch.empty(ws_shape, dtype=dtype, device=dev)
+    d_x = x.new_empty((m, T, D)) if want_d_x else None
+    d_wg, d_wu = (x.new_empty(ws_shape), x.new_empty(ws_shape)) if want_d_w else (None, None)
     ok = _aligned(a, (m, T)) and _aligned(b, ws_shape) and _aligned(c, ws_shape)
-    ws, wp, wn = _workspace(dev, "olsgd_gated_workspace", m, T, D, F, 1, ok)
+    ws, wp, wn = _workspace(x, "olsgd_gated_workspace", m, T, D, F, 1, ok)
     _run(lib.olsgd_gated_backward, dev, m, T, D, F, code, act, *d, *a, *b, *c, pre.data_ptr(), d_x.data_ptr() if want_d_x else None,
          d_wg.data_ptr() if want_d_w else None, d_wu.data_ptr() if want_d_w else None, wp, wn)
     return d_x, d_wg, d_wu
@@ -274,15 +290,15 @@ def embedding_forward(table, ids, scale=1.0):
     """olsgd_embedding_forward: scale * table[i, ids[i]] for each worker i.  table [m][V][D], rows contiguous; ids int32 [m][T],
     those outside [0, V) give rows of zeros.  Returns [m][T][D] of the table's type."""
     lib = _ops()
-    _need(table.is_cuda and table.dim() == 3 and ids.dim() == 2, "table must be a CUDA tensor [m][V][D], ids [m][T]")
+    if not table.is_cuda or table.dim() != 3 or ids.dim() != 2:
+        _refuse("table must be a CUDA tensor [m][V][D], ids [m][T]")
     code, dev = _dtype(table, "table"), table.device
     m, V, D = table.shape
     T = ids.shape[1]
-    _same_device(dev, ids=ids)
     p, sw, sr = _matrix(table, "table", (m, V, D), table.dtype, dev)
-    out = torch.empty((m, T, D), dtype=table.dtype, device=dev)
-    _run(lib.olsgd_embedding_forward, dev, m, T, V, D, code, p, sw, sr, _per_row(ids, (m, T), torch.int32, "ids"), float(scale),
-         out.data_ptr())
+    ip = _per_row(ids, (m, T), torch.int32, dev, "ids")
+    out = table.new_empty((m, T, D))
+    _run(lib.olsgd_embedding_forward, dev, m, T, V, D, code, p, sw, sr, ip, float(scale), out.data_ptr())
     return out
 
 
@@ -290,18 +306,19 @@ def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=No
     """olsgd_embedding_backward: the gradient of a table [m][vocab][D] from d_out [m][T][D] and the ids of the lookup; new, of
     type `dtype`, or written to `out` (each worker's part contiguous, for example a view of a flat gradient [m][P])."""
     lib = _ops()
-    _need(d_out.is_cuda and d_out.dim() == 3, "d_out must be a CUDA tensor [m][T][D]")
+    if not d_out.is_cuda or d_out.dim() != 3:
+        _refuse("d_out must be a CUDA tensor [m][T][D]")
     code, dev = _dtype(d_out, "d_out"), d_out.device
     m, T, D = d_out.shape
     V = int(vocab)
-    _same_device(dev, ids=ids, out=out)
     p, sw, sr = _matrix(d_out, "d_out", (m, T, D), d_out.dtype, dev)
     if out is None:
-        out = torch.empty((m, V, D), dtype=dtype, device=dev)
-    _need(out.shape == (m, V, D), "out must be of shape %s", (m, V, D))
+        out = d_out.new_empty((m, V, D), dtype=dtype)
+    if out.shape != (m, V, D) or out.device != dev:
+        _refuse("out must be of shape %s on %s", (m, V, D), dev)
     _, ow = _worker_rows(out, m, "out")
-    ip = _per_row(ids, (m, T), torch.int32, "ids")
-    ws, wp, wn = _workspace(dev, "olsgd_embedding_workspace", m, T, D)
+    ip = _per_row(ids, (m, T), torch.int32, dev, "ids")
+    ws, wp, wn = _workspace(out, "olsgd_embedding_workspace", m, T, D)
     _run(lib.olsgd_embedding_backward, dev, m, T, V, D, code, p, sw, sr, ip, float(scale), _dtype(out, "out"), out.data_ptr(), ow, wp, wn)
     return out
 
