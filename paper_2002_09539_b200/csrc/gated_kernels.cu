@@ -47,6 +47,7 @@ struct GatedArgs {
   int problems;               // workers (DW: workers x 2)
   int rows, cols;             // extents of one problem's output (FORWARD: cols = F)
   int act, f16;
+  int a_rows;                 // rows of A that are loaded (K-major): all 128 unless the problem has fewer
   bool out_vec;               // the output's rows are whole 16-byte pieces
   void* out0;                 // h, dx or dWg
   void* out1;                 // dWu
@@ -276,7 +277,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
         const int s = it % STAGES;
         if (!mbar_wait(smem_u32(&ctl->empty[s]), ((it / STAGES) & 1) ^ 1, abort_flag)) break;
         const uint32_t bar_own = smem_u32(&ctl->full[s]);
-        if (leader) mbar_expect_tx(bar_own, CTAS * kStageBytes);
+        if (leader) mbar_expect_tx(bar_own, A_MN ? CTAS * kStageBytes : CTAS * (g.a_rows * (kBK * 2) + kBBytes));
         const uint32_t a_dst = smem_u32(tiles + s * kStageBytes), b_dst = a_dst + kABytes;
         const bool second = MODE == DX && kb >= g.kb_half;
         const int k0 = (second ? kb - g.kb_half : kb) * kBK;
@@ -441,23 +442,128 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   }
 }
 
+// ------------------------------------------------------------------------- few tokens
+// Up to kFewTokens tokens a worker: every weight is used that often, so reading the weights is
+// all there is to it and the tensor cores have nothing to gain.  A warp per feature holds its
+// rows of Wg and Wu 16 bytes a lane at a time against all tokens (x comes from L1), and adds
+// the lanes up at the end.  1024 -> 4096 bf16: 4.7 us for one token and 5.3 us for two, against
+// 8.5 us by 64-column tiles on the tensor cores, which take over at three (9.0 us here).
+constexpr int kFewTokens = 2;
+
+template <typename T, int NT, bool VEC>
+__global__ void __launch_bounds__(256)
+gated_few_kernel(GatedOperand x, GatedOperand wg, GatedOperand wu, int tokens, int64_t D, int64_t F, int act, T* __restrict__ h,
+                 T* __restrict__ pre, int64_t pre_pitch) {
+  launch_gate();
+  const int lane = threadIdx.x & 31;
+  const int64_t f = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), worker = blockIdx.y;
+  if (f >= F) return;
+  const T* xw = static_cast<const T*>(x.p) + worker * x.worker_stride;
+  const T* g = static_cast<const T*>(wg.p) + worker * wg.worker_stride + f * wg.row_stride;
+  const T* u = static_cast<const T*>(wu.p) + worker * wu.worker_stride + f * wu.row_stride;
+  float a[NT], b[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) a[t] = b[t] = 0.f;
+  const T* xt[NT];   // (with fewer tokens than NT the last one is formed again, and not stored)
+#pragma unroll
+  for (int t = 0; t < NT; ++t) xt[t] = xw + min(t, tokens - 1) * x.row_stride;
+  if (VEC) {   // D a multiple of 8, every row on a 16-byte boundary
+    constexpr int U = 4;
+    f32x2 a2[NT], b2[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) a2[t] = b2[t] = 0;
+    for (int64_t j0 = lane * 8; j0 < D; j0 += 256 * U) {
+      uint4 rg[U], ru[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const bool live = j0 + i * 256 < D;
+        rg[i] = live ? ld16_stream(g + j0 + i * 256) : make_uint4(0, 0, 0, 0);
+        ru[i] = live ? ld16_stream(u + j0 + i * 256) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        uint4 rx[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) rx[t] = j0 + i * 256 < D ? ld16(xt[t] + j0 + i * 256) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x2 vg = raw_pair<T>(rg[i], e), vu = raw_pair<T>(ru[i], e);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const f32x2 vx = raw_pair<T>(rx[t], e);
+            a2[t] = fma2(vx, vg, a2[t]);
+            b2[t] = fma2(vx, vu, b2[t]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float lo, hi;
+      unpack2f(a2[t], lo, hi);
+      a[t] = lo + hi;
+      unpack2f(b2[t], lo, hi);
+      b[t] = lo + hi;
+    }
+  } else {
+#pragma unroll 4
+    for (int64_t j = lane; j < D; j += 32) {
+      const float vg = Elem<T>::to_float(g[j]), vu = Elem<T>::to_float(u[j]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float vx = Elem<T>::to_float(xt[t][j]);
+        a[t] = fmaf(vx, vg, a[t]);
+        b[t] = fmaf(vx, vu, b[t]);
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t >= tokens) break;
+    const float at = warp_sum(a[t]), bt = warp_sum(b[t]);
+    if (lane == 0) {
+      const float v = act == OLSGD_ACT_SILU   ? act_value<OLSGD_ACT_SILU>(at)
+                      : act == OLSGD_ACT_GELU ? act_value<OLSGD_ACT_GELU>(at)
+                      : act == OLSGD_ACT_RELU ? act_value<OLSGD_ACT_RELU>(at)
+                                              : act_value<OLSGD_ACT_SIGMOID>(at);
+      const int64_t row = worker * tokens + t;
+      h[row * F + f] = Elem<T>::from_float(v * bt);
+      if (pre) {
+        T* p = pre + row * 2 * pre_pitch;
+        p[f] = Elem<T>::from_float(at);
+        p[pre_pitch + f] = Elem<T>::from_float(bt);
+        if (f == F - 1)   // the padding of the rows
+          for (int64_t k = F; k < pre_pitch; ++k) p[k] = p[pre_pitch + k] = Elem<T>::from_float(0.f);
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------- element-wise kernels
 
-// Rows of any pitch to rows of a pitch that TMA takes: [m][rows][cols] of 16-bit values.  A thread
-// makes one aligned 16-byte piece out of the two that its elements lie in (`begin` and `end`
-// bound the tensor: nothing outside it is read).
-__global__ void __launch_bounds__(256)
-pad_rows_kernel(const uint16_t* __restrict__ in, uint16_t* __restrict__ out, int64_t rows, int64_t cols,
-                int64_t in_worker, int64_t in_row, int64_t pitch, const uint16_t* begin, const uint16_t* end) {
+// Rows of any pitch to rows of a pitch that TMA takes: up to three operands [m][rows][cols] of
+// 16-bit values, blockIdx.z counting them.  A thread makes one aligned 16-byte piece out of the
+// two that its elements lie in (`begin` and `end` bound the tensor: nothing outside it is read).
+struct PadOperand {
+  const uint16_t *begin, *end;
+  uint16_t* out;
+  int64_t rows, in_worker, in_row;
+};
+struct PadOperands {
+  PadOperand op[3];
+  int64_t cols, pitch;
+};
+__global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ PadOperands all) {
   launch_gate();
-  const int64_t per_row = pitch / 8, n = rows * per_row;
+  const PadOperand& o = all.op[blockIdx.z];
+  const int64_t cols = all.cols, per_row = all.pitch / 8, n = o.rows * per_row;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / per_row, j = (i - r * per_row) * 8;
-    const uint16_t* src = in + (int64_t)blockIdx.y * in_worker + r * in_row + j;
+    const uint16_t* src = o.begin + (int64_t)blockIdx.y * o.in_worker + r * o.in_row + j;
     const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
     const uint16_t* base = src - off;
     uint32_t w[8];
-    if (j + 8 <= cols && base >= begin && base + 16 <= end) {
+    if (j + 8 <= cols && base >= o.begin && base + 16 <= o.end) {
       const uint4 a = *reinterpret_cast<const uint4*>(base), b = *reinterpret_cast<const uint4*>(base + 8);
       w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
       if (off & 4) {
@@ -479,7 +585,7 @@ pad_rows_kernel(const uint16_t* __restrict__ in, uint16_t* __restrict__ out, int
         w[e] = lo | (hi << 16);
       }
     }
-    *reinterpret_cast<uint4*>(out + ((int64_t)blockIdx.y * rows + r) * pitch + j) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(o.out + ((int64_t)blockIdx.y * o.rows + r) * all.pitch + j) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -607,21 +713,38 @@ bool tma_ready(const GatedOperand& o, int64_t rows, int64_t m) {
          (m == 1 || o.worker_stride % 8 == 0);
 }
 
-// The operand itself, or its copy in rows of round8(cols) at *ws (which then moves on).
-cudaError_t ready(GatedOperand& o, int64_t rows, int64_t cols, int64_t m, uint8_t** ws, cudaStream_t s) {
-  if (tma_ready(o, rows, m)) return cudaSuccess;
-  const int64_t pitch = round8(cols);
-  uint16_t* dst = reinterpret_cast<uint16_t*>(*ws);
-  *ws += round256((size_t)m * rows * pitch * 2);
-  const uint16_t* begin = static_cast<const uint16_t*>(o.p);
-  const uint16_t* end = begin + (m > 1 ? (m - 1) * o.worker_stride : 0) + (rows > 1 ? (rows - 1) * o.row_stride : 0) + cols;
-  const int64_t want = (rows * (pitch / 8) + 255) / 256, most = (148 * 16 + m - 1) / m;
-  const cudaError_t e =
-      launch_chained(pad_rows_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)m), dim3(256), 0, s, begin, dst,
-                     rows, cols, o.worker_stride, o.row_stride, pitch, begin, end);
-  o = GatedOperand{dst, rows * pitch, pitch};
-  return e;
+// Replaces those of the operands [m][rows][cols] that TMA cannot take by copies in rows of
+// round8(cols) from ws on.
+struct Wanted {
+  GatedOperand* o;
+  int64_t rows;
+};
+cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws, cudaStream_t s) {
+  PadOperands all{};
+  all.cols = cols;
+  all.pitch = round8(cols);
+  int n = 0;
+  int64_t most_rows = 0;
+  for (int i = 0; i < count; ++i) {
+    GatedOperand& o = *wanted[i].o;
+    const int64_t rows = wanted[i].rows;
+    if (tma_ready(o, rows, m)) continue;
+    const uint16_t* begin = static_cast<const uint16_t*>(o.p);
+    const uint16_t* end = begin + (m > 1 ? (m - 1) * o.worker_stride : 0) + (rows > 1 ? (rows - 1) * o.row_stride : 0) + cols;
+    uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
+    ws += round256((size_t)m * rows * all.pitch * 2);
+    all.op[n++] = PadOperand{begin, end, dst, rows, o.worker_stride, o.row_stride};
+    o = GatedOperand{dst, rows * all.pitch, all.pitch};
+    most_rows = rows > most_rows ? rows : most_rows;
+  }
+  if (n == 0) return cudaSuccess;
+  const int64_t want = (most_rows * (all.pitch / 8) + 255) / 256, most = (148 * 16 + m - 1) / m;
+  return launch_chained(pad_rows_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)m, (unsigned)n), dim3(256), 0, s, all);
 }
+
+// Rows of A worth loading: with fewer than 128 tokens the rest of the tile stays what it was (it
+// reaches only accumulator rows that are not stored).
+int loaded_rows(int64_t T) { return T >= kBM ? kBM : (int)round8(T); }
 
 bool whole_pieces(const void* p, int64_t cols) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && cols % 8 == 0; }
 
@@ -639,6 +762,15 @@ cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* d
                         static_cast<const T*>(a.pre), static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec);
 }
 
+template <typename T>
+cudaError_t few(const GatedForward& a, cudaStream_t s) {
+  const bool vec = a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m) && tma_ready(a.wu, a.F, a.m);
+  auto k = a.T == 1 ? (vec ? gated_few_kernel<T, 1, true> : gated_few_kernel<T, 1, false>)
+                    : (vec ? gated_few_kernel<T, kFewTokens, true> : gated_few_kernel<T, kFewTokens, false>);
+  return launch_chained(k, dim3((unsigned)((a.F + 7) / 8), (unsigned)a.m), dim3(256), 0, s, a.x, a.wg, a.wu, (int)a.T, a.D, a.F,
+                        a.act, static_cast<T*>(a.h), static_cast<T*>(a.pre), round8(a.F));
+}
+
 #define OLSGD_STEP(call)                    \
   do {                                      \
     const cudaError_t e_ = (call);          \
@@ -648,6 +780,7 @@ cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* d
 }  // namespace
 
 size_t gated_workspace(const GatedShape& d, bool backward, bool copies) {
+  if (!backward && d.T <= kFewTokens) return 0;
   const int64_t m = d.m, T = d.T, D = d.D, F = d.F;
   const size_t copied = copies ? round256((size_t)m * T * round8(D) * 2) + 2 * round256((size_t)m * F * round8(D) * 2) : 0;
   return copied + (backward ? 2 * round256((size_t)m * T * round8(F) * 2) : 0);
@@ -658,10 +791,10 @@ bool gated_needs_copies(const GatedShape& d, const GatedOperand& x, const GatedO
 }
 
 cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
+  if (a.T <= kFewTokens) return a.f16 ? few<__half>(a, s) : few<__nv_bfloat16>(a, s);
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
-  OLSGD_STEP(ready(a.x, a.T, a.D, a.m, &ws, s));
-  OLSGD_STEP(ready(a.wg, a.F, a.D, a.m, &ws, s));
-  OLSGD_STEP(ready(a.wu, a.F, a.D, a.m, &ws, s));
+  const Wanted wanted[] = {{&a.x, a.T}, {&a.wg, a.F}, {&a.wu, a.F}};
+  OLSGD_STEP(make_ready(wanted, 3, a.D, a.m, ws, s));
   GatedArgs g{};
   g.num_kb = (int)((a.D + kBK - 1) / kBK);
   g.problems = (int)a.m;
@@ -676,7 +809,8 @@ cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
   const Shape sh = shape_for<FORWARD>(g);
   GatedMaps maps;
   const int b_rows = sh.bn / 2;
-  if (!make_map16(&maps.a0, a.x, a.D, a.T, a.m, kBM, a.f16) || !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, b_rows, a.f16) ||
+  g.a_rows = loaded_rows(a.T);
+  if (!make_map16(&maps.a0, a.x, a.D, a.T, a.m, g.a_rows, a.f16) || !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, b_rows, a.f16) ||
       !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, b_rows, a.f16))
     return cudaErrorInvalidValue;
   maps.a1 = maps.a0;
@@ -690,11 +824,12 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   void* da = ws;
   void* db = ws + part;
   ws += 2 * part;
+  const Wanted wanted[] = {{&a.x, a.T}, {&a.wg, a.F}, {&a.wu, a.F}};   // x for the weights' gradients, the weights for dx
+  const int from = a.dwg ? 0 : 1, to = a.dx ? 3 : 1;
+  OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s));
   OLSGD_STEP(a.f16 ? elementwise<__half>(a, pitch, da, db, s) : elementwise<__nv_bfloat16>(a, pitch, da, db, s));
   const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
   if (a.dx) {
-    OLSGD_STEP(ready(a.wg, a.F, a.D, a.m, &ws, s));
-    OLSGD_STEP(ready(a.wu, a.F, a.D, a.m, &ws, s));
     GatedArgs g{};
     g.kb_half = (int)((a.F + kBK - 1) / kBK);
     g.num_kb = 2 * g.kb_half;
@@ -705,13 +840,13 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
     g.out_vec = whole_pieces(a.dx, a.D);
     g.out0 = a.dx;
     GatedMaps maps;
-    if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, kBM, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, kBM, a.f16) ||
+    g.a_rows = loaded_rows(a.T);
+    if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, g.a_rows, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, g.a_rows, a.f16) ||
         !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, kBK, a.f16) || !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, kBK, a.f16))
       return cudaErrorInvalidValue;
     OLSGD_STEP(launch_mode<DX>(shape_for<DX>(g), maps, g, s));
   }
   if (a.dwg) {
-    OLSGD_STEP(ready(a.x, a.T, a.D, a.m, &ws, s));
     GatedArgs g{};
     g.num_kb = (int)((a.T + kBK - 1) / kBK);
     g.problems = (int)(2 * a.m);
