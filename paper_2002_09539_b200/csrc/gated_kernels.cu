@@ -199,11 +199,13 @@ __device__ __forceinline__ Tile tile_at(const GatedArgs& g, int64_t t) {
   return r;
 }
 
-// Arrives on the barrier at this offset in the pair's leader.
+// Arrives on the barrier at this offset in the pair's leader.  What it orders are this warp's reads
+// of tensor memory, which have completed (tcgen05.wait::ld): no cluster-wide release, which
+// would wait for the results on their way to global memory too (3 us a tile).
 __device__ __forceinline__ void arrive_leader(uint32_t bar) {
   uint32_t remote;
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(bar));
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
 }
 
 template <int ACT>
