@@ -5,8 +5,9 @@
 //
 // Two launches bound by HBM: the first reads every gradient and leaves one partial sum per
 // CTA, the second adds its worker's partial sums in a fixed order (every CTA for itself: a few
-// hundred numbers), reads the gradients again and writes.  Squares and sums are held in fp64:
-// no gradient of any type over- or underflows them, and the conversions hide behind the loads.
+// hundred numbers), reads the gradients again and writes.  Sums are held in fp64 (eight
+// squares of 16-bit values in fp32 first, where that is safe): no gradient of any type over- or
+// underflows them, and the conversions hide behind the loads.
 // The second kernel walks the tiles in the opposite order, so that what the first one read
 // last is still in L2 when it is read again.  No atomics: the same bits every time.
 //
@@ -21,10 +22,10 @@ namespace {
 using namespace op;
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;                 // 16-byte loads a thread has in flight
+constexpr int kUnroll = 8;                 // 16-byte loads a thread has in flight
+constexpr int kCtasPerSm = 4;              // resident, and launched: a fifth in a second wave would run alone
 constexpr int kTilePieces = kThreads * kUnroll;
 constexpr int kMaxTensors = 256;
-constexpr int kTargetCtas = 148 * 8;       // 8 CTAs of 256 threads are resident per multiprocessor
 
 struct Item {
   const void* in;
@@ -50,32 +51,55 @@ __device__ __forceinline__ int find_item(const Items& it, int64_t tile) {
   return lo;
 }
 
+// A tile's pieces of this thread; zeros past the row's ends.
+template <typename T>
+__device__ __forceinline__ void load_tile(const T* row, int64_t j0, int64_t n, uint4* w) {
+  constexpr int V = Elem<T>::kVec;
+  if (j0 >= 0 && j0 + ((kUnroll - 1) * kThreads + 1) * V <= n) {   // one address, constant distances
+    const uint4* p = reinterpret_cast<const uint4*>(row + j0);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) w[u] = p[u * kThreads];
+  } else {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) w[u] = load_raw<T>(row, j0 + (int64_t)u * kThreads * V, n, 0);
+  }
+}
+
 template <typename T>
 __device__ __forceinline__ double tile_square_sum(const Item& it, int64_t worker, int64_t tile) {
   constexpr int V = Elem<T>::kVec;
   const T* row = static_cast<const T*>(it.in) + worker * it.in_stride;
-  const int shift = row_shift(row);
-  const int64_t q0 = tile * kTilePieces + threadIdx.x;
+  uint4 w[kUnroll];
+  load_tile<T>(row, (tile * kTilePieces + threadIdx.x) * V - row_shift(row), it.n, w);
   double s = 0.0;
-  float v[kUnroll][V];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    const int64_t j = (q0 + u * kThreads) * V - shift;
-    if (j >= 0 && j + V <= it.n) {
-      // normal priority: the second kernel reads it again
-      Elem<T>::unpack(ld16(row + j), v[u]);
-    } else {
+    // Converting every element to fp64 would take longer than loading it.  Squares of 16-bit
+    // values are exact in fp32 and eight of them are added there; where that sum leaves fp32's
+    // comfortable range (or is zero) they are taken in fp64 after all.
+    if constexpr (V == 8) {
+      f32x2 p = raw_pair<T>(w[u], 0), q = mul2(p, p);
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[u][e] = (j + e >= 0 && j + e < it.n) ? Elem<T>::to_float(row[j + e]) : 0.f;
+      for (int e = 1; e < 4; ++e) {
+        p = raw_pair<T>(w[u], e);
+        q = fma2(p, p, q);
+      }
+      float lo, hi;
+      unpack2f(q, lo, hi);
+      lo += hi;
+      if (lo > 1e-20f && lo < 1e30f) {
+        s += (double)lo;
+        continue;
+      }
     }
-  }
-#pragma unroll
-  for (int u = 0; u < kUnroll; ++u)
+    float v[V];
+    Elem<T>::unpack(w[u], v);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const double d = (double)v[u][e];
+      const double d = (double)v[e];
       s = fma(d, d, s);
     }
+  }
   return s;
 }
 
@@ -92,7 +116,7 @@ __device__ __forceinline__ double block_sum(double s) {
 }
 
 // CTA (b, worker): tiles b, b + gridDim.x, ... of the worker's list.
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
 square_sum_kernel(const __grid_constant__ Items it, double* __restrict__ part, int part_ld, int part_off) {
   launch_gate();
   const int64_t worker = blockIdx.y;
@@ -119,15 +143,16 @@ __device__ __forceinline__ void scale_tile(const Item& it, int64_t worker, int64
   constexpr int kStoreBytes = V * (int)sizeof(TO) < 16 ? V * (int)sizeof(TO) : 16;
   const bool aligned =
       ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)shift * sizeof(TO)) & (kStoreBytes - 1)) == 0;
-  const int64_t q0 = tile * kTilePieces + threadIdx.x;
-  float v[kUnroll][V];
-#pragma unroll
-  for (int u = 0; u < kUnroll; ++u) load_piece<TI>(row, (q0 + u * kThreads) * V - shift, it.n, 0.f, v[u]);
+  const int64_t j0 = (tile * kTilePieces + threadIdx.x) * V - shift;
+  uint4 w[kUnroll];
+  load_tile<TI>(row, j0, it.n, w);
+  const f32x2 cc = pack2f(c, c);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
+    float v[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[u][e] *= c;
-    store_floats<TO, V>(out, (q0 + u * kThreads) * V - shift, it.n, aligned, v[u]);
+    for (int e = 0; e < V / 2; ++e) unpack2f(mul2(raw_pair<TI>(w[u], e), cc), v[2 * e], v[2 * e + 1]);
+    store_floats<TO, V>(out, j0 + (int64_t)u * kThreads * V, it.n, aligned, v);
   }
 }
 
@@ -138,7 +163,7 @@ __device__ __forceinline__ void scale_tile_to(const Item& it, int64_t worker, in
   else scale_tile<TI, __half>(it, worker, tile, c);
 }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
 clip_scale_kernel(const __grid_constant__ Items it, const double* __restrict__ part, int part_ld, int n_part,
                   float max_norm, float* __restrict__ norms) {
   launch_gate();
@@ -162,7 +187,10 @@ clip_scale_kernel(const __grid_constant__ Items it, const double* __restrict__ p
   }
 }
 
-int ctas_per_worker(int32_t m) { return m >= kTargetCtas ? 1 : kTargetCtas / m; }
+int ctas_per_worker(int32_t m) {
+  const int room = kCtasPerSm * 148;
+  return m >= room ? 1 : room / m;
+}
 
 // Descriptors of tensors [first, first + count).
 void fill(Items& it, const olsgd_clip_tensor* t, int32_t first, int32_t count) {

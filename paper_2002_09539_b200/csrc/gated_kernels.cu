@@ -558,9 +558,11 @@ struct PadOperands {
 __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ PadOperands all) {
   launch_gate();
   const PadOperand& o = all.op[blockIdx.z];
-  const int64_t cols = all.cols, per_row = all.pitch / 8, n = o.rows * per_row;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per_row, j = (i - r * per_row) * 8;
+  const int64_t cols = all.cols;
+  // a warp per row
+  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < o.rows; r += (int64_t)gridDim.x * 8)
+#pragma unroll 4
+  for (int64_t j = (threadIdx.x & 31) * 8; j < all.pitch; j += 256) {
     const uint16_t* src = o.begin + (int64_t)blockIdx.y * o.in_worker + r * o.in_row + j;
     const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
     const uint16_t* base = src - off;
@@ -591,17 +593,24 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ P
   }
 }
 
+constexpr int kStretch = 512;
 // da = dh b act'(a), db = dh act(a); a, b, da, db have rows of `pitch`.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const T* __restrict__ pre,
                       T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec) {
   launch_gate();
-  const int64_t per_row = pitch / 8, n = rows * per_row;
   const T* dh_w = dh + (int64_t)blockIdx.y * dh_worker;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per_row, j = (i - r * per_row) * 8;
-    const int64_t wr = (int64_t)blockIdx.y * rows + r;
+  // a warp per stretch of kStretch columns of a row
+  const int64_t stretches = (pitch + kStretch - 1) / kStretch;
+  const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t r = at / stretches, j_begin = (at - r * stretches) * kStretch;
+  if (r >= rows) return;
+  const int64_t wr = (int64_t)blockIdx.y * rows + r;
+#pragma unroll
+  for (int q = 0; q < kStretch / 256; ++q) {
+    const int64_t j = j_begin + q * 256 + (threadIdx.x & 31) * 8;
+    if (j >= pitch) break;
     float a[8], b[8], d[8], va[8], vb[8];
     Elem<T>::unpack(ld16_stream(pre + wr * 2 * pitch + j), a);
     Elem<T>::unpack(ld16_stream(pre + wr * 2 * pitch + pitch + j), b);
@@ -740,7 +749,7 @@ cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m,
     most_rows = rows > most_rows ? rows : most_rows;
   }
   if (n == 0) return cudaSuccess;
-  const int64_t want = (most_rows * (all.pitch / 8) + 255) / 256, most = (148 * 16 + m - 1) / m;
+  const int64_t want = (most_rows + 7) / 8, most = 1 << 20;
   return launch_chained(pad_rows_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)m, (unsigned)n), dim3(256), 0, s, all);
 }
 
@@ -752,9 +761,8 @@ bool whole_pieces(const void* p, int64_t cols) { return (reinterpret_cast<uintpt
 
 template <typename T>
 cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, cudaStream_t s) {
-  const int64_t n = a.T * (pitch / 8);
-  const int64_t want = (n + 255) / 256, most = (148 * 8 + a.m - 1) / a.m;
-  const dim3 grid((unsigned)(want < most ? want : most), (unsigned)a.m);
+  const int64_t warps = a.T * ((pitch + kStretch - 1) / kStretch);
+  const dim3 grid((unsigned)((warps + 7) / 8), (unsigned)a.m);
   const bool vec = a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m);
   auto k = a.act == OLSGD_ACT_SILU   ? gated_backward_kernel<T, OLSGD_ACT_SILU>
            : a.act == OLSGD_ACT_GELU ? gated_backward_kernel<T, OLSGD_ACT_GELU>

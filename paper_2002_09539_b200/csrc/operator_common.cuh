@@ -172,8 +172,8 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
 
 // The piece that starts at element j as it lies in memory; elements outside [0, n) are `fill`
 // (the bits of one element).
-template <typename T>
-__device__ __forceinline__ uint4 load_raw(const T* row, int j, int n, uint32_t fill) {
+template <typename T, typename Index>
+__device__ __forceinline__ uint4 load_raw(const T* row, Index j, Index n, uint32_t fill) {
   constexpr int V = Elem<T>::kVec;
   if (j >= 0 && j + V <= n) return ld16_stream(row + j);
   uint32_t w[4];
@@ -183,7 +183,7 @@ __device__ __forceinline__ uint4 load_raw(const T* row, int j, int n, uint32_t f
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int k = j + 2 * e;
+      const Index k = j + 2 * e;
       const uint32_t lo = (k >= 0 && k < n) ? reinterpret_cast<const uint16_t*>(row)[k] : fill;
       const uint32_t hi = (k + 1 >= 0 && k + 1 < n) ? reinterpret_cast<const uint16_t*>(row)[k + 1] : fill;
       w[e] = lo | (hi << 16);

@@ -226,13 +226,13 @@ def test_token_logprobs_batch_dims_empty_batches_and_refusals():
 
 def _check_clip(grads, max_norm, out, norms):
     whole = torch.stack([g.double().flatten(1).square().sum(dim=1) for g in grads]).sum(dim=0).sqrt()
-    # squares and sums in 64 bits: the norm is rounded once
-    assert bool(((norms.double() - whole).abs() <= whole * 2 * U).all())
+    # sums in 64 bits, of eight exact squares added up in fp32 in four roundings (half of that in the root); the norm is rounded once
+    assert bool(((norms.double() - whole).abs() <= whole * 3.01 * U).all())
     c = torch.clamp(max_norm / (whole + 1e-6), max=1.0)
     for g, o in zip(grads, out):
         want = g.double() * c.view(-1, *[1] * (g.dim() - 1))
-        # the factor and the product are rounded to fp32, the result to its type
-        tol = want.abs() * (3 * U + torch.finfo(o.dtype).eps / 2) + torch.finfo(o.dtype).smallest_normal * torch.finfo(o.dtype).eps
+        # the norm as above; the factor and the product are rounded to fp32, the result to its type
+        tol = want.abs() * (4.6 * U + torch.finfo(o.dtype).eps / 2) + torch.finfo(o.dtype).smallest_normal * torch.finfo(o.dtype).eps
         assert bool(((o.double() - want).abs() <= tol).all())
 
 
