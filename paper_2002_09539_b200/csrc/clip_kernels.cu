@@ -26,6 +26,7 @@ constexpr int kUnroll = 8;                 // 16-byte loads a thread has in flig
 constexpr int kCtasPerSm = 4;              // resident, and launched: a fifth in a second wave would run alone
 constexpr int kTilePieces = kThreads * kUnroll;
 constexpr int kMaxTensors = 256;
+constexpr int64_t kKeepBytes = 80LL << 20;
 
 struct Item {
   const void* in;
@@ -53,12 +54,12 @@ __device__ __forceinline__ int find_item(const Items& it, int64_t tile) {
 
 // A tile's pieces of this thread; zeros past the row's ends.
 template <typename T>
-__device__ __forceinline__ void load_tile(const T* row, int64_t j0, int64_t n, uint4* w) {
+__device__ __forceinline__ void load_tile(const T* row, int64_t j0, int64_t n, bool again, uint4* w) {
   constexpr int V = Elem<T>::kVec;
   if (j0 >= 0 && j0 + ((kUnroll - 1) * kThreads + 1) * V <= n) {   // one address, constant distances
     const uint4* p = reinterpret_cast<const uint4*>(row + j0);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) w[u] = p[u * kThreads];
+    for (int u = 0; u < kUnroll; ++u) w[u] = again ? ld16(p + u * kThreads) : ld16_stream(p + u * kThreads);
   } else {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) w[u] = load_raw<T>(row, j0 + (int64_t)u * kThreads * V, n, 0);
@@ -66,11 +67,11 @@ __device__ __forceinline__ void load_tile(const T* row, int64_t j0, int64_t n, u
 }
 
 template <typename T>
-__device__ __forceinline__ double tile_square_sum(const Item& it, int64_t worker, int64_t tile) {
+__device__ __forceinline__ double tile_square_sum(const Item& it, int64_t worker, int64_t tile, bool again) {
   constexpr int V = Elem<T>::kVec;
   const T* row = static_cast<const T*>(it.in) + worker * it.in_stride;
   uint4 w[kUnroll];
-  load_tile<T>(row, (tile * kTilePieces + threadIdx.x) * V - row_shift(row), it.n, w);
+  load_tile<T>(row, (tile * kTilePieces + threadIdx.x) * V - row_shift(row), it.n, again, w);
   double s = 0.0;
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
@@ -120,13 +121,16 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 square_sum_kernel(const __grid_constant__ Items it, double* __restrict__ part, int part_ld, int part_off) {
   launch_gate();
   const int64_t worker = blockIdx.y;
+  // what the second kernel will find in L2: the last of what is read here, at normal priority
+  const int64_t keep = kKeepBytes / (kTilePieces * 16) / gridDim.y;
   double s = 0.0;
   for (int64_t t = blockIdx.x; t < it.tiles; t += gridDim.x) {
     const Item& item = it.item[find_item(it, t)];
     const int64_t tile = t - item.first_tile;
-    if (item.in_dtype == OLSGD_F32) s += tile_square_sum<float>(item, worker, tile);
-    else if (item.in_dtype == OLSGD_BF16) s += tile_square_sum<__nv_bfloat16>(item, worker, tile);
-    else s += tile_square_sum<__half>(item, worker, tile);
+    const bool again = t >= it.tiles - keep;
+    if (item.in_dtype == OLSGD_F32) s += tile_square_sum<float>(item, worker, tile, again);
+    else if (item.in_dtype == OLSGD_BF16) s += tile_square_sum<__nv_bfloat16>(item, worker, tile, again);
+    else s += tile_square_sum<__half>(item, worker, tile, again);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) part[worker * part_ld + part_off + blockIdx.x] = s;
@@ -145,14 +149,14 @@ __device__ __forceinline__ void scale_tile(const Item& it, int64_t worker, int64
       ((reinterpret_cast<uintptr_t>(out) - (uintptr_t)shift * sizeof(TO)) & (kStoreBytes - 1)) == 0;
   const int64_t j0 = (tile * kTilePieces + threadIdx.x) * V - shift;
   uint4 w[kUnroll];
-  load_tile<TI>(row, j0, it.n, w);
+  load_tile<TI>(row, j0, it.n, false, w);
   const f32x2 cc = pack2f(c, c);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
     float v[V];
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) unpack2f(mul2(raw_pair<TI>(w[u], e), cc), v[2 * e], v[2 * e + 1]);
-    store_floats<TO, V>(out, j0 + (int64_t)u * kThreads * V, it.n, aligned, v);
+    store_floats<TO, V, true>(out, j0 + (int64_t)u * kThreads * V, it.n, aligned, v);
   }
 }
 

@@ -106,7 +106,8 @@ __device__ __forceinline__ void load_piece(const T* row, int64_t j, int64_t n, f
 
 // N floats to row[j ..], where the caller knows whether row + j starts on a boundary that
 // whole pieces can be stored at; elements outside [0, n) are left alone.
-template <typename T, int N>
+// ONCE: results that nothing reads soon; their lines are the first that L2 gives up.
+template <typename T, int N, bool ONCE = false>
 __device__ __forceinline__ void store_floats(T* row, int64_t j, int64_t n, bool aligned, const float* v) {
   constexpr int V = Elem<T>::kVec;
   if (aligned && j >= 0 && j + N <= n) {
@@ -114,15 +115,23 @@ __device__ __forceinline__ void store_floats(T* row, int64_t j, int64_t n, bool 
       // one 32-byte store (a whole sector) where the address allows it
       if ((reinterpret_cast<uintptr_t>(row + j) & 31) == 0) {
         const uint4 a = Elem<T>::pack(v), b = Elem<T>::pack(v + V);
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + j), "r"(a.x), "r"(a.y), "r"(a.z),
-                     "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
-                     : "memory");
+        if constexpr (ONCE)
+          asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + j), "r"(a.x), "r"(a.y),
+                       "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                       : "memory");
+        else
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + j), "r"(a.x), "r"(a.y),
+                       "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                       : "memory");
         return;
       }
     }
     if constexpr (N >= V) {
 #pragma unroll
-      for (int q = 0; q < N / V; ++q) reinterpret_cast<uint4*>(row + j)[q] = Elem<T>::pack(v + q * V);
+      for (int q = 0; q < N / V; ++q) {
+        if constexpr (ONCE) __stcs(reinterpret_cast<uint4*>(row + j) + q, Elem<T>::pack(v + q * V));
+        else reinterpret_cast<uint4*>(row + j)[q] = Elem<T>::pack(v + q * V);
+      }
     } else {
       float w[V];
 #pragma unroll
