@@ -66,30 +66,30 @@ embedding_kernel(const T* __restrict__ table, int64_t V, int64_t D, int64_t tabl
 
 // -------------------------------------------------------------------------------- sort
 // Entries are (id << 32 | position); ids outside [0, V) become V and end up last.
-constexpr int kSortThreads = 256;
+constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortItems = 8;                              // entries per thread
 constexpr int kSortTile = kSortThreads * kSortItems;       // entries per CTA
 constexpr int kBins = 256;
-
-__device__ __forceinline__ uint64_t entry_of(const int32_t* ids, int64_t t, uint32_t V) {
-  const int32_t id = ids[t];
-  const uint32_t key = id >= 0 && (uint32_t)id < V ? (uint32_t)id : V;
-  return ((uint64_t)key << 32) | (uint32_t)t;
-}
+constexpr int kSortCluster = 8;                            // CTAs that sort a list in one launch
 
 struct SortArgs {
   const int32_t* ids;        // [m][T]
   const uint64_t* in;        // [m][T], or null: the ids themselves
   uint64_t* out;             // [m][T]
   uint32_t* counts;          // [m][kBins][tiles]
+  uint32_t* joins;           // counter that the summing kernel starts from: zeroed here
   int64_t T;
   uint32_t V;
   int tiles, shift;
 };
 
-__device__ __forceinline__ uint64_t entry_at(const SortArgs& a, int64_t worker, int64_t t) {
-  return a.in ? a.in[worker * a.T + t] : entry_of(a.ids + worker * a.T, t, a.V);
+// (through L2: the other CTAs of a cluster wrote it)
+__device__ __forceinline__ uint64_t entry_at(const SortArgs& a, const uint64_t* in, int64_t worker, int64_t t) {
+  if (in) return __ldcg(reinterpret_cast<const unsigned long long*>(in + worker * a.T + t));
+  const int32_t id = a.ids[worker * a.T + t];
+  const uint32_t key = id >= 0 && (uint32_t)id < a.V ? (uint32_t)id : a.V;
+  return ((uint64_t)key << 32) | (uint32_t)t;
 }
 __device__ __forceinline__ uint32_t digit_of(uint64_t e, int shift) { return (uint32_t)(e >> (32 + shift)) & (kBins - 1); }
 
@@ -98,87 +98,156 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
   __shared__ uint32_t hist[kBins];
   launch_gate();
   const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile;
-  hist[threadIdx.x] = 0;
+  if (threadIdx.x < kBins) hist[threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kSortItems; ++i) {
     const int64_t t = t0 + i * kSortThreads + threadIdx.x;
-    if (t < a.T) atomicAdd(&hist[digit_of(entry_at(a, worker, t), a.shift)], 1u);
+    if (t < a.T) atomicAdd(&hist[digit_of(entry_at(a, a.in, worker, t), a.shift)], 1u);
   }
   __syncthreads();
-  a.counts[(worker * kBins + threadIdx.x) * a.tiles + blockIdx.x] = hist[threadIdx.x];
+  if (threadIdx.x < kBins) a.counts[(worker * kBins + threadIdx.x) * a.tiles + blockIdx.x] = hist[threadIdx.x];
 }
 
-// Places a tile's entries: where its digit starts among all tiles, plus what earlier tiles, earlier
-// warps and earlier entries of the warp hold of the digit.  A single tile counts for itself.
-__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs a) {
-  __shared__ uint32_t warp_count[kSortWarps][kBins];
-  __shared__ uint32_t start[kBins];
-  __shared__ uint32_t warp_total[kSortWarps];
-  launch_gate();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + warp * (32 * kSortItems);
-  for (int b = lane; b < kBins; b += 32) warp_count[warp][b] = 0;
-  __syncwarp();
+// One tile of one pass.  An entry's place is where its digit starts among all tiles, plus what
+// earlier tiles, earlier warps and earlier entries of the warp hold of the digit.
+struct TileSort {
+  uint32_t warp_count[kSortWarps][kBins];
+  uint32_t start[kBins];
+  uint32_t warp_total[kBins / 32];
+};
+struct Ranked {
   uint64_t e[kSortItems];
-  uint32_t rank[kSortItems];
+  uint32_t rank[kSortItems];   // among the warp's entries of the digit
+};
+
+__device__ __forceinline__ void rank_tile(const SortArgs& a, const uint64_t* in, int shift, int64_t worker, int64_t t0, TileSort& sh,
+                                          Ranked& r) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int b = lane; b < kBins; b += 32) sh.warp_count[warp][b] = 0;
 #pragma unroll
   for (int i = 0; i < kSortItems; ++i) {
     const int64_t t = t0 + i * 32 + lane;
-    e[i] = t < a.T ? entry_at(a, worker, t) : ~0ull;
+    r.e[i] = t < a.T ? entry_at(a, in, worker, t) : ~0ull;
   }
+  __syncwarp();
 #pragma unroll
   for (int i = 0; i < kSortItems; ++i) {
     const bool live = t0 + i * 32 + lane < a.T;
-    const uint32_t d = live ? digit_of(e[i], a.shift) : kBins;   // dead lanes match each other only
+    const uint32_t d = live ? digit_of(r.e[i], shift) : kBins;   // dead lanes match each other only
     const uint32_t same = __match_any_sync(0xffffffffu, d);
-    const uint32_t before = live ? warp_count[warp][d] : 0;
-    rank[i] = before + __popc(same & ((1u << lane) - 1));
+    const uint32_t before = live ? sh.warp_count[warp][d] : 0;
+    r.rank[i] = before + __popc(same & ((1u << lane) - 1));
     __syncwarp();
-    if (live && (same & ((1u << lane) - 1)) == 0) warp_count[warp][d] = before + __popc(same);
+    if (live && (same & ((1u << lane) - 1)) == 0) sh.warp_count[warp][d] = before + __popc(same);
     __syncwarp();
   }
   __syncthreads();
-  // thread b: digit b.  Sum over all tiles, and over the earlier ones.
-  const int b = threadIdx.x;
-  uint32_t total = 0, earlier = 0;
-  if (a.tiles == 1) {
+}
+
+// total, earlier: what thread b < kBins knows of digit b over all tiles, and over the earlier ones.
+__device__ __forceinline__ void place_tile(const SortArgs& a, uint64_t* out, int shift, int64_t worker, int64_t t0, uint32_t total,
+                                           uint32_t earlier, TileSort& sh, const Ranked& r) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = threadIdx.x;
+  uint32_t scan = total;   // inclusive over the digits
+  if (b < kBins) {
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) total += warp_count[w][b];
-  } else {
-    const uint32_t* c = a.counts + (worker * kBins + b) * a.tiles;
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t n = __shfl_up_sync(0xffffffffu, scan, o);
+      if (lane >= o) scan += n;
+    }
+    if (lane == 31) sh.warp_total[warp] = scan;
+  }
+  __syncthreads();
+  if (b < kBins) {
+    uint32_t base = scan - total + earlier;
+    for (int w = 0; w < warp; ++w) base += sh.warp_total[w];
+    sh.start[b] = base;
+    // counts of a warp become what the warps before it hold
+    uint32_t run = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+      const uint32_t n = sh.warp_count[w][b];
+      sh.warp_count[w][b] = run;
+      run += n;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSortItems; ++i) {
+    if (t0 + i * 32 + lane < a.T) {
+      const uint32_t d = digit_of(r.e[i], shift);
+      out[worker * a.T + sh.start[d] + sh.warp_count[warp][d] + r.rank[i]] = r.e[i];
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs a) {
+  __shared__ TileSort sh;
+  launch_gate();
+  const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + (threadIdx.x >> 5) * (32 * kSortItems);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.joins = 0;
+  Ranked r;
+  rank_tile(a, a.in, a.shift, worker, t0, sh, r);
+  uint32_t total = 0, earlier = 0;
+  if (threadIdx.x < kBins) {
+    const uint32_t* c = a.counts + (worker * kBins + threadIdx.x) * a.tiles;
+#pragma unroll 4
     for (int i = 0; i < a.tiles; ++i) {
       const uint32_t n = c[i];
       total += n;
       if (i < (int)blockIdx.x) earlier += n;
     }
   }
-  uint32_t scan = total;   // inclusive over the digits
+  place_tile(a, a.out, a.shift, worker, t0, total, earlier, sh, r);
+}
+
+// Lists of up to kSortCluster tiles: a cluster of CTAs, one tile each, makes all passes in one
+// launch and exchanges its counts through distributed shared memory (16384 tokens, two passes:
+// SORT_ONE us against SORT_MANY us as a count and a placing launch per pass).  `other` is the list that the
+// passes alternate with.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t cta) {
+  uint32_t addr = static_cast<uint32_t>(__cvta_generic_to_shared(p)), v;
+  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(addr) : "r"(cta));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const SortArgs a, uint64_t* first, uint64_t* second, int passes) {
+  __shared__ TileSort sh;
+  __shared__ uint32_t hist[kBins];
+  launch_gate();
+  const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + (threadIdx.x >> 5) * (32 * kSortItems);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.joins = 0;
+  const uint64_t* in = nullptr;
+  uint64_t* out = first;
+  for (int p = 0; p < passes; ++p) {
+    Ranked r;
+    rank_tile(a, in, 8 * p, worker, t0, sh, r);
+    const int b = threadIdx.x;
+    if (b < kBins) {
+      uint32_t n = 0;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t n = __shfl_up_sync(0xffffffffu, scan, o);
-    if (lane >= o) scan += n;
-  }
-  if (lane == 31) warp_total[warp] = scan;
-  __syncthreads();
-  uint32_t base = scan - total + earlier;
-  for (int w = 0; w < warp; ++w) base += warp_total[w];
-  start[b] = base;
-  // counts of a warp become what the warps before it hold
-  uint32_t run = 0;
-#pragma unroll
-  for (int w = 0; w < kSortWarps; ++w) {
-    const uint32_t n = warp_count[w][b];
-    warp_count[w][b] = run;
-    run += n;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    if (t0 + i * 32 + lane < a.T) {
-      const uint32_t d = digit_of(e[i], a.shift);
-      a.out[worker * a.T + start[d] + warp_count[warp][d] + rank[i]] = e[i];
+      for (int w = 0; w < kSortWarps; ++w) n += sh.warp_count[w][b];
+      hist[b] = n;
     }
+    cluster_sync();
+    uint32_t total = 0, earlier = 0;
+    if (b < kBins) {
+      for (int c = 0; c < a.tiles; ++c) {
+        const uint32_t n = ld_cluster(&hist[b], c);
+        total += n;
+        if (c < (int)blockIdx.x) earlier += n;
+      }
+    }
+    place_tile(a, out, 8 * p, worker, t0, total, earlier, sh, r);
+    __threadfence();
+    cluster_sync();   // the list is complete, and nobody reads this CTA's counts any more
+    in = out;
+    out = out == first ? second : first;
   }
 }
 
@@ -198,6 +267,8 @@ struct SumArgs {
   void* dtable;             // [m][V][D], workers out_worker apart
   int64_t out_worker;
   float* part;              // [m][chunks][2][pitch]: the row a chunk shares with the one before, with the one after
+  uint32_t* joins;          // how many chunks a row starts in that reaches past their end ...
+  uint32_t* join_list;      // ... and which: worker * chunks + chunk, in any order
   int64_t T, V, D, pitch;
   int chunks, zero_blocks;
   float scale;
@@ -318,6 +389,8 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
       const bool to_after = k + 1 == n && next == key;
       if (key < a.V) {
         if (from_before || to_after) {
+          if (!from_before && blockIdx.y == 0 && threadIdx.x == 0)
+            a.join_list[atomicAdd(a.joins, 1u)] = (uint32_t)worker * a.chunks + blockIdx.x;
           write_cols<float>(part + (from_before ? 0 : a.pitch), c0, a.D, VEC, !VEC, acc);
         } else {
           float r[kCols];
@@ -333,64 +406,64 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
   }
 }
 
-// CTA (c, column slice): the table row that starts in chunk c and reaches past its end, if
-// there is one: its part of chunk c, then the parts of the chunks that follow, each eighth of
-// them by a warp of its own, joined in a fixed order.
+// The table rows that start in one chunk and reach past its end, as listed by the summing kernel: an
+// item is such a row and a slice of its columns.  Its part of the first chunk, then the parts of the
+// chunks that follow, each eighth of them by a warp of its own, joined in a fixed order (so the
+// list's order does not matter).
 template <typename TO>
 __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumArgs a) {
+  __shared__ float4 sh[kJoinThreads / 32][32];
   launch_gate();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t worker = blockIdx.z;
-  const uint64_t* sorted = a.sorted + worker * a.T;
-  const int64_t c = blockIdx.x, last = (c + 1) * kChunk - 1;
-  if (last + 1 >= a.T) return;
-  const uint32_t key = key_at(sorted, last);
-  if (key >= a.V || key_at(sorted, last + 1) != key) return;
-  const int64_t first = c * kChunk;
-  // (a chunk that is all one row which began before it belongs to that row's first chunk)
-  if (first > 0 && key_at(sorted, first - 1) == key) return;
-  // the last chunk that holds the key: chunks ahead are probed a warp's width at a time
-  int64_t end = c + 1;
-  for (;;) {
-    const int64_t probe = end + lane;   // does chunk `probe` + 1 begin with the key?
-    const int64_t i = (probe + 1) * kChunk;
-    const bool more = i < a.T && key_at(sorted, i) == key;
-    const uint32_t yes = __ballot_sync(0xffffffffu, more);
-    const int run = yes == 0xffffffffu ? 32 : __ffs(~yes) - 1;
-    end += run;
-    if (run < 32) break;
-  }
-  const float* part = a.part + worker * a.chunks * 2 * a.pitch;
-  const int64_t col = (int64_t)blockIdx.y * kJoinCols + lane * 4;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](const float* p) {
-    const float4 v = *reinterpret_cast<const float4*>(p + col);
-    acc.x += v.x;
-    acc.y += v.y;
-    acc.z += v.z;
-    acc.w += v.w;
-  };
-  if (col < a.D) {   // (pitch is a multiple of four: whole pieces; those past D are not stored)
-    if (warp == 0) add(part + (c * 2 + 1) * a.pitch);
-#pragma unroll 4
-    for (int64_t k = c + 1 + warp; k <= end; k += kJoinThreads / 32) add(part + k * 2 * a.pitch);
-  }
-  __shared__ float4 sh[kJoinThreads / 32][32];
-  sh[warp][lane] = acc;
-  __syncthreads();
-  if (warp == 0 && col < a.D) {
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) {
-      r[0] += sh[w][lane].x;
-      r[1] += sh[w][lane].y;
-      r[2] += sh[w][lane].z;
-      r[3] += sh[w][lane].w;
+  const int64_t slices = (a.D + kJoinCols - 1) / kJoinCols, items = (int64_t)*a.joins * slices;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t at = a.join_list[item / slices];
+    const int64_t worker = at / a.chunks, c = at % a.chunks, slice = item % slices;
+    const uint64_t* sorted = a.sorted + worker * a.T;
+    const uint32_t key = key_at(sorted, (c + 1) * kChunk - 1);
+    // the last chunk that holds the key: chunks ahead are probed a warp's width at a time
+    int64_t end = c + 1;
+    for (;;) {
+      const int64_t probe = end + lane;   // does chunk `probe` + 1 begin with the key?
+      const int64_t i = (probe + 1) * kChunk;
+      const bool more = i < a.T && key_at(sorted, i) == key;
+      const uint32_t yes = __ballot_sync(0xffffffffu, more);
+      const int run = yes == 0xffffffffu ? 32 : __ffs(~yes) - 1;
+      end += run;
+      if (run < 32) break;
     }
-    TO* row = static_cast<TO*>(a.dtable) + worker * a.out_worker + (int64_t)key * a.D;
+    const float* part = a.part + worker * a.chunks * 2 * a.pitch;
+    const int64_t col = slice * kJoinCols + lane * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float* p) {
+      const float4 v = *reinterpret_cast<const float4*>(p + col);
+      acc.x += v.x;
+      acc.y += v.y;
+      acc.z += v.z;
+      acc.w += v.w;
+    };
+    if (col < a.D) {   // (pitch is a multiple of four: whole pieces; those past D are not stored)
+      if (warp == 0) add(part + (c * 2 + 1) * a.pitch);
+#pragma unroll 4
+      for (int64_t k = c + 1 + warp; k <= end; k += kJoinThreads / 32) add(part + k * 2 * a.pitch);
+    }
+    __syncthreads();   // (the item before has been read)
+    sh[warp][lane] = acc;
+    __syncthreads();
+    if (warp == 0 && col < a.D) {
+      float r[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (col + e < a.D) row[col + e] = Elem<TO>::from_float(r[e] * a.scale);
+      for (int w = 0; w < kJoinThreads / 32; ++w) {
+        r[0] += sh[w][lane].x;
+        r[1] += sh[w][lane].y;
+        r[2] += sh[w][lane].z;
+        r[3] += sh[w][lane].w;
+      }
+      TO* row = static_cast<TO*>(a.dtable) + worker * a.out_worker + (int64_t)key * a.D;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < a.D) row[col + e] = Elem<TO>::from_float(r[e] * a.scale);
+    }
   }
 }
 
@@ -401,7 +474,7 @@ int64_t chunks_of(int64_t T) { return (T + kChunk - 1) / kChunk; }
 int64_t pitch_of(int64_t D) { return (D + 3) / 4 * 4; }
 
 struct Layout {
-  size_t a, b, counts, part, total;
+  size_t a, b, counts, joins, part, total;
 };
 Layout layout_of(int64_t m, int64_t T, int64_t D) {
   Layout l;
@@ -409,7 +482,8 @@ Layout layout_of(int64_t m, int64_t T, int64_t D) {
   l.a = 0;
   l.b = list;
   l.counts = 2 * list;
-  l.part = l.counts + round256((size_t)m * kBins * tiles_of(T) * sizeof(uint32_t));
+  l.joins = l.counts + (tiles_of(T) > kSortCluster ? round256((size_t)m * kBins * tiles_of(T) * sizeof(uint32_t)) : 0);
+  l.part = l.joins + 256 + round256((size_t)m * chunks_of(T) * sizeof(uint32_t));
   l.total = l.part + round256((size_t)m * chunks_of(T) * 2 * pitch_of(D) * sizeof(float));
   return l;
 }
@@ -424,8 +498,8 @@ cudaError_t sum_rows(const SumArgs& a, int64_t m, cudaStream_t s) {
   auto k = a.vec_in && a.vec_out ? embedding_sum_kernel<TI, TO, true> : embedding_sum_kernel<TI, TO, false>;
   cudaError_t e = launch_chained(k, grid, dim3(kSumThreads), 0, s, a);
   if (e != cudaSuccess || a.chunks <= 1) return e;
-  return launch_chained(embedding_join_kernel<TO>, dim3((unsigned)a.chunks, (unsigned)((a.D + kJoinCols - 1) / kJoinCols), (unsigned)m),
-                        dim3(kJoinThreads), 0, s, a);
+  const int64_t most = m * a.chunks * ((a.D + kJoinCols - 1) / kJoinCols), room = 148 * 8;
+  return launch_chained(embedding_join_kernel<TO>, dim3((unsigned)(most < room ? most : room)), dim3(kJoinThreads), 0, s, a);
 }
 
 template <typename TI>
@@ -460,20 +534,38 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
   const Layout l = layout_of(g.m, g.T, g.D);
   uint8_t* ws = static_cast<uint8_t*>(g.ws);
   uint64_t* lists[2] = {reinterpret_cast<uint64_t*>(ws + l.a), reinterpret_cast<uint64_t*>(ws + l.b)};
-  SortArgs sort{g.ids, nullptr, nullptr, reinterpret_cast<uint32_t*>(ws + l.counts), g.T, (uint32_t)g.V, (int)tiles_of(g.T), 0};
+  uint32_t* joins = reinterpret_cast<uint32_t*>(ws + l.joins);
+  SortArgs sort{g.ids, nullptr, nullptr, reinterpret_cast<uint32_t*>(ws + l.counts), joins, g.T, (uint32_t)g.V, (int)tiles_of(g.T), 0};
   const dim3 sort_grid((unsigned)sort.tiles, (unsigned)g.m);
-  int which = 0;
-  for (int shift = 0; g.T > 0 && (g.V >> shift) > 0; shift += 8) {   // keys are 0 .. V
-    sort.shift = shift;
-    sort.out = lists[which];
-    if (sort.tiles > 1) {
-      const cudaError_t e = launch_chained(sort_count_kernel, sort_grid, dim3(kSortThreads), 0, s, sort);
+  int passes = 0;
+  while (g.T > 0 && (g.V >> (8 * passes)) > 0) ++passes;   // keys are 0 .. V
+  if (sort.tiles > kSortCluster) {
+    for (int p = 0; p < passes; ++p) {
+      sort.shift = 8 * p;
+      sort.out = lists[p & 1];
+      cudaError_t e = launch_chained(sort_count_kernel, sort_grid, dim3(kSortThreads), 0, s, sort);
       if (e != cudaSuccess) return e;
+      e = launch_chained(sort_place_kernel, sort_grid, dim3(kSortThreads), 0, s, sort);
+      if (e != cudaSuccess) return e;
+      sort.in = lists[p & 1];
     }
-    const cudaError_t e = launch_chained(sort_place_kernel, sort_grid, dim3(kSortThreads), 0, s, sort);
+  } else if (passes > 0) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = sort_grid;
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)sort.tiles;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = g_launch_overlap ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, sort_cluster_kernel, sort, lists[0], lists[1], passes);
     if (e != cudaSuccess) return e;
-    sort.in = lists[which];
-    which ^= 1;
+    sort.in = lists[(passes - 1) & 1];
   }
   SumArgs a;
   a.sorted = sort.in;
@@ -483,6 +575,8 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
   a.dtable = g.dtable;
   a.out_worker = g.dtable_worker;
   a.part = reinterpret_cast<float*>(ws + l.part);
+  a.joins = joins;
+  a.join_list = joins + 64;
   a.T = g.T;
   a.V = g.V;
   a.D = g.D;

@@ -523,7 +523,8 @@ def _check_embedding(table, ids, dout, scale, out_dtype, out=None):
 @pytest.mark.parametrize("tin,tout", [(torch.float32, torch.float32), (torch.bfloat16, torch.float32), (torch.float16, torch.float32),
                                       (torch.bfloat16, torch.bfloat16), (torch.float16, torch.float16), (torch.float32, torch.bfloat16)])
 @pytest.mark.parametrize("m,T,V,D", [(1, 1, 1, 1), (2, 5, 3, 7), (1, 31, 255, 8), (3, 33, 256, 24), (1, 2048, 1000, 16), (2, 2049, 70000, 9),
-                                     (1, 4500, 50, 1032), (2, 700, 300, 2050), (1, 64, 5, 4096)])
+                                     (1, 4500, 50, 1032), (2, 700, 300, 2050), (1, 64, 5, 4096),
+                                     (2, 4096, 257, 8), (3, 4097, 256, 8), (1, 32768, 70000, 8), (2, 32769, 500, 12)])
 def test_embedding(m, T, V, D, tin, tout):
     g = _gen(T + V + D)
     table, dout = _randn(g, (m, V, D), tin), _randn(g, (m, T, D), tin)
