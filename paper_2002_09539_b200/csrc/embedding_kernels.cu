@@ -116,26 +116,36 @@ struct TileSort {
   uint32_t start[kBins];
   uint32_t warp_total[kBins / 32];
 };
+template <int ITEMS>
 struct Ranked {
-  uint64_t e[kSortItems];
-  uint32_t rank[kSortItems];   // among the warp's entries of the digit
+  uint64_t e[ITEMS];
+  uint32_t rank[ITEMS];   // among the warp's entries of the digit
 };
 
+template <int ITEMS>
 __device__ __forceinline__ void rank_tile(const SortArgs& a, const uint64_t* in, int shift, int64_t worker, int64_t t0, TileSort& sh,
-                                          Ranked& r) {
+                                          Ranked<ITEMS>& r) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int b = lane; b < kBins; b += 32) sh.warp_count[warp][b] = 0;
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  for (int i = 0; i < ITEMS; ++i) {
     const int64_t t = t0 + i * 32 + lane;
     r.e[i] = t < a.T ? entry_at(a, in, worker, t) : ~0ull;
   }
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  for (int i = 0; i < ITEMS; ++i) {
     const bool live = t0 + i * 32 + lane < a.T;
-    const uint32_t d = live ? digit_of(r.e[i], shift) : kBins;   // dead lanes match each other only
-    const uint32_t same = __match_any_sync(0xffffffffu, d);
+    const uint32_t d = digit_of(r.e[i], shift);
+    // the live lanes with the same digit, bit by bit (a match instruction walks over the distinct
+    // digits instead)
+    uint32_t same = __ballot_sync(0xffffffffu, live);
+#pragma unroll
+    for (int bit = 0; bit < 8; ++bit) {
+      const bool set = (d >> bit) & 1;
+      const uint32_t with = __ballot_sync(0xffffffffu, set);
+      same &= set ? with : ~with;
+    }
     const uint32_t before = live ? sh.warp_count[warp][d] : 0;
     r.rank[i] = before + __popc(same & ((1u << lane) - 1));
     __syncwarp();
@@ -146,8 +156,9 @@ __device__ __forceinline__ void rank_tile(const SortArgs& a, const uint64_t* in,
 }
 
 // total, earlier: what thread b < kBins knows of digit b over all tiles, and over the earlier ones.
+template <int ITEMS>
 __device__ __forceinline__ void place_tile(const SortArgs& a, uint64_t* out, int shift, int64_t worker, int64_t t0, uint32_t total,
-                                           uint32_t earlier, TileSort& sh, const Ranked& r) {
+                                           uint32_t earlier, TileSort& sh, const Ranked<ITEMS>& r) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = threadIdx.x;
   uint32_t scan = total;   // inclusive over the digits
   if (b < kBins) {
@@ -174,7 +185,7 @@ __device__ __forceinline__ void place_tile(const SortArgs& a, uint64_t* out, int
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  for (int i = 0; i < ITEMS; ++i) {
     if (t0 + i * 32 + lane < a.T) {
       const uint32_t d = digit_of(r.e[i], shift);
       out[worker * a.T + sh.start[d] + sh.warp_count[warp][d] + r.rank[i]] = r.e[i];
@@ -187,7 +198,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
   launch_gate();
   const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + (threadIdx.x >> 5) * (32 * kSortItems);
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.joins = 0;
-  Ranked r;
+  Ranked<kSortItems> r;
   rank_tile(a, a.in, a.shift, worker, t0, sh, r);
   uint32_t total = 0, earlier = 0;
   if (threadIdx.x < kBins) {
@@ -203,9 +214,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
 }
 
 // Lists of up to kSortCluster tiles: a cluster of CTAs, one tile each, makes all passes in one
-// launch and exchanges its counts through distributed shared memory (16384 tokens, two passes:
-// SORT_ONE us against SORT_MANY us as a count and a placing launch per pass).  `other` is the list that the
-// passes alternate with.
+// launch and exchanges its counts through distributed shared memory (2 x 16384 tokens, two passes,
+// cold: 14 us against 29 us as a count and a placing launch per pass).  Tiles are half as
+// long (ITEMS = 4) where eight of those hold the list.  The passes alternate between two lists.
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -216,16 +227,17 @@ __device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t cta) 
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
+template <int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const SortArgs a, uint64_t* first, uint64_t* second, int passes) {
   __shared__ TileSort sh;
   __shared__ uint32_t hist[kBins];
   launch_gate();
-  const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + (threadIdx.x >> 5) * (32 * kSortItems);
+  const int64_t worker = blockIdx.y, t0 = ((int64_t)blockIdx.x * kSortThreads + (threadIdx.x & ~31u)) * ITEMS;
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.joins = 0;
   const uint64_t* in = nullptr;
   uint64_t* out = first;
   for (int p = 0; p < passes; ++p) {
-    Ranked r;
+    Ranked<ITEMS> r;
     rank_tile(a, in, 8 * p, worker, t0, sh, r);
     const int b = threadIdx.x;
     if (b < kBins) {
@@ -244,7 +256,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const SortAr
       }
     }
     place_tile(a, out, 8 * p, worker, t0, total, earlier, sh, r);
-    __threadfence();
     cluster_sync();   // the list is complete, and nobody reads this CTA's counts any more
     in = out;
     out = out == first ? second : first;
@@ -551,7 +562,9 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
     }
   } else if (passes > 0) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = sort_grid;
+    const bool half = g.T <= kSortCluster * kSortTile / 2;
+    if (half) sort.tiles = (int)((g.T + kSortTile / 2 - 1) / (kSortTile / 2));
+    cfg.gridDim = dim3((unsigned)sort.tiles, (unsigned)g.m);
     cfg.blockDim = dim3(kSortThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -563,7 +576,7 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = g_launch_overlap ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, sort_cluster_kernel, sort, lists[0], lists[1], passes);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, half ? sort_cluster_kernel<kSortItems / 2> : sort_cluster_kernel<kSortItems>, sort, lists[0], lists[1], passes);
     if (e != cudaSuccess) return e;
     sort.in = lists[(passes - 1) & 1];
   }
