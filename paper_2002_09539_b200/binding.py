@@ -207,10 +207,19 @@ class OverlapLocalSGD:
         _check(self.lib, self.lib.olsgd_local_step(self.ctx, loss.data_ptr() if loss is not None else None),
                self.ctx)
 
-    def local_step_with_grads(self, g):
+    def local_step_with_grads(self, g, max_norm=None):
+        """g: float32 [m][P].  With max_norm each worker's gradient is clipped to that norm first, in place
+        (olsgd_clip_grads on the context's main stream); returns the norms before clipping, float32 [m]."""
         assert g.is_cuda and g.dtype == torch.float32 and g.is_contiguous()
         assert g.numel() == self.m * self.P
+        norms = None
+        if max_norm is not None:
+            from .operators import clip_grads
+            rows = g.view(self.m, self.P)
+            with torch.cuda.stream(self.main):
+                norms = clip_grads(rows, max_norm, out=rows)[1]
         _check(self.lib, self.lib.olsgd_local_step_with_grads(self.ctx, g.data_ptr()), self.ctx)
+        return norms
 
     def local_step_host(self, Xb, yb, loss=None):
         """Xb, yb (and loss) are HOST tensors, ideally pinned.  Xb is float32, or bfloat16 for
