@@ -10,8 +10,10 @@
 // adds up a chunk's rows in fp32 registers and writes every table row whose tokens all lie
 // in the chunk.  Rows that reach over a chunk's end leave partial sums, which a third kernel adds
 // in chunk order: a token that fills half of the batch costs as much as any other.  Table rows
-// without a token are zeroed by further CTAs of the same launch.  Each sum is rounded once.
-// Bound by dout read once and the table's gradient written once.
+// without a token are zeroed meanwhile.  Each sum is rounded once.
+// Bound by dout read once and the table's gradient written once; writing the zeros is most of it
+// where the vocabulary is larger than the batch, so it runs beside the sort (which fills eight
+// multiprocessors a list and moves next to nothing).
 //
 // Ids outside [0, V) mark positions without a token: a zero row, no gradient.
 #include "operator_common.cuh"
@@ -72,6 +74,33 @@ constexpr int kSortItems = 8;                              // entries per thread
 constexpr int kSortTile = kSortThreads * kSortItems;       // entries per CTA
 constexpr int kBins = 256;
 constexpr int kSortCluster = 8;                            // CTAs that sort a list in one launch
+
+// Table rows without a token, kZeroBytes a CTA.
+constexpr int kZeroBytes = 256 << 10;
+constexpr int kZeroRowsMax = 2048;
+struct ZeroArgs {
+  void* dtable;              // [m][V][row_bytes], workers worker_bytes apart
+  int64_t V, row_bytes, worker_bytes;
+  int rows, ctas;            // rows of a CTA, CTAs of a worker
+};
+// Rows [v0, v0 + n) of a worker that are not present, a warp per row.  Zeros are the same in every
+// type: 32 bytes a lane between the boundaries, 2 at the ends.
+__device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t worker, int64_t v0, int n, const uint8_t* present) {
+  const int lane = threadIdx.x & 31;
+  char* base = static_cast<char*>(z.dtable) + worker * z.worker_bytes;
+  for (int r = threadIdx.x >> 5; r < n; r += blockDim.x >> 5) {
+    if (present[r]) continue;
+    char *p = base + (v0 + r) * z.row_bytes, *end = p + z.row_bytes;
+    char* body = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(p) + 31) & ~(uintptr_t)31);
+    if (body > end) body = end;
+    for (char* q = p + lane * 2; q < body; q += 64) *reinterpret_cast<uint16_t*>(q) = 0;
+    char* tail = body + ((end - body) & ~(int64_t)31);
+    const uint32_t o = 0;
+    for (char* q = body + lane * 32; q < tail; q += 1024)
+      asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(q), "r"(o) : "memory");
+    for (char* q = tail + lane * 2; q < end; q += 64) *reinterpret_cast<uint16_t*>(q) = 0;
+  }
+}
 
 struct SortArgs {
   const int32_t* ids;        // [m][T]
@@ -217,6 +246,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
 // launch and exchanges its counts through distributed shared memory (2 x 16384 tokens, two passes,
 // cold: 14 us against 29 us as a count and a placing launch per pass).  Tiles are half as
 // long (ITEMS = 4) where eight of those hold the list.  The passes alternate between two lists.
+// CTAs past the lists' zero table rows: each looks through the ids for its rows itself (they come
+// from L2), and so waits for no sort.
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -228,12 +259,31 @@ __device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t cta) 
   return v;
 }
 template <int ITEMS>
-__global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const SortArgs a, uint64_t* first, uint64_t* second, int passes) {
+__global__ void __launch_bounds__(kSortThreads)
+sort_cluster_kernel(const SortArgs a, uint64_t* first, uint64_t* second, int passes, int m, const ZeroArgs z) {
   __shared__ TileSort sh;
   __shared__ uint32_t hist[kBins];
+  __shared__ uint8_t present[kZeroRowsMax];
   launch_gate();
-  const int64_t worker = blockIdx.y, t0 = ((int64_t)blockIdx.x * kSortThreads + (threadIdx.x & ~31u)) * ITEMS;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.joins = 0;
+  if (blockIdx.x >= (unsigned)m * a.tiles) {
+    const int64_t at = blockIdx.x - (int64_t)m * a.tiles;
+    const int64_t worker = at / z.ctas, v0 = at % z.ctas * z.rows;
+    if (worker >= m) return;   // (the grid is a multiple of the cluster)
+    const int n = (int)(z.V - v0 < z.rows ? z.V - v0 : z.rows);
+    for (int r = threadIdx.x; r < n; r += kSortThreads) present[r] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int64_t t = threadIdx.x; t < a.T; t += kSortThreads) {
+      const int64_t r = a.ids[worker * a.T + t] - v0;
+      if (r >= 0 && r < n) present[r] = 1;
+    }
+    __syncthreads();
+    zero_rows(z, worker, v0, n, present);
+    return;
+  }
+  const int tile = blockIdx.x % a.tiles;
+  const int64_t worker = blockIdx.x / a.tiles, t0 = ((int64_t)tile * kSortThreads + (threadIdx.x & ~31u)) * ITEMS;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.joins = 0;
   const uint64_t* in = nullptr;
   uint64_t* out = first;
   for (int p = 0; p < passes; ++p) {
@@ -252,7 +302,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_cluster_kernel(const SortAr
       for (int c = 0; c < a.tiles; ++c) {
         const uint32_t n = ld_cluster(&hist[b], c);
         total += n;
-        if (c < (int)blockIdx.x) earlier += n;
+        if (c < tile) earlier += n;
       }
     }
     place_tile(a, out, 8 * p, worker, t0, total, earlier, sh, r);
@@ -267,7 +317,6 @@ constexpr int kChunk = 32;             // sorted tokens per CTA
 constexpr int kSumThreads = 128;
 constexpr int kCols = 8;               // columns per thread
 constexpr int kSlice = kSumThreads * kCols;   // columns per CTA
-constexpr int kZeroRows = 64;          // table rows per zeroing CTA
 constexpr int kJoinThreads = 256;
 constexpr int kJoinCols = 128;         // columns per joining CTA
 
@@ -281,7 +330,8 @@ struct SumArgs {
   uint32_t* joins;          // how many chunks a row starts in that reaches past their end ...
   uint32_t* join_list;      // ... and which: worker * chunks + chunk, in any order
   int64_t T, V, D, pitch;
-  int chunks, zero_blocks;
+  int chunks;
+  ZeroArgs zero;            // zero.ctas of a worker in the summing launch (none where the sort's launch had them)
   float scale;
   bool vec_in, vec_out;
 };
@@ -317,7 +367,7 @@ __device__ __forceinline__ void write_cols(TO* row, int64_t c0, int64_t D, bool 
   }
 }
 
-// CTAs 0 .. chunks - 1 of a worker: one chunk each; the rest: kZeroRows table rows each.
+// CTAs 0 .. chunks - 1 of a worker: one chunk each; the rest, if any: table rows without a token.
 // VEC: rows of dout and of the table start on 16-byte boundaries; a thread has 8 consecutive
 // columns then, and columns kSumThreads apart otherwise (coalesced either way).
 template <typename TI, typename TO, bool VEC>
@@ -330,24 +380,20 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
   const int64_t c0 = slice + (VEC ? threadIdx.x * kCols : threadIdx.x);
 
   if ((int)blockIdx.x >= a.chunks) {
-    // ---- rows without a token
-    __shared__ uint32_t present[kZeroRows];
+    // ---- rows without a token (long lists: the sorted one tells)
+    __shared__ uint8_t present[kZeroRowsMax];
     __shared__ int64_t range[2];
-    const int64_t v0 = (int64_t)(blockIdx.x - a.chunks) * kZeroRows;
-    const int64_t v1 = v0 + kZeroRows < a.V ? v0 + kZeroRows : a.V;
-    if (threadIdx.x < kZeroRows) present[threadIdx.x] = 0;
+    const int64_t v0 = (int64_t)(blockIdx.x - a.chunks) * a.zero.rows;
+    const int n = (int)(a.V - v0 < a.zero.rows ? a.V - v0 : a.zero.rows);
+    for (int r = threadIdx.x; r < n; r += kSumThreads) present[r] = 0;
     if (threadIdx.x < 64) {   // one warp for each end
-      const int64_t p = warp_lower_bound(sorted, a.T, (uint32_t)(threadIdx.x < 32 ? v0 : v1));
+      const int64_t p = warp_lower_bound(sorted, a.T, (uint32_t)(threadIdx.x < 32 ? v0 : v0 + n));
       if ((threadIdx.x & 31) == 0) range[threadIdx.x >> 5] = p;
     }
     __syncthreads();
     for (int64_t i = range[0] + threadIdx.x; i < range[1]; i += kSumThreads) present[key_at(sorted, i) - v0] = 1;
     __syncthreads();
-    float zero[kCols];
-#pragma unroll
-    for (int e = 0; e < kCols; ++e) zero[e] = 0.f;
-    for (int64_t v = v0; v < v1; ++v)
-      if (!present[v - v0]) write_cols<TO>(table + v * a.D, c0, a.D, VEC, !VEC, zero);
+    if (blockIdx.y == 0) zero_rows(a.zero, worker, v0, n, present);
     return;
   }
 
@@ -505,7 +551,7 @@ bool rows_of_16(const void* p, int64_t worker, int64_t row, int64_t m, int64_t r
 
 template <typename TI, typename TO>
 cudaError_t sum_rows(const SumArgs& a, int64_t m, cudaStream_t s) {
-  const dim3 grid((unsigned)(a.chunks + a.zero_blocks), (unsigned)((a.D + kSlice - 1) / kSlice), (unsigned)m);
+  const dim3 grid((unsigned)(a.chunks + a.zero.ctas), (unsigned)((a.D + kSlice - 1) / kSlice), (unsigned)m);
   auto k = a.vec_in && a.vec_out ? embedding_sum_kernel<TI, TO, true> : embedding_sum_kernel<TI, TO, false>;
   cudaError_t e = launch_chained(k, grid, dim3(kSumThreads), 0, s, a);
   if (e != cudaSuccess || a.chunks <= 1) return e;
@@ -548,6 +594,11 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
   uint32_t* joins = reinterpret_cast<uint32_t*>(ws + l.joins);
   SortArgs sort{g.ids, nullptr, nullptr, reinterpret_cast<uint32_t*>(ws + l.counts), joins, g.T, (uint32_t)g.V, (int)tiles_of(g.T), 0};
   const dim3 sort_grid((unsigned)sort.tiles, (unsigned)g.m);
+  const int out_size = g.out_dtype == OLSGD_F32 ? 4 : 2;
+  ZeroArgs zero{g.dtable, g.V, g.D * out_size, g.dtable_worker * out_size, 0, 0};
+  zero.rows = (int)(kZeroBytes / zero.row_bytes);
+  zero.rows = zero.rows < 16 ? 16 : zero.rows > kZeroRowsMax ? kZeroRowsMax : zero.rows;
+  zero.ctas = (int)((g.V + zero.rows - 1) / zero.rows);
   int passes = 0;
   while (g.T > 0 && (g.V >> (8 * passes)) > 0) ++passes;   // keys are 0 .. V
   if (sort.tiles > kSortCluster) {
@@ -564,7 +615,8 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
     cudaLaunchConfig_t cfg{};
     const bool half = g.T <= kSortCluster * kSortTile / 2;
     if (half) sort.tiles = (int)((g.T + kSortTile / 2 - 1) / (kSortTile / 2));
-    cfg.gridDim = dim3((unsigned)sort.tiles, (unsigned)g.m);
+    const int64_t zeros = (g.m * zero.ctas + sort.tiles - 1) / sort.tiles * sort.tiles;
+    cfg.gridDim = dim3((unsigned)(g.m * sort.tiles + zeros));
     cfg.blockDim = dim3(kSortThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -576,8 +628,10 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = g_launch_overlap ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, half ? sort_cluster_kernel<kSortItems / 2> : sort_cluster_kernel<kSortItems>, sort, lists[0], lists[1], passes);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, half ? sort_cluster_kernel<kSortItems / 2> : sort_cluster_kernel<kSortItems>, sort, lists[0], lists[1], passes,
+                                             (int)g.m, zero);
     if (e != cudaSuccess) return e;
+    zero.ctas = 0;   // done
     sort.in = lists[(passes - 1) & 1];
   }
   SumArgs a;
@@ -595,12 +649,12 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
   a.D = g.D;
   a.pitch = pitch_of(g.D);
   a.chunks = (int)chunks_of(g.T);
-  a.zero_blocks = (int)((g.V + kZeroRows - 1) / kZeroRows);
+  a.zero = zero;
   a.scale = g.scale;
-  const int si = g.dtype == OLSGD_F32 ? 4 : 2, so = g.out_dtype == OLSGD_F32 ? 4 : 2;
+  const int si = g.dtype == OLSGD_F32 ? 4 : 2;
   // whole pieces: the columns end on a piece's end too
   a.vec_in = g.D % kCols == 0 && rows_of_16(g.dout, g.dout_worker, g.dout_row, g.m, g.T, si);
-  a.vec_out = g.D % kCols == 0 && rows_of_16(g.dtable, g.dtable_worker, g.D, g.m, g.V, so);
+  a.vec_out = g.D % kCols == 0 && rows_of_16(g.dtable, g.dtable_worker, g.D, g.m, g.V, out_size);
   switch (g.dtype) {
     case OLSGD_F32: return sum_rows_to<float>(g.out_dtype, a, g.m, s);
     case OLSGD_BF16: return sum_rows_to<__nv_bfloat16>(g.out_dtype, a, g.m, s);
