@@ -107,7 +107,7 @@ struct SortArgs {
   const uint64_t* in;        // [m][T], or null: the ids themselves
   uint64_t* out;             // [m][T]
   uint32_t* counts;          // [m][kBins][tiles]
-  uint32_t* joins;           // counter that the summing kernel starts from: zeroed here
+  uint32_t* joins;           // two counters that the summing kernel starts from: zeroed here
   int64_t T;
   uint32_t V;
   int tiles, shift;
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const SortArgs
   __shared__ TileSort sh;
   launch_gate();
   const int64_t worker = blockIdx.y, t0 = (int64_t)blockIdx.x * kSortTile + (threadIdx.x >> 5) * (32 * kSortItems);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.joins = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.joins[0] = a.joins[1] = 0;
   Ranked<kSortItems> r;
   rank_tile(a, a.in, a.shift, worker, t0, sh, r);
   uint32_t total = 0, earlier = 0;
@@ -283,7 +283,7 @@ sort_cluster_kernel(const SortArgs a, uint64_t* first, uint64_t* second, int pas
   }
   const int tile = blockIdx.x % a.tiles;
   const int64_t worker = blockIdx.x / a.tiles, t0 = ((int64_t)tile * kSortThreads + (threadIdx.x & ~31u)) * ITEMS;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.joins = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.joins[0] = a.joins[1] = 0;
   const uint64_t* in = nullptr;
   uint64_t* out = first;
   for (int p = 0; p < passes; ++p) {
@@ -317,6 +317,7 @@ constexpr int kChunk = 32;             // sorted tokens per CTA
 constexpr int kSumThreads = 128;
 constexpr int kCols = 8;               // columns per thread
 constexpr int kSlice = kSumThreads * kCols;   // columns per CTA
+constexpr int kShortRow = 8;           // parts that one warp adds up
 constexpr int kJoinThreads = 256;
 constexpr int kJoinCols = 128;         // columns per joining CTA
 
@@ -327,8 +328,8 @@ struct SumArgs {
   void* dtable;             // [m][V][D], workers out_worker apart
   int64_t out_worker;
   float* part;              // [m][chunks][2][pitch]: the row a chunk shares with the one before, with the one after
-  uint32_t* joins;          // how many chunks a row starts in that reaches past their end ...
-  uint32_t* join_list;      // ... and which: worker * chunks + chunk, in any order
+  uint32_t* joins;          // how many chunks a row starts in that reaches past their end: short rows, long rows ...
+  uint32_t* join_list;      // ... and which: worker * chunks + chunk, in any order, short ones from the front, long from the back
   int64_t T, V, D, pitch;
   int chunks;
   ZeroArgs zero;            // zero.ctas of a worker in the summing launch (none where the sort's launch had them)
@@ -446,8 +447,12 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
       const bool to_after = k + 1 == n && next == key;
       if (key < a.V) {
         if (from_before || to_after) {
-          if (!from_before && blockIdx.y == 0 && threadIdx.x == 0)
-            a.join_list[atomicAdd(a.joins, 1u)] = (uint32_t)worker * a.chunks + blockIdx.x;
+          if (!from_before && blockIdx.y == 0 && threadIdx.x == 0) {
+            const uint32_t at = (uint32_t)worker * a.chunks + blockIdx.x;
+            const int64_t far = ((int64_t)blockIdx.x + kShortRow) * kChunk;
+            if (far < a.T && key_at(sorted, far) == key) a.join_list[gridDim.z * a.chunks - 1 - atomicAdd(a.joins + 1, 1u)] = at;
+            else a.join_list[atomicAdd(a.joins, 1u)] = at;
+          }
           write_cols<float>(part + (from_before ? 0 : a.pitch), c0, a.D, VEC, !VEC, acc);
         } else {
           float r[kCols];
@@ -463,19 +468,24 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
   }
 }
 
-// The table rows that start in one chunk and reach past its end, as listed by the summing kernel: an
-// item is such a row and a slice of its columns.  Its part of the first chunk, then the parts of the
-// chunks that follow, each eighth of them by a warp of its own, joined in a fixed order (so the
-// list's order does not matter).
+// The table rows that start in one chunk and reach past its end, as listed by the summing kernel (in
+// any order: each is formed by itself): the row's part of its first chunk, then those of the chunks
+// that follow.  A short row is one CTA's, a warp per slice of columns; of a long one each slice is,
+// each eighth of the parts by a warp of its own, joined in a fixed order.
 template <typename TO>
-__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumArgs a) {
-  __shared__ float4 sh[kJoinThreads / 32][32];
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumArgs a, int64_t n_lists) {
+  constexpr int kJoinWarps = kJoinThreads / 32;
+  __shared__ float4 sh[kJoinWarps][32];
   launch_gate();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t slices = (a.D + kJoinCols - 1) / kJoinCols, items = (int64_t)*a.joins * slices;
+  const int64_t slices = (a.D + kJoinCols - 1) / kJoinCols;
+  const uint32_t n_short = a.joins[0];
+  const int64_t items = n_short + (int64_t)a.joins[1] * slices;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const uint32_t at = a.join_list[item / slices];
-    const int64_t worker = at / a.chunks, c = at % a.chunks, slice = item % slices;
+    const bool is_short = item < n_short;
+    const int64_t of_long = item - n_short;
+    const uint32_t at = is_short ? a.join_list[item] : a.join_list[n_lists - 1 - of_long / slices];
+    const int64_t worker = at / a.chunks, c = at % a.chunks;
     const uint64_t* sorted = a.sorted + worker * a.T;
     const uint32_t key = key_at(sorted, (c + 1) * kChunk - 1);
     // the last chunk that holds the key: chunks ahead are probed a warp's width at a time
@@ -490,36 +500,51 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(const SumA
       if (run < 32) break;
     }
     const float* part = a.part + worker * a.chunks * 2 * a.pitch;
-    const int64_t col = slice * kJoinCols + lane * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](const float* p) {
-      const float4 v = *reinterpret_cast<const float4*>(p + col);
-      acc.x += v.x;
-      acc.y += v.y;
-      acc.z += v.z;
-      acc.w += v.w;
-    };
-    if (col < a.D) {   // (pitch is a multiple of four: whole pieces; those past D are not stored)
-      if (warp == 0) add(part + (c * 2 + 1) * a.pitch);
+    TO* row = static_cast<TO*>(a.dtable) + worker * a.out_worker + (int64_t)key * a.D;
+    // the parts first, first + step, ... of the row (part 0: in chunk c), columns col to col + 3
+    // (pitch is a multiple of four: whole pieces; what lies past D is not stored)
+    auto sum = [&](int64_t col, int64_t first, int64_t step) {
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (col < a.D) {
 #pragma unroll 4
-      for (int64_t k = c + 1 + warp; k <= end; k += kJoinThreads / 32) add(part + k * 2 * a.pitch);
-    }
-    __syncthreads();   // (the item before has been read)
-    sh[warp][lane] = acc;
-    __syncthreads();
-    if (warp == 0 && col < a.D) {
-      float r[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < kJoinThreads / 32; ++w) {
-        r[0] += sh[w][lane].x;
-        r[1] += sh[w][lane].y;
-        r[2] += sh[w][lane].z;
-        r[3] += sh[w][lane].w;
+        for (int64_t k = c + first; k <= end; k += step) {
+          const float4 v = *reinterpret_cast<const float4*>(part + (k * 2 + (k == c ? 1 : 0)) * a.pitch + col);
+          acc.x += v.x;
+          acc.y += v.y;
+          acc.z += v.z;
+          acc.w += v.w;
+        }
       }
-      TO* row = static_cast<TO*>(a.dtable) + worker * a.out_worker + (int64_t)key * a.D;
+      return acc;
+    };
+    auto store = [&](int64_t col, const float4& v) {
+      const float r[4] = {v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (col + e < a.D) row[col + e] = Elem<TO>::from_float(r[e] * a.scale);
+        if (col + e < a.D) row[col + e] = Elem<TO>::from_float(r[e]);
+    };
+    if (is_short) {
+      for (int64_t slice = warp; slice < slices; slice += kJoinWarps) {
+        const int64_t col = slice * kJoinCols + lane * 4;
+        store(col, sum(col, 0, 1));
+      }
+    } else {
+      const int64_t col = of_long % slices * kJoinCols + lane * 4;
+      sh[warp][lane] = sum(col, warp, kJoinWarps);
+      __syncthreads();
+      if (warp == 0) {
+        float4 t = sh[0][lane];
+#pragma unroll
+        for (int w = 1; w < kJoinWarps; ++w) {
+          const float4 v = sh[w][lane];
+          t.x += v.x;
+          t.y += v.y;
+          t.z += v.z;
+          t.w += v.w;
+        }
+        store(col, t);
+      }
+      __syncthreads();
     }
   }
 }
@@ -556,7 +581,7 @@ cudaError_t sum_rows(const SumArgs& a, int64_t m, cudaStream_t s) {
   cudaError_t e = launch_chained(k, grid, dim3(kSumThreads), 0, s, a);
   if (e != cudaSuccess || a.chunks <= 1) return e;
   const int64_t most = m * a.chunks * ((a.D + kJoinCols - 1) / kJoinCols), room = 148 * 8;
-  return launch_chained(embedding_join_kernel<TO>, dim3((unsigned)(most < room ? most : room)), dim3(kJoinThreads), 0, s, a);
+  return launch_chained(embedding_join_kernel<TO>, dim3((unsigned)(most < room ? most : room)), dim3(kJoinThreads), 0, s, a, m * a.chunks);
 }
 
 template <typename TI>
