@@ -33,6 +33,9 @@ constexpr int kWarpRowMax = 1024;     // longest row that stays in a warp's regi
 constexpr int kMaxTop = OLSGD_MAX_TOP;
 static_assert(kMaxTop == 32, "a lane holds one candidate of each warp");
 constexpr int kMaxSplit = 64;
+// The last rows that the forward kernel reads (this many bytes of them) are loaded at normal priority
+// and stay in L2; the gradient, which usually follows, starts from them.
+constexpr int64_t kKeepBytes = 64LL << 20;
 
 struct RowState {
   float m, s, t;   // running maximum; sums relative to it
@@ -256,6 +259,7 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
   const T* row = x + r * ld;
   const int shift = row_shift(row);
   const int c_begin = blockIdx.y * cps, c_end = min(nchunks, c_begin + cps);
+  const bool again = gridDim.x - r <= kKeepBytes / ((int64_t)V * (int)sizeof(T));
 
   Target target{0.f, false};
   if (WHOLE && threadIdx.x == 0) target = fetch_target<T>(o, row, r, V);
@@ -271,7 +275,7 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int q = 0; q < Q; ++q) w[u][q] = ld16_stream(p + u * (kWarps * 32 * Q) + q * 32);
+        for (int q = 0; q < Q; ++q) w[u][q] = again ? ld16(p + u * (kWarps * 32 * Q) + q * 32) : ld16_stream(p + u * (kWarps * 32 * Q) + q * 32);
     } else {
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -565,12 +569,13 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(LogprobGradArgs 
   constexpr int VEC = Elem<T>::kVec;
   constexpr int U = kUnroll;
   launch_gate();
-  const int64_t r = blockIdx.x;
+  const int64_t r = a.rows - 1 - blockIdx.x;   // from the row that was read last
   const int V = (int)a.V;
   const T* row = static_cast<const T*>(a.logits) + r * a.ld;
   T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
   const int shift = row_shift(row);
   const bool aligned = row_shift(out) == shift;
+  const bool large = a.rows * a.V * (int64_t)sizeof(T) > kKeepBytes;   // a gradient that L2 would not hold anyway
   const int j0 = ((int)blockIdx.y * (kThreads * U) + (int)threadIdx.x) * VEC - shift;
   uint4 w[U];
 #pragma unroll
@@ -588,7 +593,8 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(LogprobGradArgs 
       for (int e = 0; e < VEC; ++e)
         if (j + e == g.target) d[e] += g.d_lp;
     }
-    store_floats<T, VEC>(out, j, V, aligned, d);
+    if (large) store_floats<T, VEC, true>(out, j, V, aligned, d);
+    else store_floats<T, VEC>(out, j, V, aligned, d);
   }
 }
 
