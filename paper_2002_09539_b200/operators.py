@@ -74,17 +74,21 @@ def _stream(index):
     return torch.cuda.current_stream(index).cuda_stream
 
 
-# the same number without the Stream object around it (2 us a call)
+# the same numbers without the Stream object and the checks around them (2 us a call)
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _run(fn, dev, *args):
     """fn(*args, stream) on the tensors' device and its current stream."""
-    if torch.cuda.current_device() == dev.index:
-        st = fn(*args, _stream(dev.index))
+    index = dev.index
+    if _current_device() == index:
+        st = fn(*args, _stream(index))
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, _stream(dev.index))
+            st = fn(*args, _stream(index))
     if st:
         _check(_ops(), st)
 
@@ -108,18 +112,25 @@ def _workspace(like, query, *sizes):
 # ------------------------------------------------------------------ token log probabilities
 
 def _rows_of(t, name):
-    """(view [N][V], stride between rows) of a tensor [..., V] whose rows are evenly spaced."""
-    if not t.is_cuda or t.dim() < 1:
+    """(pointer, type, N, V, stride between rows) of a tensor [..., V] whose rows are evenly spaced."""
+    shape = t.shape
+    if not t.is_cuda or not shape:
         _refuse("%s must be a CUDA tensor with at least one dimension", name)
-    V = t.shape[-1]
-    if V < 1 or (V > 1 and t.stride(-1) != 1):
+    V, stride = shape[-1], t.stride()
+    if V < 1 or (V > 1 and stride[-1] != 1):
         _refuse("%s: the last dimension must be contiguous and not empty", name)
-    if t.dim() != 2:   # (one launch takes rows at one distance)
-        try:
-            t = t.view(-1, V)
-        except RuntimeError:
-            raise ValueError("%s: rows must be evenly spaced" % name) from None
-    return t, (t.stride(0) if t.shape[0] > 1 else V)
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        _refuse("%s must be float32, bfloat16 or float16", name)
+    if len(shape) == 2:
+        N = shape[0]
+        return t.data_ptr(), code, N, V, (stride[0] if N > 1 else V)
+    try:   # (one launch takes rows at one distance)
+        rows = t.view(-1, V)
+    except RuntimeError:
+        raise ValueError("%s: rows must be evenly spaced" % name) from None
+    N = rows.shape[0]
+    return t.data_ptr(), code, N, V, (rows.stride(0) if N > 1 else V)
 
 
 def _per_row(t, shape, dtype, dev, name):
@@ -132,27 +143,24 @@ def token_logprobs(logits, targets, top=0):
     """olsgd_token_logprobs.  logits [..., V] (rows evenly spaced), targets int32 [...]; a target outside
     [0, V) is a row without a token.  Returns TokenLogprobs(logp, entropy, stats, top_logp, top_ids): float32
     [...], [...], [..., 2], [..., top] and int32 [..., top] (the last two None when top == 0)."""
-    lib = _ops()
-    rows, ld = _rows_of(logits, "logits")
-    code, dev, lead = _dtype(logits, "logits"), logits.device, logits.shape[:-1]
+    lib = _OPS or _ops()
+    xp, code, N, V, ld = _rows_of(logits, "logits")
+    dev, lead = logits.device, logits.shape[:-1]
     tp = _per_row(targets, lead, torch.int32, dev, "targets")
-    N, V = rows.shape
-    top = int(top)
-    if not 0 <= top <= min(V, MAX_TOP):
-        _refuse("top must be in [0, min(V, %d)]", MAX_TOP)
+    if top < 0 or top > MAX_TOP or top > V or top != int(top):
+        _refuse("top must be a whole number in [0, min(V, %d)]", MAX_TOP)
     # the float outputs share one allocation: allocating is most of what the host does here
     out = targets.new_empty(N * (4 + top), dtype=torch.float32)
     p = out.data_ptr()
     ws, wp, wn = _workspace(targets, "olsgd_token_logprobs_workspace", code, N, V, top)
     if top:
         top_ids = targets.new_empty(lead + (top,))
-        _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N,
-             top_ids.data_ptr(), wp, wn)
+        _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N, top_ids.data_ptr(), wp, wn)
         logp, entropy, stats, top_logp = out.split_with_sizes((N, N, 2 * N, top * N))
-        top_logp = top_logp.view(lead + (top,))
+        top_logp = top_logp.view(top_ids.shape)
     else:
         top_logp = top_ids = None
-        _run(lib.olsgd_token_logprobs, dev, rows.data_ptr(), code, N, V, ld, tp, 0, p, p + 4 * N, p + 8 * N, None, None, wp, wn)
+        _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, 0, p, p + 4 * N, p + 8 * N, None, None, wp, wn)
         logp, entropy, stats = out.split_with_sizes((N, N, 2 * N))
     if len(lead) != 1:
         logp, entropy = logp.view(lead), entropy.view(lead)
@@ -162,16 +170,15 @@ def token_logprobs(logits, targets, top=0):
 def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
     """olsgd_token_logprobs_backward: the gradient of the logits, contiguous, of their type.  d_logp and d_entropy
     are float32 [...] or None (zeros); stats and entropy are token_logprobs' for the same logits."""
-    lib = _ops()
-    rows, ld = _rows_of(logits, "logits")
-    code, dev, lead, f32 = _dtype(logits, "logits"), logits.device, logits.shape[:-1], torch.float32
-    N, V = rows.shape
+    lib = _OPS or _ops()
+    xp, code, N, V, ld = _rows_of(logits, "logits")
+    dev, lead, f32 = logits.device, logits.shape[:-1], torch.float32
+    tp, ep = _per_row(targets, lead, torch.int32, dev, "targets"), _per_row(entropy, lead, f32, dev, "entropy")
+    sp = _per_row(stats, lead + (2,), f32, dev, "stats")
+    lp = None if d_logp is None else _per_row(d_logp, lead, f32, dev, "d_logp")
+    hp = None if d_entropy is None else _per_row(d_entropy, lead, f32, dev, "d_entropy")
     d = logits.new_empty(logits.shape)
-    _run(lib.olsgd_token_logprobs_backward, dev,
-         None if d_logp is None else _per_row(d_logp, lead, f32, dev, "d_logp"),
-         None if d_entropy is None else _per_row(d_entropy, lead, f32, dev, "d_entropy"),
-         rows.data_ptr(), code, N, V, ld, _per_row(targets, lead, torch.int32, dev, "targets"),
-         _per_row(stats, lead + (2,), f32, dev, "stats"), _per_row(entropy, lead, f32, dev, "entropy"), d.data_ptr(), V)
+    _run(lib.olsgd_token_logprobs_backward, dev, lp, hp, xp, code, N, V, ld, tp, sp, ep, d.data_ptr(), V)
     return d
 
 
