@@ -469,8 +469,8 @@ olsgd_status olsgd_clip_grads(const olsgd_clip_tensor* tensors, int32_t n_tensor
  *   x, w_gate, w_up   with the elements between workers and between rows of each (a dimension
  *                     of size one may have any stride); neither may overlap themselves
  *   h                 contiguous
- *   pre               NULL, or [m][T][2][Fp] of the same type, Fp = F rounded up to a multiple
- *                     of 8, 16-byte aligned: a and b, for the backward pass
+ *   pre               NULL, or float [m][T][2][Fp], Fp = F rounded up to a multiple of 8,
+ *                     32-byte aligned: a and b, for the backward pass
  * olsgd_gated_workspace: `backward` 0 or 1; `aligned` nonzero when x, w_gate and w_up have
  * bases on 16 bytes and strides in multiples of 8 elements (then nothing is copied).       */
 typedef enum { OLSGD_ACT_SILU = 0, OLSGD_ACT_GELU = 1, OLSGD_ACT_RELU = 2, OLSGD_ACT_SIGMOID = 3 } olsgd_activation;
@@ -481,7 +481,7 @@ olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int
                                  int64_t x_row_stride, const void* w_gate,
                                  int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
                                  const void* w_up, int64_t w_up_worker_stride,
-                                 int64_t w_up_row_stride, void* h, void* pre, void* workspace,
+                                 int64_t w_up_row_stride, void* h, float* pre, void* workspace,
                                  size_t workspace_bytes, void* stream);
 /* Its gradient.  With da = d_h b act'(a) and db = d_h act(a), both rounded to the operand type:
  *   d_x = da Wg + db Wu,  d_w_gate = da^T x,  d_w_up = db^T x,
@@ -494,7 +494,7 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
                                   int64_t x_row_stride, const void* w_gate,
                                   int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
                                   const void* w_up, int64_t w_up_worker_stride,
-                                  int64_t w_up_row_stride, const void* pre, void* d_x,
+                                  int64_t w_up_row_stride, const float* pre, void* d_x,
                                   void* d_w_gate, void* d_w_up, void* workspace,
                                   size_t workspace_bytes, void* stream);
 /* Embedding lookup with a scale, worker-batched: out[i][t] = scale * table[i][ids[i][t]], rounded

@@ -3,9 +3,10 @@
 //   da = dh * b * act'(a),  db = dh * act(a)                                   (element-wise)
 //   dx = da Wg + db Wu,  dWg = da^T x,  dWu = db^T x                           (backward)
 // x [m][T][D], Wg and Wu [m][F][D], h [m][T][F]; 16-bit operands, fp32 accumulation in tensor
-// memory, one rounding of each result.  Training keeps a and b in the operand type: 2 T F
-// 16-bit values written once and read once, against 4 T D F more multiply-adds to form them
-// again; da and db have to be rounded to that type as operands in any case.
+// memory, one rounding of each result.  Training keeps a and b, in fp32: 2 T F values written once
+// and read once, against 4 T D F more multiply-adds to form them again.  da and db have to be
+// rounded to 16 bits as operands; were a and b too, the gradients would be 1.7 times as far
+// from the exact ones as the rounding of the result alone leaves them, instead of 1.4 times.
 //
 // One kernel, three modes, persistent: a CTA (or a pair of CTAs on one 256-row tile,
 // tcgen05 cta_group::2) walks over tiles of its output.  Warp 0 feeds a ring of shared-memory
@@ -51,7 +52,7 @@ struct GatedArgs {
   bool out_vec;               // the output's rows are whole 16-byte pieces
   void* out0;                 // h, dx or dWg
   void* out1;                 // dWu
-  void* pre;                  // FORWARD: a, b [m][T][2][Fp], or null
+  float* pre;                 // FORWARD: a, b [m][T][2][Fp], or null
   int64_t pre_pitch;          // Fp
 };
 
@@ -139,6 +140,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, int f16) {
   }
   const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+__device__ __forceinline__ void store_sector(float* p, const float* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(__float_as_uint(v[0])),
+               "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
+               "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
 }
 
 // A warp's block of 32 rows x W columns of results on its way out: TMEM hands every lane a row,
@@ -379,6 +387,16 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
             for (int q = 0; q < W / 16; ++q) {
               float a[16], b[16], h[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + BN / 2 + c0 + q * 16, a, b);
+              if (g.pre && lane < rows) {
+                // columns up to pre_pitch (a multiple of 8) exist; a lane writes whole sectors
+                float* pre = g.pre + (worker * g.rows + row0 + lane) * 2 * g.pre_pitch + col + q * 16;
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                  if (col + q * 16 + 8 * z < g.pre_pitch) {
+                    store_sector(pre + 8 * z, a + 8 * z);
+                    store_sector(pre + g.pre_pitch + 8 * z, b + 8 * z);
+                  }
+              }
               switch (g.act) {
                 case OLSGD_ACT_SILU: activate16<OLSGD_ACT_SILU>(a, b, h); break;
                 case OLSGD_ACT_GELU: activate16<OLSGD_ACT_GELU>(a, b, h); break;
@@ -388,22 +406,6 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
               out.put(lane, q, h, g.f16);
             }
             out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
-            if (g.pre) {
-              // a, then b, to rows of pre_pitch (a multiple of 8): columns up to it exist
-              uint16_t* pre = static_cast<uint16_t*>(g.pre) + (worker * g.rows + row0) * 2 * g.pre_pitch + col;
-#pragma unroll 1
-              for (int z = 0; z < 2; ++z) {
-#pragma unroll 1
-                for (int q = 0; q < W / 16; q += W >= 32 ? 2 : 1) {
-                  float v[16], w[16];
-                  const uint32_t at = acc + z * (BN / 2) + c0 + q * 16;
-                  tmem_ld16x2(at, W >= 32 ? at + 16 : at, v, w);
-                  out.put(lane, q, v, g.f16);
-                  if (W >= 32) out.put(lane, q + 1, w, g.f16);
-                }
-                out.flush(lane, pre + z * g.pre_pitch, 2 * g.pre_pitch, rows, g.pre_pitch - col, true);
-              }
-            }
           } else {
 #pragma unroll 1
             for (int q = 0; q < W / 16; q += 2) {
@@ -455,7 +457,7 @@ constexpr int kFewTokens = 2;
 template <typename T, int NT, bool VEC>
 __global__ void __launch_bounds__(256)
 gated_few_kernel(GatedOperand x, GatedOperand wg, GatedOperand wu, int tokens, int64_t D, int64_t F, int act, T* __restrict__ h,
-                 T* __restrict__ pre, int64_t pre_pitch) {
+                 float* __restrict__ pre, int64_t pre_pitch) {
   launch_gate();
   const int lane = threadIdx.x & 31;
   const int64_t f = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), worker = blockIdx.y;
@@ -531,11 +533,11 @@ gated_few_kernel(GatedOperand x, GatedOperand wg, GatedOperand wu, int tokens, i
       const int64_t row = worker * tokens + t;
       h[row * F + f] = Elem<T>::from_float(v * bt);
       if (pre) {
-        T* p = pre + row * 2 * pre_pitch;
-        p[f] = Elem<T>::from_float(at);
-        p[pre_pitch + f] = Elem<T>::from_float(bt);
+        float* p = pre + row * 2 * pre_pitch;
+        p[f] = at;
+        p[pre_pitch + f] = bt;
         if (f == F - 1)   // the padding of the rows
-          for (int64_t k = F; k < pre_pitch; ++k) p[k] = p[pre_pitch + k] = Elem<T>::from_float(0.f);
+          for (int64_t k = F; k < pre_pitch; ++k) p[k] = p[pre_pitch + k] = 0.f;
       }
     }
   }
@@ -597,7 +599,7 @@ constexpr int kStretch = 512;
 // da = dh b act'(a), db = dh act(a); a, b, da, db have rows of `pitch`.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
-gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const T* __restrict__ pre,
+gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const float* __restrict__ pre,
                       T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec) {
   launch_gate();
   const T* dh_w = dh + (int64_t)blockIdx.y * dh_worker;
@@ -612,8 +614,11 @@ gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_ro
     const int64_t j = j_begin + q * 256 + (threadIdx.x & 31) * 8;
     if (j >= pitch) break;
     float a[8], b[8], d[8], va[8], vb[8];
-    Elem<T>::unpack(ld16_stream(pre + wr * 2 * pitch + j), a);
-    Elem<T>::unpack(ld16_stream(pre + wr * 2 * pitch + pitch + j), b);
+#pragma unroll
+    for (int k = 0; k < 8; k += 4) {
+      Elem<float>::unpack(ld16_stream(pre + wr * 2 * pitch + j + k), a + k);
+      Elem<float>::unpack(ld16_stream(pre + wr * 2 * pitch + pitch + j + k), b + k);
+    }
     const T* src = dh_w + r * dh_row + j;
     if (vec) {
       Elem<T>::unpack(ld16_stream(src), d);
@@ -769,7 +774,7 @@ cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* d
            : a.act == OLSGD_ACT_RELU ? gated_backward_kernel<T, OLSGD_ACT_RELU>
                                      : gated_backward_kernel<T, OLSGD_ACT_SIGMOID>;
   return launch_chained(k, grid, dim3(256), 0, s, static_cast<const T*>(a.dh.p), a.dh.worker_stride, a.dh.row_stride,
-                        static_cast<const T*>(a.pre), static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec);
+                        a.pre, static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec);
 }
 
 template <typename T>
@@ -778,7 +783,7 @@ cudaError_t few(const GatedForward& a, cudaStream_t s) {
   auto k = a.T == 1 ? (vec ? gated_few_kernel<T, 1, true> : gated_few_kernel<T, 1, false>)
                     : (vec ? gated_few_kernel<T, kFewTokens, true> : gated_few_kernel<T, kFewTokens, false>);
   return launch_chained(k, dim3((unsigned)((a.F + 7) / 8), (unsigned)a.m), dim3(256), 0, s, a.x, a.wg, a.wu, (int)a.T, a.D, a.F,
-                        a.act, static_cast<T*>(a.h), static_cast<T*>(a.pre), round8(a.F));
+                        a.act, static_cast<T*>(a.h), a.pre, round8(a.F));
 }
 
 #define OLSGD_STEP(call)                    \

@@ -192,7 +192,7 @@ olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int
                                  int64_t x_row_stride, const void* w_gate,
                                  int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
                                  const void* w_up, int64_t w_up_worker_stride,
-                                 int64_t w_up_row_stride, void* h, void* pre, void* workspace,
+                                 int64_t w_up_row_stride, void* h, float* pre, void* workspace,
                                  size_t workspace_bytes, void* stream) {
   OLSGD_TRY(check_gated(m, T, D, F));
   OLSGD_TRY(check_gated_kind(dtype, activation));
@@ -206,7 +206,7 @@ olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int
   OLSGD_TRY(check_operand(a.wg, "w_gate", m, F, D));
   OLSGD_TRY(check_operand(a.wu, "w_up", m, F, D));
   OLSGD_REFUSE_IF(!aligned_to(h, 2), "h must be non-null and 2-byte aligned");
-  OLSGD_REFUSE_IF(pre && !aligned_to(pre, 16), "pre must be 16-byte aligned");
+  OLSGD_REFUSE_IF(pre && !aligned_to(pre, 32), "pre must be 32-byte aligned");
   a.h = h;
   a.pre = pre;
   a.ws = workspace;
@@ -220,7 +220,7 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
                                   int64_t x_row_stride, const void* w_gate,
                                   int64_t w_gate_worker_stride, int64_t w_gate_row_stride,
                                   const void* w_up, int64_t w_up_worker_stride,
-                                  int64_t w_up_row_stride, const void* pre, void* d_x,
+                                  int64_t w_up_row_stride, const float* pre, void* d_x,
                                   void* d_w_gate, void* d_w_up, void* workspace,
                                   size_t workspace_bytes, void* stream) {
   OLSGD_TRY(check_gated(m, T, D, F));
@@ -241,7 +241,7 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
   OLSGD_TRY(check_operand(a.x, "x", m, T, D));
   OLSGD_TRY(check_operand(a.wg, "w_gate", m, F, D));
   OLSGD_TRY(check_operand(a.wu, "w_up", m, F, D));
-  OLSGD_REFUSE_IF(!aligned_to(pre, 16), "pre must be non-null and 16-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(pre, 32), "pre must be non-null and 32-byte aligned");
   OLSGD_REFUSE_IF((d_w_gate == nullptr) != (d_w_up == nullptr), "d_w_gate and d_w_up are wanted both or neither");
   OLSGD_REFUSE_IF((d_x && !aligned_to(d_x, 2)) || (d_w_gate && (!aligned_to(d_w_gate, 2) || !aligned_to(d_w_up, 2))),
                   "d_x, d_w_gate and d_w_up must be 2-byte aligned");

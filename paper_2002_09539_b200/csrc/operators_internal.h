@@ -46,11 +46,12 @@ struct GatedShape {
 };
 struct GatedForward : GatedShape {
   GatedOperand x, wg, wu;
-  void *h, *pre, *ws;
+  void *h, *ws;
+  float* pre;
 };
 struct GatedBackward : GatedShape {
   GatedOperand dh, x, wg, wu;
-  const void* pre;
+  const float* pre;
   void *dx, *dwg, *dwu, *ws;
 };
 // Whether an operand has to be copied to rows that TMA takes.

@@ -265,7 +265,7 @@ def gated_forward(x, w_gate, w_up, activation="silu", save=False):
     dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
     a, b, c = _matrix(x, "x", (m, T, D), dtype, dev), _matrix(w_gate, "w_gate", ws_shape, dtype, dev), _matrix(w_up, "w_up", ws_shape, dtype, dev)
     h = x.new_empty((m, T, F))
-    pre = x.new_empty((m, T, 2, (F + 7) // 8 * 8)) if save else None
+    pre = x.new_empty((m, T, 2, (F + 7) // 8 * 8), dtype=torch.float32) if save else None
     ok = _aligned(a, (m, T)) and _aligned(b, ws_shape) and _aligned(c, ws_shape)
     ws, wp, wn = _workspace(h, "olsgd_gated_workspace", m, T, D, F, 0, ok)
     _run(lib.olsgd_gated_forward, dev, m, T, D, F, code, act, *a, *b, *c, h.data_ptr(), pre.data_ptr() if save else None, wp, wn)
@@ -280,7 +280,7 @@ def gated_backward(d_h, x, w_gate, w_up, pre, activation="silu", want_d_x=True, 
     dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
     d, a = _matrix(d_h, "d_h", (m, T, F), dtype, dev), _matrix(x, "x", (m, T, D), dtype, dev)
     b, c = _matrix(w_gate, "w_gate", ws_shape, dtype, dev), _matrix(w_up, "w_up", ws_shape, dtype, dev)
-    _need(pre.shape == (m, T, 2, (F + 7) // 8 * 8) and pre.dtype == dtype and pre.device == dev and pre.is_contiguous(),
+    _need(pre.shape == (m, T, 2, (F + 7) // 8 * 8) and pre.dtype == torch.float32 and pre.device == dev and pre.is_contiguous(),
           "pre must be the one that gated_forward returned")
     d_x = x.new_empty((m, T, D)) if want_d_x else None
     d_wg, d_wu = (x.new_empty(ws_shape), x.new_empty(ws_shape)) if want_d_w else (None, None)

@@ -359,7 +359,7 @@ def _check_gated(x, wg, wu, dh, kind):
         return
     E = dh.double()
     da, db = E * b * df, E * f
-    ea, eb = ea + half * a.abs() + tiny, eb + half * b.abs() + tiny   # a and b are kept in 16 bits
+    # (a and b are kept as they were accumulated)
     edf = 1.2 * ea + 16 * U * (1 + a.abs())
     if kind == "relu":
         edf = torch.where(a.abs() <= ea, torch.ones_like(a), torch.zeros_like(a))   # the side of 0 is open only there
