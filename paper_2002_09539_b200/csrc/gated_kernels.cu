@@ -46,6 +46,7 @@ struct GatedArgs {
   int num_kb, kb_half;        // K blocks in all; of the first half (DX)
   int row_tiles, col_tiles;   // per problem
   int problems;               // workers (DW: workers x 2)
+  int splits, kb_split;       // parts that K is cut into, K blocks of a part
   int rows, cols;             // extents of one problem's output (FORWARD: cols = F)
   int act, f16;
   int a_rows;                 // rows of A that are loaded (K-major): all 128 unless the problem has fewer
@@ -54,6 +55,8 @@ struct GatedArgs {
   void* out1;                 // dWu
   float* pre;                 // FORWARD: a, b [m][T][2][Fp], or null
   int64_t pre_pitch;          // Fp
+  float* parts;               // splits > 1: sums of the parts, [splits][problems][rows][parts_row]
+  int64_t parts_row;          // (FORWARD: a, b as in pre)
 };
 
 template <int STAGES>
@@ -190,20 +193,23 @@ struct Staged {
 };
 
 struct Tile {
-  int problem, row, col;   // row and column tile
+  int problem, split, row, col;   // row and column tile
 };
-// Tiles of one problem in groups of kGroup row tiles, column by column inside a group.
-__device__ __forceinline__ Tile tile_at(const GatedArgs& g, int64_t t) {
-  const int64_t per = (int64_t)g.row_tiles * g.col_tiles;
+// Tiles of one problem in groups of kGroup row tiles, column by column inside a group.  (A launch of
+// 2^31 tiles would write terabytes: 32 bits do, and divide quickly.)
+__device__ __forceinline__ Tile tile_at(const GatedArgs& g, uint32_t t) {
+  const uint32_t per = g.row_tiles * g.col_tiles, outer = t / per, i = t - outer * per;
   Tile r;
-  r.problem = (int)(t / per);
-  const int64_t i = t - r.problem * per;
-  const int64_t group = i / ((int64_t)kGroup * g.col_tiles);
-  const int first = (int)group * kGroup;
-  const int height = min(kGroup, g.row_tiles - first);
-  const int64_t j = i - group * ((int64_t)kGroup * g.col_tiles);
-  r.row = first + (int)(j % height);
-  r.col = (int)(j / height);
+  r.problem = outer;
+  r.split = 0;
+  if (g.splits > 1) {
+    r.problem = outer / g.splits;
+    r.split = outer - r.problem * g.splits;
+  }
+  const uint32_t group_tiles = kGroup * g.col_tiles, group = i / group_tiles, first = group * kGroup;
+  const uint32_t height = min((uint32_t)kGroup, g.row_tiles - first), j = i - group * group_tiles;
+  r.col = j / height;
+  r.row = first + j - r.col * height;
   return r;
 }
 
@@ -246,8 +252,8 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
   const bool leader = rank == 0;
-  const int64_t first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
-  const int64_t total = (int64_t)g.problems * g.row_tiles * g.col_tiles;
+  const uint32_t first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+  const uint32_t total = (uint32_t)g.problems * g.splits * g.row_tiles * g.col_tiles;
 
   if (threadIdx.x == 0) {
     prefetch_tensormap(&maps.a0);
@@ -279,11 +285,11 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   if (warp == 0 && lane == 0) {
     // ---------------- TMA producer (both CTAs of a pair; the leader announces both's bytes)
     uint32_t it = 0;
-    for (int64_t t = first; t < total && !*abort_flag; t += step) {
+    for (uint32_t t = first; t < total && !*abort_flag; t += step) {
       const Tile tl = tile_at(g, t);
       const int worker = MODE == DW ? tl.problem >> 1 : tl.problem;
       const int m0 = (tl.row * CTAS + rank) * kBM;
-      for (int kb = 0; kb < g.num_kb; ++kb, ++it) {
+      for (int kb = tl.split * g.kb_split, end = min(g.num_kb, kb + g.kb_split); kb < end; ++kb, ++it) {
         const int s = it % STAGES;
         if (!mbar_wait(smem_u32(&ctl->empty[s]), ((it / STAGES) & 1) ^ 1, abort_flag)) break;
         const uint32_t bar_own = smem_u32(&ctl->full[s]);
@@ -332,13 +338,14 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
                            ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((CTAS * kBM) >> 4) << 24);
     uint32_t it = 0, n = 0;
     bool ok = true;
-    for (int64_t t = first; t < total && ok; t += step, ++n) {
+    for (uint32_t t = first; t < total && ok; t += step, ++n) {
       const uint32_t buf = n & 1;
       ok = mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((n >> 1) & 1) ^ 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
       const uint32_t acc = tmem_base + buf * BN;
-      for (int kb = 0; kb < g.num_kb; ++kb, ++it) {
+      const int kb0 = g.splits > 1 ? tile_at(g, t).split * g.kb_split : 0, kb_end = min(g.num_kb, kb0 + g.kb_split);
+      for (int kb = kb0; kb < kb_end; ++kb, ++it) {
         const int s = it % STAGES;
         ok = mbar_wait(smem_u32(&ctl->full[s]), (it / STAGES) & 1, abort_flag);
         if (!ok) break;
@@ -350,7 +357,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
         constexpr uint64_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;
 #pragma unroll
         for (int k = 0; k < kBK / kUmmaK; ++k) {
-          const uint32_t accumulate = (kb > 0 || k > 0) ? 1u : 0u;
+          const uint32_t accumulate = (kb > kb0 || k > 0) ? 1u : 0u;
           if (CTAS == 2) umma_bf16_pair(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, accumulate);
           else umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, accumulate);
         }
@@ -367,7 +374,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
     constexpr int W = kBlockCols;
     Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * (32 * W / 8)};
     uint32_t n = 0;
-    for (int64_t t = first; t < total; t += step, ++n) {
+    for (uint32_t t = first; t < total; t += step, ++n) {
       const uint32_t buf = n & 1;
       const Tile tl = tile_at(g, t);
       const int64_t worker = MODE == DW ? tl.problem >> 1 : tl.problem;
@@ -377,6 +384,10 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
       tc_fence_after();
       const uint32_t acc = tmem_base + buf * BN + ((uint32_t)(lane_group * 32) << 16);
       uint16_t* dst = static_cast<uint16_t*>(MODE == DW && (tl.problem & 1) ? g.out1 : g.out0) + (worker * g.rows + row0) * g.cols;
+      // a part of K: sums in fp32 to this part's own place
+      float* part = g.splits > 1 ? g.parts + (((int64_t)tl.split * g.problems + tl.problem) * g.rows + row0 + lane) * g.parts_row : nullptr;
+      float* pre = !g.pre ? nullptr : g.pre + (worker * g.rows + row0 + lane) * 2 * g.pre_pitch;
+      if (MODE == FORWARD && part) pre = part;
       if (rows > 0) {
         for (int c0 = half * (kColsOut / 2); c0 < (half + 1) * (kColsOut / 2); c0 += W) {
           const int64_t col = (int64_t)tl.col * kColsOut + c0;
@@ -387,16 +398,17 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
             for (int q = 0; q < W / 16; ++q) {
               float a[16], b[16], h[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + BN / 2 + c0 + q * 16, a, b);
-              if (g.pre && lane < rows) {
+              if (pre && lane < rows) {
                 // columns up to pre_pitch (a multiple of 8) exist; a lane writes whole sectors
-                float* pre = g.pre + (worker * g.rows + row0 + lane) * 2 * g.pre_pitch + col + q * 16;
+                float* p = pre + col + q * 16;
 #pragma unroll
                 for (int z = 0; z < 2; ++z)
                   if (col + q * 16 + 8 * z < g.pre_pitch) {
-                    store_sector(pre + 8 * z, a + 8 * z);
-                    store_sector(pre + g.pre_pitch + 8 * z, b + 8 * z);
+                    store_sector(p + 8 * z, a + 8 * z);
+                    store_sector(p + g.pre_pitch + 8 * z, b + 8 * z);
                   }
               }
+              if (part) continue;
               switch (g.act) {
                 case OLSGD_ACT_SILU: activate16<OLSGD_ACT_SILU>(a, b, h); break;
                 case OLSGD_ACT_GELU: activate16<OLSGD_ACT_GELU>(a, b, h); break;
@@ -405,16 +417,25 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
               }
               out.put(lane, q, h, g.f16);
             }
-            out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
+            if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
           } else {
 #pragma unroll 1
             for (int q = 0; q < W / 16; q += 2) {
               float v[16], w[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
+              if (part) {
+                if (lane < rows) {
+                  float* p = part + col + q * 16;
+#pragma unroll
+                  for (int z = 0; z < 4; ++z)
+                    if (col + q * 16 + 8 * z < g.parts_row) store_sector(p + 8 * z, z < 2 ? v + 8 * z : w + 8 * z - 16);
+                }
+                continue;
+              }
               out.put(lane, q, v, g.f16);
               out.put(lane, q + 1, w, g.f16);
             }
-            out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
+            if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
           }
         }
       }
@@ -545,6 +566,49 @@ gated_few_kernel(GatedOperand x, GatedOperand wg, GatedOperand wu, int tokens, i
 
 // ------------------------------------------------------------------- element-wise kernels
 
+// Adds up the parts that K was cut into (in order) and finishes as the epilogue would have.
+template <typename T, int MODE>
+__global__ void __launch_bounds__(256) gated_join_kernel(const GatedArgs g) {
+  launch_gate();
+  const int64_t width = MODE == FORWARD ? g.pre_pitch : g.parts_row;   // columns, rounded up to 8
+  const int64_t problem = blockIdx.y, stretches = (width + 255) / 256;
+  const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = at / stretches;
+  const int64_t c = (at - r * stretches) * 256 + (threadIdx.x & 31) * 8;
+  if (r >= g.rows || c >= width) return;
+  const float* p = g.parts + (problem * g.rows + r) * g.parts_row + c;
+  float a[8], b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.f;
+  for (int s = 0; s < g.splits; ++s, p += (int64_t)g.problems * g.rows * g.parts_row) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; k += 4) Elem<float>::unpack(ld16_stream(p + k), v + k);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] += v[e];
+    if (MODE == FORWARD) {
+#pragma unroll
+      for (int k = 0; k < 8; k += 4) Elem<float>::unpack(ld16_stream(p + g.pre_pitch + k), v + k);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] += v[e];
+    }
+  }
+  T* out = static_cast<T*>(MODE == DW && (problem & 1) ? g.out1 : g.out0) + ((MODE == DW ? problem >> 1 : problem) * g.rows + r) * g.cols;
+  if (MODE == FORWARD) {
+    if (g.pre) {
+      float* pre = g.pre + (problem * g.rows + r) * 2 * g.pre_pitch + c;
+      store_sector(pre, a);
+      store_sector(pre + g.pre_pitch, b);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      a[e] = b[e] * (g.act == OLSGD_ACT_SILU   ? act_value<OLSGD_ACT_SILU>(a[e])
+                     : g.act == OLSGD_ACT_GELU ? act_value<OLSGD_ACT_GELU>(a[e])
+                     : g.act == OLSGD_ACT_RELU ? act_value<OLSGD_ACT_RELU>(a[e])
+                                               : act_value<OLSGD_ACT_SIGMOID>(a[e]));
+  }
+  store_floats<T, 8>(out, c, g.cols, g.out_vec, a);
+}
+
 // Rows of any pitch to rows of a pitch that TMA takes: up to three operands [m][rows][cols] of
 // 16-bit values, blockIdx.z counting them.  A thread makes one aligned 16-byte piece out of the
 // two that its elements lie in (`begin` and `end` bound the tensor: nothing outside it is read).
@@ -668,7 +732,7 @@ cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   g.row_tiles = (g.rows + CTAS * kBM - 1) / (CTAS * kBM);
   g.col_tiles = (g.cols + kColsOut - 1) / kColsOut;
-  const int64_t total = (int64_t)g.problems * g.row_tiles * g.col_tiles;
+  const int64_t total = (int64_t)g.problems * g.splits * g.row_tiles * g.col_tiles;
   const int64_t room = sm_count() / CTAS;
   const unsigned ctas = (unsigned)((total < room ? total : room) * CTAS);
   g_tc_launches += 1;
@@ -690,38 +754,89 @@ cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kern, maps, g);
 }
 
-// Which tiles.  A tile's time goes by the operand bytes that one CTA takes in per K block
-// (128 rows of A and BN / CTAS rows of B), plus an epilogue that is not hidden in the last wave;
-// the launch takes as many waves as its tiles need.  The shape with the least product is taken:
-// pairs for large problems, 128 or 64 columns where wider tiles would leave multiprocessors
-// without one.
+// Which tiles, and into how many parts K is cut.  A tile's time goes by the operand bytes that one
+// CTA takes in per K block (128 rows of A and BN / CTAS rows of B), plus an epilogue that is not
+// hidden in the last wave; the launch takes as many waves as its tiles need.  Where tiles are few
+// and K is long, the parts' sums go through the workspace and a joining launch, which costs
+// about as much as 12 K blocks of 256 rows and the traffic.  The least sum is taken: pairs for
+// large problems, narrower tiles and parts of K where multiprocessors would be idle.  One worker,
+// 512 tokens, 1024 <- 2 x 4096 (element-wise pass and DX): 24 us in eight parts, 47 us uncut.
+// (Sizes alone decide, so that the workspace can be asked for anywhere.)
+constexpr int kSms = 148;
+constexpr int kMaxSplits = 16;
 struct Shape {
-  int ctas, bn;
+  int ctas, bn, splits;
+};
+struct Product {
+  int64_t problems, rows, cols, num_kb;
 };
 template <int MODE>
-Shape shape_for(const GatedArgs& g) {
-  constexpr Shape shapes[] = {{1, 64}, {1, 128}, {1, 256}, {2, 256}};
+Shape shape_for(const Product& d) {
+  constexpr Shape shapes[] = {{1, 64, 1}, {1, 128, 1}, {1, 256, 1}, {2, 256, 1}};
   Shape best = shapes[0];
-  int64_t least = INT64_MAX;
+  double least = 1e300;
   for (const Shape& sh : shapes) {
     const int64_t cols = MODE == FORWARD ? sh.bn / 2 : sh.bn;
-    const int64_t tiles = (int64_t)g.problems * ((g.rows + sh.ctas * kBM - 1) / (sh.ctas * kBM)) * ((g.cols + cols - 1) / cols);
-    const int64_t room = sm_count() / sh.ctas, waves = (tiles + room - 1) / room;
-    const int64_t cost = waves * (g.num_kb + 4) * (kBM + sh.bn / sh.ctas);
-    if (cost < least) {
-      least = cost;
-      best = sh;
+    const int64_t tiles = d.problems * ((d.rows + sh.ctas * kBM - 1) / (sh.ctas * kBM)) * ((d.cols + cols - 1) / cols);
+    const int64_t room = kSms / sh.ctas;
+    for (int splits = 1; splits <= kMaxSplits && (splits == 1 || d.num_kb >= 4 * splits); splits *= 2) {
+      const int64_t waves = (tiles * splits + room - 1) / room, kbs = (d.num_kb + splits - 1) / splits;
+      double cost = (double)waves * (kbs + 4) * (kBM + sh.bn / sh.ctas);
+      // the parts are written and read: 8 bytes an element at 6 bytes a picosecond, 900 rows a us
+      if (splits > 1)
+        cost += 3000.0 + splits * (double)d.problems * d.rows * d.cols * (MODE == FORWARD ? 2 : 1) * 8 / 6.0e6 * 900;
+      if (cost < least) {
+        least = cost;
+        best = Shape{sh.ctas, sh.bn, splits};
+      }
     }
   }
   return best;
 }
 
+Product product_of(int mode, const GatedShape& d) {
+  const auto kbs = [](int64_t k) { return (k + kBK - 1) / kBK; };
+  if (mode == FORWARD) return Product{d.m, d.T, d.F, kbs(d.D)};
+  if (mode == DX) return Product{d.m, d.T, d.D, 2 * kbs(d.F)};
+  return Product{2 * d.m, d.F, d.D, kbs(d.T)};
+}
+template <int MODE>
+size_t parts_bytes(const GatedShape& d) {
+  const Product p = product_of(MODE, d);
+  const int splits = shape_for<MODE>(p).splits;
+  return splits == 1 ? 0 : (size_t)splits * p.problems * p.rows * round8(p.cols) * (MODE == FORWARD ? 2 : 1) * sizeof(float);
+}
+// What shape_for decided, in the launch's arguments.
+template <int MODE>
+GatedArgs args_for(const GatedShape& d, const Shape& sh, uint8_t* parts) {
+  const Product p = product_of(MODE, d);
+  GatedArgs g{};
+  g.num_kb = (int)p.num_kb;
+  g.kb_half = (int)(p.num_kb / 2);
+  g.problems = (int)p.problems;
+  g.rows = (int)p.rows;
+  g.cols = (int)p.cols;
+  g.act = d.act;
+  g.f16 = d.f16;
+  g.pre_pitch = round8(p.cols);
+  g.splits = sh.splits;
+  g.kb_split = (int)((p.num_kb + sh.splits - 1) / sh.splits);
+  g.splits = (int)((p.num_kb + g.kb_split - 1) / g.kb_split);   // none is empty
+  g.parts = reinterpret_cast<float*>(parts);
+  g.parts_row = (MODE == FORWARD ? 2 : 1) * round8(p.cols);
+  return g;
+}
+
 template <int MODE>
 cudaError_t launch_mode(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
-  if (sh.bn == 64) return launch_variant<MODE, 1, 64, 8>(maps, g, s);
-  if (sh.bn == 128) return launch_variant<MODE, 1, 128, 6>(maps, g, s);
-  if (sh.ctas == 2) return launch_variant<MODE, 2, 256, 6>(maps, g, s);
-  return launch_variant<MODE, 1, 256, 4>(maps, g, s);
+  const cudaError_t e = sh.bn == 64    ? launch_variant<MODE, 1, 64, 8>(maps, g, s)
+                        : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6>(maps, g, s)
+                        : sh.ctas == 2 ? launch_variant<MODE, 2, 256, 6>(maps, g, s)
+                                       : launch_variant<MODE, 1, 256, 4>(maps, g, s);
+  if (e != cudaSuccess || g.splits == 1) return e;
+  const int64_t width = MODE == FORWARD ? g.pre_pitch : g.parts_row, warps = g.rows * ((width + 255) / 256);
+  return launch_chained(g.f16 ? gated_join_kernel<__half, MODE> : gated_join_kernel<__nv_bfloat16, MODE>,
+                        dim3((unsigned)((warps + 7) / 8), (unsigned)g.problems), dim3(256), 0, s, g);
 }
 
 bool tma_ready(const GatedOperand& o, int64_t rows, int64_t m) {
@@ -794,11 +909,31 @@ cudaError_t few(const GatedForward& a, cudaStream_t s) {
 
 }  // namespace
 
+// The workspace: copies of operands that TMA cannot take, then da and db (backward), then the parts of
+// one product at a time.
+struct Workspace {
+  size_t copies, da, db, parts, total;
+};
+Workspace layout(const GatedShape& d, bool backward, bool copies) {
+  Workspace w{};
+  w.da = copies ? round256((size_t)d.m * d.T * round8(d.D) * 2) + 2 * round256((size_t)d.m * d.F * round8(d.D) * 2) : 0;
+  const size_t part = backward ? round256((size_t)d.m * d.T * round8(d.F) * 2) : 0;
+  w.db = w.da + part;
+  w.parts = w.db + part;
+  size_t parts = 0;
+  if (backward) {
+    const size_t dx = parts_bytes<DX>(d), dw = parts_bytes<DW>(d);
+    parts = dx > dw ? dx : dw;
+  } else {
+    parts = parts_bytes<FORWARD>(d);
+  }
+  w.total = w.parts + parts;
+  return w;
+}
+
 size_t gated_workspace(const GatedShape& d, bool backward, bool copies) {
   if (!backward && d.T <= kFewTokens) return 0;
-  const int64_t m = d.m, T = d.T, D = d.D, F = d.F;
-  const size_t copied = copies ? round256((size_t)m * T * round8(D) * 2) + 2 * round256((size_t)m * F * round8(D) * 2) : 0;
-  return copied + (backward ? 2 * round256((size_t)m * T * round8(F) * 2) : 0);
+  return layout(d, backward, copies).total;
 }
 
 bool gated_needs_copies(const GatedShape& d, const GatedOperand& x, const GatedOperand& wg, const GatedOperand& wu) {
@@ -808,23 +943,17 @@ bool gated_needs_copies(const GatedShape& d, const GatedOperand& x, const GatedO
 cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
   if (a.T <= kFewTokens) return a.f16 ? few<__half>(a, s) : few<__nv_bfloat16>(a, s);
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  const Workspace at = layout(a, false, gated_needs_copies(a, a.x, a.wg, a.wu));
   const Wanted wanted[] = {{&a.x, a.T}, {&a.wg, a.F}, {&a.wu, a.F}};
   OLSGD_STEP(make_ready(wanted, 3, a.D, a.m, ws, s));
-  GatedArgs g{};
-  g.num_kb = (int)((a.D + kBK - 1) / kBK);
-  g.problems = (int)a.m;
-  g.rows = (int)a.T;
-  g.cols = (int)a.F;
-  g.act = a.act;
-  g.f16 = a.f16;
+  const Shape sh = shape_for<FORWARD>(product_of(FORWARD, a));
+  GatedArgs g = args_for<FORWARD>(a, sh, ws + at.parts);
   g.out_vec = whole_pieces(a.h, a.F);
   g.out0 = a.h;
   g.pre = a.pre;
-  g.pre_pitch = round8(a.F);
-  const Shape sh = shape_for<FORWARD>(g);
+  g.a_rows = loaded_rows(a.T);
   GatedMaps maps;
   const int b_rows = sh.bn / 2;
-  g.a_rows = loaded_rows(a.T);
   if (!make_map16(&maps.a0, a.x, a.D, a.T, a.m, g.a_rows, a.f16) || !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, b_rows, a.f16) ||
       !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, b_rows, a.f16))
     return cudaErrorInvalidValue;
@@ -834,40 +963,29 @@ cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
 
 cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   const int64_t pitch = round8(a.F);
-  const size_t part = round256((size_t)a.m * a.T * pitch * 2);
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
-  void* da = ws;
-  void* db = ws + part;
-  ws += 2 * part;
+  const Workspace at = layout(a, true, gated_needs_copies(a, a.x, a.wg, a.wu));
+  void *da = ws + at.da, *db = ws + at.db;
   const Wanted wanted[] = {{&a.x, a.T}, {&a.wg, a.F}, {&a.wu, a.F}};   // x for the weights' gradients, the weights for dx
   const int from = a.dwg ? 0 : 1, to = a.dx ? 3 : 1;
   OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s));
   OLSGD_STEP(a.f16 ? elementwise<__half>(a, pitch, da, db, s) : elementwise<__nv_bfloat16>(a, pitch, da, db, s));
   const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
   if (a.dx) {
-    GatedArgs g{};
-    g.kb_half = (int)((a.F + kBK - 1) / kBK);
-    g.num_kb = 2 * g.kb_half;
-    g.problems = (int)a.m;
-    g.rows = (int)a.T;
-    g.cols = (int)a.D;
-    g.f16 = a.f16;
+    const Shape sh = shape_for<DX>(product_of(DX, a));
+    GatedArgs g = args_for<DX>(a, sh, ws + at.parts);
     g.out_vec = whole_pieces(a.dx, a.D);
     g.out0 = a.dx;
-    GatedMaps maps;
     g.a_rows = loaded_rows(a.T);
+    GatedMaps maps;
     if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, g.a_rows, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, g.a_rows, a.f16) ||
         !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, kBK, a.f16) || !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, kBK, a.f16))
       return cudaErrorInvalidValue;
-    OLSGD_STEP(launch_mode<DX>(shape_for<DX>(g), maps, g, s));
+    OLSGD_STEP(launch_mode<DX>(sh, maps, g, s));
   }
   if (a.dwg) {
-    GatedArgs g{};
-    g.num_kb = (int)((a.T + kBK - 1) / kBK);
-    g.problems = (int)(2 * a.m);
-    g.rows = (int)a.F;
-    g.cols = (int)a.D;
-    g.f16 = a.f16;
+    const Shape sh = shape_for<DW>(product_of(DW, a));
+    GatedArgs g = args_for<DW>(a, sh, ws + at.parts);
     g.out_vec = whole_pieces(a.dwg, a.D) && whole_pieces(a.dwu, a.D);
     g.out0 = a.dwg;
     g.out1 = a.dwu;
@@ -876,7 +994,7 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
         !make_map16(&maps.b0, a.x, a.D, a.T, a.m, kBK, a.f16))
       return cudaErrorInvalidValue;
     maps.b1 = maps.b0;
-    OLSGD_STEP(launch_mode<DW>(shape_for<DW>(g), maps, g, s));
+    OLSGD_STEP(launch_mode<DW>(sh, maps, g, s));
   }
   return cudaSuccess;
 }
