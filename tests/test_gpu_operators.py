@@ -595,3 +595,66 @@ def test_embedding_empty_batches_and_refusals():
                 lambda: lib.embedding_backward(table, ids, 9), lambda: lib.embedding_backward(table[:, :4], ids, 9, out=table[:, :8])):
         with pytest.raises(ValueError):
             bad()
+
+
+# ------------------------------------------------------------------- sizes past 32-bit offsets
+
+def test_token_logprobs_past_32_bit_offsets():
+    N, V = 66000, 32800   # 2.16e9 logits
+    g = _gen(21)
+    x = torch.empty((N, V), dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=g)
+    t = torch.randint(0, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    r = lib.token_logprobs(x, t, 2)
+    d = lib.token_logprobs_backward(r.logp, None, x, t, r.stats, r.entropy)
+    for rows in (slice(0, 3), slice(N - 3, N), slice(65472, 65476)):
+        s = lib.token_logprobs(x[rows].clone(), t[rows].clone(), 2)
+        # fewer rows are split over more CTAs: sums in another order
+        assert torch.allclose(r.logp[rows], s.logp, rtol=0, atol=3 * _sum_error(V, 12.0)) and torch.equal(r.top_ids[rows], s.top_ids)
+        p = torch.softmax(x[rows].double(), dim=1)
+        want = r.logp[rows].double()[:, None] * (torch.zeros_like(p).scatter_(1, t[rows].long()[:, None], 1.0) - p)
+        assert bool(((d[rows].double() - want).abs() <= want.abs() * 2.0 ** -7).all())
+
+
+def test_embedding_past_32_bit_offsets():
+    V, D, T = 1 << 21, 1040, 300   # 2.18e9 elements of the table
+    g = _gen(22)
+    table = torch.zeros((1, V, D), dtype=torch.bfloat16, device="cuda")
+    ids = torch.randint(V - 50, V, (1, T), generator=g, device="cuda", dtype=torch.int32)
+    ids[0, :3] = torch.tensor([0, V - 1, V // 2], dtype=torch.int32, device="cuda")
+    table[0, V - 50:].normal_(generator=g)
+    out = lib.embedding_forward(table, ids)
+    assert torch.equal(out[0], table[0][ids[0].long()])
+    d = torch.full_like(table, 3.0)
+    lib.embedding_backward(out, ids, V, out=d)
+    want = torch.zeros((50, D), dtype=torch.float64, device="cuda")
+    late = ids[0] >= V - 50
+    want.index_add_(0, ids[0][late].long() - (V - 50), out[0][late].double())
+    assert bool(((d[0, V - 50:].double() - want).abs() <= want.abs() * 2.0 ** -8 + 64 * U * 20).all())
+    assert not bool(d[0, 1:V // 2].any()) and not bool(d[0, V // 2 + 1:V - 50].any())
+
+
+def test_gated_block_past_32_bit_offsets():
+    T, D, F = 66000, 16, 32800   # 2.16e9 results
+    g = _gen(23)
+    x, w = _randn(g, (1, T, D), torch.bfloat16), _randn(g, (2, F, D), torch.bfloat16)
+    h = lib.gated_forward(x, w[:1], w[1:], "relu")
+    for rows in (slice(0, 128), slice(T - 130, T)):
+        a, b = x[:, rows].double() @ w[:1].double().mT, x[:, rows].double() @ w[1:].double().mT
+        want = a.clamp(min=0) * b
+        tol = want.abs() * 2.0 ** -8 + _product_error(D) * (x[:, rows].double().abs() @ w[:1].double().abs().mT) * (b.abs() + 1) \
+            + _product_error(D) * (x[:, rows].double().abs() @ w[1:].double().abs().mT) * a.abs()
+        assert bool(((h[:, rows].double() - want).abs() <= tol).all())
+
+
+def test_clip_grads_past_32_bit_offsets_and_of_many_workers():
+    x = torch.zeros((2, 2200000000), dtype=torch.bfloat16, device="cuda")
+    x[0, -1], x[1, -2], x[1, 5] = 3.0, 4.0, 3.0
+    _, norms = lib.clip_grads(x, 1.0, out=x)
+    assert norms.tolist() == [3.0, 5.0]
+    assert abs(float(x[0, -1]) - 1.0) < 2.0 ** -8 and abs(float(x[1, -2]) - 0.8) < 2.0 ** -8 and abs(float(x[1, 5]) - 0.6) < 2.0 ** -8
+    assert int(torch.count_nonzero(x[0])) == 1 and int(torch.count_nonzero(x[1])) == 2
+    g = _gen(24)
+    grads = [_randn(g, (700, 37)), _randn(g, (700, 1), torch.float16)]
+    out, norms = lib.clip_grads(grads, 3.0)
+    _check_clip(grads, 3.0, out, norms)

@@ -254,3 +254,31 @@ def test_operators_on_the_legacy_stream_of_another_thread():
     assert not errors
     for g in got:
         assert all(torch.equal(x, y) for x, y in zip(g, want))
+
+
+def test_operators_captured_before_anything_else_ran(tmp_path):
+    """The first call a process makes of every operator may be the one that is captured."""
+    import subprocess
+    import sys
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import sys, torch
+sys.path[:0] = [%r, %r]
+from test_gpu_operators_together import _calls
+make, run = _calls(0)
+a = make(1)
+s = torch.cuda.Stream()
+s.wait_stream(torch.cuda.current_stream())
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph, stream=s):
+    got = run(a)
+graph.replay()
+torch.cuda.synchronize()
+want = run(a)
+assert all(torch.equal(x, y) for x, y in zip(got, want))
+print("captured first: ok")
+""" % (root, os.path.join(root, "tests"))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured first: ok" in r.stdout, r.stderr[-2000:]
