@@ -242,14 +242,178 @@ __host__ __device__ constexpr uint32_t minus_inf() {
   return sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
 }
 
+// Finds a row's alternatives; by a whole CTA.
+//
+// Both selections (the k best chunks, the k best elements of those) go by a floor: a value
+// that k candidates reach.  What is below it is dropped, which leaves little more than k
+// keys in a list, and each of those counts how many are larger: its place in the order.  Rows in
+// which very many elements tie can overflow the list; they take k rounds of a maximum instead.
+constexpr int kList = 1024;
+constexpr int kGroups = 64;   // of four threads
+static_assert(kGroups >= kMaxTop && kGroups * 4 == kThreads, "the k-th best group gives the floor");
+static_assert(kMaxTop * kMaxTop <= kList, "k of each of k chunks");
+struct TopShared {
+  uint64_t group_best[kGroups];
+  uint64_t list[kList];
+  uint64_t floor_key;
+  int32_t chosen[kMaxTop];
+  int n_list[2], n_chosen;
+};
+
+template <typename T>
+__device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r, int V, int nchunks, float* cm, const RowState& st,
+                                         int top, float* top_logp, int32_t* top_ids) {
+  constexpr int VEC = Elem<T>::kVec;
+  constexpr int Q = kChunkElems / 32 / VEC;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int shift = row_shift(row);
+  if (st.s != st.s) {
+    // a NaN (or +inf) in the row: the maxima passed over it, and are formed again
+    for (int c = warp; c < nchunks; c += kWarps) {
+      float v = raw_max<T, true>(load_raw<T>(row, c * kChunkElems + lane * VEC - shift, V, minus_inf<T>()));
+      if (Q == 2) v = max_nan(v, raw_max<T, true>(load_raw<T>(row, c * kChunkElems + (32 + lane) * VEC - shift, V, minus_inf<T>())));
+      const uint32_t order = __reduce_max_sync(0xffffffffu, order_of(v));
+      if (lane == 0) cm[c] = value_of(order);
+    }
+    __syncthreads();
+  }
+  // 1. the best chunks
+  uint64_t best = 0;
+  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
+    const uint64_t key = key_of(order_of(cm[c]), c);
+    best = key > best ? key : best;
+  }
+#pragma unroll
+  for (int off = 1; off < 4; off <<= 1) {
+    const uint64_t other = __shfl_xor_sync(0xffffffffu, best, off);
+    best = other > best ? other : best;
+  }
+  if ((threadIdx.x & 3) == 0) sh.group_best[threadIdx.x >> 2] = best;
+  if (threadIdx.x == 0) {
+    sh.n_list[0] = sh.n_list[1] = 0;
+    sh.n_chosen = min(top, nchunks);
+    sh.floor_key = 1;   // fewer groups than k: every chunk is a candidate
+  }
+  __syncthreads();
+  if (threadIdx.x < kGroups) {
+    const uint64_t mine = sh.group_best[threadIdx.x];
+    int larger = 0;
+    for (int i = 0; i < kGroups; ++i) larger += sh.group_best[i] > mine;
+    if (mine && larger == top - 1) sh.floor_key = mine;
+  }
+  __syncthreads();
+  const uint64_t chunk_floor = sh.floor_key;
+  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
+    const uint64_t key = key_of(order_of(cm[c]), c);
+    if (key >= chunk_floor) {
+      const int at = atomicAdd(&sh.n_list[0], 1);
+      if (at < kList) sh.list[at] = key;
+    }
+  }
+  __syncthreads();
+  const int n0 = sh.n_list[0];
+  if (threadIdx.x == 0) sh.floor_key = 0;   // (every thread has read chunk_floor)
+  __syncthreads();
+  // sh.chosen chunks in any order; the floor for their elements is the k-th one's maximum
+  if (n0 <= kList) {
+    for (int i = threadIdx.x; i < n0; i += kThreads) {
+      const uint64_t mine = sh.list[i];
+      int larger = 0;
+      for (int q = 0; q < n0; ++q) larger += sh.list[q] > mine;
+      if (larger < top) sh.chosen[larger] = index_of(mine);
+      if (larger == top - 1) sh.floor_key = mine & 0xFFFFFFFF00000000ull;
+    }
+  } else if (warp == 0) {
+    warp_select(
+        top, 0,
+        [&](uint64_t limit) {
+          uint64_t b = 0;
+          for (int c = lane; c < nchunks; c += 32) {
+            const uint64_t key = key_of(order_of(cm[c]), c);
+            if (key < limit && key > b) b = key;
+          }
+          return b;
+        },
+        [&](int q, uint64_t key) {
+          sh.chosen[q] = index_of(key);
+          if (q == top - 1) sh.floor_key = key & 0xFFFFFFFF00000000ull;
+        });
+  }
+  __syncthreads();
+
+  // 2. the elements of the sh.chosen chunks that reach the floor
+  const uint64_t elem_floor = sh.floor_key;
+  const int nc = sh.n_chosen;
+  for (int i = warp; i < nc; i += kWarps) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int j0 = sh.chosen[i] * kChunkElems + (q * 32 + lane) * VEC - shift;
+      const uint4 w = load_raw<T>(row, j0, V, minus_inf<T>());
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float v, other;
+        unpack2f(raw_pair<T>(w, e / 2), v, other);
+        const uint64_t key = key_of(order_of(e % 2 ? other : v), j0 + e);
+        if (key >= elem_floor && j0 + e >= 0 && j0 + e < V) {
+          const int at = atomicAdd(&sh.n_list[1], 1);
+          if (at < kList) sh.list[at] = key;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  int n1 = sh.n_list[1];
+  if (n1 > kList) {
+    // too many ties: the first k of each sh.chosen chunk, by rounds
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n_list[1] = 0;
+    __syncthreads();
+    for (int i = warp; i < nc; i += kWarps) {
+      const int j0 = sh.chosen[i] * kChunkElems + lane * VEC - shift;
+      float v[Q][VEC];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) load_piece<T>(row, j0 + q * 32 * VEC, V, -INFINITY, v[q]);
+      warp_select(
+          top, elem_floor,
+          [&](uint64_t limit) {
+            uint64_t b = 0;
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) {
+                const int j = j0 + q * 32 * VEC + e;
+                const uint64_t key = key_of(order_of(v[q][e]), j);
+                if (j >= 0 && j < V && key < limit && key > b) b = key;
+              }
+            return b;
+          },
+          [&](int, uint64_t key) { sh.list[atomicAdd(&sh.n_list[1], 1)] = key; });
+    }
+    __syncthreads();
+    n1 = sh.n_list[1];
+  }
+  // each takes its place (the list's own order does not matter: keys differ)
+  const float log_s = log_sum(st);
+  for (int i = threadIdx.x; i < n1; i += kThreads) {
+    const uint64_t mine = sh.list[i];
+    int larger = 0;
+    for (int q = 0; q < n1; ++q) larger += sh.list[q] > mine;
+    if (larger < top) {
+      top_ids[r * top + larger] = index_of(mine);
+      top_logp[r * top + larger] = log_prob(value_of((uint32_t)(mine >> 32)), st, log_s);
+    }
+  }
+}
+
 // CTA (r, split): chunks [split * cps, (split + 1) * cps) of row r, dealt to the warps in turn.
-// Per element the loop spends
-// about six instructions (packed fp32 for the difference, the product and both sums; the
-// maximum in the element's own type).
+// Per element the loop spends about six instructions (packed fp32 for the difference, the product
+// and both sums; the maximum in the element's own type).  An unsplit row is finished here: while
+// one CTA looks for its alternatives the others of the multiprocessor go on reading.
 template <typename T, bool TOP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads)
 logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int cps, RowOut o,
-                   float4* __restrict__ part, uint32_t* __restrict__ chunk_max) {
+                   float4* __restrict__ part, float* chunk_max, int top, float* __restrict__ top_logp,
+                   int32_t* __restrict__ top_ids) {
   constexpr int VEC = Elem<T>::kVec;
   constexpr int Q = kChunkElems / 32 / VEC;   // pieces of a chunk per lane
   constexpr int U = kUnroll / Q;              // chunks per turn
@@ -289,21 +453,16 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
     float mx = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float cm = raw_max<T, TOP>(w[u][0]);
-      if (Q == 2) {
-        const float other = raw_max<T, TOP>(w[u][Q - 1]);
-        cm = TOP ? max_nan(cm, other) : fmaxf(cm, other);
-      }
+      float cm = raw_max<T, false>(w[u][0]);
+      if (Q == 2) cm = fmaxf(cm, raw_max<T, false>(w[u][Q - 1]));
       if (TOP) {
-        // over the warp as an ordered integer, in which a NaN comes first
-        const uint32_t order = __reduce_max_sync(0xffffffffu, order_of(cm));
+        asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(cm));
         const int c = c0 + u * kWarps;
-        if (lane == 0 && c < c_end) chunk_max[r * nchunks + c] = order;
-        cm = value_of(order);   // (a NaN does not move the running maximum)
+        if (lane == 0 && c < c_end) chunk_max[r * nchunks + c] = cm;
       }
       mx = fmaxf(mx, cm);
     }
-    if (!TOP) asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(mx) : "f"(mx));
+    if (!TOP) asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(mx));
     if (mx > m) {
       rebase2(m, mx, s, t);
       m = mx;
@@ -325,6 +484,7 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
   unpack2f(t, lo, hi);
   st.t = warp_sum(lo + hi);
   __shared__ RowState sh[kWarps];
+  __shared__ RowState whole;
   if (lane == 0) sh[warp] = st;
   __syncthreads();
   if (warp == 0) {
@@ -332,42 +492,31 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
     if (lane < kWarps) a = sh[lane];
     a = shfl_join(a);
     if (lane == 0) {
+      whole = a;
       if (WHOLE) write_row(o, target, r, a);
       else part[r * gridDim.y + blockIdx.y] = make_float4(a.m, a.s, a.t, 0.f);
     }
   }
+  if constexpr (TOP && WHOLE) {
+    __shared__ TopShared ts;
+    __syncthreads();   // (the chunks' maxima too)
+    find_top<T>(ts, row, r, V, nchunks, chunk_max + r * nchunks, whole, top, top_logp, top_ids);
+  }
 }
 
-// Joins a row's parts and finds its alternatives; one CTA per row.
-//
-// Both selections (the k best chunks, the k best elements of those) go by a floor: a value
-// that k candidates reach.  What is below it is dropped, which leaves little more than k
-// keys in a list, and each of those counts how many are larger: its place in the order.  Rows in
-// which very many elements tie can overflow the list; they take k rounds of a maximum instead.
-constexpr int kList = 1024;
-
+// Joins a row's parts (and finds its alternatives); one CTA per row.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int nsplit, RowOut o,
-                      const float4* __restrict__ part, const uint32_t* __restrict__ chunk_max, int top,
-                      float* __restrict__ top_logp, int32_t* __restrict__ top_ids) {
-  constexpr int VEC = Elem<T>::kVec;
-  constexpr int Q = kChunkElems / 32 / VEC;
-  constexpr int kGroups = 64;   // of four threads
-  static_assert(kGroups >= kMaxTop && kGroups * 4 == kThreads, "the k-th best group gives the floor");
-  __shared__ uint64_t group_best[kGroups];
-  __shared__ uint64_t list[kList];
-  __shared__ int32_t chosen[kMaxTop];
-  __shared__ uint64_t floor_key;
-  __shared__ int n_list[2], n_chosen;
+                      const float4* __restrict__ part, float* chunk_max, int top, float* __restrict__ top_logp,
+                      int32_t* __restrict__ top_ids) {
+  __shared__ TopShared sh;
   __shared__ RowState whole;
   launch_gate();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
   const int64_t r = blockIdx.x;
   const T* row = x + r * ld;
-  const int shift = row_shift(row);
-
-  if (warp == kWarps - 1) {
+  if (threadIdx.x < 32) {
     const Target target = fetch_target<T>(o, row, r, V);
     RowState st{-INFINITY, 0.f, 0.f};
     for (int i = lane; i < nsplit; i += 32) {
@@ -381,137 +530,9 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
     }
   }
   if (top == 0) return;
-
-  // 1. the best chunks
-  const uint32_t* cm = chunk_max + r * nchunks;
-  uint64_t best = 0;
-  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
-    const uint64_t key = key_of(cm[c], c);
-    best = key > best ? key : best;
-  }
-#pragma unroll
-  for (int off = 1; off < 4; off <<= 1) {
-    const uint64_t other = __shfl_xor_sync(0xffffffffu, best, off);
-    best = other > best ? other : best;
-  }
-  if ((threadIdx.x & 3) == 0) group_best[threadIdx.x >> 2] = best;
-  if (threadIdx.x == 0) {
-    n_list[0] = n_list[1] = 0;
-    n_chosen = min(top, nchunks);
-    floor_key = 1;   // fewer groups than k: every chunk is a candidate
-  }
   __syncthreads();
-  if (threadIdx.x < kGroups) {
-    const uint64_t mine = group_best[threadIdx.x];
-    int larger = 0;
-    for (int i = 0; i < kGroups; ++i) larger += group_best[i] > mine;
-    if (mine && larger == top - 1) floor_key = mine;
-  }
-  __syncthreads();
-  const uint64_t chunk_floor = floor_key;
-  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
-    const uint64_t key = key_of(cm[c], c);
-    if (key >= chunk_floor) {
-      const int at = atomicAdd(&n_list[0], 1);
-      if (at < kList) list[at] = key;
-    }
-  }
-  __syncthreads();
-  const int n0 = n_list[0];
-  if (threadIdx.x == 0) floor_key = 0;   // (every thread has read chunk_floor)
-  __syncthreads();
-  // chosen chunks in any order; the floor for their elements is the k-th one's maximum
-  if (n0 <= kList) {
-    for (int i = threadIdx.x; i < n0; i += kThreads) {
-      const uint64_t mine = list[i];
-      int larger = 0;
-      for (int q = 0; q < n0; ++q) larger += list[q] > mine;
-      if (larger < top) chosen[larger] = index_of(mine);
-      if (larger == top - 1) floor_key = mine & 0xFFFFFFFF00000000ull;
-    }
-  } else if (warp == 0) {
-    warp_select(
-        top, 0,
-        [&](uint64_t limit) {
-          uint64_t b = 0;
-          for (int c = lane; c < nchunks; c += 32) {
-            const uint64_t key = key_of(cm[c], c);
-            if (key < limit && key > b) b = key;
-          }
-          return b;
-        },
-        [&](int q, uint64_t key) {
-          chosen[q] = index_of(key);
-          if (q == top - 1) floor_key = key & 0xFFFFFFFF00000000ull;
-        });
-  }
-  __syncthreads();
-
-  // 2. the elements of the chosen chunks that reach the floor
-  const uint64_t elem_floor = floor_key;
-  const int nc = n_chosen;
-  for (int i = warp; i < nc; i += kWarps) {
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const int j0 = chosen[i] * kChunkElems + (q * 32 + lane) * VEC - shift;
-      const uint4 w = load_raw<T>(row, j0, V, minus_inf<T>());
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float v, other;
-        unpack2f(raw_pair<T>(w, e / 2), v, other);
-        const uint64_t key = key_of(order_of(e % 2 ? other : v), j0 + e);
-        if (key >= elem_floor && j0 + e >= 0 && j0 + e < V) {
-          const int at = atomicAdd(&n_list[1], 1);
-          if (at < kList) list[at] = key;
-        }
-      }
-    }
-  }
-  __syncthreads();
-  int n1 = n_list[1];
-  if (n1 > kList) {
-    // too many ties: the first k of each chosen chunk, by rounds
-    __syncthreads();
-    if (threadIdx.x == 0) n_list[1] = 0;
-    __syncthreads();
-    for (int i = warp; i < nc; i += kWarps) {
-      const int j0 = chosen[i] * kChunkElems + lane * VEC - shift;
-      float v[Q][VEC];
-#pragma unroll
-      for (int q = 0; q < Q; ++q) load_piece<T>(row, j0 + q * 32 * VEC, V, -INFINITY, v[q]);
-      warp_select(
-          top, elem_floor,
-          [&](uint64_t limit) {
-            uint64_t b = 0;
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) {
-                const int j = j0 + q * 32 * VEC + e;
-                const uint64_t key = key_of(order_of(v[q][e]), j);
-                if (j >= 0 && j < V && key < limit && key > b) b = key;
-              }
-            return b;
-          },
-          [&](int, uint64_t key) { list[atomicAdd(&n_list[1], 1)] = key; });
-    }
-    __syncthreads();
-    n1 = n_list[1];
-  }
-  // each takes its place (the list's own order does not matter: keys differ)
-  const RowState st = whole;
-  const float log_s = log_sum(st);
-  for (int i = threadIdx.x; i < n1; i += kThreads) {
-    const uint64_t mine = list[i];
-    int larger = 0;
-    for (int q = 0; q < n1; ++q) larger += list[q] > mine;
-    if (larger < top) {
-      top_ids[r * top + larger] = index_of(mine);
-      top_logp[r * top + larger] = log_prob(value_of((uint32_t)(mine >> 32)), st, log_s);
-    }
-  }
+  find_top<T>(sh, row, r, V, nchunks, chunk_max + r * nchunks, whole, top, top_logp, top_ids);
 }
-static_assert(kMaxTop * kMaxTop <= kList, "k of each of k chunks");
 
 // ---------------------------------------------------------------------------- gradient
 // dx_j = dlp (1[j = t] - p_j) - dH p_j (log p_j + H): reads the logits once, writes once.
@@ -639,16 +660,16 @@ cudaError_t forward(const LogprobArgs& a, cudaStream_t s) {
   const Plan p = plan(a.rows, a.V, a.dtype);
   const int nchunks = p.nchunks, cps = p.cps, nsplit = p.nsplit;
   float4* part = static_cast<float4*>(a.ws);
-  uint32_t* cmax = reinterpret_cast<uint32_t*>(part + a.rows * nsplit);
+  float* cmax = reinterpret_cast<float*>(part + a.rows * nsplit);
   const dim3 grid((unsigned)a.rows, (unsigned)nsplit);
-  const bool whole = nsplit == 1 && a.top == 0;
-  auto k = a.top > 0 ? logprob_row_kernel<T, true, false>
-           : whole   ? logprob_row_kernel<T, false, true>
-                     : logprob_row_kernel<T, false, false>;
-  const cudaError_t e = launch_chained(k, grid, dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks, cps, o, part, cmax);
+  const bool whole = nsplit == 1;
+  auto k = a.top > 0 ? (whole ? logprob_row_kernel<T, true, true> : logprob_row_kernel<T, true, false>)
+                     : (whole ? logprob_row_kernel<T, false, true> : logprob_row_kernel<T, false, false>);
+  const cudaError_t e = launch_chained(k, grid, dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks, cps, o, part, cmax,
+                                       a.top, a.top_logp, a.top_ids);
   if (e != cudaSuccess || whole) return e;
   return launch_chained(logprob_finish_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks,
-                        nsplit, o, (const float4*)part, (const uint32_t*)cmax, a.top, a.top_logp, a.top_ids);
+                        nsplit, o, (const float4*)part, cmax, a.top, a.top_logp, a.top_ids);
 }
 
 template <typename T>
@@ -671,7 +692,7 @@ size_t logprob_workspace(int dtype, int64_t rows, int64_t V, int top) {
   const Plan p = plan(rows, V, dtype);
   if (p.nsplit == 1 && top == 0) return 0;
   // the parts of every row, and the chunk maxima
-  return (size_t)rows * p.nsplit * sizeof(float4) + (top > 0 ? (size_t)rows * p.nchunks * sizeof(uint32_t) : 0);
+  return (size_t)rows * p.nsplit * sizeof(float4) + (top > 0 ? (size_t)rows * p.nchunks * sizeof(float) : 0);
 }
 
 cudaError_t launch_logprobs(const LogprobArgs& a, cudaStream_t s) {
