@@ -75,30 +75,42 @@ constexpr int kSortTile = kSortThreads * kSortItems;       // entries per CTA
 constexpr int kBins = 256;
 constexpr int kSortCluster = 8;                            // CTAs that sort a list in one launch
 
-// Table rows without a token, kZeroBytes a CTA.
-constexpr int kZeroBytes = 256 << 10;
+// Table rows without a token: as many a CTA as give the GPU a few CTAs per multiprocessor, of 16 to 256 KB.
+constexpr int64_t kZeroBytesMin = 16 << 10, kZeroBytesMax = 256 << 10;
 constexpr int kZeroRowsMax = 2048;
 struct ZeroArgs {
   void* dtable;              // [m][V][row_bytes], workers worker_bytes apart
   int64_t V, row_bytes, worker_bytes;
   int rows, ctas;            // rows of a CTA, CTAs of a worker
 };
-// Rows [v0, v0 + n) of a worker that are not present, a warp per row.  Zeros are the same in every
-// type: 32 bytes a lane between the boundaries, 2 at the ends.
+// Rows [v0, v0 + n) of a worker that are not present.  Zeros are the same in every type: the rows are
+// walked as one run of bytes, 32 a thread, which are stored whole where no present row shares them
+// and by twos where one does (or where the run ends).
 __device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t worker, int64_t v0, int n, const uint8_t* present) {
-  const int lane = threadIdx.x & 31;
-  char* base = static_cast<char*>(z.dtable) + worker * z.worker_bytes;
-  for (int r = threadIdx.x >> 5; r < n; r += blockDim.x >> 5) {
-    if (present[r]) continue;
-    char *p = base + (v0 + r) * z.row_bytes, *end = p + z.row_bytes;
-    char* body = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(p) + 31) & ~(uintptr_t)31);
-    if (body > end) body = end;
-    for (char* q = p + lane * 2; q < body; q += 64) *reinterpret_cast<uint16_t*>(q) = 0;
-    char* tail = body + ((end - body) & ~(int64_t)31);
-    const uint32_t o = 0;
-    for (char* q = body + lane * 32; q < tail; q += 1024)
-      asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(q), "r"(o) : "memory");
-    for (char* q = tail + lane * 2; q < end; q += 64) *reinterpret_cast<uint16_t*>(q) = 0;
+  char* run = static_cast<char*>(z.dtable) + worker * z.worker_bytes + v0 * z.row_bytes;
+  const uint32_t row = (uint32_t)z.row_bytes, bytes = row * n, shift = (uint32_t)(reinterpret_cast<uintptr_t>(run) & 31);
+  for (uint32_t at = threadIdx.x * 32; at < bytes + shift; at += blockDim.x * 32) {
+    // bytes [lo, hi) of the run
+    const uint32_t lo = at < shift ? 0 : at - shift, hi = min(bytes, at + 32 - shift);
+    const uint32_t r0 = lo / row, r1 = hi - r0 * row <= row ? r0 : (hi - 1) / row;
+    bool any = false, all = true;
+    for (uint32_t r = r0; r <= r1; ++r) {
+      if (present[r]) any = true;
+      else all = false;
+    }
+    if (all) continue;
+    if (!any && hi - lo == 32) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(run + lo), "r"(0u) : "memory");
+    } else {
+      uint32_t r = r0, next = (r0 + 1) * row;   // (no row reaches past 2^30 bytes)
+      for (uint32_t b = lo; b < hi; b += 2) {
+        if (b >= next) {
+          ++r;
+          next += row;
+        }
+        if (!present[r]) *reinterpret_cast<uint16_t*>(run + b) = 0;
+      }
+    }
   }
 }
 
@@ -621,8 +633,10 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
   const dim3 sort_grid((unsigned)sort.tiles, (unsigned)g.m);
   const int out_size = g.out_dtype == OLSGD_F32 ? 4 : 2;
   ZeroArgs zero{g.dtable, g.V, g.D * out_size, g.dtable_worker * out_size, 0, 0};
-  zero.rows = (int)(kZeroBytes / zero.row_bytes);
-  zero.rows = zero.rows < 16 ? 16 : zero.rows > kZeroRowsMax ? kZeroRowsMax : zero.rows;
+  int64_t share = g.m * g.V * zero.row_bytes / (148 * 4);
+  share = share < kZeroBytesMin ? kZeroBytesMin : share > kZeroBytesMax ? kZeroBytesMax : share;
+  zero.rows = (int)(share / zero.row_bytes < kZeroRowsMax ? share / zero.row_bytes : kZeroRowsMax);   // (sixteen of the longest rows are 2^30 bytes: 32 bits count them)
+  if (zero.rows < 16) zero.rows = 16;
   zero.ctas = (int)((g.V + zero.rows - 1) / zero.rows);
   int passes = 0;
   while (g.T > 0 && (g.V >> (8 * passes)) > 0) ++passes;   // keys are 0 .. V

@@ -30,6 +30,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;            // chunks, or pieces of the gradient, in flight
 constexpr int kChunkElems = 256;      // eight elements per lane: one 16-byte piece, or two of fp32
 constexpr int kWarpRowMax = 1024;     // longest row that stays in a warp's registers
+constexpr int kWarpList = 160;        // candidates that a warp lists
 constexpr int kMaxTop = OLSGD_MAX_TOP;
 static_assert(kMaxTop == 32, "a lane holds one candidate of each warp");
 constexpr int kMaxSplit = 64;
@@ -216,23 +217,89 @@ logprob_warp_kernel(const T* __restrict__ x, int64_t rows, int V, int64_t ld, Ro
   st.t = warp_sum(st.t);
   if (lane == 0) write_row(o, target, r, st);
   if (top > 0) {
+    // As for long rows (find_top): the k-th best of the groups' maxima is a floor; what reaches it is
+    // listed, and takes its place by counting.  Should the list overflow: rounds of a maximum.
+    __shared__ uint64_t lists[kWarps][kWarpList];
+    uint64_t* list = lists[threadIdx.x >> 5];
     const float log_s = log_sum(st);
-    warp_select(
-        top, 0,
-        [&](uint64_t limit) {
-          uint64_t b = 0;
+    const auto put = [&](int q, uint64_t key) {
+      top_ids[r * top + q] = index_of(key);
+      top_logp[r * top + q] = log_prob(value_of((uint32_t)(key >> 32)), st, log_s);
+    };
+    uint32_t ord[NL];   // of an element past the row: 0, below every other
 #pragma unroll
-          for (int i = 0; i < NL; ++i) {
-            const int j = i * 32 + lane;
-            const uint64_t key = key_of(order_of(v[i]), j);
-            if (j < V && key < limit && key > b) b = key;
-          }
-          return b;
-        },
-        [&](int q, uint64_t key) {
-          top_ids[r * top + q] = index_of(key);
-          top_logp[r * top + q] = log_prob(value_of((uint32_t)(key >> 32)), st, log_s);
-        });
+    for (int i = 0; i < NL; ++i) ord[i] = i * 32 + lane < V ? order_of(v[i]) : 0u;
+    const auto key_at = [&](int i) { return ord[i] ? key_of(ord[i], i * 32 + lane) : 0ull; };
+    if (NL == 1) {
+      const uint64_t mine = key_at(0);
+      int larger = 0;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) larger += __shfl_sync(0xffffffffu, mine, i) > mine;
+      if (mine && larger < top) put(larger, mine);
+      return;
+    }
+    // 64 groups: the halves of the lanes' elements (the lower index comes first among equals)
+    uint64_t best[2];
+    int larger[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t o = 0;
+      int at = 0;
+#pragma unroll
+      for (int i = h * (NL / 2); i < (h + 1) * (NL / 2); ++i) {
+        if (ord[i] > o) {
+          o = ord[i];
+          at = i;
+        }
+      }
+      best[h] = o ? key_of(o, at * 32 + lane) : 0ull;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const uint64_t a = __shfl_sync(0xffffffffu, best[0], i), b = __shfl_sync(0xffffffffu, best[1], i);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) larger[h] += (a > best[h]) + (b > best[h]);
+    }
+    uint64_t floor_key = 1;   // fewer groups than k: all are candidates
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t here = __ballot_sync(0xffffffffu, best[h] && larger[h] == top - 1);
+      if (here) floor_key = __shfl_sync(0xffffffffu, best[h], __ffs(here) - 1);
+    }
+    const uint32_t floor_order = (uint32_t)(floor_key >> 32);
+    const int floor_at = floor_key == 1 ? V : index_of(floor_key);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const bool reaches = ord[i] > floor_order || (ord[i] == floor_order && ord[i] && i * 32 + lane <= floor_at);
+      const uint32_t in = __ballot_sync(0xffffffffu, reaches);
+      const int at = n + __popc(in & ((1u << lane) - 1));
+      if (reaches && at < kWarpList) list[at] = key_of(ord[i], i * 32 + lane);
+      n += __popc(in);
+    }
+    __syncwarp();
+    if (n <= kWarpList) {
+      for (int i = lane; i < n; i += 32) {
+        const uint64_t mine = list[i];
+        int above = 0;
+#pragma unroll 4
+        for (int q = 0; q < n; ++q) above += list[q] > mine;
+        if (above < top) put(above, mine);
+      }
+    } else {
+      warp_select(
+          top, 0,
+          [&](uint64_t limit) {
+            uint64_t b = 0;
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+              const uint64_t key = key_at(i);
+              if (key < limit && key > b) b = key;
+            }
+            return b;
+          },
+          put);
+    }
   }
 }
 
@@ -244,20 +311,23 @@ __host__ __device__ constexpr uint32_t minus_inf() {
 
 // Finds a row's alternatives; by a whole CTA.
 //
-// Both selections (the k best chunks, the k best elements of those) go by a floor: a value
-// that k candidates reach.  What is below it is dropped, which leaves little more than k
-// keys in a list, and each of those counts how many are larger: its place in the order.  Rows in
-// which very many elements tie can overflow the list; they take k rounds of a maximum instead.
+// The chunks' maxima are dealt to 64 groups.  The k-th best of the groups' maxima is a floor: k
+// chunks, so k elements, reach it, and what is below it is dropped.  Little more than k chunks are
+// left; their elements that reach the floor, little more than k again, go to a list, and each counts
+// how many are larger: its place in the order.  Rows of no more chunks than alternatives deal out their
+// elements instead.  Should the list overflow all the same (a chunk full of larger elements than
+// others have), each of the k best chunks gives its k best elements in k rounds of a maximum.
 constexpr int kList = 1024;
-constexpr int kGroups = 64;   // of four threads
-static_assert(kGroups >= kMaxTop && kGroups * 4 == kThreads, "the k-th best group gives the floor");
+constexpr int kGroups = 64;
+constexpr int kGroupThreads = kThreads / kGroups;
+static_assert(kGroups > kMaxTop && kGroupThreads == 4, "every group has a chunk where there are more chunks than alternatives");
 static_assert(kMaxTop * kMaxTop <= kList, "k of each of k chunks");
 struct TopShared {
   uint64_t group_best[kGroups];
   uint64_t list[kList];
+  int32_t chunk[kList];
   uint64_t floor_key;
-  int32_t chosen[kMaxTop];
-  int n_list[2], n_chosen;
+  int n_chunks, n_list;
 };
 
 template <typename T>
@@ -277,99 +347,124 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
     }
     __syncthreads();
   }
-  // 1. the best chunks
+  const bool few = nchunks <= top;
+  const int n_dealt = few ? V : nchunks;
+  const auto dealt_key = [&](int c) { return key_of(order_of(few ? Elem<T>::to_float(row[c]) : cm[c]), c); };
+
+  // the floor
   uint64_t best = 0;
-  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
-    const uint64_t key = key_of(order_of(cm[c]), c);
+#pragma unroll 4
+  for (int c = (threadIdx.x >> 2) + kGroups * (threadIdx.x & 3); c < n_dealt; c += kThreads) {
+    const uint64_t key = dealt_key(c);
     best = key > best ? key : best;
   }
 #pragma unroll
-  for (int off = 1; off < 4; off <<= 1) {
+  for (int off = 1; off < kGroupThreads; off <<= 1) {
     const uint64_t other = __shfl_xor_sync(0xffffffffu, best, off);
     best = other > best ? other : best;
   }
   if ((threadIdx.x & 3) == 0) sh.group_best[threadIdx.x >> 2] = best;
-  if (threadIdx.x == 0) {
-    sh.n_list[0] = sh.n_list[1] = 0;
-    sh.n_chosen = min(top, nchunks);
-    sh.floor_key = 1;   // fewer groups than k: every chunk is a candidate
-  }
+  if (threadIdx.x == 0) sh.n_chunks = sh.n_list = 0;
   __syncthreads();
   if (threadIdx.x < kGroups) {
     const uint64_t mine = sh.group_best[threadIdx.x];
     int larger = 0;
+#pragma unroll 16
     for (int i = 0; i < kGroups; ++i) larger += sh.group_best[i] > mine;
-    if (mine && larger == top - 1) sh.floor_key = mine;
+    if (larger == top - 1) sh.floor_key = mine;   // (keys differ: one group is the k-th best)
   }
   __syncthreads();
-  const uint64_t chunk_floor = sh.floor_key;
-  for (int c = threadIdx.x; c < nchunks; c += kThreads) {
-    const uint64_t key = key_of(order_of(cm[c]), c);
-    if (key >= chunk_floor) {
-      const int at = atomicAdd(&sh.n_list[0], 1);
-      if (at < kList) sh.list[at] = key;
-    }
-  }
-  __syncthreads();
-  const int n0 = sh.n_list[0];
-  if (threadIdx.x == 0) sh.floor_key = 0;   // (every thread has read chunk_floor)
-  __syncthreads();
-  // sh.chosen chunks in any order; the floor for their elements is the k-th one's maximum
-  if (n0 <= kList) {
-    for (int i = threadIdx.x; i < n0; i += kThreads) {
-      const uint64_t mine = sh.list[i];
-      int larger = 0;
-      for (int q = 0; q < n0; ++q) larger += sh.list[q] > mine;
-      if (larger < top) sh.chosen[larger] = index_of(mine);
-      if (larger == top - 1) sh.floor_key = mine & 0xFFFFFFFF00000000ull;
-    }
-  } else if (warp == 0) {
-    warp_select(
-        top, 0,
-        [&](uint64_t limit) {
-          uint64_t b = 0;
-          for (int c = lane; c < nchunks; c += 32) {
-            const uint64_t key = key_of(order_of(cm[c]), c);
-            if (key < limit && key > b) b = key;
-          }
-          return b;
-        },
-        [&](int q, uint64_t key) {
-          sh.chosen[q] = index_of(key);
-          if (q == top - 1) sh.floor_key = key & 0xFFFFFFFF00000000ull;
-        });
-  }
-  __syncthreads();
+  const uint64_t floor_key = sh.floor_key;
+  const uint64_t elem_floor = few ? floor_key : floor_key & 0xFFFFFFFF00000000ull;   // at a chunk's floor any index will do
+  const auto list_element = [&](uint64_t key) {
+    const int at = atomicAdd(&sh.n_list, 1);
+    if (at < kList) sh.list[at] = key;
+  };
 
-  // 2. the elements of the sh.chosen chunks that reach the floor
-  const uint64_t elem_floor = sh.floor_key;
-  const int nc = sh.n_chosen;
-  for (int i = warp; i < nc; i += kWarps) {
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      const int j0 = sh.chosen[i] * kChunkElems + (q * 32 + lane) * VEC - shift;
-      const uint4 w = load_raw<T>(row, j0, V, minus_inf<T>());
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float v, other;
-        unpack2f(raw_pair<T>(w, e / 2), v, other);
-        const uint64_t key = key_of(order_of(e % 2 ? other : v), j0 + e);
-        if (key >= elem_floor && j0 + e >= 0 && j0 + e < V) {
-          const int at = atomicAdd(&sh.n_list[1], 1);
-          if (at < kList) sh.list[at] = key;
-        }
+  // what reaches it
+  for (int c = threadIdx.x; c < n_dealt; c += kThreads) {
+    const uint64_t key = dealt_key(c);
+    if (key >= floor_key) {
+      if (few) {
+        list_element(key);
+      } else {
+        const int at = atomicAdd(&sh.n_chunks, 1);
+        if (at < kList) sh.chunk[at] = c;
       }
     }
   }
   __syncthreads();
-  int n1 = sh.n_list[1];
-  if (n1 > kList) {
-    // too many ties: the first k of each sh.chosen chunk, by rounds
+  int nc = few ? 0 : sh.n_chunks;
+  const bool many_chunks = nc > kList;
+  const uint32_t floor_order = (uint32_t)(elem_floor >> 32);
+  for (int i = warp; i < (many_chunks ? 0 : nc); i += kWarps) {
+    const int j0 = sh.chunk[i] * kChunkElems + lane * VEC - shift;
+    uint32_t ord[Q][VEC];   // past the row: 0
+    int equal = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const uint4 w = load_raw<T>(row, j0 + q * 32 * VEC, V, minus_inf<T>());
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const int j = j0 + q * 32 * VEC + e;
+        float v, other;
+        unpack2f(raw_pair<T>(w, e / 2), v, other);
+        ord[q][e] = j >= 0 && j < V ? order_of(e % 2 ? other : v) : 0u;
+        equal += ord[q][e] == floor_order;
+      }
+    }
+    // of the elements that tie with the floor, the first k of the chunk will do
+    const bool tied = __reduce_add_sync(0xffffffffu, equal) > top;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      int before = 0;   // in this half of the chunk (Q == 2: k of each half)
+      if (tied) {
+        int mine = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mine += ord[q][e] == floor_order;
+        int scan = mine;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int up = __shfl_up_sync(0xffffffffu, scan, off);
+          if (lane >= off) scan += up;
+        }
+        before = scan - mine;
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const bool ties = ord[q][e] == floor_order;
+        if (ord[q][e] > floor_order || (ties && (!tied || before < top))) list_element(key_of(ord[q][e], j0 + q * 32 * VEC + e));
+        before += tied && ties;
+      }
+    }
+  }
+  __syncthreads();
+  int n = sh.n_list;
+  if (many_chunks || n > kList) {
+    // the k best chunks (all of them, where there are no more), then the k best of each
     __syncthreads();
-    if (threadIdx.x == 0) sh.n_list[1] = 0;
+    if (threadIdx.x == 0) sh.n_list = 0;
+    nc = min(top, nchunks);
+    if (warp == 0) {
+      if (few) {
+        if (lane < nchunks) sh.chunk[lane] = lane;
+      } else {
+        warp_select(
+            top, 0,
+            [&](uint64_t limit) {
+              uint64_t b = 0;
+              for (int c = lane; c < nchunks; c += 32) {
+                const uint64_t key = dealt_key(c);
+                if (key < limit && key > b) b = key;
+              }
+              return b;
+            },
+            [&](int q, uint64_t key) { sh.chunk[q] = index_of(key); });
+      }
+    }
     __syncthreads();
     for (int i = warp; i < nc; i += kWarps) {
-      const int j0 = sh.chosen[i] * kChunkElems + lane * VEC - shift;
+      const int j0 = sh.chunk[i] * kChunkElems + lane * VEC - shift;
       float v[Q][VEC];
 #pragma unroll
       for (int q = 0; q < Q; ++q) load_piece<T>(row, j0 + q * 32 * VEC, V, -INFINITY, v[q]);
@@ -387,17 +482,18 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
               }
             return b;
           },
-          [&](int, uint64_t key) { sh.list[atomicAdd(&sh.n_list[1], 1)] = key; });
+          [&](int, uint64_t key) { list_element(key); });
     }
     __syncthreads();
-    n1 = sh.n_list[1];
+    n = sh.n_list;
   }
   // each takes its place (the list's own order does not matter: keys differ)
   const float log_s = log_sum(st);
-  for (int i = threadIdx.x; i < n1; i += kThreads) {
+  for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t mine = sh.list[i];
     int larger = 0;
-    for (int q = 0; q < n1; ++q) larger += sh.list[q] > mine;
+#pragma unroll 4
+    for (int q = 0; q < n; ++q) larger += sh.list[q] > mine;
     if (larger < top) {
       top_ids[r * top + larger] = index_of(mine);
       top_logp[r * top + larger] = log_prob(value_of((uint32_t)(mine >> 32)), st, log_s);
