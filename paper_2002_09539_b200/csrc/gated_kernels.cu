@@ -50,7 +50,7 @@ struct GatedArgs {
   int rows, cols;             // extents of one problem's output (FORWARD: cols = F)
   int act, f16;
   int a_rows;                 // rows of A that are loaded (K-major): all 128 unless the problem has fewer
-  bool out_vec;               // the output's rows are whole 16-byte pieces
+  int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
   void* out0;                 // h, dx or dWg
   void* out1;                 // dWu
   float* pre;                 // FORWARD: a, b [m][T][2][Fp], or null
@@ -152,6 +152,16 @@ __device__ __forceinline__ void store_sector(float* p, const float* v) {
                : "memory");
 }
 
+__device__ __forceinline__ void store_word_if(uint16_t* p, uint32_t v, bool yes) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b32 [%0], %1;\n\t}" ::"l"(p), "r"(v), "r"((int)yes)
+               : "memory");
+}
+__device__ __forceinline__ void store_half_if(uint16_t* p, uint32_t v, bool yes) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q st.global.b16 [%0], %1;\n\t}" ::"l"(p), "h"((uint16_t)v),
+               "r"((int)yes)
+               : "memory");
+}
+
 // A warp's block of 32 rows x W columns of results on its way out: TMEM hands every lane a row,
 // memory wants whole lines.  16-byte pieces, swizzled so that neither side meets bank conflicts
 // (W = 64).
@@ -168,25 +178,45 @@ struct Staged {
     buf[at(lane, 2 * q)] = make_uint4(p[0], p[1], p[2], p[3]);
     buf[at(lane, 2 * q + 1)] = make_uint4(p[4], p[5], p[6], p[7]);
   }
-  // The block to rows [0, rows) of dst (row pitch ld elements), of whose columns `cols` exist.
-  // vec: dst and ld are multiples of 16 bytes, cols of 8 elements.
-  __device__ __forceinline__ void flush(int lane, uint16_t* dst, int64_t ld, int64_t rows, int64_t cols, bool vec) {
+  // The block to rows [0, rows) of dst (row pitch ld elements), of whose columns `cols` exist.  width:
+  // bytes that dst, ld and cols are multiples of (16, 8, 4 or 2).
+  __device__ __forceinline__ void flush(int lane, uint16_t* dst, int64_t ld, int64_t rows, int64_t cols, int width) {
     __syncwarp();
-    if (vec) {
+    const int n = rows < 32 ? (int)rows : 32, nc = cols < W ? (int)cols : W;
+    if (width == 16) {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
         const int k = i * 32 + lane, r = k / kPieces, c = k % kPieces;
         const uint4 v = buf[at(r, c)];
-        if (r < rows && c * 8 < cols) *reinterpret_cast<uint4*>(dst + r * ld + c * 8) = v;
+        if (r < n && c * 8 < nc) *reinterpret_cast<uint4*>(dst + r * ld + c * 8) = v;
+      }
+    } else if (width == 8) {
+      const uint2* half = reinterpret_cast<const uint2*>(buf);
+#pragma unroll
+      for (int i = 0; i < 2 * kPieces; ++i) {
+        const int k = i * 32 + lane, r = k / (2 * kPieces), c = k % (2 * kPieces);
+        const uint2 v = half[at(r, c >> 1) * 2 + (c & 1)];
+        if (r < n && c * 4 < nc) *reinterpret_cast<uint2*>(dst + r * ld + c * 4) = v;
       }
     } else {
-      const uint16_t* h = reinterpret_cast<const uint16_t*>(buf);
-      const int n = rows < 32 ? (int)rows : 32;
-#pragma unroll 4
-      for (int r = 0; r < n; ++r)
-#pragma unroll
-        for (int c = lane; c < W; c += 32)
-          if (c < cols) dst[r * ld + c] = h[at(r, c >> 3) * 8 + (c & 7)];
+      // Two columns a lane, one word of the block.  Rows of an odd pitch start between the words every
+      // other time: there a lane stores its second column with the next lane's first, and the block's
+      // first and last column go by themselves.
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(buf);
+      constexpr int kPairs = W / 2, kRows = 32 / kPairs;   // rows a step
+      const int pair = lane % kPairs;
+      int r = lane / kPairs;
+      uint16_t* row = dst + r * ld;
+#pragma unroll 8
+      for (int step = 0; step < 32 / kRows; ++step, r += kRows, row += kRows * ld) {
+        const uint32_t w = words[at(r, pair >> 2) * 4 + (pair & 3)], next = __shfl_down_sync(0xffffffffu, w, 1);
+        const int odd = (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 1, c = 2 * pair + odd;
+        const uint32_t v = odd ? __funnelshift_r(w, next, 16) : w;
+        // (predicated: a branch a store would cost more than the store)
+        store_word_if(row + c, v, r < n && c + 1 < nc);
+        store_half_if(row + c, v, r < n && c + 1 == nc);
+        store_half_if(row, w, r < n && odd && pair == 0);   // (a block has a column)
+      }
     }
     __syncwarp();
   }
@@ -417,7 +447,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
               }
               out.put(lane, q, h, g.f16);
             }
-            if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
+            if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_width);
           } else {
 #pragma unroll 1
             for (int q = 0; q < W / 16; q += 2) {
@@ -435,7 +465,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
               out.put(lane, q, v, g.f16);
               out.put(lane, q + 1, w, g.f16);
             }
-            if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_vec);
+            if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_width);
           }
         }
       }
@@ -606,12 +636,13 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const GatedArgs g) {
                      : g.act == OLSGD_ACT_RELU ? act_value<OLSGD_ACT_RELU>(a[e])
                                                : act_value<OLSGD_ACT_SIGMOID>(a[e]));
   }
-  store_floats<T, 8>(out, c, g.cols, g.out_vec, a);
+  store_floats<T, 8>(out, c, g.cols, g.out_width == 16, a);
 }
 
 // Rows of any pitch to rows of a pitch that TMA takes: up to three operands [m][rows][cols] of
-// 16-bit values, blockIdx.z counting them.  A thread makes one aligned 16-byte piece out of the
-// two that its elements lie in (`begin` and `end` bound the tensor: nothing outside it is read).
+// 16-bit values, blockIdx.z counting them; a warp per row.  A lane makes one aligned 16-byte piece out
+// of the two that its elements lie in (`begin` and `end` bound the tensor: nothing outside it is
+// read).
 struct PadOperand {
   const uint16_t *begin, *end;
   uint16_t* out;
@@ -621,41 +652,61 @@ struct PadOperands {
   PadOperand op[3];
   int64_t cols, pitch;
 };
+// Elements off .. off + 7 of the sixteen in a, b.
+__device__ __forceinline__ uint4 eight_from(const uint4& a, const uint4& b, int off) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (off & 4) {
+#pragma unroll
+    for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+  }
+  if (off & 2) {
+#pragma unroll
+    for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+  }
+  if (off & 1) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ PadOperands all) {
   launch_gate();
   const PadOperand& o = all.op[blockIdx.z];
-  const int64_t cols = all.cols;
-  // a warp per row
-  for (int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); r < o.rows; r += (int64_t)gridDim.x * 8)
-#pragma unroll 4
-  for (int64_t j = (threadIdx.x & 31) * 8; j < all.pitch; j += 256) {
-    const uint16_t* src = o.begin + (int64_t)blockIdx.y * o.in_worker + r * o.in_row + j;
-    const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
-    const uint16_t* base = src - off;
-    uint32_t w[8];
-    if (j + 8 <= cols && base >= o.begin && base + 16 <= o.end) {
-      const uint4 a = *reinterpret_cast<const uint4*>(base), b = *reinterpret_cast<const uint4*>(base + 8);
-      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-      if (off & 4) {
+  const int lane = threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (r >= o.rows) return;
+  const int cols = (int)all.cols, whole = cols / 8, pieces = (int)(all.pitch / 8);
+  const uint16_t* src = o.begin + (int64_t)blockIdx.y * o.in_worker + r * o.in_row;
+  uint4* dst = reinterpret_cast<uint4*>(o.out + ((int64_t)blockIdx.y * o.rows + r) * all.pitch);
+  const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
+  int first_slow = 0;   // pieces from here on are made element by element
+  if (src - off >= o.begin && src - off + whole * 8 + 8 <= o.end) {
+    // every whole piece of the row, and its neighbour, lie inside the tensor
+    first_slow = whole;
+    const uint4* base = reinterpret_cast<const uint4*>(src - off);
+    constexpr int U = 4;
+    for (int p0 = lane; p0 < whole; p0 += 32 * U) {
+      uint4 a[U], b[U];
 #pragma unroll
-        for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+      for (int u = 0; u < U; ++u) {
+        const int p = min(p0 + u * 32, whole - 1);
+        a[u] = base[p];
+        b[u] = base[p + 1];
       }
-      if (off & 2) {
 #pragma unroll
-        for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
-      }
-      if (off & 1) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = j + 2 * e < cols ? src[2 * e] : 0, hi = j + 2 * e + 1 < cols ? src[2 * e + 1] : 0;
-        w[e] = lo | (hi << 16);
-      }
+      for (int u = 0; u < U; ++u)
+        if (p0 + u * 32 < whole) dst[p0 + u * 32] = eight_from(a[u], b[u], off);
     }
-    *reinterpret_cast<uint4*>(o.out + ((int64_t)blockIdx.y * o.rows + r) * all.pitch + j) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  for (int p = first_slow + lane; p < pieces; p += 32) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = p * 8 + 2 * e;
+      const uint32_t lo = j < cols ? src[j] : 0, hi = j + 1 < cols ? src[j + 1] : 0;
+      w[e] = lo | (hi << 16);
+    }
+    dst[p] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -869,15 +920,17 @@ cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m,
     most_rows = rows > most_rows ? rows : most_rows;
   }
   if (n == 0) return cudaSuccess;
-  const int64_t want = (most_rows + 7) / 8, most = 1 << 20;
-  return launch_chained(pad_rows_kernel, dim3((unsigned)(want < most ? want : most), (unsigned)m, (unsigned)n), dim3(256), 0, s, all);
+  return launch_chained(pad_rows_kernel, dim3((unsigned)((most_rows + 7) / 8), (unsigned)m, (unsigned)n), dim3(256), 0, s, all);
 }
 
 // Rows of A worth loading: with fewer than 128 tokens the rest of the tile stays what it was (it
 // reaches only accumulator rows that are not stored).
 int loaded_rows(int64_t T) { return T >= kBM ? kBM : (int)round8(T); }
 
-bool whole_pieces(const void* p, int64_t cols) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && cols % 8 == 0; }
+int store_width(const void* p, int64_t cols) {
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (uintptr_t)(cols * 2);
+  return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 2;
+}
 
 template <typename T>
 cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, cudaStream_t s) {
@@ -948,7 +1001,7 @@ cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
   OLSGD_STEP(make_ready(wanted, 3, a.D, a.m, ws, s));
   const Shape sh = shape_for<FORWARD>(product_of(FORWARD, a));
   GatedArgs g = args_for<FORWARD>(a, sh, ws + at.parts);
-  g.out_vec = whole_pieces(a.h, a.F);
+  g.out_width = store_width(a.h, a.F);
   g.out0 = a.h;
   g.pre = a.pre;
   g.a_rows = loaded_rows(a.T);
@@ -974,7 +1027,7 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   if (a.dx) {
     const Shape sh = shape_for<DX>(product_of(DX, a));
     GatedArgs g = args_for<DX>(a, sh, ws + at.parts);
-    g.out_vec = whole_pieces(a.dx, a.D);
+    g.out_width = store_width(a.dx, a.D);
     g.out0 = a.dx;
     g.a_rows = loaded_rows(a.T);
     GatedMaps maps;
@@ -986,7 +1039,8 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   if (a.dwg) {
     const Shape sh = shape_for<DW>(product_of(DW, a));
     GatedArgs g = args_for<DW>(a, sh, ws + at.parts);
-    g.out_vec = whole_pieces(a.dwg, a.D) && whole_pieces(a.dwu, a.D);
+    const int w0 = store_width(a.dwg, a.D), w1 = store_width(a.dwu, a.D);
+    g.out_width = w0 < w1 ? w0 : w1;
     g.out0 = a.dwg;
     g.out1 = a.dwu;
     GatedMaps maps;

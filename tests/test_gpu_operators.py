@@ -385,7 +385,8 @@ def _check_gated(x, wg, wu, dh, kind):
 GATED_SHAPES = [(1, 1, 1, 1), (1, 1, 64, 32), (1, 2, 8, 8), (2, 5, 33, 47), (3, 3, 1001, 37), (2, 4, 2056, 40), (2, 4, 33, 47), (1, 128, 64, 128), (3, 130, 72, 136), (1, 300, 200, 520),
                 (2, 257, 1021, 515), (1, 1, 1024, 4096), (1, 17, 4096, 24), (16, 128, 256, 1024), (8, 300, 128, 1024), (8, 600, 1024, 1024),
                 (16, 100, 2048, 72), (16, 70, 1024, 100), (5, 401, 1000, 1303),
-                (1, 200, 304, 2048), (1, 40, 4096, 64), (1, 5000, 64, 48), (1, 41, 4001, 61), (2, 3000, 67, 45), (1, 512, 1024, 4096)]
+                (1, 200, 304, 2048), (1, 40, 4096, 64), (1, 5000, 64, 48), (1, 41, 4001, 61), (2, 3000, 67, 45), (1, 512, 1024, 4096),
+                (2, 140, 100, 2556), (2, 140, 2556, 98), (1, 35, 67, 129), (1, 35, 129, 67)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
