@@ -145,10 +145,16 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, int f16) {
   return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-__device__ __forceinline__ void store_sector(float* p, const float* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(__float_as_uint(v[0])),
-               "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
-               "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+// Predicated stores: in the epilogue a branch around a store costs more than the store.
+__device__ __forceinline__ void store_sector_if(float* p, const float* v, bool yes) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %9, 0;\n\t@q st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n\t}" ::"l"(p),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+               "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])), "r"((int)yes)
+               : "memory");
+}
+__device__ __forceinline__ void store_piece_if(void* p, const uint4& v, bool yes) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t@q st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}" ::"l"(p), "r"(v.x),
+               "r"(v.y), "r"(v.z), "r"(v.w), "r"((int)yes)
                : "memory");
 }
 
@@ -188,7 +194,7 @@ struct Staged {
       for (int i = 0; i < kPieces; ++i) {
         const int k = i * 32 + lane, r = k / kPieces, c = k % kPieces;
         const uint4 v = buf[at(r, c)];
-        if (r < n && c * 8 < nc) *reinterpret_cast<uint4*>(dst + r * ld + c * 8) = v;
+        store_piece_if(dst + r * ld + c * 8, v, r < n && c * 8 < nc);
       }
     } else if (width == 8) {
       const uint2* half = reinterpret_cast<const uint2*>(buf);
@@ -212,7 +218,6 @@ struct Staged {
         const uint32_t w = words[at(r, pair >> 2) * 4 + (pair & 3)], next = __shfl_down_sync(0xffffffffu, w, 1);
         const int odd = (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 1, c = 2 * pair + odd;
         const uint32_t v = odd ? __funnelshift_r(w, next, 16) : w;
-        // (predicated: a branch a store would cost more than the store)
         store_word_if(row + c, v, r < n && c + 1 < nc);
         store_half_if(row + c, v, r < n && c + 1 == nc);
         store_half_if(row, w, r < n && odd && pair == 0);   // (a block has a column)
@@ -428,15 +433,15 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
             for (int q = 0; q < W / 16; ++q) {
               float a[16], b[16], h[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + BN / 2 + c0 + q * 16, a, b);
-              if (pre && lane < rows) {
+              if (pre) {
                 // columns up to pre_pitch (a multiple of 8) exist; a lane writes whole sectors
                 float* p = pre + col + q * 16;
 #pragma unroll
-                for (int z = 0; z < 2; ++z)
-                  if (col + q * 16 + 8 * z < g.pre_pitch) {
-                    store_sector(p + 8 * z, a + 8 * z);
-                    store_sector(p + g.pre_pitch + 8 * z, b + 8 * z);
-                  }
+                for (int z = 0; z < 2; ++z) {
+                  const bool yes = lane < rows && col + q * 16 + 8 * z < g.pre_pitch;
+                  store_sector_if(p + 8 * z, a + 8 * z, yes);
+                  store_sector_if(p + g.pre_pitch + 8 * z, b + 8 * z, yes);
+                }
               }
               if (part) continue;
               switch (g.act) {
@@ -454,12 +459,10 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
               float v[16], w[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
               if (part) {
-                if (lane < rows) {
-                  float* p = part + col + q * 16;
+                float* p = part + col + q * 16;
 #pragma unroll
-                  for (int z = 0; z < 4; ++z)
-                    if (col + q * 16 + 8 * z < g.parts_row) store_sector(p + 8 * z, z < 2 ? v + 8 * z : w + 8 * z - 16);
-                }
+                for (int z = 0; z < 4; ++z)
+                  store_sector_if(p + 8 * z, z < 2 ? v + 8 * z : w + 8 * z - 16, lane < rows && col + q * 16 + 8 * z < g.parts_row);
                 continue;
               }
               out.put(lane, q, v, g.f16);
@@ -626,8 +629,8 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const GatedArgs g) {
   if (MODE == FORWARD) {
     if (g.pre) {
       float* pre = g.pre + (problem * g.rows + r) * 2 * g.pre_pitch + c;
-      store_sector(pre, a);
-      store_sector(pre + g.pre_pitch, b);
+      store_sector_if(pre, a, true);
+      store_sector_if(pre + g.pre_pitch, b, true);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
