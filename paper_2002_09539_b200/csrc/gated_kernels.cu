@@ -190,13 +190,22 @@ struct Staged {
     __syncwarp();
     const int n = rows < 32 ? (int)rows : 32, nc = cols < W ? (int)cols : W;
     if (width == 16) {
+      // (all reads ahead of the stores, which the compiler does not move them across)
+      uint4 v[kPieces];
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) v[i] = buf[at((i * 32 + lane) / kPieces, (i * 32 + lane) % kPieces)];
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
         const int k = i * 32 + lane, r = k / kPieces, c = k % kPieces;
-        const uint4 v = buf[at(r, c)];
-        store_piece_if(dst + r * ld + c * 8, v, r < n && c * 8 < nc);
+        store_piece_if(dst + r * ld + c * 8, v[i], r < n && c * 8 < nc);
       }
-    } else if (width == 8) {
+    } else {
+      flush_narrow(buf, lane, dst, ld, n, nc, width);
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ static void flush_narrow(const uint4* buf, int lane, uint16_t* dst, int64_t ld, int n, int nc, int width) {
+    if (width == 8) {
       const uint2* half = reinterpret_cast<const uint2*>(buf);
 #pragma unroll
       for (int i = 0; i < 2 * kPieces; ++i) {
@@ -213,19 +222,50 @@ struct Staged {
       const int pair = lane % kPairs;
       int r = lane / kPairs;
       uint16_t* row = dst + r * ld;
-#pragma unroll 8
-      for (int step = 0; step < 32 / kRows; ++step, r += kRows, row += kRows * ld) {
-        const uint32_t w = words[at(r, pair >> 2) * 4 + (pair & 3)], next = __shfl_down_sync(0xffffffffu, w, 1);
-        const int odd = (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 1, c = 2 * pair + odd;
-        const uint32_t v = odd ? __funnelshift_r(w, next, 16) : w;
-        store_word_if(row + c, v, r < n && c + 1 < nc);
-        store_half_if(row + c, v, r < n && c + 1 == nc);
-        store_half_if(row, w, r < n && odd && pair == 0);   // (a block has a column)
+      constexpr int U = 8;
+#pragma unroll 1
+      for (int step = 0; step < 32 / kRows; step += U) {
+        uint32_t w[U], next[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          w[u] = words[at(r + u * kRows, pair >> 2) * 4 + (pair & 3)];
+          next[u] = __shfl_down_sync(0xffffffffu, w[u], 1);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u, r += kRows, row += kRows * ld) {
+          const int odd = (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 1, c = 2 * pair + odd;
+          const uint32_t v = odd ? __funnelshift_r(w[u], next[u], 16) : w[u];
+          store_word_if(row + c, v, r < n && c + 1 < nc);
+          store_half_if(row + c, v, r < n && c + 1 == nc);
+          store_half_if(row, w[u], r < n && odd && pair == 0);   // (a block has a column)
+        }
       }
     }
-    __syncwarp();
   }
 };
+
+// The same for fp32 sums: 32 rows x COLS (16 or 32) columns, straight from tensor memory to rows of
+// dst (pitch ld, a multiple of 8) of which `cols` columns (a multiple of 8) exist.  Lanes that stored
+// their own rows would keep the store unit busy with one sector each.
+template <int COLS>
+__device__ __forceinline__ void spill_sums(uint4* buf, int lane, uint32_t acc, float* dst, int64_t ld, int64_t rows, int64_t cols) {
+  constexpr int kPieces = COLS / 4;
+  const auto at = [](int row, int piece) { return row * kPieces + (piece ^ (row & (kPieces - 1))); };
+  float v[32];
+  tmem_ld16x2(acc, COLS == 32 ? acc + 16 : acc, v, v + 16);
+#pragma unroll
+  for (int q = 0; q < kPieces; ++q) buf[at(lane, q)] = Elem<float>::pack(v + 4 * q);
+  __syncwarp();
+  uint4 w[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) w[i] = buf[at((i * 32 + lane) / kPieces, (i * 32 + lane) % kPieces)];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int k = i * 32 + lane, r = k / kPieces, c = k % kPieces;
+    store_piece_if(dst + r * ld + c * 4, w[i], r < rows && c * 4 < cols);
+  }
+  __syncwarp();
+}
 
 struct Tile {
   int problem, split, row, col;   // row and column tile
@@ -273,7 +313,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   constexpr uint32_t kStageBytes = kABytes + kBBytes;
   constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;  // output columns of a tile
   constexpr int kBlockCols = kColsOut / 2 < 64 ? kColsOut / 2 : 64;   // columns an epilogue warp stages at a time
-  constexpr uint32_t kStagingBytes = kEpiWarps * 32 * kBlockCols * 2;
+  constexpr uint32_t kStagingBytes = kEpiWarps * 4096;
   constexpr uint32_t kTmemCols = 2 * BN;
   static_assert(kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0, "two accumulators");
   static_assert(CTAS == 1 || BN == 256, "pairs take whole tiles");
@@ -407,7 +447,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
     // left half of the tile's 16-column blocks, warps 6-9 the right half
     const int lane_group = warp & 3, half = (warp - 2) >> 2;
     constexpr int W = kBlockCols;
-    Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * (32 * W / 8)};
+    Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * 256};
     uint32_t n = 0;
     for (uint32_t t = first; t < total; t += step, ++n) {
       const uint32_t buf = n & 1;
@@ -420,8 +460,8 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
       const uint32_t acc = tmem_base + buf * BN + ((uint32_t)(lane_group * 32) << 16);
       uint16_t* dst = static_cast<uint16_t*>(MODE == DW && (tl.problem & 1) ? g.out1 : g.out0) + (worker * g.rows + row0) * g.cols;
       // a part of K: sums in fp32 to this part's own place
-      float* part = g.splits > 1 ? g.parts + (((int64_t)tl.split * g.problems + tl.problem) * g.rows + row0 + lane) * g.parts_row : nullptr;
-      float* pre = !g.pre ? nullptr : g.pre + (worker * g.rows + row0 + lane) * 2 * g.pre_pitch;
+      float* part = g.splits > 1 ? g.parts + (((int64_t)tl.split * g.problems + tl.problem) * g.rows + row0) * g.parts_row : nullptr;
+      float* pre = !g.pre ? nullptr : g.pre + (worker * g.rows + row0) * g.parts_row;   // (rows of a and b, as in parts)
       if (MODE == FORWARD && part) pre = part;
       if (rows > 0) {
         for (int c0 = half * (kColsOut / 2); c0 < (half + 1) * (kColsOut / 2); c0 += W) {
@@ -429,21 +469,20 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
           const int64_t cols = g.cols - col;
           if (cols <= 0) break;
           if (MODE == FORWARD) {
+            if (pre) {
+              // (columns up to pre_pitch exist)
+              constexpr int kCols = W < 32 ? W : 32;
 #pragma unroll 1
-            for (int q = 0; q < W / 16; ++q) {
+              for (int q = 0; q < 2 * (W / kCols); ++q) {
+                const int c = q / 2 * kCols, z = q & 1;   // a, then b
+                spill_sums<kCols>(out.buf, lane, acc + z * (BN / 2) + c0 + c, pre + z * g.pre_pitch + col + c, g.parts_row, rows,
+                                  g.pre_pitch - col - c);
+              }
+            }
+#pragma unroll 1
+            for (int q = 0; q < (part ? 0 : W / 16); ++q) {
               float a[16], b[16], h[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + BN / 2 + c0 + q * 16, a, b);
-              if (pre) {
-                // columns up to pre_pitch (a multiple of 8) exist; a lane writes whole sectors
-                float* p = pre + col + q * 16;
-#pragma unroll
-                for (int z = 0; z < 2; ++z) {
-                  const bool yes = lane < rows && col + q * 16 + 8 * z < g.pre_pitch;
-                  store_sector_if(p + 8 * z, a + 8 * z, yes);
-                  store_sector_if(p + g.pre_pitch + 8 * z, b + 8 * z, yes);
-                }
-              }
-              if (part) continue;
               switch (g.act) {
                 case OLSGD_ACT_SILU: activate16<OLSGD_ACT_SILU>(a, b, h); break;
                 case OLSGD_ACT_GELU: activate16<OLSGD_ACT_GELU>(a, b, h); break;
@@ -454,17 +493,15 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
             }
             if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_width);
           } else {
+            if (part) {
 #pragma unroll 1
-            for (int q = 0; q < W / 16; q += 2) {
+              for (int c = 0; c < W; c += 32)
+                spill_sums<32>(out.buf, lane, acc + c0 + c, part + col + c, g.parts_row, rows, g.parts_row - col - c);
+            }
+#pragma unroll 1
+            for (int q = 0; q < (part ? 0 : W / 16); q += 2) {
               float v[16], w[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
-              if (part) {
-                float* p = part + col + q * 16;
-#pragma unroll
-                for (int z = 0; z < 4; ++z)
-                  store_sector_if(p + 8 * z, z < 2 ? v + 8 * z : w + 8 * z - 16, lane < rows && col + q * 16 + 8 * z < g.parts_row);
-                continue;
-              }
               out.put(lane, q, v, g.f16);
               out.put(lane, q + 1, w, g.f16);
             }
@@ -778,7 +815,7 @@ template <int MODE, int CTAS, int BN, int STAGES>
 cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
   constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;
   constexpr size_t smem = (size_t)STAGES * (kBM * kBK * 2 + BN / CTAS * kBK * 2) +
-                          kEpiWarps * 32 * (kColsOut / 2 < 64 ? kColsOut / 2 : 64) * 2 + sizeof(Control<STAGES>) + 1024;
+                          kEpiWarps * 4096 + sizeof(Control<STAGES>) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   static PerDeviceSmem configured;
   auto kern = gated_gemm_kernel<MODE, CTAS, BN, STAGES>;
