@@ -83,12 +83,32 @@ struct ZeroArgs {
   int64_t V, row_bytes, worker_bytes;
   int rows, ctas;            // rows of a CTA, CTAs of a worker
 };
-// Rows [v0, v0 + n) of a worker that are not present.  Zeros are the same in every type: the rows are
-// walked as one run of bytes, 32 a thread, which are stored whole where no present row shares them
-// and by twos where one does (or where the run ends).
+// Rows [v0, v0 + n) of a worker that are not present.  Zeros are the same in every type.  Long rows: a
+// warp each, 32 bytes a lane between the boundaries, 2 at the ends.  Short ones are walked as one run
+// of bytes, 32 a thread, which are stored whole where no present row shares them and by twos where
+// one does (or where the run ends): a 4096-byte row costs that way 10 % more, one of 48 bytes a
+// third.
+constexpr uint32_t kLongRow = 1024;
+__device__ __forceinline__ void store_zeros(char* p) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(p), "r"(0u) : "memory");
+}
 __device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t worker, int64_t v0, int n, const uint8_t* present) {
   char* run = static_cast<char*>(z.dtable) + worker * z.worker_bytes + v0 * z.row_bytes;
-  const uint32_t row = (uint32_t)z.row_bytes, bytes = row * n, shift = (uint32_t)(reinterpret_cast<uintptr_t>(run) & 31);
+  const uint32_t row = (uint32_t)z.row_bytes;
+  if (row >= kLongRow) {
+    const int lane = threadIdx.x & 31;
+    for (int r = threadIdx.x >> 5; r < n; r += blockDim.x >> 5) {
+      if (present[r]) continue;
+      char *p = run + (int64_t)r * row, *end = p + row;
+      char* body = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(p) + 31) & ~(uintptr_t)31);
+      char* tail = body + ((end - body) & ~(int64_t)31);
+      for (char* q = p + lane * 2; q < body; q += 64) *reinterpret_cast<uint16_t*>(q) = 0;
+      for (char* q = body + lane * 32; q < tail; q += 1024) store_zeros(q);
+      for (char* q = tail + lane * 2; q < end; q += 64) *reinterpret_cast<uint16_t*>(q) = 0;
+    }
+    return;
+  }
+  const uint32_t bytes = row * n, shift = (uint32_t)(reinterpret_cast<uintptr_t>(run) & 31);
   for (uint32_t at = threadIdx.x * 32; at < bytes + shift; at += blockDim.x * 32) {
     // bytes [lo, hi) of the run
     const uint32_t lo = at < shift ? 0 : at - shift, hi = min(bytes, at + 32 - shift);
@@ -100,9 +120,9 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t worker, int
     }
     if (all) continue;
     if (!any && hi - lo == 32) {
-      asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(run + lo), "r"(0u) : "memory");
+      store_zeros(run + lo);
     } else {
-      uint32_t r = r0, next = (r0 + 1) * row;   // (no row reaches past 2^30 bytes)
+      uint32_t r = r0, next = (r0 + 1) * row;
       for (uint32_t b = lo; b < hi; b += 2) {
         if (b >= next) {
           ++r;
@@ -421,7 +441,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
   __syncthreads();
   const TI* dout = static_cast<const TI*>(a.dout) + worker * a.dout_worker;
   float* part = a.part + (worker * a.chunks + blockIdx.x) * 2 * a.pitch;
-  constexpr int U = 4;
+  constexpr int U = 8;
   float acc[kCols];
 #pragma unroll
   for (int e = 0; e < kCols; ++e) acc[e] = 0.f;
@@ -430,21 +450,18 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(const SumArg
     float v[U][kCols];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint64_t en = entry[1 + min(k0 + u, n - 1)];
-      const bool live = k0 + u < n && (uint32_t)(en >> 32) < a.V;
-      const TI* row = dout + (int64_t)(uint32_t)en * a.dout_row;
+      // Every load is made, of a row and columns that exist (no branches between them); what does not
+      // count is not stored.
+      const TI* row = dout + (int64_t)(uint32_t)entry[1 + min(k0 + u, n - 1)] * a.dout_row;
       if (VEC) {
 #pragma unroll
-        for (int q = 0; q < kCols / Elem<TI>::kVec; ++q) {
-          const int64_t c = c0 + q * Elem<TI>::kVec;
-          const uint4 w = live && c < a.D ? ld16_stream(row + c) : make_uint4(0, 0, 0, 0);
-          Elem<TI>::unpack(w, v[u] + q * Elem<TI>::kVec);
-        }
+        for (int q = 0; q < kCols / Elem<TI>::kVec; ++q)
+          Elem<TI>::unpack(ld16_stream(row + (c0 < a.D ? c0 : 0) + q * Elem<TI>::kVec), v[u] + q * Elem<TI>::kVec);
       } else {
 #pragma unroll
         for (int e = 0; e < kCols; ++e) {
           const int64_t c = c0 + e * kSumThreads;
-          v[u][e] = live && c < a.D ? Elem<TI>::to_float(row[c]) : 0.f;
+          v[u][e] = Elem<TI>::to_float(row[c < a.D ? c : 0]);
         }
       }
     }
@@ -635,7 +652,7 @@ cudaError_t launch_embedding_backward(const EmbeddingGradArgs& g, cudaStream_t s
   ZeroArgs zero{g.dtable, g.V, g.D * out_size, g.dtable_worker * out_size, 0, 0};
   int64_t share = g.m * g.V * zero.row_bytes / (148 * 4);
   share = share < kZeroBytesMin ? kZeroBytesMin : share > kZeroBytesMax ? kZeroBytesMax : share;
-  zero.rows = (int)(share / zero.row_bytes < kZeroRowsMax ? share / zero.row_bytes : kZeroRowsMax);   // (sixteen of the longest rows are 2^30 bytes: 32 bits count them)
+  zero.rows = (int)(share / zero.row_bytes < kZeroRowsMax ? share / zero.row_bytes : kZeroRowsMax);
   if (zero.rows < 16) zero.rows = 16;
   zero.ctas = (int)((g.V + zero.rows - 1) / zero.rows);
   int passes = 0;
