@@ -34,6 +34,10 @@ constexpr int kWarpList = 160;        // candidates that a warp lists
 constexpr int kMaxTop = OLSGD_MAX_TOP;
 static_assert(kMaxTop == 32, "a lane holds one candidate of each warp");
 constexpr int kMaxSplit = 64;
+// Unsplit rows that are this short, or whose alternatives are wanted, get CTAs of half the threads:
+// twice as many rows are on their way while others begin and end (3684 x 10549 bf16: 18.7 us against
+// 26.5, with five alternatives 34 against 46; 4096 x 32768 without: 3 % slower, hence the bound).
+constexpr int kNarrowRow = 16384;
 // The last rows that the forward kernel reads (this many bytes of them) are loaded at normal priority
 // and stay in L2; the gradient, which usually follows, starts from them.
 constexpr int64_t kKeepBytes = 64LL << 20;
@@ -319,8 +323,7 @@ __host__ __device__ constexpr uint32_t minus_inf() {
 // others have), each of the k best chunks gives its k best elements in k rounds of a maximum.
 constexpr int kList = 1024;
 constexpr int kGroups = 64;
-constexpr int kGroupThreads = kThreads / kGroups;
-static_assert(kGroups > kMaxTop && kGroupThreads == 4, "every group has a chunk where there are more chunks than alternatives");
+static_assert(kGroups > kMaxTop, "k groups have a chunk where there are more chunks than k");
 static_assert(kMaxTop * kMaxTop <= kList, "k of each of k chunks");
 struct TopShared {
   uint64_t group_best[kGroups];
@@ -330,11 +333,12 @@ struct TopShared {
   int n_chunks, n_list;
 };
 
-template <typename T>
+template <typename T, int NT>
 __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r, int V, int nchunks, float* cm, const RowState& st,
                                          int top, float* top_logp, int32_t* top_ids) {
   constexpr int VEC = Elem<T>::kVec;
   constexpr int Q = kChunkElems / 32 / VEC;
+  constexpr int kWarps = NT / 32, kGroupThreads = NT / kGroups;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int shift = row_shift(row);
   if (st.s != st.s) {
@@ -354,7 +358,7 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
   // the floor
   uint64_t best = 0;
 #pragma unroll 4
-  for (int c = (threadIdx.x >> 2) + kGroups * (threadIdx.x & 3); c < n_dealt; c += kThreads) {
+  for (int c = threadIdx.x / kGroupThreads + kGroups * (threadIdx.x % kGroupThreads); c < n_dealt; c += NT) {
     const uint64_t key = dealt_key(c);
     best = key > best ? key : best;
   }
@@ -363,7 +367,7 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
     const uint64_t other = __shfl_xor_sync(0xffffffffu, best, off);
     best = other > best ? other : best;
   }
-  if ((threadIdx.x & 3) == 0) sh.group_best[threadIdx.x >> 2] = best;
+  if (threadIdx.x % kGroupThreads == 0) sh.group_best[threadIdx.x / kGroupThreads] = best;
   if (threadIdx.x == 0) sh.n_chunks = sh.n_list = 0;
   __syncthreads();
   if (threadIdx.x < kGroups) {
@@ -382,7 +386,7 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
   };
 
   // what reaches it
-  for (int c = threadIdx.x; c < n_dealt; c += kThreads) {
+  for (int c = threadIdx.x; c < n_dealt; c += NT) {
     const uint64_t key = dealt_key(c);
     if (key >= floor_key) {
       if (few) {
@@ -489,7 +493,7 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
   }
   // each takes its place (the list's own order does not matter: keys differ)
   const float log_s = log_sum(st);
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  for (int i = threadIdx.x; i < n; i += NT) {
     const uint64_t mine = sh.list[i];
     int larger = 0;
 #pragma unroll 4
@@ -505,8 +509,9 @@ __device__ __forceinline__ void find_top(TopShared& sh, const T* row, int64_t r,
 // Per element the loop spends about six instructions (packed fp32 for the difference, the product
 // and both sums; the maximum in the element's own type).  An unsplit row is finished here: while
 // one CTA looks for its alternatives the others of the multiprocessor go on reading.
-template <typename T, bool TOP, bool WHOLE>
-__global__ void __launch_bounds__(kThreads)
+// NT: threads of the CTA.
+template <typename T, bool TOP, bool WHOLE, int NT>
+__global__ void __launch_bounds__(NT)
 logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int cps, RowOut o,
                    float4* __restrict__ part, float* chunk_max, int top, float* __restrict__ top_logp,
                    int32_t* __restrict__ top_ids) {
@@ -514,6 +519,7 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
   constexpr int Q = kChunkElems / 32 / VEC;   // pieces of a chunk per lane
   constexpr int U = 4;                  // chunks per turn: four 16-byte loads a lane, eight of fp32 (1021 x 50021
                                         // fp32: 39 us against 43 with four; 4096 x 32768 bf16 loses 3 % with eight)
+  constexpr int kWarps = NT / 32;
   launch_gate();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t r = blockIdx.x;
@@ -597,7 +603,7 @@ logprob_row_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, int 
   if constexpr (TOP && WHOLE) {
     __shared__ TopShared ts;
     __syncthreads();   // (the chunks' maxima too)
-    find_top<T>(ts, row, r, V, nchunks, chunk_max + r * nchunks, whole, top, top_logp, top_ids);
+    find_top<T, NT>(ts, row, r, V, nchunks, chunk_max + r * nchunks, whole, top, top_logp, top_ids);
   }
 }
 
@@ -628,7 +634,7 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
   }
   if (top == 0) return;
   __syncthreads();
-  find_top<T>(sh, row, r, V, nchunks, chunk_max + r * nchunks, whole, top, top_logp, top_ids);
+  find_top<T, kThreads>(sh, row, r, V, nchunks, chunk_max + r * nchunks, whole, top, top_logp, top_ids);
 }
 
 // ---------------------------------------------------------------------------- gradient
@@ -760,10 +766,12 @@ cudaError_t forward(const LogprobArgs& a, cudaStream_t s) {
   float* cmax = reinterpret_cast<float*>(part + a.rows * nsplit);
   const dim3 grid((unsigned)a.rows, (unsigned)nsplit);
   const bool whole = nsplit == 1;
-  auto k = a.top > 0 ? (whole ? logprob_row_kernel<T, true, true> : logprob_row_kernel<T, true, false>)
-                     : (whole ? logprob_row_kernel<T, false, true> : logprob_row_kernel<T, false, false>);
-  const cudaError_t e = launch_chained(k, grid, dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks, cps, o, part, cmax,
-                                       a.top, a.top_logp, a.top_ids);
+  const bool narrow = whole && (a.top > 0 || a.V <= kNarrowRow);
+  auto k = narrow ? (a.top > 0 ? logprob_row_kernel<T, true, true, kThreads / 2> : logprob_row_kernel<T, false, true, kThreads / 2>)
+           : whole ? logprob_row_kernel<T, false, true, kThreads>
+                   : (a.top > 0 ? logprob_row_kernel<T, true, false, kThreads> : logprob_row_kernel<T, false, false, kThreads>);
+  const cudaError_t e = launch_chained(k, grid, dim3(narrow ? kThreads / 2 : kThreads), 0, s, x, (int)a.V, a.ld, nchunks, cps,
+                                       o, part, cmax, a.top, a.top_logp, a.top_ids);
   if (e != cudaSuccess || whole) return e;
   return launch_chained(logprob_finish_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, x, (int)a.V, a.ld, nchunks,
                         nsplit, o, (const float4*)part, cmax, a.top, a.top_logp, a.top_ids);
