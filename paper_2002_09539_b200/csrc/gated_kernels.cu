@@ -92,8 +92,8 @@ __device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t tb, float* a, 
 }
 
 // ------------------------------------------------------------------------- activations
-// tanh(z) = 1 - 2 / (1 + e^{2z}): exact limits at both ends, no cancellation that matters to
-// a result of 16 bits.
+// By one exponential and one division: sigmoid(a) = 1 / (1 + e^-a), and 0.5 (1 + tanh z) =
+// sigmoid(2 z) for gelu.  Limits are exact at both ends.
 struct ActPair {
   float f, df;   // act(a), act'(a)
 };
@@ -106,7 +106,6 @@ template <int ACT>
 __device__ __forceinline__ float act_value(float a) {
   if (ACT == OLSGD_ACT_RELU) return a > 0.f ? a : (a != a ? a : 0.f);
   if (ACT == OLSGD_ACT_SIGMOID) return sigmoid_of(a);
-  // gelu: 0.5 a (1 + tanh z) = a sigmoid(2 z)
   const float s = ACT == OLSGD_ACT_SILU ? sigmoid_of(a) : sigmoid_of(2.f * kGeluK * a * fmaf(kGeluC * a, a, 1.f));
   // a = -inf (an overflowed product) meets s = 0: the limit is 0
   return s == 0.f ? 0.f : a * s;

@@ -10,6 +10,7 @@ between them but what the caller passes on.
 """
 import ctypes as C
 import functools
+import operator
 from collections import namedtuple
 
 import torch
@@ -147,8 +148,9 @@ def token_logprobs(logits, targets, top=0):
     xp, code, N, V, ld = _rows_of(logits, "logits")
     dev, lead = logits.device, logits.shape[:-1]
     tp = _per_row(targets, lead, torch.int32, dev, "targets")
-    if top < 0 or top > MAX_TOP or top > V or top != int(top):
-        _refuse("top must be a whole number in [0, min(V, %d)]", MAX_TOP)
+    top = operator.index(top)
+    if top < 0 or top > MAX_TOP or top > V:
+        _refuse("top must be in [0, min(V, %d)]", MAX_TOP)
     # the float outputs share one allocation: allocating is most of what the host does here
     out = targets.new_empty(N * (4 + top), dtype=torch.float32)
     p = out.data_ptr()
