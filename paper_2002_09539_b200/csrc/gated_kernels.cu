@@ -750,13 +750,47 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ P
 }
 
 constexpr int kStretch = 512;
+
+// x . w over D in 64 bits, by a warp (every lane gets it).  Products of 16-bit values are exact in fp32.
+template <typename T>
+__device__ __forceinline__ double warp_dot(const T* x, const T* w, int64_t D, bool vec) {
+  const int lane = threadIdx.x & 31;
+  double s = 0.0;
+  if (vec) {
+#pragma unroll 2
+    for (int64_t k = lane * 8; k < D; k += 256) {
+      float vx[8], vw[8];
+      Elem<T>::unpack(ld16(x + k), vx);
+      Elem<T>::unpack(ld16(w + k), vw);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += (double)(vx[e] * vw[e]);
+    }
+  } else {
+#pragma unroll 4
+    for (int64_t k = lane; k < D; k += 32) s += (double)(Elem<T>::to_float(x[k]) * Elem<T>::to_float(w[k]));
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+
 // da = dh b act'(a), db = dh act(a); a, b, da, db have rows of `pitch`.
+//
+// relu's derivative jumps at 0, and an accumulation in fp32 is off by about 1e-6 of the values around
+// it: where a lies within 8e-6 of their mean size, its side of the border is not to be trusted, and
+// a is formed again in 64 bits (some ten of a million, a microsecond each, by a warp at a time).
+struct Border {
+  GatedOperand x, wg;
+  int64_t D;
+  bool vec;
+};
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const float* __restrict__ pre,
-                      T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec) {
+                      T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec, const Border border) {
   launch_gate();
   const T* dh_w = dh + (int64_t)blockIdx.y * dh_worker;
+  const int lane = threadIdx.x & 31;
   // a warp per stretch of kStretch columns of a row
   const int64_t stretches = (pitch + kStretch - 1) / kStretch;
   const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -765,20 +799,33 @@ gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_ro
   const int64_t wr = (int64_t)blockIdx.y * rows + r;
 #pragma unroll
   for (int q = 0; q < kStretch / 256; ++q) {
-    const int64_t j = j_begin + q * 256 + (threadIdx.x & 31) * 8;
-    if (j >= pitch) break;
+    const int64_t j0 = j_begin + q * 256, j = j0 + lane * 8;
+    if (j0 >= pitch) break;
+    const bool live = j < pitch;
     float a[8], b[8], d[8], va[8], vb[8];
 #pragma unroll
     for (int k = 0; k < 8; k += 4) {
-      Elem<float>::unpack(ld16_stream(pre + wr * 2 * pitch + j + k), a + k);
-      Elem<float>::unpack(ld16_stream(pre + wr * 2 * pitch + pitch + j + k), b + k);
+      const int64_t from = wr * 2 * pitch + (live ? j : 0) + k;
+      Elem<float>::unpack(ld16_stream(pre + from), a + k);
+      Elem<float>::unpack(ld16_stream(pre + pitch + from), b + k);
     }
     const T* src = dh_w + r * dh_row + j;
     if (vec) {
-      Elem<T>::unpack(ld16_stream(src), d);
+      Elem<T>::unpack(live ? ld16_stream(src) : make_uint4(0, 0, 0, 0), d);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] = j + e < F ? Elem<T>::to_float(src[e]) : 0.f;
+    }
+    uint32_t border_mask = 0;
+    if constexpr (ACT == OLSGD_ACT_RELU) {
+      float size = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) size += j + e < F ? fabsf(a[e]) : 0.f;
+      size = warp_sum(size);
+      const int64_t n = F - j0 < 256 ? F - j0 : 256;
+      const float near = size < 1e38f ? size / (float)n * 7.62939453125e-6f : 0.f;   // 2^-17; not beside infinities and NaN
+#pragma unroll
+      for (int e = 0; e < 8; ++e) border_mask |= (j + e < F && fabsf(a[e]) < near ? 1u : 0u) << e;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -786,8 +833,28 @@ gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_ro
       va[e] = d[e] * b[e] * p.df;
       vb[e] = d[e] * p.f;
     }
-    *reinterpret_cast<uint4*>(da + wr * pitch + j) = Elem<T>::pack(va);
-    *reinterpret_cast<uint4*>(db + wr * pitch + j) = Elem<T>::pack(vb);
+    if (live) {
+      *reinterpret_cast<uint4*>(da + wr * pitch + j) = Elem<T>::pack(va);
+      *reinterpret_cast<uint4*>(db + wr * pitch + j) = Elem<T>::pack(vb);
+    }
+    if constexpr (ACT == OLSGD_ACT_RELU) {
+      // those next to the border once more, after what their lane has stored
+      for (uint32_t lanes = __ballot_sync(0xffffffffu, border_mask != 0); lanes; lanes &= lanes - 1) {
+        const int from = __ffs(lanes) - 1;
+        for (uint32_t bits = __shfl_sync(0xffffffffu, border_mask, from); bits; bits &= bits - 1) {
+          const int64_t col = j0 + from * 8 + __ffs(bits) - 1;
+          const T* x = static_cast<const T*>(border.x.p) + (int64_t)blockIdx.y * border.x.worker_stride + r * border.x.row_stride;
+          const T* w = static_cast<const T*>(border.wg.p) + (int64_t)blockIdx.y * border.wg.worker_stride + col * border.wg.row_stride;
+          const float exact = (float)warp_dot(x, w, border.D, border.vec);
+          if (lane == from) {
+            const ActPair p = act_pair<ACT>(exact);
+            const float dv = Elem<T>::to_float(dh_w[r * dh_row + col]);
+            da[wr * pitch + col] = Elem<T>::from_float(dv * pre[wr * 2 * pitch + pitch + col] * p.df);
+            db[wr * pitch + col] = Elem<T>::from_float(dv * p.f);
+          }
+        }
+      }
+    }
   }
 }
 
@@ -981,7 +1048,8 @@ cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* d
            : a.act == OLSGD_ACT_RELU ? gated_backward_kernel<T, OLSGD_ACT_RELU>
                                      : gated_backward_kernel<T, OLSGD_ACT_SIGMOID>;
   return launch_chained(k, grid, dim3(256), 0, s, static_cast<const T*>(a.dh.p), a.dh.worker_stride, a.dh.row_stride,
-                        a.pre, static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec);
+                        a.pre, static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec,
+                        Border{a.x, a.wg, a.D, a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m)});
 }
 
 template <typename T>

@@ -659,3 +659,34 @@ def test_clip_grads_past_32_bit_offsets_and_of_many_workers():
     grads = [_randn(g, (700, 37)), _randn(g, (700, 1), torch.float16)]
     out, norms = lib.clip_grads(grads, 3.0)
     _check_clip(grads, 3.0, out, norms)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("D", [64, 63])
+@pytest.mark.parametrize("parts", ["all", "d_x alone"])
+def test_gated_relu_border_is_found_in_64_bits(D, dtype, parts):
+    """Pre-activations that fp32 rounds to nothing, of both signs: terms of 2^10, -2^10 and a last one of +-2^-18."""
+    g = _gen(D)
+    T, F = 4, 40
+    x, wg, wu = _randn(g, (1, T, D), dtype), _randn(g, (1, F, D), dtype), _randn(g, (1, F, D), dtype)
+    dh = _randn(g, (1, T, F), dtype)
+    x[0, 2] = 0.0
+    x[0, 2, 0] = x[0, 2, 1] = 32.0
+    x[0, 2, 2] = 2.0 ** -9
+    x[0, 2, 3:] = 0.0
+    wg[0, :, 2] = 1.0
+    for f, sign in ((3, 1.0), (17, -1.0), (39, 1.0)):
+        wg[0, f, 0], wg[0, f, 1], wg[0, f, 2] = 32.0, -32.0, sign * 2.0 ** -9
+    a = x.double() @ wg.double().mT
+    assert float(a[0, 2, 3]) == 2.0 ** -18 and float(a[0, 2, 17]) == -2.0 ** -18
+    _, pre = lib.gated_forward(x, wg, wu, "relu", save=True)
+    db, da = dh.double() * a.clamp(min=0), dh.double() * (x.double() @ wu.double().mT) * (a > 0)
+    dx, dwg, _ = lib.gated_backward(dh, x, wg, wu, pre, "relu", want_d_w=parts == "all")
+    want = (da @ wg.double() + db @ wu.double())[0, 2]
+    size = (da.abs() @ wg.double().abs() + db.abs() @ wu.double().abs())[0, 2]
+    assert bool(((dx[0, 2].double() - want).abs() <= size * (2 * torch.finfo(dtype).eps + _product_error(2 * F))).all())
+    if dwg is not None:
+        want = (da.mT @ x.double())[0]
+        size = (da.abs().mT @ x.double().abs())[0]
+        for f in (3, 17, 39):
+            assert bool(((dwg[0, f].double() - want[f]).abs() <= size[f] * (2 * torch.finfo(dtype).eps + _product_error(T))).all())
