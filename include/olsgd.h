@@ -416,7 +416,8 @@ typedef enum { OLSGD_F32 = 0, OLSGD_BF16 = 1, OLSGD_F16 = 2 } olsgd_dtype;
  * Logits of -inf are tokens that are masked out.  A row of nothing but -inf has no
  * distribution: logp of a token and top_logp are -inf, the entropy is 0, the gradient is 0.
  * A row with a NaN or +inf has logp (of a token), entropy and gradients of NaN; its
- * alternatives are ordered with NaN first.
+ * alternatives are ordered with NaN first.  A row whose d_logp (or token) and d_entropy are
+ * both 0 has a gradient of 0 whatever it holds: rows of padding need no clearing.
  *   logits   [rows][V], rows row_stride >= V elements apart; V in [1, 2^27]
  *   targets  int32 [rows]                                                               */
 #define OLSGD_MAX_TOP 32

@@ -644,7 +644,6 @@ logprob_finish_kernel(const T* __restrict__ x, int V, int64_t ld, int nchunks, i
 struct GradRow {
   float base, minus_log2_s, d_h, k, d_lp;
   int32_t target;
-  bool empty;
   __device__ __forceinline__ float operator()(float x) const {
     const float y = fmaxf(x - base, kFarBelow);
     return -ex2(fmaf(y, kLog2e, minus_log2_s)) * fmaf(d_h, y, k);
@@ -661,16 +660,20 @@ struct GradRow {
 __device__ __forceinline__ GradRow grad_row(const LogprobGradArgs& a, int64_t r) {
   GradRow g;
   const float m = a.stats[2 * r], log_s = a.stats[2 * r + 1];
-  g.empty = m == -INFINITY && log_s == 0.f;
-  g.base = base_of(m);
-  g.minus_log2_s = -log_s * kLog2e;
   const int32_t t = a.targets[r];
   const bool has = t >= 0 && t < a.V;
   g.target = has ? t : -1;
   g.d_lp = has && a.d_logp ? a.d_logp[r] : 0.f;
   g.d_h = a.d_entropy ? a.d_entropy[r] : 0.f;
+  g.base = base_of(m);
+  g.minus_log2_s = -log_s * kLog2e;
   g.k = fmaf(g.d_h, a.entropy[r] - log_s, g.d_lp);
-  if (g.empty) g.d_h = g.k = g.d_lp = 0.f;   // p times zero
+  // A row that nothing is asked of, or without a distribution: p = 0 for every x, NaN and
+  // infinities included (padding may hold anything).
+  if ((g.d_lp == 0.f && g.d_h == 0.f) || (m == -INFINITY && log_s == 0.f)) {
+    g.base = INFINITY;
+    g.minus_log2_s = g.d_h = g.k = g.d_lp = 0.f;
+  }
   return g;
 }
 

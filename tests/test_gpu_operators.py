@@ -690,3 +690,23 @@ def test_gated_relu_border_is_found_in_64_bits(D, dtype, parts):
         size = (da.abs().mT @ x.double().abs())[0]
         for f in (3, 17, 39):
             assert bool(((dwg[0, f].double() - want[f]).abs() <= size[f] * (2 * torch.finfo(dtype).eps + _product_error(T))).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [70, 3000])
+def test_token_logprobs_gradient_of_padding_is_zero_whatever_it_holds(V, dtype):
+    g = _gen(V)
+    x = _randn(g, (6, V), dtype)
+    x[1, 3], x[2, 5], x[3, 7] = math.nan, math.inf, -math.inf
+    x[4] = math.nan
+    t = torch.tensor([0, -1, V, 7, -1, 2], dtype=torch.int32, device="cuda")
+    r = lib.token_logprobs(x, t, 2)
+    assert r.logp[[1, 2, 4]].tolist() == [0.0, 0.0, 0.0] and float(r.logp[3]) == -math.inf
+    dlp = torch.ones(6, device="cuda")
+    dlp[5] = 0.0
+    for dh in (None, torch.zeros(6, device="cuda")):
+        d = lib.token_logprobs_backward(dlp, dh, x, t, r.stats, r.entropy)
+        assert not bool(d[[1, 2, 4, 5]].any()) and bool(torch.isfinite(d).all())
+        assert bool(d[0].any()) and bool(d[3].any())
+    d = lib.token_logprobs_backward(dlp, torch.ones(6, device="cuda"), x, t, r.stats, r.entropy)
+    assert bool(torch.isnan(d[[1, 2, 4]]).all()) and bool(torch.isfinite(d[[0, 3, 5]]).all())
