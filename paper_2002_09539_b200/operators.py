@@ -151,22 +151,28 @@ def token_logprobs(logits, targets, top=0):
     top = operator.index(top)
     if top < 0 or top > MAX_TOP or top > V:
         _refuse("top must be in [0, min(V, %d)]", MAX_TOP)
-    # the float outputs share one allocation: allocating is most of what the host does here
-    out = targets.new_empty(N * (4 + top), dtype=torch.float32)
+    # the float outputs and the workspace behind them share one allocation (the workspace is 4 bytes for 256
+    # logits and little more): allocating and viewing is most of what the host does here
+    n_out = N * (4 + top)
+    wn = _workspace_bytes("olsgd_token_logprobs_workspace", code, N, V, top)
+    at = (n_out + 63) // 64 * 64   # 256 bytes
+    out = targets.new_empty(at + wn // 4 if wn else n_out, dtype=torch.float32)
     p = out.data_ptr()
-    ws, wp, wn = _workspace(targets, "olsgd_token_logprobs_workspace", code, N, V, top)
+    wp = p + 4 * at if wn else None
+    sizes = (N, N, 2 * N, top * N, out.shape[0] - n_out)
     if top:
-        top_ids = targets.new_empty(lead + (top,))
+        top_ids = targets.new_empty((N, top))
         _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N, top_ids.data_ptr(), wp, wn)
-        logp, entropy, stats, top_logp = out.split_with_sizes((N, N, 2 * N, top * N))
-        top_logp = top_logp.view(top_ids.shape)
+        logp, entropy, stats, top_logp, _ = out.split_with_sizes(sizes)
+        top_logp = top_logp.view(N, top)
     else:
         top_logp = top_ids = None
         _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, 0, p, p + 4 * N, p + 8 * N, None, None, wp, wn)
-        logp, entropy, stats = out.split_with_sizes((N, N, 2 * N))
-    if len(lead) != 1:
-        logp, entropy = logp.view(lead), entropy.view(lead)
-    return TokenLogprobs(logp, entropy, stats.view(lead + (2,)), top_logp, top_ids)
+        logp, entropy, stats, _, _ = out.split_with_sizes(sizes)
+    if len(lead) == 1:
+        return TokenLogprobs(logp, entropy, stats.view(N, 2), top_logp, top_ids)
+    return TokenLogprobs(logp.view(lead), entropy.view(lead), stats.view(lead + (2,)), top_logp.view(lead + (top,)) if top else None,
+                         top_ids.view(lead + (top,)) if top else None)
 
 
 def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
@@ -212,16 +218,17 @@ def clip_grads(grads, max_norm, out=None):
     first = grads[0]
     m, dev = first.shape[0] if first.dim() else 0, first.device
     _need(first.is_cuda and m >= 1, "grads must be CUDA tensors with the workers first")
-    flat = []
+    index, codes, flat = dev.index, DTYPES, []
     for g, o in zip(grads, out):
         shape = g.shape
-        if shape != o.shape or len(shape) == 0 or shape[0] != m or g.device != dev or o.device != dev:
+        if shape != o.shape or not shape or shape[0] != m or g.get_device() != index or o.get_device() != index:
             _refuse("gradients and out must be on one device, of the same shapes, with %d workers first", m)
-        gc, oc = DTYPES.get(g.dtype), DTYPES.get(o.dtype)
+        gc, oc = codes.get(g.dtype), codes.get(o.dtype)
         if gc is None or oc is None:
             _refuse("gradients and out must be float32, bfloat16 or float16")
-        n, gs = _worker_rows(g, m, "a gradient")
-        flat += (g.data_ptr(), o.data_ptr(), n, gs, n if o.is_contiguous() else _worker_rows(o, m, "out")[1], gc | (oc << 32))
+        n = g.numel() // m
+        flat += (g.data_ptr(), o.data_ptr(), n, n if g.is_contiguous() else _worker_rows(g, m, "a gradient")[1],
+                 n if o.is_contiguous() else _worker_rows(o, m, "out")[1], gc | (oc << 32))
     table = (_i64 * len(flat))(*flat)
     norms = first.new_empty(m, dtype=torch.float32)
     ws, wp, wn = _workspace(norms, "olsgd_clip_grads_workspace", m, len(grads))
