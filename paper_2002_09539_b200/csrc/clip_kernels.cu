@@ -35,14 +35,20 @@ struct Item {
   int64_t first_tile;                 // of this worker's tile list
   int32_t in_dtype, out_dtype;
 };
+// N: descriptors a launch has room for.  Short lists go with few, since the host copies the parameters
+// several times with each launch (a call on one tensor takes 12.9 us of its time, 16.2 with room for
+// all; on twenty, with room for kSomeTensors, 37 and 43).
+template <int N>
 struct Items {
   int32_t count, pad;
   int64_t tiles;                      // per worker
-  Item item[kMaxTensors];
+  Item item[N];
 };
-static_assert(sizeof(Items) <= 32764 - 64, "kernel parameter space");
+constexpr int kFewTensors = 8, kSomeTensors = 48;
+static_assert(sizeof(Items<kMaxTensors>) <= 32764 - 64, "kernel parameter space");
 
-__device__ __forceinline__ int find_item(const Items& it, int64_t tile) {
+template <int N>
+__device__ __forceinline__ int find_item(const Items<N>& it, int64_t tile) {
   int lo = 0, hi = it.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -117,8 +123,9 @@ __device__ __forceinline__ double block_sum(double s) {
 }
 
 // CTA (b, worker): tiles b, b + gridDim.x, ... of the worker's list.
+template <int N>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-square_sum_kernel(const __grid_constant__ Items it, double* __restrict__ part, int part_ld, int part_off) {
+square_sum_kernel(const __grid_constant__ Items<N> it, double* __restrict__ part, int part_ld, int part_off) {
   launch_gate();
   const int64_t worker = blockIdx.y;
   // what the second kernel will find in L2: the last of what is read here, at normal priority
@@ -167,8 +174,9 @@ __device__ __forceinline__ void scale_tile_to(const Item& it, int64_t worker, in
   else scale_tile<TI, __half>(it, worker, tile, c);
 }
 
+template <int N>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-clip_scale_kernel(const __grid_constant__ Items it, const double* __restrict__ part, int part_ld, int n_part,
+clip_scale_kernel(const __grid_constant__ Items<N> it, const double* __restrict__ part, int part_ld, int n_part,
                   float max_norm, float* __restrict__ norms) {
   launch_gate();
   const int64_t worker = blockIdx.y;
@@ -197,7 +205,8 @@ int ctas_per_worker(int32_t m) {
 }
 
 // Descriptors of tensors [first, first + count).
-void fill(Items& it, const olsgd_clip_tensor* t, int32_t first, int32_t count) {
+template <int N>
+void fill(Items<N>& it, const olsgd_clip_tensor* t, int32_t first, int32_t count) {
   it.count = 0;
   it.pad = 0;
   it.tiles = 0;
@@ -219,31 +228,41 @@ size_t clip_workspace(int32_t m, int32_t n_tensors) {
   return (size_t)m * ctas_per_worker(m) * (launches < 1 ? 1 : launches) * sizeof(double);
 }
 
-cudaError_t launch_clip(const olsgd_clip_tensor* t, int32_t n_tensors, int32_t m, float max_norm,
-                        float* norms, void* ws, cudaStream_t s) {
+namespace {
+template <int N>
+cudaError_t clip(const olsgd_clip_tensor* t, int32_t n_tensors, int32_t m, float max_norm, float* norms, void* ws,
+                 cudaStream_t s) {
   double* part = static_cast<double*>(ws);
-  const int launches = n_tensors <= kMaxTensors ? 1 : (n_tensors + kMaxTensors - 1) / kMaxTensors;
+  const int launches = n_tensors <= N ? 1 : (n_tensors + N - 1) / N;
   const int per = ctas_per_worker(m), part_ld = per * launches;
-  Items it;
+  Items<N> it;
   // every launch writes all of its `ctas` partial sums (zero where it has no tile); the grids
   // of a single launch are cut to the tiles there are
   int ctas = per;
   for (int l = 0; l < launches; ++l) {
-    fill(it, t, l * kMaxTensors, n_tensors - l * kMaxTensors < kMaxTensors ? n_tensors - l * kMaxTensors : kMaxTensors);
+    fill(it, t, l * N, n_tensors - l * N < N ? n_tensors - l * N : N);
     if (launches == 1) ctas = it.tiles < per ? (it.tiles < 1 ? 1 : (int)it.tiles) : per;
-    const cudaError_t e = launch_chained(square_sum_kernel, dim3((unsigned)ctas, (unsigned)m), dim3(kThreads), 0, s, it,
+    const cudaError_t e = launch_chained(square_sum_kernel<N>, dim3((unsigned)ctas, (unsigned)m), dim3(kThreads), 0, s, it,
                                          part, part_ld, l * per);
     if (e != cudaSuccess) return e;
   }
   for (int l = 0; l < launches; ++l) {
     if (launches > 1)
-      fill(it, t, l * kMaxTensors, n_tensors - l * kMaxTensors < kMaxTensors ? n_tensors - l * kMaxTensors : kMaxTensors);
+      fill(it, t, l * N, n_tensors - l * N < N ? n_tensors - l * N : N);
     const cudaError_t e =
-        launch_chained(clip_scale_kernel, dim3((unsigned)ctas, (unsigned)m), dim3(kThreads), 0, s, it,
+        launch_chained(clip_scale_kernel<N>, dim3((unsigned)ctas, (unsigned)m), dim3(kThreads), 0, s, it,
                        (const double*)part, part_ld, launches == 1 ? ctas : part_ld, max_norm, l == 0 ? norms : nullptr);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
+}
+}  // namespace
+
+cudaError_t launch_clip(const olsgd_clip_tensor* t, int32_t n_tensors, int32_t m, float max_norm, float* norms, void* ws,
+                        cudaStream_t s) {
+  if (n_tensors <= kFewTensors) return clip<kFewTensors>(t, n_tensors, m, max_norm, norms, ws, s);
+  if (n_tensors <= kSomeTensors) return clip<kSomeTensors>(t, n_tensors, m, max_norm, norms, ws, s);
+  return clip<kMaxTensors>(t, n_tensors, m, max_norm, norms, ws, s);
 }
 
 }  // namespace olsgd
