@@ -49,6 +49,7 @@ struct GatedArgs {
   int splits, kb_split;       // parts that K is cut into, K blocks of a part
   int rows, cols;             // extents of one problem's output (FORWARD: cols = F)
   int act, f16;
+  int beside;                 // runs beside the kernel ahead of it: see launch_gated_backward
   int a_rows;                 // rows of A that are loaded (K-major): all 128 unless the problem has fewer
   int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
   void* out0;                 // h, dx or dWg
@@ -354,7 +355,7 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   if (CTAS == 2) cluster_barrier();   // the peer's barriers are initialised
   tc_fence_after();
   const uint32_t tmem_base = ctl->tmem_base;
-  launch_gate();
+  if (!g.beside) launch_gate();
 
   if (warp == 0 && lane == 0) {
     // ---------------- TMA producer (both CTAs of a pair; the leader announces both's bytes)
@@ -534,6 +535,8 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
     if (CTAS == 2) tmem_dealloc_pair(tmem_base, kTmemCols);
     else tmem_dealloc(tmem_base, kTmemCols);
   }
+  // what follows in the stream waits for this kernel: so this one waits for the kernel it ran beside
+  if (g.beside) launch_gate();
 }
 
 // ------------------------------------------------------------------------- few tokens
@@ -985,12 +988,16 @@ GatedArgs args_for(const GatedShape& d, const Shape& sh, uint8_t* parts) {
 }
 
 template <int MODE>
-cudaError_t launch_mode(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
-  const cudaError_t e = sh.bn == 64    ? launch_variant<MODE, 1, 64, 8>(maps, g, s)
-                        : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6>(maps, g, s)
-                        : sh.ctas == 2 ? launch_variant<MODE, 2, 256, 6>(maps, g, s)
-                                       : launch_variant<MODE, 1, 256, 4>(maps, g, s);
-  if (e != cudaSuccess || g.splits == 1) return e;
+cudaError_t launch_product(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
+  return sh.bn == 64    ? launch_variant<MODE, 1, 64, 8>(maps, g, s)
+         : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6>(maps, g, s)
+         : sh.ctas == 2 ? launch_variant<MODE, 2, 256, 6>(maps, g, s)
+                        : launch_variant<MODE, 1, 256, 4>(maps, g, s);
+}
+// Where K was cut: the joining launch.
+template <int MODE>
+cudaError_t launch_join(const GatedArgs& g, cudaStream_t s) {
+  if (g.splits == 1) return cudaSuccess;
   const int64_t width = MODE == FORWARD ? g.pre_pitch : g.parts_row, warps = g.rows * ((width + 255) / 256);
   return launch_chained(g.f16 ? gated_join_kernel<__half, MODE> : gated_join_kernel<__nv_bfloat16, MODE>,
                         dim3((unsigned)((warps + 7) / 8), (unsigned)g.problems), dim3(256), 0, s, g);
@@ -1070,9 +1077,9 @@ cudaError_t few(const GatedForward& a, cudaStream_t s) {
 }  // namespace
 
 // The workspace: copies of operands that TMA cannot take, then da and db (backward), then the parts of
-// one product at a time.
+// the products (backward: dx, then the weights' gradients, which run side by side).
 struct Workspace {
-  size_t copies, da, db, parts, total;
+  size_t da, db, parts, parts_dw, total;
 };
 Workspace layout(const GatedShape& d, bool backward, bool copies) {
   Workspace w{};
@@ -1080,14 +1087,8 @@ Workspace layout(const GatedShape& d, bool backward, bool copies) {
   const size_t part = backward ? round256((size_t)d.m * d.T * round8(d.F) * 2) : 0;
   w.db = w.da + part;
   w.parts = w.db + part;
-  size_t parts = 0;
-  if (backward) {
-    const size_t dx = parts_bytes<DX>(d), dw = parts_bytes<DW>(d);
-    parts = dx > dw ? dx : dw;
-  } else {
-    parts = parts_bytes<FORWARD>(d);
-  }
-  w.total = w.parts + parts;
+  w.parts_dw = w.parts + (backward ? round256(parts_bytes<DX>(d)) : 0);
+  w.total = w.parts_dw + (backward ? parts_bytes<DW>(d) : parts_bytes<FORWARD>(d));
   return w;
 }
 
@@ -1118,7 +1119,8 @@ cudaError_t launch_gated_forward(GatedForward a, cudaStream_t s) {
       !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, b_rows, a.f16))
     return cudaErrorInvalidValue;
   maps.a1 = maps.a0;
-  return launch_mode<FORWARD>(sh, maps, g, s);
+  OLSGD_STEP(launch_product<FORWARD>(sh, maps, g, s));
+  return launch_join<FORWARD>(g, s);
 }
 
 cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
@@ -1131,32 +1133,41 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s));
   OLSGD_STEP(a.f16 ? elementwise<__half>(a, pitch, da, db, s) : elementwise<__nv_bfloat16>(a, pitch, da, db, s));
   const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
+  // Both products read what the element-wise kernel has written, and neither what the other writes.  The
+  // second one is launched beside the first: its CTAs may start once all of the first one's have
+  // passed their gate (the element-wise kernel, and all before it, have completed then), it takes the
+  // multiprocessors as they become free, and at its end it waits for the first.  The joining
+  // launches come after both.
+  GatedArgs dx{}, dw{};
   if (a.dx) {
     const Shape sh = shape_for<DX>(product_of(DX, a));
-    GatedArgs g = args_for<DX>(a, sh, ws + at.parts);
-    g.out_width = store_width(a.dx, a.D);
-    g.out0 = a.dx;
-    g.a_rows = loaded_rows(a.T);
+    dx = args_for<DX>(a, sh, ws + at.parts);
+    dx.out_width = store_width(a.dx, a.D);
+    dx.out0 = a.dx;
+    dx.a_rows = loaded_rows(a.T);
     GatedMaps maps;
-    if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, g.a_rows, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, g.a_rows, a.f16) ||
+    if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, dx.a_rows, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, dx.a_rows, a.f16) ||
         !make_map16(&maps.b0, a.wg, a.D, a.F, a.m, kBK, a.f16) || !make_map16(&maps.b1, a.wu, a.D, a.F, a.m, kBK, a.f16))
       return cudaErrorInvalidValue;
-    OLSGD_STEP(launch_mode<DX>(sh, maps, g, s));
+    OLSGD_STEP(launch_product<DX>(sh, maps, dx, s));
   }
   if (a.dwg) {
     const Shape sh = shape_for<DW>(product_of(DW, a));
-    GatedArgs g = args_for<DW>(a, sh, ws + at.parts);
+    dw = args_for<DW>(a, sh, ws + at.parts_dw);
+    dw.beside = a.dx != nullptr;
     const int w0 = store_width(a.dwg, a.D), w1 = store_width(a.dwu, a.D);
-    g.out_width = w0 < w1 ? w0 : w1;
-    g.out0 = a.dwg;
-    g.out1 = a.dwu;
+    dw.out_width = w0 < w1 ? w0 : w1;
+    dw.out0 = a.dwg;
+    dw.out1 = a.dwu;
     GatedMaps maps;
     if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, kBK, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, kBK, a.f16) ||
         !make_map16(&maps.b0, a.x, a.D, a.T, a.m, kBK, a.f16))
       return cudaErrorInvalidValue;
     maps.b1 = maps.b0;
-    OLSGD_STEP(launch_mode<DW>(sh, maps, g, s));
+    OLSGD_STEP(launch_product<DW>(sh, maps, dw, s));
   }
+  if (a.dx) OLSGD_STEP(launch_join<DX>(dx, s));
+  if (a.dwg) OLSGD_STEP(launch_join<DW>(dw, s));
   return cudaSuccess;
 }
 

@@ -282,3 +282,39 @@ print("captured first: ok")
 """ % (root, os.path.join(root, "tests"))
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "captured first: ok" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("m,T,D,F", [(16, 128, 256, 256), (1, 512, 512, 1024), (2, 65, 1000, 72), (1, 3, 64, 40), (4, 300, 1024, 512), (1, 4000, 64, 64)])
+def test_gated_gradients_side_by_side_keep_the_stream_s_order(m, T, D, F):
+    """The two products of the backward pass overlap.  What follows them at once (a torch kernel, the next call in the same
+    memory) sees both done: the same bits as with launches in plain order, over and over."""
+    g = _gen(m + T)
+    x, wg, wu = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((m, T, D), (m, F, D), (m, F, D)))
+    dhs = [torch.randn((m, T, F), generator=g, device="cuda").bfloat16() for _ in range(3)]
+    _, pre = lib.gated_forward(x, wg, wu, "gelu", save=True)
+
+    def once(dh):
+        dx, dwg, dwu = lib.gated_backward(dh, x, wg, wu, pre, "gelu")
+        return dx + 1, dwg + 1, dwu + 1   # the gradients themselves go back to the allocator at once
+
+    before = lib.set_launch_overlap(False)
+    try:
+        want = [once(dh) for dh in dhs]
+        torch.cuda.synchronize()
+    finally:
+        lib.set_launch_overlap(before)
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(60):
+        for dh, w in zip(dhs, want):
+            for a, b in zip(once(dh), w):
+                bad += (a != b).sum()
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        got = [once(dh) for dh in dhs]
+    for _ in range(20):
+        graph.replay()
+        for a, b in zip(got, want):
+            for u, v in zip(a, b):
+                bad += (u != v).sum()
+    assert int(bad) == 0
