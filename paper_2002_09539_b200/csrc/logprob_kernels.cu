@@ -4,19 +4,19 @@
 //   log p_j = (x_j - m) - log S,   H = log S - (1/S) sum exp(x_j - m) (x_j - m).
 // One pass keeps a running maximum and, relative to it, s = sum e^d and t = sum e^d d
 // (d = x - m): when the maximum rises from m to m', both are carried over by s' = s f,
-// t' = (t + s delta) f with delta = m - m', f = e^delta.  The
-// difference x - m is formed before it is scaled, so rows of the type's lowest value, or far
-// from zero, keep their probabilities.  All of it is held in fp32.
+// t' = (t + s delta) f with delta = m - m', f = e^delta.  The difference x - m is formed before it
+// is scaled, so rows of the type's lowest value, or far from zero, keep their probabilities.
+// All of it is held in fp32.
 //
 // Alternatives: a warp reads 256 consecutive logits (a chunk) at a time and needs the chunk's
-// maximum for the running maximum anyway, so it also stores it.  The k largest
-// elements (ties to the lowest index) lie in the k chunks that come first by (maximum, lowest
-// index): if an element's chunk is not among them, each of those k chunks holds an element
-// that comes before it.  The finishing kernel therefore reads k chunks again and nothing else.
+// maximum for the running maximum anyway, so it also stores it.  The k largest elements (ties to
+// the lowest index) lie in the k chunks that come first by (maximum, lowest index): if an
+// element's chunk is not among them, each of those k chunks holds an element that comes before
+// it.  So k chunks, and few more, are read again and nothing else (find_top).
 //
 // Rows of up to 1024 logits stay in a warp's registers (one launch, no second read).  Longer
 // ones are bound by reading the logits once; a row is split over several CTAs when there are
-// fewer rows than the GPU has room for, and the parts are joined by the finishing kernel.
+// fewer rows than the GPU has room for, and the parts are joined by a finishing kernel.
 #include "operator_common.cuh"
 #include "operators_internal.h"
 
@@ -32,7 +32,7 @@ constexpr int kChunkElems = 256;      // eight elements per lane: one 16-byte pi
 constexpr int kWarpRowMax = 1024;     // longest row that stays in a warp's registers
 constexpr int kWarpList = 160;        // candidates that a warp lists
 constexpr int kMaxTop = OLSGD_MAX_TOP;
-static_assert(kMaxTop == 32, "a lane holds one candidate of each warp");
+static_assert(kMaxTop <= 32, "a lane for each chunk of a row that has no more than k");
 constexpr int kMaxSplit = 64;
 // Unsplit rows that are this short, or whose alternatives are wanted, get CTAs of half the threads:
 // twice as many rows are on their way while others begin and end (3684 x 10549 bf16: 18.7 us against
