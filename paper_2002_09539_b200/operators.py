@@ -322,8 +322,8 @@ def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=No
     """olsgd_embedding_backward: the gradient of a table [m][vocab][D] from d_out [m][T][D] and the ids of the lookup; new, of
     type `dtype`, or written to `out` (each worker's part contiguous, for example a view of a flat gradient [m][P])."""
     lib = _ops()
-    if not d_out.is_cuda or d_out.dim() != 3:
-        _refuse("d_out must be a CUDA tensor [m][T][D]")
+    if not d_out.is_cuda or d_out.dim() != 3 or d_out.shape[0] < 1:
+        _refuse("d_out must be a CUDA tensor [m][T][D] of at least one worker")
     code, dev = _dtype(d_out, "d_out"), d_out.device
     m, T, D = d_out.shape
     V = int(vocab)
@@ -342,6 +342,7 @@ def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=No
 def operators_join(device="cuda"):
     """olsgd_operators_join on the device's current stream: waits for it, and raises if an operator's bounded wait gave up."""
     dev = torch.device(device)
+    _need(dev.type == "cuda", "device must be a CUDA device")
     if dev.index is None:
         dev = torch.device(dev.type, torch.cuda.current_device())
     _run(_ops().olsgd_operators_join, dev)

@@ -711,3 +711,14 @@ def test_token_logprobs_gradient_of_padding_is_zero_whatever_it_holds(V, dtype):
         assert bool(d[0].any()) and bool(d[3].any())
     d = lib.token_logprobs_backward(dlp, torch.ones(6, device="cuda"), x, t, r.stats, r.entropy)
     assert bool(torch.isnan(d[[1, 2, 4]]).all()) and bool(torch.isfinite(d[[0, 3, 5]]).all())
+
+
+def test_operators_of_no_workers_are_refused():
+    x = torch.zeros(0, 4, 8, device="cuda")
+    ids = torch.zeros(0, 4, dtype=torch.int32, device="cuda")
+    for call in (lambda: lib.embedding_forward(x, ids), lambda: lib.embedding_backward(x, ids, 8), lambda: lib.clip_grads(x, 1.0),
+                 lambda: lib.gated_forward(x.bfloat16(), x.bfloat16(), x.bfloat16())):
+        with pytest.raises((ValueError, lib.OlsgdError)):
+            call()
+    with pytest.raises(ValueError):
+        lib.operators_join("cpu")

@@ -318,3 +318,47 @@ def test_gated_gradients_side_by_side_keep_the_stream_s_order(m, T, D, F):
             for u, v in zip(a, b):
                 bad += (u != v).sum()
     assert int(bad) == 0
+
+
+def _forked(run, inputs, busy, side):
+    """One set of calls on the current stream and one on `side`, each behind an event of the other stream: the operators' first
+    launches follow event waits, not kernels."""
+    here = torch.cuda.current_stream()
+    a = {k: torch.empty_strided(v.shape, v.stride(), dtype=v.dtype, device=v.device).zero_() for k, v in inputs.items()}
+    # what the side stream reads is written here, late
+    for _ in range(4):
+        busy = busy @ busy
+    for k in a:
+        a[k].copy_(inputs[k])
+    side.wait_stream(here)
+    with torch.cuda.stream(side):
+        first = run(a)
+    here.wait_stream(side)
+    second = run(a)   # and again here, behind the side stream
+    return first, second, busy
+
+
+def test_operators_behind_events_of_other_streams():
+    make, run = _calls(0)
+    a = make(5)
+    want = run(a)
+    busy = torch.eye(4096, device="cuda")
+    here, side = torch.cuda.Stream(), torch.cuda.Stream()
+    here.wait_stream(torch.cuda.current_stream())
+    kept = []
+    with torch.cuda.stream(here):
+        for _ in range(3):
+            kept.append(_forked(run, a, busy, side))
+    torch.cuda.synchronize()
+    for first, second, _ in kept:
+        assert all(torch.equal(x, y) for x, y in zip(first, want)) and all(torch.equal(x, y) for x, y in zip(second, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=here):
+        first, second, _ = _forked(run, a, busy, side)
+    for _ in range(3):
+        for t in list(first) + list(second):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(first, want)) and all(torch.equal(x, y) for x, y in zip(second, want))
+    lib.operators_join()
