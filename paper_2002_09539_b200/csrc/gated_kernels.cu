@@ -790,8 +790,9 @@ struct Border {
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const float* __restrict__ pre,
-                      T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec, const Border border) {
-  launch_gate();
+                      T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec, const Border border,
+                      bool beside) {
+  if (!beside) launch_gate();
   const T* dh_w = dh + (int64_t)blockIdx.y * dh_worker;
   const int lane = threadIdx.x & 31;
   // a warp per stretch of kStretch columns of a row
@@ -859,6 +860,7 @@ gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_ro
       }
     }
   }
+  if (beside) launch_gate();
 }
 
 // --------------------------------------------------------------------------------- host
@@ -1009,12 +1011,12 @@ bool tma_ready(const GatedOperand& o, int64_t rows, int64_t m) {
 }
 
 // Replaces those of the operands [m][rows][cols] that TMA cannot take by copies in rows of
-// round8(cols) from ws on.
+// round8(cols) from ws on; says whether there were any.
 struct Wanted {
   GatedOperand* o;
   int64_t rows;
 };
-cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws, cudaStream_t s) {
+cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws, cudaStream_t s, bool* any = nullptr) {
   PadOperands all{};
   all.cols = cols;
   all.pitch = round8(cols);
@@ -1032,6 +1034,7 @@ cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m,
     o = GatedOperand{dst, rows * all.pitch, all.pitch};
     most_rows = rows > most_rows ? rows : most_rows;
   }
+  if (any) *any = n > 0;
   if (n == 0) return cudaSuccess;
   return launch_chained(pad_rows_kernel, dim3((unsigned)((most_rows + 7) / 8), (unsigned)m, (unsigned)n), dim3(256), 0, s, all);
 }
@@ -1046,7 +1049,7 @@ int store_width(const void* p, int64_t cols) {
 }
 
 template <typename T>
-cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, cudaStream_t s) {
+cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, bool beside, cudaStream_t s) {
   const int64_t warps = a.T * ((pitch + kStretch - 1) / kStretch);
   const dim3 grid((unsigned)((warps + 7) / 8), (unsigned)a.m);
   const bool vec = a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m);
@@ -1056,7 +1059,8 @@ cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* d
                                      : gated_backward_kernel<T, OLSGD_ACT_SIGMOID>;
   return launch_chained(k, grid, dim3(256), 0, s, static_cast<const T*>(a.dh.p), a.dh.worker_stride, a.dh.row_stride,
                         a.pre, static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec,
-                        Border{a.x, a.wg, a.D, a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m)});
+                        Border{a.x, a.wg, a.D, a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m)},
+                        beside);
 }
 
 template <typename T>
@@ -1130,8 +1134,13 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   void *da = ws + at.da, *db = ws + at.db;
   const Wanted wanted[] = {{&a.x, a.T}, {&a.wg, a.F}, {&a.wu, a.F}};   // x for the weights' gradients, the weights for dx
   const int from = a.dwg ? 0 : 1, to = a.dx ? 3 : 1;
-  OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s));
-  OLSGD_STEP(a.f16 ? elementwise<__half>(a, pitch, da, db, s) : elementwise<__nv_bfloat16>(a, pitch, da, db, s));
+  // The element-wise kernel needs none of the copies: where there are any it runs beside them (as the second product
+  // does below), on the operands as they were given.  3 workers, 333 tokens, 1021 -> 2035: backward 56.5 -> 54.9 us; one
+  // worker, 40 tokens, 333 -> 1003: 12.7 -> 11.9.
+  const GatedBackward given = a;
+  bool copies = false;
+  OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s, &copies));
+  OLSGD_STEP(a.f16 ? elementwise<__half>(given, pitch, da, db, copies, s) : elementwise<__nv_bfloat16>(given, pitch, da, db, copies, s));
   const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
   // Both products read what the element-wise kernel has written, and neither what the other writes.  The
   // second one is launched beside the first: its CTAs may start once all of the first one's have

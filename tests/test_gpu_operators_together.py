@@ -362,3 +362,45 @@ def test_operators_behind_events_of_other_streams():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(first, want)) and all(torch.equal(x, y) for x, y in zip(second, want))
     lib.operators_join()
+
+
+@pytest.mark.parametrize("m,T,D,F", [(3, 65, 333, 203), (1, 300, 1021, 77), (2, 130, 67, 640), (2, 4, 9, 3)])
+@pytest.mark.parametrize("kind", ["silu", "relu"])
+def test_gated_gradients_beside_their_copies_keep_the_stream_s_order(m, T, D, F, kind):
+    """With rows that have to be copied the element-wise kernel runs beside the copies, on operands that were written just before
+    and in memory that the call before used: the same bits as in plain order, eager and captured."""
+    g = _gen(m * T + D)
+    x, wg, wu = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((m, T, D), (m, F, D), (m, F, D)))
+    dh = torch.randn((m, T, F), generator=g, device="cuda").bfloat16()
+
+    def once(scale):
+        xs, ws = x * scale, wg * scale
+        _, pre = lib.gated_forward(xs, ws, wu, kind, save=True)
+        both = lib.gated_backward(dh * scale, xs, ws, wu, pre, kind)
+        dx = lib.gated_backward(dh, xs, ws, wu, pre, kind, want_d_w=False)[0]
+        dw = lib.gated_backward(dh, xs, ws, wu, pre, kind, want_d_x=False)[1:]
+        return [t + 1 for t in (*both, dx, *dw)]
+
+    scales = (1.0, -2.0, 0.5)
+    before = lib.set_launch_overlap(False)
+    try:
+        want = [once(s) for s in scales]
+        torch.cuda.synchronize()
+    finally:
+        lib.set_launch_overlap(before)
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(30):
+        for s, w in zip(scales, want):
+            for a, b in zip(once(s), w):
+                bad += (a != b).sum()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        got = [once(s) for s in scales]
+    for _ in range(10):
+        graph.replay()
+        for a, b in zip(got, want):
+            for u, v in zip(a, b):
+                bad += (u != v).sum()
+    assert int(bad) == 0
+    lib.operators_join()
