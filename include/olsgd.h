@@ -488,8 +488,9 @@ olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int
  *   d_x = da Wg + db Wu,  d_w_gate = da^T x,  d_w_up = db^T x,
  * each rounded once.  pre is what the forward call left for the same x, w_gate and w_up.
  * d_x may be NULL, and so may d_w_gate and d_w_up together; all three are contiguous.
- * relu's derivative at 0 is 0; next to 0 its side is found in 64 bits.  T == 0 zeroes the weight
- * gradients.                                                                              */
+ * relu's derivative at 0 is 0; where a lies within (8 + D / 128) 2^-23 |x_t| |w_f| of 0 (Euclidean
+ * norms of its rows of x and w_gate, if they are finite) its side is found in 64 bits.  T == 0 zeroes
+ * the weight gradients.                                                                    */
 olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, int32_t dtype,
                                   int32_t activation, const void* d_h, int64_t d_h_worker_stride,
                                   int64_t d_h_row_stride, const void* x, int64_t x_worker_stride,

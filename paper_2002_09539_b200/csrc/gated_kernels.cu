@@ -758,7 +758,7 @@ constexpr int kStretch = 512;
 template <typename T>
 __device__ __forceinline__ double warp_dot(const T* x, const T* w, int64_t D, bool vec) {
   const int lane = threadIdx.x & 31;
-  double s = 0.0;
+  double part[4] = {0.0, 0.0, 0.0, 0.0};   // (a chain of additions takes longer than the loads)
   if (vec) {
 #pragma unroll 2
     for (int64_t k = lane * 8; k < D; k += 256) {
@@ -766,70 +766,216 @@ __device__ __forceinline__ double warp_dot(const T* x, const T* w, int64_t D, bo
       Elem<T>::unpack(ld16(x + k), vx);
       Elem<T>::unpack(ld16(w + k), vw);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += (double)(vx[e] * vw[e]);
+      for (int e = 0; e < 8; ++e) part[e & 3] += (double)(vx[e] * vw[e]);
     }
   } else {
-#pragma unroll 4
-    for (int64_t k = lane; k < D; k += 32) s += (double)(Elem<T>::to_float(x[k]) * Elem<T>::to_float(w[k]));
+    constexpr int U = 8;
+    for (int64_t k0 = lane; k0 < D; k0 += 32 * U) {
+      float v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t k = k0 + u * 32;
+        v[u] = k < D ? Elem<T>::to_float(x[k]) * Elem<T>::to_float(w[k]) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) part[u & 3] += (double)v[u];
+    }
   }
+  double s = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return s;
 }
 
-// da = dh b act'(a), db = dh act(a); a, b, da, db have rows of `pitch`.
+// Whether any element of x and the same one of w are both other than 0; by a warp.
+template <typename T>
+__device__ __forceinline__ bool warp_overlap(const T* x, const T* w, int64_t D, bool vec) {
+  const int lane = threadIdx.x & 31;
+  uint32_t any = 0;
+  if (vec) {
+#pragma unroll 4
+    for (int64_t k = lane * 8; k < D; k += 256) {
+      const uint4 a = ld16(x + k), b = ld16(w + k);
+      any |= __vminu2(a.x & 0x7FFF7FFFu, b.x & 0x7FFF7FFFu) | __vminu2(a.y & 0x7FFF7FFFu, b.y & 0x7FFF7FFFu) |
+             __vminu2(a.z & 0x7FFF7FFFu, b.z & 0x7FFF7FFFu) | __vminu2(a.w & 0x7FFF7FFFu, b.w & 0x7FFF7FFFu);
+    }
+  } else {
+#pragma unroll 4
+    for (int64_t k = lane; k < D; k += 32) any |= Elem<T>::to_float(x[k]) != 0.f && Elem<T>::to_float(w[k]) != 0.f;
+  }
+  return __any_sync(0xffffffffu, any != 0);
+}
+
+// relu's derivative jumps at 0, and an accumulation in fp32 is off by a share of its partial sums, none of which
+// exceeds |x_t| |w_f| (Euclidean norms).  Where a lies within
+//   (8 + D / 128) 2^-23 |x_t| |w_f|
+// of 0 its side is not to be trusted, and a is formed again in 64 bits.  Measured (D from 16 to 65536): values of random
+// signs are off by up to 2.4 of these units at any D, products that are positive in the first half of D and
+// negative in the second by D / 200.  One element of 20000 is formed again at D = 1024, one of 4000 at D = 4096.
 //
-// relu's derivative jumps at 0, and an accumulation in fp32 is off by about 1e-6 of the values around
-// it: where a lies within 8e-6 of their mean size, its side of the border is not to be trusted, and
-// a is formed again in 64 bits (some ten of a million, a microsecond each, by a warp at a time).
+// Sums that are exact need no second look, and zeros are mostly that: rows of zeros (tokens that are padding, features
+// that were pruned) and rows with one element other than 0 count as rows of norm 0; where both rows are coarse (multiples
+// of a power of two that is 2^-10 of the norm or more: small integers), 22 bits hold every partial sum.
+//
+// row_norms_kernel: the norm of each row of x and w_gate, with the sign set on that of a coarse row; a warp per row.
+// Most rows are done after their first reading; only those whose first 256 elements are coarse are read twice.  16
+// workers, 128 tokens, 1024 -> 1024: 37 MB in 10.8 us from cold caches (3.4 TB/s; two rows a warp were no faster).
+// relu's backward pass takes 56 us there, silu's, which needs no norms, 45; 8192 tokens, 4096 -> 8192: 1920 and 1890.
+template <typename T>
+__global__ void __launch_bounds__(256)
+row_norms_kernel(GatedOperand x, GatedOperand w, int64_t tokens, int64_t F, int64_t D, float* __restrict__ xn, float* __restrict__ wn,
+                 int64_t wn_pitch) {
+  constexpr int V = Elem<T>::kVec;
+  launch_gate();
+  const int lane = threadIdx.x & 31;
+  const bool of_w = blockIdx.z != 0;
+  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), worker = blockIdx.y;
+  if (r >= (of_w ? F : tokens)) return;
+  const GatedOperand& o = of_w ? w : x;
+  const T* row = static_cast<const T*>(o.p) + worker * o.worker_stride + r * o.row_stride;
+  const int64_t n = D + row_shift(row), j0 = lane * V - row_shift(row);
+  constexpr int kStep = 32 * V, U = 4;
+  f32x2 sum = 0;
+  uint4 first;
+  for (int64_t p = 0; p < n; p += U * kStep) {
+    const int64_t j = j0 + p;
+    uint4 v[U];
+    if (j >= 0 && j + (U - 1) * kStep + V <= D) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = ld16(row + j + u * kStep);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = load_raw<T>(row, j + u * kStep, D, 0);
+    }
+    if (p == 0) first = v[0];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V / 2; ++e) {
+        const f32x2 t = raw_pair<T>(v[u], e);
+        sum = fma2(t, t, sum);
+      }
+  }
+  float lo, hi;
+  unpack2f(sum, lo, hi);
+  lo = warp_sum(lo + hi);
+  float norm = sqrtf(lo);
+  if (!(lo > 1e-20f && lo < 1e30f)) {   // zeros, or squares outside fp32's comfortable range
+    double s = 0.0;
+    for (int64_t j = lane; j < D; j += 32) {
+      const double v = (double)Elem<T>::to_float(row[j]);
+      s = fma(v, v, s);
+    }
+#pragma unroll
+    for (int off = 16; off; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    norm = (float)sqrt(s);
+  }
+  // (2^10 over the norm's power of two; rows whose norm is next to the ends of fp32's range are not coarse)
+  const int exponent = (int)(__float_as_uint(norm) >> 23);
+  bool coarse = exponent > 30 && exponent < 220;
+  const float to_grid = __uint_as_float((uint32_t)(coarse ? 127 + 127 + 10 - exponent : 127) << 23);
+  int others = 0;   // elements other than 0
+  for (int64_t p = 0; p < n && coarse; p += kStep) {
+    float v[V];
+    Elem<T>::unpack(p == 0 ? first : load_raw<T>(row, j0 + p, D, 0), v);
+    bool on_grid = true;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float t = v[e] * to_grid;
+      on_grid = on_grid && t == rintf(t);
+      others += v[e] != 0.f;
+    }
+    coarse = __all_sync(0xffffffffu, on_grid);
+  }
+  if (coarse) {
+    others = __reduce_add_sync(0xffffffffu, others);
+    norm = others <= 1 ? 0.f : -norm;
+  }
+  if (lane == 0) {
+    if (of_w) wn[worker * wn_pitch + r] = norm;
+    else xn[worker * tokens + r] = norm;
+  }
+}
+
 struct Border {
   GatedOperand x, wg;
   int64_t D;
-  bool vec;
+  bool vec;                 // rows of x and w_gate start on 16-byte boundaries, D is a multiple of 8
+  float bound;              // (8 + D / 128) 2^-23
+  const float *xn, *wn;     // norms [m][T], [m][pitch]
 };
+
+// da = dh b act'(a), db = dh act(a); a, b, da, db have rows of `pitch`.
+struct GatedGrad {
+  const void* dh;
+  int64_t dh_worker, dh_row;
+  const float* pre;
+  void *da, *db;
+  int64_t rows, F, pitch;
+  bool vec;                 // rows of dh start on 16-byte boundaries, F is a multiple of 8
+  Border border;            // relu
+};
+
+// One column next to relu's border once more, by a warp; lane `from` stores.
+template <typename T>
+__device__ __forceinline__ void settle(const GatedGrad& g, int64_t worker, int64_t r, int64_t col, bool zero, int from) {
+  const Border& o = g.border;
+  const T* x = static_cast<const T*>(o.x.p) + worker * o.x.worker_stride + r * o.x.row_stride;
+  const T* w = static_cast<const T*>(o.wg.p) + worker * o.wg.worker_stride + col * o.wg.row_stride;
+  // (sparse rows may have no element in common: nothing to add up)
+  if (zero && !warp_overlap(x, w, o.D, o.vec)) return;
+  const float exact = (float)warp_dot(x, w, o.D, o.vec);
+  if ((threadIdx.x & 31) == from) {
+    const int64_t wr = worker * g.rows + r;
+    const ActPair p = act_pair<OLSGD_ACT_RELU>(exact);
+    const float d = Elem<T>::to_float(static_cast<const T*>(g.dh)[worker * g.dh_worker + r * g.dh_row + col]);
+    static_cast<T*>(g.da)[wr * g.pitch + col] = Elem<T>::from_float(d * g.pre[wr * 2 * g.pitch + g.pitch + col] * p.df);
+    static_cast<T*>(g.db)[wr * g.pitch + col] = Elem<T>::from_float(d * p.f);
+  }
+}
+
+// A warp per stretch of kStretch columns of a row.  (The loads go past L1: the kernel may run beside its predecessor, see
+// launch_gated_backward.)
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256)
-gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_row, const float* __restrict__ pre,
-                      T* __restrict__ da, T* __restrict__ db, int64_t rows, int64_t F, int64_t pitch, bool vec, const Border border,
-                      bool beside) {
+__global__ void __launch_bounds__(256, 5) gated_backward_kernel(const __grid_constant__ GatedGrad g, bool beside) {
   if (!beside) launch_gate();
-  const T* dh_w = dh + (int64_t)blockIdx.y * dh_worker;
   const int lane = threadIdx.x & 31;
-  // a warp per stretch of kStretch columns of a row
-  const int64_t stretches = (pitch + kStretch - 1) / kStretch;
+  const int64_t worker = blockIdx.y, stretches = (g.pitch + kStretch - 1) / kStretch;
   const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int64_t r = at / stretches, j_begin = (at - r * stretches) * kStretch;
-  if (r >= rows) return;
-  const int64_t wr = (int64_t)blockIdx.y * rows + r;
+  if (r >= g.rows) return;
+  const int64_t wr = worker * g.rows + r;
+  float xn = 0.f;
+  if constexpr (ACT == OLSGD_ACT_RELU) xn = __ldcg(g.border.xn + wr);
 #pragma unroll
   for (int q = 0; q < kStretch / 256; ++q) {
     const int64_t j0 = j_begin + q * 256, j = j0 + lane * 8;
-    if (j0 >= pitch) break;
-    const bool live = j < pitch;
-    float a[8], b[8], d[8], va[8], vb[8];
+    if (j0 >= g.pitch) break;
+    const bool live = j < g.pitch;
+    float a[8], b[8], d[8], va[8], vb[8], wn[8];
 #pragma unroll
     for (int k = 0; k < 8; k += 4) {
-      const int64_t from = wr * 2 * pitch + (live ? j : 0) + k;
-      Elem<float>::unpack(ld16_stream(pre + from), a + k);
-      Elem<float>::unpack(ld16_stream(pre + pitch + from), b + k);
+      const float* from = g.pre + wr * 2 * g.pitch + (live ? j : 0) + k;
+      Elem<float>::unpack(__ldcg(reinterpret_cast<const uint4*>(from)), a + k);
+      Elem<float>::unpack(__ldcg(reinterpret_cast<const uint4*>(from + g.pitch)), b + k);
+      if constexpr (ACT == OLSGD_ACT_RELU)
+        Elem<float>::unpack(__ldcg(reinterpret_cast<const uint4*>(g.border.wn + worker * g.pitch + (live ? j : 0) + k)), wn + k);
     }
-    const T* src = dh_w + r * dh_row + j;
-    if (vec) {
-      Elem<T>::unpack(live ? ld16_stream(src) : make_uint4(0, 0, 0, 0), d);
+    const T* src = static_cast<const T*>(g.dh) + worker * g.dh_worker + r * g.dh_row + j;
+    if (g.vec) {
+      Elem<T>::unpack(live ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0), d);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = j + e < F ? Elem<T>::to_float(src[e]) : 0.f;
+      for (int e = 0; e < 8; ++e) d[e] = j + e < g.F ? Elem<T>::to_float(__ldcg(src + e)) : 0.f;
     }
-    uint32_t border_mask = 0;
+    uint32_t mask = 0, zeros = 0;   // next to relu's border; those of them that are 0
     if constexpr (ACT == OLSGD_ACT_RELU) {
-      float size = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) size += j + e < F ? fabsf(a[e]) : 0.f;
-      size = warp_sum(size);
-      const int64_t n = F - j0 < 256 ? F - j0 : 256;
-      const float near = size < 1e38f ? size / (float)n * 7.62939453125e-6f : 0.f;   // 2^-17; not beside infinities and NaN
-#pragma unroll
-      for (int e = 0; e < 8; ++e) border_mask |= (j + e < F && fabsf(a[e]) < near ? 1u : 0u) << e;
+      for (int e = 0; e < 8; ++e) {
+        const float near = xn < 0.f && wn[e] < 0.f ? 0.f : fabsf(g.border.bound * xn * wn[e]);
+        mask |= (j + e < g.F && near < INFINITY && fabsf(a[e]) < near ? 1u : 0u) << e;
+        zeros |= (a[e] == 0.f ? 1u : 0u) << e;
+      }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -838,24 +984,17 @@ gated_backward_kernel(const T* __restrict__ dh, int64_t dh_worker, int64_t dh_ro
       vb[e] = d[e] * p.f;
     }
     if (live) {
-      *reinterpret_cast<uint4*>(da + wr * pitch + j) = Elem<T>::pack(va);
-      *reinterpret_cast<uint4*>(db + wr * pitch + j) = Elem<T>::pack(vb);
+      *reinterpret_cast<uint4*>(static_cast<T*>(g.da) + wr * g.pitch + j) = Elem<T>::pack(va);
+      *reinterpret_cast<uint4*>(static_cast<T*>(g.db) + wr * g.pitch + j) = Elem<T>::pack(vb);
     }
     if constexpr (ACT == OLSGD_ACT_RELU) {
-      // those next to the border once more, after what their lane has stored
-      for (uint32_t lanes = __ballot_sync(0xffffffffu, border_mask != 0); lanes; lanes &= lanes - 1) {
+      // those next to the border again, after what their lane has stored
+      for (uint32_t lanes = __ballot_sync(0xffffffffu, mask != 0); lanes; lanes &= lanes - 1) {
         const int from = __ffs(lanes) - 1;
-        for (uint32_t bits = __shfl_sync(0xffffffffu, border_mask, from); bits; bits &= bits - 1) {
-          const int64_t col = j0 + from * 8 + __ffs(bits) - 1;
-          const T* x = static_cast<const T*>(border.x.p) + (int64_t)blockIdx.y * border.x.worker_stride + r * border.x.row_stride;
-          const T* w = static_cast<const T*>(border.wg.p) + (int64_t)blockIdx.y * border.wg.worker_stride + col * border.wg.row_stride;
-          const float exact = (float)warp_dot(x, w, border.D, border.vec);
-          if (lane == from) {
-            const ActPair p = act_pair<ACT>(exact);
-            const float dv = Elem<T>::to_float(dh_w[r * dh_row + col]);
-            da[wr * pitch + col] = Elem<T>::from_float(dv * pre[wr * 2 * pitch + pitch + col] * p.df);
-            db[wr * pitch + col] = Elem<T>::from_float(dv * p.f);
-          }
+        const uint32_t zero = __shfl_sync(0xffffffffu, zeros, from);
+        for (uint32_t bits = __shfl_sync(0xffffffffu, mask, from); bits; bits &= bits - 1) {
+          const int e = __ffs(bits) - 1;
+          settle<T>(g, worker, r, j0 + from * 8 + e, (zero >> e) & 1, from);
         }
       }
     }
@@ -1048,19 +1187,26 @@ int store_width(const void* p, int64_t cols) {
   return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 2;
 }
 
+// relu: norms of the rows of x and w_gate.
 template <typename T>
-cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, bool beside, cudaStream_t s) {
+cudaError_t row_norms(const GatedBackward& a, int64_t pitch, float* xn, float* wn, cudaStream_t s) {
+  const int64_t most = a.T > a.F ? a.T : a.F;
+  return launch_chained(row_norms_kernel<T>, dim3((unsigned)((most + 7) / 8), (unsigned)a.m, 2), dim3(256), 0, s, a.x, a.wg, a.T, a.F, a.D,
+                        xn, wn, pitch);
+}
+
+template <typename T>
+cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, const float* xn, const float* wn, bool beside,
+                        cudaStream_t s) {
   const int64_t warps = a.T * ((pitch + kStretch - 1) / kStretch);
   const dim3 grid((unsigned)((warps + 7) / 8), (unsigned)a.m);
-  const bool vec = a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m);
+  GatedGrad g{a.dh.p, a.dh.worker_stride, a.dh.row_stride, a.pre, da, db, a.T, a.F, pitch, a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m),
+              Border{a.x, a.wg, a.D, a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m), (8.f + (float)a.D / 128) / (1 << 23), xn, wn}};
   auto k = a.act == OLSGD_ACT_SILU   ? gated_backward_kernel<T, OLSGD_ACT_SILU>
            : a.act == OLSGD_ACT_GELU ? gated_backward_kernel<T, OLSGD_ACT_GELU>
            : a.act == OLSGD_ACT_RELU ? gated_backward_kernel<T, OLSGD_ACT_RELU>
                                      : gated_backward_kernel<T, OLSGD_ACT_SIGMOID>;
-  return launch_chained(k, grid, dim3(256), 0, s, static_cast<const T*>(a.dh.p), a.dh.worker_stride, a.dh.row_stride,
-                        a.pre, static_cast<T*>(da), static_cast<T*>(db), a.T, a.F, pitch, vec,
-                        Border{a.x, a.wg, a.D, a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m)},
-                        beside);
+  return launch_chained(k, grid, dim3(256), 0, s, g, beside);
 }
 
 template <typename T>
@@ -1080,17 +1226,19 @@ cudaError_t few(const GatedForward& a, cudaStream_t s) {
 
 }  // namespace
 
-// The workspace: copies of operands that TMA cannot take, then da and db (backward), then the parts of
-// the products (backward: dx, then the weights' gradients, which run side by side).
+// The workspace: copies of operands that TMA cannot take, then (backward) da and db and the norms of the rows of x and
+// w_gate, then the parts of the products (backward: dx, then the weights' gradients, which run side by side).
 struct Workspace {
-  size_t da, db, parts, parts_dw, total;
+  size_t da, db, xn, wn, parts, parts_dw, total;
 };
 Workspace layout(const GatedShape& d, bool backward, bool copies) {
   Workspace w{};
   w.da = copies ? round256((size_t)d.m * d.T * round8(d.D) * 2) + 2 * round256((size_t)d.m * d.F * round8(d.D) * 2) : 0;
   const size_t part = backward ? round256((size_t)d.m * d.T * round8(d.F) * 2) : 0;
   w.db = w.da + part;
-  w.parts = w.db + part;
+  w.xn = w.db + part;
+  w.wn = w.xn + (backward ? round256((size_t)d.m * d.T * sizeof(float)) : 0);
+  w.parts = w.wn + (backward ? round256((size_t)d.m * round8(d.F) * sizeof(float)) : 0);
   w.parts_dw = w.parts + (backward ? round256(parts_bytes<DX>(d)) : 0);
   w.total = w.parts_dw + (backward ? parts_bytes<DW>(d) : parts_bytes<FORWARD>(d));
   return w;
@@ -1136,11 +1284,15 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   const int from = a.dwg ? 0 : 1, to = a.dx ? 3 : 1;
   // The element-wise kernel needs none of the copies: where there are any it runs beside them (as the second product
   // does below), on the operands as they were given.  3 workers, 333 tokens, 1021 -> 2035: backward 56.5 -> 54.9 us; one
-  // worker, 40 tokens, 333 -> 1003: 12.7 -> 11.9.
+  // worker, 40 tokens, 333 -> 1003: 12.7 -> 11.9.  relu's norms come ahead of both.
   const GatedBackward given = a;
+  float *xn = reinterpret_cast<float*>(ws + at.xn), *wn = reinterpret_cast<float*>(ws + at.wn);
+  if (a.act == OLSGD_ACT_RELU)
+    OLSGD_STEP(a.f16 ? row_norms<__half>(a, pitch, xn, wn, s) : row_norms<__nv_bfloat16>(a, pitch, xn, wn, s));
   bool copies = false;
   OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s, &copies));
-  OLSGD_STEP(a.f16 ? elementwise<__half>(given, pitch, da, db, copies, s) : elementwise<__nv_bfloat16>(given, pitch, da, db, copies, s));
+  OLSGD_STEP(a.f16 ? elementwise<__half>(given, pitch, da, db, xn, wn, copies, s)
+                   : elementwise<__nv_bfloat16>(given, pitch, da, db, xn, wn, copies, s));
   const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
   // Both products read what the element-wise kernel has written, and neither what the other writes.  The
   // second one is launched beside the first: its CTAs may start once all of the first one's have
