@@ -484,7 +484,9 @@ olsgd_status olsgd_gated_forward(int32_t m, int64_t T, int64_t D, int64_t F, int
                                  const void* w_up, int64_t w_up_worker_stride,
                                  int64_t w_up_row_stride, void* h, float* pre, void* workspace,
                                  size_t workspace_bytes, void* stream);
-/* Its gradient.  With da = d_h b act'(a) and db = d_h act(a), both rounded to the operand type:
+/* Its gradient.  With da = d_h b act'(a) and db = d_h act(a), both rounded to the operand type
+ * (in fp16 after a power of two that brings the largest value of a worker's da and db to 2^14 or
+ * more, where it lies outside [2^-4, 2^15): the results are scaled back before they are rounded):
  *   d_x = da Wg + db Wu,  d_w_gate = da^T x,  d_w_up = db^T x,
  * each rounded once.  pre is what the forward call left for the same x, w_gate and w_up.
  * d_x may be NULL, and so may d_w_gate and d_w_up together; all three are contiguous.

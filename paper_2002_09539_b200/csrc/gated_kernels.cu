@@ -6,7 +6,8 @@
 // memory, one rounding of each result.  Training keeps a and b, in fp32: 2 T F values written once
 // and read once, against 4 T D F more multiply-adds to form them again.  da and db have to be
 // rounded to 16 bits as operands; were a and b too, the gradients would be 1.7 times as far
-// from the exact ones as the rounding of the result alone leaves them, instead of 1.4 times.
+// from the exact ones as the rounding of the result alone leaves them, instead of 1.4 times.  In fp16 they
+// are scaled by a power of two where they would leave the type's range (scale_for).
 //
 // One kernel, three modes, persistent: a CTA (or a pair of CTAs on one 256-row tile,
 // tcgen05 cta_group::2) walks over tiles of its output.  Warp 0 feeds a ring of shared-memory
@@ -56,6 +57,7 @@ struct GatedArgs {
   void* out1;                 // dWu
   float* pre;                 // FORWARD: a, b [m][T][2][Fp], or null
   int64_t pre_pitch;          // Fp
+  const float* unscale;       // DX, DW: factors of the workers' results, or null
   float* parts;               // splits > 1: sums of the parts, [splits][problems][rows][parts_row]
   int64_t parts_row;          // (FORWARD: a, b as in pre)
 };
@@ -177,10 +179,10 @@ struct Staged {
   uint4* buf;
   __device__ __forceinline__ static int at(int row, int piece) { return row * kPieces + (piece ^ (row & (kPieces - 1))); }
   // 16 values of this lane's row, from column 16 q of the block on
-  __device__ __forceinline__ void put(int lane, int q, const float* v, int f16) {
+  __device__ __forceinline__ void put(int lane, int q, const float* v, int f16, float scale = 1.f) {
     uint32_t p[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] = pack2(v[2 * j], v[2 * j + 1], f16);
+    for (int j = 0; j < 8; ++j) p[j] = pack2(v[2 * j] * scale, v[2 * j + 1] * scale, f16);
     buf[at(lane, 2 * q)] = make_uint4(p[0], p[1], p[2], p[3]);
     buf[at(lane, 2 * q + 1)] = make_uint4(p[4], p[5], p[6], p[7]);
   }
@@ -303,7 +305,9 @@ __device__ __forceinline__ void activate16(const float* a, const float* b, float
   for (int j = 0; j < 16; ++j) h[j] = act_value<ACT>(a[j]) * b[j];
 }
 
-template <int MODE, int CTAS, int BN, int STAGES>
+// SCALED: the results are fp16, times their worker's factor (as a variant: the factor's register costs bf16's weight gradients of
+// 16 workers 2 us of 21).
+template <int MODE, int CTAS, int BN, int STAGES, bool SCALED>
 __global__ void __launch_bounds__(kThreads, 1)
 gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
   constexpr bool A_MN = MODE == DW, B_MN = MODE != FORWARD;
@@ -463,6 +467,8 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
       float* part = g.splits > 1 ? g.parts + (((int64_t)tl.split * g.problems + tl.problem) * g.rows + row0) * g.parts_row : nullptr;
       float* pre = !g.pre ? nullptr : g.pre + (worker * g.rows + row0) * g.parts_row;   // (rows of a and b, as in parts)
       if (MODE == FORWARD && part) pre = part;
+      // (past L1: this kernel may run beside its predecessor)
+      const float unscale = SCALED ? __ldcg(g.unscale + worker) : 1.f;
       if (rows > 0) {
         for (int c0 = half * (kColsOut / 2); c0 < (half + 1) * (kColsOut / 2); c0 += W) {
           const int64_t col = (int64_t)tl.col * kColsOut + c0;
@@ -502,8 +508,8 @@ gated_gemm_kernel(const __grid_constant__ GatedMaps maps, const GatedArgs g) {
             for (int q = 0; q < (part ? 0 : W / 16); q += 2) {
               float v[16], w[16];
               tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
-              out.put(lane, q, v, g.f16);
-              out.put(lane, q + 1, w, g.f16);
+              out.put(lane, q, v, SCALED || g.f16, unscale);
+              out.put(lane, q + 1, w, SCALED || g.f16, unscale);
             }
             if (!part) out.flush(lane, dst + col, g.cols, rows, cols, g.out_width);
           }
@@ -677,6 +683,10 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const GatedArgs g) {
                      : g.act == OLSGD_ACT_GELU ? act_value<OLSGD_ACT_GELU>(a[e])
                      : g.act == OLSGD_ACT_RELU ? act_value<OLSGD_ACT_RELU>(a[e])
                                                : act_value<OLSGD_ACT_SIGMOID>(a[e]));
+  } else if (g.unscale) {
+    const float unscale = g.unscale[MODE == DW ? problem >> 1 : problem];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] *= unscale;
   }
   store_floats<T, 8>(out, c, g.cols, g.out_width == 16, a);
 }
@@ -914,11 +924,13 @@ struct GatedGrad {
   int64_t rows, F, pitch;
   bool vec;                 // rows of dh start on 16-byte boundaries, F is a multiple of 8
   Border border;            // relu
+  float* maxima;            // fp16: the largest value of each CTA [m][CTAs] ...
+  float* unscale;           // ... and one over the factor of each worker's da and db
 };
 
 // One column next to relu's border once more, by a warp; lane `from` stores.
 template <typename T>
-__device__ __forceinline__ void settle(const GatedGrad& g, int64_t worker, int64_t r, int64_t col, bool zero, int from) {
+__device__ __forceinline__ void settle(const GatedGrad& g, int64_t worker, int64_t r, int64_t col, bool zero, int from, float scale) {
   const Border& o = g.border;
   const T* x = static_cast<const T*>(o.x.p) + worker * o.x.worker_stride + r * o.x.row_stride;
   const T* w = static_cast<const T*>(o.wg.p) + worker * o.wg.worker_stride + col * o.wg.row_stride;
@@ -929,21 +941,16 @@ __device__ __forceinline__ void settle(const GatedGrad& g, int64_t worker, int64
     const int64_t wr = worker * g.rows + r;
     const ActPair p = act_pair<OLSGD_ACT_RELU>(exact);
     const float d = Elem<T>::to_float(static_cast<const T*>(g.dh)[worker * g.dh_worker + r * g.dh_row + col]);
-    static_cast<T*>(g.da)[wr * g.pitch + col] = Elem<T>::from_float(d * g.pre[wr * 2 * g.pitch + g.pitch + col] * p.df);
-    static_cast<T*>(g.db)[wr * g.pitch + col] = Elem<T>::from_float(d * p.f);
+    static_cast<T*>(g.da)[wr * g.pitch + col] = Elem<T>::from_float(d * g.pre[wr * 2 * g.pitch + g.pitch + col] * p.df * scale);
+    static_cast<T*>(g.db)[wr * g.pitch + col] = Elem<T>::from_float(d * p.f * scale);
   }
 }
 
-// A warp per stretch of kStretch columns of a row.  (The loads go past L1: the kernel may run beside its predecessor, see
-// launch_gated_backward.)
+// A stretch of kStretch columns of row r, by a warp; da and db times `scale`.  most: the largest of their values (fp16).
+// (The loads go past L1: the kernel may run beside its predecessor, see launch_gated_backward.)
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256, 5) gated_backward_kernel(const __grid_constant__ GatedGrad g, bool beside) {
-  if (!beside) launch_gate();
+__device__ __forceinline__ void form_stretch(const GatedGrad& g, int64_t worker, int64_t r, int64_t j_begin, float scale, float& most) {
   const int lane = threadIdx.x & 31;
-  const int64_t worker = blockIdx.y, stretches = (g.pitch + kStretch - 1) / kStretch;
-  const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int64_t r = at / stretches, j_begin = (at - r * stretches) * kStretch;
-  if (r >= g.rows) return;
   const int64_t wr = worker * g.rows + r;
   float xn = 0.f;
   if constexpr (ACT == OLSGD_ACT_RELU) xn = __ldcg(g.border.xn + wr);
@@ -982,6 +989,13 @@ __global__ void __launch_bounds__(256, 5) gated_backward_kernel(const __grid_con
       const ActPair p = act_pair<ACT>(a[e]);
       va[e] = d[e] * b[e] * p.df;
       vb[e] = d[e] * p.f;
+      if constexpr (std::is_same<T, __half>::value) {
+        // (relu: as if its derivative were 1, as it may turn out to be next to the border)
+        const float u = fabsf(ACT == OLSGD_ACT_RELU ? d[e] * b[e] : va[e]), v = fabsf(vb[e]);
+        most = fmaxf(most, fmaxf(u < INFINITY ? u : 0.f, v < INFINITY ? v : 0.f));
+        va[e] *= scale;
+        vb[e] *= scale;
+      }
     }
     if (live) {
       *reinterpret_cast<uint4*>(static_cast<T*>(g.da) + wr * g.pitch + j) = Elem<T>::pack(va);
@@ -994,12 +1008,64 @@ __global__ void __launch_bounds__(256, 5) gated_backward_kernel(const __grid_con
         const uint32_t zero = __shfl_sync(0xffffffffu, zeros, from);
         for (uint32_t bits = __shfl_sync(0xffffffffu, mask, from); bits; bits &= bits - 1) {
           const int e = __ffs(bits) - 1;
-          settle<T>(g, worker, r, j0 + from * 8 + e, (zero >> e) & 1, from);
+          settle<T>(g, worker, r, j0 + from * 8 + e, (zero >> e) & 1, from, scale);
         }
       }
     }
   }
+}
+
+__device__ __forceinline__ float block_max(float v) {
+  __shared__ float sh[8];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v = fmaxf(v, sh[w]);
+  return v;
+}
+
+// A warp per stretch.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256, 5) gated_backward_kernel(const __grid_constant__ GatedGrad g, bool beside) {
+  if (!beside) launch_gate();
+  const int64_t stretches = (g.pitch + kStretch - 1) / kStretch;
+  const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = at / stretches;
+  float most = 0.f;
+  if (r < g.rows) form_stretch<T, ACT>(g, blockIdx.y, r, (at - r * stretches) * kStretch, 1.f, most);
   if (beside) launch_gate();
+  if constexpr (std::is_same<T, __half>::value) {
+    most = block_max(most);
+    if (threadIdx.x == 0) g.maxima[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = most;
+  }
+}
+
+// fp16 ends at 65504 and 2^-24, where the sums over F and T that follow would still be values.  The largest value of a worker's
+// da and db decides: from 2^-4 to 2^15 they stay as they are (what is below 2^-14, rounded to steps of 2^-24, is off by
+// 2^-21 of the largest then).  Otherwise they are formed again times the power of two that brings the largest to
+// [2^14, 2^15): 29 binary orders below it keep all their bits, and the products are scaled back in fp32 before they are
+// rounded.  A backward pass takes 4 to 8 us longer for it with nothing to scale (16 workers, 128 tokens, 1024 -> 1024: 44.0 ->
+// 48.5 us; 3 workers, 333 tokens, 1021 -> 2035: 55.5 -> 63), and 53 and 70 us where everything is scaled.
+__device__ __forceinline__ float scale_for(float most) {
+  if (most == 0.f || (most >= 0.0625f && most < 32768.f)) return 1.f;
+  const int k = 14 - ((int)(__float_as_uint(most) >> 23) - 127);
+  return __uint_as_float((uint32_t)(127 + (k < 120 ? k : 120)) << 23);
+}
+template <int ACT>
+__global__ void __launch_bounds__(256, 5) gated_rescale_kernel(const __grid_constant__ GatedGrad g, int64_t maxima) {
+  launch_gate();
+  const int64_t worker = blockIdx.y, stretches = (g.pitch + kStretch - 1) / kStretch;
+  float most = 0.f;
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < maxima; i += 256) most = fmaxf(most, g.maxima[worker * maxima + i]);
+  const float scale = scale_for(block_max(most));
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.unscale[worker] = 1.f / scale;
+  if (scale == 1.f) return;
+  for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < g.rows * stretches; at += (int64_t)gridDim.x * 8) {
+    const int64_t r = at / stretches;
+    form_stretch<__half, ACT>(g, worker, r, (at - r * stretches) * kStretch, scale, most);
+  }
 }
 
 // --------------------------------------------------------------------------------- host
@@ -1021,14 +1087,14 @@ bool make_map16(CUtensorMap* map, const GatedOperand& o, int64_t cols, int64_t r
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, int CTAS, int BN, int STAGES>
+template <int MODE, int CTAS, int BN, int STAGES, bool SCALED>
 cudaError_t launch_variant(const GatedMaps& maps, GatedArgs g, cudaStream_t s) {
   constexpr int kColsOut = MODE == FORWARD ? BN / 2 : BN;
   constexpr size_t smem = (size_t)STAGES * (kBM * kBK * 2 + BN / CTAS * kBK * 2) +
                           kEpiWarps * 4096 + sizeof(Control<STAGES>) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   static PerDeviceSmem configured;
-  auto kern = gated_gemm_kernel<MODE, CTAS, BN, STAGES>;
+  auto kern = gated_gemm_kernel<MODE, CTAS, BN, STAGES, SCALED>;
   cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
   if (e != cudaSuccess) return e;
   g.row_tiles = (g.rows + CTAS * kBM - 1) / (CTAS * kBM);
@@ -1128,12 +1194,18 @@ GatedArgs args_for(const GatedShape& d, const Shape& sh, uint8_t* parts) {
   return g;
 }
 
+template <int MODE, bool SCALED>
+cudaError_t launch_shape(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
+  return sh.bn == 64    ? launch_variant<MODE, 1, 64, 8, SCALED>(maps, g, s)
+         : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6, SCALED>(maps, g, s)
+         : sh.ctas == 2 ? launch_variant<MODE, 2, 256, 6, SCALED>(maps, g, s)
+                        : launch_variant<MODE, 1, 256, 4, SCALED>(maps, g, s);
+}
 template <int MODE>
 cudaError_t launch_product(const Shape& sh, const GatedMaps& maps, const GatedArgs& g, cudaStream_t s) {
-  return sh.bn == 64    ? launch_variant<MODE, 1, 64, 8>(maps, g, s)
-         : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6>(maps, g, s)
-         : sh.ctas == 2 ? launch_variant<MODE, 2, 256, 6>(maps, g, s)
-                        : launch_variant<MODE, 1, 256, 4>(maps, g, s);
+  if constexpr (MODE != FORWARD)
+    if (g.unscale) return launch_shape<MODE, true>(sh, maps, g, s);
+  return launch_shape<MODE, false>(sh, maps, g, s);
 }
 // Where K was cut: the joining launch.
 template <int MODE>
@@ -1195,18 +1267,35 @@ cudaError_t row_norms(const GatedBackward& a, int64_t pitch, float* xn, float* w
                         xn, wn, pitch);
 }
 
+int64_t elementwise_ctas(int64_t T, int64_t pitch) { return (T * ((pitch + kStretch - 1) / kStretch) + 7) / 8; }
+
 template <typename T>
-cudaError_t elementwise(const GatedBackward& a, int64_t pitch, void* da, void* db, const float* xn, const float* wn, bool beside,
-                        cudaStream_t s) {
-  const int64_t warps = a.T * ((pitch + kStretch - 1) / kStretch);
-  const dim3 grid((unsigned)((warps + 7) / 8), (unsigned)a.m);
-  GatedGrad g{a.dh.p, a.dh.worker_stride, a.dh.row_stride, a.pre, da, db, a.T, a.F, pitch, a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m),
-              Border{a.x, a.wg, a.D, a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m), (8.f + (float)a.D / 128) / (1 << 23), xn, wn}};
+cudaError_t elementwise(const GatedBackward& a, GatedGrad g, bool beside, cudaStream_t s) {
+  const int64_t ctas = elementwise_ctas(a.T, g.pitch);
+  g.dh = a.dh.p;
+  g.dh_worker = a.dh.worker_stride;
+  g.dh_row = a.dh.row_stride;
+  g.pre = a.pre;
+  g.rows = a.T;
+  g.F = a.F;
+  g.vec = a.F % 8 == 0 && tma_ready(a.dh, a.T, a.m);
+  g.border.x = a.x;
+  g.border.wg = a.wg;
+  g.border.D = a.D;
+  g.border.vec = a.D % 8 == 0 && tma_ready(a.x, a.T, a.m) && tma_ready(a.wg, a.F, a.m);
+  g.border.bound = (8.f + (float)a.D / 128) / (1 << 23);
   auto k = a.act == OLSGD_ACT_SILU   ? gated_backward_kernel<T, OLSGD_ACT_SILU>
            : a.act == OLSGD_ACT_GELU ? gated_backward_kernel<T, OLSGD_ACT_GELU>
            : a.act == OLSGD_ACT_RELU ? gated_backward_kernel<T, OLSGD_ACT_RELU>
                                      : gated_backward_kernel<T, OLSGD_ACT_SIGMOID>;
-  return launch_chained(k, grid, dim3(256), 0, s, g, beside);
+  const cudaError_t e = launch_chained(k, dim3((unsigned)ctas, (unsigned)a.m), dim3(256), 0, s, g, beside);
+  if (e != cudaSuccess || !std::is_same<T, __half>::value) return e;
+  auto again = a.act == OLSGD_ACT_SILU   ? gated_rescale_kernel<OLSGD_ACT_SILU>
+               : a.act == OLSGD_ACT_GELU ? gated_rescale_kernel<OLSGD_ACT_GELU>
+               : a.act == OLSGD_ACT_RELU ? gated_rescale_kernel<OLSGD_ACT_RELU>
+                                         : gated_rescale_kernel<OLSGD_ACT_SIGMOID>;
+  const int64_t room = 4 * kSms / a.m < 1 ? 1 : 4 * kSms / a.m;   // every CTA reads its worker's maxima
+  return launch_chained(again, dim3((unsigned)(ctas < room ? ctas : room), (unsigned)a.m), dim3(256), 0, s, g, ctas);
 }
 
 template <typename T>
@@ -1226,10 +1315,11 @@ cudaError_t few(const GatedForward& a, cudaStream_t s) {
 
 }  // namespace
 
-// The workspace: copies of operands that TMA cannot take, then (backward) da and db and the norms of the rows of x and
-// w_gate, then the parts of the products (backward: dx, then the weights' gradients, which run side by side).
+// The workspace: copies of operands that TMA cannot take, then (backward) da and db, the norms of the rows of x and w_gate,
+// the largest values and the factors, then the parts of the products (backward: dx, then the weights' gradients, which run
+// side by side).
 struct Workspace {
-  size_t da, db, xn, wn, parts, parts_dw, total;
+  size_t da, db, xn, wn, maxima, unscale, parts, parts_dw, total;
 };
 Workspace layout(const GatedShape& d, bool backward, bool copies) {
   Workspace w{};
@@ -1238,7 +1328,9 @@ Workspace layout(const GatedShape& d, bool backward, bool copies) {
   w.db = w.da + part;
   w.xn = w.db + part;
   w.wn = w.xn + (backward ? round256((size_t)d.m * d.T * sizeof(float)) : 0);
-  w.parts = w.wn + (backward ? round256((size_t)d.m * round8(d.F) * sizeof(float)) : 0);
+  w.maxima = w.wn + (backward ? round256((size_t)d.m * round8(d.F) * sizeof(float)) : 0);
+  w.unscale = w.maxima + (backward ? round256((size_t)d.m * elementwise_ctas(d.T, round8(d.F)) * sizeof(float)) : 0);
+  w.parts = w.unscale + (backward ? round256((size_t)d.m * sizeof(float)) : 0);
   w.parts_dw = w.parts + (backward ? round256(parts_bytes<DX>(d)) : 0);
   w.total = w.parts_dw + (backward ? parts_bytes<DW>(d) : parts_bytes<FORWARD>(d));
   return w;
@@ -1286,13 +1378,20 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
   // does below), on the operands as they were given.  3 workers, 333 tokens, 1021 -> 2035: backward 56.5 -> 54.9 us; one
   // worker, 40 tokens, 333 -> 1003: 12.7 -> 11.9.  relu's norms come ahead of both.
   const GatedBackward given = a;
-  float *xn = reinterpret_cast<float*>(ws + at.xn), *wn = reinterpret_cast<float*>(ws + at.wn);
+  const auto floats = [&](size_t offset) { return reinterpret_cast<float*>(ws + offset); };
   if (a.act == OLSGD_ACT_RELU)
-    OLSGD_STEP(a.f16 ? row_norms<__half>(a, pitch, xn, wn, s) : row_norms<__nv_bfloat16>(a, pitch, xn, wn, s));
+    OLSGD_STEP(a.f16 ? row_norms<__half>(a, pitch, floats(at.xn), floats(at.wn), s) : row_norms<__nv_bfloat16>(a, pitch, floats(at.xn), floats(at.wn), s));
   bool copies = false;
   OLSGD_STEP(make_ready(wanted + from, to - from, a.D, a.m, ws, s, &copies));
-  OLSGD_STEP(a.f16 ? elementwise<__half>(given, pitch, da, db, xn, wn, copies, s)
-                   : elementwise<__nv_bfloat16>(given, pitch, da, db, xn, wn, copies, s));
+  GatedGrad grad{};
+  grad.da = da;
+  grad.db = db;
+  grad.pitch = pitch;
+  grad.border.xn = floats(at.xn);
+  grad.border.wn = floats(at.wn);
+  grad.maxima = floats(at.maxima);
+  grad.unscale = floats(at.unscale);
+  OLSGD_STEP(a.f16 ? elementwise<__half>(given, grad, copies, s) : elementwise<__nv_bfloat16>(given, grad, copies, s));
   const GatedOperand oa{da, a.T * pitch, pitch}, ob{db, a.T * pitch, pitch};
   // Both products read what the element-wise kernel has written, and neither what the other writes.  The
   // second one is launched beside the first: its CTAs may start once all of the first one's have
@@ -1305,6 +1404,7 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
     dx = args_for<DX>(a, sh, ws + at.parts);
     dx.out_width = store_width(a.dx, a.D);
     dx.out0 = a.dx;
+    dx.unscale = a.f16 ? grad.unscale : nullptr;
     dx.a_rows = loaded_rows(a.T);
     GatedMaps maps;
     if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, dx.a_rows, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, dx.a_rows, a.f16) ||
@@ -1320,6 +1420,7 @@ cudaError_t launch_gated_backward(GatedBackward a, cudaStream_t s) {
     dw.out_width = w0 < w1 ? w0 : w1;
     dw.out0 = a.dwg;
     dw.out1 = a.dwu;
+    dw.unscale = a.f16 ? grad.unscale : nullptr;
     GatedMaps maps;
     if (!make_map16(&maps.a0, oa, a.F, a.T, a.m, kBK, a.f16) || !make_map16(&maps.a1, ob, a.F, a.T, a.m, kBK, a.f16) ||
         !make_map16(&maps.b0, a.x, a.D, a.T, a.m, kBK, a.f16))

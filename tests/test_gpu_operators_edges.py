@@ -2,6 +2,8 @@
 ends of a type's range, and data whose cost must not depend on its values.
 
 Tolerances count roundings, as in test_gpu_operators.py."""
+import math
+
 import pytest
 import torch
 
@@ -84,8 +86,8 @@ def test_relu_border_goes_by_the_feature_s_own_size(F, features, how, D, dtype):
     assert bool(((dx[0, 2].double() - want).abs() <= size * (2 * eps + _product_error(2 * F)) + below).all())
 
 
-@pytest.mark.parametrize("data,dtype", [(d, t) for d in ("zero features", "zero tokens", "integers", "one element", "large", "small")
-                                        for t in (torch.bfloat16, torch.float16) if (d, t) != ("large", torch.float16)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("data", ["zero features", "zero tokens", "integers", "one element", "large", "small"])
 def test_relu_gradient_of_exact_zeros(data, dtype):
     """Data whose gates are exactly 0, or whose rows' norms are at the ends of fp32: against the definition in 64 bits."""
     g = _gen(7)
@@ -112,15 +114,16 @@ def test_relu_gradient_of_exact_zeros(data, dtype):
     dx, dwg, _ = lib.gated_backward(dh, x, wg, wu, pre, "relu")
     da, db = E * b * (a > 0), E * a.clamp(min=0)
     ea, eb = (_product_error(D) * (x.double().abs() @ w.double().abs().mT) for w in (wg, wu))
-    eda, edb = E.abs() * eb + da.abs() * (half + 4 * U) + 2.0 ** -24, E.abs() * ea + db.abs() * (half + 4 * U) + 2.0 ** -24
-    if dtype == torch.bfloat16:
-        eda, edb = eda - 2.0 ** -24, edb - 2.0 ** -24
+    # fp16's steps below its normal range: 2^-24, or 2^-38 of a worker's largest value where that is beyond 2^15
+    step = torch.maximum(da.abs().amax(dim=(1, 2)), db.abs().amax(dim=(1, 2))).mul(2.0 ** -38).clamp(min=2.0 ** -24)[:, None, None]
+    step = step if dtype == torch.float16 else 0.0
+    eda, edb = E.abs() * eb + da.abs() * (half + 4 * U) + step, E.abs() * ea + db.abs() * (half + 4 * U) + step
     wants = ((dx, da @ wg.double() + db @ wu.double(), eda @ wg.double().abs() + edb @ wu.double().abs(), da.abs() @ wg.double().abs() + db.abs() @ wu.double().abs(), 2 * F),
              (dwg, da.mT @ x.double(), eda.mT @ x.double().abs(), da.abs().mT @ x.double().abs(), T))
     for got, want, err, size, K in wants:
         tol = err * 1.01 + _product_error(K) * (size + err) + want.abs() * half * 1.01 + (2.0 ** -24 if dtype == torch.float16 else 2.0 ** -126)
-        finite = want.abs() < torch.finfo(dtype).max
-        assert bool((((got.double() - want).abs() <= tol) | ~finite).all())
+        there = want.abs() + tol < torch.finfo(dtype).max   # (what comes closer to the largest may be rounded to infinity)
+        assert bool((((got.double() - want).abs() <= tol) | ~there).all())
 
 
 def test_relu_gradient_costs_the_same_whatever_the_zeros():
@@ -143,3 +146,96 @@ def test_relu_gradient_costs_the_same_whatever_the_zeros():
     times = {"zero features": cost(x, zero_w), "zero tokens": cost(zero_x, wg),
              "integers": cost(torch.sign(x) * some(x), torch.sign(wg) * some(wg))}
     assert all(t <= 1.5 * random + 5 for t in times.values()), (random, times)
+
+
+# ------------------------------------------------------------------- the range of fp16
+
+def _activation_64(kind, a):
+    if kind == "sigmoid":
+        return torch.sigmoid(a), torch.sigmoid(a) * torch.sigmoid(-a)
+    if kind == "relu":
+        return a.clamp(min=0.0), (a > 0).double()
+    return a * torch.sigmoid(a), torch.sigmoid(a) * (1 + a * torch.sigmoid(-a))
+
+
+def _check_fp16_gradients(x, wg, wu, dh, kind):
+    X, G, Up, E = x.double(), wg.double(), wu.double(), dh.double()
+    T, D, F = X.shape[1], X.shape[2], G.shape[1]
+    half = 2.0 ** -11
+    a, b = X @ G.mT, X @ Up.mT
+    f, df = _activation_64(kind, a)
+    ea, eb = _product_error(D) * (X.abs() @ G.abs().mT), _product_error(D) * (X.abs() @ Up.abs().mT)
+    da, db = E * b * df, E * f
+    # act' <= 1.1, act'' <= 0.5; the device's exponential and division: 8 steps
+    edf = (a.abs() < ea).double() if kind == "relu" else 0.5 * ea + 16 * U * (1 + a.abs())
+    most = torch.maximum(da.abs().amax(dim=(1, 2)), db.abs().amax(dim=(1, 2)))[:, None, None]
+    # unscaled, the least step is 2^-24; scaled, the largest is 2^14 or more, so that it is 2^-38 of that (half of it is lost at most)
+    step = torch.where((most >= 2.0 ** -4) & (most < 2.0 ** 15), torch.full_like(most, 2.0 ** -25), most * 2.0 ** -39) * 1.01
+    eda = E.abs() * (b.abs() * edf + df * eb + edf * eb) + (half + 4 * U) * da.abs() + step
+    edb = E.abs() * (1.1 * ea + 8 * U * (f.abs() + a.abs())) + (half + 4 * U) * db.abs() + step
+    _, pre = lib.gated_forward(x, wg, wu, kind, save=True)
+    got = lib.gated_backward(dh, x, wg, wu, pre, kind)
+    sums = ((da @ G + db @ Up, eda @ G.abs() + edb @ Up.abs(), da.abs() @ G.abs() + db.abs() @ Up.abs(), 2 * F),
+            (da.mT @ X, eda.mT @ X.abs(), da.abs().mT @ X.abs(), T), (db.mT @ X, edb.mT @ X.abs(), db.abs().mT @ X.abs(), T))
+    for g, (want, err, size, K) in zip(got, sums):
+        tol = err * 1.01 + _product_error(K) * (size + err) + half * want.abs() * 1.01 + 2.0 ** -25
+        there = want.abs() + tol < 65504   # what the result's own type holds
+        assert bool((((g.double() - want).abs() <= tol) | ~there).all()) and float(there.double().mean()) > 0.7
+    return most.flatten().tolist(), got
+
+
+@pytest.mark.parametrize("kind", ["silu", "relu", "sigmoid"])
+@pytest.mark.parametrize("T,D,F", [(40, 333, 203), (300, 128, 1024), (4096, 64, 64), (130, 2048, 72), (2, 64, 40), (600, 1024, 520)])
+def test_fp16_gradients_whose_intermediates_leave_the_type_s_range(T, D, F, kind):
+    """Workers whose da and db lie below fp16's normal range, in it, and above it: each is scaled by itself."""
+    g = _gen(T + D + F)
+    m, dtype = 4, torch.float16
+    x, wg, wu, dh = _randn(g, (m, T, D)), _randn(g, (m, F, D), std=D ** -0.5), _randn(g, (m, F, D), std=D ** -0.5), _randn(g, (m, T, F))
+    dh[0] *= 2.0 ** -19          # a few of fp16's least steps ...
+    wu[0] *= 2.0 ** -6           # ... times a small factor
+    wg[0] *= 2.0 ** -6
+    x[1], wu[1], wg[1], dh[1] = x[1] * 2.0 ** -9, wu[1] * 2.0 ** 15, wg[1] * 2.0 ** -8, dh[1] * 2.0 ** 12   # above: 2^18
+    if kind == "sigmoid":
+        wu[1] *= 2.0 ** -8       # (db wu is no larger than da wg)
+        x[1] *= 2.0 ** 2
+    dh[3] = 0.0
+    x, wg, wu, dh = (t.to(dtype) for t in (x, wg, wu, dh))
+    most, got = _check_fp16_gradients(x, wg, wu, dh, kind)
+    assert most[0] < 2.0 ** -14 and most[3] == 0.0
+    if kind != "sigmoid":
+        assert most[1] > 65504
+    assert all(not bool(t[3].any()) for t in got) and bool(got[1][0].any()) and bool(got[2][0].any())
+    # a worker's bits do not depend on the others (the same launches, with every other worker an ordinary one)
+    for i in (0, 2):
+        rest = [torch.stack([t[i if j == i else 2] for j in range(m)]) for t in (x, wg, wu, dh)]
+        _, pre = lib.gated_forward(*rest[:3], kind, save=True)
+        for u, v in zip(lib.gated_backward(rest[3], *rest[:3], pre, kind), got):
+            assert torch.equal(u[i], v[i])
+
+
+def test_fp16_weight_gradients_of_many_tokens_of_small_gradients():
+    """d_h of 2^-22 times a factor of 2^-8: nothing in fp16, 2^-18 in a sum over 4096 tokens."""
+    dtype, (T, D, F) = torch.float16, (4096, 64, 64)
+    x, wg = torch.ones((1, T, D), dtype=dtype, device="cuda"), torch.zeros((1, F, D), dtype=dtype, device="cuda")
+    wu, dh = torch.full((1, F, D), 2.0 ** -12, dtype=dtype, device="cuda"), torch.full((1, T, F), 2.0 ** -22, dtype=dtype, device="cuda")
+    _, pre = lib.gated_forward(x, wg, wu, "sigmoid", save=True)
+    dx, dwg, dwu = lib.gated_backward(dh, x, wg, wu, pre, "sigmoid")   # act(0) = 1/2, act'(0) = 1/4, b = 2^-6
+    assert bool((dwg == 2.0 ** (12 - 22 - 6 - 2)).all()) and bool((dwu == 2.0 ** (12 - 22 - 1)).all())
+
+
+def test_fp16_gradients_with_infinities_keep_to_their_rows():
+    """A token of infinities does not decide the others' factor."""
+    g = _gen(9)
+    dtype = torch.float16
+    x, wg, wu = _randn(g, (1, 40, 64), dtype), _randn(g, (1, 48, 64), dtype, 0.125), _randn(g, (1, 48, 64), dtype, 0.125)
+    for std in (1.0, 2.0 ** -19):
+        dh = _randn(g, (1, 40, 48), dtype, std)
+        bad = dh.clone()
+        bad[0, 5], bad[0, 9, 3] = math.inf, math.nan
+        for kind in ("silu", "relu"):
+            _, pre = lib.gated_forward(x, wg, wu, kind, save=True)
+            want = lib.gated_backward(dh, x, wg, wu, pre, kind)[0]
+            got = lib.gated_backward(bad, x, wg, wu, pre, kind)[0]
+            keep = [i for i in range(40) if i not in (5, 9)]
+            assert torch.allclose(got[0, keep].float(), want[0, keep].float(), rtol=2.0 ** -9, atol=2.0 ** -23)
+            assert bool(torch.isnan(got[0, 9]).all()) and not bool(torch.isfinite(got[0, 5]).any())
