@@ -121,8 +121,10 @@ __device__ __forceinline__ ActPair act_pair(float a) {
     r.f = a > 0.f ? a : (a != a ? a : 0.f);
     r.df = a > 0.f ? 1.f : (a != a ? a : 0.f);
   } else if (ACT == OLSGD_ACT_SIGMOID) {
-    r.f = sigmoid_of(a);
-    r.df = r.f * (1.f - r.f);
+    // e^-|a| and 1 / (1 + e^-|a|) give f and 1 - f, whichever is small, without a difference
+    const float e = ex2(-kLog2e * fabsf(a)), q = __fdividef(1.f, 1.f + e);
+    r.f = a < 0.f ? e * q : q;
+    r.df = e * q * q;
   } else if (ACT == OLSGD_ACT_SILU) {
     const float s = sigmoid_of(a);
     r.f = s == 0.f ? 0.f : a * s;

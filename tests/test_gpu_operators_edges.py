@@ -239,3 +239,25 @@ def test_fp16_gradients_with_infinities_keep_to_their_rows():
             keep = [i for i in range(40) if i not in (5, 9)]
             assert torch.allclose(got[0, keep].float(), want[0, keep].float(), rtol=2.0 ** -9, atol=2.0 ** -23)
             assert bool(torch.isnan(got[0, 9]).all()) and not bool(torch.isfinite(got[0, 5]).any())
+
+
+# ---------------------------------------------------------------------- saturated gates
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("tokens", [1, 3])
+def test_sigmoid_gradient_of_saturated_gates(tokens, dtype):
+    """act'(a) = e^-|a| / (1 + e^-|a|)^2 keeps its digits on both sides: relative to itself, not to 1."""
+    a = torch.cat([torch.arange(-20, 21, device="cuda") * 0.75, torch.tensor([16.0, 17.0], device="cuda")]).to(dtype)
+    F = len(a)
+    x, wg, wu = torch.zeros((1, tokens, 8), dtype=dtype, device="cuda"), torch.zeros((1, F, 8), dtype=dtype, device="cuda"), torch.zeros((1, F, 8), dtype=dtype, device="cuda")
+    x[0, -1, 0], wg[0, :, 0], wu[0, :, 0] = 1.0, a, 1.0
+    dh = torch.full((1, tokens, F), 2.0 ** 12, dtype=dtype, device="cuda")
+    _, pre = lib.gated_forward(x, wg, wu, "sigmoid", save=True)
+    _, dwg, dwu = lib.gated_backward(dh, x, wg, wu, pre, "sigmoid")
+    d = a.double()
+    want_g, want_u = 2.0 ** 12 * torch.sigmoid(d) * torch.sigmoid(-d), 2.0 ** 12 * torch.sigmoid(d)
+    # rounded to the type twice; the exponent |a| log2 e < 32 is rounded twice (32 u ln 2 each), the power of two and the quotient
+    # have 2 steps each, three products one
+    tol = torch.finfo(dtype).eps * 1.01 + 60 * U
+    assert bool(((dwg[0, :, 0].double() - want_g).abs() <= want_g * tol + 2.0 ** -25).all())
+    assert bool(((dwu[0, :, 0].double() - want_u).abs() <= want_u * tol + 2.0 ** -25).all())
