@@ -215,6 +215,9 @@ olsgd_status olsgd_selftest_per_device_table(void);
  * zero column) come from the caller.
  *   g_device  float32 [m][P], device, row stride P; read on the main stream */
 olsgd_status olsgd_local_step_with_grads(olsgd_ctx* ctx, const float* g_device);
+/* What olsgd_local_step_with_grads would refuse now, without doing anything: OLSGD_OK if it would
+ * take g_device.  For callers that change the gradient in place first (olsgd_clip_grads).    */
+olsgd_status olsgd_check_local_step_with_grads(olsgd_ctx* ctx, const float* g_device);
 
 /* Anchor refresh at the end of a period: Eq. 5 (beta = 0) or Eq. 10-11, as a
  * reduction over the worker dimension launched on the side stream after the

@@ -63,6 +63,7 @@ def load_library():
                              C.POINTER(_Data), vp, vp, C.c_size_t, vp, vp]),
         "olsgd_local_step": (i32, [vp, vp]),
         "olsgd_local_step_with_grads": (i32, [vp, vp]),
+        "olsgd_check_local_step_with_grads": (i32, [vp, vp]),
         "olsgd_local_step_host": (i32, [vp, vp, vp, vp]),
         "olsgd_local_step_host_bf16": (i32, [vp, vp, vp, vp]),
         "olsgd_join": (i32, [vp]),
@@ -209,12 +210,14 @@ class OverlapLocalSGD:
 
     def local_step_with_grads(self, g, max_norm=None):
         """g: float32 [m][P].  With max_norm each worker's gradient is clipped to that norm first, in place
-        (olsgd_clip_grads on the context's main stream); returns the norms before clipping, float32 [m]."""
+        (olsgd_clip_grads on the context's main stream); returns the norms before clipping, float32 [m].  A step that is
+        refused leaves g as it was."""
         assert g.is_cuda and g.dtype == torch.float32 and g.is_contiguous()
         assert g.numel() == self.m * self.P
         norms = None
         if max_norm is not None:
             from .operators import clip_grads
+            _check(self.lib, self.lib.olsgd_check_local_step_with_grads(self.ctx, g.data_ptr()), self.ctx)
             rows = g.view(self.m, self.P)
             with torch.cuda.stream(self.main):
                 norms = clip_grads(rows, max_norm, out=rows)[1]

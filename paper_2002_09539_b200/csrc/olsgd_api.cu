@@ -709,7 +709,7 @@ olsgd_status olsgd_init(olsgd_ctx** out, const olsgd_model_spec* spec, const ols
   return OLSGD_OK;
 }
 
-olsgd_status olsgd_local_step_with_grads(olsgd_ctx* c, const float* g_device) {
+olsgd_status olsgd_check_local_step_with_grads(olsgd_ctx* c, const float* g_device) {
   if (!c) return fail(nullptr, OLSGD_EINVAL, "ctx is NULL");
   OLSGD_ON_DEVICE(c);
   if (c->spec.kind != OLSGD_FLAT)
@@ -717,6 +717,12 @@ olsgd_status olsgd_local_step_with_grads(olsgd_ctx* c, const float* g_device) {
   if (!g_device || (reinterpret_cast<uintptr_t>(g_device) & 3))
     return fail(c, OLSGD_EINVAL, "g_device must be non-null and 4-byte aligned");
   if (c->need_sync) return fail(c, OLSGD_ESTATE, "a period ended: call olsgd_period_sync first");
+  return OLSGD_OK;
+}
+
+olsgd_status olsgd_local_step_with_grads(olsgd_ctx* c, const float* g_device) {
+  const olsgd_status st = olsgd_check_local_step_with_grads(c, g_device);
+  if (st != OLSGD_OK) return st;
   return apply_update(c, g_device, c->P);
 }
 

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2002_09539_b200 as lib
+from paper_2002_09539_b200 import OverlapLocalSGD
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -261,3 +262,39 @@ def test_sigmoid_gradient_of_saturated_gates(tokens, dtype):
     tol = torch.finfo(dtype).eps * 1.01 + 60 * U
     assert bool(((dwg[0, :, 0].double() - want_g).abs() <= want_g * tol + 2.0 ** -25).all())
     assert bool(((dwu[0, :, 0].double() - want_u).abs() <= want_u * tol + 2.0 ** -25).all())
+
+
+# --------------------------------------------------------------- clipping in the local step
+
+def test_a_refused_local_step_leaves_the_gradient_as_it_was():
+    g = _gen(5)
+    m, P = 3, 1003
+    grad = _randn(g, (m, P))
+    want = grad.double().norm(dim=1)
+    opt = OverlapLocalSGD("flat", flat_P=P, m=m, tau=1, gamma=0.1, alpha=0.5, x0=torch.zeros(P, device="cuda"))
+    h = grad.clone()
+    opt.local_step_with_grads(h)              # the period ends
+    params = opt.get_params(0).copy()
+    with pytest.raises(lib.OlsgdError, match="period"):
+        opt.local_step_with_grads(h, max_norm=0.5)
+    for norm in (0.0, math.nan):
+        with pytest.raises(lib.OlsgdError):
+            opt.local_step_with_grads(h, max_norm=norm)
+    torch.cuda.synchronize()
+    assert torch.equal(h, grad) and (opt.get_params(0) == params).all()
+    opt.period_sync()
+    norms = opt.local_step_with_grads(h, max_norm=0.5)
+    torch.cuda.synchronize()
+    assert bool(((norms.double() - want).abs() <= 4 * U * want).all())   # of the gradient itself, not of a clipped one
+    assert bool((h.double().norm(dim=1) <= 0.5 * (1 + 1e-5)).all())
+    opt.close()
+    # a context that takes no gradients
+    X, y = torch.zeros((2, 8, 4), device="cuda"), torch.zeros((2, 8), device="cuda")
+    opt = OverlapLocalSGD("linreg", dims=(4,), m=2, batch=2, tau=4, gamma=0.1, alpha=0.5, X=X, y=y, x0=torch.zeros(4, device="cuda"))
+    h = _randn(g, (2, opt.P))
+    keep = h.clone()
+    with pytest.raises(lib.OlsgdError, match="FLAT"):
+        opt.local_step_with_grads(h, max_norm=0.1)
+    torch.cuda.synchronize()
+    assert torch.equal(h, keep)
+    opt.close()
