@@ -210,8 +210,8 @@ class OverlapLocalSGD:
 
     def local_step_with_grads(self, g, max_norm=None):
         """g: float32 [m][P].  With max_norm each worker's gradient is clipped to that norm first, in place
-        (olsgd_clip_grads on the context's main stream); returns the norms before clipping, float32 [m].  A step that is
-        refused leaves g as it was."""
+        (olsgd_clip_grads on the context's main stream, which must be ordered behind what wrote g); returns the norms
+        before clipping, float32 [m], ready on the current stream.  A step that is refused leaves g as it was."""
         assert g.is_cuda and g.dtype == torch.float32 and g.is_contiguous()
         assert g.numel() == self.m * self.P
         norms = None
@@ -221,6 +221,10 @@ class OverlapLocalSGD:
             rows = g.view(self.m, self.P)
             with torch.cuda.stream(self.main):
                 norms = clip_grads(rows, max_norm, out=rows)[1]
+            here = torch.cuda.current_stream(g.device)
+            if here != self.main:
+                here.wait_stream(self.main)   # the norms come from there
+                norms.record_stream(here)
         _check(self.lib, self.lib.olsgd_local_step_with_grads(self.ctx, g.data_ptr()), self.ctx)
         return norms
 

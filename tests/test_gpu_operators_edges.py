@@ -298,3 +298,30 @@ def test_a_refused_local_step_leaves_the_gradient_as_it_was():
     torch.cuda.synchronize()
     assert torch.equal(h, keep)
     opt.close()
+
+
+def test_norms_are_ready_on_the_caller_s_stream():
+    """The context works on its own stream, which is busy; the norms are read on another one at once."""
+    g = _gen(6)
+    m, P = 3, 1003
+    grad = _randn(g, (m, P))
+    want = lib.clip_grads(grad, 1.0)[1]
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(main):
+        opt = OverlapLocalSGD("flat", flat_P=P, m=m, tau=8, gamma=0.1, alpha=0.5, x0=torch.zeros(P, device="cuda"))
+        busy = torch.eye(4096, device="cuda")
+        opt.local_step_with_grads(grad.clone(), max_norm=1.0)   # (everything is loaded by now)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(main):
+            h = grad.clone()
+            torch.full((m,), math.nan, device="cuda")           # what the norms' memory holds
+            for _ in range(20):
+                busy = busy @ busy
+        with torch.cuda.stream(side):
+            norms = opt.local_step_with_grads(h, max_norm=1.0)
+            got = norms * 1.0
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+    opt.close()
