@@ -225,8 +225,11 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
                                   size_t workspace_bytes, void* stream) {
   OLSGD_TRY(check_gated(m, T, D, F));
   OLSGD_TRY(check_gated_kind(dtype, activation));
+  OLSGD_REFUSE_IF((d_w_gate == nullptr) != (d_w_up == nullptr), "d_w_gate and d_w_up are wanted both or neither");
+  OLSGD_REFUSE_IF((d_x && !aligned_to(d_x, 2)) || (d_w_gate && (!aligned_to(d_w_gate, 2) || !aligned_to(d_w_up, 2))),
+                  "d_x, d_w_gate and d_w_up must be 2-byte aligned");
   if (T == 0) {   // no tokens: the weights' gradients are zero
-    if (!d_w_gate || !d_w_up) return OLSGD_OK;
+    if (!d_w_gate) return OLSGD_OK;
     const size_t bytes = (size_t)m * F * D * 2;
     OLSGD_TRY(launched(cudaMemsetAsync(d_w_gate, 0, bytes, static_cast<cudaStream_t>(stream)), "olsgd_gated_backward"));
     return launched(cudaMemsetAsync(d_w_up, 0, bytes, static_cast<cudaStream_t>(stream)), "olsgd_gated_backward");
@@ -242,9 +245,6 @@ olsgd_status olsgd_gated_backward(int32_t m, int64_t T, int64_t D, int64_t F, in
   OLSGD_TRY(check_operand(a.wg, "w_gate", m, F, D));
   OLSGD_TRY(check_operand(a.wu, "w_up", m, F, D));
   OLSGD_REFUSE_IF(!aligned_to(pre, 32), "pre must be non-null and 32-byte aligned");
-  OLSGD_REFUSE_IF((d_w_gate == nullptr) != (d_w_up == nullptr), "d_w_gate and d_w_up are wanted both or neither");
-  OLSGD_REFUSE_IF((d_x && !aligned_to(d_x, 2)) || (d_w_gate && (!aligned_to(d_w_gate, 2) || !aligned_to(d_w_up, 2))),
-                  "d_x, d_w_gate and d_w_up must be 2-byte aligned");
   if (!d_x && !d_w_gate) return OLSGD_OK;
   a.pre = pre;
   a.dx = d_x;
