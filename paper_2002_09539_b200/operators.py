@@ -6,7 +6,8 @@ carry the worker dimension first.  Every call runs on the current stream of its 
 device, allocates its outputs and workspace with torch (so it may be captured into a CUDA
 graph), and returns without waiting.  Tensors that live on another stream are the caller's to
 order, as with any torch operation.  Forward and backward are separate calls; nothing is kept
-between them but what the caller passes on.
+between them but what the caller passes on.  They record no graph: tensors that require
+gradients are refused while torch records (detach them, or call under torch.no_grad()).
 """
 import ctypes as C
 import functools
@@ -62,6 +63,13 @@ def _refuse(text, *args):
 def _need(ok, text, *args):
     if not ok:
         _refuse(text, *args)
+
+
+def _recorded(*tensors):
+    """Refuses tensors whose gradients would be lost without a word."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            _refuse("the operators record no graph: detach tensors that require gradients, or call under torch.no_grad()")
 
 
 def _dtype(t, name):
@@ -144,6 +152,8 @@ def token_logprobs(logits, targets, top=0):
     """olsgd_token_logprobs.  logits [..., V] (rows evenly spaced), targets int32 [...]; a target outside
     [0, V) is a row without a token.  Returns TokenLogprobs(logp, entropy, stats, top_logp, top_ids): float32
     [...], [...], [..., 2], [..., top] and int32 [..., top] (the last two None when top == 0)."""
+    if logits.requires_grad:
+        _recorded(logits)
     lib = _OPS or _ops()
     xp, code, N, V, ld = _rows_of(logits, "logits")
     dev, lead = logits.device, logits.shape[:-1]
@@ -178,6 +188,7 @@ def token_logprobs(logits, targets, top=0):
 def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):
     """olsgd_token_logprobs_backward: the gradient of the logits, contiguous, of their type.  d_logp and d_entropy
     are float32 [...] or None (zeros); stats and entropy are token_logprobs' for the same logits."""
+    _recorded(d_logp, d_entropy, logits, stats, entropy)
     lib = _OPS or _ops()
     xp, code, N, V, ld = _rows_of(logits, "logits")
     dev, lead, f32 = logits.device, logits.shape[:-1], torch.float32
@@ -216,11 +227,15 @@ def clip_grads(grads, max_norm, out=None):
         out = [g.new_empty(g.shape) for g in grads]
     _need(len(out) == len(grads), "out must hold one tensor for each gradient")
     first = grads[0]
+    if first.requires_grad:
+        _recorded(first)
     m, dev = first.shape[0] if first.dim() else 0, first.device
     _need(first.is_cuda and m >= 1, "grads must be CUDA tensors with the workers first")
     index, codes, flat = dev.index, DTYPES, []
     for g, o in zip(grads, out):
         shape = g.shape
+        if g.requires_grad or o.requires_grad:
+            _recorded(g, o)
         if shape != o.shape or not shape or shape[0] != m or g.get_device() != index or o.get_device() != index:
             _refuse("gradients and out must be on one device, of the same shapes, with %d workers first", m)
         gc, oc = codes.get(g.dtype), codes.get(o.dtype)
@@ -269,6 +284,7 @@ def gated_forward(x, w_gate, w_up, activation="silu", save=False):
     """olsgd_gated_forward: h = act(x w_gate^T) * (x w_up^T) for each worker.  x [m][T][D], w_gate and w_up [m][F][D], bfloat16
     or float16, rows contiguous, any worker and row strides.  Returns h [m][T][F], and with save=True (h, pre), pre being what
     gated_backward takes."""
+    _recorded(x, w_gate, w_up)
     lib = _ops()
     m, T, D, F, code, act = _gated_sizes(x, w_gate, activation)
     dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
@@ -284,6 +300,7 @@ def gated_forward(x, w_gate, w_up, activation="silu", save=False):
 def gated_backward(d_h, x, w_gate, w_up, pre, activation="silu", want_d_x=True, want_d_w=True):
     """olsgd_gated_backward: (d_x, d_w_gate, d_w_up) from d_h [m][T][F] and the forward call's operands and pre; None for
     those not wanted."""
+    _recorded(d_h, x, w_gate, w_up, pre)
     lib = _ops()
     m, T, D, F, code, act = _gated_sizes(x, w_gate, activation)
     dtype, dev, ws_shape = x.dtype, x.device, (m, F, D)
@@ -305,6 +322,7 @@ def gated_backward(d_h, x, w_gate, w_up, pre, activation="silu", want_d_x=True, 
 def embedding_forward(table, ids, scale=1.0):
     """olsgd_embedding_forward: scale * table[i, ids[i]] for each worker i.  table [m][V][D], rows contiguous; ids int32 [m][T],
     those outside [0, V) give rows of zeros.  Returns [m][T][D] of the table's type."""
+    _recorded(table)
     lib = _ops()
     if not table.is_cuda or table.dim() != 3 or ids.dim() != 2:
         _refuse("table must be a CUDA tensor [m][V][D], ids [m][T]")
@@ -321,6 +339,7 @@ def embedding_forward(table, ids, scale=1.0):
 def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=None):
     """olsgd_embedding_backward: the gradient of a table [m][vocab][D] from d_out [m][T][D] and the ids of the lookup; new, of
     type `dtype`, or written to `out` (each worker's part contiguous, for example a view of a flat gradient [m][P])."""
+    _recorded(d_out, out)
     lib = _ops()
     if not d_out.is_cuda or d_out.dim() != 3 or d_out.shape[0] < 1:
         _refuse("d_out must be a CUDA tensor [m][T][D] of at least one worker")

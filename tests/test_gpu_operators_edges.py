@@ -325,3 +325,20 @@ def test_norms_are_ready_on_the_caller_s_stream():
         torch.cuda.synchronize()
         assert torch.equal(got, want)
     opt.close()
+
+
+# ------------------------------------------------------------------- torch's own bookkeeping
+
+def test_tensors_that_require_gradients():
+    """Refused while torch records, taken under no_grad; also where only a later one of a list does."""
+    g = _gen(7)
+    x, t = _randn(g, (4, 50)), torch.zeros(4, dtype=torch.int32, device="cuda")
+    want = lib.token_logprobs(x, t)
+    leaf = x.clone().requires_grad_()
+    for bad in (lambda: lib.token_logprobs(leaf, t), lambda: lib.token_logprobs(leaf * 2, t), lambda: lib.clip_grads([x, leaf], 1.0),
+                lambda: lib.clip_grads([x], 1.0, out=[leaf])):
+        with pytest.raises(ValueError, match="no graph"):
+            bad()
+    with torch.no_grad():
+        assert torch.equal(lib.token_logprobs(leaf, t).logp, want.logp)
+    assert torch.equal(lib.token_logprobs(leaf.detach(), t).logp, want.logp)
