@@ -24,6 +24,8 @@ MAX_TOP = 32
 
 TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy stats top_logp top_ids")
 
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+_strided, _like, _ONE, _TWO = torch.empty_strided, torch.empty_like, (1,), (2, 1)
 _vp, _i32, _i64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 _SIGNATURES = {
     "olsgd_token_logprobs_workspace": [_i32, _i64, _i64, _i32, C.POINTER(_sz)],
@@ -114,7 +116,7 @@ def _workspace(like, query, *sizes):
     n = _workspace_bytes(query, *sizes)
     if n == 0:
         return None, None, 0
-    ws = like.new_empty(n, dtype=torch.uint8)
+    ws = _strided((n,), _ONE, dtype=_U8, device=like.device)
     return ws, ws.data_ptr(), n
 
 
@@ -157,32 +159,27 @@ def token_logprobs(logits, targets, top=0):
     lib = _OPS or _ops()
     xp, code, N, V, ld = _rows_of(logits, "logits")
     dev, lead = logits.device, logits.shape[:-1]
-    tp = _per_row(targets, lead, torch.int32, dev, "targets")
+    tp = _per_row(targets, lead, _I32, dev, "targets")
     top = operator.index(top)
     if top < 0 or top > MAX_TOP or top > V:
         _refuse("top must be in [0, min(V, %d)]", MAX_TOP)
-    # the float outputs and the workspace behind them share one allocation (the workspace is 4 bytes for 256
-    # logits and little more): allocating and viewing is most of what the host does here
-    n_out = N * (4 + top)
-    wn = _workspace_bytes("olsgd_token_logprobs_workspace", code, N, V, top)
-    at = (n_out + 63) // 64 * 64   # 256 bytes
-    out = targets.new_empty(at + wn // 4 if wn else n_out, dtype=torch.float32)
-    p = out.data_ptr()
-    wp = p + 4 * at if wn else None
-    sizes = (N, N, 2 * N, top * N, out.shape[0] - n_out)
-    if top:
-        top_ids = targets.new_empty((N, top))
-        _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, top, p, p + 4 * N, p + 8 * N, p + 16 * N, top_ids.data_ptr(), wp, wn)
-        logp, entropy, stats, top_logp, _ = out.split_with_sizes(sizes)
-        top_logp = top_logp.view(N, top)
-    else:
-        top_logp = top_ids = None
-        _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, 0, p, p + 4 * N, p + 8 * N, None, None, wp, wn)
-        logp, entropy, stats, _, _ = out.split_with_sizes(sizes)
+    # Tensors of their own: whoever keeps one of them keeps, saves or changes nothing else.  (Allocated the quickest way there
+    # is, which is most of what the host does here.)
+    top_logp = top_ids = tlp = tip = None
     if len(lead) == 1:
-        return TokenLogprobs(logp, entropy, stats.view(N, 2), top_logp, top_ids)
-    return TokenLogprobs(logp.view(lead), entropy.view(lead), stats.view(lead + (2,)), top_logp.view(lead + (top,)) if top else None,
-                         top_ids.view(lead + (top,)) if top else None)
+        logp, stats = _strided(lead, _ONE, dtype=_F32, device=dev), _strided((N, 2), _TWO, dtype=_F32, device=dev)
+        if top:
+            top_logp, top_ids = _strided((N, top), (top, 1), dtype=_F32, device=dev), _strided((N, top), (top, 1), dtype=_I32, device=dev)
+    else:
+        logp, stats = torch.empty(lead, dtype=_F32, device=dev), torch.empty(lead + (2,), dtype=_F32, device=dev)
+        if top:
+            top_logp, top_ids = torch.empty(lead + (top,), dtype=_F32, device=dev), torch.empty(lead + (top,), dtype=_I32, device=dev)
+    entropy = _like(logp)
+    if top:
+        tlp, tip = top_logp.data_ptr(), top_ids.data_ptr()
+    ws, wp, wn = _workspace(targets, "olsgd_token_logprobs_workspace", code, N, V, top)
+    _run(lib.olsgd_token_logprobs, dev, xp, code, N, V, ld, tp, top, logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(), tlp, tip, wp, wn)
+    return TokenLogprobs(logp, entropy, stats, top_logp, top_ids)
 
 
 def token_logprobs_backward(d_logp, d_entropy, logits, targets, stats, entropy):

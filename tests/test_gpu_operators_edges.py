@@ -342,3 +342,20 @@ def test_tensors_that_require_gradients():
     with torch.no_grad():
         assert torch.equal(lib.token_logprobs(leaf, t).logp, want.logp)
     assert torch.equal(lib.token_logprobs(leaf.detach(), t).logp, want.logp)
+
+
+@pytest.mark.parametrize("N,V,top", [(4, 50, 0), (4, 50, 3), (8, 131072, 20), (3, 5000, 0)])
+def test_log_probabilities_are_tensors_of_their_own(N, V, top):
+    """Whoever keeps, saves or changes one of them keeps, saves or changes nothing else; autograd takes them like any tensors."""
+    g = _gen(8)
+    x, t = _randn(g, (N, V)), torch.zeros(N, dtype=torch.int32, device="cuda")
+    want = [None if v is None else v.clone() for v in lib.token_logprobs(x, t, top)]
+    r = lib.token_logprobs(x, t, top)
+    tensors = [v for v in r if v is not None]
+    assert all(v.untyped_storage().nbytes() == v.numel() * 4 for v in tensors)
+    assert len({v.untyped_storage().data_ptr() for v in tensors}) == len(tensors)
+    weights = torch.full((N,), 2.0, device="cuda", requires_grad=True)
+    r.logp.mul_(weights)
+    r.logp.sum().backward()
+    assert torch.equal(weights.grad, want[0])
+    assert all(torch.equal(a, b) and a._version == 0 and not a._is_view() for a, b in zip(tensors[1:], want[1:]))
