@@ -214,7 +214,8 @@ def clip_grads(grads, max_norm, out=None):
     """olsgd_clip_grads.  grads: a tensor or a list of tensors [m, ...], each worker's part contiguous.  Each worker's
     gradients, over all tensors, are scaled by min(1, max_norm / (norm + 1e-6)).  out: tensors of the same shapes, of any
     of the three types, that take the result (the gradients themselves: in place; views of a flat float32 gradient [m][P]:
-    widened into it); None: new tensors like the gradients.  Returns (out, norms), norms float32 [m]."""
+    widened into it); None: new tensors like the gradients; no two of them may overlap, and none twice.  Returns (out, norms),
+    norms float32 [m]."""
     lib = _ops()
     single = isinstance(grads, torch.Tensor)
     if single:
@@ -241,6 +242,9 @@ def clip_grads(grads, max_norm, out=None):
         n = g.numel() // m
         flat += (g.data_ptr(), o.data_ptr(), n, n if g.is_contiguous() else _worker_rows(g, m, "a gradient")[1],
                  n if o.is_contiguous() else _worker_rows(o, m, "out")[1], gc | (oc << 32))
+    places = [p for p in flat[1::6] if p]   # (of those that hold anything)
+    if len(set(places)) < len(places):
+        _refuse("out holds a tensor twice: it would be scaled twice")
     table = (_i64 * len(flat))(*flat)
     norms = first.new_empty(m, dtype=torch.float32)
     ws, wp, wn = _workspace(norms, "olsgd_clip_grads_workspace", m, len(grads))

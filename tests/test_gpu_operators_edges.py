@@ -359,3 +359,17 @@ def test_log_probabilities_are_tensors_of_their_own(N, V, top):
     r.logp.sum().backward()
     assert torch.equal(weights.grad, want[0])
     assert all(torch.equal(a, b) and a._version == 0 and not a._is_view() for a, b in zip(tensors[1:], want[1:]))
+
+
+# ------------------------------------------------------------------------- refusals
+
+def test_clip_grads_refuses_to_scale_a_tensor_twice():
+    a, b, none = torch.ones((2, 10), device="cuda"), torch.ones((2, 7), device="cuda"), torch.empty((2, 0), device="cuda")
+    for grads, out in (([a, b, a], [a, b, a]), ([a, a], [b.new_empty((2, 10))] * 2)):
+        with pytest.raises(ValueError, match="twice"):
+            lib.clip_grads(grads, 1.0, out=out)
+    torch.cuda.synchronize()
+    assert bool((a == 1).all()) and bool((b == 1).all())
+    # a gradient that counts twice may be read twice, and what is empty may be there as often as it likes
+    _, norms = lib.clip_grads([a, none, a, none], 1.0, out=[torch.empty_like(a), none, torch.empty_like(a), none])
+    assert bool(((norms.double() - math.sqrt(20)).abs() <= 4 * U * math.sqrt(20)).all())
