@@ -346,7 +346,9 @@ def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=No
         _refuse("d_out must be a CUDA tensor [m][T][D] of at least one worker")
     code, dev = _dtype(d_out, "d_out"), d_out.device
     m, T, D = d_out.shape
-    V = int(vocab)
+    V = operator.index(vocab)
+    if V < 1:
+        _refuse("vocab must be positive")
     p, sw, sr = _matrix(d_out, "d_out", (m, T, D), d_out.dtype, dev)
     if out is None:
         out = d_out.new_empty((m, V, D), dtype=dtype)

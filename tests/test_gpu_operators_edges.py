@@ -373,3 +373,13 @@ def test_clip_grads_refuses_to_scale_a_tensor_twice():
     # a gradient that counts twice may be read twice, and what is empty may be there as often as it likes
     _, norms = lib.clip_grads([a, none, a, none], 1.0, out=[torch.empty_like(a), none, torch.empty_like(a), none])
     assert bool(((norms.double() - math.sqrt(20)).abs() <= 4 * U * math.sqrt(20)).all())
+
+
+def test_embedding_gradient_refuses_a_vocabulary_that_is_no_positive_integer():
+    d, ids = torch.ones((1, 2, 4), device="cuda"), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    for vocab in (0, -1):
+        with pytest.raises(ValueError, match="vocab"):
+            lib.embedding_backward(d, ids, vocab)
+    with pytest.raises(TypeError):
+        lib.embedding_backward(d, ids, 3.7)
+    assert lib.embedding_backward(d, ids, torch.tensor(3)).shape == (1, 3, 4)
