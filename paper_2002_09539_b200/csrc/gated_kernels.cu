@@ -829,10 +829,17 @@ __device__ __forceinline__ bool warp_overlap(const T* x, const T* w, int64_t D, 
 // that were pruned) and rows with one element other than 0 count as rows of norm 0; where both rows are coarse (multiples
 // of a power of two that is 2^-10 of the norm or more: small integers), 22 bits hold every partial sum.
 //
+template <typename T>
+__device__ __forceinline__ float raw_lowest(const uint4& w) {   // its first element
+  float lo, hi;
+  unpack2f(raw_pair<T>(w, 0), lo, hi);
+  return lo;
+}
+
 // row_norms_kernel: the norm of each row of x and w_gate, with the sign set on that of a coarse row; a warp per row.
 // Most rows are done after their first reading; only those whose first 256 elements are coarse are read twice.  16
-// workers, 128 tokens, 1024 -> 1024: 37 MB in 10.8 us from cold caches (3.4 TB/s; two rows a warp were no faster).
-// relu's backward pass takes 56 us there, silu's, which needs no norms, 45; 8192 tokens, 4096 -> 8192: 1920 and 1890.
+// workers, 128 tokens, 1024 -> 1024: 37 MB in 10.4 us from cold caches (3.6 TB/s; two rows a warp were no faster).
+// relu's backward pass takes 54.6 us there, silu's, which needs no norms, 44.8; 8192 tokens, 4096 -> 8192: 1895 and 1872.
 template <typename T>
 __global__ void __launch_bounds__(256)
 row_norms_kernel(GatedOperand x, GatedOperand w, int64_t tokens, int64_t F, int64_t D, float* __restrict__ xn, float* __restrict__ wn,
@@ -886,6 +893,11 @@ row_norms_kernel(GatedOperand x, GatedOperand w, int64_t tokens, int64_t F, int6
   const int exponent = (int)(__float_as_uint(norm) >> 23);
   bool coarse = exponent > 30 && exponent < 220;
   const float to_grid = __uint_as_float((uint32_t)(coarse ? 127 + 127 + 10 - exponent : 127) << 23);
+  // (one element a lane tells nearly every row that is not)
+  if (coarse) {
+    const float t = raw_lowest<T>(first) * to_grid;
+    coarse = __all_sync(0xffffffffu, t == rintf(t));
+  }
   int others = 0;   // elements other than 0
   for (int64_t p = 0; p < n && coarse; p += kStep) {
     float v[V];
@@ -936,14 +948,15 @@ __device__ __forceinline__ void settle(const GatedGrad& g, int64_t worker, int64
   const Border& o = g.border;
   const T* x = static_cast<const T*>(o.x.p) + worker * o.x.worker_stride + r * o.x.row_stride;
   const T* w = static_cast<const T*>(o.wg.p) + worker * o.wg.worker_stride + col * o.wg.row_stride;
+  const int64_t wr = worker * g.rows + r;
+  const float d = Elem<T>::to_float(__ldcg(static_cast<const T*>(g.dh) + worker * g.dh_worker + r * g.dh_row + col));
+  const float b = __ldcg(g.pre + wr * 2 * g.pitch + g.pitch + col);
   // (sparse rows may have no element in common: nothing to add up)
   if (zero && !warp_overlap(x, w, o.D, o.vec)) return;
   const float exact = (float)warp_dot(x, w, o.D, o.vec);
   if ((threadIdx.x & 31) == from) {
-    const int64_t wr = worker * g.rows + r;
     const ActPair p = act_pair<OLSGD_ACT_RELU>(exact);
-    const float d = Elem<T>::to_float(static_cast<const T*>(g.dh)[worker * g.dh_worker + r * g.dh_row + col]);
-    static_cast<T*>(g.da)[wr * g.pitch + col] = Elem<T>::from_float(d * g.pre[wr * 2 * g.pitch + g.pitch + col] * p.df * scale);
+    static_cast<T*>(g.da)[wr * g.pitch + col] = Elem<T>::from_float(d * b * p.df * scale);
     static_cast<T*>(g.db)[wr * g.pitch + col] = Elem<T>::from_float(d * p.f * scale);
   }
 }
@@ -1028,9 +1041,9 @@ __device__ __forceinline__ float block_max(float v) {
   return v;
 }
 
-// A warp per stretch.
+// A warp per stretch.  (relu's border takes registers: with 48 of them some are spilled, 1 us of 16 workers' pass.)
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256, 5) gated_backward_kernel(const __grid_constant__ GatedGrad g, bool beside) {
+__global__ void __launch_bounds__(256, ACT == OLSGD_ACT_RELU ? 4 : 5) gated_backward_kernel(const __grid_constant__ GatedGrad g, bool beside) {
   if (!beside) launch_gate();
   const int64_t stretches = (g.pitch + kStretch - 1) / kStretch;
   const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = at / stretches;
@@ -1055,7 +1068,7 @@ __device__ __forceinline__ float scale_for(float most) {
   return __uint_as_float((uint32_t)(127 + (k < 120 ? k : 120)) << 23);
 }
 template <int ACT>
-__global__ void __launch_bounds__(256, 5) gated_rescale_kernel(const __grid_constant__ GatedGrad g, int64_t maxima) {
+__global__ void __launch_bounds__(256, ACT == OLSGD_ACT_RELU ? 4 : 5) gated_rescale_kernel(const __grid_constant__ GatedGrad g, int64_t maxima) {
   launch_gate();
   const int64_t worker = blockIdx.y, stretches = (g.pitch + kStretch - 1) / kStretch;
   float most = 0.f;
