@@ -242,6 +242,38 @@ def test_fp16_gradients_with_infinities_keep_to_their_rows():
             assert bool(torch.isnan(got[0, 9]).all()) and not bool(torch.isfinite(got[0, 5]).any())
 
 
+@pytest.mark.parametrize("m,T,D,F", [(3, 65, 64, 96), (2, 40, 333, 203), (700, 3, 16, 24), (1, 200, 304, 2048)])
+@pytest.mark.parametrize("kind", ["silu", "relu"])
+def test_captured_fp16_gradients_follow_the_inputs_factor(kind, m, T, D, F):
+    """A graph is replayed with gradients of other magnitudes, each with another factor: the bits of eager calls, in plain stream
+    order too."""
+    g = _gen(m + T + D)
+    dtype = torch.float16
+    x, wg, wu = _randn(g, (m, T, D), dtype), _randn(g, (m, F, D), dtype, D ** -0.5), _randn(g, (m, F, D), dtype, D ** -0.5)
+    dhs = [_randn(g, (m, T, F), dtype, std) for std in (1.0, 2.0 ** -18, 2.0 ** 13, 2.0 ** -12)]
+    _, pre = lib.gated_forward(x, wg, wu, kind, save=True)
+    before = lib.set_launch_overlap(False)
+    try:
+        want = [lib.gated_backward(dh, x, wg, wu, pre, kind) for dh in dhs]
+        torch.cuda.synchronize()
+    finally:
+        lib.set_launch_overlap(before)
+    dh, stream, graph = dhs[0].clone(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        got = lib.gated_backward(dh, x, wg, wu, pre, kind)
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(10):
+        for other, w in zip(dhs, want):
+            dh.copy_(other)
+            graph.replay()
+            eager = lib.gated_backward(other, x, wg, wu, pre, kind)
+            for u, v, e in zip(got, w, eager):
+                bad += (u != v).sum() + (e != v).sum()
+    assert int(bad) == 0 and all(bool(torch.isfinite(t).all()) for t in want[1])
+    lib.operators_join()
+
+
 # ---------------------------------------------------------------------- saturated gates
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
