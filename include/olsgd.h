@@ -197,7 +197,8 @@ olsgd_status olsgd_join(olsgd_ctx* ctx);
 
 /* Every wait a kernel of this library performs on a barrier is bounded; a wait that runs
  * out makes the kernel return early and the next joining call (olsgd_join,
- * olsgd_get_params) return OLSGD_ETIMEOUT.  olsgd_selftest_wait_timeout exercises that
+ * olsgd_get_params; for the operators on caller-owned tensors olsgd_operators_join) return
+ * OLSGD_ETIMEOUT.  olsgd_selftest_wait_timeout exercises that
  * path without any fault: it launches a kernel whose one thread waits, for at most
  * limit_ms milliseconds, on a barrier that nothing ever arrives on.  After it, olsgd_join
  * returns OLSGD_ETIMEOUT until olsgd_clear_status is called; the context and the GPU
@@ -404,7 +405,9 @@ olsgd_status olsgd_class_pairs_noalloc(uint64_t seed, int32_t m, int32_t* dst, v
  * aligned to their element (workspaces to 256 bytes); strides are in elements and need not be
  * multiples of 16 bytes.  Outputs must not overlap inputs unless stated, nor other outputs.
  * Errors are reported as everywhere: a status, and olsgd_last_error(NULL).  Sizes of zero
- * rows, tokens or tensors are no error (a gradient of no tokens is zero).                   */
+ * rows, tokens or tensors are no error (a gradient of no tokens is zero; of no rows or tensors
+ * nothing is written).  The same call gives the same bits every time; the same values at another
+ * alignment of pointers or strides may be added up in another order.                        */
 typedef enum { OLSGD_F32 = 0, OLSGD_BF16 = 1, OLSGD_F16 = 2 } olsgd_dtype;
 
 /* Log probabilities of given tokens, with entropy and the most likely alternatives.
