@@ -818,6 +818,14 @@ __device__ __forceinline__ bool warp_overlap(const T* x, const T* w, int64_t D, 
   return __any_sync(0xffffffffu, any != 0);
 }
 
+// The first element of a piece.
+template <typename T>
+__device__ __forceinline__ float raw_first(const uint4& w) {
+  float lo, hi;
+  unpack2f(raw_pair<T>(w, 0), lo, hi);
+  return lo;
+}
+
 // relu's derivative jumps at 0, and an accumulation in fp32 is off by a share of its partial sums, none of which
 // exceeds |x_t| |w_f| (Euclidean norms).  Where a lies within
 //   (8 + D / 128) 2^-23 |x_t| |w_f|
@@ -829,13 +837,6 @@ __device__ __forceinline__ bool warp_overlap(const T* x, const T* w, int64_t D, 
 // that were pruned) and rows with one element other than 0 count as rows of norm 0; where both rows are coarse (multiples
 // of a power of two that is 2^-10 of the norm or more: small integers), 22 bits hold every partial sum.
 //
-template <typename T>
-__device__ __forceinline__ float raw_lowest(const uint4& w) {   // its first element
-  float lo, hi;
-  unpack2f(raw_pair<T>(w, 0), lo, hi);
-  return lo;
-}
-
 // row_norms_kernel: the norm of each row of x and w_gate, with the sign set on that of a coarse row; a warp per row.
 // Most rows are done after their first reading; only those whose first 256 elements are coarse are read twice.  16
 // workers, 128 tokens, 1024 -> 1024: 37 MB in 10.4 us from cold caches (3.6 TB/s; two rows a warp were no faster).
@@ -895,7 +896,7 @@ row_norms_kernel(GatedOperand x, GatedOperand w, int64_t tokens, int64_t F, int6
   const float to_grid = __uint_as_float((uint32_t)(coarse ? 127 + 127 + 10 - exponent : 127) << 23);
   // (one element a lane tells nearly every row that is not)
   if (coarse) {
-    const float t = raw_lowest<T>(first) * to_grid;
+    const float t = raw_first<T>(first) * to_grid;
     coarse = __all_sync(0xffffffffu, t == rintf(t));
   }
   int others = 0;   // elements other than 0
