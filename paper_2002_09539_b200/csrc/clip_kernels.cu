@@ -37,7 +37,8 @@ struct Item {
 };
 // N: descriptors a launch has room for.  Short lists go with few, since the host copies the parameters
 // several times with each launch (a call on one tensor takes 12.9 us of its time, 16.2 with room for
-// all; on twenty, with room for kSomeTensors, 37 and 43).
+// all; on twenty, with room for kSomeTensors, 37 and 43; 48 and 49, either side of that, 78 and 82: from there on the
+// descriptors themselves are what takes the time).
 template <int N>
 struct Items {
   int32_t count, pad;
