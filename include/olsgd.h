@@ -529,6 +529,116 @@ olsgd_status olsgd_embedding_backward(int32_t m, int64_t T, int64_t V, int64_t D
                                       int32_t d_table_dtype, void* d_table,
                                       int64_t d_table_worker_stride, void* workspace,
                                       size_t workspace_bytes, void* stream);
+/* ---- Experts: a block whose tokens choose among E weight matrices, for each worker.
+ *
+ * olsgd_expert_route: the k experts of each token.  logits [m][T][E] (row r of the m T rows begins
+ * row_stride elements behind row r - 1), E in [1, OLSGD_MAX_EXPERTS], k in [1, min(E, OLSGD_MAX_TOP)].
+ * A token's experts are its k largest logits in falling order, ties to the lowest expert; a logit of -inf
+ * is never chosen, so a token may have fewer than k, or (padding: all -inf) none.  NaN counts as largest.
+ *   weights  float [m][T][k]: softmax over the chosen logits (normalise != 0), or the chosen ones' share of
+ *            the softmax over all E; 0 where there is no expert
+ *   ids      int32 [m][T][k]: the experts; -1: none
+ *   offsets  int32 [m][E + 1], tokens int32 [m][T k], places int32 [m][T][k]: the (token, expert) pairs
+ *            in order of expert, then token, are the rows 0, 1, ... of a worker; rows offsets[e] to
+ *            offsets[e + 1] - 1 are expert e's.  tokens: the token of each row, -1 behind the last;
+ *            places: the row of each pair, -1: none.
+ * olsgd_embedding_forward(x as the table, tokens as the ids) gathers the rows' inputs.
+ * T k must not exceed 2^31 - 1, T not 2^24.                                                      */
+#define OLSGD_MAX_EXPERTS 1024
+olsgd_status olsgd_expert_route_workspace(int32_t m, int64_t T, int64_t E, size_t* out_bytes);
+olsgd_status olsgd_expert_route(int32_t m, int64_t T, int64_t E, int32_t dtype, const void* logits,
+                                int64_t row_stride, int32_t k, int32_t normalise, float* weights,
+                                int32_t* ids, int32_t* places, int32_t* tokens, int32_t* offsets,
+                                void* workspace, size_t workspace_bytes, void* stream);
+/* Its gradient: d_logits [rows][E] contiguous, of the logits' type, for rows = m T tokens, from d_weights
+ * float [rows][k] and the ids and weights of the forward call (the same `normalise`).  Logits are
+ * read where normalise == 0.  Pairs without an expert take no part; a token without experts has a
+ * gradient of 0.  d_logits must not overlap the logits.                                           */
+olsgd_status olsgd_expert_route_backward(int64_t rows, int64_t E, int32_t dtype, const float* d_weights,
+                                         const void* logits, int64_t row_stride, int32_t k,
+                                         int32_t normalise, const int32_t* ids, const float* weights,
+                                         void* d_logits, void* stream);
+
+/* y[i][t] = sum over j of weights[i][t][j] rows[i][places[i][t][j]], added up in order of j in fp32,
+ * rounded once.  A place outside [0, R) adds nothing, whatever its weight.  With weights == NULL
+ * (all 1) it is the gradient of gathering.
+ *   rows  [m][R][D] of type dtype (any of the three), strides as given, D contiguous
+ *   places int32 [m][T][k], weights float [m][T][k], y [m][T][D] of type dtype: contiguous;  k >= 1 */
+olsgd_status olsgd_expert_combine(int32_t m, int64_t T, int32_t k, int64_t R, int64_t D, int32_t dtype,
+                                  const void* rows, int64_t rows_worker_stride, int64_t rows_row_stride,
+                                  const int32_t* places, const float* weights, void* y, void* stream);
+/* Its gradient.  places name each row at most once, and tokens int32 [m][R] are negative exactly where
+ * they do not name a row (both as olsgd_expert_route leaves them): such a row has a gradient of 0.
+ *   d_y       [m][T][D] of type dtype, strides as given
+ *   d_rows    [m][R][D] of type dtype, contiguous;  d_weights  float [m][T][k], 0 where there is no row */
+olsgd_status olsgd_expert_combine_backward(int32_t m, int64_t T, int32_t k, int64_t R, int64_t D,
+                                           int32_t dtype, const void* d_y, int64_t d_y_worker_stride,
+                                           int64_t d_y_row_stride, const void* rows,
+                                           int64_t rows_worker_stride, int64_t rows_row_stride,
+                                           const int32_t* places, const int32_t* tokens,
+                                           const float* weights, void* d_rows, float* d_weights,
+                                           void* stream);
+
+/* y[i][r] = w[i][e] x[i][r] for the rows r of expert e: offsets[i][e] <= r < offsets[i][e + 1].  Rows that
+ * belong to no expert (before offsets[i][0], from offsets[i][E] on) become zeros.  fp32 accumulation, one
+ * rounding.  Operands are bf16 or fp16.  Offsets lie on the device and are not checked by the
+ * host: values outside [0, R] count as the nearest of the two, one that is below an earlier one of its
+ * worker as that one (d_w of the experts concerned is undefined).
+ *   x [m][R][D], w [m][E][F][D]: strides in elements, the last dimension contiguous (w may be a view of
+ *   rows that hold all of a worker's parameters);  offsets int32 [m][E + 1];  y [m][R][F] contiguous
+ *   E in [1, OLSGD_MAX_EXPERTS], m E <= 65535, m R <= 2^31 - 1, D and F in [1, 2^24]
+ * aligned != 0 promises 16-byte alignment of every operand's base and strides (x and w; d_y too
+ * for the backward call): no copies then.                                                        */
+olsgd_status olsgd_expert_product_workspace(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F,
+                                            int32_t backward, int32_t aligned, size_t* out_bytes);
+olsgd_status olsgd_expert_product(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F, int32_t dtype,
+                                  const void* x, int64_t x_worker_stride, int64_t x_row_stride,
+                                  const void* w, int64_t w_worker_stride, int64_t w_expert_stride,
+                                  int64_t w_row_stride, const int32_t* offsets, void* y, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+/* Its gradients, either of which may be NULL: d_x[i][r] = w[i][e]^T d_y[i][r] (zeros for rows of no expert) and
+ * d_w[i][e] = sum over the expert's rows of d_y[i][r] x[i][r]^T (zeros for an expert without rows), contiguous.
+ * What rows of no expert hold is not used.                                                        */
+olsgd_status olsgd_expert_product_backward(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F,
+                                           int32_t dtype, const void* d_y, int64_t d_y_worker_stride,
+                                           int64_t d_y_row_stride, const void* x, int64_t x_worker_stride,
+                                           int64_t x_row_stride, const void* w, int64_t w_worker_stride,
+                                           int64_t w_expert_stride, int64_t w_row_stride,
+                                           const int32_t* offsets, void* d_x,
+                                           void* d_w, void* workspace, size_t workspace_bytes,
+                                           void* stream);
+
+/* ---- Distillation from a teacher's top logits.  For each of `rows` rows of V logits and its K pairs
+ * (ids, teacher):  q = softmax(teacher / temperature) over the pairs, p = softmax(logits / temperature)
+ * over all tokens,  loss = sum over j of q_j (log q_j - log p[ids_j]).
+ * A pair whose id lies outside [0, V) is none; a row without a pair (or whose teacher logits are all -inf) has
+ * loss 0 and gradient 0 whatever its logits hold.  An id may occur in several pairs.  Where q_j = 0 the pair
+ * adds nothing; a token that the teacher gives weight and the student masks with -inf makes the loss
+ * +inf, and the gradient stays p - q.  A row of nothing but -inf has loss +inf and gradient 0.  NaN and
+ * +inf among the logits make loss and gradient of their row NaN.
+ *   logits  [rows][V] of type dtype, rows row_stride >= V elements apart; V in [1, 2^27]
+ *   ids     int32 [rows][K], teacher [rows][K] of type teacher_dtype: contiguous; K in [1, OLSGD_MAX_TEACHER]
+ *   temperature   in [2^-20, 2^20]
+ *   loss    float [rows];  stats  float [rows][2]: max x, and log sum exp((x - max x) / temperature)
+ *   d_loss  float [rows] or NULL: with it d_logits [rows][V], of type dtype, rows d_row_stride >= V apart, takes
+ *           d_loss (p - q) / temperature (q: 0 but at the pairs) from the same read of the logits, where a
+ *           row fits eight multiprocessors' registers.  A row whose d_loss is 0 has a gradient of 0.
+ * d_logits may be the logits themselves (with the same stride).                                   */
+#define OLSGD_MAX_TEACHER 256
+olsgd_status olsgd_distill_workspace(int32_t dtype, int64_t rows, int64_t V, int32_t gradient,
+                                     size_t* out_bytes);
+olsgd_status olsgd_distill(const void* logits, int32_t dtype, int64_t rows, int64_t V, int64_t row_stride,
+                           const int32_t* ids, const void* teacher, int32_t teacher_dtype, int32_t K,
+                           float temperature, const float* d_loss, float* loss, float* stats,
+                           void* d_logits, int64_t d_row_stride, void* workspace,
+                           size_t workspace_bytes, void* stream);
+/* The gradient alone, for a d_loss that is known later; stats as olsgd_distill left them.         */
+olsgd_status olsgd_distill_backward(const float* d_loss, const void* logits, int32_t dtype, int64_t rows,
+                                    int64_t V, int64_t row_stride, const int32_t* ids, const void* teacher,
+                                    int32_t teacher_dtype, int32_t K, float temperature,
+                                    const float* stats, void* d_logits, int64_t d_row_stride,
+                                    void* stream);
+
 /* Blocks the host until `stream` is idle.  OLSGD_ETIMEOUT if a bounded wait inside an operator
  * on the current device gave up since the last such call (the outputs of the calls in between
  * are not valid then); the report is cleared.                                              */

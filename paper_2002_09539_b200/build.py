@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libolsgd.so")
 SOURCES = ["olsgd_api.cu", "update_kernels.cu", "sampling_kernels.cu", "simt_kernels.cu", "head_kernels.cu",
            "model.cu", "tc_gemm.cu", "tc_wgrad.cu", "operators_api.cu", "logprob_kernels.cu", "clip_kernels.cu",
-           "gated_kernels.cu", "embedding_kernels.cu"]
+           "gated_kernels.cu", "embedding_kernels.cu", "expert_kernels.cu", "product_kernels.cu", "distill_kernels.cu"]
 
 
 def _stale():

@@ -1,0 +1,629 @@
+// Distillation from a teacher's top logits: for a row x of V logits and K pairs (token, teacher's logit z),
+//   q = softmax(z / tau) over the pairs, p = softmax(x / tau) over all tokens,
+//   loss = sum q_j (log q_j - log p_id_j),    d_x = (d_loss / tau) (p - q at the pairs' tokens).
+// With m = max x: log p = (x - m) / tau - log sum exp((x - m) / tau); the difference is formed before it is
+// scaled.  Sums and statistics are held in fp32.
+//
+// Bound by the logits' way in and, for a gradient, its way out.  Where the rows' weights are known when
+// the loss is formed, both come from one read: a row lies in the registers of a cluster of up to
+// eight CTAs as exp(x - the CTA's own max), 32 values a thread, until the whole row's sum is known.
+// Longer rows, losses alone and gradients that are asked for later take one pass each.  Rows of up to
+// 1024 logits belong to a warp.
+//
+// A gradient at the pairs' tokens is formed apart from the others, from the logit and the sum of the q of
+// all pairs with that token, and stored behind them, so that it is rounded once.
+#include "operator_common.cuh"
+#include "operators_internal.h"
+
+namespace olsgd {
+namespace {
+
+using namespace op;
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kChunkElems = 256;     // of a warp's turn: eight elements a lane
+constexpr int kWarpRowMax = 1024;    // longest row that stays in a warp's registers
+constexpr int kMaxSplit = 64;
+constexpr int kMaxPairs = OLSGD_MAX_TEACHER;
+static_assert(kMaxPairs <= kThreads, "a thread for each pair");
+constexpr int kFusedThreads = 512, kFusedValues = 32;
+constexpr int kFusedPart = kFusedThreads * kFusedValues;   // elements of a row that a CTA holds
+constexpr int kMaxCluster = 8;
+
+struct Sum {
+  float m, s;   // maximum; sum of exp((x - m) / tau)
+};
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+// c = log2(e) / tau
+__device__ __forceinline__ Sum join(const Sum& a, const Sum& b, float c) {
+  Sum r;
+  r.m = fmaxf(a.m, b.m);
+  const float base = base_of(r.m);
+  // (a part of nothing but -inf has the sum 0, or NaN)
+  r.s = a.s * (a.m == -INFINITY ? 1.f : ex2((a.m - base) * c)) + b.s * (b.m == -INFINITY ? 1.f : ex2((b.m - base) * c));
+  return r;
+}
+__device__ __forceinline__ Sum shfl_join(Sum v, float c) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    Sum w;
+    w.m = __shfl_xor_sync(0xffffffffu, v.m, o);
+    w.s = __shfl_xor_sync(0xffffffffu, v.s, o);
+    v = join(v, w, c);
+  }
+  return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+// A row of nothing but -inf has no distribution: log p = -inf, no gradient.
+__device__ __forceinline__ bool empty(const Sum& v) { return v.m == -INFINITY && v.s == 0.f; }
+__device__ __forceinline__ float log_sum(const Sum& v) { return empty(v) ? 0.f : logf(v.s); }
+
+template <typename T>
+__host__ __device__ constexpr uint32_t minus_inf() {
+  return sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
+}
+__device__ __forceinline__ float load_any(const void* p, int dtype, int64_t i) {
+  if (dtype == OLSGD_F32) return static_cast<const float*>(p)[i];
+  if (dtype == OLSGD_BF16) return Elem<__nv_bfloat16>::to_float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return Elem<__half>::to_float(static_cast<const __half*>(p)[i]);
+}
+
+// A pair as its thread holds it.  A token outside [0, V) is no pair.
+struct Pair {
+  int32_t id;
+  float z, x;   // the teacher's logit, the student's
+};
+template <typename T>
+__device__ __forceinline__ Pair fetch_pair(const DistillArgs& a, const T* row, int64_t r, int j) {
+  Pair p{-1, -INFINITY, 0.f};
+  if (j < a.K) {
+    p.id = a.ids[r * a.K + j];
+    if (p.id < 0 || p.id >= a.V) {
+      p.id = -1;
+    } else {
+      p.z = load_any(a.teacher, a.teacher_dtype, r * a.K + j);
+      p.x = Elem<T>::to_float(row[p.id]);
+    }
+  }
+  return p;
+}
+
+// The teacher's side of a row: maximum and sum of its logits as the student's.  A maximum that passes over
+// NaN is followed by a sum that does not.
+struct PairTerm {
+  float q, loss;
+};
+__device__ __forceinline__ PairTerm pair_term(const Pair& p, const Sum& teacher, float log_teacher, const Sum& row, float log_s,
+                                              float inv_t, float c) {
+  PairTerm t{0.f, 0.f};
+  if (p.id < 0 || empty(teacher)) return t;
+  const float z = (p.z - base_of(teacher.m)) * inv_t;
+  t.q = ex2((p.z - base_of(teacher.m)) * c) / teacher.s;
+  if (t.q == 0.f) return t;
+  const float lp = empty(row) ? -INFINITY : (p.x - base_of(row.m)) * inv_t - log_s;
+  t.loss = t.q * ((z - log_teacher) - lp);
+  return t;
+}
+
+// What a gradient takes from a row.  Rows that nothing is asked of (no teacher, a weight of 0) and rows without
+// a distribution have a gradient of 0 whatever they hold.
+struct GradRow {
+  float base, scale;   // gradient of an ordinary token: scale exp((x - base) / tau)
+  float g;             // d_loss / tau
+  bool zero;
+  __device__ __forceinline__ float at(float x, float c) const { return zero ? 0.f : scale * ex2((x - base) * c); }
+};
+
+// ------------------------------------------------------------ rows in a warp's registers
+// LOSS: loss and statistics are written; GRAD: the gradient (from `stats` where LOSS is false).
+template <typename T, int NL, bool LOSS, bool GRAD>
+__global__ void __launch_bounds__(kThreads) distill_warp_kernel(const DistillArgs a) {
+  __shared__ float q_of[kWarps][kMaxPairs];
+  __shared__ float x_of[kWarps][kMaxPairs];
+  __shared__ int32_t id_of[kWarps][kMaxPairs];
+  launch_gate();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t r = (int64_t)blockIdx.x * kWarps + warp;
+  if (r >= a.rows) return;
+  const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+  const int V = (int)a.V;
+  const float c = a.inv_t * kLog2e;
+  float v[NL], mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int j = i * 32 + lane;
+    v[i] = j < V ? Elem<T>::to_float(row[j]) : -INFINITY;
+    mx = fmaxf(mx, v[i]);
+  }
+  Sum student, teacher{-INFINITY, 0.f};
+  float log_s;
+  if (LOSS) {
+    student.m = warp_max(mx);
+    student.s = 0.f;
+    const float base = base_of(student.m);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) student.s += ex2((v[i] - base) * c);
+    student.s = warp_sum(student.s);
+    log_s = log_sum(student);
+  } else {
+    student.m = a.stats[2 * r];
+    log_s = a.stats[2 * r + 1];
+    student.s = student.m == -INFINITY && log_s == 0.f ? 0.f : ex2(log_s * kLog2e);
+  }
+  for (int j = lane; j < a.K; j += 32) teacher.m = fmaxf(teacher.m, fetch_pair<T>(a, row, r, j).z);
+  teacher.m = warp_max(teacher.m);
+  for (int j = lane; j < a.K; j += 32) teacher.s += ex2((fetch_pair<T>(a, row, r, j).z - base_of(teacher.m)) * c);
+  teacher.s = warp_sum(teacher.s);
+  const float log_teacher = log_sum(teacher);
+  float loss = 0.f;
+  for (int j = lane; j < a.K; j += 32) {
+    const Pair p = fetch_pair<T>(a, row, r, j);
+    const PairTerm t = pair_term(p, teacher, log_teacher, student, log_s, a.inv_t, c);
+    loss += t.loss;
+    q_of[warp][j] = t.q;
+    x_of[warp][j] = p.x;
+    id_of[warp][j] = p.id;
+  }
+  if (LOSS) {
+    loss = warp_sum(loss);
+    if (lane == 0) {
+      a.loss[r] = loss;
+      a.stats[2 * r] = student.m;
+      a.stats[2 * r + 1] = log_s;
+    }
+  }
+  if (GRAD) {
+    __syncwarp();
+    T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
+    const float weight = a.d_loss[r];
+    GradRow g;
+    g.zero = weight == 0.f || empty(teacher) || empty(student);
+    g.g = weight * a.inv_t;
+    g.base = base_of(student.m);
+    g.scale = g.g / student.s;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int j = i * 32 + lane;
+      if (j < V) out[j] = Elem<T>::from_float(g.at(v[i], c));
+    }
+    if (g.zero) return;
+    __syncwarp();
+    // the pairs' tokens; the first of the pairs with a token adds up all of them
+    for (int j = lane; j < a.K; j += 32) {
+      const int32_t id = id_of[warp][j];
+      float q = 0.f;
+      int first = j;
+      for (int e = 0; e < a.K; ++e)
+        if (id_of[warp][e] == id) {
+          q += q_of[warp][e];
+          first = min(first, e);
+        }
+      if (id >= 0 && first == j) out[id] = Elem<T>::from_float(fmaf(-g.g, q, g.at(x_of[warp][j], c)));
+    }
+  }
+}
+
+// -------------------------------------------------------------------------- long rows
+// Sums over a CTA's threads, every thread gets them.
+template <int NT>
+__device__ __forceinline__ Sum block_join(Sum v, float c, Sum* sh) {
+  v = shfl_join(v, c);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = (threadIdx.x & 31) < NT / 32 ? sh[threadIdx.x & 31] : Sum{-INFINITY, 0.f};
+  v = shfl_join(v, c);
+  __syncthreads();
+  return v;
+}
+
+// The loss of a row whose statistics are known, by a whole CTA.
+template <typename T, int NT>
+__device__ __forceinline__ void write_loss(const DistillArgs& a, const T* row, int64_t r, const Sum& student, Sum* sh, float* sums) {
+  const float c = a.inv_t * kLog2e;
+  const Pair p = fetch_pair<T>(a, row, r, threadIdx.x);
+  // (a thread's own term: relative to itself 1, or NaN, or nothing)
+  const Sum teacher = block_join<NT>(Sum{p.z == p.z ? p.z : -INFINITY, p.z == -INFINITY ? 0.f : p.z == p.z ? ex2((p.z - p.z) * c) : p.z}, c, sh);
+  const float log_s = log_sum(student);
+  const PairTerm t = pair_term(p, teacher, log_sum(teacher), student, log_s, a.inv_t, c);
+  const float loss = warp_sum(t.loss);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = loss;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float all = 0.f;
+    for (int i = 0; i < NT / 32; ++i) all += sums[i];
+    a.loss[r] = all;
+    a.stats[2 * r] = student.m;
+    a.stats[2 * r + 1] = log_s;
+  }
+}
+
+// CTA (r, split): chunks [split * cps, (split + 1) * cps) of row r, dealt to the warps in turn.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) distill_row_kernel(const DistillArgs a, int nchunks, int cps, float2* __restrict__ part) {
+  constexpr int VEC = Elem<T>::kVec;
+  constexpr int Q = kChunkElems / 32 / VEC;   // pieces of a chunk per lane
+  constexpr int U = 4;                        // chunks a turn
+  __shared__ Sum sh[kWarps];
+  __shared__ float sums[kWarps];
+  launch_gate();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, V = (int)a.V;
+  const int64_t r = blockIdx.x;
+  const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+  const int shift = row_shift(row);
+  const float c = a.inv_t * kLog2e;
+  const f32x2 c2 = pack2f(c, c);
+  const int c_end = min(nchunks, (int)(blockIdx.y + 1) * cps);
+  float m = -INFINITY;
+  f32x2 s = 0;
+  for (int c0 = blockIdx.y * cps + warp; c0 < c_end; c0 += kWarps * U) {
+    uint4 w[U][Q];
+    const int first = c0 * kChunkElems - shift, last = (c0 + (U - 1) * kWarps) * kChunkElems - shift;
+    if (first >= 0 && c0 + (U - 1) * kWarps < c_end && last + kChunkElems <= V) {
+      const uint4* p = reinterpret_cast<const uint4*>(row + first) + lane;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) w[u][q] = ld16_stream(p + u * (kWarps * 32 * Q) + q * 32);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          const int at = c0 + u * kWarps;
+          w[u][q] = load_raw<T>(row, at < c_end ? at * kChunkElems + (q * 32 + lane) * VEC - shift : V, V, minus_inf<T>());
+        }
+    }
+    float mx = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) mx = fmaxf(mx, raw_max<T, false>(w[u][q]));
+    if (mx > m) {   // (each lane has a maximum of its own)
+      if (m > -INFINITY) {
+        const float f = ex2((m - mx) * c);
+        s = mul2(s, pack2f(f, f));
+      }
+      m = mx;
+    }
+    const float base = -base_of(m);
+    const f32x2 minus_base = pack2f(base, base);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+          float lo, hi;
+          unpack2f(mul2(add2(raw_pair<T>(w[u][q], i), minus_base), c2), lo, hi);
+          s = add2(s, pack2f(ex2(lo), ex2(hi)));
+        }
+  }
+  float lo, hi;
+  unpack2f(s, lo, hi);
+  const Sum whole = block_join<kThreads>(Sum{m, lo + hi}, c, sh);
+  if (part) {
+    if (threadIdx.x == 0) part[r * gridDim.y + blockIdx.y] = make_float2(whole.m, whole.s);
+  } else {
+    write_loss<T, kThreads>(a, row, r, whole, sh, sums);
+  }
+}
+
+// Joins a row's parts.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) distill_finish_kernel(const DistillArgs a, int nsplit, const float2* __restrict__ part) {
+  __shared__ Sum sh[kWarps];
+  __shared__ float sums[kWarps];
+  launch_gate();
+  const int64_t r = blockIdx.x;
+  Sum v{-INFINITY, 0.f};
+  if ((int)threadIdx.x < nsplit) {
+    const float2 p = part[r * nsplit + threadIdx.x];
+    v = Sum{p.x, p.y};
+  }
+  v = block_join<kThreads>(v, a.inv_t * kLog2e, sh);
+  write_loss<T, kThreads>(a, static_cast<const T*>(a.logits) + r * a.ld, r, v, sh, sums);
+}
+
+// The pairs of a row in shared memory, for its gradient.
+struct PairTable {
+  float q[kMaxPairs];
+  int32_t id[kMaxPairs];
+};
+// After the CTA's stores of the elements [begin, end): those of them that are the pairs' tokens.  The first of
+// the pairs with a token adds up all of them.
+template <typename T>
+__device__ __forceinline__ void store_pairs(const DistillArgs& a, const PairTable& t, const Pair& p, const GradRow& g, int begin, int end,
+                                            float c, T* out) {
+  __syncthreads();
+  if (p.id >= 0 && p.id >= begin && p.id < end) {   // (-1: no pair; a segment may begin ahead of the row)
+    float q = 0.f;
+    int first = kMaxPairs;
+    for (int e = 0; e < a.K; ++e)
+      if (t.id[e] == p.id) {
+        q += t.q[e];
+        first = min(first, e);
+      }
+    if (first == (int)threadIdx.x) out[p.id] = Elem<T>::from_float(fmaf(-g.g, q, g.at(p.x, c)));
+  }
+}
+
+// CTA (r, segment): kThreads * U pieces of row r.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) distill_grad_kernel(const DistillArgs a) {
+  constexpr int VEC = Elem<T>::kVec, U = 4;
+  __shared__ Sum sh[kWarps];
+  __shared__ PairTable table;
+  launch_gate();
+  const int64_t r = a.rows - 1 - blockIdx.x;   // from the row that was read last
+  const int V = (int)a.V;
+  const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+  T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
+  const int shift = row_shift(row);
+  const bool aligned = row_shift(out) == shift;
+  const float c = a.inv_t * kLog2e;
+  const int begin = (int)blockIdx.y * (kThreads * U) * VEC - shift, j0 = begin + (int)threadIdx.x * VEC;
+  uint4 w[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = load_raw<T>(row, j0 + u * kThreads * VEC, V, 0);
+  const Pair p = fetch_pair<T>(a, row, r, threadIdx.x);
+  const Sum teacher = block_join<kThreads>(Sum{p.z == p.z ? p.z : -INFINITY, p.z == -INFINITY ? 0.f : p.z == p.z ? ex2((p.z - p.z) * c) : p.z}, c, sh);
+  const float m = a.stats[2 * r], log_s = a.stats[2 * r + 1], weight = a.d_loss[r];
+  const Sum student{m, m == -INFINITY && log_s == 0.f ? 0.f : ex2(log_s * kLog2e)};
+  GradRow g;
+  g.zero = weight == 0.f || empty(teacher) || empty(student);
+  g.g = weight * a.inv_t;
+  g.base = base_of(m);
+  g.scale = g.g / student.s;
+  if ((int)threadIdx.x < a.K) {
+    table.q[threadIdx.x] = p.id < 0 || empty(teacher) ? 0.f : ex2((p.z - base_of(teacher.m)) * c) / teacher.s;
+    table.id[threadIdx.x] = p.id;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int j = j0 + u * kThreads * VEC;
+    if (j >= V) break;
+    float d[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) {
+      float lo, hi;
+      unpack2f(raw_pair<T>(w[u], i), lo, hi);
+      d[2 * i] = g.at(lo, c);
+      d[2 * i + 1] = g.at(hi, c);
+    }
+    store_floats<T, VEC>(out, j, V, aligned, d);
+  }
+  if (!g.zero) store_pairs<T>(a, table, p, g, begin, begin + kThreads * U * VEC, c, out);
+}
+
+// -------------------------------------------------------- loss and gradient from one read
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float remote_float(const float* p, uint32_t rank) {
+  uint32_t local = (uint32_t)__cvta_generic_to_shared(p), at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// Cluster: row r; its CTAs hold kFusedPart elements each.
+template <typename T, bool CLUSTER>
+__global__ void __launch_bounds__(kFusedThreads, 2) distill_fused_kernel(const DistillArgs a, int ctas) {
+  constexpr int VEC = Elem<T>::kVec, U = kFusedValues / VEC, NT = kFusedThreads;
+  __shared__ Sum sh[NT / 32];
+  __shared__ float sums[NT / 32];
+  __shared__ float mine[2];
+  __shared__ PairTable table;
+  launch_gate();
+  const int rank = CLUSTER ? (int)cluster_rank() : 0;
+  const int64_t r = CLUSTER ? blockIdx.x / ctas : blockIdx.x;
+  const int V = (int)a.V;
+  const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+  T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
+  const int shift = row_shift(row);
+  const bool aligned = row_shift(out) == shift;
+  const float c = a.inv_t * kLog2e;
+  const int begin = rank * kFusedPart - shift, j0 = begin + (int)threadIdx.x * VEC;
+  uint4 w[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = load_raw<T>(row, j0 + u * NT * VEC, V, minus_inf<T>());
+  const Pair p = fetch_pair<T>(a, row, r, threadIdx.x);
+  float mx = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u) mx = fmaxf(mx, raw_max<T, false>(w[u]));
+  // both maxima, then both sums
+  Sum part, teacher;
+  {
+    const float a0 = warp_max(mx), b0 = warp_max(p.z);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = Sum{a0, b0};
+    __syncthreads();
+    const Sum v = (threadIdx.x & 31) < NT / 32 ? sh[threadIdx.x & 31] : Sum{-INFINITY, -INFINITY};
+    part.m = warp_max(v.m);
+    teacher.m = warp_max(v.s);
+    __syncthreads();
+  }
+  float e[U][VEC];
+  f32x2 s2 = 0;
+  {
+    const float base = -base_of(part.m);
+    const f32x2 minus_base = pack2f(base, base), c2 = pack2f(c, c);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) {
+        float lo, hi;
+        unpack2f(mul2(add2(raw_pair<T>(w[u], i), minus_base), c2), lo, hi);
+        e[u][2 * i] = ex2(lo);
+        e[u][2 * i + 1] = ex2(hi);
+        s2 = add2(s2, pack2f(e[u][2 * i], e[u][2 * i + 1]));
+      }
+  }
+  {
+    float lo, hi;
+    unpack2f(s2, lo, hi);
+    const float a0 = warp_sum(lo + hi), b0 = warp_sum(ex2((p.z - base_of(teacher.m)) * c));
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = Sum{a0, b0};
+    __syncthreads();
+    const Sum v = (threadIdx.x & 31) < NT / 32 ? sh[threadIdx.x & 31] : Sum{0.f, 0.f};
+    part.s = warp_sum(v.m);
+    teacher.s = warp_sum(v.s);
+  }
+  Sum student = part;
+  if (CLUSTER) {
+    if (threadIdx.x == 0) {
+      mine[0] = part.m;
+      mine[1] = part.s;
+    }
+    cluster_sync();
+    const int lane = threadIdx.x & 31;
+    Sum v{-INFINITY, 0.f};
+    if (lane < ctas) v = Sum{remote_float(&mine[0], lane), remote_float(&mine[1], lane)};
+    student = shfl_join(v, c);
+    cluster_sync();   // no CTA leaves while another reads its sums
+  }
+  const float log_s = log_sum(student), log_teacher = log_sum(teacher);
+  const PairTerm t = pair_term(p, teacher, log_teacher, student, log_s, a.inv_t, c);
+  if ((int)threadIdx.x < a.K) {
+    table.q[threadIdx.x] = t.q;
+    table.id[threadIdx.x] = p.id;
+  }
+  const float loss = warp_sum(t.loss);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = loss;
+  const float weight = a.d_loss[r];
+  GradRow g;
+  g.zero = weight == 0.f || empty(teacher) || empty(student);
+  g.g = weight * a.inv_t;
+  g.base = base_of(student.m);
+  g.scale = g.g / student.s;
+  // (values relative to the CTA's own maximum)
+  const float scale = g.zero || (part.m == -INFINITY && part.s == 0.f) ? 0.f : g.scale * (part.m == -INFINITY ? 1.f : ex2((part.m - g.base) * c));
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int j = j0 + u * NT * VEC;
+    if (j >= V) break;
+    float d[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) d[i] = scale == 0.f ? 0.f : e[u][i] * scale;
+    store_floats<T, VEC, true>(out, j, V, aligned, d);
+  }
+  __syncthreads();
+  if (!g.zero) store_pairs<T>(a, table, p, g, begin, begin + kFusedPart, c, out);
+  if (rank == 0 && threadIdx.x == 0) {
+    float all = 0.f;
+    for (int i = 0; i < NT / 32; ++i) all += sums[i];
+    a.loss[r] = all;
+    a.stats[2 * r] = student.m;
+    a.stats[2 * r + 1] = log_s;
+  }
+}
+
+// ------------------------------------------------------------------------------ host
+int64_t chunk_count(int64_t V, int dtype) {
+  return (V + (dtype == OLSGD_F32 ? 3 : 7) + kChunkElems - 1) / kChunkElems;
+}
+struct Plan {
+  int nchunks, cps, nsplit;   // chunks of a row; chunks per part; parts
+};
+// Parts of a row: as many as give every multiprocessor four CTAs, none shorter than a turn of a CTA's warps.
+Plan plan(int64_t rows, int64_t V, int dtype) {
+  Plan p;
+  p.nchunks = (int)chunk_count(V, dtype);
+  const int64_t want = (4LL * 148 + rows - 1) / rows, most = (p.nchunks + kWarps * 4 - 1) / (kWarps * 4);
+  int64_t n = want < most ? want : most;
+  if (n > kMaxSplit) n = kMaxSplit;
+  if (n < 1) n = 1;
+  p.cps = (int)((p.nchunks + n - 1) / n);
+  p.nsplit = (p.nchunks + p.cps - 1) / p.cps;
+  return p;
+}
+// CTAs of a cluster that hold a row; 0: too long.  aligned: all rows start on a 16-byte boundary.
+int cluster_of(int64_t V, int dtype, bool aligned) {
+  const int64_t n = (V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7) + kFusedPart - 1) / kFusedPart;
+  return n > kMaxCluster ? 0 : (int)n;
+}
+template <typename T>
+bool rows_aligned(const DistillArgs& a) {
+  return ((reinterpret_cast<uintptr_t>(a.logits) | (uintptr_t)(a.ld * sizeof(T))) & 15) == 0;
+}
+
+template <typename T, bool LOSS, bool GRAD>
+cudaError_t warp_rows(const DistillArgs& a, cudaStream_t s) {
+  const dim3 grid((unsigned)((a.rows + kWarps - 1) / kWarps));
+  auto k = a.V <= 32    ? distill_warp_kernel<T, 1, LOSS, GRAD>
+           : a.V <= 256 ? distill_warp_kernel<T, 8, LOSS, GRAD>
+                        : distill_warp_kernel<T, 32, LOSS, GRAD>;
+  return launch_chained(k, grid, dim3(kThreads), 0, s, a);
+}
+
+template <typename T>
+cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
+  if (a.V <= kWarpRowMax) return warp_rows<T, false, true>(a, s);
+  const int64_t pieces = (a.V + (rows_aligned<T>(a) ? 1 : 2) * (Elem<T>::kVec - 1)) / Elem<T>::kVec, per = kThreads * 4;
+  return launch_chained(distill_grad_kernel<T>, dim3((unsigned)a.rows, (unsigned)((pieces + per - 1) / per)), dim3(kThreads), 0, s, a);
+}
+
+template <typename T>
+cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
+  if (a.V <= kWarpRowMax) return a.d_loss ? warp_rows<T, true, true>(a, s) : warp_rows<T, true, false>(a, s);
+  const int ctas = a.d_loss ? cluster_of(a.V, a.dtype, rows_aligned<T>(a)) : 0;
+  if (ctas == 1) return launch_chained(distill_fused_kernel<T, false>, dim3((unsigned)a.rows), dim3(kFusedThreads), 0, s, a, 1);
+  if (ctas > 1) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(a.rows * ctas));
+    cfg.blockDim = dim3(kFusedThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = g_launch_overlap ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, distill_fused_kernel<T, true>, a, ctas);
+  }
+  const Plan p = plan(a.rows, a.V, a.dtype);
+  float2* part = p.nsplit > 1 ? static_cast<float2*>(a.ws) : nullptr;
+  cudaError_t e = launch_chained(distill_row_kernel<T>, dim3((unsigned)a.rows, (unsigned)p.nsplit), dim3(kThreads), 0, s, a, p.nchunks, p.cps, part);
+  if (e == cudaSuccess && part)
+    e = launch_chained(distill_finish_kernel<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a, p.nsplit, (const float2*)part);
+  return e == cudaSuccess && a.d_loss ? gradient<T>(a, s) : e;
+}
+
+}  // namespace
+
+size_t distill_workspace(int dtype, int64_t rows, int64_t V, bool gradient) {
+  if (V <= kWarpRowMax || (gradient && cluster_of(V, dtype, false))) return 0;   // (whatever the alignment)
+  const Plan p = plan(rows, V, dtype);
+  return p.nsplit == 1 ? 0 : (size_t)rows * p.nsplit * sizeof(float2);
+}
+
+cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s) {
+  switch (a.dtype) {
+    case OLSGD_F32: return forward<float>(a, s);
+    case OLSGD_BF16: return forward<__nv_bfloat16>(a, s);
+    default: return forward<__half>(a, s);
+  }
+}
+cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s) {
+  switch (a.dtype) {
+    case OLSGD_F32: return gradient<float>(a, s);
+    case OLSGD_BF16: return gradient<__nv_bfloat16>(a, s);
+    default: return gradient<__half>(a, s);
+  }
+}
+
+}  // namespace olsgd

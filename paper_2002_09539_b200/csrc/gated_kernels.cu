@@ -1158,6 +1158,9 @@ cudaError_t operators_status(int* status, cudaStream_t s) {
     const int zero = 0;
     OLSGD_STEP(cudaMemcpyToSymbol(g_operator_status, &zero, sizeof(int)));
   }
+  int product = 0;
+  OLSGD_STEP(product_status(&product));
+  if (*status == 0) *status = product;
   return cudaSuccess;
 }
 

@@ -34,6 +34,12 @@ bool aligned_to(const void* p, size_t a) { return p && (reinterpret_cast<uintptr
     if (cond) return refuse(OLSGD_EINVAL, __VA_ARGS__); \
   } while (0)
 
+#define OLSGD_TRY(call)                      \
+  do {                                       \
+    const olsgd_status st_ = (call);         \
+    if (st_ != OLSGD_OK) return st_;         \
+  } while (0)
+
 constexpr int64_t kMaxVocab = 1LL << 27;
 constexpr int64_t kMaxRows = 0x7FFFFFFF;
 
@@ -80,11 +86,54 @@ olsgd_status check_embedding(int32_t m, int64_t T, int64_t V, int64_t D, int32_t
   return OLSGD_OK;
 }
 
-#define OLSGD_TRY(call)                      \
-  do {                                       \
-    const olsgd_status st_ = (call);         \
-    if (st_ != OLSGD_OK) return st_;         \
-  } while (0)
+olsgd_status check_experts(int32_t m, int64_t T, int64_t E) {
+  OLSGD_REFUSE_IF(m < 1 || m > 65535, "m must be in [1, 65535]");
+  OLSGD_REFUSE_IF(T < 0 || T > (1 << 24), "T must be in [0, 2^24]");
+  OLSGD_REFUSE_IF(E < 1 || E > OLSGD_MAX_EXPERTS, "E must be in [1, %d]", OLSGD_MAX_EXPERTS);
+  return OLSGD_OK;
+}
+olsgd_status check_combine(int32_t m, int64_t T, int32_t k, int64_t R, int64_t D, int32_t dtype) {
+  OLSGD_REFUSE_IF(m < 1 || m > 65535, "m must be in [1, 65535]");
+  OLSGD_REFUSE_IF(k < 1 || T < 0 || T > kMaxRows / k || R < 0 || R > kMaxRows, "k must be positive, T k and R at most 2^31 - 1");
+  OLSGD_REFUSE_IF(D < 1 || D > (1 << 24), "D must be in [1, 2^24]");
+  OLSGD_REFUSE_IF(!is_dtype(dtype), "unknown element type %d", (int)dtype);
+  return OLSGD_OK;
+}
+olsgd_status check_product(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F) {
+  OLSGD_REFUSE_IF(E < 1 || E > OLSGD_MAX_EXPERTS, "E must be in [1, %d]", OLSGD_MAX_EXPERTS);
+  OLSGD_REFUSE_IF(m < 1 || (int64_t)m * E > 65535, "m must be positive, m E at most 65535");
+  OLSGD_REFUSE_IF(R < 0 || R > kMaxRows / m, "R must not be negative, m R at most 2^31 - 1");
+  OLSGD_REFUSE_IF(D < 1 || D > (1 << 24) || F < 1 || F > (1 << 24), "D and F must be in [1, 2^24]");
+  return OLSGD_OK;
+}
+olsgd_status check_weights(const ExpertOperand& w, int64_t m, int64_t E, int64_t F, int64_t D) {
+  OLSGD_TRY(check_operand(GatedOperand{w.p, w.expert_stride, w.row_stride}, "w", E, F, D));
+  const int64_t expert = (F > 1 ? (F - 1) * w.row_stride : 0) + D;
+  OLSGD_REFUSE_IF(m > 1 && (w.worker_stride < (E > 1 ? (E - 1) * w.expert_stride : 0) + expert || w.worker_stride > (1LL << 38)),
+                  "w: workers must not overlap");
+  return OLSGD_OK;
+}
+olsgd_status check_distill(int32_t dtype, int64_t rows, int64_t V, int64_t row_stride, const int32_t* ids, const void* teacher,
+                           int32_t teacher_dtype, int32_t K, float temperature, const void* logits) {
+  OLSGD_REFUSE_IF(!is_dtype(teacher_dtype), "unknown element type %d of the teacher", (int)teacher_dtype);
+  OLSGD_REFUSE_IF(K < 1 || K > OLSGD_MAX_TEACHER, "K must be in [1, %d]", OLSGD_MAX_TEACHER);
+  OLSGD_REFUSE_IF(!(temperature >= 0x1p-20f && temperature <= 0x1p20f), "temperature must be in [2^-20, 2^20]");
+  if (rows == 0) return OLSGD_OK;
+  OLSGD_REFUSE_IF(row_stride < V, "row_stride must be at least V");
+  OLSGD_REFUSE_IF(!aligned_to(logits, elem_size(dtype)), "logits must be non-null and aligned to their type");
+  OLSGD_REFUSE_IF(!aligned_to(ids, 4), "ids must be non-null and 4-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(teacher, elem_size(teacher_dtype)), "teacher must be non-null and aligned to its type");
+  return OLSGD_OK;
+}
+olsgd_status check_distill_grad(int32_t dtype, int64_t V, int64_t row_stride, const void* logits, const float* d_loss,
+                                const void* d_logits, int64_t d_row_stride) {
+  OLSGD_REFUSE_IF(!aligned_to(d_loss, 4), "d_loss must be non-null and 4-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(d_logits, elem_size(dtype)) || d_row_stride < V,
+                  "d_logits must be non-null and aligned to its type, d_row_stride at least V");
+  OLSGD_REFUSE_IF(logits == d_logits && row_stride != d_row_stride, "d_logits in place of the logits needs the same stride");
+  return OLSGD_OK;
+}
+
 
 }  // namespace
 
@@ -297,6 +346,194 @@ olsgd_status olsgd_embedding_backward(int32_t m, int64_t T, int64_t V, int64_t D
   const EmbeddingGradArgs a{dtype, d_table_dtype, m, T, V, D, d_out, d_out_worker_stride, d_out_row_stride, ids, scale,
                             d_table, d_table_worker_stride, workspace};
   return launched(launch_embedding_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_embedding_backward");
+}
+
+// ----------------------------------------------------------------------------------- experts
+
+olsgd_status olsgd_expert_route_workspace(int32_t m, int64_t T, int64_t E, size_t* out_bytes) {
+  OLSGD_REFUSE_IF(!out_bytes, "out_bytes is NULL");
+  OLSGD_TRY(check_experts(m, T, E));
+  *out_bytes = T == 0 ? 0 : route_workspace(m, T, E);
+  return OLSGD_OK;
+}
+
+olsgd_status olsgd_expert_route(int32_t m, int64_t T, int64_t E, int32_t dtype, const void* logits,
+                                int64_t row_stride, int32_t k, int32_t normalise, float* weights,
+                                int32_t* ids, int32_t* places, int32_t* tokens, int32_t* offsets,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  OLSGD_TRY(check_experts(m, T, E));
+  OLSGD_REFUSE_IF(!is_dtype(dtype), "unknown element type %d", (int)dtype);
+  OLSGD_REFUSE_IF(k < 1 || k > OLSGD_MAX_TOP || k > E, "k must be in [1, min(E, %d)]", OLSGD_MAX_TOP);
+  OLSGD_REFUSE_IF(T * k > kMaxRows, "T k must be at most 2^31 - 1");
+  OLSGD_REFUSE_IF(!aligned_to(offsets, 4), "offsets must be non-null and 4-byte aligned");
+  if (T == 0)
+    return launched(cudaMemsetAsync(offsets, 0, (size_t)m * (E + 1) * sizeof(int32_t), static_cast<cudaStream_t>(stream)), "olsgd_expert_route");
+  OLSGD_REFUSE_IF(row_stride < E, "row_stride must be at least E");
+  OLSGD_REFUSE_IF(!aligned_to(logits, elem_size(dtype)), "logits must be non-null and aligned to their type");
+  OLSGD_REFUSE_IF(!aligned_to(weights, 4) || !aligned_to(ids, 4) || !aligned_to(places, 4) || !aligned_to(tokens, 4),
+                  "weights, ids, places and tokens must be non-null and 4-byte aligned");
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, route_workspace(m, T, E)));
+  const RouteArgs a{dtype, m, T, E, logits, row_stride, k, normalise != 0, weights, ids, places, tokens, offsets, workspace};
+  return launched(launch_route(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_route");
+}
+
+olsgd_status olsgd_expert_route_backward(int64_t rows, int64_t E, int32_t dtype, const float* d_weights,
+                                         const void* logits, int64_t row_stride, int32_t k,
+                                         int32_t normalise, const int32_t* ids, const float* weights,
+                                         void* d_logits, void* stream) {
+  OLSGD_TRY(check_experts(1, 0, E));
+  OLSGD_REFUSE_IF(rows < 0 || rows > kMaxRows, "rows must be in [0, 2^31 - 1]");
+  OLSGD_REFUSE_IF(!is_dtype(dtype), "unknown element type %d", (int)dtype);
+  OLSGD_REFUSE_IF(k < 1 || k > OLSGD_MAX_TOP || k > E, "k must be in [1, min(E, %d)]", OLSGD_MAX_TOP);
+  if (rows == 0) return OLSGD_OK;
+  OLSGD_REFUSE_IF(normalise == 0 && (!aligned_to(logits, elem_size(dtype)) || row_stride < E),
+                  "logits must be non-null and aligned to their type, row_stride at least E");
+  OLSGD_REFUSE_IF(!aligned_to(d_weights, 4) || !aligned_to(ids, 4) || !aligned_to(weights, 4),
+                  "d_weights, ids and weights must be non-null and 4-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(d_logits, elem_size(dtype)) || d_logits == logits,
+                  "d_logits must be non-null, aligned to its type and apart from the logits");
+  const RouteGradArgs a{dtype, rows, (int)E, k, normalise != 0, logits, row_stride, ids, weights, d_weights, d_logits};
+  return launched(launch_route_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_route_backward");
+}
+
+olsgd_status olsgd_expert_combine(int32_t m, int64_t T, int32_t k, int64_t R, int64_t D, int32_t dtype,
+                                  const void* rows, int64_t rows_worker_stride, int64_t rows_row_stride,
+                                  const int32_t* places, const float* weights, void* y, void* stream) {
+  OLSGD_TRY(check_combine(m, T, k, R, D, dtype));
+  if (T == 0) return OLSGD_OK;
+  if (R > 0) OLSGD_TRY(check_operand(GatedOperand{rows, rows_worker_stride, rows_row_stride}, "rows", m, R, D, elem_size(dtype)));
+  OLSGD_REFUSE_IF(!aligned_to(places, 4) || (weights && !aligned_to(weights, 4)), "places must be non-null, places and weights 4-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(y, elem_size(dtype)), "y must be non-null and aligned to its type");
+  const CombineArgs a{dtype, k, m, T, R, D, rows, rows_worker_stride, rows_row_stride, places, weights, y};
+  return launched(launch_combine(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_combine");
+}
+
+olsgd_status olsgd_expert_combine_backward(int32_t m, int64_t T, int32_t k, int64_t R, int64_t D,
+                                           int32_t dtype, const void* d_y, int64_t d_y_worker_stride,
+                                           int64_t d_y_row_stride, const void* rows,
+                                           int64_t rows_worker_stride, int64_t rows_row_stride,
+                                           const int32_t* places, const int32_t* tokens,
+                                           const float* weights, void* d_rows, float* d_weights,
+                                           void* stream) {
+  OLSGD_TRY(check_combine(m, T, k, R, D, dtype));
+  if (T == 0 && R == 0) return OLSGD_OK;
+  if (R > 0) {
+    OLSGD_TRY(check_operand(GatedOperand{rows, rows_worker_stride, rows_row_stride}, "rows", m, R, D, elem_size(dtype)));
+    OLSGD_REFUSE_IF(!aligned_to(tokens, 4), "tokens must be non-null and 4-byte aligned");
+    OLSGD_REFUSE_IF(!aligned_to(d_rows, elem_size(dtype)), "d_rows must be non-null and aligned to its type");
+  }
+  if (T > 0) {
+    OLSGD_TRY(check_operand(GatedOperand{d_y, d_y_worker_stride, d_y_row_stride}, "d_y", m, T, D, elem_size(dtype)));
+    OLSGD_REFUSE_IF(!aligned_to(places, 4) || !aligned_to(weights, 4) || !aligned_to(d_weights, 4),
+                    "places, weights and d_weights must be non-null and 4-byte aligned");
+  }
+  const CombineGradArgs a{dtype, k, m, T, R, D, d_y, d_y_worker_stride, d_y_row_stride, rows, rows_worker_stride, rows_row_stride,
+                          places, tokens, weights, d_rows, d_weights};
+  return launched(launch_combine_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_combine_backward");
+}
+
+olsgd_status olsgd_expert_product_workspace(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F,
+                                            int32_t backward, int32_t aligned, size_t* out_bytes) {
+  OLSGD_REFUSE_IF(!out_bytes, "out_bytes is NULL");
+  OLSGD_TRY(check_product(m, R, E, D, F));
+  *out_bytes = R == 0 ? 0 : product_workspace(ProductShape{m, R, E, D, F, false}, backward != 0, aligned == 0);
+  return OLSGD_OK;
+}
+
+olsgd_status olsgd_expert_product(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F, int32_t dtype,
+                                  const void* x, int64_t x_worker_stride, int64_t x_row_stride,
+                                  const void* w, int64_t w_worker_stride,
+                                  int64_t w_expert_stride, int64_t w_row_stride,
+                                  const int32_t* offsets, void* y, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  OLSGD_TRY(check_product(m, R, E, D, F));
+  OLSGD_REFUSE_IF(dtype != OLSGD_BF16 && dtype != OLSGD_F16, "products by expert take bf16 and fp16 operands");
+  if (R == 0) return OLSGD_OK;
+  ProductForward a;
+  static_cast<ProductShape&>(a) = ProductShape{m, R, E, D, F, dtype == OLSGD_F16};
+  a.x = GatedOperand{x, x_worker_stride, x_row_stride};
+  a.w = ExpertOperand{w, w_worker_stride, w_expert_stride, w_row_stride};
+  OLSGD_TRY(check_operand(a.x, "x", m, R, D));
+  OLSGD_TRY(check_weights(a.w, m, E, F, D));
+  OLSGD_REFUSE_IF(!aligned_to(offsets, 4), "offsets must be non-null and 4-byte aligned");
+  OLSGD_REFUSE_IF(!aligned_to(y, 2), "y must be non-null and 2-byte aligned");
+  a.offsets = offsets;
+  a.y = y;
+  a.ws = workspace;
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, product_workspace(a, false, product_needs_copies(a, a.x, a.w, nullptr))));
+  return launched(launch_product(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_product");
+}
+
+olsgd_status olsgd_expert_product_backward(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F,
+                                           int32_t dtype, const void* d_y, int64_t d_y_worker_stride,
+                                           int64_t d_y_row_stride, const void* x, int64_t x_worker_stride,
+                                           int64_t x_row_stride, const void* w, int64_t w_worker_stride,
+                                           int64_t w_expert_stride, int64_t w_row_stride, const int32_t* offsets, void* d_x,
+                                           void* d_w, void* workspace, size_t workspace_bytes,
+                                           void* stream) {
+  OLSGD_TRY(check_product(m, R, E, D, F));
+  OLSGD_REFUSE_IF(dtype != OLSGD_BF16 && dtype != OLSGD_F16, "products by expert take bf16 and fp16 operands");
+  OLSGD_REFUSE_IF((d_x && !aligned_to(d_x, 2)) || (d_w && !aligned_to(d_w, 2)), "d_x and d_w must be 2-byte aligned");
+  if (R == 0) {   // no rows: the weights' gradients are zero
+    if (!d_w) return OLSGD_OK;
+    return launched(cudaMemsetAsync(d_w, 0, (size_t)m * E * F * D * 2, static_cast<cudaStream_t>(stream)), "olsgd_expert_product_backward");
+  }
+  ProductBackward a;
+  static_cast<ProductShape&>(a) = ProductShape{m, R, E, D, F, dtype == OLSGD_F16};
+  a.dy = GatedOperand{d_y, d_y_worker_stride, d_y_row_stride};
+  a.x = GatedOperand{x, x_worker_stride, x_row_stride};
+  a.w = ExpertOperand{w, w_worker_stride, w_expert_stride, w_row_stride};
+  OLSGD_TRY(check_operand(a.dy, "d_y", m, R, F));
+  OLSGD_TRY(check_operand(a.x, "x", m, R, D));
+  OLSGD_TRY(check_weights(a.w, m, E, F, D));
+  OLSGD_REFUSE_IF(!aligned_to(offsets, 4), "offsets must be non-null and 4-byte aligned");
+  if (!d_x && !d_w) return OLSGD_OK;
+  a.offsets = offsets;
+  a.dx = d_x;
+  a.dw = d_w;
+  a.ws = workspace;
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, product_workspace(a, true, product_needs_copies(a, a.x, a.w, &a.dy))));
+  return launched(launch_product_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_product_backward");
+}
+
+// ------------------------------------------------------------------------------ distillation
+
+olsgd_status olsgd_distill_workspace(int32_t dtype, int64_t rows, int64_t V, int32_t gradient, size_t* out_bytes) {
+  OLSGD_REFUSE_IF(!out_bytes, "out_bytes is NULL");
+  OLSGD_TRY(check_rows(dtype, rows, V));
+  *out_bytes = rows == 0 ? 0 : distill_workspace(dtype, rows, V, gradient != 0);
+  return OLSGD_OK;
+}
+
+olsgd_status olsgd_distill(const void* logits, int32_t dtype, int64_t rows, int64_t V, int64_t row_stride,
+                           const int32_t* ids, const void* teacher, int32_t teacher_dtype, int32_t K,
+                           float temperature, const float* d_loss, float* loss, float* stats,
+                           void* d_logits, int64_t d_row_stride, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  OLSGD_TRY(check_rows(dtype, rows, V));
+  OLSGD_TRY(check_distill(dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, temperature, logits));
+  if (rows == 0) return OLSGD_OK;
+  OLSGD_REFUSE_IF(!aligned_to(loss, 4) || !aligned_to(stats, 4), "loss and stats must be non-null and 4-byte aligned");
+  if (d_loss) OLSGD_TRY(check_distill_grad(dtype, V, row_stride, logits, d_loss, d_logits, d_row_stride));
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, distill_workspace(dtype, rows, V, d_loss != nullptr)));
+  const DistillArgs a{logits, dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, (float)(1.0 / temperature),
+                      d_loss, loss, stats, d_logits, d_row_stride, workspace};
+  return launched(launch_distill(a, static_cast<cudaStream_t>(stream)), "olsgd_distill");
+}
+
+olsgd_status olsgd_distill_backward(const float* d_loss, const void* logits, int32_t dtype, int64_t rows,
+                                    int64_t V, int64_t row_stride, const int32_t* ids, const void* teacher,
+                                    int32_t teacher_dtype, int32_t K, float temperature,
+                                    const float* stats, void* d_logits, int64_t d_row_stride,
+                                    void* stream) {
+  OLSGD_TRY(check_rows(dtype, rows, V));
+  OLSGD_TRY(check_distill(dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, temperature, logits));
+  if (rows == 0) return OLSGD_OK;
+  OLSGD_REFUSE_IF(!aligned_to(stats, 4), "stats must be non-null and 4-byte aligned");
+  OLSGD_TRY(check_distill_grad(dtype, V, row_stride, logits, d_loss, d_logits, d_row_stride));
+  const DistillArgs a{logits, dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, (float)(1.0 / temperature),
+                      d_loss, nullptr, const_cast<float*>(stats), d_logits, d_row_stride, nullptr};
+  return launched(launch_distill_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_distill_backward");
 }
 
 olsgd_status olsgd_operators_join(void* stream) {

@@ -84,6 +84,101 @@ struct EmbeddingGradArgs {
 size_t embedding_workspace(int64_t m, int64_t T, int64_t D);
 cudaError_t launch_embedding_backward(const EmbeddingGradArgs& a, cudaStream_t s);
 
+// ---- expert_kernels.cu --------------------------------------------------------
+struct RouteArgs {
+  int dtype;
+  int64_t m, T, E;
+  const void* logits;
+  int64_t ld;
+  int k, normalise;
+  float* weights;
+  int32_t *ids, *places, *tokens, *offsets;
+  void* ws;
+};
+size_t route_workspace(int64_t m, int64_t T, int64_t E);
+cudaError_t launch_route(const RouteArgs& a, cudaStream_t s);
+struct RouteGradArgs {
+  int dtype;
+  int64_t rows;
+  int E, k, normalise;
+  const void* logits;
+  int64_t ld;
+  const int32_t* ids;
+  const float *weights, *d_weights;
+  void* d_logits;
+};
+cudaError_t launch_route_backward(const RouteGradArgs& a, cudaStream_t s);
+struct CombineArgs {
+  int dtype, k;
+  int64_t m, T, R, D;
+  const void* rows;
+  int64_t rows_worker, rows_row;
+  const int32_t* places;
+  const float* weights;
+  void* y;
+};
+cudaError_t launch_combine(const CombineArgs& a, cudaStream_t s);
+struct CombineGradArgs {
+  int dtype, k;
+  int64_t m, T, R, D;
+  const void* d_y;
+  int64_t dy_worker, dy_row;
+  const void* rows;
+  int64_t rows_worker, rows_row;
+  const int32_t *places, *tokens;
+  const float* weights;
+  void* d_rows;
+  float* d_weights;
+};
+cudaError_t launch_combine_backward(const CombineGradArgs& a, cudaStream_t s);
+
+// ---- product_kernels.cu -------------------------------------------------------
+struct ProductShape {
+  int64_t m, R, E, D, F;
+  bool f16;
+};
+struct ExpertOperand {     // [m][E][rows][cols], cols contiguous; strides in elements
+  const void* p;
+  int64_t worker_stride, expert_stride, row_stride;
+};
+struct ProductForward : ProductShape {
+  GatedOperand x;
+  ExpertOperand w;
+  const int32_t* offsets;
+  void *y, *ws;
+};
+struct ProductBackward : ProductShape {
+  GatedOperand dy, x;
+  ExpertOperand w;
+  const int32_t* offsets;
+  void *dx, *dw, *ws;
+};
+// Whether an operand has to be copied to rows that TMA takes (dy: of the backward call).
+bool product_needs_copies(const ProductShape& d, const GatedOperand& x, const ExpertOperand& w, const GatedOperand* dy);
+size_t product_workspace(const ProductShape& d, bool backward, bool copies);
+cudaError_t launch_product(ProductForward a, cudaStream_t s);
+cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s);
+cudaError_t product_status(int* status);   // of its bounded waits, for operators_status
+
+// ---- distill_kernels.cu -------------------------------------------------------
+struct DistillArgs {
+  const void* logits;
+  int dtype;
+  int64_t rows, V, ld;
+  const int32_t* ids;
+  const void* teacher;
+  int teacher_dtype, K;
+  float inv_t;               // 1 / temperature
+  const float* d_loss;       // or null: no gradient
+  float *loss, *stats;
+  void* d_logits;
+  int64_t ldd;
+  void* ws;
+};
+size_t distill_workspace(int dtype, int64_t rows, int64_t V, bool gradient);
+cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s);
+cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s);
+
 // Joins the stream; *status: OLSGD_OK, or what a bounded wait left since the last call.
 cudaError_t operators_status(int* status, cudaStream_t s);
 

@@ -1,0 +1,740 @@
+// Products grouped by expert on the fifth-generation tensor cores, worker-batched.  Rows
+// offsets[e] .. offsets[e + 1] - 1 of a worker belong to its expert e:
+//   y_r = W_e x_r           (forward)        x [m][R][D], W [m][E][F][D], y [m][R][F]
+//   dx_r = W_e^T dy_r,  dW_e = sum over the expert's rows of dy_r x_r^T      (backward)
+// 16-bit operands, fp32 accumulation in tensor memory, one rounding of each result.
+//
+// The sizes of the groups are known to the GPU alone.  The kernel is persistent; each CTA turns the offsets into a table
+// of row tiles in its shared memory first.
+//
+// One kernel, three modes.  Warp 0 feeds a ring of shared-memory stages with TMA, warp 1 issues the MMAs into
+// accumulators in tensor memory, eight warps empty them.  A tile has 128 features and two accumulators take turns,
+// or it has 256, as two MMAs that share their B (HALVES = 2): then a CTA takes in 64 KB for 256 x 256 x 64
+// multiply-adds, which L2 keeps up with, and the halves are emptied one by one while the next tile's first MMAs run.
+//   FORWARD   A = W (K-major), B = the tile's rows of x (K-major)
+//   DX        A = W read along D (MN-major), B = the tile's rows of dy
+//   DW        A = dy, B = x, both read along their features (MN-major), K = the group's rows
+// The weights are the MMA's M, so that the ragged dimension is its N: a tile of n rows costs n rounded
+// up to 16, not to 128, in MMAs and in loads.  Rows of other groups that come
+// with a box end up in columns of the accumulator that are not stored.  Along K they would be
+// summed: there a group's rows are loaded in boxes of 64, then of 16, and the last n mod 16 come from a copy
+// padded with zeros, which a small kernel makes ahead.
+//
+// TMA wants 16-byte row pitches: operands that do not have them are copied to padded rows in
+// the workspace first.  Every wait is bounded, as in the library's other tensor-core kernels.
+#include "operator_tiles.cuh"
+
+namespace olsgd {
+namespace {
+
+enum Mode { FORWARD = 0, DX = 1, DW = 2 };
+constexpr int kGroup = 8;            // DW: row tiles walked together (operand reuse in L2)
+constexpr int kSmallBox = 16;        // rows of a box of B where a tile is not full; K of an MMA
+constexpr int kMaxGroups = 2048;     // of a launch of FORWARD or DX: its table's room
+constexpr int kMaxStarts = 2 * kMaxGroups;
+
+__device__ int g_product_status;     // a bounded wait gave up (olsgd_operators_join)
+
+// a, b: boxes of whole tiles; _small: of 16 rows; DW: _tail: of the copies of last rows.
+struct alignas(64) ProductMaps {
+  CUtensorMap a, b, a_small, b_small, a_tail, b_tail;
+};
+struct ProductArgs {
+  int num_kb, k_extent;       // FORWARD, DX: K in blocks of 64, and in elements
+  int m_tiles, n_tiles;       // tiles of the features; DW: and of the columns
+  int features, cols;         // rows of A in all; DW: columns of the output
+  int R, E, m, first_worker;  // rows and experts of a worker; workers of this launch
+  int f16;
+  int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
+  const int32_t* offsets;     // [workers][E + 1]
+  void* out;
+};
+
+template <int STAGES>
+struct Control {
+  uint64_t full[STAGES], empty[STAGES];
+  uint64_t acc_full[2], acc_empty[2];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+// FORWARD, DX: where the rows of each expert begin, [m][E + 1], and the first row tile of each group.
+struct Table {
+  int32_t start[kMaxStarts];
+  int32_t first[kMaxGroups + 1];
+  int32_t sums[kThreads / 32];
+};
+
+// Rows [x, y) of a group, whatever the offsets hold.
+__device__ __forceinline__ int2 group_rows(const int32_t* offsets, int group, int E, int R) {
+  const int32_t* o = offsets + group + group / E;   // (a worker has E + 1 of them)
+  const int a = min(max(o[0], 0), R);
+  return make_int2(a, min(max(o[1], a), R));
+}
+
+// ------------------------------------------------------------------------- last rows
+// The n mod 16 last rows of each group in 16 rows of zeros: [groups][16][pitch] of dy and of x.
+struct TailOperand {
+  const uint16_t* p;
+  int64_t worker, row;       // elements between workers and rows
+  uint16_t* out;
+  int64_t cols;
+};
+struct TailArgs {
+  TailOperand op[2];
+  const int32_t* offsets;
+  int E, R;
+};
+__global__ void __launch_bounds__(256) tail_kernel(const TailArgs a) {
+  launch_gate();
+  const TailOperand& o = a.op[blockIdx.y];
+  const int group = blockIdx.x, worker = group / a.E, lane = threadIdx.x & 31;
+  const int2 rows = group_rows(a.offsets, group, a.E, a.R);
+  const int n = (rows.y - rows.x) % kSmallBox;
+  if (n == 0) return;
+  for (int r = threadIdx.x >> 5; r < kSmallBox; r += 8) {
+    const uint16_t* src = o.p + worker * o.worker + (int64_t)(rows.y - n + r) * o.row;
+    const int pieces = (int)((o.cols + 7) / 8);
+    uint4* dst = reinterpret_cast<uint4*>(o.out) + ((int64_t)group * kSmallBox + r) * pieces;
+    for (int c = lane; c < pieces; c += 32)
+      dst[c] = r < n ? load_raw<__nv_bfloat16, int64_t>(reinterpret_cast<const __nv_bfloat16*>(src), c * 8, o.cols, 0) : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ------------------------------------------------------------------------------- products
+// By a whole CTA.  Offsets that fall, or leave [0, R], are taken as the largest so far, so that groups never overlap.
+__device__ __forceinline__ void make_table(const ProductArgs& g, Table& tb, int bn) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, width = g.E + 1, groups = g.m * g.E;
+  for (int w = warp; w < g.m; w += kThreads / 32) {
+    int most = 0;
+    for (int e0 = 0; e0 < width; e0 += 32) {
+      int v = e0 + lane < width ? min(max(g.offsets[(int64_t)(g.first_worker + w) * width + e0 + lane], 0), g.R) : 0;
+      v = max(v, most);
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, v, off);
+        if (lane >= off) v = max(v, up);
+      }
+      if (e0 + lane < width) tb.start[w * width + e0 + lane] = v;
+      most = __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  __syncthreads();
+  const auto tiles_of = [&](int i) {
+    const int32_t* s = tb.start + i + i / g.E;
+    return (s[1] - s[0] + bn - 1) / bn;
+  };
+  const int per = (groups + kThreads - 1) / kThreads, begin = min(groups, (int)threadIdx.x * per), end = min(groups, begin + per);
+  int mine = 0;
+  for (int i = begin; i < end; ++i) mine += tiles_of(i);
+  int scan = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, scan, off);
+    if (lane >= off) scan += up;
+  }
+  if (lane == 31) tb.sums[warp] = scan;
+  __syncthreads();
+  int before = scan - mine;
+  for (int w = 0; w < warp; ++w) before += tb.sums[w];
+  for (int i = begin; i < end; ++i) {
+    tb.first[i] = before;
+    before += tiles_of(i);
+  }
+  if (threadIdx.x == kThreads - 1) tb.first[groups] = before;
+  __syncthreads();
+}
+
+// Of the weights: [m][E][F][D].
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
+// A unit of work, and a role's walk over them.
+struct Unit {
+  int worker, group;     // DW: group of the worker's and all before it; FORWARD, DX: expert of the worker
+  int m, col;            // feature tile; DW: column tile
+  int row0, n;           // rows (FORWARD, DX: the tile's, DW: the group's)
+};
+template <int MODE, int BN>
+struct Walk {
+  const ProductArgs& g;
+  const Table& tb;
+  uint32_t total;
+  int at_group = 0;
+  __device__ __forceinline__ Walk(const ProductArgs& args, const Table& table) : g(args), tb(table) {
+    total = MODE == DW ? (uint32_t)(g.m * g.E) * g.m_tiles * g.n_tiles : (uint32_t)tb.first[g.m * g.E] * g.m_tiles;
+  }
+  // t: no less than at the call before
+  __device__ __forceinline__ Unit at(uint32_t t) {
+    Unit u;
+    if (MODE == DW) {
+      const uint32_t per = g.m_tiles * g.n_tiles;
+      u.group = t / per;
+      const uint32_t i = t - u.group * per;
+      const uint32_t group_tiles = kGroup * g.n_tiles, block = i / group_tiles, first = block * kGroup;
+      const uint32_t height = min((uint32_t)kGroup, g.m_tiles - first), j = i - block * group_tiles;
+      u.col = j / height;
+      u.m = first + j - u.col * height;
+      const int2 r = group_rows(g.offsets, u.group, g.E, g.R);
+      u.worker = u.group / g.E;
+      u.row0 = r.x;
+      u.n = r.y - r.x;
+    } else {
+      const int i = t / g.m_tiles;
+      while (tb.first[at_group + 1] <= i) ++at_group;
+      const int worker = at_group / g.E;
+      const int32_t* s = tb.start + at_group + worker;
+      u.row0 = s[0] + (i - tb.first[at_group]) * BN;
+      u.n = min(BN, s[1] - u.row0);
+      u.worker = g.first_worker + worker;
+      u.group = at_group - worker * g.E;
+      u.m = t - i * g.m_tiles;
+      u.col = 0;
+    }
+    return u;
+  }
+};
+
+// 32 accumulator columns of this lane's feature, rows row .. row + 31 of the output, of which n exist: a row's 32 features
+// leave by one store of 64 bytes.
+__device__ __forceinline__ void store_rows(const float* v, uint16_t* dst, int64_t pitch, int n, bool live, int f16) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    const uint32_t two = pack2(v[j], v[j + 1], f16);
+    store_half_if(dst + j * pitch, two, live && j < n);
+    store_half_if(dst + (j + 1) * pitch, two >> 16, live && j + 1 < n);
+  }
+}
+
+// FORWARD, DX: rows outside every group become zeros; by warps `at`, `at + warps`, ... of the grid.
+__device__ __forceinline__ void zero_rows(const ProductArgs& g, const Table& tb, int at, int warps, int lane) {
+  const int64_t bytes = (int64_t)g.features * 2;
+  for (int w = 0; w < g.m; ++w) {
+    const int head = tb.start[w * (g.E + 1)], tail = g.R - tb.start[w * (g.E + 1) + g.E];
+    for (int i = at; i < head + tail; i += warps) {
+      const int row = i < head ? i : g.R - tail + (i - head);
+      uint8_t* dst = static_cast<uint8_t*>(g.out) + ((int64_t)(g.first_worker + w) * g.R + row) * bytes;
+      if (g.out_width == 16)
+        for (int64_t c = lane * 16; c < bytes; c += 512) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
+      else
+        for (int64_t c = lane * 2; c < bytes; c += 64) *reinterpret_cast<uint16_t*>(dst + c) = 0;
+    }
+  }
+}
+
+template <int MODE, int HALVES, int BN, int STAGES>
+__global__ void __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
+  constexpr bool A_MN = MODE != FORWARD, B_MN = MODE == DW;
+  constexpr int kTileM = HALVES * kBM;
+  constexpr uint32_t kHalfBytes = kBM * kBK * 2;          // of A
+  constexpr uint32_t kABytes = HALVES * kHalfBytes;
+  constexpr uint32_t kBBytes = BN * kBK * 2;
+  constexpr uint32_t kStageBytes = kABytes + kBBytes;
+  constexpr int kBlockCols = BN / 2 < 64 ? BN / 2 : 64;   // DW: columns an epilogue warp stages at a time
+  constexpr uint32_t kStagingBytes = MODE == DW ? kEpiWarps * 4096 : 0;
+  constexpr uint32_t kTmemCols = 2 * BN;                  // two buffers, or two halves
+  static_assert(kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols >= 32, "two accumulators");
+  static_assert(MODE != DW || BN % 64 == 0, "boxes of 64 columns");
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  Control<STAGES>* ctl = reinterpret_cast<Control<STAGES>*>(tiles + STAGES * kStageBytes + kStagingBytes);
+  Table& table = *reinterpret_cast<Table*>(ctl + 1);   // (FORWARD, DX)
+  volatile int* abort_flag = &ctl->abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t first = blockIdx.x, step = gridDim.x;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&maps.a);
+    prefetch_tensormap(&maps.b);
+    prefetch_tensormap(&maps.b_small);
+    if (MODE == DW) {
+      prefetch_tensormap(&maps.a_small);
+      prefetch_tensormap(&maps.a_tail);
+      prefetch_tensormap(&maps.b_tail);
+    }
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&ctl->full[s]), 1);
+      mbar_init(smem_u32(&ctl->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&ctl->acc_full[b]), 1);
+      mbar_init(smem_u32(&ctl->acc_empty[b]), kEpiWarps);
+    }
+    ctl->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  launch_gate();
+  if (warp == 1) tmem_alloc(smem_u32(&ctl->tmem_base), kTmemCols);
+  tc_fence_before();
+  if (MODE != DW) make_table(g, table, BN);
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = ctl->tmem_base;
+  Walk<MODE, BN> walk(g, table);
+  const uint32_t total = walk.total;
+  const auto blocks_of = [&](const Unit& u) { return MODE == DW ? (u.n + kBK - 1) / kBK : g.num_kb; };
+  const auto mma_cols = [&](const Unit& u) { return MODE == DW ? BN : (u.n + kSmallBox - 1) / kSmallBox * kSmallBox; };
+  // Boxes of A and (DW) of B: none lies wholly outside its tensor.  What stays in their place reaches only parts of the
+  // accumulator that are not stored.
+  const auto a_boxes = [&](const Unit& u) {
+    constexpr int kBox = A_MN ? 64 : kBM;
+    return min(kTileM / kBox, (g.features - u.m * kTileM + kBox - 1) / kBox);
+  };
+  const auto b_boxes = [&](const Unit& u) { return min(BN / 64, (g.cols - u.col * BN + 63) / 64); };
+
+  if (warp == 0 && lane == 0) {
+    // ---------------- TMA producer
+    uint32_t it = 0;
+    for (uint32_t t = first; t < total && !*abort_flag; t += step) {
+      const Unit u = walk.at(t);
+      const int m0 = u.m * kTileM, held = mma_cols(u), na = a_boxes(u), nb = MODE == DW ? b_boxes(u) : 0;
+      for (int kb = 0, end = blocks_of(u); kb < end; ++kb, ++it) {
+        const int s = it % STAGES, k0 = kb * kBK;
+        if (!mbar_wait(smem_u32(&ctl->empty[s]), ((it / STAGES) & 1) ^ 1, abort_flag)) break;
+        const uint32_t bar = smem_u32(&ctl->full[s]);
+        const uint32_t a_dst = smem_u32(tiles + s * kStageBytes), b_dst = a_dst + kABytes;
+        if (MODE == DW) {
+          const int n0 = u.col * BN, left = u.n - k0;
+          const int rows = left >= kBK ? kBK : (left + kSmallBox - 1) / kSmallBox * kSmallBox;
+          mbar_expect_tx(bar, (uint32_t)((na + nb) * rows * 128));
+          if (left >= kBK) {
+            for (int j = 0; j < na; ++j) tma_load_3d(a_dst + j * 8192, &maps.a, bar, m0 + 64 * j, u.row0 + k0, u.worker);
+            for (int j = 0; j < nb; ++j) tma_load_3d(b_dst + j * 8192, &maps.b, bar, n0 + 64 * j, u.row0 + k0, u.worker);
+          } else {
+            for (int r = 0; r < rows; r += kSmallBox) {
+              const bool tail = left - r < kSmallBox;   // the last rows, from their copy
+              const int row = tail ? 0 : u.row0 + k0 + r, outer = tail ? u.group : u.worker;
+              for (int j = 0; j < na; ++j)
+                tma_load_3d(a_dst + j * 8192 + r * 128, tail ? &maps.a_tail : &maps.a_small, bar, m0 + 64 * j, row, outer);
+              for (int j = 0; j < nb; ++j)
+                tma_load_3d(b_dst + j * 8192 + r * 128, tail ? &maps.b_tail : &maps.b_small, bar, n0 + 64 * j, row, outer);
+            }
+          }
+        } else {
+          mbar_expect_tx(bar, (uint32_t)(na * (A_MN ? 8192 : (int)kHalfBytes) + held * 128));
+          for (int j = 0; j < na; ++j) {
+            if (A_MN) tma_load_4d(a_dst + j * 8192, &maps.a, bar, m0 + 64 * j, k0, u.group, u.worker);
+            else tma_load_4d(a_dst + j * kHalfBytes, &maps.a, bar, k0, m0 + j * kBM, u.group, u.worker);
+          }
+          if (held == BN) {
+            tma_load_3d(b_dst, &maps.b, bar, k0, u.row0, u.worker);
+          } else {
+            for (int j = 0; j < held; j += kSmallBox) tma_load_3d(b_dst + j * 128, &maps.b_small, bar, k0, u.row0 + j, u.worker);
+          }
+        }
+      }
+    }
+    // drain: whoever gave up waits (bounded) for the copies still in flight
+    if (*abort_flag) {
+      const uint32_t from = it > STAGES ? it - STAGES : 0;
+      const uint64_t t0 = global_ns();
+      for (uint32_t i = from; i < it; ++i)
+        while (!mbar_try_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1) && global_ns() - t0 < 10000000ull) {
+        }
+    }
+  } else if (warp == 1 && lane == 0) {
+    // ---------------- MMA issuer
+    const uint32_t fmt = g.f16 ? 0u : ((1u << 7) | (1u << 10));
+    const uint32_t idesc0 = (1u << 4) | fmt | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kBM >> 4) << 24);
+    uint32_t it = 0, n = 0;
+    bool ok = true;
+    for (uint32_t t = first; t < total && ok; t += step) {
+      const Unit u = walk.at(t);
+      const int end = blocks_of(u);
+      if (end == 0) continue;
+      const uint32_t idesc = idesc0 | ((uint32_t)(mma_cols(u) >> 3) << 17);
+      const int k_extent = MODE == DW ? u.n : g.k_extent;
+      const auto multiply = [&](int kb, uint32_t s, int half, uint32_t acc) {
+        const uint32_t a_addr = smem_u32(tiles + s * kStageBytes) + half * kHalfBytes, b_addr = smem_u32(tiles + s * kStageBytes) + kABytes;
+        const uint64_t a_desc = A_MN ? smem_desc_mn_sw128(a_addr) : smem_desc_k_sw128(a_addr);
+        const uint64_t b_desc = B_MN ? smem_desc_mn_sw128(b_addr) : smem_desc_k_sw128(b_addr);
+        // 16 K elements: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major tile
+        constexpr uint64_t a_step = A_MN ? 128 : 2, b_step = B_MN ? 128 : 2;
+        const int left = k_extent - kb * kBK;   // (what lies behind is zeros, or was not loaded)
+#pragma unroll
+        for (int k = 0; k < kBK / kUmmaK; ++k)
+          if (k * kUmmaK < left) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+      };
+      const auto arrived = [&](uint32_t i) {
+        ok = mbar_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1, abort_flag);
+        tc_fence_after();
+        return ok;
+      };
+      if constexpr (HALVES == 1) {
+        const uint32_t buf = n & 1, acc = tmem_base + buf * BN;
+        ok = mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((n >> 1) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        for (int kb = 0; kb < end; ++kb, ++it) {
+          if (!arrived(it)) break;
+          multiply(kb, it % STAGES, 0, acc);
+          umma_commit(smem_u32(&ctl->empty[it % STAGES]));
+        }
+        umma_commit(smem_u32(&ctl->acc_full[buf]));
+      } else {
+        // The first blocks' MMAs of the first half run while the second is emptied.
+        const int lead = min(end, STAGES);
+        ok = mbar_wait(smem_u32(&ctl->acc_empty[0]), (n & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        for (int kb = 0; kb < lead; ++kb) {
+          if (!arrived(it + kb)) break;
+          multiply(kb, (it + kb) % STAGES, 0, tmem_base);
+        }
+        if (!ok) break;
+        ok = mbar_wait(smem_u32(&ctl->acc_empty[1]), (n & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        for (int kb = 0; kb < lead; ++kb, ++it) {
+          multiply(kb, it % STAGES, 1, tmem_base + BN);
+          umma_commit(smem_u32(&ctl->empty[it % STAGES]));
+        }
+        for (int kb = lead; kb < end; ++kb, ++it) {
+          if (!arrived(it)) break;
+          multiply(kb, it % STAGES, 0, tmem_base);
+          multiply(kb, it % STAGES, 1, tmem_base + BN);
+          umma_commit(smem_u32(&ctl->empty[it % STAGES]));
+        }
+        umma_commit(smem_u32(&ctl->acc_full[0]));
+      }
+      ++n;
+    }
+  } else if (warp >= 2) {
+    // ---------------- epilogue: warp w reads TMEM lanes 32 (w % 4) .. + 31; warps 2-5 and 6-9 share the columns
+    const int lane_group = warp & 3, side = (warp - 2) >> 2;
+    if (MODE != DW) zero_rows(g, table, blockIdx.x * kEpiWarps + warp - 2, gridDim.x * kEpiWarps, lane);
+    uint32_t n = 0;
+    for (uint32_t t = first; t < total; t += step) {
+      const Unit u = walk.at(t);
+      const bool none = MODE == DW && u.n == 0;   // zeros, and no accumulator
+      const uint32_t buf = HALVES == 1 ? n & 1 : 0, parity = HALVES == 1 ? (n >> 1) & 1 : n & 1;
+      // one lane waits for its warp: what follows wants all lanes together
+      int ok = 1;
+      if (lane == 0 && !none) ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), parity, abort_flag);
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll 1
+      for (int half = 0; half < HALVES; ++half) {
+        const int feature0 = u.m * kTileM + half * kBM + lane_group * 32;
+        const uint32_t acc = tmem_base + (HALVES == 1 ? buf : half) * BN + ((uint32_t)(lane_group * 32) << 16);
+        if (feature0 < g.features) {
+          if (MODE == DW) {
+            constexpr int W = kBlockCols;
+            Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * 256};
+            uint16_t* dst = static_cast<uint16_t*>(g.out) + ((int64_t)u.group * g.features + feature0) * g.cols;
+            for (int c0 = side * (BN / 2); c0 < (side + 1) * (BN / 2); c0 += W) {
+              const int64_t col = (int64_t)u.col * BN + c0, cols = g.cols - col;
+              if (cols <= 0) break;
+#pragma unroll 1
+              for (int q = 0; q < W / 16; q += 2) {
+                float v[16], w[16];
+                if (none) {
+#pragma unroll
+                  for (int j = 0; j < 16; ++j) v[j] = w[j] = 0.f;
+                } else {
+                  tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
+                }
+                out.put(lane, q, v, g.f16);
+                out.put(lane, q + 1, w, g.f16);
+              }
+              out.flush(lane, dst + col, g.cols, g.features - feature0, cols, g.out_width);
+            }
+          } else {
+            uint16_t* dst = static_cast<uint16_t*>(g.out) + ((int64_t)u.worker * g.R + u.row0) * g.features + feature0 + lane;
+            const bool live = feature0 + lane < g.features;
+            if (BN == 32) {
+              // (sixteen columns for either side)
+              if (side * 16 < u.n) {
+                float v[32];
+                tmem_ld16x2(acc + side * 16, acc + side * 16, v, v + 16);
+                store_rows(v, dst + (int64_t)side * 16 * g.features, g.features, min(16, u.n - side * 16), live, g.f16);
+              }
+            } else {
+#pragma unroll 1
+              for (int c = side * 32; c < u.n; c += 64) {
+                float v[32];
+                tmem_ld32(acc + c, v);
+                store_rows(v, dst + (int64_t)c * g.features, g.features, u.n - c, live, g.f16);
+              }
+            }
+          }
+        }
+        if (none) continue;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[HALVES == 1 ? buf : half]));
+        __syncwarp();
+      }
+      if (!none) ++n;
+    }
+  }
+
+  // ---------------- teardown: every role arrives here, all waits above are bounded
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag && threadIdx.x == 0) {
+    // bounded grace period for copies and MMAs that may still be in flight
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 1000000ull) {
+    }
+    atomicExch(&g_product_status, (int)OLSGD_ETIMEOUT);
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// --------------------------------------------------------------------------------- host
+constexpr int kSms = 148;
+
+template <int MODE, int HALVES, int BN, int STAGES>
+cudaError_t launch_variant(const ProductMaps& maps, ProductArgs g, cudaStream_t s) {
+  constexpr size_t smem = (size_t)STAGES * (HALVES * kBM + BN) * kBK * 2 + (MODE == DW ? kEpiWarps * 4096 : sizeof(Table)) +
+                          sizeof(Control<STAGES>) + 1024;
+  static_assert(smem <= 227 * 1024, "shared memory of one CTA");
+  static PerDeviceSmem configured;
+  auto kern = product_kernel<MODE, HALVES, BN, STAGES>;
+  cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
+  if (e != cudaSuccess) return e;
+  g.m_tiles = (g.features + HALVES * kBM - 1) / (HALVES * kBM);
+  g.n_tiles = (g.cols + BN - 1) / BN;
+  // (of row tiles, disjoint groups have no more)
+  const int64_t total = (int64_t)g.m_tiles * g.m * (MODE == DW ? (int64_t)g.E * g.n_tiles : g.R / BN + (g.E < g.R ? g.E : g.R));
+  const int64_t room = sm_count();
+  g_tc_launches += 1;
+  return launch_chained(kern, dim3((unsigned)(total < room ? total : room)), dim3(kThreads), smem, s, maps, g);
+}
+
+// Which tiles: by the sizes alone; how the rows fall to the experts is not known here and taken as even.  A tile's
+// time goes by the operand bytes that it takes in per K block (its rows of A and of B), plus an epilogue that is
+// not hidden in the last wave; the launch takes as many waves as its tiles need.
+struct Shape {
+  int halves, bn;
+};
+Shape shape_rows(const ProductShape& d, int64_t features, int64_t k) {
+  constexpr Shape shapes[] = {{1, 32}, {1, 64}, {1, 128}, {1, 256}, {2, 256}};
+  Shape best = shapes[0];
+  double least = 1e300;
+  const int64_t used = d.E < d.R ? d.E : d.R;
+  const double rows = (double)d.R / used, kbs = (double)((k + kBK - 1) / kBK);
+  for (const Shape& sh : shapes) {
+    const double per_group = rows <= sh.bn ? 1.0 : rows / sh.bn + 0.5;
+    const double tiles = d.m * used * per_group * ((features + sh.halves * kBM - 1) / (sh.halves * kBM));
+    const double waves = tiles < kSms ? 1.0 : tiles / kSms + 0.5;
+    const double held = rows < sh.bn ? rows : sh.bn;
+    const double cost = waves * (kbs + 4) * (sh.halves * kBM + held);
+    if (cost < least) {
+      least = cost;
+      best = sh;
+    }
+  }
+  return best;
+}
+Shape shape_weights(const ProductShape& d) {
+  constexpr Shape shapes[] = {{1, 64}, {1, 128}, {1, 256}, {2, 256}};
+  Shape best = shapes[0];
+  double least = 1e300;
+  const double kbs = (double)d.R / d.E / kBK + 0.5;
+  for (const Shape& sh : shapes) {
+    const int64_t tiles = d.m * d.E * ((d.F + sh.halves * kBM - 1) / (sh.halves * kBM)) * ((d.D + sh.bn - 1) / sh.bn);
+    const double cost = (double)((tiles + kSms - 1) / kSms) * (kbs + 4) * (sh.halves * kBM + sh.bn);
+    if (cost < least) {
+      least = cost;
+      best = sh;
+    }
+  }
+  return best;
+}
+
+// The workspace: copies of operands that TMA cannot take, then (backward) the groups' last rows of dy and of x.
+struct Workspace {
+  size_t tail_dy, tail_x, total;
+};
+Workspace layout(const ProductShape& d, bool backward, bool copies) {
+  Workspace w{};
+  size_t at = 0;
+  if (copies) {
+    at += round256((size_t)d.m * d.R * round8(d.D) * 2) + round256((size_t)d.m * d.E * d.F * round8(d.D) * 2);
+    if (backward) at += round256((size_t)d.m * d.R * round8(d.F) * 2);
+  }
+  w.tail_dy = at;
+  at += backward ? round256((size_t)d.m * d.E * kSmallBox * round8(d.F) * 2) : 0;
+  w.tail_x = at;
+  at += backward ? round256((size_t)d.m * d.E * kSmallBox * round8(d.D) * 2) : 0;
+  w.total = at;
+  return w;
+}
+
+#define OLSGD_STEP(call)                    \
+  do {                                      \
+    const cudaError_t e_ = (call);          \
+    if (e_ != cudaSuccess) return e_;       \
+  } while (0)
+
+// [m][E][F][D] 16-bit; boxes of 64 columns by box_rows rows.
+bool make_map_weights(CUtensorMap* map, const ExpertOperand& w, const ProductShape& d, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const int64_t row = d.F > 1 ? w.row_stride : round8(d.D), expert = d.E > 1 ? w.expert_stride : row * d.F,
+                worker = d.m > 1 ? w.worker_stride : expert * d.E;
+  cuuint64_t dims[4] = {(cuuint64_t)d.D, (cuuint64_t)d.F, (cuuint64_t)d.E, (cuuint64_t)d.m};
+  cuuint64_t strides[3] = {(cuuint64_t)row * 2, (cuuint64_t)expert * 2, (cuuint64_t)worker * 2};
+  cuuint32_t box[4] = {(cuuint32_t)kBK, (cuuint32_t)box_rows, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, d.f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(w.p), dims, strides,
+            box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool weights_ready(const ExpertOperand& w, const ProductShape& d) {
+  return (reinterpret_cast<uintptr_t>(w.p) & 15) == 0 && (d.F == 1 || w.row_stride % 8 == 0) && (d.E == 1 || w.expert_stride % 8 == 0) &&
+         (d.m == 1 || w.worker_stride % 8 == 0);
+}
+// Weights that TMA cannot take, copied to padded rows at dst: all experts at once where they lie at one distance, else worker by
+// worker.
+cudaError_t weights_copied(ExpertOperand& w, const ProductShape& d, uint8_t* dst, cudaStream_t s) {
+  if (weights_ready(w, d)) return cudaSuccess;
+  const int64_t pitch = round8(d.D), bytes = d.E * d.F * pitch * 2;
+  const bool even = d.m == 1 || d.E == 1 || w.worker_stride == d.E * w.expert_stride;
+  for (int64_t i = 0; i < (even ? 1 : d.m); ++i) {
+    const int64_t groups = even ? d.m * d.E : d.E;
+    PadOperands all{};
+    all.cols = d.D;
+    all.pitch = pitch;
+    const uint16_t* begin = static_cast<const uint16_t*>(w.p) + i * w.worker_stride;
+    const int64_t distance = d.E > 1 ? w.expert_stride : w.worker_stride;
+    const uint16_t* end = begin + (groups > 1 ? (groups - 1) * distance : 0) + (d.F > 1 ? (d.F - 1) * w.row_stride : 0) + d.D;
+    all.op[0] = PadOperand{begin, end, reinterpret_cast<uint16_t*>(dst + i * bytes), d.F, distance, w.row_stride};
+    const cudaError_t e = launch_chained(pad_rows_kernel, dim3((unsigned)((d.F + 7) / 8), (unsigned)groups, 1), dim3(256), 0, s, all);
+    if (e != cudaSuccess) return e;
+  }
+  w = ExpertOperand{dst, d.E * d.F * pitch, d.F * pitch, pitch};
+  return cudaSuccess;
+}
+
+// FORWARD and DX: out rows = weights x rows of `in`.  Workers go by as many a launch as its table holds.
+template <int MODE>
+cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const GatedOperand& in, const int32_t* offsets, void* out, cudaStream_t s) {
+  const int64_t k = MODE == FORWARD ? d.D : d.F, features = MODE == FORWARD ? d.F : d.D;
+  const Shape sh = shape_rows(d, features, k);
+  ProductMaps maps;
+  if (!make_map_weights(&maps.a, w, d, MODE == FORWARD ? kBM : kBK) ||
+      !make_map16(&maps.b, in, k, d.R, d.m, sh.bn, d.f16) || !make_map16(&maps.b_small, in, k, d.R, d.m, kSmallBox, d.f16))
+    return cudaErrorInvalidValue;
+  maps.a_small = maps.a_tail = maps.a;
+  maps.b_tail = maps.b;
+  ProductArgs g{};
+  g.R = (int)d.R;
+  g.E = (int)d.E;
+  g.f16 = d.f16;
+  g.offsets = offsets;
+  g.k_extent = (int)k;
+  g.num_kb = (int)((k + kBK - 1) / kBK);
+  g.features = (int)features;
+  g.out = out;
+  g.out_width = store_width(out, features);
+  const int64_t most = kMaxStarts / (d.E + 1) < kMaxGroups / d.E ? kMaxStarts / (d.E + 1) : kMaxGroups / d.E;
+  for (int64_t at = 0; at < d.m; at += most) {
+    g.first_worker = (int)at;
+    g.m = (int)(d.m - at < most ? d.m - at : most);
+    const cudaError_t e = sh.halves == 2 ? launch_variant<MODE, 2, 256, 3>(maps, g, s)
+                          : sh.bn == 256 ? launch_variant<MODE, 1, 256, 4>(maps, g, s)
+                          : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6>(maps, g, s)
+                          : sh.bn == 64  ? launch_variant<MODE, 1, 64, 8>(maps, g, s)
+                                         : launch_variant<MODE, 1, 32, 9>(maps, g, s);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_weights(const ProductBackward& a, uint16_t* tail_dy, uint16_t* tail_x, cudaStream_t s) {
+  const int64_t groups = a.m * a.E;
+  TailArgs tails{};
+  tails.op[0] = TailOperand{static_cast<const uint16_t*>(a.dy.p), a.dy.worker_stride, a.dy.row_stride, tail_dy, a.F};
+  tails.op[1] = TailOperand{static_cast<const uint16_t*>(a.x.p), a.x.worker_stride, a.x.row_stride, tail_x, a.D};
+  tails.offsets = a.offsets;
+  tails.E = (int)a.E;
+  tails.R = (int)a.R;
+  OLSGD_STEP(launch_chained(tail_kernel, dim3((unsigned)groups, 2), dim3(256), 0, s, tails));
+  const GatedOperand tdy{tail_dy, kSmallBox * round8(a.F), round8(a.F)}, tx{tail_x, kSmallBox * round8(a.D), round8(a.D)};
+  ProductMaps maps;
+  if (!make_map16(&maps.a, a.dy, a.F, a.R, a.m, kBK, a.f16) || !make_map16(&maps.b, a.x, a.D, a.R, a.m, kBK, a.f16) ||
+      !make_map16(&maps.a_small, a.dy, a.F, a.R, a.m, kSmallBox, a.f16) || !make_map16(&maps.b_small, a.x, a.D, a.R, a.m, kSmallBox, a.f16) ||
+      !make_map16(&maps.a_tail, tdy, a.F, kSmallBox, groups, kSmallBox, a.f16) || !make_map16(&maps.b_tail, tx, a.D, kSmallBox, groups, kSmallBox, a.f16))
+    return cudaErrorInvalidValue;
+  ProductArgs g{};
+  g.R = (int)a.R;
+  g.E = (int)a.E;
+  g.m = (int)a.m;
+  g.f16 = a.f16;
+  g.offsets = a.offsets;
+  g.features = (int)a.F;
+  g.cols = (int)a.D;
+  g.out = a.dw;
+  g.out_width = store_width(a.dw, a.D);
+  const Shape sh = shape_weights(a);
+  return sh.halves == 2 ? launch_variant<DW, 2, 256, 3>(maps, g, s)
+         : sh.bn == 256 ? launch_variant<DW, 1, 256, 4>(maps, g, s)
+         : sh.bn == 128 ? launch_variant<DW, 1, 128, 6>(maps, g, s)
+                        : launch_variant<DW, 1, 64, 7>(maps, g, s);
+}
+
+}  // namespace
+
+bool product_needs_copies(const ProductShape& d, const GatedOperand& x, const ExpertOperand& w, const GatedOperand* dy) {
+  return !tma_ready(x, d.R, d.m) || !weights_ready(w, d) || (dy && !tma_ready(*dy, d.R, d.m));
+}
+size_t product_workspace(const ProductShape& d, bool backward, bool copies) { return layout(d, backward, copies).total; }
+
+cudaError_t launch_product(ProductForward a, cudaStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  uint8_t* copies = ws;
+  const Wanted x[] = {{&a.x, a.R}};
+  if (!tma_ready(a.x, a.R, a.m)) {
+    OLSGD_STEP(make_ready(x, 1, a.D, a.m, copies, s));
+    copies += round256((size_t)a.m * a.R * round8(a.D) * 2);
+  }
+  OLSGD_STEP(weights_copied(a.w, a, copies, s));
+  return launch_rows<FORWARD>(a, a.w, a.x, a.offsets, a.y, s);
+}
+
+cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  const Workspace at = layout(a, true, product_needs_copies(a, a.x, a.w, &a.dy));
+  uint8_t* copies = ws;
+  // dy for both, the weights for dx, x for the weights' gradient
+  const Wanted x[] = {{&a.x, a.R}}, dy[] = {{&a.dy, a.R}};
+  if (!tma_ready(a.dy, a.R, a.m)) {
+    OLSGD_STEP(make_ready(dy, 1, a.F, a.m, copies, s));
+    copies += round256((size_t)a.m * a.R * round8(a.F) * 2);
+  }
+  if (a.dw && !tma_ready(a.x, a.R, a.m)) {
+    OLSGD_STEP(make_ready(x, 1, a.D, a.m, copies, s));
+    copies += round256((size_t)a.m * a.R * round8(a.D) * 2);
+  }
+  if (a.dx) {
+    OLSGD_STEP(weights_copied(a.w, a, copies, s));
+    OLSGD_STEP(launch_rows<DX>(a, a.w, a.dy, a.offsets, a.dx, s));
+  }
+  return a.dw ? launch_weights(a, reinterpret_cast<uint16_t*>(ws + at.tail_dy), reinterpret_cast<uint16_t*>(ws + at.tail_x), s) : cudaSuccess;
+}
+
+cudaError_t product_status(int* status) {
+  OLSGD_STEP(cudaMemcpyFromSymbol(status, g_product_status, sizeof(int)));
+  if (*status != 0) {
+    const int zero = 0;
+    OLSGD_STEP(cudaMemcpyToSymbol(g_product_status, &zero, sizeof(int)));
+  }
+  return cudaSuccess;
+}
+
+}  // namespace olsgd

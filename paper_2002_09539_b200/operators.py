@@ -21,8 +21,12 @@ from .binding import _check, load_library
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 MAX_TOP = 32
+MAX_EXPERTS = 1024
+MAX_TEACHER = 256
 
 TokenLogprobs = namedtuple("TokenLogprobs", "logp entropy stats top_logp top_ids")
+ExpertRoute = namedtuple("ExpertRoute", "weights ids places tokens offsets")
+DistillLoss = namedtuple("DistillLoss", "loss stats d_logits")
 
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 _strided, _like, _ONE, _TWO = torch.empty_strided, torch.empty_like, (1,), (2, 1)
@@ -38,6 +42,17 @@ _SIGNATURES = {
     "olsgd_embedding_forward": [_i32, _i64, _i64, _i64, _i32, _vp, _i64, _i64, _vp, C.c_float, _vp, _vp],
     "olsgd_embedding_workspace": [_i32, _i64, _i64, C.POINTER(_sz)],
     "olsgd_embedding_backward": [_i32, _i64, _i64, _i64, _i32, _vp, _i64, _i64, _vp, C.c_float, _i32, _vp, _i64, _vp, _sz, _vp],
+    "olsgd_expert_route_workspace": [_i32, _i64, _i64, C.POINTER(_sz)],
+    "olsgd_expert_route": [_i32, _i64, _i64, _i32, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "olsgd_expert_route_backward": [_i64, _i64, _i32, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp],
+    "olsgd_expert_combine": [_i32, _i64, _i32, _i64, _i64, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _vp],
+    "olsgd_expert_combine_backward": [_i32, _i64, _i32, _i64, _i64, _i32] + 2 * [_vp, _i64, _i64] + [_vp, _vp, _vp, _vp, _vp, _vp],
+    "olsgd_expert_product_workspace": [_i32, _i64, _i64, _i64, _i64, _i32, _i32, C.POINTER(_sz)],
+    "olsgd_expert_product": [_i32, _i64, _i64, _i64, _i64, _i32] + 2 * [_vp, _i64, _i64] + [_i64, _vp, _vp, _vp, _sz, _vp],
+    "olsgd_expert_product_backward": [_i32, _i64, _i64, _i64, _i64, _i32] + 3 * [_vp, _i64, _i64] + [_i64, _vp, _vp, _vp, _vp, _sz, _vp],
+    "olsgd_distill_workspace": [_i32, _i64, _i64, _i32, C.POINTER(_sz)],
+    "olsgd_distill": [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _i32, _i32, C.c_float, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp],
+    "olsgd_distill_backward": [_vp, _vp, _i32, _i64, _i64, _i64, _vp, _vp, _i32, _i32, C.c_float, _vp, _vp, _i64, _vp],
     "olsgd_operators_join": [_vp],
     "olsgd_clip_grads": [_vp, _i32, _i32, C.c_float, _vp, _vp, _sz, _vp],
 }
@@ -359,6 +374,196 @@ def embedding_backward(d_out, ids, vocab, scale=1.0, dtype=torch.float32, out=No
     ws, wp, wn = _workspace(out, "olsgd_embedding_workspace", m, T, D)
     _run(lib.olsgd_embedding_backward, dev, m, T, V, D, code, p, sw, sr, ip, float(scale), _dtype(out, "out"), out.data_ptr(), ow, wp, wn)
     return out
+
+
+# ----------------------------------------------------------------------------------- experts
+
+def _route_sizes(logits, k):
+    if logits.dim() != 3:
+        _refuse("logits must be [m][T][E]")
+    xp, code, _, E, ld = _rows_of(logits, "logits")
+    k = operator.index(k)
+    if E > MAX_EXPERTS:
+        _refuse("there may be %d experts at most", MAX_EXPERTS)
+    if k < 1 or k > MAX_TOP or k > E:
+        _refuse("k must be in [1, min(E, %d)]", MAX_TOP)
+    return xp, code, logits.shape[0], logits.shape[1], E, ld, k
+
+
+def expert_route(logits, k, normalise=True):
+    """olsgd_expert_route: the k experts of each token.  logits [m][T][E] (rows evenly spaced); -inf is never chosen.
+    normalise: softmax over the chosen, else the chosen ones' share of the softmax over all.  Returns ExpertRoute(weights, ids,
+    places, tokens, offsets): float32 [m][T][k], int32 [m][T][k], [m][T][k], [m][T k], [m][E + 1].  The rows' inputs:
+    embedding_forward(x, route.tokens); their gradient: expert_combine(d_rows, route.places)."""
+    _recorded(logits)
+    lib = _ops()
+    xp, code, m, T, E, ld, k = _route_sizes(logits, k)
+    dev = logits.device
+    if m < 1:
+        _refuse("logits must be of one worker at least")
+    lead = (m, T, k)
+    weights = torch.empty(lead, dtype=_F32, device=dev)
+    ids, places = torch.empty(lead, dtype=_I32, device=dev), torch.empty(lead, dtype=_I32, device=dev)
+    tokens, offsets = torch.empty((m, T * k), dtype=_I32, device=dev), torch.empty((m, E + 1), dtype=_I32, device=dev)
+    ws, wp, wn = _workspace(offsets, "olsgd_expert_route_workspace", m, T, E)
+    _run(lib.olsgd_expert_route, dev, m, T, E, code, xp, ld, k, 1 if normalise else 0, weights.data_ptr(), ids.data_ptr(), places.data_ptr(),
+         tokens.data_ptr(), offsets.data_ptr(), wp, wn)
+    return ExpertRoute(weights, ids, places, tokens, offsets)
+
+
+def expert_route_backward(d_weights, logits, ids, weights, normalise=True):
+    """olsgd_expert_route_backward: the gradient of the logits, contiguous, of their type.  d_weights float32 [m][T][k]; ids and
+    weights are expert_route's for the same logits and `normalise`."""
+    _recorded(d_weights, logits, weights)
+    lib = _ops()
+    if ids.dim() != 3:
+        _refuse("ids must be [m][T][k]")
+    xp, code, m, T, E, ld, k = _route_sizes(logits, ids.shape[2])
+    dev, lead = logits.device, (m, T, k)
+    gp, ip, wp = _per_row(d_weights, lead, _F32, dev, "d_weights"), _per_row(ids, lead, _I32, dev, "ids"), _per_row(weights, lead, _F32, dev, "weights")
+    d = logits.new_empty(logits.shape)
+    _run(lib.olsgd_expert_route_backward, dev, m * T, E, code, gp, xp, ld, k, 1 if normalise else 0, ip, wp, d.data_ptr())
+    return d
+
+
+def _combine_sizes(rows, places):
+    if not rows.is_cuda or rows.dim() != 3 or places.dim() != 3 or rows.shape[0] < 1 or places.shape[2] < 1:
+        _refuse("rows must be a CUDA tensor [m][R][D], places [m][T][k]")
+    code = _dtype(rows, "rows")
+    m, R, D = rows.shape
+    T, k = places.shape[1:]
+    return code, m, T, k, R, D
+
+
+def expert_combine(rows, places, weights=None):
+    """olsgd_expert_combine: y[i][t] = sum over j of weights[i][t][j] rows[i][places[i][t][j]].  rows [m][R][D], any of the three
+    types, D contiguous; places int32 [m][T][k], those outside [0, R) add nothing; weights float32 [m][T][k], None: all 1.  Returns
+    [m][T][D] of the rows' type."""
+    _recorded(rows, weights)
+    lib = _ops()
+    code, m, T, k, R, D = _combine_sizes(rows, places)
+    dev, lead = rows.device, (m, T, k)
+    p, sw, sr = _matrix(rows, "rows", (m, R, D), rows.dtype, dev)
+    pp = _per_row(places, lead, _I32, dev, "places")
+    wp = None if weights is None else _per_row(weights, lead, _F32, dev, "weights")
+    y = rows.new_empty((m, T, D))
+    _run(lib.olsgd_expert_combine, dev, m, T, k, R, D, code, p, sw, sr, pp, wp, y.data_ptr())
+    return y
+
+
+def expert_combine_backward(d_y, rows, places, tokens, weights):
+    """olsgd_expert_combine_backward: (d_rows, d_weights) from d_y [m][T][D] and the forward call's operands; places and tokens as
+    expert_route gives them (each row is named once at most; tokens is negative for the others)."""
+    _recorded(d_y, rows, weights)
+    lib = _ops()
+    code, m, T, k, R, D = _combine_sizes(rows, places)
+    dev, lead = rows.device, (m, T, k)
+    g, r = _matrix(d_y, "d_y", (m, T, D), rows.dtype, dev), _matrix(rows, "rows", (m, R, D), rows.dtype, dev)
+    pp, tp = _per_row(places, lead, _I32, dev, "places"), _per_row(tokens, (m, R), _I32, dev, "tokens")
+    wp = _per_row(weights, lead, _F32, dev, "weights")
+    d_rows, d_weights = rows.new_empty((m, R, D)), torch.empty(lead, dtype=_F32, device=dev)
+    _run(lib.olsgd_expert_combine_backward, dev, m, T, k, R, D, code, *g, *r, pp, tp, wp, d_rows.data_ptr(), d_weights.data_ptr())
+    return d_rows, d_weights
+
+
+def _product_sizes(x, w, offsets):
+    if not x.is_cuda or x.dim() != 3 or w.dim() != 4 or x.shape[0] < 1:
+        _refuse("x and w must be CUDA tensors [m][R][D] and [m][E][F][D]")
+    code = DTYPES.get(x.dtype)
+    if not code:
+        _refuse("x must be bfloat16 or float16")
+    m, R, D = x.shape
+    E, F = w.shape[1:3]
+    if w.shape != (m, E, F, D) or w.dtype != x.dtype or w.device != x.device:
+        _refuse("w must be %s of shape %s on %s", x.dtype, (m, "E", "F", D), x.device)
+    sw, se, sr, sc = w.stride()
+    if sc != 1 and D != 1:
+        _refuse("w: the last dimension must be contiguous")
+    op = _per_row(offsets, (m, E + 1), _I32, x.device, "offsets")
+    p = w.data_ptr()
+    ok = p % 16 == 0 and (m == 1 or sw % 8 == 0) and (E == 1 or se % 8 == 0) and (F == 1 or sr % 8 == 0)
+    return m, R, E, D, F, code, op, (p, sw, se, sr), ok
+
+
+def expert_product(x, w, offsets):
+    """olsgd_expert_product: y[i][r] = w[i][e] x[i][r] for the rows offsets[i][e] <= r < offsets[i][e + 1] of expert e; rows of no
+    expert become zeros.  x [m][R][D], rows contiguous, any worker and row strides; w [m][E][F][D], any strides but the last; bfloat16
+    or float16; offsets int32 [m][E + 1], rising.  Returns [m][R][F]."""
+    _recorded(x, w)
+    lib = _ops()
+    m, R, E, D, F, code, op, wm, ok = _product_sizes(x, w, offsets)
+    a = _matrix(x, "x", (m, R, D), x.dtype, x.device)
+    y = x.new_empty((m, R, F))
+    ok = ok and _aligned(a, (m, R))
+    ws, wp, wn = _workspace(y, "olsgd_expert_product_workspace", m, R, E, D, F, 0, ok)
+    _run(lib.olsgd_expert_product, x.device, m, R, E, D, F, code, *a, *wm, op, y.data_ptr(), wp, wn)
+    return y
+
+
+def expert_product_backward(d_y, x, w, offsets, want_d_x=True, want_d_w=True):
+    """olsgd_expert_product_backward: (d_x, d_w) from d_y [m][R][F] and the forward call's operands; None for one that is not
+    wanted."""
+    _recorded(d_y, x, w)
+    lib = _ops()
+    m, R, E, D, F, code, op, wm, ok = _product_sizes(x, w, offsets)
+    dtype, dev = x.dtype, x.device
+    g, a = _matrix(d_y, "d_y", (m, R, F), dtype, dev), _matrix(x, "x", (m, R, D), dtype, dev)
+    d_x = x.new_empty((m, R, D)) if want_d_x else None
+    d_w = x.new_empty((m, E, F, D)) if want_d_w else None
+    ok = ok and _aligned(g, (m, R)) and _aligned(a, (m, R))
+    ws, wp, wn = _workspace(x, "olsgd_expert_product_workspace", m, R, E, D, F, 1, ok)
+    _run(lib.olsgd_expert_product_backward, dev, m, R, E, D, F, code, *g, *a, *wm, op, d_x.data_ptr() if want_d_x else None,
+         d_w.data_ptr() if want_d_w else None, wp, wn)
+    return d_x, d_w
+
+
+# ------------------------------------------------------------------------------ distillation
+
+def _teacher(logits, ids, teacher, temperature):
+    lead, dev = logits.shape[:-1], logits.device
+    if ids.dim() != logits.dim() or ids.shape[:-1] != lead or not 1 <= ids.shape[-1] <= MAX_TEACHER:
+        _refuse("ids must be [..., K], K in [1, %d], for logits [..., V]", MAX_TEACHER)
+    code = _dtype(teacher, "teacher")
+    ip, tp = _per_row(ids, ids.shape, _I32, dev, "ids"), _per_row(teacher, ids.shape, teacher.dtype, dev, "teacher")
+    t = float(temperature)
+    if not 2.0 ** -20 <= t <= 2.0 ** 20:
+        _refuse("temperature must be in [2^-20, 2^20]")
+    return ip, tp, code, ids.shape[-1], t
+
+
+def distill_loss(logits, ids, teacher, temperature=1.0, d_loss=None):
+    """olsgd_distill: the divergence of a teacher's top logits from the student's distribution, row by row: with
+    q = softmax(teacher / temperature) over the K pairs and p = softmax(logits / temperature) over all tokens, sum q (log q -
+    log p[ids]).  logits [..., V] (rows evenly spaced), ids int32 [..., K] (outside [0, V): no pair), teacher [..., K] of any of the
+    three types.  d_loss float32 [...]: the weight of each row's loss, where it is known by now; the logits' gradient then
+    comes from the same read of them.  Returns DistillLoss(loss, stats, d_logits): float32 [...] and [..., 2], and the gradient
+    (contiguous, of the logits' type) or None."""
+    _recorded(logits, teacher, d_loss)
+    lib = _ops()
+    xp, code, N, V, ld = _rows_of(logits, "logits")
+    dev, lead = logits.device, logits.shape[:-1]
+    ip, tp, tcode, K, t = _teacher(logits, ids, teacher, temperature)
+    gp = None if d_loss is None else _per_row(d_loss, lead, _F32, dev, "d_loss")
+    loss, stats = torch.empty(lead, dtype=_F32, device=dev), torch.empty(lead + (2,), dtype=_F32, device=dev)
+    d = None if d_loss is None else logits.new_empty(logits.shape)
+    ws, wp, wn = _workspace(loss, "olsgd_distill_workspace", code, N, V, 0 if d_loss is None else 1)
+    _run(lib.olsgd_distill, dev, xp, code, N, V, ld, ip, tp, tcode, K, t, gp, loss.data_ptr(), stats.data_ptr(),
+         None if d is None else d.data_ptr(), V, wp, wn)
+    return DistillLoss(loss, stats, d)
+
+
+def distill_backward(d_loss, logits, ids, teacher, stats, temperature=1.0):
+    """olsgd_distill_backward: the logits' gradient alone, contiguous, of their type.  d_loss float32 [...]; stats are
+    distill_loss's for the same logits and temperature."""
+    _recorded(d_loss, logits, teacher, stats)
+    lib = _ops()
+    xp, code, N, V, ld = _rows_of(logits, "logits")
+    dev, lead = logits.device, logits.shape[:-1]
+    ip, tp, tcode, K, t = _teacher(logits, ids, teacher, temperature)
+    gp, sp = _per_row(d_loss, lead, _F32, dev, "d_loss"), _per_row(stats, lead + (2,), _F32, dev, "stats")
+    d = logits.new_empty(logits.shape)
+    _run(lib.olsgd_distill_backward, dev, gp, xp, code, N, V, ld, ip, tp, tcode, K, t, sp, d.data_ptr(), V)
+    return d
 
 
 def operators_join(device="cuda"):
