@@ -35,9 +35,11 @@ constexpr int kMaxStarts = 2 * kMaxGroups;
 
 __device__ int g_product_status;     // a bounded wait gave up (olsgd_operators_join)
 
-// a, b: boxes of whole tiles; _small: of 16 rows; DW: _tail: of the copies of last rows.
+// Rows come in boxes of 16, 32, 64, 128 and 256, one of each at most (a TMA instruction takes some 200 cycles however
+// small its box is).  DW: boxes of 16, 32 and 64 rows, and of 16 rows of the copies of last rows.
+constexpr int kBoxes = 5;
 struct alignas(64) ProductMaps {
-  CUtensorMap a, b, a_small, b_small, a_tail, b_tail;
+  CUtensorMap a[kBoxes], b[kBoxes], a_tail, b_tail;   // FORWARD, DX: a[0] are the weights
 };
 struct ProductArgs {
   int num_kb, k_extent;       // FORWARD, DX: K in blocks of 64, and in elements
@@ -251,14 +253,8 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   const uint32_t first = blockIdx.x, step = gridDim.x;
 
   if (threadIdx.x == 0) {
-    prefetch_tensormap(&maps.a);
-    prefetch_tensormap(&maps.b);
-    prefetch_tensormap(&maps.b_small);
-    if (MODE == DW) {
-      prefetch_tensormap(&maps.a_small);
-      prefetch_tensormap(&maps.a_tail);
-      prefetch_tensormap(&maps.b_tail);
-    }
+    prefetch_tensormap(&maps.a[MODE == DW ? 2 : 0]);
+    prefetch_tensormap(&maps.b[MODE == DW ? 2 : 0]);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&ctl->full[s]), 1);
       mbar_init(smem_u32(&ctl->empty[s]), 1);
@@ -304,30 +300,35 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
           const int n0 = u.col * BN, left = u.n - k0;
           const int rows = left >= kBK ? kBK : (left + kSmallBox - 1) / kSmallBox * kSmallBox;
           mbar_expect_tx(bar, (uint32_t)((na + nb) * rows * 128));
+          const auto load = [&](const CUtensorMap* ma, const CUtensorMap* mb, int at, int row, int outer) {
+            for (int j = 0; j < na; ++j) tma_load_3d(a_dst + j * 8192 + at * 128, ma, bar, m0 + 64 * j, row, outer);
+            for (int j = 0; j < nb; ++j) tma_load_3d(b_dst + j * 8192 + at * 128, mb, bar, n0 + 64 * j, row, outer);
+          };
           if (left >= kBK) {
-            for (int j = 0; j < na; ++j) tma_load_3d(a_dst + j * 8192, &maps.a, bar, m0 + 64 * j, u.row0 + k0, u.worker);
-            for (int j = 0; j < nb; ++j) tma_load_3d(b_dst + j * 8192, &maps.b, bar, n0 + 64 * j, u.row0 + k0, u.worker);
+            load(&maps.a[2], &maps.b[2], 0, u.row0 + k0, u.worker);
           } else {
-            for (int r = 0; r < rows; r += kSmallBox) {
-              const bool tail = left - r < kSmallBox;   // the last rows, from their copy
-              const int row = tail ? 0 : u.row0 + k0 + r, outer = tail ? u.group : u.worker;
-              for (int j = 0; j < na; ++j)
-                tma_load_3d(a_dst + j * 8192 + r * 128, tail ? &maps.a_tail : &maps.a_small, bar, m0 + 64 * j, row, outer);
-              for (int j = 0; j < nb; ++j)
-                tma_load_3d(b_dst + j * 8192 + r * 128, tail ? &maps.b_tail : &maps.b_small, bar, n0 + 64 * j, row, outer);
-            }
+            int at = 0;
+#pragma unroll
+            for (int i = 1; i >= 0; --i)
+              if (left & (kSmallBox << i)) {
+                load(&maps.a[i], &maps.b[i], at, u.row0 + k0 + at, u.worker);
+                at += kSmallBox << i;
+              }
+            if (at < left) load(&maps.a_tail, &maps.b_tail, at, 0, u.group);   // the last rows, from their copy
           }
         } else {
           mbar_expect_tx(bar, (uint32_t)(na * (A_MN ? 8192 : (int)kHalfBytes) + held * 128));
           for (int j = 0; j < na; ++j) {
-            if (A_MN) tma_load_4d(a_dst + j * 8192, &maps.a, bar, m0 + 64 * j, k0, u.group, u.worker);
-            else tma_load_4d(a_dst + j * kHalfBytes, &maps.a, bar, k0, m0 + j * kBM, u.group, u.worker);
+            if (A_MN) tma_load_4d(a_dst + j * 8192, &maps.a[0], bar, m0 + 64 * j, k0, u.group, u.worker);
+            else tma_load_4d(a_dst + j * kHalfBytes, &maps.a[0], bar, k0, m0 + j * kBM, u.group, u.worker);
           }
-          if (held == BN) {
-            tma_load_3d(b_dst, &maps.b, bar, k0, u.row0, u.worker);
-          } else {
-            for (int j = 0; j < held; j += kSmallBox) tma_load_3d(b_dst + j * 128, &maps.b_small, bar, k0, u.row0 + j, u.worker);
-          }
+          int at = 0;
+#pragma unroll
+          for (int i = kBoxes - 1; i >= 0; --i)
+            if (held & (kSmallBox << i)) {
+              tma_load_3d(b_dst + at * 128, &maps.b[i], bar, k0, u.row0 + at, u.worker);
+              at += kSmallBox << i;
+            }
         }
       }
     }
@@ -627,11 +628,14 @@ cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const Gat
   const int64_t k = MODE == FORWARD ? d.D : d.F, features = MODE == FORWARD ? d.F : d.D;
   const Shape sh = shape_rows(d, features, k);
   ProductMaps maps;
-  if (!make_map_weights(&maps.a, w, d, MODE == FORWARD ? kBM : kBK) ||
-      !make_map16(&maps.b, in, k, d.R, d.m, sh.bn, d.f16) || !make_map16(&maps.b_small, in, k, d.R, d.m, kSmallBox, d.f16))
-    return cudaErrorInvalidValue;
-  maps.a_small = maps.a_tail = maps.a;
-  maps.b_tail = maps.b;
+  bool ok = make_map_weights(&maps.a[0], w, d, MODE == FORWARD ? kBM : kBK);
+  for (int i = 0; i < kBoxes; ++i) {
+    // (boxes that the tile has no room for are not used)
+    ok = ok && make_map16(&maps.b[i], in, k, d.R, d.m, kSmallBox << i, d.f16);
+    if (i > 0) maps.a[i] = maps.a[0];
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  maps.a_tail = maps.b_tail = maps.a[0];
   ProductArgs g{};
   g.R = (int)d.R;
   g.E = (int)d.E;
@@ -667,10 +671,12 @@ cudaError_t launch_weights(const ProductBackward& a, uint16_t* tail_dy, uint16_t
   OLSGD_STEP(launch_chained(tail_kernel, dim3((unsigned)groups, 2), dim3(256), 0, s, tails));
   const GatedOperand tdy{tail_dy, kSmallBox * round8(a.F), round8(a.F)}, tx{tail_x, kSmallBox * round8(a.D), round8(a.D)};
   ProductMaps maps;
-  if (!make_map16(&maps.a, a.dy, a.F, a.R, a.m, kBK, a.f16) || !make_map16(&maps.b, a.x, a.D, a.R, a.m, kBK, a.f16) ||
-      !make_map16(&maps.a_small, a.dy, a.F, a.R, a.m, kSmallBox, a.f16) || !make_map16(&maps.b_small, a.x, a.D, a.R, a.m, kSmallBox, a.f16) ||
-      !make_map16(&maps.a_tail, tdy, a.F, kSmallBox, groups, kSmallBox, a.f16) || !make_map16(&maps.b_tail, tx, a.D, kSmallBox, groups, kSmallBox, a.f16))
-    return cudaErrorInvalidValue;
+  bool ok = make_map16(&maps.a_tail, tdy, a.F, kSmallBox, groups, kSmallBox, a.f16) && make_map16(&maps.b_tail, tx, a.D, kSmallBox, groups, kSmallBox, a.f16);
+  for (int i = 0; i < kBoxes; ++i) {
+    const int rows = i < 2 ? kSmallBox << i : kBK;
+    ok = ok && make_map16(&maps.a[i], a.dy, a.F, a.R, a.m, rows, a.f16) && make_map16(&maps.b[i], a.x, a.D, a.R, a.m, rows, a.f16);
+  }
+  if (!ok) return cudaErrorInvalidValue;
   ProductArgs g{};
   g.R = (int)a.R;
   g.E = (int)a.E;
