@@ -25,6 +25,7 @@ using namespace op;
 constexpr int kSms = 148;
 constexpr int kRouteWarps = 32;
 constexpr int kRouteThreads = 32 * kRouteWarps;
+constexpr int kSorted = 4;   // elements of a lane that are sorted ahead of the rounds
 static_assert(OLSGD_MAX_EXPERTS <= kRouteThreads, "a thread for each expert");
 static_assert(OLSGD_MAX_TOP <= 32, "a lane for each slot of a token");
 
@@ -135,39 +136,79 @@ __global__ void __launch_bounds__(kRouteThreads, 1) route_kernel(const RouteKern
     if (kAhead && t + 1 < last) load_lane<T, NL>(rows + (t + 1) * a.ld, E, a.vec, -INFINITY, x);
     int id = -1;
     uint32_t chosen = 0, top = 0;
-    for (int j = 0; j < k; ++j) {
-      const uint32_t most = __reduce_max_sync(0xffffffffu, best);
-      if (most == 0) break;
-      if (j == 0) top = most;
-      const int winner = __ffs(__ballot_sync(0xffffffffu, best == most)) - 1;
-      int at = 0;
-      if (lane == winner) {
-        // the lowest of this lane's that equal it leaves
-        bool gone = false;
-        best = 0;
+    if constexpr (NL <= kSorted) {
+      // Each lane's keys in falling order (equal ones stay as they are), so that what a round takes is a head.
+      int at[NL];
+      uint32_t own[NL];
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        own[i] = key[i];
+        at[i] = lane * NL + i;
+      }
+#pragma unroll
+      for (int pass = NL - 1; pass > 0; --pass)
+#pragma unroll
+        for (int i = 0; i < pass; ++i) {
+          const bool swap = own[i + 1] > own[i];
+          const uint32_t big = swap ? own[i + 1] : own[i], small = swap ? own[i] : own[i + 1];
+          const int big_at = swap ? at[i + 1] : at[i], small_at = swap ? at[i] : at[i + 1];
+          own[i] = big;
+          own[i + 1] = small;
+          at[i] = big_at;
+          at[i + 1] = small_at;
+        }
+      for (int j = 0; j < k; ++j) {
+        const uint32_t most = __reduce_max_sync(0xffffffffu, own[0]);
+        if (most == 0) break;
+        if (j == 0) top = most;
+        const int winner = __ffs(__ballot_sync(0xffffffffu, own[0] == most)) - 1;
+        const int from = __shfl_sync(0xffffffffu, at[0], winner);
+        if (lane == j) {
+          id = from;
+          chosen = most;
+        }
+        const bool mine_left = lane == winner;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-          if (!gone && key[i] == most) {
-            gone = true;
-            at = i;
-            key[i] = 0;
-          }
-          best = max(best, key[i]);
+          own[i] = mine_left ? (i + 1 < NL ? own[i + 1 < NL ? i + 1 : i] : 0u) : own[i];
+          at[i] = mine_left && i + 1 < NL ? at[i + 1 < NL ? i + 1 : i] : at[i];
         }
       }
-      at = __shfl_sync(0xffffffffu, at, winner) + winner * NL;
-      if (lane == j) {
-        id = at;
-        chosen = most;
+    } else {
+      for (int j = 0; j < k; ++j) {
+        const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+        if (most == 0) break;
+        if (j == 0) top = most;
+        const int winner = __ffs(__ballot_sync(0xffffffffu, best == most)) - 1;
+        int at = 0;
+        if (lane == winner) {
+          // the lowest of this lane's that equal it leaves
+          bool gone = false;
+          best = 0;
+#pragma unroll
+          for (int i = 0; i < NL; ++i) {
+            if (!gone && key[i] == most) {
+              gone = true;
+              at = i;
+              key[i] = 0;
+            }
+            best = max(best, key[i]);
+          }
+        }
+        at = __shfl_sync(0xffffffffu, at, winner) + winner * NL;
+        if (lane == j) {
+          id = at;
+          chosen = most;
+        }
       }
     }
     const float base = value_of(top);
     float e = id >= 0 ? expf(value_of(chosen) - base) : 0.f, total = e;
     if (!a.normalise) {
-      // the others, too (those chosen have left)
+      // all of them (NL > kSorted: those chosen have left, and count already)
+      if (NL <= kSorted) total = 0.f;
 #pragma unroll
-      for (int i = 0; i < NL; ++i)
-        if (key[i]) total += expf(value_of(key[i]) - base);
+      for (int i = 0; i < NL; ++i) total += key[i] ? expf(value_of(key[i]) - base) : 0.f;
     }
     total = warp_sum(total);
     if (lane < k) {
@@ -270,38 +311,40 @@ __global__ void __launch_bounds__(kRouteThreads, 1) place_kernel(const RouteKern
   for (int64_t r = all + (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; r < slots; r += (int64_t)tiles * kRouteThreads) tokens[r] = -1;
 }
 
-// The gradient of a token's logits, by a warp.
+// The gradient of a token's logits, by a warp: what is asked at the chosen goes through shared memory to the lanes
+// that hold them.
 template <typename T, int NL>
 __global__ void __launch_bounds__(256) route_backward_kernel(const RouteGradArgs a, int vec_in, int vec_out) {
+  extern __shared__ float asked[];   // [8][32 NL]
   launch_gate();
   const int lane = threadIdx.x & 31, k = a.k, E = a.E;
   const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (r >= a.rows) return;
+  float* mine = asked + (threadIdx.x >> 5) * 32 * NL;
+  float x[NL];
+  if (!a.normalise) load_lane<T, NL>(static_cast<const T*>(a.logits) + r * a.ld, E, vec_in, -INFINITY, x);
   int id = -1;
   float w = 0.f, dw = 0.f;
   if (lane < k) {
     id = a.ids[r * k + lane];
-    if (id >= E) id = -1;
-    if (id >= 0) {
-      w = a.weights[r * k + lane];
-      dw = a.d_weights[r * k + lane];
-    }
+    w = a.weights[r * k + lane];
+    dw = a.d_weights[r * k + lane];
+  }
+#pragma unroll
+  for (int i = 0; i < NL; ++i) mine[i * 32 + lane] = 0.f;
+  if (id < 0 || id >= E) {   // no expert: whatever its gradient holds
+    id = -1;
+    w = dw = 0.f;
   }
   const float mean = warp_sum(w * dw);
+  __syncwarp();
+  if (id >= 0) atomicAdd(mine + id, a.normalise ? w * (dw - mean) : dw);   // (a token's experts differ)
+  __syncwarp();
   float d[NL];
 #pragma unroll
-  for (int i = 0; i < NL; ++i) d[i] = 0.f;
-  const float at_chosen = a.normalise ? w * (dw - mean) : dw;
-  for (int j = 0; j < k; ++j) {
-    const int e = __shfl_sync(0xffffffffu, id, j) - lane * NL;
-    const float g = __shfl_sync(0xffffffffu, at_chosen, j);
-#pragma unroll
-    for (int i = 0; i < NL; ++i)
-      if (e == i) d[i] += g;
-  }
+  for (int i = 0; i < NL; ++i) d[i] = mine[lane * NL + i];
   if (!a.normalise) {
-    float x[NL], most = -INFINITY, total = 0.f;
-    load_lane<T, NL>(static_cast<const T*>(a.logits) + r * a.ld, E, vec_in, -INFINITY, x);
+    float most = -INFINITY, total = 0.f;
 #pragma unroll
     for (int i = 0; i < NL; ++i) most = fmaxf(most, x[i]);
 #pragma unroll
@@ -313,9 +356,9 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteGradArgs
       x[i] = empty ? 0.f : expf(x[i] - most);
       total += x[i];
     }
-    total = empty ? 1.f : warp_sum(total);
+    const float share = empty ? 0.f : 1.f / warp_sum(total);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) d[i] = x[i] / total * (d[i] - mean);
+    for (int i = 0; i < NL; ++i) d[i] = x[i] * share * (d[i] - mean);
   }
   T* out = static_cast<T*>(a.d_logits) + r * E;
   const int j0 = lane * NL;
@@ -343,108 +386,135 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteGradArgs
 
 // ------------------------------------------------------------------------------ combine
 
-// V elements at p as they lie in memory, to floats and back.  (V == 1: rows of any alignment.)
-template <typename T, int V>
-__device__ __forceinline__ void load_some(const T* p, float* v) {
-  if constexpr (V == 1) v[0] = Elem<T>::to_float(*p);
-  else Elem<T>::unpack(ld16(p), v);
+// 16 bytes of a row from element j on.  SHIFTED: rows start anywhere.
+template <typename T, bool SHIFTED>
+__device__ __forceinline__ uint4 load_sixteen(const T* row, int64_t j, int64_t n, const T* begin, const T* end) {
+  if (SHIFTED) return load_shifted<T>(row, j, n, begin, end);
+  return ld16_stream(row + j);
 }
-template <typename T, int V>
-__device__ __forceinline__ void store_some(T* p, const float* v) {
-  if constexpr (V == 1) *p = Elem<T>::from_float(v[0]);
-  else *reinterpret_cast<uint4*>(p) = Elem<T>::pack(v);
+// Pieces of a result's row, counted from the boundary at or before it.
+template <typename T>
+int64_t row_pieces(int64_t D, bool shifted) {
+  constexpr int V = Elem<T>::kVec;
+  return shifted ? (D + 2 * V - 2) / V : D / V;
 }
 
-// Thread: V elements of a token.
-template <typename T, int V>
-__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a) {
+// Thread: 16 bytes of a token's row.  U: rows on their way at a time.
+template <typename T, bool SHIFTED, int U>
+__global__ void __launch_bounds__(256, SHIFTED || U > 2 ? 4 : 6) combine_kernel(const CombineArgs a, int64_t pieces) {
+  constexpr int V = Elem<T>::kVec;
   launch_gate();
-  const int64_t pieces = a.D / V, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t token = at / pieces, c = (at - token * pieces) * V;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t token = at / pieces;
   if (token >= a.m * a.T) return;
+  T* y = static_cast<T*>(a.y) + token * a.D;
+  const int64_t j = (at - token * pieces) * V - (SHIFTED ? row_shift(y) : 0);
+  if (SHIFTED && j >= a.D) return;
   const int64_t worker = token / a.T;
-  const T* rows = static_cast<const T*>(a.rows) + worker * a.rows_worker + c;
+  const T* rows = static_cast<const T*>(a.rows) + worker * a.rows_worker;
+  const T *begin = static_cast<const T*>(a.rows), *end = static_cast<const T*>(a.rows_end);
   const int32_t* places = a.places + token * a.k;
   const float* weights = a.weights ? a.weights + token * a.k : nullptr;
-  float y[V];
+  float sum[V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) y[e] = 0.f;
-  constexpr int U = 4;
-  for (int j0 = 0; j0 < a.k; j0 += U) {
+  for (int e = 0; e < V; ++e) sum[e] = 0.f;
+  for (int s0 = 0; s0 < a.k; s0 += U) {
     int32_t p[U];
-    float w[U], v[U][V];
+    float w[U];
+    uint4 raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      p[u] = j0 + u < a.k ? places[j0 + u] : -1;
-      if (p[u] >= a.R) p[u] = -1;
-      w[u] = weights && j0 + u < a.k ? weights[j0 + u] : 1.f;
+      p[u] = s0 + u < a.k ? places[s0 + u] : -1;
+      w[u] = weights && s0 + u < a.k ? weights[s0 + u] : 1.f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (p[u] >= 0) load_some<T, V>(rows + p[u] * a.rows_row, v[u]);
+      if (p[u] >= 0 && p[u] < a.R) raw[u] = load_sixteen<T, SHIFTED>(rows + p[u] * a.rows_row, j, a.D, begin, end);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (p[u] >= 0)
+      if (p[u] >= 0 && p[u] < a.R) {
+        float v[V];
+        Elem<T>::unpack(raw[u], v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = fmaf(w[u], v[u][e], y[e]);
+        for (int e = 0; e < V; ++e) sum[e] = fmaf(w[u], v[e], sum[e]);
+      }
   }
-  store_some<T, V>(static_cast<T*>(a.y) + token * a.D + c, y);
+  store_floats<T, V>(y, j, a.D, true, sum);
 }
 
 // NT threads for each slot: the row's gradient, and the weight's.  Slots of a token follow one another, so
 // that its gradient comes from L1 after the first.  The same threads zero the row of their own number if no
 // token has it.
-template <typename T, int V, int NT>
-__global__ void __launch_bounds__(256) combine_backward_kernel(const CombineGradArgs a) {
+template <typename T, bool SHIFTED, int NT>
+__global__ void __launch_bounds__(256, 4) combine_backward_kernel(const CombineGradArgs a, int pieces) {
+  constexpr int V = Elem<T>::kVec, U = SHIFTED ? 2 : 4;
   launch_gate();
   const int64_t slots = a.T * a.k, per = slots > a.R ? slots : a.R;
   const int64_t at = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT, worker = blockIdx.y;
   const int t0 = threadIdx.x % NT;
   float dot = 0.f;
-  bool has = false;
-  if (at < per) {
-    T* d_rows = static_cast<T*>(a.d_rows) + worker * a.R * a.D;
-    if (at < a.R && a.tokens[worker * a.R + at] < 0) {
-      float zero[V];
+  const bool has = at < slots;
+  T* d_rows = static_cast<T*>(a.d_rows) + worker * a.R * a.D;
+  const bool zero = at < a.R && a.tokens[worker * a.R + at] < 0;
+  const int32_t p = has ? a.places[worker * slots + at] : -1;
+  const float w = has ? a.weights[worker * slots + at] : 0.f;
+  if (zero) {
+    T* out = d_rows + at * a.D;
+    const int shift = SHIFTED ? row_shift(out) : 0;
+    float none[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) zero[e] = 0.f;
-      for (int64_t c = (int64_t)t0 * V; c < a.D; c += NT * V) store_some<T, V>(d_rows + at * a.D + c, zero);
-    }
-    has = at < slots;
-    if (has) {
-      const int32_t p = a.places[worker * slots + at];
-      if (p >= 0 && p < a.R) {
-        const float w = a.weights[worker * slots + at];
-        const T* dy = static_cast<const T*>(a.d_y) + worker * a.dy_worker + at / a.k * a.dy_row;
-        const T* row = static_cast<const T*>(a.rows) + worker * a.rows_worker + p * a.rows_row;
-        T* out = d_rows + (int64_t)p * a.D;
-        constexpr int U = V == 1 ? 8 : 4;
-        for (int64_t c0 = (int64_t)t0 * V; c0 < a.D; c0 += NT * V * U) {
-          float g[U][V], x[U][V];
+    for (int e = 0; e < V; ++e) none[e] = 0.f;
+    for (int q = t0; q < pieces; q += NT) store_floats<T, V>(out, (int64_t)q * V - shift, a.D, true, none);
+  }
+  if (p >= 0 && p < a.R) {
+    const T *dy_all = static_cast<const T*>(a.d_y), *rows_all = static_cast<const T*>(a.rows);
+    const T* dy = dy_all + worker * a.dy_worker + at / a.k * a.dy_row;
+    const T* row = rows_all + worker * a.rows_worker + p * a.rows_row;
+    T* out = d_rows + (int64_t)p * a.D;
+    const int shift = SHIFTED ? row_shift(out) : 0;
+    f32x2 sum = 0;
+    const f32x2 w2 = pack2f(w, w);
+    for (int q0 = t0; q0 < pieces; q0 += NT * U) {
+      uint4 g[U], x[U];
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int64_t c = c0 + u * NT * V;
-            if (c < a.D) {
-              load_some<T, V>(dy + c, g[u]);
-              load_some<T, V>(row + c, x[u]);
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int64_t c = c0 + u * NT * V;
-            if (c < a.D) {
-              float d[V];
-#pragma unroll
-              for (int e = 0; e < V; ++e) {
-                dot = fmaf(g[u][e], x[u][e], dot);
-                d[e] = w * g[u][e];
-              }
-              store_some<T, V>(out + c, d);
-            }
-          }
+      for (int u = 0; u < U; ++u) {
+        const int64_t j = (int64_t)(q0 + u * NT) * V - shift;
+        const bool live = q0 + u * NT < pieces && j < a.D;
+        g[u] = x[u] = make_uint4(0, 0, 0, 0);
+        if (live) {
+          // (the token's gradient is read again by its other slots)
+          g[u] = SHIFTED ? load_shifted<T>(dy, j, a.D, dy_all, static_cast<const T*>(a.dy_end)) : ld16(dy + j);
+          x[u] = load_sixteen<T, SHIFTED>(row, j, a.D, rows_all, static_cast<const T*>(a.rows_end));
         }
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t j = (int64_t)(q0 + u * NT) * V - shift;
+        if (q0 + u * NT >= pieces || j >= a.D) continue;
+        float d[V];
+        if (!SHIFTED || (j >= 0 && j + V <= a.D)) {
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) {
+            const f32x2 gi = raw_pair<T>(g[u], i);
+            sum = fma2(gi, raw_pair<T>(x[u], i), sum);
+            unpack2f(mul2(w2, gi), d[2 * i], d[2 * i + 1]);
+          }
+        } else {   // an end of the row
+          float gf[V], xf[V];
+          Elem<T>::unpack(g[u], gf);
+          Elem<T>::unpack(x[u], xf);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            if (j + e >= 0 && j + e < a.D) dot = fmaf(gf[e], xf[e], dot);
+            d[e] = w * gf[e];
+          }
+        }
+        store_floats<T, V>(out, j, a.D, true, d);
+      }
     }
+    float lo, hi;
+    unpack2f(sum, lo, hi);
+    dot += lo + hi;
   }
   dot = warp_sum(dot);
   if constexpr (NT > 32) {
@@ -514,7 +584,7 @@ cudaError_t route_of(const RouteArgs& r, cudaStream_t s) {
 
 template <typename T, int NL>
 cudaError_t route_backward_as(const RouteGradArgs& a, cudaStream_t s) {
-  return launch_chained(route_backward_kernel<T, NL>, dim3((unsigned)((a.rows + 7) / 8)), dim3(256), 0, s, a,
+  return launch_chained(route_backward_kernel<T, NL>, dim3((unsigned)((a.rows + 7) / 8)), dim3(256), 8 * 32 * NL * sizeof(float), s, a,
                         (int)lanes_aligned(a.logits, a.ld, a.E, NL, sizeof(T)), (int)lanes_aligned(a.d_logits, a.E, a.E, NL, sizeof(T)));
 }
 template <typename T>
@@ -533,29 +603,42 @@ bool whole_pieces(const void* p, int64_t worker, int64_t row, int size) {
   return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(worker * size) | (uintptr_t)(row * size)) % 16 == 0;
 }
 
+// One past the last element of [m][rows][cols].
 template <typename T>
-cudaError_t combine_of(const CombineArgs& a, cudaStream_t s) {
-  constexpr int V = Elem<T>::kVec;
-  const bool vec = a.D % V == 0 && whole_pieces(a.rows, a.rows_worker, a.rows_row, sizeof(T)) && whole_pieces(a.y, 0, a.D, sizeof(T));
-  const int64_t threads = a.m * a.T * (vec ? a.D / V : a.D);
-  return launch_chained(vec ? combine_kernel<T, V> : combine_kernel<T, 1>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+const void* tensor_end(const void* p, int64_t m, int64_t worker, int64_t rows, int64_t row, int64_t cols) {
+  if (!p || rows == 0) return p;
+  return static_cast<const T*>(p) + (m > 1 ? (m - 1) * worker : 0) + (rows - 1) * row + cols;
 }
 
-template <typename T, int V>
-cudaError_t combine_backward_as(const CombineGradArgs& a, cudaStream_t s) {
-  const int64_t slots = a.T * a.k, per = slots > a.R ? slots : a.R;
-  // a CTA for a slot where its row is long enough to keep all threads busy
-  const bool wide = a.D >= 256 * V * 2;
-  const int64_t ctas = wide ? per : (per + 7) / 8;
-  return launch_chained(wide ? combine_backward_kernel<T, V, 256> : combine_backward_kernel<T, V, 32>, dim3((unsigned)ctas, (unsigned)a.m),
-                        dim3(256), 0, s, a);
+template <typename T, bool SHIFTED>
+cudaError_t combine_as(const CombineArgs& a, cudaStream_t s) {
+  const int64_t pieces = row_pieces<T>(a.D, SHIFTED), threads = a.m * a.T * pieces;
+  auto k = a.k == 1 ? combine_kernel<T, SHIFTED, 1> : a.k == 2 ? combine_kernel<T, SHIFTED, 2> : combine_kernel<T, SHIFTED, 4>;
+  return launch_chained(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, pieces);
 }
 template <typename T>
-cudaError_t combine_backward_of(const CombineGradArgs& a, cudaStream_t s) {
-  constexpr int V = Elem<T>::kVec;
-  const bool vec = a.D % V == 0 && whole_pieces(a.rows, a.rows_worker, a.rows_row, sizeof(T)) &&
-                   whole_pieces(a.d_y, a.dy_worker, a.dy_row, sizeof(T)) && whole_pieces(a.d_rows, 0, a.D, sizeof(T));
-  return vec ? combine_backward_as<T, V>(a, s) : combine_backward_as<T, 1>(a, s);
+cudaError_t combine_of(CombineArgs a, cudaStream_t s) {
+  const bool whole = a.D % Elem<T>::kVec == 0 && whole_pieces(a.rows, a.rows_worker, a.rows_row, sizeof(T)) && whole_pieces(a.y, 0, a.D, sizeof(T));
+  a.rows_end = tensor_end<T>(a.rows, a.m, a.rows_worker, a.R, a.rows_row, a.D);
+  return whole ? combine_as<T, false>(a, s) : combine_as<T, true>(a, s);
+}
+
+template <typename T, bool SHIFTED>
+cudaError_t combine_backward_as(const CombineGradArgs& a, cudaStream_t s) {
+  const int64_t slots = a.T * a.k, per = slots > a.R ? slots : a.R, pieces = row_pieces<T>(a.D, SHIFTED);
+  // a CTA for a slot where its row is long enough to keep all threads busy
+  const bool wide = pieces >= 512;
+  const int64_t ctas = wide ? per : (per + 7) / 8;
+  return launch_chained(wide ? combine_backward_kernel<T, SHIFTED, 256> : combine_backward_kernel<T, SHIFTED, 32>,
+                        dim3((unsigned)ctas, (unsigned)a.m), dim3(256), 0, s, a, (int)pieces);
+}
+template <typename T>
+cudaError_t combine_backward_of(CombineGradArgs a, cudaStream_t s) {
+  const bool whole = a.D % Elem<T>::kVec == 0 && whole_pieces(a.rows, a.rows_worker, a.rows_row, sizeof(T)) &&
+                     whole_pieces(a.d_y, a.dy_worker, a.dy_row, sizeof(T)) && whole_pieces(a.d_rows, 0, a.D, sizeof(T));
+  a.rows_end = tensor_end<T>(a.rows, a.m, a.rows_worker, a.R, a.rows_row, a.D);
+  a.dy_end = tensor_end<T>(a.d_y, a.m, a.dy_worker, a.T, a.dy_row, a.D);
+  return whole ? combine_backward_as<T, false>(a, s) : combine_backward_as<T, true>(a, s);
 }
 
 }  // namespace

@@ -213,6 +213,54 @@ __device__ __forceinline__ f32x2 raw_pair(const uint4& w, int i) {
     return pack2f(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
   }
 }
+// Elements off .. off + 7 of the sixteen in a, b.
+__device__ __forceinline__ uint4 eight_from(const uint4& a, const uint4& b, int off) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (off & 4) {
+#pragma unroll
+    for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+  }
+  if (off & 2) {
+#pragma unroll
+    for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+  }
+  if (off & 1) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// 16 bytes from element j of a row of n on, whatever its alignment: out of the two aligned pieces they lie in, where the tensor
+// ([begin, end)) holds both, else element by element.  Elements outside [0, n) may be anything.
+template <typename T>
+__device__ __forceinline__ uint4 load_shifted(const T* row, int64_t j, int64_t n, const T* begin, const T* end) {
+  constexpr int V = Elem<T>::kVec;
+  const T* p = row + j;
+  const int off = row_shift(p);
+  const T* base = p - off;
+  if (off == 0 && j >= 0 && j + V <= n) return ld16_stream(p);
+  if (base >= begin && base + 2 * V <= end) {
+    const uint4 a = ld16(base), b = ld16(base + V);
+    if constexpr (V == 8) {
+      return eight_from(a, b, off);
+    } else {
+      return off == 0 ? a : off == 1 ? make_uint4(a.y, a.z, a.w, b.x) : off == 2 ? make_uint4(a.z, a.w, b.x, b.y) : make_uint4(a.w, b.x, b.y, b.z);
+    }
+  }
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (V == 4) {
+      w[e] = j + e >= 0 && j + e < n ? reinterpret_cast<const uint32_t*>(row)[j + e] : 0u;
+    } else {
+      const int64_t k = j + 2 * e;
+      const uint32_t lo = k >= 0 && k < n ? reinterpret_cast<const uint16_t*>(row)[k] : 0u;
+      const uint32_t hi = k + 1 >= 0 && k + 1 < n ? reinterpret_cast<const uint16_t*>(row)[k + 1] : 0u;
+      w[e] = lo | (hi << 16);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // The largest element of a piece; KEEP_NAN: NaN if there is one (else it is passed over).
 template <typename T, bool KEEP_NAN>
 __device__ __forceinline__ float raw_max(const uint4& w) {

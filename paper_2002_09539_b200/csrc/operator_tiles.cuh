@@ -192,23 +192,6 @@ struct PadOperands {
   PadOperand op[3];
   int64_t cols, pitch;
 };
-// Elements off .. off + 7 of the sixteen in a, b.
-__device__ __forceinline__ uint4 eight_from(const uint4& a, const uint4& b, int off) {
-  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  if (off & 4) {
-#pragma unroll
-    for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
-  }
-  if (off & 2) {
-#pragma unroll
-    for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
-  }
-  if (off & 1) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ PadOperands all) {
   launch_gate();
   const PadOperand& o = all.op[blockIdx.z];

@@ -404,7 +404,7 @@ olsgd_status olsgd_expert_combine(int32_t m, int64_t T, int32_t k, int64_t R, in
   if (R > 0) OLSGD_TRY(check_operand(GatedOperand{rows, rows_worker_stride, rows_row_stride}, "rows", m, R, D, elem_size(dtype)));
   OLSGD_REFUSE_IF(!aligned_to(places, 4) || (weights && !aligned_to(weights, 4)), "places must be non-null, places and weights 4-byte aligned");
   OLSGD_REFUSE_IF(!aligned_to(y, elem_size(dtype)), "y must be non-null and aligned to its type");
-  const CombineArgs a{dtype, k, m, T, R, D, rows, rows_worker_stride, rows_row_stride, places, weights, y};
+  const CombineArgs a{dtype, k, m, T, R, D, rows, rows_worker_stride, rows_row_stride, places, weights, y, nullptr};
   return launched(launch_combine(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_combine");
 }
 
@@ -428,7 +428,7 @@ olsgd_status olsgd_expert_combine_backward(int32_t m, int64_t T, int32_t k, int6
                     "places, weights and d_weights must be non-null and 4-byte aligned");
   }
   const CombineGradArgs a{dtype, k, m, T, R, D, d_y, d_y_worker_stride, d_y_row_stride, rows, rows_worker_stride, rows_row_stride,
-                          places, tokens, weights, d_rows, d_weights};
+                          places, tokens, weights, d_rows, d_weights, nullptr, nullptr};
   return launched(launch_combine_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_expert_combine_backward");
 }
 

@@ -116,6 +116,7 @@ struct CombineArgs {
   const int32_t* places;
   const float* weights;
   void* y;
+  const void* rows_end;      // (set by the launch)
 };
 cudaError_t launch_combine(const CombineArgs& a, cudaStream_t s);
 struct CombineGradArgs {
@@ -129,6 +130,7 @@ struct CombineGradArgs {
   const float* weights;
   void* d_rows;
   float* d_weights;
+  const void *rows_end, *dy_end;   // (set by the launch)
 };
 cudaError_t launch_combine_backward(const CombineGradArgs& a, cudaStream_t s);
 
