@@ -529,6 +529,287 @@ __global__ void __launch_bounds__(kFusedThreads, 2) distill_fused_kernel(const D
   }
 }
 
+// The same for rows that all start on a 16-byte boundary, by clusters that stay.  Sixteen warps have the row's
+// elements: each takes its own maximum and sum, so that a row has one barrier, behind which every warp joins what
+// all warps of the cluster have left in its shared memory.  A seventeenth warp brings the rows in (bulk copies, two
+// buffers), has the pairs and writes the loss; it stores the gradients at the pairs' tokens behind the next row's
+// barrier, when the others' stores of this row are done.
+// 4096 x 32768 bf16, 32 pairs: 200 us one row a cluster, 175 with the rows on their way early but the pairs and two more
+// barriers in all warps (816 instructions a warp and row, half of them reductions).
+constexpr int kStages = 2;
+constexpr int kStreamWarps = kFusedThreads / 32, kStreamThreads = kFusedThreads + 32;
+struct StreamShared {
+  uint64_t full[kStages];
+  Sum stats[2][kMaxCluster * kStreamWarps];   // of the cluster's warps, of rows in turn
+  int teacher[2];                             // whether the row has one
+};
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ int g_distill_status;   // a bounded wait gave up (olsgd_operators_join)
+
+// Waits for a copy, a second at most.
+__device__ __forceinline__ bool copy_arrived(uint32_t bar, uint32_t parity) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    if (ok) return true;
+    if (it % 64 == 0) {
+      uint64_t now;
+      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > 1000000000ull) return false;
+    }
+  }
+}
+
+// v to this CTA-relative address in the cluster's CTA `rank`.
+__device__ __forceinline__ void remote_store(void* p, uint32_t rank, float a, float b) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(shared_address(p)), "r"(rank));
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(a), "f"(b) : "memory");
+}
+__device__ __forceinline__ float redux_max(float v) {
+  asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v));
+  return v;
+}
+
+// KP: pairs of a lane of the seventeenth warp.
+template <typename T, bool CLUSTER, int KP>
+__global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const DistillArgs a, int ctas) {
+  constexpr int VEC = Elem<T>::kVec, U = kFusedValues / VEC, NT = kFusedThreads;
+  extern __shared__ __align__(16) uint8_t stage_memory[];   // [kStages][kFusedPart] elements
+  __shared__ StreamShared sh;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rank = CLUSTER ? (int)cluster_rank() : 0;
+  const int64_t first = CLUSTER ? blockIdx.x / ctas : blockIdx.x, step = CLUSTER ? gridDim.x / ctas : gridDim.x;
+  const int V = (int)a.V, begin = rank * kFusedPart;
+  const int here = min(kFusedPart, V - begin);                                // elements of this CTA's part
+  const uint32_t bytes = (uint32_t)(here * (int)sizeof(T)) & ~15u;            // (a last partial piece is loaded by itself)
+  const float c = a.inv_t * kLog2e;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i)
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sh.full[i])));
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  launch_gate();
+  __syncthreads();
+  if (CLUSTER) cluster_sync();   // every CTA has begun: its memory can be written
+  const auto meet = [&] {
+    __syncwarp();
+    if (CLUSTER) cluster_sync();
+    else __syncthreads();
+  };
+  // A row's statistics, behind its barrier, by a warp.
+  const auto joined = [&](int n) {
+    const int all = CLUSTER ? ctas * kStreamWarps : kStreamWarps;
+    float m = -INFINITY;
+    for (int i = lane; i < all; i += 32) m = fmaxf(m, sh.stats[n & 1][i].m);
+    Sum r;
+    r.m = redux_max(m);
+    r.s = 0.f;
+    for (int i = lane; i < all; i += 32) {
+      const Sum v = sh.stats[n & 1][i];
+      r.s += v.m == -INFINITY ? v.s : v.s * ex2((v.m - base_of(r.m)) * c);
+    }
+    r.s = warp_sum(r.s);
+    return r;
+  };
+
+  if (warp < kStreamWarps) {
+    bool gave_up = false;
+    int n = 0;
+    for (int64_t r = first; r < a.rows; r += step, ++n) {
+      const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+      const float weight = a.d_loss[r];   // (used behind the barrier)
+      if (bytes && !copy_arrived(shared_address(&sh.full[n % kStages]), (n / kStages) & 1)) gave_up = true;
+      const T* part_row = reinterpret_cast<const T*>(stage_memory) + (n % kStages) * kFusedPart;
+      uint4 w[U];
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = (u * NT + (int)threadIdx.x) * VEC;
+        if (j + VEC <= here) w[u] = *reinterpret_cast<const uint4*>(part_row + j);
+        else w[u] = load_raw<T>(row, j < here ? begin + j : V, V, minus_inf<T>());
+        mx = fmaxf(mx, raw_max<T, false>(w[u]));
+      }
+      const float m = redux_max(mx);
+      f32x2 e[U][VEC / 2];
+      f32x2 s2 = 0;
+      {
+        const float base = -base_of(m);
+        const f32x2 minus_base = pack2f(base, base), c2 = pack2f(c, c);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < VEC / 2; ++i) {
+            float lo, hi;
+            unpack2f(mul2(add2(raw_pair<T>(w[u], i), minus_base), c2), lo, hi);
+            e[u][i] = pack2f(ex2(lo), ex2(hi));
+            s2 = add2(s2, e[u][i]);
+          }
+      }
+      float lo, hi;
+      unpack2f(s2, lo, hi);
+      const float s = warp_sum(lo + hi);
+      if (CLUSTER) {
+        if (lane < ctas) remote_store(&sh.stats[n & 1][rank * kStreamWarps + warp], lane, m, s);
+      } else if (lane == 0) {
+        sh.stats[n & 1][warp] = Sum{m, s};
+      }
+      meet();
+      const Sum student = joined(n);
+      T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
+      const bool aligned = row_shift(out) == 0;
+      if (weight == 0.f || empty(student) || !sh.teacher[n & 1]) {
+        const float none[VEC] = {};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int j = (u * NT + (int)threadIdx.x) * VEC;
+          if (j < here) store_floats<T, VEC, true>(out, begin + j, V, aligned, none);
+        }
+      } else {
+        // (values relative to the warp's own maximum)
+        const float scale = weight * a.inv_t / student.s * (m == -INFINITY ? 1.f : ex2((m - base_of(student.m)) * c));
+        const f32x2 scale2 = pack2f(scale, scale);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int j = (u * NT + (int)threadIdx.x) * VEC;
+          float d[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC / 2; ++i) unpack2f(mul2(e[u][i], scale2), d[2 * i], d[2 * i + 1]);
+          if (j < here) store_floats<T, VEC, true>(out, begin + j, V, aligned, d);
+        }
+      }
+    }
+    if (n > 0) meet();   // the last row's stores are done
+    if (gave_up) atomicExch(&g_distill_status, (int)OLSGD_ETIMEOUT);
+  } else {
+    const auto request = [&](int64_t r, int n) {
+      if (lane == 0 && bytes && r < a.rows)
+        bulk_load(shared_address(stage_memory) + (n % kStages) * kFusedPart * (int)sizeof(T), static_cast<const T*>(a.logits) + r * a.ld + begin, bytes,
+                  shared_address(&sh.full[n % kStages]));
+    };
+    // Three loads deep (the id, the logits there): the ids come two rows ahead, the rest one.
+    const auto fetch_ids = [&](int64_t r, int32_t* id) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) id[i] = r < a.rows && i * 32 + lane < a.K ? a.ids[r * a.K + i * 32 + lane] : -1;
+    };
+    const auto fetch_pairs = [&](int64_t r, const int32_t* id, Pair* p) {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        p[i] = Pair{-1, -INFINITY, 0.f};
+        if (id[i] >= 0 && id[i] < V) {
+          p[i].id = id[i];
+          p[i].z = load_any(a.teacher, a.teacher_dtype, r * a.K + i * 32 + lane);
+          p[i].x = Elem<T>::to_float(static_cast<const T*>(a.logits)[r * a.ld + id[i]]);
+        }
+      }
+    };
+    for (int i = 0; i < kStages; ++i) request(first + i * step, i);
+    int32_t ids[KP];
+    Pair now[KP], next[KP];
+    fetch_ids(first, ids);
+    fetch_pairs(first, ids, next);
+    fetch_ids(first + step, ids);
+    int32_t old_id[KP];
+    float old_d[KP];   // gradients at the last row's tokens
+    T* old_out = nullptr;
+    const auto store_old = [&] {
+      if (!old_out) return;
+#pragma unroll
+      for (int i = 0; i < KP; ++i)
+        if (old_id[i] >= begin && old_id[i] < begin + here) old_out[old_id[i]] = Elem<T>::from_float(old_d[i]);
+    };
+    int n = 0;
+    for (int64_t r = first; r < a.rows; r += step, ++n) {
+      const float weight = a.d_loss[r];
+#pragma unroll
+      for (int i = 0; i < KP; ++i) now[i] = next[i];
+      if (r + step < a.rows) fetch_pairs(r + step, ids, next);
+      fetch_ids(r + 2 * step, ids);
+      // the teacher's side
+      Sum teacher{-INFINITY, 0.f};
+#pragma unroll
+      for (int i = 0; i < KP; ++i) teacher.m = fmaxf(teacher.m, now[i].z);
+      teacher.m = redux_max(teacher.m);
+#pragma unroll
+      for (int i = 0; i < KP; ++i) teacher.s += ex2((now[i].z - base_of(teacher.m)) * c);
+      teacher.s = warp_sum(teacher.s);
+      const bool none = empty(teacher);
+      const float log_teacher = log_sum(teacher);
+      if (lane == 0) sh.teacher[n & 1] = !none;
+      meet();
+      store_old();
+      request(r + kStages * step, n + kStages);   // (the buffer was read ahead of the barrier)
+      const Sum student = joined(n);
+      const float log_s = log_sum(student);
+      float loss = 0.f, q[KP];
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        const PairTerm t = pair_term(now[i], teacher, log_teacher, student, log_s, a.inv_t, c);
+        q[i] = t.q;
+        loss += t.loss;
+      }
+      loss = warp_sum(loss);
+      if (rank == 0 && lane == 0) {
+        a.loss[r] = loss;
+        a.stats[2 * r] = student.m;
+        a.stats[2 * r + 1] = log_s;
+      }
+      old_out = weight == 0.f || none || empty(student) ? nullptr : static_cast<T*>(a.d_logits) + r * a.ldd;
+      // the first of the pairs with a token has the sum of all of them
+      float sum[KP];
+      bool leads[KP];
+      if (KP == 1) {
+        const uint32_t same = __match_any_sync(0xffffffffu, now[0].id);
+        leads[0] = __ffs(same) - 1 == lane;
+        sum[0] = q[0];
+        if (__any_sync(0xffffffffu, now[0].id >= 0 && (same & (same - 1)))) {
+          sum[0] = 0.f;
+          for (int o = 0; o < 32; ++o) {
+            const float other = __shfl_sync(0xffffffffu, q[0], o);
+            if (same >> o & 1) sum[0] += other;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < KP; ++i) {
+          sum[i] = 0.f;
+          leads[i] = true;
+        }
+#pragma unroll
+        for (int k = 0; k < KP; ++k)
+          for (int o = 0; o < 32 && k * 32 + o < a.K; ++o) {
+            const int32_t id = __shfl_sync(0xffffffffu, now[k].id, o);
+            const float other = __shfl_sync(0xffffffffu, q[k], o);
+#pragma unroll
+            for (int i = 0; i < KP; ++i)
+              if (id == now[i].id) {
+                sum[i] += other;
+                if (k * 32 + o < i * 32 + lane) leads[i] = false;
+              }
+          }
+      }
+      const float g = weight * a.inv_t, base = base_of(student.m), scale = g / student.s;
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        old_id[i] = leads[i] ? now[i].id : -1;
+        old_d[i] = fmaf(-g, sum[i], scale * ex2((now[i].x - base) * c));
+      }
+    }
+    if (n > 0) meet();
+    store_old();
+  }
+}
+
 // ------------------------------------------------------------------------------ host
 int64_t chunk_count(int64_t V, int dtype) {
   return (V + (dtype == OLSGD_F32 ? 3 : 7) + kChunkElems - 1) / kChunkElems;
@@ -574,10 +855,44 @@ cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
   return launch_chained(distill_grad_kernel<T>, dim3((unsigned)a.rows, (unsigned)((pieces + per - 1) / per)), dim3(kThreads), 0, s, a);
 }
 
+// As many clusters as the GPU holds at once.
+template <typename T, bool CLUSTER, int KP>
+cudaError_t stream_as(const DistillArgs& a, int ctas, cudaStream_t s) {
+  constexpr size_t smem = (size_t)kStages * kFusedPart * sizeof(T);
+  static PerDeviceSmem configured;
+  auto kern = distill_stream_kernel<T, CLUSTER, KP>;
+  const cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
+  if (e != cudaSuccess) return e;
+  const int64_t resident = sizeof(T) == 2 ? 2 : 1, room = sm_count() * resident / ctas, clusters = a.rows < room ? a.rows : room;
+  if (!CLUSTER) return launch_chained(kern, dim3((unsigned)clusters), dim3(kStreamThreads), smem, s, a, 1);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(clusters * ctas));
+  cfg.blockDim = dim3(kStreamThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = g_launch_overlap ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, a, ctas);
+}
+template <typename T>
+cudaError_t stream_rows(const DistillArgs& a, int ctas, cudaStream_t s) {
+  if (a.K <= 32) return ctas == 1 ? stream_as<T, false, 1>(a, ctas, s) : stream_as<T, true, 1>(a, ctas, s);
+  if (a.K <= 64) return ctas == 1 ? stream_as<T, false, 2>(a, ctas, s) : stream_as<T, true, 2>(a, ctas, s);
+  return ctas == 1 ? stream_as<T, false, 8>(a, ctas, s) : stream_as<T, true, 8>(a, ctas, s);
+}
+
 template <typename T>
 cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax) return a.d_loss ? warp_rows<T, true, true>(a, s) : warp_rows<T, true, false>(a, s);
   const int ctas = a.d_loss ? cluster_of(a.V, a.dtype, rows_aligned<T>(a)) : 0;
+  if (ctas > 0 && rows_aligned<T>(a)) return stream_rows<T>(a, ctas, s);
   if (ctas == 1) return launch_chained(distill_fused_kernel<T, false>, dim3((unsigned)a.rows), dim3(kFusedThreads), 0, s, a, 1);
   if (ctas > 1) {
     cudaLaunchConfig_t cfg{};
@@ -624,6 +939,15 @@ cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s) {
     case OLSGD_BF16: return gradient<__nv_bfloat16>(a, s);
     default: return gradient<__half>(a, s);
   }
+}
+
+cudaError_t distill_status(int* status) {
+  cudaError_t e = cudaMemcpyFromSymbol(status, g_distill_status, sizeof(int));
+  if (e == cudaSuccess && *status != 0) {
+    const int zero = 0;
+    e = cudaMemcpyToSymbol(g_distill_status, &zero, sizeof(int));
+  }
+  return e;
 }
 
 }  // namespace olsgd

@@ -1158,9 +1158,10 @@ cudaError_t operators_status(int* status, cudaStream_t s) {
     const int zero = 0;
     OLSGD_STEP(cudaMemcpyToSymbol(g_operator_status, &zero, sizeof(int)));
   }
-  int product = 0;
+  int product = 0, distill = 0;
   OLSGD_STEP(product_status(&product));
-  if (*status == 0) *status = product;
+  OLSGD_STEP(distill_status(&distill));
+  if (*status == 0) *status = product != 0 ? product : distill;
   return cudaSuccess;
 }
 

@@ -180,6 +180,7 @@ struct DistillArgs {
 size_t distill_workspace(int dtype, int64_t rows, int64_t V, bool gradient);
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s);
 cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s);
+cudaError_t distill_status(int* status);   // of its bounded waits, for operators_status
 
 // Joins the stream; *status: OLSGD_OK, or what a bounded wait left since the last call.
 cudaError_t operators_status(int* status, cudaStream_t s);

@@ -83,7 +83,8 @@ def _pairs(g, N, V, K):
 
 
 SHAPES = [(1, 1, 1), (5, 2, 2), (3, 10, 3), (33, 32, 32), (7, 33, 5), (9, 257, 64), (4, 1000, 256), (6, 1024, 8), (5, 1025, 7), (3, 4099, 32), (300, 2049, 4),
-          (2, 16384, 20), (3, 16385, 16), (2, 32768, 128), (2, 50021, 32), (1, 131072, 256), (1, 131079, 9), (1, 200003, 64), (700, 1500, 3), (3, 7, 40)]
+          (2, 16384, 20), (3, 16385, 16), (2, 32768, 128), (2, 50021, 32), (1, 131072, 256), (1, 131079, 9), (1, 200003, 64), (700, 1500, 3), (3, 7, 40),
+          (900, 2048, 8), (400, 20000, 5), (350, 33000, 2), (330, 1032, 3), (90, 100000, 4)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
