@@ -410,129 +410,10 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float remote_float(const float* p, uint32_t rank) {
-  uint32_t local = (uint32_t)__cvta_generic_to_shared(p), at;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(local), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-  return v;
-}
-
-// Cluster: row r; its CTAs hold kFusedPart elements each.
-template <typename T, bool CLUSTER>
-__global__ void __launch_bounds__(kFusedThreads, 2) distill_fused_kernel(const DistillArgs a, int ctas) {
-  constexpr int VEC = Elem<T>::kVec, U = kFusedValues / VEC, NT = kFusedThreads;
-  __shared__ Sum sh[NT / 32];
-  __shared__ float sums[NT / 32];
-  __shared__ float mine[2];
-  __shared__ PairTable table;
-  launch_gate();
-  const int rank = CLUSTER ? (int)cluster_rank() : 0;
-  const int64_t r = CLUSTER ? blockIdx.x / ctas : blockIdx.x;
-  const int V = (int)a.V;
-  const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-  T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
-  const int shift = row_shift(row);
-  const bool aligned = row_shift(out) == shift;
-  const float c = a.inv_t * kLog2e;
-  const int begin = rank * kFusedPart - shift, j0 = begin + (int)threadIdx.x * VEC;
-  uint4 w[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) w[u] = load_raw<T>(row, j0 + u * NT * VEC, V, minus_inf<T>());
-  const Pair p = fetch_pair<T>(a, row, r, threadIdx.x);
-  float mx = -INFINITY;
-#pragma unroll
-  for (int u = 0; u < U; ++u) mx = fmaxf(mx, raw_max<T, false>(w[u]));
-  // both maxima, then both sums
-  Sum part, teacher;
-  {
-    const float a0 = warp_max(mx), b0 = warp_max(p.z);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = Sum{a0, b0};
-    __syncthreads();
-    const Sum v = (threadIdx.x & 31) < NT / 32 ? sh[threadIdx.x & 31] : Sum{-INFINITY, -INFINITY};
-    part.m = warp_max(v.m);
-    teacher.m = warp_max(v.s);
-    __syncthreads();
-  }
-  float e[U][VEC];
-  f32x2 s2 = 0;
-  {
-    const float base = -base_of(part.m);
-    const f32x2 minus_base = pack2f(base, base), c2 = pack2f(c, c);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) {
-        float lo, hi;
-        unpack2f(mul2(add2(raw_pair<T>(w[u], i), minus_base), c2), lo, hi);
-        e[u][2 * i] = ex2(lo);
-        e[u][2 * i + 1] = ex2(hi);
-        s2 = add2(s2, pack2f(e[u][2 * i], e[u][2 * i + 1]));
-      }
-  }
-  {
-    float lo, hi;
-    unpack2f(s2, lo, hi);
-    const float a0 = warp_sum(lo + hi), b0 = warp_sum(ex2((p.z - base_of(teacher.m)) * c));
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = Sum{a0, b0};
-    __syncthreads();
-    const Sum v = (threadIdx.x & 31) < NT / 32 ? sh[threadIdx.x & 31] : Sum{0.f, 0.f};
-    part.s = warp_sum(v.m);
-    teacher.s = warp_sum(v.s);
-  }
-  Sum student = part;
-  if (CLUSTER) {
-    if (threadIdx.x == 0) {
-      mine[0] = part.m;
-      mine[1] = part.s;
-    }
-    cluster_sync();
-    const int lane = threadIdx.x & 31;
-    Sum v{-INFINITY, 0.f};
-    if (lane < ctas) v = Sum{remote_float(&mine[0], lane), remote_float(&mine[1], lane)};
-    student = shfl_join(v, c);
-    cluster_sync();   // no CTA leaves while another reads its sums
-  }
-  const float log_s = log_sum(student), log_teacher = log_sum(teacher);
-  const PairTerm t = pair_term(p, teacher, log_teacher, student, log_s, a.inv_t, c);
-  if ((int)threadIdx.x < a.K) {
-    table.q[threadIdx.x] = t.q;
-    table.id[threadIdx.x] = p.id;
-  }
-  const float loss = warp_sum(t.loss);
-  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = loss;
-  const float weight = a.d_loss[r];
-  GradRow g;
-  g.zero = weight == 0.f || empty(teacher) || empty(student);
-  g.g = weight * a.inv_t;
-  g.base = base_of(student.m);
-  g.scale = g.g / student.s;
-  // (values relative to the CTA's own maximum)
-  const float scale = g.zero || (part.m == -INFINITY && part.s == 0.f) ? 0.f : g.scale * (part.m == -INFINITY ? 1.f : ex2((part.m - g.base) * c));
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int j = j0 + u * NT * VEC;
-    if (j >= V) break;
-    float d[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) d[i] = scale == 0.f ? 0.f : e[u][i] * scale;
-    store_floats<T, VEC, true>(out, j, V, aligned, d);
-  }
-  __syncthreads();
-  if (!g.zero) store_pairs<T>(a, table, p, g, begin, begin + kFusedPart, c, out);
-  if (rank == 0 && threadIdx.x == 0) {
-    float all = 0.f;
-    for (int i = 0; i < NT / 32; ++i) all += sums[i];
-    a.loss[r] = all;
-    a.stats[2 * r] = student.m;
-    a.stats[2 * r + 1] = log_s;
-  }
-}
-
-// The same for rows that all start on a 16-byte boundary, by clusters that stay.  Sixteen warps have the row's
-// elements: each takes its own maximum and sum, so that a row has one barrier, behind which every warp joins what
-// all warps of the cluster have left in its shared memory.  A seventeenth warp brings the rows in (bulk copies, two
-// buffers), has the pairs and writes the loss; it stores the gradients at the pairs' tokens behind the next row's
+// Clusters that stay, a row at a time; its CTAs hold kFusedPart elements each, counted from the 16-byte boundary at
+// or before the row.  Sixteen warps have the row's elements: each takes its own maximum and sum, so that a row has one barrier, behind which every warp joins what
+// all warps of the cluster have left in its shared memory.  A seventeenth warp brings the rows in (bulk copies of
+// its whole 16-byte pieces, two buffers), has the pairs and writes the loss; it stores the gradients at the pairs' tokens behind the next row's
 // barrier, when the others' stores of this row are done.
 // 4096 x 32768 bf16, 32 pairs: 200 us one row a cluster, 175 with the rows on their way early but the pairs and two more
 // barriers in all warps (816 instructions a warp and row, half of them reductions).
@@ -590,10 +471,17 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rank = CLUSTER ? (int)cluster_rank() : 0;
   const int64_t first = CLUSTER ? blockIdx.x / ctas : blockIdx.x, step = CLUSTER ? gridDim.x / ctas : gridDim.x;
-  const int V = (int)a.V, begin = rank * kFusedPart;
-  const int here = min(kFusedPart, V - begin);                                // elements of this CTA's part
-  const uint32_t bytes = (uint32_t)(here * (int)sizeof(T)) & ~15u;            // (a last partial piece is loaded by itself)
+  const int V = (int)a.V;
   const float c = a.inv_t * kLog2e;
+  // Of a row: its first element; where this CTA's part begins (ahead of the row by up to a piece); the part's
+  // whole pieces, which are copied (partial ones are loaded by the threads that have them).
+  const auto row_at = [&](int64_t r) { return static_cast<const T*>(a.logits) + r * a.ld; };
+  const auto begin_of = [&](const T* row) { return rank * kFusedPart - row_shift(row); };
+  const auto first_whole = [&](int begin) { return begin < 0 ? 1 : 0; };
+  const auto whole_bytes = [&](int begin) {
+    const int last = min(kFusedPart / VEC, max(0, V - begin) / VEC);
+    return (uint32_t)max(0, last - first_whole(begin)) * 16u;
+  };
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i)
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sh.full[i])));
@@ -625,19 +513,24 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
 
   if (warp < kStreamWarps) {
     bool gave_up = false;
+    uint32_t copies = 0;   // bit i: parity of the next copy to buffer i
     int n = 0;
     for (int64_t r = first; r < a.rows; r += step, ++n) {
-      const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+      const T* row = row_at(r);
+      const int begin = begin_of(row);
       const float weight = a.d_loss[r];   // (used behind the barrier)
-      if (bytes && !copy_arrived(shared_address(&sh.full[n % kStages]), (n / kStages) & 1)) gave_up = true;
+      if (whole_bytes(begin)) {
+        if (!copy_arrived(shared_address(&sh.full[n % kStages]), copies >> (n % kStages) & 1)) gave_up = true;
+        copies ^= 1u << (n % kStages);
+      }
       const T* part_row = reinterpret_cast<const T*>(stage_memory) + (n % kStages) * kFusedPart;
       uint4 w[U];
       float mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int j = (u * NT + (int)threadIdx.x) * VEC;
-        if (j + VEC <= here) w[u] = *reinterpret_cast<const uint4*>(part_row + j);
-        else w[u] = load_raw<T>(row, j < here ? begin + j : V, V, minus_inf<T>());
+        const int at = (u * NT + (int)threadIdx.x) * VEC, j = begin + at;
+        if (j >= 0 && j + VEC <= V) w[u] = *reinterpret_cast<const uint4*>(part_row + at);
+        else w[u] = load_raw<T>(row, j, V, minus_inf<T>());
         mx = fmaxf(mx, raw_max<T, false>(w[u]));
       }
       const float m = redux_max(mx);
@@ -667,13 +560,13 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
       meet();
       const Sum student = joined(n);
       T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
-      const bool aligned = row_shift(out) == 0;
+      const bool aligned = row_shift(out) == row_shift(row);
       if (weight == 0.f || empty(student) || !sh.teacher[n & 1]) {
         const float none[VEC] = {};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int j = (u * NT + (int)threadIdx.x) * VEC;
-          if (j < here) store_floats<T, VEC, true>(out, begin + j, V, aligned, none);
+          const int j = begin + (u * NT + (int)threadIdx.x) * VEC;
+          if (j < V) store_floats<T, VEC, true>(out, j, V, aligned, none);
         }
       } else {
         // (values relative to the warp's own maximum)
@@ -681,11 +574,11 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
         const f32x2 scale2 = pack2f(scale, scale);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int j = (u * NT + (int)threadIdx.x) * VEC;
+          const int j = begin + (u * NT + (int)threadIdx.x) * VEC;
           float d[VEC];
 #pragma unroll
           for (int i = 0; i < VEC / 2; ++i) unpack2f(mul2(e[u][i], scale2), d[2 * i], d[2 * i + 1]);
-          if (j < here) store_floats<T, VEC, true>(out, begin + j, V, aligned, d);
+          if (j < V) store_floats<T, VEC, true>(out, j, V, aligned, d);
         }
       }
     }
@@ -693,8 +586,12 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
     if (gave_up) atomicExch(&g_distill_status, (int)OLSGD_ETIMEOUT);
   } else {
     const auto request = [&](int64_t r, int n) {
-      if (lane == 0 && bytes && r < a.rows)
-        bulk_load(shared_address(stage_memory) + (n % kStages) * kFusedPart * (int)sizeof(T), static_cast<const T*>(a.logits) + r * a.ld + begin, bytes,
+      if (lane != 0 || r >= a.rows) return;
+      const T* row = row_at(r);
+      const int begin = begin_of(row), skip = first_whole(begin) * VEC;
+      const uint32_t bytes = whole_bytes(begin);
+      if (bytes)
+        bulk_load(shared_address(stage_memory) + ((n % kStages) * kFusedPart + skip) * (int)sizeof(T), row + begin + skip, bytes,
                   shared_address(&sh.full[n % kStages]));
     };
     // Three loads deep (the id, the logits there): the ids come two rows ahead, the rest one.
@@ -709,7 +606,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
         if (id[i] >= 0 && id[i] < V) {
           p[i].id = id[i];
           p[i].z = load_any(a.teacher, a.teacher_dtype, r * a.K + i * 32 + lane);
-          p[i].x = Elem<T>::to_float(static_cast<const T*>(a.logits)[r * a.ld + id[i]]);
+          p[i].x = Elem<T>::to_float(row_at(r)[id[i]]);
         }
       }
     };
@@ -722,11 +619,12 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
     int32_t old_id[KP];
     float old_d[KP];   // gradients at the last row's tokens
     T* old_out = nullptr;
+    int old_begin = 0;
     const auto store_old = [&] {
       if (!old_out) return;
 #pragma unroll
       for (int i = 0; i < KP; ++i)
-        if (old_id[i] >= begin && old_id[i] < begin + here) old_out[old_id[i]] = Elem<T>::from_float(old_d[i]);
+        if (old_id[i] >= 0 && old_id[i] >= old_begin && old_id[i] < old_begin + kFusedPart) old_out[old_id[i]] = Elem<T>::from_float(old_d[i]);
     };
     int n = 0;
     for (int64_t r = first; r < a.rows; r += step, ++n) {
@@ -764,6 +662,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
         a.stats[2 * r] = student.m;
         a.stats[2 * r + 1] = log_s;
       }
+      old_begin = begin_of(row_at(r));
       old_out = weight == 0.f || none || empty(student) ? nullptr : static_cast<T*>(a.d_logits) + r * a.ldd;
       // the first of the pairs with a token has the sum of all of them
       float sum[KP];
@@ -892,24 +791,7 @@ template <typename T>
 cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax) return a.d_loss ? warp_rows<T, true, true>(a, s) : warp_rows<T, true, false>(a, s);
   const int ctas = a.d_loss ? cluster_of(a.V, a.dtype, rows_aligned<T>(a)) : 0;
-  if (ctas > 0 && rows_aligned<T>(a)) return stream_rows<T>(a, ctas, s);
-  if (ctas == 1) return launch_chained(distill_fused_kernel<T, false>, dim3((unsigned)a.rows), dim3(kFusedThreads), 0, s, a, 1);
-  if (ctas > 1) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(a.rows * ctas));
-    cfg.blockDim = dim3(kFusedThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ctas;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = g_launch_overlap ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, distill_fused_kernel<T, true>, a, ctas);
-  }
+  if (ctas > 0) return stream_rows<T>(a, ctas, s);
   const Plan p = plan(a.rows, a.V, a.dtype);
   float2* part = p.nsplit > 1 ? static_cast<float2*>(a.ws) : nullptr;
   cudaError_t e = launch_chained(distill_row_kernel<T>, dim3((unsigned)a.rows, (unsigned)p.nsplit), dim3(kThreads), 0, s, a, p.nchunks, p.cps, part);

@@ -449,7 +449,7 @@ template <typename T, bool SHIFTED, int NT>
 __global__ void __launch_bounds__(256, 4) combine_backward_kernel(const CombineGradArgs a, int pieces) {
   constexpr int V = Elem<T>::kVec, U = SHIFTED ? 2 : 4;
   launch_gate();
-  const int64_t slots = a.T * a.k, per = slots > a.R ? slots : a.R;
+  const int64_t slots = a.T * a.k;
   const int64_t at = (int64_t)blockIdx.x * (256 / NT) + threadIdx.x / NT, worker = blockIdx.y;
   const int t0 = threadIdx.x % NT;
   float dot = 0.f;
