@@ -6,7 +6,7 @@
 //
 // Bound by the logits' way in and, for a gradient, its way out.  Where the rows' weights are known when
 // the loss is formed, both come from one read: a row lies in the registers of a cluster of up to
-// eight CTAs as exp(x - the CTA's own max), 32 values a thread, until the whole row's sum is known.
+// eight CTAs as exp(x - the warp's own max), 32 values a thread, until the whole row's sum is known.
 // Longer rows, losses alone and gradients that are asked for later take one pass each.  Rows of up to
 // 1024 logits belong to a warp.
 //
@@ -27,9 +27,7 @@ constexpr int kWarpRowMax = 1024;    // longest row that stays in a warp's regis
 constexpr int kMaxSplit = 64;
 constexpr int kMaxPairs = OLSGD_MAX_TEACHER;
 static_assert(kMaxPairs <= kThreads, "a thread for each pair");
-constexpr int kFusedThreads = 512, kFusedValues = 32;
-constexpr int kFusedPart = kFusedThreads * kFusedValues;   // elements of a row that a CTA holds
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 8, kKnownDevices = 8;
 
 struct Sum {
   float m, s;   // maximum; sum of exp((x - m) / tau)
@@ -410,39 +408,45 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Clusters that stay, a row at a time; its CTAs hold kFusedPart elements each, counted from the 16-byte boundary at
-// or before the row.  Sixteen warps have the row's elements: each takes its own maximum and sum, so that a row has one barrier, behind which every warp joins what
-// all warps of the cluster have left in its shared memory.  A seventeenth warp brings the rows in (bulk copies of
-// its whole 16-byte pieces, two buffers), has the pairs and writes the loss; it stores the gradients at the pairs' tokens behind the next row's
-// barrier, when the others' stores of this row are done.
-// 4096 x 32768 bf16, 32 pairs: 200 us one row a cluster, 175 with the rows on their way early but the pairs and two more
-// barriers in all warps (816 instructions a warp and row, half of them reductions).
+// Clusters that stay, a row at a time; each of its CTAs holds a part of the row, 32 elements a thread, counted from the
+// 16-byte boundary at or before the row.  The warps have the row's elements: each takes its own maximum and sum and sends
+// them to every CTA of the cluster, where every warp joins them all behind the row's one barrier.
+// One more warp brings the rows in (bulk copies of the whole 16-byte pieces, two buffers), has the pairs and writes
+// the loss; it stores the gradients at the pairs' tokens a row later, when the others' stores of their row are done.
+// 4096 x 32768 bf16, 32 pairs: 200 us with one row a cluster and all in all warps, 115 with one warp for the pairs and one
+// barrier of the cluster a row.
 constexpr int kStages = 2;
-constexpr int kStreamWarps = kFusedThreads / 32, kStreamThreads = kFusedThreads + 32;
+constexpr int kMostWarps = 31;
 struct StreamShared {
-  uint64_t full[kStages];
-  Sum stats[2][kMaxCluster * kStreamWarps];   // of the cluster's warps, of rows in turn
-  int teacher[2];                             // whether the row has one
+  uint64_t full[kStages];                  // copies
+  Sum stats[2][kMaxCluster * kMostWarps];  // of the cluster's warps, of rows in turn
+  int teacher[2];                          // whether the row has one
+  uint32_t seen[kMostWarps * 40];          // a bit for each element of the part
+  int32_t id[kMaxPairs];                   // where a token occurs twice
+  float q[kMaxPairs];
 };
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  expect_bytes(bar, bytes);
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
 __device__ int g_distill_status;   // a bounded wait gave up (olsgd_operators_join)
 
-// Waits for a copy, a second at most.
-__device__ __forceinline__ bool copy_arrived(uint32_t bar, uint32_t parity) {
+// Waits for a phase of a barrier, a second at most.
+__device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity) {
   uint64_t t0 = 0;
   for (uint32_t it = 1;; ++it) {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok)
-                 : "r"(bar), "r"(parity)
+                 : "r"(bar), "r"(parity), "r"(100000)
                  : "memory");
     if (ok) return true;
-    if (it % 64 == 0) {
+    if (it % 8 == 0) {
       uint64_t now;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
       if (t0 == 0) t0 = now;
@@ -450,25 +454,25 @@ __device__ __forceinline__ bool copy_arrived(uint32_t bar, uint32_t parity) {
     }
   }
 }
-
-// v to this CTA-relative address in the cluster's CTA `rank`.
-__device__ __forceinline__ void remote_store(void* p, uint32_t rank, float a, float b) {
+// v to this place of the cluster's CTA `rank`.
+__device__ __forceinline__ void tell(void* p, uint32_t rank, const Sum& v) {
   uint32_t at;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(shared_address(p)), "r"(rank));
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(a), "f"(b) : "memory");
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.m), "f"(v.s) : "memory");
 }
 __device__ __forceinline__ float redux_max(float v) {
   asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v));
   return v;
 }
 
-// KP: pairs of a lane of the seventeenth warp.
-template <typename T, bool CLUSTER, int KP>
-__global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const DistillArgs a, int ctas) {
-  constexpr int VEC = Elem<T>::kVec, U = kFusedValues / VEC, NT = kFusedThreads;
-  extern __shared__ __align__(16) uint8_t stage_memory[];   // [kStages][kFusedPart] elements
+// blockDim.x: 32 threads for every warp with elements, and 32.  KP: pairs of a lane of the last warp.
+template <typename T, bool CLUSTER, int KP, int kValues>
+__global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, kValues == 32 ? 2 : 1) distill_stream_kernel(const DistillArgs a, int ctas) {
+  constexpr int VEC = Elem<T>::kVec, U = kValues / VEC;
+  extern __shared__ __align__(16) uint8_t stage_memory[];   // [kStages][part] elements
   __shared__ StreamShared sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int warps = blockDim.x / 32 - 1, NT = warps * 32, part = NT * kValues;
   const int rank = CLUSTER ? (int)cluster_rank() : 0;
   const int64_t first = CLUSTER ? blockIdx.x / ctas : blockIdx.x, step = CLUSTER ? gridDim.x / ctas : gridDim.x;
   const int V = (int)a.V;
@@ -476,10 +480,10 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
   // Of a row: its first element; where this CTA's part begins (ahead of the row by up to a piece); the part's
   // whole pieces, which are copied (partial ones are loaded by the threads that have them).
   const auto row_at = [&](int64_t r) { return static_cast<const T*>(a.logits) + r * a.ld; };
-  const auto begin_of = [&](const T* row) { return rank * kFusedPart - row_shift(row); };
+  const auto begin_of = [&](const T* row) { return rank * part - row_shift(row); };
   const auto first_whole = [&](int begin) { return begin < 0 ? 1 : 0; };
   const auto whole_bytes = [&](int begin) {
-    const int last = min(kFusedPart / VEC, max(0, V - begin) / VEC);
+    const int last = min(part / VEC, max(0, V - begin) / VEC);
     return (uint32_t)max(0, last - first_whole(begin)) * 16u;
   };
   if (threadIdx.x == 0) {
@@ -487,17 +491,19 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sh.full[i])));
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  for (int i = threadIdx.x; i < kMostWarps * 40; i += blockDim.x) sh.seen[i] = 0;
   launch_gate();
   __syncthreads();
   if (CLUSTER) cluster_sync();   // every CTA has begun: its memory can be written
+  const int all = CLUSTER ? ctas * warps : warps;
+  // The one barrier of a row.  (Nobody is a whole row ahead of it: two buffers for the statistics do.)
   const auto meet = [&] {
     __syncwarp();
     if (CLUSTER) cluster_sync();
     else __syncthreads();
   };
-  // A row's statistics, behind its barrier, by a warp.
+  // Statistics of row n, behind its barrier, by a warp.
   const auto joined = [&](int n) {
-    const int all = CLUSTER ? ctas * kStreamWarps : kStreamWarps;
     float m = -INFINITY;
     for (int i = lane; i < all; i += 32) m = fmaxf(m, sh.stats[n & 1][i].m);
     Sum r;
@@ -510,20 +516,25 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
     r.s = warp_sum(r.s);
     return r;
   };
+  bool gave_up = false;
+  // (one lane waits for its warp: of all lanes' polling the other warps would feel)
+  const auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (lane == 0 && !gave_up && !phase_done(shared_address(bar), parity)) gave_up = true;
+    __syncwarp();
+  };
 
-  if (warp < kStreamWarps) {
-    bool gave_up = false;
+  if (warp < warps) {
     uint32_t copies = 0;   // bit i: parity of the next copy to buffer i
     int n = 0;
     for (int64_t r = first; r < a.rows; r += step, ++n) {
       const T* row = row_at(r);
       const int begin = begin_of(row);
-      const float weight = a.d_loss[r];   // (used behind the barrier)
+      const float weight = a.d_loss[r];   // (used behind the wait)
       if (whole_bytes(begin)) {
-        if (!copy_arrived(shared_address(&sh.full[n % kStages]), copies >> (n % kStages) & 1)) gave_up = true;
+        wait(&sh.full[n % kStages], copies >> (n % kStages) & 1);
         copies ^= 1u << (n % kStages);
       }
-      const T* part_row = reinterpret_cast<const T*>(stage_memory) + (n % kStages) * kFusedPart;
+      const T* part_row = reinterpret_cast<const T*>(stage_memory) + (n % kStages) * part;
       uint4 w[U];
       float mx = -INFINITY;
 #pragma unroll
@@ -553,10 +564,11 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
       unpack2f(s2, lo, hi);
       const float s = warp_sum(lo + hi);
       if (CLUSTER) {
-        if (lane < ctas) remote_store(&sh.stats[n & 1][rank * kStreamWarps + warp], lane, m, s);
+        if (lane < ctas) tell(&sh.stats[n & 1][rank * warps + warp], lane, Sum{m, s});
       } else if (lane == 0) {
         sh.stats[n & 1][warp] = Sum{m, s};
       }
+      // (behind this the last warp reuses the row's buffer, and stores where this warp stored for the row before)
       meet();
       const Sum student = joined(n);
       T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
@@ -582,8 +594,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
         }
       }
     }
-    if (n > 0) meet();   // the last row's stores are done
-    if (gave_up) atomicExch(&g_distill_status, (int)OLSGD_ETIMEOUT);
+    meet();   // the last row's stores are done
   } else {
     const auto request = [&](int64_t r, int n) {
       if (lane != 0 || r >= a.rows) return;
@@ -591,7 +602,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
       const int begin = begin_of(row), skip = first_whole(begin) * VEC;
       const uint32_t bytes = whole_bytes(begin);
       if (bytes)
-        bulk_load(shared_address(stage_memory) + ((n % kStages) * kFusedPart + skip) * (int)sizeof(T), row + begin + skip, bytes,
+        bulk_load(shared_address(stage_memory) + ((n % kStages) * part + skip) * (int)sizeof(T), row + begin + skip, bytes,
                   shared_address(&sh.full[n % kStages]));
     };
     // Three loads deep (the id, the logits there): the ids come two rows ahead, the rest one.
@@ -616,15 +627,14 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
     fetch_ids(first, ids);
     fetch_pairs(first, ids, next);
     fetch_ids(first + step, ids);
-    int32_t old_id[KP];
-    float old_d[KP];   // gradients at the last row's tokens
+    int32_t old_id[KP];   // of this part's tokens of the last row, and their gradients
+    float old_d[KP];
     T* old_out = nullptr;
-    int old_begin = 0;
     const auto store_old = [&] {
       if (!old_out) return;
 #pragma unroll
       for (int i = 0; i < KP; ++i)
-        if (old_id[i] >= 0 && old_id[i] >= old_begin && old_id[i] < old_begin + kFusedPart) old_out[old_id[i]] = Elem<T>::from_float(old_d[i]);
+        if (old_id[i] >= 0) old_out[old_id[i]] = Elem<T>::from_float(old_d[i]);
     };
     int n = 0;
     for (int64_t r = first; r < a.rows; r += step, ++n) {
@@ -644,9 +654,24 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
       const bool none = empty(teacher);
       const float log_teacher = log_sum(teacher);
       if (lane == 0) sh.teacher[n & 1] = !none;
+      // Whether a token of this part occurs twice: a bit for each (cleared at once: one warp's own).
+      const int begin = begin_of(row_at(r));
+      uint32_t twice = 0;
+      const auto in_part = [&](int32_t id) { return id >= 0 && id >= begin && id < begin + part; };
+#pragma unroll
+      for (int i = 0; i < KP; ++i)
+        if (in_part(now[i].id)) {
+          const int at = now[i].id - begin;
+          twice |= atomicOr(&sh.seen[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u;
+        }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < KP; ++i)
+        if (in_part(now[i].id)) sh.seen[(now[i].id - begin) >> 5] = 0;
+      const bool any_twice = __any_sync(0xffffffffu, twice != 0);
       meet();
       store_old();
-      request(r + kStages * step, n + kStages);   // (the buffer was read ahead of the barrier)
+      request(r + kStages * step, n + kStages);
       const Sum student = joined(n);
       const float log_s = log_sum(student);
       float loss = 0.f, q[KP];
@@ -662,51 +687,36 @@ __global__ void __launch_bounds__(kStreamThreads, 2) distill_stream_kernel(const
         a.stats[2 * r] = student.m;
         a.stats[2 * r + 1] = log_s;
       }
-      old_begin = begin_of(row_at(r));
       old_out = weight == 0.f || none || empty(student) ? nullptr : static_cast<T*>(a.d_logits) + r * a.ldd;
-      // the first of the pairs with a token has the sum of all of them
-      float sum[KP];
-      bool leads[KP];
-      if (KP == 1) {
-        const uint32_t same = __match_any_sync(0xffffffffu, now[0].id);
-        leads[0] = __ffs(same) - 1 == lane;
-        sum[0] = q[0];
-        if (__any_sync(0xffffffffu, now[0].id >= 0 && (same & (same - 1)))) {
-          sum[0] = 0.f;
-          for (int o = 0; o < 32; ++o) {
-            const float other = __shfl_sync(0xffffffffu, q[0], o);
-            if (same >> o & 1) sum[0] += other;
-          }
-        }
-      } else {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) old_id[i] = in_part(now[i].id) ? now[i].id : -1;
+      if (any_twice) {
+        // the first of the pairs with a token has the sum of all of them
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
-          sum[i] = 0.f;
-          leads[i] = true;
+          sh.id[i * 32 + lane] = now[i].id;
+          sh.q[i * 32 + lane] = q[i];
         }
+        __syncwarp();
 #pragma unroll
-        for (int k = 0; k < KP; ++k)
-          for (int o = 0; o < 32 && k * 32 + o < a.K; ++o) {
-            const int32_t id = __shfl_sync(0xffffffffu, now[k].id, o);
-            const float other = __shfl_sync(0xffffffffu, q[k], o);
-#pragma unroll
-            for (int i = 0; i < KP; ++i)
-              if (id == now[i].id) {
-                sum[i] += other;
-                if (k * 32 + o < i * 32 + lane) leads[i] = false;
-              }
-          }
+        for (int i = 0; i < KP; ++i) {
+          q[i] = 0.f;
+          for (int e = 0; e < a.K; ++e)
+            if (sh.id[e] == now[i].id) {
+              q[i] += sh.q[e];
+              if (e < i * 32 + lane) old_id[i] = -1;
+            }
+        }
+        __syncwarp();
       }
       const float g = weight * a.inv_t, base = base_of(student.m), scale = g / student.s;
 #pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        old_id[i] = leads[i] ? now[i].id : -1;
-        old_d[i] = fmaf(-g, sum[i], scale * ex2((now[i].x - base) * c));
-      }
+      for (int i = 0; i < KP; ++i) old_d[i] = fmaf(-g, q[i], scale * ex2((now[i].x - base) * c));
     }
-    if (n > 0) meet();
+    meet();
     store_old();
   }
+  if (gave_up) atomicExch(&g_distill_status, (int)OLSGD_ETIMEOUT);
 }
 
 // ------------------------------------------------------------------------------ host
@@ -728,10 +738,20 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
   p.nsplit = (p.nchunks + p.cps - 1) / p.cps;
   return p;
 }
-// CTAs of a cluster that hold a row; 0: too long.  aligned: all rows start on a 16-byte boundary.
-int cluster_of(int64_t V, int dtype, bool aligned) {
-  const int64_t n = (V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7) + kFusedPart - 1) / kFusedPart;
-  return n > kMaxCluster ? 0 : (int)n;
+// CTAs of a cluster that hold a row, their warps with elements and a thread's elements; no CTAs where the row is too long.
+// Up to 16384 elements a CTA of 32 a thread, of which a multiprocessor holds several; above, as few CTAs as do with 40 a
+// thread, each with a multiprocessor to itself: a cluster's barrier costs more than that (4096 x 32768 bf16 123 us; two
+// CTAs of 16 warps 142; 3532 x 38000 121 us, three CTAs 275).  aligned: all rows start on a 16-byte boundary.
+struct Cluster {
+  int ctas, warps, values;
+};
+Cluster cluster_of(int64_t V, int dtype, bool aligned) {
+  const int64_t n = V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7);
+  if (n <= 16 * 1024) return Cluster{1, (int)((n + 1023) / 1024), 32};
+  const int most = (dtype == OLSGD_F32 ? 19 : kMostWarps) * 1280;   // (two buffers of 97 or 78 KB)
+  const int64_t ctas = (n + most - 1) / most;
+  if (ctas > kMaxCluster) return Cluster{0, 0, 0};
+  return Cluster{(int)ctas, (int)((n + ctas * 1280 - 1) / (ctas * 1280)), 40};
 }
 template <typename T>
 bool rows_aligned(const DistillArgs& a) {
@@ -755,43 +775,71 @@ cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
 }
 
 // As many clusters as the GPU holds at once.
-template <typename T, bool CLUSTER, int KP>
-cudaError_t stream_as(const DistillArgs& a, int ctas, cudaStream_t s) {
-  constexpr size_t smem = (size_t)kStages * kFusedPart * sizeof(T);
+template <typename T, bool CLUSTER, int KP, int kValues>
+cudaError_t stream_as(const DistillArgs& a, const Cluster& c, cudaStream_t s) {
+  const int threads = c.warps * 32 + 32;
+  const size_t smem = (size_t)kStages * c.warps * 32 * kValues * sizeof(T);
   static PerDeviceSmem configured;
-  auto kern = distill_stream_kernel<T, CLUSTER, KP>;
-  const cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
+  auto kern = distill_stream_kernel<T, CLUSTER, KP, kValues>;
+  const cudaError_t e = ensure_dynamic_smem(configured, kern, 200 * 1024);
   if (e != cudaSuccess) return e;
-  const int64_t resident = sizeof(T) == 2 ? 2 : 1, room = sm_count() * resident / ctas, clusters = a.rows < room ? a.rows : room;
-  if (!CLUSTER) return launch_chained(kern, dim3((unsigned)clusters), dim3(kStreamThreads), smem, s, a, 1);
+  // (registers, and 227 KB a multiprocessor)
+  int64_t resident = 65536 / ((kValues == 40 ? 64 : 56) * threads), by_memory = 227 * 1024 / (smem + sizeof(StreamShared) + 1024);
+  resident = resident < by_memory ? resident : by_memory;
+  if (!CLUSTER) {
+    const int64_t room = sm_count() * (resident < 1 ? 1 : resident);
+    return launch_chained(kern, dim3((unsigned)(a.rows < room ? a.rows : room)), dim3(threads), smem, s, a, 1);
+  }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(clusters * ctas));
-  cfg.blockDim = dim3(kStreamThreads);
+  cfg.gridDim = dim3((unsigned)c.ctas);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ctas;
+  attr[0].val.clusterDim.x = c.ctas;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  // Groups of multiprocessors need not be a multiple of a cluster: asked once for each shape.  (Of a grid that does not fit
+  // the rest would start when the others end.)
+  static std::atomic<int> known[kKnownDevices][kMaxCluster + 1][kMostWarps + 1];
+  const int dev = current_device();
+  const bool keeps = dev >= 0 && dev < kKnownDevices;
+  int room = keeps ? known[dev][c.ctas][c.warps].load(std::memory_order_relaxed) : 0;
+  if (room == 0) {
+    if (cudaOccupancyMaxActiveClusters(&room, kern, &cfg) != cudaSuccess || room < 1) {
+      cudaGetLastError();
+      room = 1;
+    }
+    if (keeps) known[dev][c.ctas][c.warps].store(room, std::memory_order_relaxed);
+  }
+  cfg.gridDim = dim3((unsigned)((a.rows < room ? a.rows : room) * c.ctas));
   cfg.numAttrs = g_launch_overlap ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, a, ctas);
+  return cudaLaunchKernelEx(&cfg, kern, a, c.ctas);
+}
+template <typename T, bool CLUSTER, int kValues>
+cudaError_t stream_pairs(const DistillArgs& a, const Cluster& c, cudaStream_t s) {
+  return a.K <= 32    ? stream_as<T, CLUSTER, 1, kValues>(a, c, s)
+         : a.K <= 128 ? stream_as<T, CLUSTER, 4, kValues>(a, c, s)
+                      : stream_as<T, CLUSTER, 8, kValues>(a, c, s);
 }
 template <typename T>
-cudaError_t stream_rows(const DistillArgs& a, int ctas, cudaStream_t s) {
-  if (a.K <= 32) return ctas == 1 ? stream_as<T, false, 1>(a, ctas, s) : stream_as<T, true, 1>(a, ctas, s);
-  if (a.K <= 64) return ctas == 1 ? stream_as<T, false, 2>(a, ctas, s) : stream_as<T, true, 2>(a, ctas, s);
-  return ctas == 1 ? stream_as<T, false, 8>(a, ctas, s) : stream_as<T, true, 8>(a, ctas, s);
+cudaError_t stream_rows(const DistillArgs& a, const Cluster& c, cudaStream_t s) {
+  if (c.ctas > 1) return stream_pairs<T, true, 40>(a, c, s);
+  return c.values == 40 ? stream_pairs<T, false, 40>(a, c, s) : stream_pairs<T, false, 32>(a, c, s);
 }
 
 template <typename T>
 cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax) return a.d_loss ? warp_rows<T, true, true>(a, s) : warp_rows<T, true, false>(a, s);
-  const int ctas = a.d_loss ? cluster_of(a.V, a.dtype, rows_aligned<T>(a)) : 0;
-  if (ctas > 0) return stream_rows<T>(a, ctas, s);
+  if (a.d_loss) {
+    const Cluster c = cluster_of(a.V, a.dtype, rows_aligned<T>(a));
+    if (c.ctas > 0) return stream_rows<T>(a, c, s);
+  }
   const Plan p = plan(a.rows, a.V, a.dtype);
   float2* part = p.nsplit > 1 ? static_cast<float2*>(a.ws) : nullptr;
   cudaError_t e = launch_chained(distill_row_kernel<T>, dim3((unsigned)a.rows, (unsigned)p.nsplit), dim3(kThreads), 0, s, a, p.nchunks, p.cps, part);
@@ -803,7 +851,7 @@ cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
 }  // namespace
 
 size_t distill_workspace(int dtype, int64_t rows, int64_t V, bool gradient) {
-  if (V <= kWarpRowMax || (gradient && cluster_of(V, dtype, false))) return 0;   // (whatever the alignment)
+  if (V <= kWarpRowMax || (gradient && cluster_of(V, dtype, false).ctas > 0)) return 0;   // (whatever the alignment)
   const Plan p = plan(rows, V, dtype);
   return p.nsplit == 1 ? 0 : (size_t)rows * p.nsplit * sizeof(float2);
 }
