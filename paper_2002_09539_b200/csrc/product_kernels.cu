@@ -8,21 +8,23 @@
 // of row tiles in its shared memory first.
 //
 // One kernel, three modes.  Warp 0 feeds a ring of shared-memory stages with TMA, warp 1 issues the MMAs into
-// accumulators in tensor memory, eight warps empty them.  A tile has 128 features and two accumulators take turns,
-// or it has 256, as two MMAs that share their B (HALVES = 2): then a CTA takes in 64 KB for 256 x 256 x 64
-// multiply-adds, which L2 keeps up with, and the halves are emptied one by one while the next tile's first MMAs run.
+// accumulators in tensor memory, eight warps empty them.  A tile has 128 features, or 256 as two MMAs that share their B
+// (HALVES = 2); two accumulators take turns.  A tile of 256 x 256, for which a CTA takes in 64 KB a
+// 256 x 256 x 64 multiply-adds, which L2 keeps up with, fills tensor memory: its halves are emptied one by one while the
+// next tile's first MMAs run.
 //   FORWARD   A = W (K-major), B = the tile's rows of x (K-major)
 //   DX        A = W read along D (MN-major), B = the tile's rows of dy
 //   DW        A = dy, B = x, both read along their features (MN-major), K = the group's rows
 // The weights are the MMA's M, so that the ragged dimension is its N: a tile of n rows costs n rounded
 // up to 16, not to 128, in MMAs and in loads.  Rows of other groups that come
 // with a box end up in columns of the accumulator that are not stored.  Along K they would be
-// summed: there a group's rows are loaded in boxes of 64, then of 16, and the last n mod 16 come from a copy
-// padded with zeros, which a small kernel makes ahead.
+// summed: there the warp that issues the MMAs zeroes them in shared memory first (up to 15 rows of a group's last block).
 //
 // TMA wants 16-byte row pitches: operands that do not have them are copied to padded rows in
 // the workspace first.  Every wait is bounded, as in the library's other tensor-core kernels.
 #include "operator_tiles.cuh"
+#include <cstdlib>
+#include <cstdio>
 
 namespace olsgd {
 namespace {
@@ -30,16 +32,16 @@ namespace {
 enum Mode { FORWARD = 0, DX = 1, DW = 2 };
 constexpr int kGroup = 8;            // DW: row tiles walked together (operand reuse in L2)
 constexpr int kSmallBox = 16;        // rows of a box of B where a tile is not full; K of an MMA
-constexpr int kMaxGroups = 2048;     // of a launch of FORWARD or DX: its table's room
+constexpr int kMaxGroups = 1024;     // of a launch of FORWARD or DX: its table's room
 constexpr int kMaxStarts = 2 * kMaxGroups;
 
 __device__ int g_product_status;     // a bounded wait gave up (olsgd_operators_join)
 
 // Rows come in boxes of 16, 32, 64, 128 and 256, one of each at most (a TMA instruction takes some 200 cycles however
-// small its box is).  DW: boxes of 16, 32 and 64 rows, and of 16 rows of the copies of last rows.
+// small its box is).  DW: boxes of 16, 32 and 64 rows.
 constexpr int kBoxes = 5;
 struct alignas(64) ProductMaps {
-  CUtensorMap a[kBoxes], b[kBoxes], a_tail, b_tail;   // FORWARD, DX: a[0] are the weights
+  CUtensorMap a[kBoxes], b[kBoxes];   // FORWARD, DX: a[0] are the weights
 };
 struct ProductArgs {
   int num_kb, k_extent;       // FORWARD, DX: K in blocks of 64, and in elements
@@ -47,6 +49,7 @@ struct ProductArgs {
   int features, cols;         // rows of A in all; DW: columns of the output
   int R, E, m, first_worker;  // rows and experts of a worker; workers of this launch
   int f16;
+  int beside;                 // runs beside the kernel ahead of it: see launch_product_backward
   int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
   const int32_t* offsets;     // [workers][E + 1]
   void* out;
@@ -69,37 +72,9 @@ struct Table {
 // Rows [x, y) of a group, whatever the offsets hold.
 __device__ __forceinline__ int2 group_rows(const int32_t* offsets, int group, int E, int R) {
   const int32_t* o = offsets + group + group / E;   // (a worker has E + 1 of them)
-  const int a = min(max(o[0], 0), R);
-  return make_int2(a, min(max(o[1], a), R));
-}
-
-// ------------------------------------------------------------------------- last rows
-// The n mod 16 last rows of each group in 16 rows of zeros: [groups][16][pitch] of dy and of x.
-struct TailOperand {
-  const uint16_t* p;
-  int64_t worker, row;       // elements between workers and rows
-  uint16_t* out;
-  int64_t cols;
-};
-struct TailArgs {
-  TailOperand op[2];
-  const int32_t* offsets;
-  int E, R;
-};
-__global__ void __launch_bounds__(256) tail_kernel(const TailArgs a) {
-  launch_gate();
-  const TailOperand& o = a.op[blockIdx.y];
-  const int group = blockIdx.x, worker = group / a.E, lane = threadIdx.x & 31;
-  const int2 rows = group_rows(a.offsets, group, a.E, a.R);
-  const int n = (rows.y - rows.x) % kSmallBox;
-  if (n == 0) return;
-  for (int r = threadIdx.x >> 5; r < kSmallBox; r += 8) {
-    const uint16_t* src = o.p + worker * o.worker + (int64_t)(rows.y - n + r) * o.row;
-    const int pieces = (int)((o.cols + 7) / 8);
-    uint4* dst = reinterpret_cast<uint4*>(o.out) + ((int64_t)group * kSmallBox + r) * pieces;
-    for (int c = lane; c < pieces; c += 32)
-      dst[c] = r < n ? load_raw<__nv_bfloat16, int64_t>(reinterpret_cast<const __nv_bfloat16*>(src), c * 8, o.cols, 0) : make_uint4(0, 0, 0, 0);
-  }
+  // (past L1: DW may run beside its predecessor)
+  const int a = min(max(__ldcg(o), 0), R);
+  return make_int2(a, min(max(__ldcg(o + 1), a), R));
 }
 
 // ------------------------------------------------------------------------------- products
@@ -202,7 +177,7 @@ struct Walk {
 };
 
 // 32 accumulator columns of this lane's feature, rows row .. row + 31 of the output, of which n exist: a row's 32 features
-// leave by one store of 64 bytes.
+// leave by one store of 64 bytes.  For outputs whose rows are not multiples of 16 bytes.
 __device__ __forceinline__ void store_rows(const float* v, uint16_t* dst, int64_t pitch, int n, bool live, int f16) {
 #pragma unroll
   for (int j = 0; j < 32; j += 2) {
@@ -210,6 +185,55 @@ __device__ __forceinline__ void store_rows(const float* v, uint16_t* dst, int64_
     store_half_if(dst + j * pitch, two, live && j < n);
     store_half_if(dst + (j + 1) * pitch, two >> 16, live && j + 1 < n);
   }
+}
+
+// 16 lanes x (8 BLOCKS) columns of tensor memory, as the fragments of 8 x 8 matrices: of block i, v[4 i] and v[4 i + 1] are
+// row lane / 4, columns 2 (lane % 4) and the next, v[4 i + 2] and v[4 i + 3] eight rows below.
+template <int BLOCKS>
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t taddr, uint32_t* r) {
+  static_assert(BLOCKS == 2 || BLOCKS == 4, "");
+  if constexpr (BLOCKS == 4) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+  } else {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+  }
+}
+// 8 BLOCKS accumulator columns (rows of the output) of a warp's 32 features, to rows of dst, of which n rows and `features`
+// features (a multiple of 8) exist.  The accumulator has the features in its lanes, memory wants them side by side:
+// fragments are stored transposed (stmatrix), 8 x 8 values an instruction and matrix, and leave by 16 bytes a lane.
+template <int BLOCKS>
+__device__ __forceinline__ void store_transposed(uint8_t* buf, int lane, uint32_t acc, uint16_t* dst, int64_t pitch, int n, int features, int f16) {
+  uint32_t lo[4 * BLOCKS], hi[4 * BLOCKS];   // features 0 .. 15 and 16 .. 31
+  tmem_ld_fragments<BLOCKS>(acc, lo);
+  tmem_ld_fragments<BLOCKS>(acc + (16u << 16), hi);
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+  const auto at = [&](int row, int piece) { return row * 64 + ((piece ^ ((row >> 1) & 3)) * 16); };
+  const uint32_t base = smem_u32(buf);
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) {
+    const auto pair = [&](const uint32_t* v) { return pack2(__uint_as_float(v[0]), __uint_as_float(v[1]), f16); };
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(base + at(8 * i + (lane & 7), lane >> 3)),
+                 "r"(pair(lo + 4 * i)), "r"(pair(lo + 4 * i + 2)), "r"(pair(hi + 4 * i)), "r"(pair(hi + 4 * i + 2))
+                 : "memory");
+  }
+  __syncwarp();
+  uint4 w[BLOCKS];
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) w[i] = *reinterpret_cast<const uint4*>(buf + at(8 * i + (lane >> 2), lane & 3));
+#pragma unroll
+  for (int i = 0; i < BLOCKS; ++i) {
+    const int row = 8 * i + (lane >> 2), f = (lane & 3) * 8;
+    store_piece_if(dst + row * pitch + f, w[i], row < n && f < features);
+  }
+  __syncwarp();
 }
 
 // FORWARD, DX: rows outside every group become zeros; by warps `at`, `at + warps`, ... of the grid.
@@ -238,9 +262,10 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   constexpr uint32_t kBBytes = BN * kBK * 2;
   constexpr uint32_t kStageBytes = kABytes + kBBytes;
   constexpr int kBlockCols = BN / 2 < 64 ? BN / 2 : 64;   // DW: columns an epilogue warp stages at a time
-  constexpr uint32_t kStagingBytes = MODE == DW ? kEpiWarps * 4096 : 0;
-  constexpr uint32_t kTmemCols = 2 * BN;                  // two buffers, or two halves
-  static_assert(kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols >= 32, "two accumulators");
+  constexpr uint32_t kStagingBytes = kEpiWarps * (MODE == DW ? 4096 : 2048);
+  constexpr int kBufs = HALVES * BN <= 256 ? 2 : 1;       // accumulators
+  constexpr uint32_t kTmemCols = kBufs * HALVES * BN;
+  static_assert(kTmemCols <= 512 && (kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols >= 32, "columns of tensor memory");
   static_assert(MODE != DW || BN % 64 == 0, "boxes of 64 columns");
 
   extern __shared__ uint8_t smem_raw[];
@@ -266,7 +291,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
     ctl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  launch_gate();
+  if (!g.beside) launch_gate();
   if (warp == 1) tmem_alloc(smem_u32(&ctl->tmem_base), kTmemCols);
   tc_fence_before();
   if (MODE != DW) make_table(g, table, BN);
@@ -298,24 +323,17 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         const uint32_t a_dst = smem_u32(tiles + s * kStageBytes), b_dst = a_dst + kABytes;
         if (MODE == DW) {
           const int n0 = u.col * BN, left = u.n - k0;
-          const int rows = left >= kBK ? kBK : (left + kSmallBox - 1) / kSmallBox * kSmallBox;
+          const int rows = left >= kBK ? kBK : (left + kSmallBox - 1) / kSmallBox * kSmallBox;   // (some of them not the group's)
           mbar_expect_tx(bar, (uint32_t)((na + nb) * rows * 128));
-          const auto load = [&](const CUtensorMap* ma, const CUtensorMap* mb, int at, int row, int outer) {
-            for (int j = 0; j < na; ++j) tma_load_3d(a_dst + j * 8192 + at * 128, ma, bar, m0 + 64 * j, row, outer);
-            for (int j = 0; j < nb; ++j) tma_load_3d(b_dst + j * 8192 + at * 128, mb, bar, n0 + 64 * j, row, outer);
-          };
-          if (left >= kBK) {
-            load(&maps.a[2], &maps.b[2], 0, u.row0 + k0, u.worker);
-          } else {
-            int at = 0;
+          int at = 0;
 #pragma unroll
-            for (int i = 1; i >= 0; --i)
-              if (left & (kSmallBox << i)) {
-                load(&maps.a[i], &maps.b[i], at, u.row0 + k0 + at, u.worker);
-                at += kSmallBox << i;
-              }
-            if (at < left) load(&maps.a_tail, &maps.b_tail, at, 0, u.group);   // the last rows, from their copy
-          }
+          for (int i = 2; i >= 0; --i)
+            if (rows & (kSmallBox << i)) {
+              const int row = u.row0 + k0 + at;
+              for (int j = 0; j < na; ++j) tma_load_3d(a_dst + j * 8192 + at * 128, &maps.a[i], bar, m0 + 64 * j, row, u.worker);
+              for (int j = 0; j < nb; ++j) tma_load_3d(b_dst + j * 8192 + at * 128, &maps.b[i], bar, n0 + 64 * j, row, u.worker);
+              at += kSmallBox << i;
+            }
         } else {
           mbar_expect_tx(bar, (uint32_t)(na * (A_MN ? 8192 : (int)kHalfBytes) + held * 128));
           for (int j = 0; j < na; ++j) {
@@ -340,8 +358,8 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         while (!mbar_try_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1) && global_ns() - t0 < 10000000ull) {
         }
     }
-  } else if (warp == 1 && lane == 0) {
-    // ---------------- MMA issuer
+  } else if (warp == 1 && (MODE == DW || lane == 0)) {
+    // ---------------- MMA issuer: one lane; DW: its warp comes along, for the zeros
     const uint32_t fmt = g.f16 ? 0u : ((1u << 7) | (1u << 10));
     const uint32_t idesc0 = (1u << 4) | fmt | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kBM >> 4) << 24);
     uint32_t it = 0, n = 0;
@@ -361,49 +379,68 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         const int left = k_extent - kb * kBK;   // (what lies behind is zeros, or was not loaded)
 #pragma unroll
         for (int k = 0; k < kBK / kUmmaK; ++k)
-          if (k * kUmmaK < left) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          if (k * kUmmaK < left && lane == 0) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > 0 || k > 0) ? 1u : 0u);
       };
-      const auto arrived = [&](uint32_t i) {
-        ok = mbar_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1, abort_flag);
+      const auto wait = [&](uint64_t* bar, uint32_t parity) {
+        int done = 1;
+        if (MODE != DW || lane == 0) done = mbar_wait(smem_u32(bar), parity, abort_flag);
+        if (MODE == DW) done = __shfl_sync(0xffffffffu, done, 0);
         tc_fence_after();
+        return done != 0;
+      };
+      const auto commit = [&](uint64_t* bar) {
+        if (lane == 0) umma_commit(smem_u32(bar));
+      };
+      const auto arrived = [&](int kb, uint32_t i) {
+        ok = wait(&ctl->full[i % STAGES], (i / STAGES) & 1);
+        const int left = k_extent - kb * kBK;
+        if (MODE == DW && ok && left < kBK && left % kSmallBox) {
+          // (rows of 128 bytes, whatever the swizzle does inside them)
+          const int zeros = kSmallBox - left % kSmallBox, boxes = kTileM / 64 + BN / 64;
+          uint8_t* stage = tiles + (i % STAGES) * kStageBytes;
+          for (int p = lane; p < boxes * zeros * 8; p += 32) {
+            const int box = p / (zeros * 8), at = p - box * (zeros * 8);
+            reinterpret_cast<uint4*>(stage + box * 8192 + left * 128)[at] = make_uint4(0, 0, 0, 0);
+          }
+          fence_async_smem();
+          __syncwarp();
+        }
         return ok;
       };
-      if constexpr (HALVES == 1) {
-        const uint32_t buf = n & 1, acc = tmem_base + buf * BN;
-        ok = mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((n >> 1) & 1) ^ 1, abort_flag);
+      if constexpr (kBufs == 2) {
+        const uint32_t buf = n & 1, acc = tmem_base + buf * (HALVES * BN);
+        ok = wait(&ctl->acc_empty[buf], ((n >> 1) & 1) ^ 1);
         if (!ok) break;
-        tc_fence_after();
         for (int kb = 0; kb < end; ++kb, ++it) {
-          if (!arrived(it)) break;
-          multiply(kb, it % STAGES, 0, acc);
-          umma_commit(smem_u32(&ctl->empty[it % STAGES]));
+          if (!arrived(kb, it)) break;
+#pragma unroll
+          for (int half = 0; half < HALVES; ++half) multiply(kb, it % STAGES, half, acc + half * BN);
+          commit(&ctl->empty[it % STAGES]);
         }
-        umma_commit(smem_u32(&ctl->acc_full[buf]));
+        commit(&ctl->acc_full[buf]);
       } else {
         // The first blocks' MMAs of the first half run while the second is emptied.
         const int lead = min(end, STAGES);
-        ok = mbar_wait(smem_u32(&ctl->acc_empty[0]), (n & 1) ^ 1, abort_flag);
+        ok = wait(&ctl->acc_empty[0], (n & 1) ^ 1);
         if (!ok) break;
-        tc_fence_after();
         for (int kb = 0; kb < lead; ++kb) {
-          if (!arrived(it + kb)) break;
+          if (!arrived(kb, it + kb)) break;
           multiply(kb, (it + kb) % STAGES, 0, tmem_base);
         }
         if (!ok) break;
-        ok = mbar_wait(smem_u32(&ctl->acc_empty[1]), (n & 1) ^ 1, abort_flag);
+        ok = wait(&ctl->acc_empty[1], (n & 1) ^ 1);
         if (!ok) break;
-        tc_fence_after();
         for (int kb = 0; kb < lead; ++kb, ++it) {
           multiply(kb, it % STAGES, 1, tmem_base + BN);
-          umma_commit(smem_u32(&ctl->empty[it % STAGES]));
+          commit(&ctl->empty[it % STAGES]);
         }
         for (int kb = lead; kb < end; ++kb, ++it) {
-          if (!arrived(it)) break;
+          if (!arrived(kb, it)) break;
           multiply(kb, it % STAGES, 0, tmem_base);
           multiply(kb, it % STAGES, 1, tmem_base + BN);
-          umma_commit(smem_u32(&ctl->empty[it % STAGES]));
+          commit(&ctl->empty[it % STAGES]);
         }
-        umma_commit(smem_u32(&ctl->acc_full[0]));
+        commit(&ctl->acc_full[0]);
       }
       ++n;
     }
@@ -415,7 +452,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
     for (uint32_t t = first; t < total; t += step) {
       const Unit u = walk.at(t);
       const bool none = MODE == DW && u.n == 0;   // zeros, and no accumulator
-      const uint32_t buf = HALVES == 1 ? n & 1 : 0, parity = HALVES == 1 ? (n >> 1) & 1 : n & 1;
+      const uint32_t buf = kBufs == 2 ? n & 1 : 0, parity = kBufs == 2 ? (n >> 1) & 1 : n & 1;
       // one lane waits for its warp: what follows wants all lanes together
       int ok = 1;
       if (lane == 0 && !none) ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), parity, abort_flag);
@@ -425,7 +462,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
 #pragma unroll 1
       for (int half = 0; half < HALVES; ++half) {
         const int feature0 = u.m * kTileM + half * kBM + lane_group * 32;
-        const uint32_t acc = tmem_base + (HALVES == 1 ? buf : half) * BN + ((uint32_t)(lane_group * 32) << 16);
+        const uint32_t acc = tmem_base + (buf * HALVES + half) * BN + ((uint32_t)(lane_group * 32) << 16);
         if (feature0 < g.features) {
           if (MODE == DW) {
             constexpr int W = kBlockCols;
@@ -449,29 +486,39 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
               out.flush(lane, dst + col, g.cols, g.features - feature0, cols, g.out_width);
             }
           } else {
-            uint16_t* dst = static_cast<uint16_t*>(g.out) + ((int64_t)u.worker * g.R + u.row0) * g.features + feature0 + lane;
+            uint16_t* dst = static_cast<uint16_t*>(g.out) + ((int64_t)u.worker * g.R + u.row0) * g.features + feature0;
             const bool live = feature0 + lane < g.features;
+            uint8_t* buf_out = tiles + STAGES * kStageBytes + (warp - 2) * 2048;
             if (BN == 32) {
               // (sixteen columns for either side)
+              uint16_t* first_row = dst + (int64_t)side * 16 * g.features;
               if (side * 16 < u.n) {
-                float v[32];
-                tmem_ld16x2(acc + side * 16, acc + side * 16, v, v + 16);
-                store_rows(v, dst + (int64_t)side * 16 * g.features, g.features, min(16, u.n - side * 16), live, g.f16);
+                if (g.out_width == 16) {
+                  store_transposed<2>(buf_out, lane, acc + side * 16, first_row, g.features, u.n - side * 16, g.features - feature0, g.f16);
+                } else {
+                  float v[32];
+                  tmem_ld16x2(acc + side * 16, acc + side * 16, v, v + 16);
+                  store_rows(v, first_row + lane, g.features, min(16, u.n - side * 16), live, g.f16);
+                }
               }
+            } else if (g.out_width == 16) {
+#pragma unroll 1
+              for (int c = side * 32; c < u.n; c += 64)
+                store_transposed<4>(buf_out, lane, acc + c, dst + (int64_t)c * g.features, g.features, u.n - c, g.features - feature0, g.f16);
             } else {
 #pragma unroll 1
               for (int c = side * 32; c < u.n; c += 64) {
                 float v[32];
                 tmem_ld32(acc + c, v);
-                store_rows(v, dst + (int64_t)c * g.features, g.features, u.n - c, live, g.f16);
+                store_rows(v, dst + (int64_t)c * g.features + lane, g.features, u.n - c, live, g.f16);
               }
             }
           }
         }
-        if (none) continue;
+        if (none || (kBufs == 2 && half + 1 < HALVES)) continue;
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[HALVES == 1 ? buf : half]));
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[kBufs == 2 ? buf : half]));
         __syncwarp();
       }
       if (!none) ++n;
@@ -493,6 +540,8 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
     tc_fence_after();
     tmem_dealloc(tmem_base, kTmemCols);
   }
+  // what follows in the stream waits for this kernel: so this one waits for the kernel it ran beside
+  if (g.beside) launch_gate();
 }
 
 // --------------------------------------------------------------------------------- host
@@ -500,7 +549,7 @@ constexpr int kSms = 148;
 
 template <int MODE, int HALVES, int BN, int STAGES>
 cudaError_t launch_variant(const ProductMaps& maps, ProductArgs g, cudaStream_t s) {
-  constexpr size_t smem = (size_t)STAGES * (HALVES * kBM + BN) * kBK * 2 + (MODE == DW ? kEpiWarps * 4096 : sizeof(Table)) +
+  constexpr size_t smem = (size_t)STAGES * (HALVES * kBM + BN) * kBK * 2 + kEpiWarps * (MODE == DW ? 4096 : 2048) + (MODE == DW ? 0 : sizeof(Table)) +
                           sizeof(Control<STAGES>) + 1024;
   static_assert(smem <= 227 * 1024, "shared memory of one CTA");
   static PerDeviceSmem configured;
@@ -516,24 +565,32 @@ cudaError_t launch_variant(const ProductMaps& maps, ProductArgs g, cudaStream_t 
   return launch_chained(kern, dim3((unsigned)(total < room ? total : room)), dim3(kThreads), smem, s, maps, g);
 }
 
-// Which tiles: by the sizes alone; how the rows fall to the experts is not known here and taken as even.  A tile's
-// time goes by the operand bytes that it takes in per K block (its rows of A and of B), plus an epilogue that is
-// not hidden in the last wave; the launch takes as many waves as its tiles need.
+// Which tiles: by the sizes alone; how the rows fall to the experts is not known here and taken as even.  A tile takes, in
+// cycles: per K block the longest of its operands' way from L2 (36 bytes a cycle), its MMAs (M N / 64) and, where
+// each weight is used by one tile only, the weights' way from memory (23 bytes a cycle and multiprocessor); then its results'
+// way out, at its side where there are two accumulators.  The launch takes as many waves as its tiles need.
 struct Shape {
   int halves, bn;
 };
+double tile_cycles(const Shape& sh, double rows, double kbs, bool once, double out_rate) {
+  const double m = sh.halves * kBM;
+  double block = (m + rows) * 128 / 36;
+  if (m * rows / 64 > block) block = m * rows / 64;
+  if (once && m * 128 / 23 > block) block = m * 128 / 23;
+  const double in = kbs * block, out = m * rows * 2 / out_rate;
+  return 400 + (sh.halves * sh.bn > 256 ? in + 0.6 * out : in > out ? in : out);
+}
 Shape shape_rows(const ProductShape& d, int64_t features, int64_t k) {
-  constexpr Shape shapes[] = {{1, 32}, {1, 64}, {1, 128}, {1, 256}, {2, 256}};
+  constexpr Shape shapes[] = {{1, 32}, {1, 64}, {1, 128}, {1, 256}, {2, 128}, {2, 256}};
   Shape best = shapes[0];
   double least = 1e300;
   const int64_t used = d.E < d.R ? d.E : d.R;
   const double rows = (double)d.R / used, kbs = (double)((k + kBK - 1) / kBK);
   for (const Shape& sh : shapes) {
-    const double per_group = rows <= sh.bn ? 1.0 : rows / sh.bn + 0.5;
+    const double per_group = rows <= 0.7 * sh.bn ? 1.0 : rows / sh.bn + 0.5, held = rows / per_group;
     const double tiles = d.m * used * per_group * ((features + sh.halves * kBM - 1) / (sh.halves * kBM));
-    const double waves = tiles < kSms ? 1.0 : tiles / kSms + 0.5;
-    const double held = rows < sh.bn ? rows : sh.bn;
-    const double cost = waves * (kbs + 4) * (sh.halves * kBM + held);
+    const double waves = tiles <= kSms ? 1.0 : tiles / kSms + 0.4;
+    const double cost = waves * tile_cycles(sh, held, kbs, per_group < 1.5, 30.0) + sh.halves * kBM * held * 2 / 30.0;
     if (cost < least) {
       least = cost;
       best = sh;
@@ -542,13 +599,13 @@ Shape shape_rows(const ProductShape& d, int64_t features, int64_t k) {
   return best;
 }
 Shape shape_weights(const ProductShape& d) {
-  constexpr Shape shapes[] = {{1, 64}, {1, 128}, {1, 256}, {2, 256}};
+  constexpr Shape shapes[] = {{1, 64}, {1, 128}, {1, 256}, {2, 128}, {2, 256}};
   Shape best = shapes[0];
   double least = 1e300;
   const double kbs = (double)d.R / d.E / kBK + 0.5;
   for (const Shape& sh : shapes) {
     const int64_t tiles = d.m * d.E * ((d.F + sh.halves * kBM - 1) / (sh.halves * kBM)) * ((d.D + sh.bn - 1) / sh.bn);
-    const double cost = (double)((tiles + kSms - 1) / kSms) * (kbs + 4) * (sh.halves * kBM + sh.bn);
+    const double cost = (double)((tiles + kSms - 1) / kSms) * tile_cycles(sh, sh.bn, kbs, false, 18.0) + sh.halves * kBM * sh.bn * 2 / 18.0;
     if (cost < least) {
       least = cost;
       best = sh;
@@ -557,24 +614,8 @@ Shape shape_weights(const ProductShape& d) {
   return best;
 }
 
-// The workspace: copies of operands that TMA cannot take, then (backward) the groups' last rows of dy and of x.
-struct Workspace {
-  size_t tail_dy, tail_x, total;
-};
-Workspace layout(const ProductShape& d, bool backward, bool copies) {
-  Workspace w{};
-  size_t at = 0;
-  if (copies) {
-    at += round256((size_t)d.m * d.R * round8(d.D) * 2) + round256((size_t)d.m * d.E * d.F * round8(d.D) * 2);
-    if (backward) at += round256((size_t)d.m * d.R * round8(d.F) * 2);
-  }
-  w.tail_dy = at;
-  at += backward ? round256((size_t)d.m * d.E * kSmallBox * round8(d.F) * 2) : 0;
-  w.tail_x = at;
-  at += backward ? round256((size_t)d.m * d.E * kSmallBox * round8(d.D) * 2) : 0;
-  w.total = at;
-  return w;
-}
+// The workspace: copies of operands that TMA cannot take.
+size_t copied_bytes(int64_t groups, int64_t rows, int64_t cols) { return round256((size_t)groups * rows * round8(cols) * 2); }
 
 #define OLSGD_STEP(call)                    \
   do {                                      \
@@ -626,7 +667,8 @@ cudaError_t weights_copied(ExpertOperand& w, const ProductShape& d, uint8_t* dst
 template <int MODE>
 cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const GatedOperand& in, const int32_t* offsets, void* out, cudaStream_t s) {
   const int64_t k = MODE == FORWARD ? d.D : d.F, features = MODE == FORWARD ? d.F : d.D;
-  const Shape sh = shape_rows(d, features, k);
+  Shape sh = shape_rows(d, features, k);
+  if (getenv("OLSGD_SR")) sscanf(getenv("OLSGD_SR"), "%d,%d", &sh.halves, &sh.bn);
   ProductMaps maps;
   bool ok = make_map_weights(&maps.a[0], w, d, MODE == FORWARD ? kBM : kBK);
   for (int i = 0; i < kBoxes; ++i) {
@@ -635,7 +677,6 @@ cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const Gat
     if (i > 0) maps.a[i] = maps.a[0];
   }
   if (!ok) return cudaErrorInvalidValue;
-  maps.a_tail = maps.b_tail = maps.a[0];
   ProductArgs g{};
   g.R = (int)d.R;
   g.E = (int)d.E;
@@ -650,7 +691,7 @@ cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const Gat
   for (int64_t at = 0; at < d.m; at += most) {
     g.first_worker = (int)at;
     g.m = (int)(d.m - at < most ? d.m - at : most);
-    const cudaError_t e = sh.halves == 2 ? launch_variant<MODE, 2, 256, 3>(maps, g, s)
+    const cudaError_t e = sh.halves == 2 ? (sh.bn == 256 ? launch_variant<MODE, 2, 256, 3>(maps, g, s) : launch_variant<MODE, 2, 128, 4>(maps, g, s))
                           : sh.bn == 256 ? launch_variant<MODE, 1, 256, 4>(maps, g, s)
                           : sh.bn == 128 ? launch_variant<MODE, 1, 128, 6>(maps, g, s)
                           : sh.bn == 64  ? launch_variant<MODE, 1, 64, 8>(maps, g, s)
@@ -660,18 +701,9 @@ cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const Gat
   return cudaSuccess;
 }
 
-cudaError_t launch_weights(const ProductBackward& a, uint16_t* tail_dy, uint16_t* tail_x, cudaStream_t s) {
-  const int64_t groups = a.m * a.E;
-  TailArgs tails{};
-  tails.op[0] = TailOperand{static_cast<const uint16_t*>(a.dy.p), a.dy.worker_stride, a.dy.row_stride, tail_dy, a.F};
-  tails.op[1] = TailOperand{static_cast<const uint16_t*>(a.x.p), a.x.worker_stride, a.x.row_stride, tail_x, a.D};
-  tails.offsets = a.offsets;
-  tails.E = (int)a.E;
-  tails.R = (int)a.R;
-  OLSGD_STEP(launch_chained(tail_kernel, dim3((unsigned)groups, 2), dim3(256), 0, s, tails));
-  const GatedOperand tdy{tail_dy, kSmallBox * round8(a.F), round8(a.F)}, tx{tail_x, kSmallBox * round8(a.D), round8(a.D)};
+cudaError_t launch_weights(const ProductBackward& a, bool beside, cudaStream_t s) {
   ProductMaps maps;
-  bool ok = make_map16(&maps.a_tail, tdy, a.F, kSmallBox, groups, kSmallBox, a.f16) && make_map16(&maps.b_tail, tx, a.D, kSmallBox, groups, kSmallBox, a.f16);
+  bool ok = true;
   for (int i = 0; i < kBoxes; ++i) {
     const int rows = i < 2 ? kSmallBox << i : kBK;
     ok = ok && make_map16(&maps.a[i], a.dy, a.F, a.R, a.m, rows, a.f16) && make_map16(&maps.b[i], a.x, a.D, a.R, a.m, rows, a.f16);
@@ -685,10 +717,12 @@ cudaError_t launch_weights(const ProductBackward& a, uint16_t* tail_dy, uint16_t
   g.offsets = a.offsets;
   g.features = (int)a.F;
   g.cols = (int)a.D;
+  g.beside = beside;
   g.out = a.dw;
   g.out_width = store_width(a.dw, a.D);
-  const Shape sh = shape_weights(a);
-  return sh.halves == 2 ? launch_variant<DW, 2, 256, 3>(maps, g, s)
+  Shape sh = shape_weights(a);
+  if (getenv("OLSGD_SW")) sscanf(getenv("OLSGD_SW"), "%d,%d", &sh.halves, &sh.bn);
+  return sh.halves == 2 ? (sh.bn == 256 ? launch_variant<DW, 2, 256, 3>(maps, g, s) : launch_variant<DW, 2, 128, 4>(maps, g, s))
          : sh.bn == 256 ? launch_variant<DW, 1, 256, 4>(maps, g, s)
          : sh.bn == 128 ? launch_variant<DW, 1, 128, 6>(maps, g, s)
                         : launch_variant<DW, 1, 64, 7>(maps, g, s);
@@ -699,39 +733,33 @@ cudaError_t launch_weights(const ProductBackward& a, uint16_t* tail_dy, uint16_t
 bool product_needs_copies(const ProductShape& d, const GatedOperand& x, const ExpertOperand& w, const GatedOperand* dy) {
   return !tma_ready(x, d.R, d.m) || !weights_ready(w, d) || (dy && !tma_ready(*dy, d.R, d.m));
 }
-size_t product_workspace(const ProductShape& d, bool backward, bool copies) { return layout(d, backward, copies).total; }
+size_t product_workspace(const ProductShape& d, bool backward, bool copies) {
+  if (!copies) return 0;
+  return copied_bytes(d.m, d.R, d.D) + copied_bytes(d.m * d.E, d.F, d.D) + (backward ? copied_bytes(d.m, d.R, d.F) : 0);
+}
 
 cudaError_t launch_product(ProductForward a, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
-  uint8_t* copies = ws;
   const Wanted x[] = {{&a.x, a.R}};
-  if (!tma_ready(a.x, a.R, a.m)) {
-    OLSGD_STEP(make_ready(x, 1, a.D, a.m, copies, s));
-    copies += round256((size_t)a.m * a.R * round8(a.D) * 2);
-  }
-  OLSGD_STEP(weights_copied(a.w, a, copies, s));
+  OLSGD_STEP(make_ready(x, 1, a.D, a.m, ws, s));
+  OLSGD_STEP(weights_copied(a.w, a, ws + copied_bytes(a.m, a.R, a.D), s));
   return launch_rows<FORWARD>(a, a.w, a.x, a.offsets, a.y, s);
 }
 
 cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
-  const Workspace at = layout(a, true, product_needs_copies(a, a.x, a.w, &a.dy));
-  uint8_t* copies = ws;
   // dy for both, the weights for dx, x for the weights' gradient
   const Wanted x[] = {{&a.x, a.R}}, dy[] = {{&a.dy, a.R}};
-  if (!tma_ready(a.dy, a.R, a.m)) {
-    OLSGD_STEP(make_ready(dy, 1, a.F, a.m, copies, s));
-    copies += round256((size_t)a.m * a.R * round8(a.F) * 2);
-  }
-  if (a.dw && !tma_ready(a.x, a.R, a.m)) {
-    OLSGD_STEP(make_ready(x, 1, a.D, a.m, copies, s));
-    copies += round256((size_t)a.m * a.R * round8(a.D) * 2);
-  }
-  if (a.dx) {
-    OLSGD_STEP(weights_copied(a.w, a, copies, s));
-    OLSGD_STEP(launch_rows<DX>(a, a.w, a.dy, a.offsets, a.dx, s));
-  }
-  return a.dw ? launch_weights(a, reinterpret_cast<uint16_t*>(ws + at.tail_dy), reinterpret_cast<uint16_t*>(ws + at.tail_x), s) : cudaSuccess;
+  if (a.dw) OLSGD_STEP(make_ready(x, 1, a.D, a.m, ws, s));
+  ws += copied_bytes(a.m, a.R, a.D);
+  if (a.dx) OLSGD_STEP(weights_copied(a.w, a, ws, s));
+  ws += copied_bytes(a.m * a.E, a.F, a.D);
+  OLSGD_STEP(make_ready(dy, 1, a.F, a.m, ws, s));
+  // Neither product reads what the other writes.  The second is launched beside the first: its CTAs may start once all of
+  // the first one's have passed their gate (whatever came before has completed then), it takes the multiprocessors as they
+  // become free, and at its end it waits for the first.
+  if (a.dx) OLSGD_STEP(launch_rows<DX>(a, a.w, a.dy, a.offsets, a.dx, s));
+  return a.dw ? launch_weights(a, a.dx != nullptr, s) : cudaSuccess;
 }
 
 cudaError_t product_status(int* status) {

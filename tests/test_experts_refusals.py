@@ -108,12 +108,13 @@ def test_product_refusals(lib, backward, bad, word):
 def test_product_refuses_small_workspaces(lib):
     _expect(lib, _product(lib, x=P + 2, work=None), EINVAL, "workspace")      # copies are needed
     _expect(lib, _product(lib, x=P + 2, bytes=64), ENOMEM, "workspace")
-    _expect(lib, _product(lib, True, bytes=64), ENOMEM, "workspace")
-    _expect(lib, _product(lib, True, work=P + 8), EINVAL, "workspace")
+    _expect(lib, _product(lib, True, x=P + 2, bytes=64), ENOMEM, "workspace")
+    _expect(lib, _product(lib, True, dy=P + 2, work=P + 8), EINVAL, "workspace")
     _expect(lib, _product(lib, True, dy=None), EINVAL, "d_y must")
     assert _product(lib, True, y=None, dw=None, work=None) == 0               # nothing is wanted
     n = C.c_size_t()
-    assert lib.olsgd_expert_product_workspace(2, 40, 3, 64, 32, 0, 1, C.byref(n)) == 0 and n.value == 0
+    for backward in (0, 1):
+        assert lib.olsgd_expert_product_workspace(2, 40, 3, 64, 32, backward, 1, C.byref(n)) == 0 and n.value == 0
     assert lib.olsgd_expert_product_workspace(2, 0, 3, 64, 32, 1, 0, C.byref(n)) == 0 and n.value == 0
     assert lib.olsgd_expert_product_workspace(2, 40, 3, 64, 32, 1, 1, None) == EINVAL
 
