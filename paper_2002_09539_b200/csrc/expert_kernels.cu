@@ -25,24 +25,25 @@ using namespace op;
 constexpr int kSms = 148;
 constexpr int kRouteWarps = 32;
 constexpr int kRouteThreads = 32 * kRouteWarps;
+constexpr int kKeptSlots = 64 * 1024;
 constexpr int kSorted = 4;   // elements of a lane that are sorted ahead of the rounds
 static_assert(OLSGD_MAX_EXPERTS <= kRouteThreads, "a thread for each expert");
 static_assert(OLSGD_MAX_TOP <= 32, "a lane for each slot of a token");
+static_assert(OLSGD_MAX_EXPERTS <= 1024, "ten bits");
 
-// Values that order as the logits do: 0 for -inf (never chosen), NaN above all.
-constexpr uint32_t kNanKey = 0xFFFFFFFEu;
+// Values that order as the logits do: 0 for -inf (never chosen), NaN above all.  (Adding 0 makes -0 +0, and any NaN the one
+// with sign 0.)
+constexpr uint32_t kLowest = 0x007FFFFFu;   // of -inf before it is moved to 0
 __device__ __forceinline__ uint32_t key_of(float v) {
-  uint32_t u = __float_as_uint(v);
-  if (u == 0x80000000u) u = 0;
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return kNanKey;
-  if (u == 0xFF800000u) return 0;
-  return (u >> 31) ? ~u : (u | 0x80000000u);
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return (u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) - kLowest;
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
-  if (key == kNanKey) return __uint_as_float(0x7FFFFFFFu);
-  if (key == 0) return -INFINITY;
-  return __uint_as_float((key >> 31) ? (key & 0x7FFFFFFFu) : ~key);
+  const uint32_t o = key + kLowest;
+  return __uint_as_float((o >> 31) ? (o ^ 0x80000000u) : ~o);
 }
+// e^d by the hardware's power of two: off by 2 steps and the rounding of d log2 e.
+__device__ __forceinline__ float power(float d) { return ex2(d * kLog2e); }
 
 // A lane's NL consecutive elements of a row of n; those past it are `fill`.  vec: E is a multiple of NL and rows start on
 // boundaries of the NL elements (or of 16 bytes).
@@ -78,6 +79,7 @@ struct RouteKernelArgs {
   int64_t ld;
   int T, E, k, per_warp;     // tokens of a worker, experts, slots of a token, tokens of a warp
   int normalise, vec;
+  int keep;                  // whether a CTA's slots have room in shared memory
   float* weights;
   int32_t *ids, *places, *tokens, *offsets;
   int32_t* counts;           // [m][tiles][E], where a worker's tokens take several CTAs
@@ -110,11 +112,13 @@ __device__ __forceinline__ int block_before(int v, int* warp_sums) {
 // CTA (tile, worker): tokens tile * 32 * per_warp and up.
 template <typename T, int NL, bool ONE>
 __global__ void __launch_bounds__(kRouteThreads, 1) route_kernel(const RouteKernelArgs a) {
-  extern __shared__ int count[];   // [kRouteWarps][E]
+  extern __shared__ int count[];   // [kRouteWarps][E]; then (keep) the slots' experts and ranks, [kRouteWarps][per_warp][k]
   __shared__ int warp_sums[32];
+  __shared__ int2 picked[kRouteWarps][32];   // expert and key of a token's slots (NL <= kSorted)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, E = a.E, k = a.k;
   const int64_t worker = blockIdx.y;
   int* mine = count + warp * E;
+  uint32_t* slots = reinterpret_cast<uint32_t*>(count + kRouteWarps * E) + (int64_t)warp * a.per_warp * k;
   for (int e = lane; e < E; e += 32) mine[e] = 0;
   __syncwarp();
   launch_gate();
@@ -138,7 +142,7 @@ __global__ void __launch_bounds__(kRouteThreads, 1) route_kernel(const RouteKern
     uint32_t chosen = 0, top = 0;
     if constexpr (NL <= kSorted) {
       // Each lane's keys in falling order (equal ones stay as they are), so that what a round takes is a head.
-      int at[NL];
+      int at[NL], found = 0;
       uint32_t own[NL];
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
@@ -161,19 +165,25 @@ __global__ void __launch_bounds__(kRouteThreads, 1) route_kernel(const RouteKern
         const uint32_t most = __reduce_max_sync(0xffffffffu, own[0]);
         if (most == 0) break;
         if (j == 0) top = most;
-        const int winner = __ffs(__ballot_sync(0xffffffffu, own[0] == most)) - 1;
-        const int from = __shfl_sync(0xffffffffu, at[0], winner);
-        if (lane == j) {
-          id = from;
-          chosen = most;
-        }
-        const bool mine_left = lane == winner;
+        const uint32_t equal = __ballot_sync(0xffffffffu, own[0] == most);
+        if ((equal & (0u - equal)) == 1u << lane) {   // the lowest of the lanes that have it: its head leaves
+          picked[warp][j] = make_int2(at[0], (int)most);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          own[i] = mine_left ? (i + 1 < NL ? own[i + 1 < NL ? i + 1 : i] : 0u) : own[i];
-          at[i] = mine_left && i + 1 < NL ? at[i + 1 < NL ? i + 1 : i] : at[i];
+          for (int i = 0; i + 1 < NL; ++i) {
+            own[i] = own[i + 1];
+            at[i] = at[i + 1];
+          }
+          own[NL - 1] = 0;
         }
+        found = j + 1;
       }
+      __syncwarp();
+      if (lane < found) {
+        const int2 p = picked[warp][lane];
+        id = p.x;
+        chosen = (uint32_t)p.y;
+      }
+      __syncwarp();
     } else {
       for (int j = 0; j < k; ++j) {
         const uint32_t most = __reduce_max_sync(0xffffffffu, best);
@@ -203,19 +213,22 @@ __global__ void __launch_bounds__(kRouteThreads, 1) route_kernel(const RouteKern
       }
     }
     const float base = value_of(top);
-    float e = id >= 0 ? expf(value_of(chosen) - base) : 0.f, total = e;
+    float e = id >= 0 ? power(value_of(chosen) - base) : 0.f, total = e;
     if (!a.normalise) {
       // all of them (NL > kSorted: those chosen have left, and count already)
       if (NL <= kSorted) total = 0.f;
 #pragma unroll
-      for (int i = 0; i < NL; ++i) total += key[i] ? expf(value_of(key[i]) - base) : 0.f;
+      for (int i = 0; i < NL; ++i) total += key[i] ? power(value_of(key[i]) - base) : 0.f;
     }
     total = warp_sum(total);
     if (lane < k) {
       const int64_t slot = (worker * a.T + t) * k + lane;
       a.ids[slot] = id;
       a.weights[slot] = id >= 0 ? e / total : 0.f;
-      a.places[slot] = id >= 0 ? mine[id]++ : -1;   // (for now: its rank among the warp's slots of this expert)
+      // its rank among the warp's slots of this expert
+      const int rank = id >= 0 ? mine[id]++ : -1;
+      if (a.keep) slots[(t - first) * k + lane] = id >= 0 ? (uint32_t)rank << 10 | (uint32_t)id : ~0u;
+      else a.places[slot] = rank;
     }
     __syncwarp();
   }
@@ -244,16 +257,22 @@ __global__ void __launch_bounds__(kRouteThreads, 1) route_kernel(const RouteKern
     a.counts[(worker * gridDim.x + blockIdx.x) * E + threadIdx.x] = sum;
   }
   __syncthreads();
-  // (each lane reads what it has written)
+  // (each lane reads what it has written; not kept: in global memory)
   for (int64_t t = first; t < last; ++t) {
     const int64_t slot = (worker * a.T + t) * k + lane;
     if (lane < k) {
-      const int id = a.ids[slot];
-      if (id >= 0) {
-        const int place = a.places[slot] + mine[id];
-        a.places[slot] = place;
-        if (ONE) a.tokens[worker * a.T * k + place] = (int32_t)t;
+      int id, rank;
+      if (a.keep) {
+        const uint32_t s = slots[(t - first) * k + lane];
+        id = s == ~0u ? -1 : (int)(s & 1023u);
+        rank = (int)(s >> 10);
+      } else {
+        id = a.ids[slot];
+        rank = a.places[slot];
       }
+      const int place = id >= 0 ? rank + mine[id] : -1;
+      a.places[slot] = place;
+      if (ONE && id >= 0) a.tokens[worker * a.T * k + place] = (int32_t)t;
     }
   }
 }
@@ -353,7 +372,7 @@ __global__ void __launch_bounds__(256) route_backward_kernel(const RouteGradArgs
     const bool empty = __ballot_sync(0xffffffffu, id >= 0) == 0;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      x[i] = empty ? 0.f : expf(x[i] - most);
+      x[i] = empty ? 0.f : power(x[i] - most);
       total += x[i];
     }
     const float share = empty ? 0.f : 1.f / warp_sum(total);
@@ -556,14 +575,16 @@ bool lanes_aligned(const void* p, int64_t ld, int64_t E, int nl, int size) {
 
 template <typename T, int NL>
 cudaError_t route_as(const RouteArgs& r, cudaStream_t s) {
-  RouteKernelArgs a{r.logits, r.ld, (int)r.T, (int)r.E, r.k, route_per_warp(r.m, r.T), r.normalise,
-                    lanes_aligned(r.logits, r.ld, r.E, NL, sizeof(T)), r.weights, r.ids, r.places, r.tokens, r.offsets,
+  const int per_warp = route_per_warp(r.m, r.T);
+  const int64_t tiles = route_tiles(r.m, r.T), slots = (int64_t)kRouteWarps * per_warp * r.k * sizeof(int);
+  const bool keep = slots <= kKeptSlots;
+  RouteKernelArgs a{r.logits, r.ld, (int)r.T, (int)r.E, r.k, per_warp, r.normalise,
+                    lanes_aligned(r.logits, r.ld, r.E, NL, sizeof(T)), keep, r.weights, r.ids, r.places, r.tokens, r.offsets,
                     static_cast<int32_t*>(r.ws)};
-  const int64_t tiles = route_tiles(r.m, r.T);
-  const size_t smem = (size_t)kRouteWarps * r.E * sizeof(int);
+  const size_t smem = (size_t)kRouteWarps * r.E * sizeof(int) + (keep ? slots : 0);
   static PerDeviceSmem configured[2];
   auto kern = tiles == 1 ? route_kernel<T, NL, true> : route_kernel<T, NL, false>;
-  cudaError_t e = ensure_dynamic_smem(configured[tiles == 1], kern, (size_t)kRouteWarps * 32 * NL * sizeof(int));
+  cudaError_t e = ensure_dynamic_smem(configured[tiles == 1], kern, (size_t)kRouteWarps * 32 * NL * sizeof(int) + kKeptSlots);
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)tiles, (unsigned)r.m);
   e = launch_chained(kern, grid, dim3(kRouteThreads), smem, s, a);

@@ -567,7 +567,8 @@ cudaError_t launch_variant(const ProductMaps& maps, ProductArgs g, cudaStream_t 
 
 // Which tiles: by the sizes alone; how the rows fall to the experts is not known here and taken as even.  A tile takes, in
 // cycles: per K block the longest of its operands' way from L2 (36 bytes a cycle), its MMAs (M N / 64) and, where
-// each weight is used by one tile only, the weights' way from memory (23 bytes a cycle and multiprocessor); then its results'
+// each weight is used by one tile only, the weights' way from memory (19 bytes a cycle and multiprocessor in rows of 256, 16 in
+// rows of 128); then its results'
 // way out, at its side where there are two accumulators.  The launch takes as many waves as its tiles need.
 struct Shape {
   int halves, bn;
@@ -576,7 +577,8 @@ double tile_cycles(const Shape& sh, double rows, double kbs, bool once, double o
   const double m = sh.halves * kBM;
   double block = (m + rows) * 128 / 36;
   if (m * rows / 64 > block) block = m * rows / 64;
-  if (once && m * 128 / 23 > block) block = m * 128 / 23;
+  const double far = sh.halves == 2 ? 19 : 16;
+  if (once && m * 128 / far > block) block = m * 128 / far;
   const double in = kbs * block, out = m * rows * 2 / out_rate;
   return 400 + (sh.halves * sh.bn > 256 ? in + 0.6 * out : in > out ? in : out);
 }
