@@ -151,6 +151,8 @@ def _rows_of(t, name):
     if len(shape) == 2:
         N = shape[0]
         return t.data_ptr(), code, N, V, (stride[0] if N > 1 else V)
+    if t.is_contiguous():
+        return t.data_ptr(), code, t.numel() // V, V, V
     try:   # (one launch takes rows at one distance)
         rows = t.view(-1, V)
     except RuntimeError:
@@ -395,16 +397,17 @@ def expert_route(logits, k, normalise=True):
     normalise: softmax over the chosen, else the chosen ones' share of the softmax over all.  Returns ExpertRoute(weights, ids,
     places, tokens, offsets): float32 [m][T][k], int32 [m][T][k], [m][T][k], [m][T k], [m][E + 1].  The rows' inputs:
     embedding_forward(x, route.tokens); their gradient: expert_combine(d_rows, route.places)."""
-    _recorded(logits)
-    lib = _ops()
+    if logits.requires_grad:
+        _recorded(logits)
+    lib = _OPS or _ops()
     xp, code, m, T, E, ld, k = _route_sizes(logits, k)
     dev = logits.device
     if m < 1:
         _refuse("logits must be of one worker at least")
-    lead = (m, T, k)
-    weights = torch.empty(lead, dtype=_F32, device=dev)
-    ids, places = torch.empty(lead, dtype=_I32, device=dev), torch.empty(lead, dtype=_I32, device=dev)
-    tokens, offsets = torch.empty((m, T * k), dtype=_I32, device=dev), torch.empty((m, E + 1), dtype=_I32, device=dev)
+    lead, by = (m, T, k), (T * k, k, 1)
+    weights, ids = _strided(lead, by, dtype=_F32, device=dev), _strided(lead, by, dtype=_I32, device=dev)
+    places = _like(ids)
+    tokens, offsets = _strided((m, T * k), (T * k, 1), dtype=_I32, device=dev), _strided((m, E + 1), (E + 1, 1), dtype=_I32, device=dev)
     ws, wp, wn = _workspace(offsets, "olsgd_expert_route_workspace", m, T, E)
     _run(lib.olsgd_expert_route, dev, m, T, E, code, xp, ld, k, 1 if normalise else 0, weights.data_ptr(), ids.data_ptr(), places.data_ptr(),
          tokens.data_ptr(), offsets.data_ptr(), wp, wn)
@@ -415,7 +418,7 @@ def expert_route_backward(d_weights, logits, ids, weights, normalise=True):
     """olsgd_expert_route_backward: the gradient of the logits, contiguous, of their type.  d_weights float32 [m][T][k]; ids and
     weights are expert_route's for the same logits and `normalise`."""
     _recorded(d_weights, logits, weights)
-    lib = _ops()
+    lib = _OPS or _ops()
     if ids.dim() != 3:
         _refuse("ids must be [m][T][k]")
     xp, code, m, T, E, ld, k = _route_sizes(logits, ids.shape[2])
@@ -440,7 +443,7 @@ def expert_combine(rows, places, weights=None):
     types, D contiguous; places int32 [m][T][k], those outside [0, R) add nothing; weights float32 [m][T][k], None: all 1.  Returns
     [m][T][D] of the rows' type."""
     _recorded(rows, weights)
-    lib = _ops()
+    lib = _OPS or _ops()
     code, m, T, k, R, D = _combine_sizes(rows, places)
     dev, lead = rows.device, (m, T, k)
     p, sw, sr = _matrix(rows, "rows", (m, R, D), rows.dtype, dev)
@@ -455,13 +458,13 @@ def expert_combine_backward(d_y, rows, places, tokens, weights):
     """olsgd_expert_combine_backward: (d_rows, d_weights) from d_y [m][T][D] and the forward call's operands; places and tokens as
     expert_route gives them (each row is named once at most; tokens is negative for the others)."""
     _recorded(d_y, rows, weights)
-    lib = _ops()
+    lib = _OPS or _ops()
     code, m, T, k, R, D = _combine_sizes(rows, places)
     dev, lead = rows.device, (m, T, k)
     g, r = _matrix(d_y, "d_y", (m, T, D), rows.dtype, dev), _matrix(rows, "rows", (m, R, D), rows.dtype, dev)
     pp, tp = _per_row(places, lead, _I32, dev, "places"), _per_row(tokens, (m, R), _I32, dev, "tokens")
     wp = _per_row(weights, lead, _F32, dev, "weights")
-    d_rows, d_weights = rows.new_empty((m, R, D)), torch.empty(lead, dtype=_F32, device=dev)
+    d_rows, d_weights = rows.new_empty((m, R, D)), _like(weights)
     _run(lib.olsgd_expert_combine_backward, dev, m, T, k, R, D, code, *g, *r, pp, tp, wp, d_rows.data_ptr(), d_weights.data_ptr())
     return d_rows, d_weights
 
@@ -490,7 +493,7 @@ def expert_product(x, w, offsets):
     expert become zeros.  x [m][R][D], rows contiguous, any worker and row strides; w [m][E][F][D], any strides but the last; bfloat16
     or float16; offsets int32 [m][E + 1], rising.  Returns [m][R][F]."""
     _recorded(x, w)
-    lib = _ops()
+    lib = _OPS or _ops()
     m, R, E, D, F, code, op, wm, ok = _product_sizes(x, w, offsets)
     a = _matrix(x, "x", (m, R, D), x.dtype, x.device)
     y = x.new_empty((m, R, F))
@@ -504,7 +507,7 @@ def expert_product_backward(d_y, x, w, offsets, want_d_x=True, want_d_w=True):
     """olsgd_expert_product_backward: (d_x, d_w) from d_y [m][R][F] and the forward call's operands; None for one that is not
     wanted."""
     _recorded(d_y, x, w)
-    lib = _ops()
+    lib = _OPS or _ops()
     m, R, E, D, F, code, op, wm, ok = _product_sizes(x, w, offsets)
     dtype, dev = x.dtype, x.device
     g, a = _matrix(d_y, "d_y", (m, R, F), dtype, dev), _matrix(x, "x", (m, R, D), dtype, dev)
@@ -539,12 +542,15 @@ def distill_loss(logits, ids, teacher, temperature=1.0, d_loss=None):
     comes from the same read of them.  Returns DistillLoss(loss, stats, d_logits): float32 [...] and [..., 2], and the gradient
     (contiguous, of the logits' type) or None."""
     _recorded(logits, teacher, d_loss)
-    lib = _ops()
+    lib = _OPS or _ops()
     xp, code, N, V, ld = _rows_of(logits, "logits")
     dev, lead = logits.device, logits.shape[:-1]
     ip, tp, tcode, K, t = _teacher(logits, ids, teacher, temperature)
     gp = None if d_loss is None else _per_row(d_loss, lead, _F32, dev, "d_loss")
-    loss, stats = torch.empty(lead, dtype=_F32, device=dev), torch.empty(lead + (2,), dtype=_F32, device=dev)
+    if len(lead) == 1:
+        loss, stats = _strided(lead, _ONE, dtype=_F32, device=dev), _strided((N, 2), _TWO, dtype=_F32, device=dev)
+    else:
+        loss, stats = torch.empty(lead, dtype=_F32, device=dev), torch.empty(lead + (2,), dtype=_F32, device=dev)
     d = None if d_loss is None else logits.new_empty(logits.shape)
     ws, wp, wn = _workspace(loss, "olsgd_distill_workspace", code, N, V, 0 if d_loss is None else 1)
     _run(lib.olsgd_distill, dev, xp, code, N, V, ld, ip, tp, tcode, K, t, gp, loss.data_ptr(), stats.data_ptr(),
@@ -556,7 +562,7 @@ def distill_backward(d_loss, logits, ids, teacher, stats, temperature=1.0):
     """olsgd_distill_backward: the logits' gradient alone, contiguous, of their type.  d_loss float32 [...]; stats are
     distill_loss's for the same logits and temperature."""
     _recorded(d_loss, logits, teacher, stats)
-    lib = _ops()
+    lib = _OPS or _ops()
     xp, code, N, V, ld = _rows_of(logits, "logits")
     dev, lead = logits.device, logits.shape[:-1]
     ip, tp, tcode, K, t = _teacher(logits, ids, teacher, temperature)
