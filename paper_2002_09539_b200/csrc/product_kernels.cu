@@ -22,9 +22,9 @@
 //
 // TMA wants 16-byte row pitches: operands that do not have them are copied to padded rows in
 // the workspace first.  Every wait is bounded, as in the library's other tensor-core kernels.
+#include <cmath>
+
 #include "operator_tiles.cuh"
-#include <cstdlib>
-#include <cstdio>
 
 namespace olsgd {
 namespace {
@@ -53,6 +53,11 @@ struct ProductArgs {
   int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
   const int32_t* offsets;     // [workers][E + 1]
   void* out;
+  // K by parts, where the tiles are few: `splits` units for a tile, whose sums go to parts[split][...] in fp32 (rows of
+  // features; DW: [group][column][feature]), part_size values each, for join_kernel
+  int splits;
+  float* parts;
+  int64_t part_size;
 };
 
 template <int STAGES>
@@ -121,6 +126,14 @@ __device__ __forceinline__ void make_table(const ProductArgs& g, Table& tb, int 
   __syncthreads();
 }
 
+// One lane of a whole warp.  (Of lanes chosen this way the compiler knows that they are one: operands of TMA and MMA
+// instructions stay in uniform registers.  193 cycles a block of 64 along K, 160 a copy and 100 an MMA where lane 0 was asked for.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
+
 // Of the weights: [m][E][F][D].
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
   asm volatile(
@@ -135,6 +148,7 @@ struct Unit {
   int worker, group;     // DW: group of the worker's and all before it; FORWARD, DX: expert of the worker
   int m, col;            // feature tile; DW: column tile
   int row0, n;           // rows (FORWARD, DX: the tile's, DW: the group's)
+  int split, kb, end;    // blocks of K
 };
 template <int MODE, int BN>
 struct Walk {
@@ -143,11 +157,16 @@ struct Walk {
   uint32_t total;
   int at_group = 0;
   __device__ __forceinline__ Walk(const ProductArgs& args, const Table& table) : g(args), tb(table) {
-    total = MODE == DW ? (uint32_t)(g.m * g.E) * g.m_tiles * g.n_tiles : (uint32_t)tb.first[g.m * g.E] * g.m_tiles;
+    total = (MODE == DW ? (uint32_t)(g.m * g.E) * g.m_tiles * g.n_tiles : (uint32_t)tb.first[g.m * g.E] * g.m_tiles) * g.splits;
   }
   // t: no less than at the call before
   __device__ __forceinline__ Unit at(uint32_t t) {
     Unit u;
+    u.split = 0;
+    if (g.splits > 1) {
+      u.split = t % g.splits;
+      t /= g.splits;
+    }
     if (MODE == DW) {
       const uint32_t per = g.m_tiles * g.n_tiles;
       u.group = t / per;
@@ -171,6 +190,13 @@ struct Walk {
       u.group = at_group - worker * g.E;
       u.m = t - i * g.m_tiles;
       u.col = 0;
+    }
+    const int blocks = MODE == DW ? (u.n + kBK - 1) / kBK : g.num_kb;
+    u.kb = 0;
+    u.end = blocks;
+    if (g.splits > 1) {
+      u.kb = (int)((int64_t)blocks * u.split / g.splits);
+      u.end = (int)((int64_t)blocks * (u.split + 1) / g.splits);
     }
     return u;
   }
@@ -243,6 +269,12 @@ __device__ __forceinline__ void zero_rows(const ProductArgs& g, const Table& tb,
     const int head = tb.start[w * (g.E + 1)], tail = g.R - tb.start[w * (g.E + 1) + g.E];
     for (int i = at; i < head + tail; i += warps) {
       const int row = i < head ? i : g.R - tail + (i - head);
+      if (g.parts) {
+        float* dst = g.parts + ((int64_t)(g.first_worker + w) * g.R + row) * g.features;
+        for (int split = 0; split < g.splits; ++split)
+          for (int c = lane; c < g.features; c += 32) dst[split * g.part_size + c] = 0.f;
+        continue;
+      }
       uint8_t* dst = static_cast<uint8_t*>(g.out) + ((int64_t)(g.first_worker + w) * g.R + row) * bytes;
       if (g.out_width == 16)
         for (int64_t c = lane * 16; c < bytes; c += 512) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
@@ -300,7 +332,6 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   const uint32_t tmem_base = ctl->tmem_base;
   Walk<MODE, BN> walk(g, table);
   const uint32_t total = walk.total;
-  const auto blocks_of = [&](const Unit& u) { return MODE == DW ? (u.n + kBK - 1) / kBK : g.num_kb; };
   const auto mma_cols = [&](const Unit& u) { return MODE == DW ? BN : (u.n + kSmallBox - 1) / kSmallBox * kSmallBox; };
   // Boxes of A and (DW) of B: none lies wholly outside its tensor.  What stays in their place reaches only parts of the
   // accumulator that are not stored.
@@ -310,13 +341,14 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   };
   const auto b_boxes = [&](const Unit& u) { return min(BN / 64, (g.cols - u.col * BN + 63) / 64); };
 
-  if (warp == 0 && lane == 0) {
+  const bool one = MODE == DW ? lane == 0 : elect_one();   // (DW: its MMA warp has work for all lanes)
+  if (warp == 0 && one) {
     // ---------------- TMA producer
     uint32_t it = 0;
     for (uint32_t t = first; t < total && !*abort_flag; t += step) {
       const Unit u = walk.at(t);
       const int m0 = u.m * kTileM, held = mma_cols(u), na = a_boxes(u), nb = MODE == DW ? b_boxes(u) : 0;
-      for (int kb = 0, end = blocks_of(u); kb < end; ++kb, ++it) {
+      for (int kb = u.kb; kb < u.end; ++kb, ++it) {
         const int s = it % STAGES, k0 = kb * kBK;
         if (!mbar_wait(smem_u32(&ctl->empty[s]), ((it / STAGES) & 1) ^ 1, abort_flag)) break;
         const uint32_t bar = smem_u32(&ctl->full[s]);
@@ -358,7 +390,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         while (!mbar_try_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1) && global_ns() - t0 < 10000000ull) {
         }
     }
-  } else if (warp == 1 && (MODE == DW || lane == 0)) {
+  } else if (warp == 1 && (MODE == DW || one)) {
     // ---------------- MMA issuer: one lane; DW: its warp comes along, for the zeros
     const uint32_t fmt = g.f16 ? 0u : ((1u << 7) | (1u << 10));
     const uint32_t idesc0 = (1u << 4) | fmt | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(kBM >> 4) << 24);
@@ -366,8 +398,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
     bool ok = true;
     for (uint32_t t = first; t < total && ok; t += step) {
       const Unit u = walk.at(t);
-      const int end = blocks_of(u);
-      if (end == 0) continue;
+      if (u.kb == u.end) continue;
       const uint32_t idesc = idesc0 | ((uint32_t)(mma_cols(u) >> 3) << 17);
       const int k_extent = MODE == DW ? u.n : g.k_extent;
       const auto multiply = [&](int kb, uint32_t s, int half, uint32_t acc) {
@@ -379,7 +410,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         const int left = k_extent - kb * kBK;   // (what lies behind is zeros, or was not loaded)
 #pragma unroll
         for (int k = 0; k < kBK / kUmmaK; ++k)
-          if (k * kUmmaK < left && lane == 0) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          if (k * kUmmaK < left && (MODE != DW || lane == 0)) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > u.kb || k > 0) ? 1u : 0u);
       };
       const auto wait = [&](uint64_t* bar, uint32_t parity) {
         int done = 1;
@@ -389,7 +420,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         return done != 0;
       };
       const auto commit = [&](uint64_t* bar) {
-        if (lane == 0) umma_commit(smem_u32(bar));
+        if (MODE != DW || lane == 0) umma_commit(smem_u32(bar));
       };
       const auto arrived = [&](int kb, uint32_t i) {
         ok = wait(&ctl->full[i % STAGES], (i / STAGES) & 1);
@@ -411,7 +442,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         const uint32_t buf = n & 1, acc = tmem_base + buf * (HALVES * BN);
         ok = wait(&ctl->acc_empty[buf], ((n >> 1) & 1) ^ 1);
         if (!ok) break;
-        for (int kb = 0; kb < end; ++kb, ++it) {
+        for (int kb = u.kb; kb < u.end; ++kb, ++it) {
           if (!arrived(kb, it)) break;
 #pragma unroll
           for (int half = 0; half < HALVES; ++half) multiply(kb, it % STAGES, half, acc + half * BN);
@@ -420,21 +451,22 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         commit(&ctl->acc_full[buf]);
       } else {
         // The first blocks' MMAs of the first half run while the second is emptied.
-        const int lead = min(end, STAGES);
+        const int lead = u.kb + min(u.end - u.kb, STAGES);
         ok = wait(&ctl->acc_empty[0], (n & 1) ^ 1);
         if (!ok) break;
-        for (int kb = 0; kb < lead; ++kb) {
-          if (!arrived(kb, it + kb)) break;
-          multiply(kb, (it + kb) % STAGES, 0, tmem_base);
+        for (int kb = u.kb; kb < lead; ++kb) {
+          const uint32_t i = it + (kb - u.kb);
+          if (!arrived(kb, i)) break;
+          multiply(kb, i % STAGES, 0, tmem_base);
         }
         if (!ok) break;
         ok = wait(&ctl->acc_empty[1], (n & 1) ^ 1);
         if (!ok) break;
-        for (int kb = 0; kb < lead; ++kb, ++it) {
+        for (int kb = u.kb; kb < lead; ++kb, ++it) {
           multiply(kb, it % STAGES, 1, tmem_base + BN);
           commit(&ctl->empty[it % STAGES]);
         }
-        for (int kb = lead; kb < end; ++kb, ++it) {
+        for (int kb = lead; kb < u.end; ++kb, ++it) {
           if (!arrived(kb, it)) break;
           multiply(kb, it % STAGES, 0, tmem_base);
           multiply(kb, it % STAGES, 1, tmem_base + BN);
@@ -451,7 +483,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
     uint32_t n = 0;
     for (uint32_t t = first; t < total; t += step) {
       const Unit u = walk.at(t);
-      const bool none = MODE == DW && u.n == 0;   // zeros, and no accumulator
+      const bool none = MODE == DW && u.kb == u.end;   // zeros, and no accumulator
       const uint32_t buf = kBufs == 2 ? n & 1 : 0, parity = kBufs == 2 ? (n >> 1) & 1 : n & 1;
       // one lane waits for its warp: what follows wants all lanes together
       int ok = 1;
@@ -464,7 +496,28 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         const int feature0 = u.m * kTileM + half * kBM + lane_group * 32;
         const uint32_t acc = tmem_base + (buf * HALVES + half) * BN + ((uint32_t)(lane_group * 32) << 16);
         if (feature0 < g.features) {
-          if (MODE == DW) {
+          if (g.parts) {
+            // a row of 32 features a store; join_kernel rounds
+            const int columns = MODE == DW ? min(BN, g.cols - u.col * BN) : u.n;
+            const int64_t row = MODE == DW ? (int64_t)u.group * g.cols + u.col * BN : (int64_t)u.worker * g.R + u.row0;
+            float* dst = g.parts + u.split * g.part_size + row * g.features + feature0 + lane;
+#pragma unroll 1
+            for (int c = side * 32; c < columns; c += 64) {
+              float v[32];
+              if (none) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = 0.f;
+              } else {
+                tmem_ld32(acc + c, v);
+              }
+              if (feature0 + lane < g.features) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                  if (c + j < columns) dst[(int64_t)(c + j) * g.features] = v[j];
+              }
+              __syncwarp();
+            }
+          } else if (MODE == DW) {
             constexpr int W = kBlockCols;
             Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * 256};
             uint16_t* dst = static_cast<uint16_t*>(g.out) + ((int64_t)u.group * g.features + feature0) * g.cols;
@@ -544,6 +597,83 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   if (g.beside) launch_gate();
 }
 
+// The sums of the parts of K, in their order, and the one rounding.  At most two products at a time (a backward call's),
+// the first by the first blocks.  FORWARD, DX: the parts lie as the output does, V values a thread.  DW: they lie with features
+// side by side, the output with columns: 32 x 32 at a time through shared memory.
+struct JoinJob {
+  const float* parts;
+  void* out;
+  int64_t part_size;
+  int64_t blocks;
+  int64_t features, cols;   // DW
+  int splits, transposed, wide;   // wide: 4 values of the output are aligned together (and of the parts)
+};
+struct JoinArgs {
+  JoinJob job[2];
+  int f16;
+};
+template <int V>
+__device__ __forceinline__ void sum_parts(const float* p, int64_t part_size, int splits, float* v) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    if (V == 4) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(p + s * part_size));
+      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+    } else {
+      v[0] += __ldcg(p + s * part_size);
+    }
+  }
+}
+__global__ void __launch_bounds__(256) join_kernel(const JoinArgs a) {
+  launch_gate();
+  __shared__ float tile[32][33];
+  int64_t block = blockIdx.x;
+  const bool second = block >= a.job[0].blocks;
+  const JoinJob& j = a.job[second];
+  if (second) block -= a.job[0].blocks;
+  uint16_t* out = static_cast<uint16_t*>(j.out);
+  if (!j.transposed) {
+    const int64_t i = (block * 256 + threadIdx.x) * (j.wide ? 4 : 1);
+    if (i >= j.part_size) return;
+    float v[4];
+    if (j.wide) {
+      sum_parts<4>(j.parts + i, j.part_size, j.splits, v);
+      *reinterpret_cast<uint2*>(out + i) = make_uint2(pack2(v[0], v[1], a.f16), pack2(v[2], v[3], a.f16));
+    } else {
+      sum_parts<1>(j.parts + i, j.part_size, j.splits, v);
+      out[i] = (uint16_t)pack2(v[0], 0.f, a.f16);
+    }
+    return;
+  }
+  const int64_t f_tiles = (j.features + 31) / 32, c_tiles = (j.cols + 31) / 32;
+  const int64_t group = block / (f_tiles * c_tiles), at = block - group * f_tiles * c_tiles;
+  const int64_t c0 = at / f_tiles * 32, f0 = (at % f_tiles) * 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int64_t c = c0 + warp * 4 + q, f = f0 + lane;
+    float v = 0.f;
+    if (c < j.cols && f < j.features) sum_parts<1>(j.parts + (group * j.cols + c) * j.features + f, j.part_size, j.splits, &v);
+    tile[lane][warp * 4 + q] = v;
+  }
+  __syncthreads();
+  const int64_t f = f0 + threadIdx.x / 8, c = c0 + threadIdx.x % 8 * 4;
+  if (f >= j.features || c >= j.cols) return;
+  const float* v = tile[threadIdx.x / 8] + threadIdx.x % 8 * 4;
+  uint16_t* dst = out + (group * j.features + f) * j.cols + c;
+  const uint32_t lo = pack2(v[0], v[1], a.f16), hi = pack2(v[2], v[3], a.f16);
+  if (j.wide) {
+    *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+  } else {
+    store_half_if(dst, lo, true);
+    store_half_if(dst + 1, lo >> 16, c + 1 < j.cols);
+    store_half_if(dst + 2, hi, c + 2 < j.cols);
+    store_half_if(dst + 3, hi >> 16, c + 3 < j.cols);
+  }
+}
+
 // --------------------------------------------------------------------------------- host
 constexpr int kSms = 148;
 
@@ -559,64 +689,84 @@ cudaError_t launch_variant(const ProductMaps& maps, ProductArgs g, cudaStream_t 
   g.m_tiles = (g.features + HALVES * kBM - 1) / (HALVES * kBM);
   g.n_tiles = (g.cols + BN - 1) / BN;
   // (of row tiles, disjoint groups have no more)
-  const int64_t total = (int64_t)g.m_tiles * g.m * (MODE == DW ? (int64_t)g.E * g.n_tiles : g.R / BN + (g.E < g.R ? g.E : g.R));
+  const int64_t total = (int64_t)g.splits * g.m_tiles * g.m * (MODE == DW ? (int64_t)g.E * g.n_tiles : g.R / BN + (g.E < g.R ? g.E : g.R));
   const int64_t room = sm_count();
   g_tc_launches += 1;
   return launch_chained(kern, dim3((unsigned)(total < room ? total : room)), dim3(kThreads), smem, s, maps, g);
 }
 
-// Which tiles: by the sizes alone; how the rows fall to the experts is not known here and taken as even.  A tile takes, in
-// cycles: per K block the longest of its operands' way from L2 (36 bytes a cycle), its MMAs (M N / 64) and, where
-// each weight is used by one tile only, the weights' way from memory (19 bytes a cycle and multiprocessor in rows of 256, 16 in
-// rows of 128); then its results'
-// way out, at its side where there are two accumulators.  The launch takes as many waves as its tiles need.
+// Which tiles, and how many parts of K: by the sizes alone; how the rows fall to the experts is not known here and taken as even.
+// A tile takes, in cycles, 1000 and per K block the longest of its operands' way from L2 (36 bytes a cycle and multiprocessor
+// when all take in something, 44 when few do), its MMAs (M N / 64) and, where each weight is used by one tile only, the weights'
+// way from memory (26 bytes a cycle of 148); its results' way out (24 bytes a cycle) passes beside the next tile where
+// there are two accumulators, and for the most part does not where there is one.  The launch takes as many waves as its tiles need.
+//   Tiles: of 23 sizes (16 to 65536 rows, 1 to 128 experts, widths of 128 to 8192) each tile was timed: what this
+// picks is 1.1, 0.7 and 0.3 percent slower than the best of each on average (FORWARD, DX, DW), and up to 9 percent at the worst; one
+// tile for all would be 6 (256 x 128 or 128 x 128, FORWARD) to 92 percent (128 x 32).
+//   Parts: where the tiles leave multiprocessors without work, up to as many as fill one wave, of two blocks or more.  Adding
+// them takes a launch and their way through L2.  us without and with them: DW of 65536 rows, 4 experts, 128 -> 256: 168 and 30; of
+// 20000 rows, 512 -> 512: 129 and 34; FORWARD of one row, 4096 -> 4096: 17.9 and 10.2; of 64 rows, 4 experts, 2048 -> 1024: 11.3 and
+// 8.9.  Forced where this does not take them: FORWARD of 3000 rows, 1024 -> 1024: 11.7 and 24.6; of 512 rows, 8 experts, 512 -> 512:
+// 6.6 and 9.2; of 300 rows, 4096 -> 4096: 20.5 and 25.1.
 struct Shape {
-  int halves, bn;
+  int halves, bn, splits;
 };
-double tile_cycles(const Shape& sh, double rows, double kbs, bool once, double out_rate) {
-  const double m = sh.halves * kBM;
-  double block = (m + rows) * 128 / 36;
+constexpr double kOutRate = 24;
+double tile_cycles(const Shape& sh, double rows, double kbs, bool once, int bytes, double tiles) {
+  const double m = sh.halves * kBM, share = kSms / (tiles < kSms ? tiles : kSms);
+  const auto rate = [&](double all) { return all * share < 44 ? all * share : 44; };
+  double block = (m + rows) * 128 / rate(36);
   if (m * rows / 64 > block) block = m * rows / 64;
-  const double far = sh.halves == 2 ? 19 : 16;
-  if (once && m * 128 / far > block) block = m * 128 / far;
-  const double in = kbs * block, out = m * rows * 2 / out_rate;
-  return 400 + (sh.halves * sh.bn > 256 ? in + 0.6 * out : in > out ? in : out);
+  if (once && m * 128 / rate(26) > block) block = m * 128 / rate(26);
+  const double in = kbs * block, out = m * rows * bytes / kOutRate;
+  return 1000 + (sh.halves * sh.bn > 256 ? in + 0.8 * out : in > out ? in : out);
+}
+// The least of a launch's cost over tiles and parts of K: cost(shape), which knows its splits.
+template <typename Tiles, typename Cost>
+Shape least(double kbs, double values, const Tiles& tiles, const Cost& cost) {
+  constexpr Shape shapes[] = {{1, 32, 1}, {1, 64, 1}, {1, 128, 1}, {1, 256, 1}, {2, 128, 1}, {2, 256, 1}};
+  Shape best = shapes[0];
+  double lowest = 1e300;
+  for (Shape sh : shapes) {
+    const double room = kSms / tiles(sh), deep = kbs / 2;
+    const int fit = (int)(room < deep ? room : deep), most = fit < 32 ? fit : 32;
+    for (sh.splits = 1;; sh.splits = 2 * sh.splits < most ? 2 * sh.splits : most) {
+      double c = cost(sh);
+      if (sh.splits > 1) c = 1.15 * (c + 4500 + 300 * sh.splits + values * (4 * sh.splits + 2) / (kSms * kOutRate));
+      if (c < lowest) {
+        lowest = c;
+        best = sh;
+      }
+      if (sh.splits >= most) break;
+    }
+  }
+  return best;
 }
 Shape shape_rows(const ProductShape& d, int64_t features, int64_t k) {
-  constexpr Shape shapes[] = {{1, 32}, {1, 64}, {1, 128}, {1, 256}, {2, 128}, {2, 256}};
-  Shape best = shapes[0];
-  double least = 1e300;
   const int64_t used = d.E < d.R ? d.E : d.R;
   const double rows = (double)d.R / used, kbs = (double)((k + kBK - 1) / kBK);
-  for (const Shape& sh : shapes) {
-    const double per_group = rows <= 0.7 * sh.bn ? 1.0 : rows / sh.bn + 0.5, held = rows / per_group;
-    const double tiles = d.m * used * per_group * ((features + sh.halves * kBM - 1) / (sh.halves * kBM));
-    const double waves = tiles <= kSms ? 1.0 : tiles / kSms + 0.4;
-    const double cost = waves * tile_cycles(sh, held, kbs, per_group < 1.5, 30.0) + sh.halves * kBM * held * 2 / 30.0;
-    if (cost < least) {
-      least = cost;
-      best = sh;
-    }
-  }
-  return best;
+  const auto per_group = [&](const Shape& sh) { return rows <= 0.7 * sh.bn ? 1.0 : rows / sh.bn + 0.5; };
+  const auto tiles = [&](const Shape& sh) { return d.m * used * per_group(sh) * ((features + sh.halves * kBM - 1) / (sh.halves * kBM)); };
+  return least(kbs, (double)d.m * d.R * features, tiles, [&](const Shape& sh) {
+    const double held = rows / per_group(sh), all = tiles(sh) * sh.splits, waves = all <= kSms ? 1.0 : all / kSms + 0.5;
+    const int bytes = sh.splits > 1 ? 4 : 2;
+    return waves * tile_cycles(sh, held, kbs / sh.splits, per_group(sh) < 1.5, bytes, all) + sh.halves * kBM * held * bytes / kOutRate;
+  });
 }
 Shape shape_weights(const ProductShape& d) {
-  constexpr Shape shapes[] = {{1, 64}, {1, 128}, {1, 256}, {2, 128}, {2, 256}};
-  Shape best = shapes[0];
-  double least = 1e300;
   const double kbs = (double)d.R / d.E / kBK + 0.5;
-  for (const Shape& sh : shapes) {
-    const int64_t tiles = d.m * d.E * ((d.F + sh.halves * kBM - 1) / (sh.halves * kBM)) * ((d.D + sh.bn - 1) / sh.bn);
-    const double cost = (double)((tiles + kSms - 1) / kSms) * tile_cycles(sh, sh.bn, kbs, false, 18.0) + sh.halves * kBM * sh.bn * 2 / 18.0;
-    if (cost < least) {
-      least = cost;
-      best = sh;
-    }
-  }
-  return best;
+  const auto tiles = [&](const Shape& sh) {
+    return (double)(d.m * d.E * ((d.F + sh.halves * kBM - 1) / (sh.halves * kBM)) * ((d.D + sh.bn - 1) / sh.bn));
+  };
+  return least(kbs, (double)d.m * d.E * d.F * d.D, tiles, [&](const Shape& sh) {
+    if (sh.bn < 64) return 1e300;   // (a box of its operands has 64 columns)
+    const int bytes = sh.splits > 1 ? 4 : 2;
+    return ceil(tiles(sh) * sh.splits / kSms) * tile_cycles(sh, sh.bn, kbs / sh.splits, false, bytes, tiles(sh) * sh.splits) + sh.halves * kBM * sh.bn * bytes / kOutRate;
+  });
 }
 
-// The workspace: copies of operands that TMA cannot take.
+// The workspace: copies of operands that TMA cannot take, and parts of K.
+size_t parts_bytes(const Shape& sh, int64_t values) { return sh.splits > 1 ? round256((size_t)sh.splits * values * 4) : 0; }
 size_t copied_bytes(int64_t groups, int64_t rows, int64_t cols) { return round256((size_t)groups * rows * round8(cols) * 2); }
 
 #define OLSGD_STEP(call)                    \
@@ -667,10 +817,9 @@ cudaError_t weights_copied(ExpertOperand& w, const ProductShape& d, uint8_t* dst
 
 // FORWARD and DX: out rows = weights x rows of `in`.  Workers go by as many a launch as its table holds.
 template <int MODE>
-cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const GatedOperand& in, const int32_t* offsets, void* out, cudaStream_t s) {
+cudaError_t launch_rows(const ProductShape& d, const Shape& sh, const ExpertOperand& w, const GatedOperand& in, const int32_t* offsets, void* out,
+                        float* parts, cudaStream_t s) {
   const int64_t k = MODE == FORWARD ? d.D : d.F, features = MODE == FORWARD ? d.F : d.D;
-  Shape sh = shape_rows(d, features, k);
-  if (getenv("OLSGD_SR")) sscanf(getenv("OLSGD_SR"), "%d,%d", &sh.halves, &sh.bn);
   ProductMaps maps;
   bool ok = make_map_weights(&maps.a[0], w, d, MODE == FORWARD ? kBM : kBK);
   for (int i = 0; i < kBoxes; ++i) {
@@ -689,6 +838,9 @@ cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const Gat
   g.features = (int)features;
   g.out = out;
   g.out_width = store_width(out, features);
+  g.splits = sh.splits;
+  g.parts = sh.splits > 1 ? parts : nullptr;
+  g.part_size = d.m * d.R * features;
   const int64_t most = kMaxStarts / (d.E + 1) < kMaxGroups / d.E ? kMaxStarts / (d.E + 1) : kMaxGroups / d.E;
   for (int64_t at = 0; at < d.m; at += most) {
     g.first_worker = (int)at;
@@ -703,7 +855,7 @@ cudaError_t launch_rows(const ProductShape& d, const ExpertOperand& w, const Gat
   return cudaSuccess;
 }
 
-cudaError_t launch_weights(const ProductBackward& a, bool beside, cudaStream_t s) {
+cudaError_t launch_weights(const ProductBackward& a, const Shape& sh, bool beside, float* parts, cudaStream_t s) {
   ProductMaps maps;
   bool ok = true;
   for (int i = 0; i < kBoxes; ++i) {
@@ -722,12 +874,43 @@ cudaError_t launch_weights(const ProductBackward& a, bool beside, cudaStream_t s
   g.beside = beside;
   g.out = a.dw;
   g.out_width = store_width(a.dw, a.D);
-  Shape sh = shape_weights(a);
-  if (getenv("OLSGD_SW")) sscanf(getenv("OLSGD_SW"), "%d,%d", &sh.halves, &sh.bn);
+  g.splits = sh.splits;
+  g.parts = sh.splits > 1 ? parts : nullptr;
+  g.part_size = a.m * a.E * a.F * a.D;
   return sh.halves == 2 ? (sh.bn == 256 ? launch_variant<DW, 2, 256, 3>(maps, g, s) : launch_variant<DW, 2, 128, 4>(maps, g, s))
          : sh.bn == 256 ? launch_variant<DW, 1, 256, 4>(maps, g, s)
          : sh.bn == 128 ? launch_variant<DW, 1, 128, 6>(maps, g, s)
                         : launch_variant<DW, 1, 64, 7>(maps, g, s);
+}
+
+JoinJob join_rows(const Shape& sh, const float* parts, void* out, int64_t rows, int64_t features) {
+  JoinJob j{};
+  if (sh.splits == 1) return j;
+  j.parts = parts;
+  j.out = out;
+  j.part_size = rows * features;
+  j.splits = sh.splits;
+  j.wide = store_width(out, features) >= 8;
+  j.blocks = (j.part_size + 256 * (j.wide ? 4 : 1) - 1) / (256 * (j.wide ? 4 : 1));
+  return j;
+}
+JoinJob join_weights(const Shape& sh, const float* parts, const ProductBackward& a) {
+  JoinJob j{};
+  if (sh.splits == 1) return j;
+  j.parts = parts;
+  j.out = a.dw;
+  j.part_size = a.m * a.E * a.F * a.D;
+  j.features = a.F;
+  j.cols = a.D;
+  j.splits = sh.splits;
+  j.transposed = 1;
+  j.wide = store_width(a.dw, a.D) >= 8;
+  j.blocks = a.m * a.E * ((a.F + 31) / 32) * ((a.D + 31) / 32);
+  return j;
+}
+cudaError_t launch_join(const JoinJob& x, const JoinJob& y, bool f16, cudaStream_t s) {
+  if (x.blocks + y.blocks == 0) return cudaSuccess;
+  return launch_chained(join_kernel, dim3((unsigned)(x.blocks + y.blocks)), dim3(256), 0, s, JoinArgs{{x, y}, f16});
 }
 
 }  // namespace
@@ -736,20 +919,31 @@ bool product_needs_copies(const ProductShape& d, const GatedOperand& x, const Ex
   return !tma_ready(x, d.R, d.m) || !weights_ready(w, d) || (dy && !tma_ready(*dy, d.R, d.m));
 }
 size_t product_workspace(const ProductShape& d, bool backward, bool copies) {
-  if (!copies) return 0;
-  return copied_bytes(d.m, d.R, d.D) + copied_bytes(d.m * d.E, d.F, d.D) + (backward ? copied_bytes(d.m, d.R, d.F) : 0);
+  size_t bytes = 0;
+  if (copies) bytes += copied_bytes(d.m, d.R, d.D) + copied_bytes(d.m * d.E, d.F, d.D) + (backward ? copied_bytes(d.m, d.R, d.F) : 0);
+  if (!backward) return bytes + parts_bytes(shape_rows(d, d.F, d.D), d.m * d.R * d.F);
+  return bytes + parts_bytes(shape_rows(d, d.D, d.F), d.m * d.R * d.D) + parts_bytes(shape_weights(d), d.m * d.E * d.F * d.D);
 }
 
 cudaError_t launch_product(ProductForward a, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  const Shape sh = shape_rows(a, a.F, a.D);
+  float* parts = reinterpret_cast<float*>(ws);
+  ws += parts_bytes(sh, a.m * a.R * a.F);
   const Wanted x[] = {{&a.x, a.R}};
   OLSGD_STEP(make_ready(x, 1, a.D, a.m, ws, s));
   OLSGD_STEP(weights_copied(a.w, a, ws + copied_bytes(a.m, a.R, a.D), s));
-  return launch_rows<FORWARD>(a, a.w, a.x, a.offsets, a.y, s);
+  OLSGD_STEP(launch_rows<FORWARD>(a, sh, a.w, a.x, a.offsets, a.y, parts, s));
+  return launch_join(join_rows(sh, parts, a.y, a.m * a.R, a.F), JoinJob{}, a.f16, s);
 }
 
 cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  const Shape rows = shape_rows(a, a.D, a.F), weights = shape_weights(a);
+  float* row_parts = reinterpret_cast<float*>(ws);
+  ws += parts_bytes(rows, a.m * a.R * a.D);
+  float* weight_parts = reinterpret_cast<float*>(ws);
+  ws += parts_bytes(weights, a.m * a.E * a.F * a.D);
   // dy for both, the weights for dx, x for the weights' gradient
   const Wanted x[] = {{&a.x, a.R}}, dy[] = {{&a.dy, a.R}};
   if (a.dw) OLSGD_STEP(make_ready(x, 1, a.D, a.m, ws, s));
@@ -760,8 +954,10 @@ cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
   // Neither product reads what the other writes.  The second is launched beside the first: its CTAs may start once all of
   // the first one's have passed their gate (whatever came before has completed then), it takes the multiprocessors as they
   // become free, and at its end it waits for the first.
-  if (a.dx) OLSGD_STEP(launch_rows<DX>(a, a.w, a.dy, a.offsets, a.dx, s));
-  return a.dw ? launch_weights(a, a.dx != nullptr, s) : cudaSuccess;
+  if (a.dx) OLSGD_STEP(launch_rows<DX>(a, rows, a.w, a.dy, a.offsets, a.dx, row_parts, s));
+  if (a.dw) OLSGD_STEP(launch_weights(a, weights, a.dx != nullptr, weight_parts, s));
+  return launch_join(a.dx ? join_rows(rows, row_parts, a.dx, a.m * a.R, a.D) : JoinJob{}, a.dw ? join_weights(weights, weight_parts, a) : JoinJob{},
+                     a.f16, s);
 }
 
 cudaError_t product_status(int* status) {

@@ -333,6 +333,23 @@ def _check_many(x, w, offsets, dy, n):
         assert bool(((got.double() - want).abs() <= size * _product_error(K) + _rounding(want, x.dtype)).all())
 
 
+# few tiles and a long sum: over the features, over a group's rows (one group with nearly all of them, groups with none), or both
+PARTS = [(1, [[5, 0, 3]], 4, 4096, 136), (1, [[3000, 0]], 2, 72, 40), (2, [[2000], [7]], 1, 77, 45), (1, [[9000, 70, 0, 1]], 10, 128, 256),
+         (1, [[1, 0]], 0, 8192, 4096), (1, [[300]], 50, 4095, 1030), (3, [[2, 700], [1, 1], [0, 0]], 9, 130, 2050), (1, [[40000]], 0, 32, 32)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m,sizes,behind,D,F", PARTS)
+def test_product_in_parts(dtype, m, sizes, behind, D, F):
+    g = _gen(D + F + 1)
+    R, E = max(sum(n) for n in sizes) + behind, len(sizes[0])
+    offsets = _offsets(sizes, lead=min(behind, 1))
+    x, w, dy = _randn(g, (m, R, D), dtype), _randn(g, (m, E, F, D), dtype, 0.1), _randn(g, (m, R, F), dtype, 0.1)
+    first = _check_product(x, w, offsets, dy)
+    x2 = torch.cat([x.flip(1), x], dim=1)[:, R:]   # (same values, other strides between workers)
+    assert all(torch.equal(a, b) for a, b in zip(_check_product(x2, w, offsets, dy), first))
+
+
 @pytest.mark.parametrize("pad", [0, 1, 8])
 def test_product_of_strided_operands(pad):
     """Weights as views of rows that hold all of a worker's parameters, rows as slices; with 16-byte pitches and without."""
