@@ -180,27 +180,30 @@ __device__ __forceinline__ void arrive_leader(uint32_t bar) {
 }
 
 // Rows of any pitch to rows of a pitch that TMA takes: up to three operands [m][rows][cols] of
-// 16-bit values, blockIdx.z counting them; a warp per row.  A lane makes one aligned 16-byte piece out
+// 16-bit values, one after another in the grid; a warp per row.  A lane makes one aligned 16-byte piece out
 // of the two that its elements lie in (`begin` and `end` bound the tensor: nothing outside it is
 // read).
 struct PadOperand {
   const uint16_t *begin, *end;
   uint16_t* out;
-  int64_t rows, in_worker, in_row;
+  int64_t rows, workers, in_worker, in_row;   // rows of a worker
+  int64_t cols, first;                        // first: block
 };
 struct PadOperands {
   PadOperand op[3];
-  int64_t cols, pitch;
+  int count;
 };
 __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ PadOperands all) {
   launch_gate();
-  const PadOperand& o = all.op[blockIdx.z];
+  int which = 0;
+  while (which + 1 < all.count && blockIdx.x >= all.op[which + 1].first) ++which;
+  const PadOperand& o = all.op[which];
   const int lane = threadIdx.x & 31;
-  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (r >= o.rows) return;
-  const int cols = (int)all.cols, whole = cols / 8, pieces = (int)(all.pitch / 8);
-  const uint16_t* src = o.begin + (int64_t)blockIdx.y * o.in_worker + r * o.in_row;
-  uint4* dst = reinterpret_cast<uint4*>(o.out + ((int64_t)blockIdx.y * o.rows + r) * all.pitch);
+  const int64_t at = (blockIdx.x - o.first) * 8 + (threadIdx.x >> 5), worker = at / o.rows, r = at - worker * o.rows;
+  if (worker >= o.workers) return;
+  const int cols = (int)o.cols, whole = cols / 8, pieces = (cols + 7) / 8;
+  const uint16_t* src = o.begin + worker * o.in_worker + r * o.in_row;
+  uint4* dst = reinterpret_cast<uint4*>(o.out) + at * pieces;
   const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
   int first_slow = 0;   // pieces from here on are made element by element
   if (src - off >= o.begin && src - off + whole * 8 + 8 <= o.end) {
@@ -263,27 +266,35 @@ struct Wanted {
   GatedOperand* o;
   int64_t rows;
 };
-cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws, cudaStream_t s, bool* any = nullptr) {
+// Copies of a call, made by one launch.
+struct Pads {
   PadOperands all{};
-  all.cols = cols;
-  all.pitch = round8(cols);
-  int n = 0;
-  int64_t most_rows = 0;
+  int64_t blocks = 0;
+  void add(const void* begin, int64_t workers, int64_t worker_stride, int64_t rows, int64_t row_stride, int64_t cols, uint8_t* dst) {
+    const uint16_t* p = static_cast<const uint16_t*>(begin);
+    const uint16_t* end = p + (workers > 1 ? (workers - 1) * worker_stride : 0) + (rows > 1 ? (rows - 1) * row_stride : 0) + cols;
+    all.op[all.count++] = PadOperand{p, end, reinterpret_cast<uint16_t*>(dst), rows, workers, worker_stride, row_stride, cols, blocks};
+    blocks += (rows * workers + 7) / 8;
+  }
+  cudaError_t launch(cudaStream_t s) const {
+    return all.count == 0 ? cudaSuccess : launch_chained(pad_rows_kernel, dim3((unsigned)blocks), dim3(256), 0, s, all);
+  }
+};
+void make_ready(Pads& pads, const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws) {
   for (int i = 0; i < count; ++i) {
     GatedOperand& o = *wanted[i].o;
-    const int64_t rows = wanted[i].rows;
+    const int64_t rows = wanted[i].rows, pitch = round8(cols);
     if (tma_ready(o, rows, m)) continue;
-    const uint16_t* begin = static_cast<const uint16_t*>(o.p);
-    const uint16_t* end = begin + (m > 1 ? (m - 1) * o.worker_stride : 0) + (rows > 1 ? (rows - 1) * o.row_stride : 0) + cols;
-    uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
-    ws += round256((size_t)m * rows * all.pitch * 2);
-    all.op[n++] = PadOperand{begin, end, dst, rows, o.worker_stride, o.row_stride};
-    o = GatedOperand{dst, rows * all.pitch, all.pitch};
-    most_rows = rows > most_rows ? rows : most_rows;
+    pads.add(o.p, m, o.worker_stride, rows, o.row_stride, cols, ws);
+    o = GatedOperand{ws, rows * pitch, pitch};
+    ws += round256((size_t)m * rows * pitch * 2);
   }
-  if (any) *any = n > 0;
-  if (n == 0) return cudaSuccess;
-  return launch_chained(pad_rows_kernel, dim3((unsigned)((most_rows + 7) / 8), (unsigned)m, (unsigned)n), dim3(256), 0, s, all);
+}
+cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws, cudaStream_t s, bool* any = nullptr) {
+  Pads pads;
+  make_ready(pads, wanted, count, cols, m, ws);
+  if (any) *any = pads.all.count > 0;
+  return pads.launch(s);
 }
 
 int store_width(const void* p, int64_t cols) {

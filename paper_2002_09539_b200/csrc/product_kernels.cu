@@ -794,22 +794,18 @@ bool weights_ready(const ExpertOperand& w, const ProductShape& d) {
          (d.m == 1 || w.worker_stride % 8 == 0);
 }
 // Weights that TMA cannot take, copied to padded rows at dst: all experts at once where they lie at one distance, else worker by
-// worker.
-cudaError_t weights_copied(ExpertOperand& w, const ProductShape& d, uint8_t* dst, cudaStream_t s) {
+// worker in launches of their own.
+cudaError_t weights_copied(Pads& pads, ExpertOperand& w, const ProductShape& d, uint8_t* dst, cudaStream_t s) {
   if (weights_ready(w, d)) return cudaSuccess;
-  const int64_t pitch = round8(d.D), bytes = d.E * d.F * pitch * 2;
-  const bool even = d.m == 1 || d.E == 1 || w.worker_stride == d.E * w.expert_stride;
-  for (int64_t i = 0; i < (even ? 1 : d.m); ++i) {
-    const int64_t groups = even ? d.m * d.E : d.E;
-    PadOperands all{};
-    all.cols = d.D;
-    all.pitch = pitch;
-    const uint16_t* begin = static_cast<const uint16_t*>(w.p) + i * w.worker_stride;
-    const int64_t distance = d.E > 1 ? w.expert_stride : w.worker_stride;
-    const uint16_t* end = begin + (groups > 1 ? (groups - 1) * distance : 0) + (d.F > 1 ? (d.F - 1) * w.row_stride : 0) + d.D;
-    all.op[0] = PadOperand{begin, end, reinterpret_cast<uint16_t*>(dst + i * bytes), d.F, distance, w.row_stride};
-    const cudaError_t e = launch_chained(pad_rows_kernel, dim3((unsigned)((d.F + 7) / 8), (unsigned)groups, 1), dim3(256), 0, s, all);
-    if (e != cudaSuccess) return e;
+  const int64_t pitch = round8(d.D);
+  if (d.m == 1 || d.E == 1 || w.worker_stride == d.E * w.expert_stride) {
+    pads.add(w.p, d.m * d.E, d.E > 1 ? w.expert_stride : w.worker_stride, d.F, w.row_stride, d.D, dst);
+  } else {
+    for (int64_t i = 0; i < d.m; ++i) {
+      Pads one;
+      one.add(static_cast<const uint16_t*>(w.p) + i * w.worker_stride, d.E, w.expert_stride, d.F, w.row_stride, d.D, dst + i * d.E * d.F * pitch * 2);
+      OLSGD_STEP(one.launch(s));
+    }
   }
   w = ExpertOperand{dst, d.E * d.F * pitch, d.F * pitch, pitch};
   return cudaSuccess;
@@ -931,8 +927,10 @@ cudaError_t launch_product(ProductForward a, cudaStream_t s) {
   float* parts = reinterpret_cast<float*>(ws);
   ws += parts_bytes(sh, a.m * a.R * a.F);
   const Wanted x[] = {{&a.x, a.R}};
-  OLSGD_STEP(make_ready(x, 1, a.D, a.m, ws, s));
-  OLSGD_STEP(weights_copied(a.w, a, ws + copied_bytes(a.m, a.R, a.D), s));
+  Pads pads;
+  make_ready(pads, x, 1, a.D, a.m, ws);
+  OLSGD_STEP(weights_copied(pads, a.w, a, ws + copied_bytes(a.m, a.R, a.D), s));
+  OLSGD_STEP(pads.launch(s));
   OLSGD_STEP(launch_rows<FORWARD>(a, sh, a.w, a.x, a.offsets, a.y, parts, s));
   return launch_join(join_rows(sh, parts, a.y, a.m * a.R, a.F), JoinJob{}, a.f16, s);
 }
@@ -946,11 +944,13 @@ cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
   ws += parts_bytes(weights, a.m * a.E * a.F * a.D);
   // dy for both, the weights for dx, x for the weights' gradient
   const Wanted x[] = {{&a.x, a.R}}, dy[] = {{&a.dy, a.R}};
-  if (a.dw) OLSGD_STEP(make_ready(x, 1, a.D, a.m, ws, s));
+  Pads pads;
+  if (a.dw) make_ready(pads, x, 1, a.D, a.m, ws);
   ws += copied_bytes(a.m, a.R, a.D);
-  if (a.dx) OLSGD_STEP(weights_copied(a.w, a, ws, s));
+  if (a.dx) OLSGD_STEP(weights_copied(pads, a.w, a, ws, s));
   ws += copied_bytes(a.m * a.E, a.F, a.D);
-  OLSGD_STEP(make_ready(dy, 1, a.F, a.m, ws, s));
+  make_ready(pads, dy, 1, a.F, a.m, ws);
+  OLSGD_STEP(pads.launch(s));
   // Neither product reads what the other writes.  The second is launched beside the first: its CTAs may start once all of
   // the first one's have passed their gate (whatever came before has completed then), it takes the multiprocessors as they
   // become free, and at its end it waits for the first.
