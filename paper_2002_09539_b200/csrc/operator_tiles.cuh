@@ -187,7 +187,7 @@ struct PadOperand {
   const uint16_t *begin, *end;
   uint16_t* out;
   int64_t rows, workers, in_worker, in_row;   // rows of a worker
-  int64_t cols, first;                        // first: block
+  int64_t cols, pitch, first;                 // pitch of the copies, zeros behind cols; first: block
 };
 struct PadOperands {
   PadOperand op[3];
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const __grid_constant__ P
   const int lane = threadIdx.x & 31;
   const int64_t at = (blockIdx.x - o.first) * 8 + (threadIdx.x >> 5), worker = at / o.rows, r = at - worker * o.rows;
   if (worker >= o.workers) return;
-  const int cols = (int)o.cols, whole = cols / 8, pieces = (cols + 7) / 8;
+  const int cols = (int)o.cols, whole = cols / 8, pieces = (int)(o.pitch / 8);
   const uint16_t* src = o.begin + worker * o.in_worker + r * o.in_row;
   uint4* dst = reinterpret_cast<uint4*>(o.out) + at * pieces;
   const int off = (int)((reinterpret_cast<uintptr_t>(src) & 15) / 2);
@@ -270,29 +270,30 @@ struct Wanted {
 struct Pads {
   PadOperands all{};
   int64_t blocks = 0;
-  void add(const void* begin, int64_t workers, int64_t worker_stride, int64_t rows, int64_t row_stride, int64_t cols, uint8_t* dst) {
+  void add(const void* begin, int64_t workers, int64_t worker_stride, int64_t rows, int64_t row_stride, int64_t cols, int64_t pitch,
+           uint8_t* dst) {
     const uint16_t* p = static_cast<const uint16_t*>(begin);
     const uint16_t* end = p + (workers > 1 ? (workers - 1) * worker_stride : 0) + (rows > 1 ? (rows - 1) * row_stride : 0) + cols;
-    all.op[all.count++] = PadOperand{p, end, reinterpret_cast<uint16_t*>(dst), rows, workers, worker_stride, row_stride, cols, blocks};
+    all.op[all.count++] = PadOperand{p, end, reinterpret_cast<uint16_t*>(dst), rows, workers, worker_stride, row_stride, cols, pitch, blocks};
     blocks += (rows * workers + 7) / 8;
   }
   cudaError_t launch(cudaStream_t s) const {
     return all.count == 0 ? cudaSuccess : launch_chained(pad_rows_kernel, dim3((unsigned)blocks), dim3(256), 0, s, all);
   }
 };
-void make_ready(Pads& pads, const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws) {
+void make_ready(Pads& pads, const Wanted* wanted, int count, int64_t cols, int64_t pitch, int64_t m, uint8_t* ws) {
   for (int i = 0; i < count; ++i) {
     GatedOperand& o = *wanted[i].o;
-    const int64_t rows = wanted[i].rows, pitch = round8(cols);
+    const int64_t rows = wanted[i].rows;
     if (tma_ready(o, rows, m)) continue;
-    pads.add(o.p, m, o.worker_stride, rows, o.row_stride, cols, ws);
+    pads.add(o.p, m, o.worker_stride, rows, o.row_stride, cols, pitch, ws);
     o = GatedOperand{ws, rows * pitch, pitch};
     ws += round256((size_t)m * rows * pitch * 2);
   }
 }
 cudaError_t make_ready(const Wanted* wanted, int count, int64_t cols, int64_t m, uint8_t* ws, cudaStream_t s, bool* any = nullptr) {
   Pads pads;
-  make_ready(pads, wanted, count, cols, m, ws);
+  make_ready(pads, wanted, count, cols, round8(cols), m, ws);
   if (any) *any = pads.all.count > 0;
   return pads.launch(s);
 }

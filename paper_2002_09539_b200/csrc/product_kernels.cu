@@ -38,10 +38,11 @@ constexpr int kMaxStarts = 2 * kMaxGroups;
 __device__ int g_product_status;     // a bounded wait gave up (olsgd_operators_join)
 
 // Rows come in boxes of 16, 32, 64, 128 and 256, one of each at most (a TMA instruction takes some 200 cycles however
-// small its box is).  DW: boxes of 16, 32 and 64 rows.
-constexpr int kBoxes = 5;
+// small its box is).  DW: boxes of 16, 32 and 64 rows by 64 columns; or, of operands whose rows are made of whole panels of 64
+// columns, one of 64 rows by all the panels of the tile (rows behind the group's reach no MMA, or are zeroed).
+constexpr int kBoxes = 5, kPanels = 3;
 struct alignas(64) ProductMaps {
-  CUtensorMap a[kBoxes], b[kBoxes];   // FORWARD, DX: a[0] are the weights
+  CUtensorMap a[kBoxes], b[kBoxes];   // FORWARD, DX: a[0] are the weights; DW: [kPanels] the operand by panels
 };
 struct ProductArgs {
   int num_kb, k_extent;       // FORWARD, DX: K in blocks of 64, and in elements
@@ -49,6 +50,7 @@ struct ProductArgs {
   int features, cols;         // rows of A in all; DW: columns of the output
   int R, E, m, first_worker;  // rows and experts of a worker; workers of this launch
   int f16;
+  int a_panels, b_panels;     // DW: the operand goes by panels
   int beside;                 // runs beside the kernel ahead of it: see launch_product_backward
   int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
   const int32_t* offsets;     // [workers][E + 1]
@@ -356,16 +358,21 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         if (MODE == DW) {
           const int n0 = u.col * BN, left = u.n - k0;
           const int rows = left >= kBK ? kBK : (left + kSmallBox - 1) / kSmallBox * kSmallBox;   // (some of them not the group's)
-          mbar_expect_tx(bar, (uint32_t)((na + nb) * rows * 128));
-          int at = 0;
+          // (what lies outside the tensor, as zeros, counts in a box)
+          mbar_expect_tx(bar, (g.a_panels ? kABytes : (uint32_t)(na * rows * 128)) + (g.b_panels ? kBBytes : (uint32_t)(nb * rows * 128)));
+          if (g.a_panels) tma_load_4d(a_dst, &maps.a[kPanels], bar, 0, u.row0 + k0, m0 / 64, u.worker);
+          if (g.b_panels) tma_load_4d(b_dst, &maps.b[kPanels], bar, 0, u.row0 + k0, n0 / 64, u.worker);
+          if (!g.a_panels || !g.b_panels) {
+            int at = 0;
 #pragma unroll
-          for (int i = 2; i >= 0; --i)
-            if (rows & (kSmallBox << i)) {
-              const int row = u.row0 + k0 + at;
-              for (int j = 0; j < na; ++j) tma_load_3d(a_dst + j * 8192 + at * 128, &maps.a[i], bar, m0 + 64 * j, row, u.worker);
-              for (int j = 0; j < nb; ++j) tma_load_3d(b_dst + j * 8192 + at * 128, &maps.b[i], bar, n0 + 64 * j, row, u.worker);
-              at += kSmallBox << i;
-            }
+            for (int i = 2; i >= 0; --i)
+              if (rows & (kSmallBox << i)) {
+                const int row = u.row0 + k0 + at;
+                for (int j = 0; j < na && !g.a_panels; ++j) tma_load_3d(a_dst + j * 8192 + at * 128, &maps.a[i], bar, m0 + 64 * j, row, u.worker);
+                for (int j = 0; j < nb && !g.b_panels; ++j) tma_load_3d(b_dst + j * 8192 + at * 128, &maps.b[i], bar, n0 + 64 * j, row, u.worker);
+                at += kSmallBox << i;
+              }
+          }
         } else {
           mbar_expect_tx(bar, (uint32_t)(na * (A_MN ? 8192 : (int)kHalfBytes) + held * 128));
           for (int j = 0; j < na; ++j) {
@@ -767,7 +774,9 @@ Shape shape_weights(const ProductShape& d) {
 
 // The workspace: copies of operands that TMA cannot take, and parts of K.
 size_t parts_bytes(const Shape& sh, int64_t values) { return sh.splits > 1 ? round256((size_t)sh.splits * values * 4) : 0; }
-size_t copied_bytes(int64_t groups, int64_t rows, int64_t cols) { return round256((size_t)groups * rows * round8(cols) * 2); }
+size_t copied_bytes(int64_t groups, int64_t rows, int64_t pitch) { return round256((size_t)groups * rows * pitch * 2); }
+// Of rows for a backward call: whole panels.
+constexpr int64_t panels64(int64_t cols) { return (cols + 63) / 64 * 64; }
 
 #define OLSGD_STEP(call)                    \
   do {                                      \
@@ -799,11 +808,11 @@ cudaError_t weights_copied(Pads& pads, ExpertOperand& w, const ProductShape& d, 
   if (weights_ready(w, d)) return cudaSuccess;
   const int64_t pitch = round8(d.D);
   if (d.m == 1 || d.E == 1 || w.worker_stride == d.E * w.expert_stride) {
-    pads.add(w.p, d.m * d.E, d.E > 1 ? w.expert_stride : w.worker_stride, d.F, w.row_stride, d.D, dst);
+    pads.add(w.p, d.m * d.E, d.E > 1 ? w.expert_stride : w.worker_stride, d.F, w.row_stride, d.D, pitch, dst);
   } else {
     for (int64_t i = 0; i < d.m; ++i) {
       Pads one;
-      one.add(static_cast<const uint16_t*>(w.p) + i * w.worker_stride, d.E, w.expert_stride, d.F, w.row_stride, d.D, dst + i * d.E * d.F * pitch * 2);
+      one.add(static_cast<const uint16_t*>(w.p) + i * w.worker_stride, d.E, w.expert_stride, d.F, w.row_stride, d.D, pitch, dst + i * d.E * d.F * pitch * 2);
       OLSGD_STEP(one.launch(s));
     }
   }
@@ -851,15 +860,34 @@ cudaError_t launch_rows(const ProductShape& d, const Shape& sh, const ExpertOper
   return cudaSuccess;
 }
 
-cudaError_t launch_weights(const ProductBackward& a, const Shape& sh, bool beside, float* parts, cudaStream_t s) {
+// [m][rows][cols] 16-bit by panels of 64 columns: boxes of 64 rows by `panels` panels.
+bool make_map_panels(CUtensorMap* map, const GatedOperand& o, int64_t cols, int64_t rows, int64_t m, int panels, bool f16) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const int64_t row = rows > 1 ? o.row_stride : cols, worker = m > 1 ? o.worker_stride : rows * row;
+  cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64), (cuuint64_t)m};
+  cuuint64_t strides[3] = {(cuuint64_t)row * 2, 128, (cuuint64_t)worker * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)kBK, (cuuint32_t)panels, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(o.p), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+         CUDA_SUCCESS;
+}
+
+// x_width, dy_width: columns of their rows in memory (of copies, with the zeros behind).
+cudaError_t launch_weights(const ProductBackward& a, int64_t x_width, int64_t dy_width, const Shape& sh, bool beside, float* parts, cudaStream_t s) {
   ProductMaps maps;
   bool ok = true;
   for (int i = 0; i < kBoxes; ++i) {
     const int rows = i < 2 ? kSmallBox << i : kBK;
     ok = ok && make_map16(&maps.a[i], a.dy, a.F, a.R, a.m, rows, a.f16) && make_map16(&maps.b[i], a.x, a.D, a.R, a.m, rows, a.f16);
   }
-  if (!ok) return cudaErrorInvalidValue;
   ProductArgs g{};
+  g.a_panels = dy_width % 64 == 0;
+  g.b_panels = x_width % 64 == 0;
+  if (g.a_panels) ok = ok && make_map_panels(&maps.a[kPanels], a.dy, dy_width, a.R, a.m, sh.halves * kBM / 64, a.f16);
+  if (g.b_panels) ok = ok && make_map_panels(&maps.b[kPanels], a.x, x_width, a.R, a.m, sh.bn / 64, a.f16);
+  if (!ok) return cudaErrorInvalidValue;
   g.R = (int)a.R;
   g.E = (int)a.E;
   g.m = (int)a.m;
@@ -916,7 +944,8 @@ bool product_needs_copies(const ProductShape& d, const GatedOperand& x, const Ex
 }
 size_t product_workspace(const ProductShape& d, bool backward, bool copies) {
   size_t bytes = 0;
-  if (copies) bytes += copied_bytes(d.m, d.R, d.D) + copied_bytes(d.m * d.E, d.F, d.D) + (backward ? copied_bytes(d.m, d.R, d.F) : 0);
+  if (copies) bytes += copied_bytes(d.m, d.R, backward ? panels64(d.D) : round8(d.D)) + copied_bytes(d.m * d.E, d.F, round8(d.D));
+  if (copies && backward) bytes += copied_bytes(d.m, d.R, panels64(d.F));
   if (!backward) return bytes + parts_bytes(shape_rows(d, d.F, d.D), d.m * d.R * d.F);
   return bytes + parts_bytes(shape_rows(d, d.D, d.F), d.m * d.R * d.D) + parts_bytes(shape_weights(d), d.m * d.E * d.F * d.D);
 }
@@ -928,8 +957,8 @@ cudaError_t launch_product(ProductForward a, cudaStream_t s) {
   ws += parts_bytes(sh, a.m * a.R * a.F);
   const Wanted x[] = {{&a.x, a.R}};
   Pads pads;
-  make_ready(pads, x, 1, a.D, a.m, ws);
-  OLSGD_STEP(weights_copied(pads, a.w, a, ws + copied_bytes(a.m, a.R, a.D), s));
+  make_ready(pads, x, 1, a.D, round8(a.D), a.m, ws);
+  OLSGD_STEP(weights_copied(pads, a.w, a, ws + copied_bytes(a.m, a.R, round8(a.D)), s));
   OLSGD_STEP(pads.launch(s));
   OLSGD_STEP(launch_rows<FORWARD>(a, sh, a.w, a.x, a.offsets, a.y, parts, s));
   return launch_join(join_rows(sh, parts, a.y, a.m * a.R, a.F), JoinJob{}, a.f16, s);
@@ -945,17 +974,18 @@ cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
   // dy for both, the weights for dx, x for the weights' gradient
   const Wanted x[] = {{&a.x, a.R}}, dy[] = {{&a.dy, a.R}};
   Pads pads;
-  if (a.dw) make_ready(pads, x, 1, a.D, a.m, ws);
-  ws += copied_bytes(a.m, a.R, a.D);
+  const int64_t x_width = tma_ready(a.x, a.R, a.m) ? a.D : panels64(a.D), dy_width = tma_ready(a.dy, a.R, a.m) ? a.F : panels64(a.F);
+  if (a.dw) make_ready(pads, x, 1, a.D, x_width, a.m, ws);
+  ws += copied_bytes(a.m, a.R, panels64(a.D));
   if (a.dx) OLSGD_STEP(weights_copied(pads, a.w, a, ws, s));
-  ws += copied_bytes(a.m * a.E, a.F, a.D);
-  make_ready(pads, dy, 1, a.F, a.m, ws);
+  ws += copied_bytes(a.m * a.E, a.F, round8(a.D));
+  make_ready(pads, dy, 1, a.F, dy_width, a.m, ws);
   OLSGD_STEP(pads.launch(s));
   // Neither product reads what the other writes.  The second is launched beside the first: its CTAs may start once all of
   // the first one's have passed their gate (whatever came before has completed then), it takes the multiprocessors as they
   // become free, and at its end it waits for the first.
   if (a.dx) OLSGD_STEP(launch_rows<DX>(a, rows, a.w, a.dy, a.offsets, a.dx, row_parts, s));
-  if (a.dw) OLSGD_STEP(launch_weights(a, weights, a.dx != nullptr, weight_parts, s));
+  if (a.dw) OLSGD_STEP(launch_weights(a, x_width, dy_width, weights, a.dx != nullptr, weight_parts, s));
   return launch_join(a.dx ? join_rows(rows, row_parts, a.dx, a.m * a.R, a.D) : JoinJob{}, a.dw ? join_weights(weights, weight_parts, a) : JoinJob{},
                      a.f16, s);
 }
