@@ -284,6 +284,19 @@ __global__ void __launch_bounds__(kRouteThreads, 1) place_kernel(const RouteKern
   launch_gate();
   const int E = a.E, tiles = gridDim.x;
   const int64_t worker = blockIdx.y;
+  const int64_t slots = (int64_t)a.T * a.k, per_tile = (int64_t)kRouteWarps * a.per_warp * a.k;
+  const int64_t first = blockIdx.x * per_tile + threadIdx.x, end = min(slots, (blockIdx.x + 1) * per_tile);
+  int32_t *places = a.places + worker * slots, *tokens = a.tokens + worker * slots;
+  const int32_t* ids = a.ids + worker * slots;
+  // the first slots are on their way while the counts are added up
+  constexpr int kAhead = 2;
+  int ids_ahead[kAhead], ranks_ahead[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int64_t s = first + u * kRouteThreads;
+    ids_ahead[u] = s < end ? ids[s] : -1;
+    ranks_ahead[u] = s < end ? places[s] : 0;
+  }
   // threads (part, expert): every part adds up its share of the tiles
   const int parts = kRouteThreads / E, part = threadIdx.x / E, e = threadIdx.x - part * E;
   int total = 0, before = 0;
@@ -315,18 +328,15 @@ __global__ void __launch_bounds__(kRouteThreads, 1) place_kernel(const RouteKern
   const int all = warp_sums[31];
   if (blockIdx.x == 0 && threadIdx.x == 0) a.offsets[worker * (E + 1) + E] = all;
   __syncthreads();
-  const int64_t slots = (int64_t)a.T * a.k, per_tile = (int64_t)kRouteWarps * a.per_warp * a.k;
-  const int64_t end = min(slots, (blockIdx.x + 1) * per_tile);
-  int32_t *places = a.places + worker * slots, *tokens = a.tokens + worker * slots;
-  const int32_t* ids = a.ids + worker * slots;
-  for (int64_t s = blockIdx.x * per_tile + threadIdx.x; s < end; s += kRouteThreads) {
-    const int id = ids[s];
-    if (id >= 0) {
-      const int place = places[s] + befores[id];
-      places[s] = place;
-      tokens[place] = (int32_t)(s / a.k);
-    }
-  }
+  const auto put = [&](int64_t s, int id, int rank) {
+    if (id < 0) return;
+    const int place = rank + befores[id];
+    places[s] = place;
+    tokens[place] = (int32_t)((uint32_t)s / (uint32_t)a.k);
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) put(first + u * kRouteThreads, ids_ahead[u], ranks_ahead[u]);
+  for (int64_t s = first + kAhead * kRouteThreads; s < end; s += kRouteThreads) put(s, ids[s], places[s]);
   for (int64_t r = all + (int64_t)blockIdx.x * kRouteThreads + threadIdx.x; r < slots; r += (int64_t)tiles * kRouteThreads) tokens[r] = -1;
 }
 
@@ -420,16 +430,17 @@ int64_t row_pieces(int64_t D, bool shifted) {
 
 // Thread: 16 bytes of a token's row.  U: rows on their way at a time.
 template <typename T, bool SHIFTED, int U>
-__global__ void __launch_bounds__(256, SHIFTED || U > 2 ? 4 : 6) combine_kernel(const CombineArgs a, int64_t pieces) {
+__global__ void __launch_bounds__(256, SHIFTED || U > 2 ? 4 : 6) combine_kernel(const CombineArgs a, int64_t pieces, bool narrow) {
   constexpr int V = Elem<T>::kVec;
   launch_gate();
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t token = at / pieces;
+  // (narrow: the launch's threads fit 32 bits; a division of 64 takes a hundred instructions)
+  const int64_t token = narrow ? (uint32_t)at / (uint32_t)pieces : at / pieces;
   if (token >= a.m * a.T) return;
   T* y = static_cast<T*>(a.y) + token * a.D;
   const int64_t j = (at - token * pieces) * V - (SHIFTED ? row_shift(y) : 0);
   if (SHIFTED && j >= a.D) return;
-  const int64_t worker = token / a.T;
+  const int64_t worker = narrow ? (uint32_t)token / (uint32_t)a.T : token / a.T;
   const T* rows = static_cast<const T*>(a.rows) + worker * a.rows_worker;
   const T *begin = static_cast<const T*>(a.rows), *end = static_cast<const T*>(a.rows_end);
   const int32_t* places = a.places + token * a.k;
@@ -487,10 +498,13 @@ __global__ void __launch_bounds__(256, 4) combine_backward_kernel(const CombineG
   }
   if (p >= 0 && p < a.R) {
     const T *dy_all = static_cast<const T*>(a.d_y), *rows_all = static_cast<const T*>(a.rows);
-    const T* dy = dy_all + worker * a.dy_worker + at / a.k * a.dy_row;
+    const T* dy = dy_all + worker * a.dy_worker + (int64_t)((uint32_t)at / (uint32_t)a.k) * a.dy_row;
     const T* row = rows_all + worker * a.rows_worker + p * a.rows_row;
     T* out = d_rows + (int64_t)p * a.D;
     const int shift = SHIFTED ? row_shift(out) : 0;
+    // (not SHIFTED: unused)
+    const ShiftedRow<T> dy_at(dy, -shift, a.D, pieces, dy_all, static_cast<const T*>(a.dy_end));
+    const ShiftedRow<T> row_at(row, -shift, a.D, pieces, rows_all, static_cast<const T*>(a.rows_end));
     f32x2 sum = 0;
     const f32x2 w2 = pack2f(w, w);
     for (int q0 = t0; q0 < pieces; q0 += NT * U) {
@@ -502,8 +516,8 @@ __global__ void __launch_bounds__(256, 4) combine_backward_kernel(const CombineG
         g[u] = x[u] = make_uint4(0, 0, 0, 0);
         if (live) {
           // (the token's gradient is read again by its other slots)
-          g[u] = SHIFTED ? load_shifted<T>(dy, j, a.D, dy_all, static_cast<const T*>(a.dy_end)) : ld16(dy + j);
-          x[u] = load_sixteen<T, SHIFTED>(row, j, a.D, rows_all, static_cast<const T*>(a.rows_end));
+          g[u] = SHIFTED ? dy_at.load(q0 + u * NT) : ld16(dy + j);
+          x[u] = SHIFTED ? row_at.load(q0 + u * NT) : ld16_stream(row + j);
         }
       }
 #pragma unroll
@@ -635,7 +649,7 @@ template <typename T, bool SHIFTED>
 cudaError_t combine_as(const CombineArgs& a, cudaStream_t s) {
   const int64_t pieces = row_pieces<T>(a.D, SHIFTED), threads = a.m * a.T * pieces;
   auto k = a.k == 1 ? combine_kernel<T, SHIFTED, 1> : a.k == 2 ? combine_kernel<T, SHIFTED, 2> : combine_kernel<T, SHIFTED, 4>;
-  return launch_chained(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, pieces);
+  return launch_chained(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, pieces, threads <= 0xffffffffll);
 }
 template <typename T>
 cudaError_t combine_of(CombineArgs a, cudaStream_t s) {

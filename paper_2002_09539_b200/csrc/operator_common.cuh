@@ -261,6 +261,31 @@ __device__ __forceinline__ uint4 load_shifted(const T* row, int64_t j, int64_t n
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// The same for pieces of one row from element j0 on: the distance to the boundary and whether the tensor holds all that is
+// read are found once.
+template <typename T>
+struct ShiftedRow {
+  const T *row, *begin, *end, *base;
+  int64_t j0, n;
+  int off;
+  bool inside;
+  __device__ __forceinline__ ShiftedRow(const T* r, int64_t first, int64_t count, int pieces, const T* b, const T* e)
+      : row(r), begin(b), end(e), j0(first), n(count) {
+    constexpr int V = Elem<T>::kVec;
+    off = row_shift(r + first);
+    base = r + first - off;
+    inside = base >= begin && base + (int64_t)(pieces + 1) * V <= end;
+  }
+  __device__ __forceinline__ uint4 load(int piece) const {
+    constexpr int V = Elem<T>::kVec;
+    if (!inside) return load_shifted<T>(row, j0 + (int64_t)piece * V, n, begin, end);
+    const uint4 a = ld16(base + (int64_t)piece * V);
+    if (off == 0) return a;
+    const uint4 b = ld16(base + (int64_t)(piece + 1) * V);
+    if constexpr (V == 8) return eight_from(a, b, off);
+    else return off == 1 ? make_uint4(a.y, a.z, a.w, b.x) : off == 2 ? make_uint4(a.z, a.w, b.x, b.y) : make_uint4(a.w, b.x, b.y, b.z);
+  }
+};
 // The largest element of a piece; KEEP_NAN: NaN if there is one (else it is passed over).
 template <typename T, bool KEEP_NAN>
 __device__ __forceinline__ float raw_max(const uint4& w) {
