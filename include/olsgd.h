@@ -586,9 +586,9 @@ olsgd_status olsgd_expert_combine_backward(int32_t m, int64_t T, int32_t k, int6
  * worker as that one (d_w of the experts concerned is undefined).
  *   x [m][R][D], w [m][E][F][D]: strides in elements, the last dimension contiguous (w may be a view of
  *   rows that hold all of a worker's parameters);  offsets int32 [m][E + 1];  y [m][R][F] contiguous
- *   E in [1, OLSGD_MAX_EXPERTS], m E <= 65535, m R <= 2^31 - 1, D and F in [1, 2^24]
+ *   E in [1, OLSGD_MAX_EXPERTS], m E <= 65535, m R <= 2^31 - 4096, D and F in [1, 2^24]
  * aligned != 0 promises 16-byte alignment of every operand's base and strides (x and w; d_y too
- * for the backward call): no copies then.                                                        */
+ * for the backward call): no copies then, and room only for sums that go by parts.               */
 olsgd_status olsgd_expert_product_workspace(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F,
                                             int32_t backward, int32_t aligned, size_t* out_bytes);
 olsgd_status olsgd_expert_product(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F, int32_t dtype,

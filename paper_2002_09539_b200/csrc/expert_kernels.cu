@@ -428,30 +428,32 @@ int64_t row_pieces(int64_t D, bool shifted) {
   return shifted ? (D + 2 * V - 2) / V : D / V;
 }
 
-// Thread: 16 bytes of a token's row.  U: rows on their way at a time.
-template <typename T, bool SHIFTED, int U>
-__global__ void __launch_bounds__(256, SHIFTED || U > 2 ? 4 : 6) combine_kernel(const CombineArgs a, int64_t pieces, bool narrow) {
+// Thread: 16 bytes of each of a token's row's P parts.  U: rows on their way at a time.
+template <typename T, bool SHIFTED, int U, int P>
+__global__ void __launch_bounds__(256, U > 2 && P > 1 ? 3 : SHIFTED || U > 2 || P > 1 ? 4 : 6) combine_kernel(const CombineArgs a, int64_t pieces, bool narrow) {
   constexpr int V = Elem<T>::kVec;
   launch_gate();
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, share = pieces / P;
   // (narrow: the launch's threads fit 32 bits; a division of 64 takes a hundred instructions)
-  const int64_t token = narrow ? (uint32_t)at / (uint32_t)pieces : at / pieces;
+  const int64_t token = narrow ? (uint32_t)at / (uint32_t)share : at / share;
   if (token >= a.m * a.T) return;
   T* y = static_cast<T*>(a.y) + token * a.D;
-  const int64_t j = (at - token * pieces) * V - (SHIFTED ? row_shift(y) : 0);
+  const int64_t j = (at - token * share) * V - (SHIFTED ? row_shift(y) : 0), part = share * V;
   if (SHIFTED && j >= a.D) return;
   const int64_t worker = narrow ? (uint32_t)token / (uint32_t)a.T : token / a.T;
   const T* rows = static_cast<const T*>(a.rows) + worker * a.rows_worker;
   const T *begin = static_cast<const T*>(a.rows), *end = static_cast<const T*>(a.rows_end);
   const int32_t* places = a.places + token * a.k;
   const float* weights = a.weights ? a.weights + token * a.k : nullptr;
-  float sum[V];
+  float sum[P][V];
 #pragma unroll
-  for (int e = 0; e < V; ++e) sum[e] = 0.f;
+  for (int q = 0; q < P; ++q)
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[q][e] = 0.f;
   for (int s0 = 0; s0 < a.k; s0 += U) {
     int32_t p[U];
     float w[U];
-    uint4 raw[U];
+    uint4 raw[U][P];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       p[u] = s0 + u < a.k ? places[s0 + u] : -1;
@@ -459,17 +461,24 @@ __global__ void __launch_bounds__(256, SHIFTED || U > 2 ? 4 : 6) combine_kernel(
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (p[u] >= 0 && p[u] < a.R) raw[u] = load_sixteen<T, SHIFTED>(rows + p[u] * a.rows_row, j, a.D, begin, end);
+      if (p[u] >= 0 && p[u] < a.R) {
+#pragma unroll
+        for (int q = 0; q < P; ++q) raw[u][q] = load_sixteen<T, SHIFTED>(rows + p[u] * a.rows_row, j + q * part, a.D, begin, end);
+      }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (p[u] >= 0 && p[u] < a.R) {
-        float v[V];
-        Elem<T>::unpack(raw[u], v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] = fmaf(w[u], v[e], sum[e]);
+        for (int q = 0; q < P; ++q) {
+          float v[V];
+          Elem<T>::unpack(raw[u][q], v);
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[q][e] = fmaf(w[u], v[e], sum[q][e]);
+        }
       }
   }
-  store_floats<T, V>(y, j, a.D, true, sum);
+#pragma unroll
+  for (int q = 0; q < P; ++q) store_floats<T, V>(y, j + q * part, a.D, true, sum[q]);
 }
 
 // NT threads for each slot: the row's gradient, and the weight's.  Slots of a token follow one another, so
@@ -647,8 +656,18 @@ const void* tensor_end(const void* p, int64_t m, int64_t worker, int64_t rows, i
 
 template <typename T, bool SHIFTED>
 cudaError_t combine_as(const CombineArgs& a, cudaStream_t s) {
-  const int64_t pieces = row_pieces<T>(a.D, SHIFTED), threads = a.m * a.T * pieces;
-  auto k = a.k == 1 ? combine_kernel<T, SHIFTED, 1> : a.k == 2 ? combine_kernel<T, SHIFTED, 2> : combine_kernel<T, SHIFTED, 4>;
+  const int64_t pieces = row_pieces<T>(a.D, SHIFTED);
+  // More pieces a thread, hence more bytes on their way, where enough threads remain: two, or four where a token has one row.  us with
+  // one and with these: bf16, 16384 tokens x 2 x 1024: 18 and 17, 8192 x 4 x 1024: 16 and 14; fp32, 2 x 8192 x 4 x 512: 37 and 27,
+  // 8192 x 6 x 1024: 49 and 39.  (Of rows of any alignment, 16 x 333 x 3 x 1021: 15.5 and 18.)
+  const int64_t all = a.m * a.T * pieces;
+  const int share = SHIFTED || all < kSms * 4096 ? 1 : a.k == 1 && pieces % 4 == 0 ? 4 : pieces % 2 == 0 ? 2 : 1;
+  const int64_t threads = all / share;
+  auto k = a.k == 1 ? combine_kernel<T, SHIFTED, 1, 1> : a.k == 2 ? combine_kernel<T, SHIFTED, 2, 1> : combine_kernel<T, SHIFTED, 4, 1>;
+  if constexpr (!SHIFTED) {
+    if (share == 4) k = combine_kernel<T, false, 1, 4>;
+    if (share == 2) k = a.k == 1 ? combine_kernel<T, false, 1, 2> : a.k == 2 ? combine_kernel<T, false, 2, 2> : combine_kernel<T, false, 4, 2>;
+  }
   return launch_chained(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, pieces, threads <= 0xffffffffll);
 }
 template <typename T>

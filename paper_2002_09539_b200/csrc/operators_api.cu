@@ -102,7 +102,8 @@ olsgd_status check_combine(int32_t m, int64_t T, int32_t k, int64_t R, int64_t D
 olsgd_status check_product(int32_t m, int64_t R, int64_t E, int64_t D, int64_t F) {
   OLSGD_REFUSE_IF(E < 1 || E > OLSGD_MAX_EXPERTS, "E must be in [1, %d]", OLSGD_MAX_EXPERTS);
   OLSGD_REFUSE_IF(m < 1 || (int64_t)m * E > 65535, "m must be positive, m E at most 65535");
-  OLSGD_REFUSE_IF(R < 0 || R > kMaxRows / m, "R must not be negative, m R at most 2^31 - 1");
+  // (4095: a tile's end, or the grid's next row, still fits 32 bits)
+  OLSGD_REFUSE_IF(R < 0 || R > (kMaxRows - 4095) / m, "R must not be negative, m R at most 2^31 - 4096");
   OLSGD_REFUSE_IF(D < 1 || D > (1 << 24) || F < 1 || F > (1 << 24), "D and F must be in [1, 2^24]");
   return OLSGD_OK;
 }
