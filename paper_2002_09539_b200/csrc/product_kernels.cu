@@ -76,12 +76,10 @@ struct Table {
   int32_t sums[kThreads / 32];
 };
 
-// Rows [x, y) of a group, whatever the offsets hold.
-__device__ __forceinline__ int2 group_rows(const int32_t* offsets, int group, int E, int R) {
+// A group's two offsets, as they are.
+__device__ __forceinline__ int2 group_offsets(const int32_t* offsets, uint32_t group, uint32_t E) {
   const int32_t* o = offsets + group + group / E;   // (a worker has E + 1 of them)
-  // (past L1: DW may run beside its predecessor)
-  const int a = min(max(__ldcg(o), 0), R);
-  return make_int2(a, min(max(__ldcg(o + 1), a), R));
+  return make_int2(__ldcg(o), __ldcg(o + 1));       // (past L1: DW may run beside its predecessor)
 }
 
 // ------------------------------------------------------------------------------- products
@@ -156,14 +154,18 @@ template <int MODE, int BN>
 struct Walk {
   const ProductArgs& g;
   const Table& tb;
-  uint32_t total;
+  uint32_t total, step;
   int at_group = 0;
-  __device__ __forceinline__ Walk(const ProductArgs& args, const Table& table) : g(args), tb(table) {
+  // DW: the offsets of the next unit's group, on their way while this unit is worked at (each unit would wait for L2 first)
+  int2 ahead;
+  uint32_t ahead_of = ~0u;
+  __device__ __forceinline__ Walk(const ProductArgs& args, const Table& table, uint32_t by) : g(args), tb(table), step(by) {
     total = (MODE == DW ? (uint32_t)(g.m * g.E) * g.m_tiles * g.n_tiles : (uint32_t)tb.first[g.m * g.E] * g.m_tiles) * g.splits;
   }
-  // t: no less than at the call before
+  // t: `step` more than at the call before
   __device__ __forceinline__ Unit at(uint32_t t) {
     Unit u;
+    const uint32_t next = t + step;
     u.split = 0;
     if (g.splits > 1) {
       u.split = t % g.splits;
@@ -177,10 +179,15 @@ struct Walk {
       const uint32_t height = min((uint32_t)kGroup, g.m_tiles - first), j = i - block * group_tiles;
       u.col = j / height;
       u.m = first + j - u.col * height;
-      const int2 r = group_rows(g.offsets, u.group, g.E, g.R);
+      const int2 r = ahead_of == (uint32_t)u.group ? ahead : group_offsets(g.offsets, u.group, g.E);
+      if (next < total) {
+        ahead_of = next / (per * g.splits);
+        ahead = group_offsets(g.offsets, ahead_of, g.E);
+      }
       u.worker = u.group / g.E;
-      u.row0 = r.x;
-      u.n = r.y - r.x;
+      // (whatever the offsets hold)
+      u.row0 = min(max(r.x, 0), g.R);
+      u.n = min(max(r.y, u.row0), g.R) - u.row0;
     } else {
       const int i = t / g.m_tiles;
       while (tb.first[at_group + 1] <= i) ++at_group;
@@ -332,7 +339,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = ctl->tmem_base;
-  Walk<MODE, BN> walk(g, table);
+  Walk<MODE, BN> walk(g, table, step);
   const uint32_t total = walk.total;
   const auto mma_cols = [&](const Unit& u) { return MODE == DW ? BN : (u.n + kSmallBox - 1) / kSmallBox * kSmallBox; };
   // Boxes of A and (DW) of B: none lies wholly outside its tensor.  What stays in their place reaches only parts of the
@@ -409,6 +416,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
       const uint32_t idesc = idesc0 | ((uint32_t)(mma_cols(u) >> 3) << 17);
       const int k_extent = MODE == DW ? u.n : g.k_extent;
       const auto multiply = [&](int kb, uint32_t s, int half, uint32_t acc) {
+        if (MODE == DW && lane != 0) return;
         const uint32_t a_addr = smem_u32(tiles + s * kStageBytes) + half * kHalfBytes, b_addr = smem_u32(tiles + s * kStageBytes) + kABytes;
         const uint64_t a_desc = A_MN ? smem_desc_mn_sw128(a_addr) : smem_desc_k_sw128(a_addr);
         const uint64_t b_desc = B_MN ? smem_desc_mn_sw128(b_addr) : smem_desc_k_sw128(b_addr);
@@ -417,7 +425,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         const int left = k_extent - kb * kBK;   // (what lies behind is zeros, or was not loaded)
 #pragma unroll
         for (int k = 0; k < kBK / kUmmaK; ++k)
-          if (k * kUmmaK < left && (MODE != DW || lane == 0)) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > u.kb || k > 0) ? 1u : 0u);
+          if (k * kUmmaK < left) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > u.kb || k > 0) ? 1u : 0u);
       };
       const auto wait = [&](uint64_t* bar, uint32_t parity) {
         int done = 1;
