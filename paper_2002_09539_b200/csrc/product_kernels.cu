@@ -76,12 +76,6 @@ struct Table {
   int32_t sums[kThreads / 32];
 };
 
-// A group's two offsets, as they are.
-__device__ __forceinline__ int2 group_offsets(const int32_t* offsets, uint32_t group, uint32_t E) {
-  const int32_t* o = offsets + group + group / E;   // (a worker has E + 1 of them)
-  return make_int2(__ldcg(o), __ldcg(o + 1));       // (past L1: DW may run beside its predecessor)
-}
-
 // ------------------------------------------------------------------------------- products
 // By a whole CTA.  Offsets that fall, or leave [0, R], are taken as the largest so far, so that groups never overlap.
 __device__ __forceinline__ void make_table(const ProductArgs& g, Table& tb, int bn) {
@@ -158,37 +152,49 @@ struct Walk {
   int at_group = 0;
   // DW: the offsets of the next unit's group, on their way while this unit is worked at (each unit would wait for L2 first)
   int2 ahead;
-  uint32_t ahead_of = ~0u;
+  uint32_t ahead_group = 0, ahead_worker = 0, ahead_tile = 0;
+  bool has_ahead = false;
   __device__ __forceinline__ Walk(const ProductArgs& args, const Table& table, uint32_t by) : g(args), tb(table), step(by) {
     total = (MODE == DW ? (uint32_t)(g.m * g.E) * g.m_tiles * g.n_tiles : (uint32_t)tb.first[g.m * g.E] * g.m_tiles) * g.splits;
+  }
+  // DW: unit t's group, worker, place in the group, and offsets
+  __device__ __forceinline__ void look(uint32_t t) {
+    const uint32_t per = (uint32_t)g.m_tiles * g.n_tiles * g.splits;
+    ahead_group = t / per;
+    ahead_tile = t - ahead_group * per;
+    ahead_worker = ahead_group / g.E;
+    const int32_t* o = g.offsets + ahead_group + ahead_worker;   // (a worker has E + 1 of them)
+    ahead = make_int2(__ldcg(o), __ldcg(o + 1));                 // (past L1: DW may run beside its predecessor)
   }
   // t: `step` more than at the call before
   __device__ __forceinline__ Unit at(uint32_t t) {
     Unit u;
-    const uint32_t next = t + step;
     u.split = 0;
-    if (g.splits > 1) {
-      u.split = t % g.splits;
-      t /= g.splits;
-    }
     if (MODE == DW) {
-      const uint32_t per = g.m_tiles * g.n_tiles;
-      u.group = t / per;
-      const uint32_t i = t - u.group * per;
+      if (!has_ahead) look(t);
+      u.group = ahead_group;
+      u.worker = ahead_worker;
+      uint32_t i = ahead_tile;
+      if (g.splits > 1) {
+        const uint32_t tile = i / g.splits;
+        u.split = i - tile * g.splits;
+        i = tile;
+      }
+      const int2 r = ahead;
+      has_ahead = t + step < total;
+      if (has_ahead) look(t + step);
       const uint32_t group_tiles = kGroup * g.n_tiles, block = i / group_tiles, first = block * kGroup;
       const uint32_t height = min((uint32_t)kGroup, g.m_tiles - first), j = i - block * group_tiles;
-      u.col = j / height;
+      u.col = height == kGroup ? j / kGroup : j / height;
       u.m = first + j - u.col * height;
-      const int2 r = ahead_of == (uint32_t)u.group ? ahead : group_offsets(g.offsets, u.group, g.E);
-      if (next < total) {
-        ahead_of = next / (per * g.splits);
-        ahead = group_offsets(g.offsets, ahead_of, g.E);
-      }
-      u.worker = u.group / g.E;
       // (whatever the offsets hold)
       u.row0 = min(max(r.x, 0), g.R);
       u.n = min(max(r.y, u.row0), g.R) - u.row0;
     } else {
+      if (g.splits > 1) {
+        u.split = t % g.splits;
+        t /= g.splits;
+      }
       const int i = t / g.m_tiles;
       while (tb.first[at_group + 1] <= i) ++at_group;
       const int worker = at_group / g.E;
@@ -220,6 +226,30 @@ __device__ __forceinline__ void store_rows(const float* v, uint16_t* dst, int64_
     store_half_if(dst + j * pitch, two, live && j < n);
     store_half_if(dst + (j + 1) * pitch, two >> 16, live && j + 1 < n);
   }
+}
+
+// 32 or 64 columns of this lane's row of tensor memory.
+template <int W>
+__device__ __forceinline__ void tmem_ld_wide(uint32_t taddr, float* v) {
+  static_assert(W == 32 || W == 64, "");
+  uint32_t r[W];
+#pragma unroll
+  for (int c = 0; c < W; c += 32) {
+    uint32_t* p = r + c;
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3]), "=r"(p[4]), "=r"(p[5]), "=r"(p[6]), "=r"(p[7]), "=r"(p[8]), "=r"(p[9]), "=r"(p[10]),
+          "=r"(p[11]), "=r"(p[12]), "=r"(p[13]), "=r"(p[14]), "=r"(p[15]), "=r"(p[16]), "=r"(p[17]), "=r"(p[18]), "=r"(p[19]), "=r"(p[20]),
+          "=r"(p[21]), "=r"(p[22]), "=r"(p[23]), "=r"(p[24]), "=r"(p[25]), "=r"(p[26]), "=r"(p[27]), "=r"(p[28]), "=r"(p[29]), "=r"(p[30]),
+          "=r"(p[31])
+        : "r"(taddr + c)
+        : "memory");
+  }
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < W; ++k) v[k] = __uint_as_float(r[k]);
 }
 
 // 16 lanes x (8 BLOCKS) columns of tensor memory, as the fragments of 8 x 8 matrices: of block i, v[4 i] and v[4 i + 1] are
@@ -441,13 +471,14 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
         ok = wait(&ctl->full[i % STAGES], (i / STAGES) & 1);
         const int left = k_extent - kb * kBK;
         if (MODE == DW && ok && left < kBK && left % kSmallBox) {
-          // (rows of 128 bytes, whatever the swizzle does inside them)
-          const int zeros = kSmallBox - left % kSmallBox, boxes = kTileM / 64 + BN / 64;
-          uint8_t* stage = tiles + (i % STAGES) * kStageBytes;
-          for (int p = lane; p < boxes * zeros * 8; p += 32) {
-            const int box = p / (zeros * 8), at = p - box * (zeros * 8);
-            reinterpret_cast<uint4*>(stage + box * 8192 + left * 128)[at] = make_uint4(0, 0, 0, 0);
-          }
+          // (rows of 128 bytes, whatever the swizzle does inside them; up to 120 pieces a box)
+          const int zeros = (kSmallBox - left % kSmallBox) * 8;
+          uint4* row = reinterpret_cast<uint4*>(tiles + (i % STAGES) * kStageBytes + left * 128);
+#pragma unroll
+          for (int box = 0; box < kTileM / 64 + BN / 64; ++box)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (q * 32 + lane < zeros) row[box * 512 + q * 32 + lane] = make_uint4(0, 0, 0, 0);
           fence_async_smem();
           __syncwarp();
         }
@@ -532,25 +563,22 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
               }
               __syncwarp();
             }
-          } else if (MODE == DW) {
+          } else if constexpr (MODE == DW) {
             constexpr int W = kBlockCols;
             Staged<W> out{reinterpret_cast<uint4*>(tiles + STAGES * kStageBytes) + (warp - 2) * 256};
             uint16_t* dst = static_cast<uint16_t*>(g.out) + ((int64_t)u.group * g.features + feature0) * g.cols;
             for (int c0 = side * (BN / 2); c0 < (side + 1) * (BN / 2); c0 += W) {
               const int64_t col = (int64_t)u.col * BN + c0, cols = g.cols - col;
               if (cols <= 0) break;
-#pragma unroll 1
-              for (int q = 0; q < W / 16; q += 2) {
-                float v[16], w[16];
-                if (none) {
+              float v[W];
+              if (none) {
 #pragma unroll
-                  for (int j = 0; j < 16; ++j) v[j] = w[j] = 0.f;
-                } else {
-                  tmem_ld16x2(acc + c0 + q * 16, acc + c0 + q * 16 + 16, v, w);
-                }
-                out.put(lane, q, v, g.f16);
-                out.put(lane, q + 1, w, g.f16);
+                for (int k = 0; k < W; ++k) v[k] = 0.f;
+              } else {
+                tmem_ld_wide<W>(acc + c0, v);
               }
+#pragma unroll
+              for (int q = 0; q < W / 16; ++q) out.put(lane, q, v + 16 * q, g.f16);
               out.flush(lane, dst + col, g.cols, g.features - feature0, cols, g.out_width);
             }
           } else {
