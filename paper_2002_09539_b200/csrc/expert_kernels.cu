@@ -12,8 +12,13 @@
 // warps of a CTA are added up there, those of the CTAs by the placing kernel, each of whose CTAs reads
 // them all: where one CTA holds all tokens of a worker there is one launch.  No order depends on timing.
 //
+// Bound by the instructions of the selection (8 of 128, 2 x 16384 tokens, fp32: 20 us and 7 for the placing, 25 MB); a few
+// tokens by their one CTA's way through its barriers (8 tokens: 6 us).  Gradient: 11 us for 37 MB.
+//
 // Combine: y_t = sum_j w_tj rows[place_tj], in order of j in fp32; its gradient is a product and a dot
-// product for each slot.  Both are bound by reading (and writing) each row once.
+// product for each slot.  Both are bound by reading (and writing) each row once (16384 tokens x 2 x 1024 bf16: 19 us for
+// 101 MB, 5.2 TB/s, and 25 for 168 MB, part of them still in L2); rows of any alignment by the instructions that shift them
+// (16 x 333 x 3 x 1021 fp16: 21 us for 43 MB, 27 for 76).
 #include "operator_common.cuh"
 #include "operators_internal.h"
 
