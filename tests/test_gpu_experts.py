@@ -366,6 +366,60 @@ def test_product_of_strided_operands(pad):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("D,F", [(192, 128), (64, 136), (136, 320)])
+def test_product_of_slices_among_nan(D, F):
+    """Operands inside larger tensors of NaN, rows of whole panels of 64 columns and others: nothing around a slice is used."""
+    g = _gen(D + F)
+    m, E, R, dtype = 2, 3, 151, torch.float16
+    offsets = _offsets([[70, 0, 61], [1, 129, 3]], lead=9)
+
+    def inside(shape, std=1.0):
+        big = torch.full((shape[0], *(n + 16 for n in shape[1:])), math.nan, dtype=dtype, device="cuda")
+        part = big[(slice(None),) + tuple(slice(8, 8 + n) for n in shape[1:])]
+        part.copy_(_randn(g, shape, dtype, std))
+        return part
+    x, w, dy = inside((m, R, D)), inside((m, E, F, D), 0.3), inside((m, R, F))
+    for i, (a, b) in enumerate(((9, 140), (9, 142))):   # rows of no expert
+        x[i, :a], x[i, b:], dy[i, :a], dy[i, b:] = math.nan, math.nan, math.nan, math.nan
+    y, dx, dw = lib.expert_product(x, w, offsets), *lib.expert_product_backward(dy, x, w, offsets)
+    assert bool(y.isfinite().all()) and bool(dx.isfinite().all()) and bool(dw.isfinite().all())
+    x, dy = x.nan_to_num(0.0), dy.nan_to_num(0.0)
+    got = _check_product(x, w.contiguous(), offsets, dy)
+    assert all(torch.equal(a, b) for a, b in zip(got, (y, dx, dw)))
+
+
+def test_product_in_parts_side_by_side_and_replayed():
+    """Sums by parts use a workspace: two streams at once, and a captured call whose inputs change, each get their own."""
+    g = _gen(4)
+    m, R, E, D, F, dtype = 1, 3000, 2, 512, 64, torch.bfloat16
+    offsets = [_offsets([[2100, 900]]), _offsets([[0, 2999]])]
+    x, w, dy = [_randn(g, (m, R, D), dtype) for _ in range(2)], _randn(g, (m, E, F, D), dtype, 0.2), [_randn(g, (m, R, F), dtype) for _ in range(2)]
+
+    def both(i):
+        return (lib.expert_product(x[i], w, offsets[i]), *lib.expert_product_backward(dy[i], x[i], w, offsets[i]))
+    want = [both(0), both(1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got.append(both(i))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for i in range(2) for a, b in zip(got[i], want[i]))
+    graph = torch.cuda.CUDAGraph()
+    kept = [t.clone() for t in (x[0], dy[0], offsets[0])]
+    with torch.cuda.graph(graph):
+        out = both(0)
+    for i in (1, 0, 1):
+        for t, new in zip((x[0], dy[0], offsets[0]), (x[1], dy[1], offsets[1]) if i else kept):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+    lib.operators_join()
+
+
 @pytest.mark.parametrize("D,F", [(64, 128), (70, 50)])
 def test_product_extremes_stay_in_their_rows_and_experts(D, F):
     g = _gen(D)
