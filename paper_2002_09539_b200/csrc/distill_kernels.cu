@@ -26,6 +26,8 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kChunkElems = 256;     // of a warp's turn: eight elements a lane
 constexpr int kWarpRowMax = 1024;    // longest row that stays in a warp's registers
 constexpr int kMaxSplit = 64;
+constexpr int kGradPieces = 4;       // of a thread's turn
+constexpr int64_t kGradCtas = 148 * 16, kKeepBytes = 64 << 20;
 constexpr int kMaxPairs = OLSGD_MAX_TEACHER;
 static_assert(kMaxPairs <= kThreads, "a thread for each pair");
 constexpr int kMaxCluster = 8, kKnownDevices = 8;
@@ -351,10 +353,11 @@ __device__ __forceinline__ void store_pairs(const DistillArgs& a, const PairTabl
   }
 }
 
-// CTA (r, segment): kThreads * U pieces of row r.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_grad_kernel(const DistillArgs a) {
-  constexpr int VEC = Elem<T>::kVec, U = 4;
+// CTA (r, segment): `turns` times kThreads * U pieces of row r, the next on their way while the last leave.  What the pairs cost is
+// paid once a segment, so that these are as long as leave the GPU full.
+template <typename T, bool STREAM>
+__global__ void __launch_bounds__(kThreads, 4) distill_grad_kernel(const DistillArgs a, int turns) {
+  constexpr int VEC = Elem<T>::kVec, U = kGradPieces, kTurn = kThreads * U * VEC;
   __shared__ Sum sh[kWarps];
   __shared__ PairTable table;
   launch_gate();
@@ -365,7 +368,8 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(const DistillArg
   const int shift = row_shift(row);
   const bool aligned = row_shift(out) == shift;
   const float c = a.inv_t * kLog2e;
-  const int begin = (int)blockIdx.y * (kThreads * U) * VEC - shift, j0 = begin + (int)threadIdx.x * VEC;
+  const int begin = (int)blockIdx.y * turns * kTurn - shift, end = min(V, begin + turns * kTurn);
+  int j0 = begin + (int)threadIdx.x * VEC;
   uint4 w[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) w[u] = load_raw<T>(row, j0 + u * kThreads * VEC, V, 0);
@@ -382,21 +386,31 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(const DistillArg
     table.q[threadIdx.x] = p.id < 0 || empty(teacher) ? 0.f : ex2((p.z - base_of(teacher.m)) * c) / teacher.s;
     table.id[threadIdx.x] = p.id;
   }
+  for (; j0 < end; j0 += kTurn) {
+    uint4 next[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int j = j0 + u * kThreads * VEC;
-    if (j >= V) break;
-    float d[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) {
-      float lo, hi;
-      unpack2f(raw_pair<T>(w[u], i), lo, hi);
-      d[2 * i] = g.at(lo, c);
-      d[2 * i + 1] = g.at(hi, c);
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + kTurn + u * kThreads * VEC;
+      if (j < end) next[u] = load_raw<T>(row, j, V, 0);
     }
-    store_floats<T, VEC>(out, j, V, aligned, d);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * kThreads * VEC;
+      if (j >= end) break;
+      float d[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) {
+        float lo, hi;
+        unpack2f(raw_pair<T>(w[u], i), lo, hi);
+        d[2 * i] = g.at(lo, c);
+        d[2 * i + 1] = g.at(hi, c);
+      }
+      store_floats<T, VEC, STREAM>(out, j, V, aligned, d);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = next[u];
   }
-  if (!g.zero) store_pairs<T>(a, table, p, g, begin, begin + kThreads * U * VEC, c, out);
+  if (!g.zero) store_pairs<T>(a, table, p, g, begin, end, c, out);
 }
 
 // -------------------------------------------------------- loss and gradient from one read
@@ -771,8 +785,12 @@ cudaError_t warp_rows(const DistillArgs& a, cudaStream_t s) {
 template <typename T>
 cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax) return warp_rows<T, false, true>(a, s);
-  const int64_t pieces = (a.V + (rows_aligned<T>(a) ? 1 : 2) * (Elem<T>::kVec - 1)) / Elem<T>::kVec, per = kThreads * 4;
-  return launch_chained(distill_grad_kernel<T>, dim3((unsigned)a.rows, (unsigned)((pieces + per - 1) / per)), dim3(kThreads), 0, s, a);
+  const int64_t pieces = (a.V + (rows_aligned<T>(a) ? 1 : 2) * (Elem<T>::kVec - 1)) / Elem<T>::kVec, per = kThreads * kGradPieces;
+  const int64_t whole = (pieces + per - 1) / per, want = (kGradCtas + a.rows - 1) / a.rows;   // turns of a row; segments
+  const int64_t turns = want >= whole ? 1 : (whole + want - 1) / want;
+  const bool large = a.rows * a.V * (int64_t)sizeof(T) > kKeepBytes;   // a gradient that L2 would not hold anyway
+  return launch_chained(large ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>,
+                        dim3((unsigned)a.rows, (unsigned)((whole + turns - 1) / turns)), dim3(kThreads), 0, s, a, (int)turns);
 }
 
 // As many clusters as the GPU holds at once.
