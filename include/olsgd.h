@@ -622,7 +622,8 @@ olsgd_status olsgd_expert_product_backward(int32_t m, int64_t R, int64_t E, int6
  *   loss    float [rows];  stats  float [rows][2]: max x, and log sum exp((x - max x) / temperature)
  *   d_loss  float [rows] or NULL: with it d_logits [rows][V], of type dtype, rows d_row_stride >= V apart, takes
  *           d_loss (p - q) / temperature (q: 0 but at the pairs) from the same read of the logits, where a
- *           row fits eight multiprocessors' registers.  A row whose d_loss is 0 has a gradient of 0.
+ *           row fits a multiprocessor's registers and the pairs are few.  A row whose d_loss is 0 has a
+ *           gradient of 0.
  * d_logits may be the logits themselves (with the same stride).                                   */
 #define OLSGD_MAX_TEACHER 256
 olsgd_status olsgd_distill_workspace(int32_t dtype, int64_t rows, int64_t V, int32_t gradient,

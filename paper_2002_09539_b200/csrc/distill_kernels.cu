@@ -6,10 +6,9 @@
 //
 // Bound by the logits' way in and, for a gradient, its way out (4096 x 32768 bf16 with gradient: 118 us, 537 MB, 4.6 TB/s; loss
 // of 1021 x 50021 fp32: 39 us, 204 MB, 5.2 TB/s).  Where the rows' weights are known when
-// the loss is formed, both come from one read: a row lies in the registers of a cluster of up to
-// eight CTAs as exp(x - the warp's own max), 32 values a thread, until the whole row's sum is known.
-// Longer rows, losses alone and gradients that are asked for later take one pass each.  Rows of up to
-// 1024 logits belong to a warp.
+// the loss is formed, both come from one read: a row lies in the registers of a CTA as exp(x - the warp's own max), 32 or 40
+// values a thread, until the whole row's sum is known.  Longer rows, losses alone and gradients that are asked for later take
+// one pass each (4096 x 32768 bf16: 57 and 91 us).  Rows of up to 1024 logits belong to a warp.
 //
 // A gradient at the pairs' tokens is formed apart from the others, from the logit and the sum of the q of
 // all pairs with that token, and stored behind them, so that it is rounded once.
@@ -30,7 +29,6 @@ constexpr int kGradPieces = 4;       // of a thread's turn
 constexpr int64_t kGradCtas = 148 * 16, kKeepBytes = 64 << 20;
 constexpr int kMaxPairs = OLSGD_MAX_TEACHER;
 static_assert(kMaxPairs <= kThreads, "a thread for each pair");
-constexpr int kMaxCluster = 8, kKnownDevices = 8;
 
 struct Sum {
   float m, s;   // maximum; sum of exp((x - m) / tau)
@@ -414,29 +412,18 @@ __global__ void __launch_bounds__(kThreads, 4) distill_grad_kernel(const Distill
 }
 
 // -------------------------------------------------------- loss and gradient from one read
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Clusters that stay, a row at a time; each of its CTAs holds a part of the row, 32 elements a thread, counted from the
-// 16-byte boundary at or before the row.  The warps have the row's elements: each takes its own maximum and sum and sends
-// them to every CTA of the cluster, where every warp joins them all behind the row's one barrier.
+// CTAs that stay, a row at a time, 32 or 40 elements a thread, counted from the 16-byte boundary at or before the row.  The warps
+// have the row's elements: each takes its own maximum and sum, and joins them all behind the row's one barrier.
 // One more warp brings the rows in (bulk copies of the whole 16-byte pieces, two buffers), has the pairs and writes
 // the loss; it stores the gradients at the pairs' tokens a row later, when the others' stores of their row are done.
-// 4096 x 32768 bf16, 32 pairs: 200 us with one row a cluster and all in all warps, 115 with one warp for the pairs and one
-// barrier of the cluster a row.
+// 4096 x 32768 bf16, 32 pairs: 200 us with a row's loss and gradient behind one another in all warps, 117 like this.
 constexpr int kStages = 2;
 constexpr int kMostWarps = 31;
 struct StreamShared {
   uint64_t full[kStages];                  // copies
-  Sum stats[2][kMaxCluster * kMostWarps];  // of the cluster's warps, of rows in turn
+  Sum stats[2][kMostWarps];                // of the warps, of rows in turn
   int teacher[2];                          // whether the row has one
-  uint32_t seen[kMostWarps * 40];          // a bit for each element of the part
+  uint32_t seen[kMostWarps * 40];          // a bit for each element
   int32_t id[kMaxPairs];                   // where a token occurs twice
   float q[kMaxPairs];
 };
@@ -469,33 +456,26 @@ __device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity) {
     }
   }
 }
-// v to this place of the cluster's CTA `rank`.
-__device__ __forceinline__ void tell(void* p, uint32_t rank, const Sum& v) {
-  uint32_t at;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(shared_address(p)), "r"(rank));
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.m), "f"(v.s) : "memory");
-}
 __device__ __forceinline__ float redux_max(float v) {
   asm volatile("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v));
   return v;
 }
 
 // blockDim.x: 32 threads for every warp with elements, and 32.  KP: pairs of a lane of the last warp.
-template <typename T, bool CLUSTER, int KP, int kValues>
-__global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, kValues == 32 ? 2 : 1) distill_stream_kernel(const DistillArgs a, int ctas) {
+template <typename T, int KP, int kValues>
+__global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, kValues == 32 ? 2 : 1) distill_stream_kernel(const DistillArgs a) {
   constexpr int VEC = Elem<T>::kVec, U = kValues / VEC;
   extern __shared__ __align__(16) uint8_t stage_memory[];   // [kStages][part] elements
   __shared__ StreamShared sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int warps = blockDim.x / 32 - 1, NT = warps * 32, part = NT * kValues;
-  const int rank = CLUSTER ? (int)cluster_rank() : 0;
-  const int64_t first = CLUSTER ? blockIdx.x / ctas : blockIdx.x, step = CLUSTER ? gridDim.x / ctas : gridDim.x;
+  const int64_t first = blockIdx.x, step = gridDim.x;
   const int V = (int)a.V;
   const float c = a.inv_t * kLog2e;
-  // Of a row: its first element; where this CTA's part begins (ahead of the row by up to a piece); the part's
+  // Of a row: its first element; where what the threads hold begins (ahead of the row by up to a piece); its
   // whole pieces, which are copied (partial ones are loaded by the threads that have them).
   const auto row_at = [&](int64_t r) { return static_cast<const T*>(a.logits) + r * a.ld; };
-  const auto begin_of = [&](const T* row) { return rank * part - row_shift(row); };
+  const auto begin_of = [&](const T* row) { return -row_shift(row); };
   const auto first_whole = [&](int begin) { return begin < 0 ? 1 : 0; };
   const auto whole_bytes = [&](int begin) {
     const int last = min(part / VEC, max(0, V - begin) / VEC);
@@ -509,22 +489,19 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
   for (int i = threadIdx.x; i < kMostWarps * 40; i += blockDim.x) sh.seen[i] = 0;
   launch_gate();
   __syncthreads();
-  if (CLUSTER) cluster_sync();   // every CTA has begun: its memory can be written
-  const int all = CLUSTER ? ctas * warps : warps;
   // The one barrier of a row.  (Nobody is a whole row ahead of it: two buffers for the statistics do.)
   const auto meet = [&] {
     __syncwarp();
-    if (CLUSTER) cluster_sync();
-    else __syncthreads();
+    __syncthreads();
   };
   // Statistics of row n, behind its barrier, by a warp.
   const auto joined = [&](int n) {
     float m = -INFINITY;
-    for (int i = lane; i < all; i += 32) m = fmaxf(m, sh.stats[n & 1][i].m);
+    for (int i = lane; i < warps; i += 32) m = fmaxf(m, sh.stats[n & 1][i].m);
     Sum r;
     r.m = redux_max(m);
     r.s = 0.f;
-    for (int i = lane; i < all; i += 32) {
+    for (int i = lane; i < warps; i += 32) {
       const Sum v = sh.stats[n & 1][i];
       r.s += v.m == -INFINITY ? v.s : v.s * ex2((v.m - base_of(r.m)) * c);
     }
@@ -578,11 +555,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
       float lo, hi;
       unpack2f(s2, lo, hi);
       const float s = warp_sum(lo + hi);
-      if (CLUSTER) {
-        if (lane < ctas) tell(&sh.stats[n & 1][rank * warps + warp], lane, Sum{m, s});
-      } else if (lane == 0) {
-        sh.stats[n & 1][warp] = Sum{m, s};
-      }
+      if (lane == 0) sh.stats[n & 1][warp] = Sum{m, s};
       // (behind this the last warp reuses the row's buffer, and stores where this warp stored for the row before)
       meet();
       const Sum student = joined(n);
@@ -642,7 +615,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
     fetch_ids(first, ids);
     fetch_pairs(first, ids, next);
     fetch_ids(first + step, ids);
-    int32_t old_id[KP];   // of this part's tokens of the last row, and their gradients
+    int32_t old_id[KP];   // the last row's tokens, and their gradients
     float old_d[KP];
     T* old_out = nullptr;
     const auto store_old = [&] {
@@ -669,7 +642,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
       const bool none = empty(teacher);
       const float log_teacher = log_sum(teacher);
       if (lane == 0) sh.teacher[n & 1] = !none;
-      // Whether a token of this part occurs twice: a bit for each (cleared at once: one warp's own).
+      // Whether a token occurs twice: a bit for each (cleared at once: one warp's own).
       const int begin = begin_of(row_at(r));
       uint32_t twice = 0;
       const auto in_part = [&](int32_t id) { return id >= 0 && id >= begin && id < begin + part; };
@@ -697,7 +670,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
         loss += t.loss;
       }
       loss = warp_sum(loss);
-      if (rank == 0 && lane == 0) {
+      if (lane == 0) {
         a.loss[r] = loss;
         a.stats[2 * r] = student.m;
         a.stats[2 * r + 1] = log_s;
@@ -753,20 +726,21 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
   p.nsplit = (p.nchunks + p.cps - 1) / p.cps;
   return p;
 }
-// CTAs of a cluster that hold a row, their warps with elements and a thread's elements; no CTAs where the row is too long.
-// Up to 16384 elements a CTA of 32 a thread, of which a multiprocessor holds several; above, as few CTAs as do with 40 a
-// thread, each with a multiprocessor to itself: a cluster's barrier costs more than that (4096 x 32768 bf16 123 us; two
-// CTAs of 16 warps 142; 3532 x 38000 121 us, three CTAs 275).  aligned: all rows start on a 16-byte boundary.
-struct Cluster {
-  int ctas, warps, values;
+// Loss and gradient from one read, by a CTA that holds the row: its warps with elements and a thread's elements; no warps where two
+// passes are taken.  Up to 16384 elements of 32 a thread, of which a multiprocessor holds several CTAs; above, 40 a thread, one CTA.
+// Longer rows take two passes: by clusters of two to eight CTAs they took 146 to 175 us (2048 x 65536 to 837 x 160001 bf16), by
+// two passes 145 to 148.  So do more pairs than the one warp deals with beside the row: one read and two passes, us, bf16, 96M
+// logits: 64 pairs, V = 4000 187 and 323, 16000 121 and 131, 38000 116 and 114; 128 pairs, V = 1500 711 and 926,
+// 4000 352 and 365, 8000 271 and 212, 38000 164 and 118; 256 pairs 1330 and more against 135 to 1370.
+// aligned: all rows start on a 16-byte boundary.
+struct Held {
+  int warps, values;
 };
-Cluster cluster_of(int64_t V, int dtype, bool aligned) {
+Held held_by(int64_t V, int K, int dtype, bool aligned) {
   const int64_t n = V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7);
-  if (n <= 16 * 1024) return Cluster{1, (int)((n + 1023) / 1024), 32};
   const int most = (dtype == OLSGD_F32 ? 19 : kMostWarps) * 1280;   // (two buffers of 97 or 78 KB)
-  const int64_t ctas = (n + most - 1) / most;
-  if (ctas > kMaxCluster) return Cluster{0, 0, 0};
-  return Cluster{(int)ctas, (int)((n + ctas * 1280 - 1) / (ctas * 1280)), 40};
+  if (n > most || K > 128 || (K > 64 && V > 4096)) return Held{0, 0};
+  return n <= 16 * 1024 ? Held{(int)((n + 1023) / 1024), 32} : Held{(int)((n + 1279) / 1280), 40};
 }
 template <typename T>
 bool rows_aligned(const DistillArgs& a) {
@@ -793,71 +767,39 @@ cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
                         dim3((unsigned)a.rows, (unsigned)((whole + turns - 1) / turns)), dim3(kThreads), 0, s, a, (int)turns);
 }
 
-// As many clusters as the GPU holds at once.
-template <typename T, bool CLUSTER, int KP, int kValues>
-cudaError_t stream_as(const DistillArgs& a, const Cluster& c, cudaStream_t s) {
-  const int threads = c.warps * 32 + 32;
-  const size_t smem = (size_t)kStages * c.warps * 32 * kValues * sizeof(T);
+// As many CTAs as the GPU holds at once.
+template <typename T, int KP, int kValues>
+cudaError_t stream_as(const DistillArgs& a, const Held& h, cudaStream_t s) {
+  const int threads = h.warps * 32 + 32;
+  const size_t smem = (size_t)kStages * h.warps * 32 * kValues * sizeof(T);
   static PerDeviceSmem configured;
-  auto kern = distill_stream_kernel<T, CLUSTER, KP, kValues>;
+  auto kern = distill_stream_kernel<T, KP, kValues>;
   const cudaError_t e = ensure_dynamic_smem(configured, kern, 200 * 1024);
   if (e != cudaSuccess) return e;
   // (registers, and 227 KB a multiprocessor)
   int64_t resident = 65536 / ((kValues == 40 ? 64 : 56) * threads), by_memory = 227 * 1024 / (smem + sizeof(StreamShared) + 1024);
   resident = resident < by_memory ? resident : by_memory;
-  if (!CLUSTER) {
-    const int64_t room = sm_count() * (resident < 1 ? 1 : resident);
-    return launch_chained(kern, dim3((unsigned)(a.rows < room ? a.rows : room)), dim3(threads), smem, s, a, 1);
-  }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)c.ctas);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = c.ctas;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  // Groups of multiprocessors need not be a multiple of a cluster: asked once for each shape.  (Of a grid that does not fit
-  // the rest would start when the others end.)
-  static std::atomic<int> known[kKnownDevices][kMaxCluster + 1][kMostWarps + 1];
-  const int dev = current_device();
-  const bool keeps = dev >= 0 && dev < kKnownDevices;
-  int room = keeps ? known[dev][c.ctas][c.warps].load(std::memory_order_relaxed) : 0;
-  if (room == 0) {
-    if (cudaOccupancyMaxActiveClusters(&room, kern, &cfg) != cudaSuccess || room < 1) {
-      cudaGetLastError();
-      room = 1;
-    }
-    if (keeps) known[dev][c.ctas][c.warps].store(room, std::memory_order_relaxed);
-  }
-  cfg.gridDim = dim3((unsigned)((a.rows < room ? a.rows : room) * c.ctas));
-  cfg.numAttrs = g_launch_overlap ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, a, c.ctas);
+  const int64_t room = sm_count() * (resident < 1 ? 1 : resident);
+  return launch_chained(kern, dim3((unsigned)(a.rows < room ? a.rows : room)), dim3(threads), smem, s, a);
 }
-template <typename T, bool CLUSTER, int kValues>
-cudaError_t stream_pairs(const DistillArgs& a, const Cluster& c, cudaStream_t s) {
-  return a.K <= 32    ? stream_as<T, CLUSTER, 1, kValues>(a, c, s)
-         : a.K <= 128 ? stream_as<T, CLUSTER, 4, kValues>(a, c, s)
-                      : stream_as<T, CLUSTER, 8, kValues>(a, c, s);
+template <typename T, int kValues>
+cudaError_t stream_pairs(const DistillArgs& a, const Held& h, cudaStream_t s) {
+  if (a.K <= 32) return stream_as<T, 1, kValues>(a, h, s);
+  if constexpr (kValues == 32)
+    if (a.K > 64) return stream_as<T, 4, kValues>(a, h, s);
+  return stream_as<T, 2, kValues>(a, h, s);
 }
 template <typename T>
-cudaError_t stream_rows(const DistillArgs& a, const Cluster& c, cudaStream_t s) {
-  if (c.ctas > 1) return stream_pairs<T, true, 40>(a, c, s);
-  return c.values == 40 ? stream_pairs<T, false, 40>(a, c, s) : stream_pairs<T, false, 32>(a, c, s);
+cudaError_t stream_rows(const DistillArgs& a, const Held& h, cudaStream_t s) {
+  return h.values == 40 ? stream_pairs<T, 40>(a, h, s) : stream_pairs<T, 32>(a, h, s);
 }
 
 template <typename T>
 cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax) return a.d_loss ? warp_rows<T, true, true>(a, s) : warp_rows<T, true, false>(a, s);
   if (a.d_loss) {
-    const Cluster c = cluster_of(a.V, a.dtype, rows_aligned<T>(a));
-    if (c.ctas > 0) return stream_rows<T>(a, c, s);
+    const Held h = held_by(a.V, a.K, a.dtype, rows_aligned<T>(a));
+    if (h.warps > 0) return stream_rows<T>(a, h, s);
   }
   const Plan p = plan(a.rows, a.V, a.dtype);
   float2* part = p.nsplit > 1 ? static_cast<float2*>(a.ws) : nullptr;
@@ -869,8 +811,8 @@ cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-size_t distill_workspace(int dtype, int64_t rows, int64_t V, bool gradient) {
-  if (V <= kWarpRowMax || (gradient && cluster_of(V, dtype, false).ctas > 0)) return 0;   // (whatever the alignment)
+size_t distill_workspace(int dtype, int64_t rows, int64_t V, int K, bool gradient) {
+  if (V <= kWarpRowMax || (gradient && held_by(V, K, dtype, false).warps > 0)) return 0;   // (whatever the alignment)
   const Plan p = plan(rows, V, dtype);
   return p.nsplit == 1 ? 0 : (size_t)rows * p.nsplit * sizeof(float2);
 }

@@ -502,7 +502,7 @@ olsgd_status olsgd_expert_product_backward(int32_t m, int64_t R, int64_t E, int6
 olsgd_status olsgd_distill_workspace(int32_t dtype, int64_t rows, int64_t V, int32_t gradient, size_t* out_bytes) {
   OLSGD_REFUSE_IF(!out_bytes, "out_bytes is NULL");
   OLSGD_TRY(check_rows(dtype, rows, V));
-  *out_bytes = rows == 0 ? 0 : distill_workspace(dtype, rows, V, gradient != 0);
+  *out_bytes = rows == 0 ? 0 : distill_workspace(dtype, rows, V, OLSGD_MAX_TEACHER, gradient != 0);
   return OLSGD_OK;
 }
 
@@ -516,7 +516,7 @@ olsgd_status olsgd_distill(const void* logits, int32_t dtype, int64_t rows, int6
   if (rows == 0) return OLSGD_OK;
   OLSGD_REFUSE_IF(!aligned_to(loss, 4) || !aligned_to(stats, 4), "loss and stats must be non-null and 4-byte aligned");
   if (d_loss) OLSGD_TRY(check_distill_grad(dtype, V, row_stride, logits, d_loss, d_logits, d_row_stride));
-  OLSGD_TRY(check_workspace(workspace, workspace_bytes, distill_workspace(dtype, rows, V, d_loss != nullptr)));
+  OLSGD_TRY(check_workspace(workspace, workspace_bytes, distill_workspace(dtype, rows, V, K, d_loss != nullptr)));
   const DistillArgs a{logits, dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, (float)(1.0 / temperature),
                       d_loss, loss, stats, d_logits, d_row_stride, workspace};
   return launched(launch_distill(a, static_cast<cudaStream_t>(stream)), "olsgd_distill");

@@ -177,7 +177,7 @@ struct DistillArgs {
   int64_t ldd;
   void* ws;
 };
-size_t distill_workspace(int dtype, int64_t rows, int64_t V, bool gradient);
+size_t distill_workspace(int dtype, int64_t rows, int64_t V, int K, bool gradient);
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s);
 cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s);
 cudaError_t distill_status(int* status);   // of its bounded waits, for operators_status
