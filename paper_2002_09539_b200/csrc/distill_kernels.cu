@@ -521,7 +521,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
     for (int64_t r = first; r < a.rows; r += step, ++n) {
       const T* row = row_at(r);
       const int begin = begin_of(row);
-      const float weight = a.d_loss[r];   // (used behind the wait)
+      const float weight = a.d_loss ? a.d_loss[r] : 0.f;   // (used behind the wait)
       if (whole_bytes(begin)) {
         wait(&sh.full[n % kStages], copies >> (n % kStages) & 1);
         copies ^= 1u << (n % kStages);
@@ -558,6 +558,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
       if (lane == 0) sh.stats[n & 1][warp] = Sum{m, s};
       // (behind this the last warp reuses the row's buffer, and stores where this warp stored for the row before)
       meet();
+      if (!a.d_loss) continue;   // the loss alone
       const Sum student = joined(n);
       T* out = static_cast<T*>(a.d_logits) + r * a.ldd;
       const bool aligned = row_shift(out) == row_shift(row);
@@ -626,7 +627,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
     };
     int n = 0;
     for (int64_t r = first; r < a.rows; r += step, ++n) {
-      const float weight = a.d_loss[r];
+      const float weight = a.d_loss ? a.d_loss[r] : 0.f;
 #pragma unroll
       for (int i = 0; i < KP; ++i) now[i] = next[i];
       if (r + step < a.rows) fetch_pairs(r + step, ids, next);
@@ -732,13 +733,17 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
 // two passes 145 to 148.  So do more pairs than the one warp deals with beside the row: one read and two passes, us, bf16, 96M
 // logits: 64 pairs, V = 4000 187 and 323, 16000 121 and 131, 38000 116 and 114; 128 pairs, V = 1500 711 and 926,
 // 4000 352 and 365, 8000 271 and 212, 38000 164 and 118; 256 pairs 1330 and more against 135 to 1370.
+// A loss alone takes a CTA that stays where the row is short, which else costs a CTA's start and its barriers each: like
+// this and a CTA a row, us, 96M logits (fp32 48M): 32 pairs, bf16, V = 1500 113 and 370, 4000 64 and 148, 8000 57 and 69,
+// 16000 59 and 50; fp32 4000 48 and 77, 8000 44 and 39; 64 pairs, bf16, 4000 111 and 150, 8000 90 and 70.
 // aligned: all rows start on a 16-byte boundary.
 struct Held {
   int warps, values;
 };
-Held held_by(int64_t V, int K, int dtype, bool aligned) {
+Held held_by(int64_t V, int K, int dtype, bool aligned, bool gradient) {
   const int64_t n = V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7);
   const int most = (dtype == OLSGD_F32 ? 19 : kMostWarps) * 1280;   // (two buffers of 97 or 78 KB)
+  if (!gradient && (K > 64 || V * (dtype == OLSGD_F32 ? 4 : 2) > (K <= 32 ? 16384 : 8192))) return Held{0, 0};
   if (n > most || K > 128 || (K > 64 && V > 4096)) return Held{0, 0};
   return n <= 16 * 1024 ? Held{(int)((n + 1023) / 1024), 32} : Held{(int)((n + 1279) / 1280), 40};
 }
@@ -797,10 +802,8 @@ cudaError_t stream_rows(const DistillArgs& a, const Held& h, cudaStream_t s) {
 template <typename T>
 cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
   if (a.V <= kWarpRowMax) return a.d_loss ? warp_rows<T, true, true>(a, s) : warp_rows<T, true, false>(a, s);
-  if (a.d_loss) {
-    const Held h = held_by(a.V, a.K, a.dtype, rows_aligned<T>(a));
-    if (h.warps > 0) return stream_rows<T>(a, h, s);
-  }
+  const Held h = held_by(a.V, a.K, a.dtype, rows_aligned<T>(a), a.d_loss != nullptr);
+  if (h.warps > 0) return stream_rows<T>(a, h, s);
   const Plan p = plan(a.rows, a.V, a.dtype);
   float2* part = p.nsplit > 1 ? static_cast<float2*>(a.ws) : nullptr;
   cudaError_t e = launch_chained(distill_row_kernel<T>, dim3((unsigned)a.rows, (unsigned)p.nsplit), dim3(kThreads), 0, s, a, p.nchunks, p.cps, part);
@@ -812,7 +815,7 @@ cudaError_t forward(const DistillArgs& a, cudaStream_t s) {
 }  // namespace
 
 size_t distill_workspace(int dtype, int64_t rows, int64_t V, int K, bool gradient) {
-  if (V <= kWarpRowMax || (gradient && held_by(V, K, dtype, false).warps > 0)) return 0;   // (whatever the alignment)
+  if (V <= kWarpRowMax || held_by(V, K, dtype, false, gradient).warps > 0) return 0;   // (whatever the alignment)
   const Plan p = plan(rows, V, dtype);
   return p.nsplit == 1 ? 0 : (size_t)rows * p.nsplit * sizeof(float2);
 }

@@ -96,6 +96,15 @@ def test_distill(dtype, N, V, K):
     _check(x, ids, _randn(g, (N, K), dtype, 3.0), 2.5, _randn(g, (N,)))
 
 
+# pairs and lengths on either side of every choice between one read and two, and rows enough for a CTA's turn and a segment's
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,K", [(310, 1030, 33), (400, 4096, 64), (7, 4096, 65), (500, 3000, 100), (9, 4097, 128), (5, 2500, 129), (3, 8192, 32), (340, 8193, 32), (6, 8200, 64),
+                                   (160, 24313, 33), (12, 24321, 20), (155, 39673, 40), (8, 39681, 32), (6, 65536, 200), (2400, 9000, 256)])
+def test_distill_by_one_read_and_by_two(dtype, N, V, K):
+    g = _gen(N * 999 + V)
+    _check(_randn(g, (N, V), dtype, 3.0), _pairs(g, N, V, K), _randn(g, (N, K), torch.float32, 3.0), 1.5, _randn(g, (N,)))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [40, 1500, 20011, 140001])
 @pytest.mark.parametrize("pattern", ["no pairs", "some pairs", "one token", "teacher masked", "student masked", "student empty", "constant", "lowest", "far", "learnt", "certain"])
