@@ -7,8 +7,8 @@
 // Bound by the logits' way in and, for a gradient, its way out (4096 x 32768 bf16 with gradient: 118 us, 537 MB, 4.6 TB/s; loss
 // of 1021 x 50021 fp32: 39 us, 204 MB, 5.2 TB/s).  Where the rows' weights are known when
 // the loss is formed, both come from one read: a row lies in the registers of a CTA as exp(x - the warp's own max), 32 or 40
-// values a thread, until the whole row's sum is known.  Longer rows, losses alone and gradients that are asked for later take
-// one pass each (4096 x 32768 bf16: 57 and 91 us).  Rows of up to 1024 logits belong to a warp.
+// values a thread, until the whole row's sum is known.  Longer rows take two passes; so do losses alone and gradients that are asked for
+// later, one each, unless the row is short (4096 x 32768 bf16: 57 and 91 us).  Rows of up to 1024 logits belong to a warp.
 //
 // A gradient at the pairs' tokens is formed apart from the others, from the logit and the sum of the q of
 // all pairs with that token, and stored behind them, so that it is rounded once.
@@ -671,7 +671,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
         loss += t.loss;
       }
       loss = warp_sum(loss);
-      if (lane == 0) {
+      if (lane == 0 && a.loss) {   // (none: a gradient that is asked for later)
         a.loss[r] = loss;
         a.stats[2 * r] = student.m;
         a.stats[2 * r + 1] = log_s;
@@ -735,15 +735,17 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
 // 4000 352 and 365, 8000 271 and 212, 38000 164 and 118; 256 pairs 1330 and more against 135 to 1370.
 // A loss alone takes a CTA that stays where the row is short, which else costs a CTA's start and its barriers each: like
 // this and a CTA a row, us, 96M logits (fp32 48M): 32 pairs, bf16, V = 1500 113 and 370, 4000 64 and 148, 8000 57 and 69,
-// 16000 59 and 50; fp32 4000 48 and 77, 8000 44 and 39; 64 pairs, bf16, 4000 111 and 150, 8000 90 and 70.
+// 16000 59 and 50; fp32 4000 48 and 77, 8000 44 and 39; 64 pairs, bf16, 4000 111 and 150, 8000 90 and 70.  So does a
+// gradient that is asked for later: bf16, V = 1500 157 and 406, 4000 91 and 144, 8000 82 and 91, 16000 83 and 76.
 // aligned: all rows start on a 16-byte boundary.
 struct Held {
   int warps, values;
 };
+bool is_short(int64_t V, int K, int dtype) { return K <= 64 && V * (dtype == OLSGD_F32 ? 4 : 2) <= (K <= 32 ? 16384 : 8192); }
 Held held_by(int64_t V, int K, int dtype, bool aligned, bool gradient) {
   const int64_t n = V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7);
   const int most = (dtype == OLSGD_F32 ? 19 : kMostWarps) * 1280;   // (two buffers of 97 or 78 KB)
-  if (!gradient && (K > 64 || V * (dtype == OLSGD_F32 ? 4 : 2) > (K <= 32 ? 16384 : 8192))) return Held{0, 0};
+  if (!gradient && !is_short(V, K, dtype)) return Held{0, 0};
   if (n > most || K > 128 || (K > 64 && V > 4096)) return Held{0, 0};
   return n <= 16 * 1024 ? Held{(int)((n + 1023) / 1024), 32} : Held{(int)((n + 1279) / 1280), 40};
 }
@@ -759,17 +761,6 @@ cudaError_t warp_rows(const DistillArgs& a, cudaStream_t s) {
            : a.V <= 256 ? distill_warp_kernel<T, 8, LOSS, GRAD>
                         : distill_warp_kernel<T, 32, LOSS, GRAD>;
   return launch_chained(k, grid, dim3(kThreads), 0, s, a);
-}
-
-template <typename T>
-cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
-  if (a.V <= kWarpRowMax) return warp_rows<T, false, true>(a, s);
-  const int64_t pieces = (a.V + (rows_aligned<T>(a) ? 1 : 2) * (Elem<T>::kVec - 1)) / Elem<T>::kVec, per = kThreads * kGradPieces;
-  const int64_t whole = (pieces + per - 1) / per, want = (kGradCtas + a.rows - 1) / a.rows;   // turns of a row; segments
-  const int64_t turns = want >= whole ? 1 : (whole + want - 1) / want;
-  const bool large = a.rows * a.V * (int64_t)sizeof(T) > kKeepBytes;   // a gradient that L2 would not hold anyway
-  return launch_chained(large ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>,
-                        dim3((unsigned)a.rows, (unsigned)((whole + turns - 1) / turns)), dim3(kThreads), 0, s, a, (int)turns);
 }
 
 // As many CTAs as the GPU holds at once.
@@ -797,6 +788,20 @@ cudaError_t stream_pairs(const DistillArgs& a, const Held& h, cudaStream_t s) {
 template <typename T>
 cudaError_t stream_rows(const DistillArgs& a, const Held& h, cudaStream_t s) {
   return h.values == 40 ? stream_pairs<T, 40>(a, h, s) : stream_pairs<T, 32>(a, h, s);
+}
+
+template <typename T>
+cudaError_t gradient(const DistillArgs& a, cudaStream_t s) {
+  if (a.V <= kWarpRowMax) return warp_rows<T, false, true>(a, s);
+  // (of short rows the statistics are formed again: a CTA for each row and its barriers take longer)
+  const Held h = held_by(a.V, a.K, a.dtype, rows_aligned<T>(a), true);
+  if (h.warps > 0 && is_short(a.V, a.K, a.dtype)) return stream_rows<T>(a, h, s);
+  const int64_t pieces = (a.V + (rows_aligned<T>(a) ? 1 : 2) * (Elem<T>::kVec - 1)) / Elem<T>::kVec, per = kThreads * kGradPieces;
+  const int64_t whole = (pieces + per - 1) / per, want = (kGradCtas + a.rows - 1) / a.rows;   // turns of a row; segments
+  const int64_t turns = want >= whole ? 1 : (whole + want - 1) / want;
+  const bool large = a.rows * a.V * (int64_t)sizeof(T) > kKeepBytes;   // a gradient that L2 would not hold anyway
+  return launch_chained(large ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>,
+                        dim3((unsigned)a.rows, (unsigned)((whole + turns - 1) / turns)), dim3(kThreads), 0, s, a, (int)turns);
 }
 
 template <typename T>
