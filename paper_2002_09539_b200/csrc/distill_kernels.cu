@@ -731,7 +731,7 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
 // passes are taken.  Up to 16384 elements of 32 a thread, of which a multiprocessor holds several CTAs; above, 40 a thread, one CTA.
 // Longer rows take two passes: by clusters of two to eight CTAs they took 146 to 175 us (2048 x 65536 to 837 x 160001 bf16), by
 // two passes 145 to 148.  So do more pairs than the one warp deals with beside the row: one read and two passes, us, bf16, 96M
-// logits: 64 pairs, V = 4000 187 and 323, 16000 121 and 131, 38000 116 and 114; 128 pairs, V = 1500 711 and 926,
+// logits: 64 pairs, V = 4000 131 and 326, 16000 100 and 131, 38000 93 and 114; 128 pairs, V = 1500 711 and 926,
 // 4000 352 and 365, 8000 271 and 212, 38000 164 and 118; 256 pairs 1330 and more against 135 to 1370.
 // A loss alone takes a CTA that stays where the row is short, which else costs a CTA's start and its barriers each: like
 // this and a CTA a row, us, 96M logits (fp32 48M): 32 pairs, bf16, V = 1500 113 and 370, 4000 64 and 148, 8000 57 and 69,
