@@ -463,9 +463,14 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
           if (k * kUmmaK < left) umma_bf16(acc, a_desc + a_step * k, b_desc + b_step * k, idesc, (kb > u.kb || k > 0) ? 1u : 0u);
       };
       const auto wait = [&](uint64_t* bar, uint32_t parity) {
+        // (DW: one lane waits, for MMAs and commits of its own.  The others store zeros over what the barrier says has come: a
+        // shuffle tells them so, but orders no memory)
         int done = 1;
         if (MODE != DW || lane == 0) done = mbar_wait(smem_u32(bar), parity, abort_flag);
-        if (MODE == DW) done = __shfl_sync(0xffffffffu, done, 0);
+        if (MODE == DW) {
+          __syncwarp();
+          done = __shfl_sync(0xffffffffu, done, 0);
+        }
         tc_fence_after();
         return done != 0;
       };
@@ -536,9 +541,10 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
       const Unit u = walk.at(t);
       const bool none = MODE == DW && u.kb == u.end;   // zeros, and no accumulator
       const uint32_t buf = kBufs == 2 ? n & 1 : 0, parity = kBufs == 2 ? (n >> 1) & 1 : n & 1;
-      // one lane waits for its warp: what follows wants all lanes together
+      // one lane waits for its warp (ordered by __syncwarp: the shuffle orders no memory): what follows wants all lanes together
       int ok = 1;
       if (lane == 0 && !none) ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), parity, abort_flag);
+      __syncwarp();
       ok = __shfl_sync(0xffffffffu, ok, 0);
       if (!ok) break;
       tc_fence_after();
