@@ -71,6 +71,7 @@ template <int STAGES>
 struct Control {
   uint64_t full[STAGES], empty[STAGES];
   uint64_t acc_full[2], acc_empty[2];
+  uint64_t last;             // MMAs in flight when a wait gave up
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -364,6 +365,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
       mbar_init(smem_u32(&ctl->acc_full[b]), 1);
       mbar_init(smem_u32(&ctl->acc_empty[b]), kEpiWarps);
     }
+    mbar_init(smem_u32(&ctl->last), 1);
     ctl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -386,9 +388,10 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   const auto b_boxes = [&](const Unit& u) { return min(BN / 64, (g.cols - u.col * BN + 63) / 64); };
 
   const bool one = MODE == DW ? lane == 0 : elect_one();   // (DW: its MMA warp has work for all lanes)
+  uint32_t copied = 0;   // blocks that this thread has asked for
   if (warp == 0 && one) {
     // ---------------- TMA producer
-    uint32_t it = 0;
+    uint32_t& it = copied;
     for (uint32_t t = first; t < total && !*abort_flag; t += step) {
       const Unit u = walk.at(t);
       const int m0 = u.m * kTileM, held = mma_cols(u), na = a_boxes(u), nb = MODE == DW ? b_boxes(u) : 0;
@@ -430,14 +433,6 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
             }
         }
       }
-    }
-    // drain: whoever gave up waits (bounded) for the copies still in flight
-    if (*abort_flag) {
-      const uint32_t from = it > STAGES ? it - STAGES : 0;
-      const uint64_t t0 = global_ns();
-      for (uint32_t i = from; i < it; ++i)
-        while (!mbar_try_wait(smem_u32(&ctl->full[i % STAGES]), (i / STAGES) & 1) && global_ns() - t0 < 10000000ull) {
-        }
     }
   } else if (warp == 1 && (MODE == DW || one)) {
     // ---------------- MMA issuer: one lane; DW: its warp comes along, for the zeros
@@ -635,14 +630,24 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
   // ---------------- teardown: every role arrives here, all waits above are bounded
   tc_fence_before();
   __syncthreads();
-  if (*abort_flag && threadIdx.x == 0) {
-    // bounded grace period for copies and MMAs that may still be in flight
+  if (*abort_flag) {
+    // Somebody gave up: what is still on its way into shared or tensor memory arrives (or is waited for long enough) before the CTA
+    // gives them back.  The thread that asked for the copies waits for each stage's last one, whether it had left its loop before or
+    // not; the thread that issued the MMAs, committed or not, for all of them.
     const uint64_t t0 = global_ns();
-    while (global_ns() - t0 < 1000000ull) {
+    const auto arrives = [&](uint64_t* bar, uint32_t parity) {
+      while (!mbar_try_wait(smem_u32(bar), parity) && global_ns() - t0 < 10000000ull) {
+      }
+    };
+    for (uint32_t i = copied > STAGES ? copied - STAGES : 0; i < copied; ++i) arrives(&ctl->full[i % STAGES], (i / STAGES) & 1);
+    if (warp == 1 && one) {
+      umma_commit(smem_u32(&ctl->last));
+      arrives(&ctl->last, 0);
     }
-    atomicExch(&g_product_status, (int)OLSGD_ETIMEOUT);
+    if (threadIdx.x == 0) atomicExch(&g_product_status, (int)OLSGD_ETIMEOUT);
   }
   __syncthreads();
+  __syncwarp();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, kTmemCols);
