@@ -423,6 +423,7 @@ struct StreamShared {
   uint64_t full[kStages];                  // copies
   Sum stats[2][kMostWarps];                // of the warps, of rows in turn
   int teacher[2];                          // whether the row has one
+  int gave_up, asked;                      // whether a wait for a copy did; rows, from the CTA's first on, that were asked for
   uint32_t seen[kMostWarps * 40];          // a bit for each element
   int32_t id[kMaxPairs];                   // where a token occurs twice
   float q[kMaxPairs];
@@ -461,9 +462,18 @@ __device__ __forceinline__ float redux_max(float v) {
   return v;
 }
 
-// blockDim.x: 32 threads for every warp with elements, and 32.  KP: pairs of a lane of the last warp.
+// Waits for the last copy to each buffer of the rows that were asked for; a copy's parity is that of its turn of the buffer.  (A
+// function of its own: inlined, it took registers from the rows' loop, 4096 x 32768 with 64 pairs 121 and 129 us.)
+__device__ __noinline__ void copies_end(uint32_t full, int asked) {
+  for (int i = max(0, asked - kStages); i < asked; ++i) phase_done(full + i % kStages * 8, i / kStages & 1);
+}
+
+// blockDim.x: 32 threads for every warp with elements, and 32.  KP: pairs of a lane of the last warp (4: of short rows alone,
+// which have registers for them).
+template <int KP, int kValues>
+constexpr int kStreamThreads = KP == 4 ? 192 : (kValues == 32 ? 16 : kMostWarps) * 32 + 32;
 template <typename T, int KP, int kValues>
-__global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, kValues == 32 ? 2 : 1) distill_stream_kernel(const DistillArgs a) {
+__global__ void __launch_bounds__(kStreamThreads<KP, kValues>, KP == 4 ? 5 : kValues == 32 ? 2 : 1) distill_stream_kernel(const DistillArgs a) {
   constexpr int VEC = Elem<T>::kVec, U = kValues / VEC;
   extern __shared__ __align__(16) uint8_t stage_memory[];   // [kStages][part] elements
   __shared__ StreamShared sh;
@@ -487,6 +497,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = threadIdx.x; i < kMostWarps * 40; i += blockDim.x) sh.seen[i] = 0;
+  if (threadIdx.x == 0) sh.gave_up = 0;
   launch_gate();
   __syncthreads();
   // The one barrier of a row.  (Nobody is a whole row ahead of it: two buffers for the statistics do.)
@@ -509,9 +520,11 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
     return r;
   };
   bool gave_up = false;
-  // (one lane waits for its warp: of all lanes' polling the other warps would feel)
+  // (one lane waits for its warp: of all lanes' polling the other warps would feel.)  A warp that gives up waits no more, and says so
+  // ahead of its row's barrier.  The last warp, behind it, asks for no more copies then, so that no barrier sees more turns than have
+  // ended, and at its end waits for those that are on their way, before the CTA gives their memory back.
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (lane == 0 && !gave_up && !phase_done(shared_address(bar), parity)) gave_up = true;
+    if (lane == 0 && !gave_up && !phase_done(shared_address(bar), parity)) sh.gave_up = gave_up = true;
     __syncwarp();
   };
 
@@ -587,6 +600,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
   } else {
     const auto request = [&](int64_t r, int n) {
       if (lane != 0 || r >= a.rows) return;
+      sh.asked = n + 1;
       const T* row = row_at(r);
       const int begin = begin_of(row), skip = first_whole(begin) * VEC;
       const uint32_t bytes = whole_bytes(begin);
@@ -660,7 +674,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
       const bool any_twice = __any_sync(0xffffffffu, twice != 0);
       meet();
       store_old();
-      request(r + kStages * step, n + kStages);
+      if (!sh.gave_up) request(r + kStages * step, n + kStages);
       const Sum student = joined(n);
       const float log_s = log_sum(student);
       float loss = 0.f, q[KP];
@@ -704,6 +718,7 @@ __global__ void __launch_bounds__((kValues == 32 ? 16 : kMostWarps) * 32 + 32, k
     }
     meet();
     store_old();
+    if (sh.gave_up) copies_end(shared_address(sh.full), sh.asked);
   }
   if (gave_up) atomicExch(&g_distill_status, (int)OLSGD_ETIMEOUT);
 }
@@ -741,12 +756,14 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
 struct Held {
   int warps, values;
 };
+constexpr int kManyPairsMax = 4096;   // longest row that is held with more than 64 pairs
+static_assert((kManyPairsMax + 7 + 1023) / 1024 * 32 + 32 <= kStreamThreads<4, 32>, "threads of a row with many pairs");
 bool is_short(int64_t V, int K, int dtype) { return K <= 64 && V * (dtype == OLSGD_F32 ? 4 : 2) <= (K <= 32 ? 16384 : 8192); }
 Held held_by(int64_t V, int K, int dtype, bool aligned, bool gradient) {
   const int64_t n = V + (aligned ? 0 : dtype == OLSGD_F32 ? 3 : 7);
   const int most = (dtype == OLSGD_F32 ? 19 : kMostWarps) * 1280;   // (two buffers of 97 or 78 KB)
   if (!gradient && !is_short(V, K, dtype)) return Held{0, 0};
-  if (n > most || K > 128 || (K > 64 && V > 4096)) return Held{0, 0};
+  if (n > most || K > 128 || (K > 64 && V > kManyPairsMax)) return Held{0, 0};
   return n <= 16 * 1024 ? Held{(int)((n + 1023) / 1024), 32} : Held{(int)((n + 1279) / 1280), 40};
 }
 template <typename T>
@@ -773,7 +790,7 @@ cudaError_t stream_as(const DistillArgs& a, const Held& h, cudaStream_t s) {
   const cudaError_t e = ensure_dynamic_smem(configured, kern, 200 * 1024);
   if (e != cudaSuccess) return e;
   // (registers, and 227 KB a multiprocessor)
-  int64_t resident = 65536 / ((kValues == 40 ? 64 : 56) * threads), by_memory = 227 * 1024 / (smem + sizeof(StreamShared) + 1024);
+  int64_t resident = 65536 / ((kValues == 40 || KP == 4 ? 64 : 56) * threads), by_memory = 227 * 1024 / (smem + sizeof(StreamShared) + 1024);
   resident = resident < by_memory ? resident : by_memory;
   const int64_t room = sm_count() * (resident < 1 ? 1 : resident);
   return launch_chained(kern, dim3((unsigned)(a.rows < room ? a.rows : room)), dim3(threads), smem, s, a);
