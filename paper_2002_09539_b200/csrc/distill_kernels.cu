@@ -437,7 +437,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
-__device__ int g_distill_status;   // a bounded wait gave up (olsgd_operators_join)
 
 // Waits for a phase of a barrier, a second at most.
 __device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity) {
@@ -720,7 +719,7 @@ __global__ void __launch_bounds__(kStreamThreads<KP, kValues>, KP == 4 ? 5 : kVa
     store_old();
     if (sh.gave_up) copies_end(shared_address(sh.full), sh.asked);
   }
-  if (gave_up) atomicExch(&g_distill_status, (int)OLSGD_ETIMEOUT);
+  if (gave_up) atomicExch(a.status, (int)OLSGD_ETIMEOUT);
 }
 
 // ------------------------------------------------------------------------------ host
@@ -782,12 +781,13 @@ cudaError_t warp_rows(const DistillArgs& a, cudaStream_t s) {
 
 // As many CTAs as the GPU holds at once.
 template <typename T, int KP, int kValues>
-cudaError_t stream_as(const DistillArgs& a, const Held& h, cudaStream_t s) {
+cudaError_t stream_as(DistillArgs a, const Held& h, cudaStream_t s) {
   const int threads = h.warps * 32 + 32;
   const size_t smem = (size_t)kStages * h.warps * 32 * kValues * sizeof(T);
   static PerDeviceSmem configured;
   auto kern = distill_stream_kernel<T, KP, kValues>;
-  const cudaError_t e = ensure_dynamic_smem(configured, kern, 200 * 1024);
+  cudaError_t e = ensure_dynamic_smem(configured, kern, 200 * 1024);
+  if (e == cudaSuccess) e = status_word(&a.status);
   if (e != cudaSuccess) return e;
   // (registers, and 227 KB a multiprocessor)
   int64_t resident = 65536 / ((kValues == 40 || KP == 4 ? 64 : 56) * threads), by_memory = 227 * 1024 / (smem + sizeof(StreamShared) + 1024);
@@ -855,15 +855,6 @@ cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s) {
     case OLSGD_BF16: return gradient<__nv_bfloat16>(a, s);
     default: return gradient<__half>(a, s);
   }
-}
-
-cudaError_t distill_status(int* status) {
-  cudaError_t e = cudaMemcpyFromSymbol(status, g_distill_status, sizeof(int));
-  if (e == cudaSuccess && *status != 0) {
-    const int zero = 0;
-    e = cudaMemcpyToSymbol(g_distill_status, &zero, sizeof(int));
-  }
-  return e;
 }
 
 }  // namespace olsgd

@@ -518,7 +518,7 @@ olsgd_status olsgd_distill(const void* logits, int32_t dtype, int64_t rows, int6
   if (d_loss) OLSGD_TRY(check_distill_grad(dtype, V, row_stride, logits, d_loss, d_logits, d_row_stride));
   OLSGD_TRY(check_workspace(workspace, workspace_bytes, distill_workspace(dtype, rows, V, K, d_loss != nullptr)));
   const DistillArgs a{logits, dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, (float)(1.0 / temperature),
-                      d_loss, loss, stats, d_logits, d_row_stride, workspace};
+                      d_loss, loss, stats, d_logits, d_row_stride, workspace, nullptr};
   return launched(launch_distill(a, static_cast<cudaStream_t>(stream)), "olsgd_distill");
 }
 
@@ -533,7 +533,7 @@ olsgd_status olsgd_distill_backward(const float* d_loss, const void* logits, int
   OLSGD_REFUSE_IF(!aligned_to(stats, 4), "stats must be non-null and 4-byte aligned");
   OLSGD_TRY(check_distill_grad(dtype, V, row_stride, logits, d_loss, d_logits, d_row_stride));
   const DistillArgs a{logits, dtype, rows, V, row_stride, ids, teacher, teacher_dtype, K, (float)(1.0 / temperature),
-                      d_loss, nullptr, const_cast<float*>(stats), d_logits, d_row_stride, nullptr};
+                      d_loss, nullptr, const_cast<float*>(stats), d_logits, d_row_stride, nullptr, nullptr};
   return launched(launch_distill_backward(a, static_cast<cudaStream_t>(stream)), "olsgd_distill_backward");
 }
 

@@ -160,7 +160,6 @@ bool product_needs_copies(const ProductShape& d, const GatedOperand& x, const Ex
 size_t product_workspace(const ProductShape& d, bool backward, bool copies);
 cudaError_t launch_product(ProductForward a, cudaStream_t s);
 cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s);
-cudaError_t product_status(int* status);   // of its bounded waits, for operators_status
 
 // ---- distill_kernels.cu -------------------------------------------------------
 struct DistillArgs {
@@ -176,12 +175,14 @@ struct DistillArgs {
   void* d_logits;
   int64_t ldd;
   void* ws;
+  int* status;               // (set by the launch)
 };
 size_t distill_workspace(int dtype, int64_t rows, int64_t V, int K, bool gradient);
 cudaError_t launch_distill(const DistillArgs& a, cudaStream_t s);
 cudaError_t launch_distill_backward(const DistillArgs& a, cudaStream_t s);
-cudaError_t distill_status(int* status);   // of its bounded waits, for operators_status
 
+// One word of the current device, which takes OLSGD_ETIMEOUT where a bounded wait of any operator gives up.
+cudaError_t status_word(int** word);
 // Joins the stream; *status: OLSGD_OK, or what a bounded wait left since the last call.
 cudaError_t operators_status(int* status, cudaStream_t s);
 

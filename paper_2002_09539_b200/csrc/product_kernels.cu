@@ -40,8 +40,6 @@ constexpr int kSmallBox = 16;        // rows of a box of B where a tile is not f
 constexpr int kMaxGroups = 1024;     // of a launch of FORWARD or DX: its table's room
 constexpr int kMaxStarts = 2 * kMaxGroups;
 
-__device__ int g_product_status;     // a bounded wait gave up (olsgd_operators_join)
-
 // Rows come in boxes of 16, 32, 64, 128 and 256, one of each at most (a TMA instruction takes some 200 cycles however
 // small its box is).  DW: boxes of 16, 32 and 64 rows by 64 columns; or, of operands whose rows are made of whole panels of 64
 // columns, one of 64 rows by all the panels of the tile (rows behind the group's reach no MMA, or are zeroed).
@@ -60,6 +58,7 @@ struct ProductArgs {
   int out_width;              // bytes (16, 8, 4, 2) that the output's base and rows are multiples of
   const int32_t* offsets;     // [workers][E + 1]
   void* out;
+  int* status;                // status_word()
   // K by parts, where the tiles are few: `splits` units for a tile, whose sums go to parts[split][...] in fp32 (rows of
   // features; DW: [group][column][feature]), part_size values each, for join_kernel
   int splits;
@@ -644,7 +643,7 @@ product_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs g) {
       umma_commit(smem_u32(&ctl->last));
       arrives(&ctl->last, 0);
     }
-    if (threadIdx.x == 0) atomicExch(&g_product_status, (int)OLSGD_ETIMEOUT);
+    if (threadIdx.x == 0) atomicExch(g.status, (int)OLSGD_ETIMEOUT);
   }
   __syncthreads();
   __syncwarp();
@@ -744,6 +743,7 @@ cudaError_t launch_variant(const ProductMaps& maps, ProductArgs g, cudaStream_t 
   static PerDeviceSmem configured;
   auto kern = product_kernel<MODE, HALVES, BN, STAGES>;
   cudaError_t e = ensure_dynamic_smem(configured, kern, smem);
+  if (e == cudaSuccess) e = status_word(&g.status);
   if (e != cudaSuccess) return e;
   g.m_tiles = (g.features + HALVES * kBM - 1) / (HALVES * kBM);
   g.n_tiles = (g.cols + BN - 1) / BN;
@@ -1040,15 +1040,6 @@ cudaError_t launch_product_backward(ProductBackward a, cudaStream_t s) {
   if (a.dw) OLSGD_STEP(launch_weights(a, x_width, dy_width, weights, a.dx != nullptr, weight_parts, s));
   return launch_join(a.dx ? join_rows(rows, row_parts, a.dx, a.m * a.R, a.D) : JoinJob{}, a.dw ? join_weights(weights, weight_parts, a) : JoinJob{},
                      a.f16, s);
-}
-
-cudaError_t product_status(int* status) {
-  OLSGD_STEP(cudaMemcpyFromSymbol(status, g_product_status, sizeof(int)));
-  if (*status != 0) {
-    const int zero = 0;
-    OLSGD_STEP(cudaMemcpyToSymbol(g_product_status, &zero, sizeof(int)));
-  }
-  return cudaSuccess;
 }
 
 }  // namespace olsgd
