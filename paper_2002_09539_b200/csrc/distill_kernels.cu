@@ -4,11 +4,11 @@
 // With m = max x: log p = (x - m) / tau - log sum exp((x - m) / tau); the difference is formed before it is
 // scaled.  Sums and statistics are held in fp32.
 //
-// Bound by the logits' way in and, for a gradient, its way out (4096 x 32768 bf16 with gradient: 118 us, 537 MB, 4.6 TB/s; loss
+// Bound by the logits' way in and, for a gradient, its way out (4096 x 32768 bf16 with gradient: 122 us, 537 MB, 4.4 TB/s; loss
 // of 1021 x 50021 fp32: 39 us, 204 MB, 5.2 TB/s).  Where the rows' weights are known when
 // the loss is formed, both come from one read: a row lies in the registers of a CTA as exp(x - the warp's own max), 32 or 40
 // values a thread, until the whole row's sum is known.  Longer rows take two passes; so do losses alone and gradients that are asked for
-// later, one each, unless the row is short (4096 x 32768 bf16: 57 and 91 us).  Rows of up to 1024 logits belong to a warp.
+// later, one each, unless the row is short (4096 x 32768 bf16: 55 and 91 us).  Rows of up to 1024 logits belong to a warp.
 //
 // A gradient at the pairs' tokens is formed apart from the others, from the logit and the sum of the q of
 // all pairs with that token, and stored behind them, so that it is rounded once.
@@ -745,12 +745,13 @@ Plan plan(int64_t rows, int64_t V, int dtype) {
 // passes are taken.  Up to 16384 elements of 32 a thread, of which a multiprocessor holds several CTAs; above, 40 a thread, one CTA.
 // Longer rows take two passes: by clusters of two to eight CTAs they took 146 to 175 us (2048 x 65536 to 837 x 160001 bf16), by
 // two passes 145 to 148.  So do more pairs than the one warp deals with beside the row: one read and two passes, us, bf16, 96M
-// logits: 64 pairs, V = 4000 131 and 326, 16000 100 and 131, 38000 93 and 114; 128 pairs, V = 1500 711 and 926,
-// 4000 352 and 365, 8000 271 and 212, 38000 164 and 118; 256 pairs 1330 and more against 135 to 1370.
+// logits: 64 pairs, V = 4000 97 and 315, 16000 87 and 128, 38000 88 and 110; 128 pairs, V = 1500 252 and 909, 4000 152 and 354.
+// (Past kManyPairsMax, 128 pairs: 8000 128 and 195, 16000 127 and 142, of a kernel that has become faster since the bound was
+// set by 271 and 212.)  256 pairs took 1330 and more by one read, by two passes 134 (38000) to 1360 (1500).
 // A loss alone takes a CTA that stays where the row is short, which else costs a CTA's start and its barriers each: like
-// this and a CTA a row, us, 96M logits (fp32 48M): 32 pairs, bf16, V = 1500 113 and 370, 4000 64 and 148, 8000 57 and 69,
-// 16000 59 and 50; fp32 4000 48 and 77, 8000 44 and 39; 64 pairs, bf16, 4000 111 and 150, 8000 90 and 70.  So does a
-// gradient that is asked for later: bf16, V = 1500 157 and 406, 4000 91 and 144, 8000 82 and 91, 16000 83 and 76.
+// this and a CTA a row, us, 96M logits (fp32 48M): 32 pairs, bf16, V = 1500 107 and 369, 4000 62 and 147, 8000 56 and 68,
+// 16000 59 and 50; fp32 4000 48 and 76, 8000 44 and 39; 64 pairs, bf16, 4000 77 and 150, 8000 90 and 70.  So does a
+// gradient that is asked for later: bf16, V = 1500 154 and 403, 4000 92 and 153, 8000 81 and 92, 16000 83 and 76.
 // aligned: all rows start on a 16-byte boundary.
 struct Held {
   int warps, values;

@@ -300,7 +300,7 @@ def _gated_sizes(x, w_gate, activation):
 
 def gated_forward(x, w_gate, w_up, activation="silu", save=False):
     """olsgd_gated_forward: h = act(x w_gate^T) * (x w_up^T) for each worker.  x [m][T][D], w_gate and w_up [m][F][D], bfloat16
-    or float16, rows contiguous, any worker and row strides.  Returns h [m][T][F], and with save=True (h, pre), pre being what
+    or float16, rows contiguous, with or without gaps behind rows and workers.  Returns h [m][T][F], and with save=True (h, pre), pre being what
     gated_backward takes."""
     _recorded(x, w_gate, w_up)
     lib = _ops()
@@ -490,8 +490,8 @@ def _product_sizes(x, w, offsets):
 
 def expert_product(x, w, offsets):
     """olsgd_expert_product: y[i][r] = w[i][e] x[i][r] for the rows offsets[i][e] <= r < offsets[i][e + 1] of expert e; rows of no
-    expert become zeros.  x [m][R][D], rows contiguous, any worker and row strides; w [m][E][F][D], any strides but the last; bfloat16
-    or float16; offsets int32 [m][E + 1], rising.  Returns [m][R][F]."""
+    expert become zeros.  x [m][R][D] and w [m][E][F][D], bfloat16 or float16, the last dimension contiguous, with or without gaps behind
+    the others (rows, experts and workers lie one behind another); offsets int32 [m][E + 1], rising.  Returns [m][R][F]."""
     _recorded(x, w)
     lib = _OPS or _ops()
     m, R, E, D, F, code, op, wm, ok = _product_sizes(x, w, offsets)
@@ -539,7 +539,8 @@ def distill_loss(logits, ids, teacher, temperature=1.0, d_loss=None):
     q = softmax(teacher / temperature) over the K pairs and p = softmax(logits / temperature) over all tokens, sum q (log q -
     log p[ids]).  logits [..., V] (rows evenly spaced), ids int32 [..., K] (outside [0, V): no pair), teacher [..., K] of any of the
     three types.  d_loss float32 [...]: the weight of each row's loss, where it is known by now; the logits' gradient then
-    comes from the same read of them.  Returns DistillLoss(loss, stats, d_logits): float32 [...] and [..., 2], and the gradient
+    comes with it, from the same read of them where a row fits a multiprocessor and the pairs are few (some 39000 logits of 16 bits or
+    24000 of 32, and 64 pairs), else from a second one.  Returns DistillLoss(loss, stats, d_logits): float32 [...] and [..., 2], and the gradient
     (contiguous, of the logits' type) or None."""
     _recorded(logits, teacher, d_loss)
     lib = _OPS or _ops()
